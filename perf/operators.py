@@ -393,7 +393,7 @@ def _map_plain(lens, new, table, held, free, count, T, P):
     free[n - m:n] = -1
     held.copy_(torch.where(fails, held, need))
     count.fill_(n - m)
-    t = torch.arange(T, device=table.device)[None]
+    t = torch.arange(T, device=table.device, dtype=torch.int32)[None]
     p = lens[:, None] + t
     slot = table.gather(1, (p // P).clamp_max(blocks - 1).long()) * P + p % P
     return torch.where((t < new[:, None]) & ~fails[:, None], slot, torch.full_like(slot, -1)), fails.to(torch.int32)

@@ -1,4 +1,5 @@
-"""ctypes binding of libswitchsd.so: the C ABI of include/switchsd.h and include/switchsd_harness.h.
+"""ctypes binding of libswitchsd.so: the C ABI of include/switchsd.h, include/switchsd_target.h and
+include/switchsd_harness.h.
 
 Argument marshalling only: every function takes torch CUDA tensors, checks dtype / device / layout,
 and passes raw device pointers and the current CUDA stream to the library.  All computation runs in
@@ -97,6 +98,68 @@ class switchsd_harness_params(ctypes.Structure):
     ]
 
 
+# element types and limits of include/switchsd_target.h
+BF16, F16, F32 = 0, 1, 2
+MAP_ROWS, VMAX, BIAS_MAX = 8192, 262144, 4096
+_DTYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+_c_i64x3 = ctypes.c_int64 * 3
+
+
+class switchsd_kv_map_params(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("page", ctypes.c_int32), ("blocks", ctypes.c_int32),
+        ("pages", ctypes.c_int32), ("lens", ctypes.c_void_p), ("new_lens", ctypes.c_void_p),
+        ("lens_add", ctypes.c_int32), ("new_add", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+        ("held", ctypes.c_void_p), ("free_list", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p), ("status", ctypes.c_void_p), ("stream", ctypes.c_void_p),
+    ]
+
+
+class switchsd_kv4_append_params(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("page", ctypes.c_int32), ("pages", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", _c_i64x3), ("v_stride", _c_i64x3),
+        ("slots", ctypes.c_void_p), ("cache", ctypes.c_void_p), ("stream", ctypes.c_void_p),
+    ]
+
+
+class switchsd_kv4_read_params(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("page", ctypes.c_int32), ("pages", ctypes.c_int32), ("cache", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p), ("out_k", ctypes.c_void_p), ("out_v", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class switchsd_kv4_attention_params(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+        ("D", ctypes.c_int32), ("page", ctypes.c_int32), ("pages", ctypes.c_int32), ("blocks", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("q", ctypes.c_void_p), ("q_stride", _c_i64x3), ("cache", ctypes.c_void_p),
+        ("block_table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("new_lens", ctypes.c_void_p),
+        ("lens_add", ctypes.c_int32), ("new_add", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("out", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("status", ctypes.c_void_p), ("stream", ctypes.c_void_p),
+    ]
+
+
+class switchsd_logits_params(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("cap", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("logits", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+        ("stride_t", ctypes.c_int64), ("ctx_tokens", ctypes.c_void_p), ("ctx_lens", ctypes.c_void_p),
+        ("draft", ctypes.c_void_p), ("draft_stride", ctypes.c_int32), ("new_lens", ctypes.c_void_p),
+        ("new_add", ctypes.c_int32), ("rep", ctypes.c_void_p), ("freq", ctypes.c_void_p),
+        ("pres", ctypes.c_void_p), ("prompt_lens", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p), ("nbias", ctypes.c_int32), ("mask", ctypes.c_void_p),
+        ("mask_words", ctypes.c_int32), ("out", ctypes.c_void_p), ("out_stride_b", ctypes.c_int64),
+        ("out_stride_t", ctypes.c_int64), ("argmax", ctypes.c_void_p), ("status", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
 _lock = threading.Lock()
 _lib = None
 
@@ -153,6 +216,13 @@ _SIGNATURES = {
                                 + [ctypes.POINTER(switchsd_harness_params)]),
     "switchsd_harness_sampled": (ctypes.c_int, [ctypes.c_void_p] * 11
                                  + [ctypes.POINTER(switchsd_harness_params)]),
+    "switchsd_kv_map": (ctypes.c_int, [ctypes.POINTER(switchsd_kv_map_params)]),
+    "switchsd_kv4_bytes": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32]),
+    "switchsd_kv4_append": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_append_params)]),
+    "switchsd_kv4_read": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_read_params)]),
+    "switchsd_kv4_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(switchsd_kv4_attention_params)]),
+    "switchsd_kv4_attention": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_attention_params)]),
+    "switchsd_logits": (ctypes.c_int, [ctypes.POINTER(switchsd_logits_params)]),
 }
 
 
@@ -438,3 +508,167 @@ def switchsd_copy_labels(ctx_tokens, ctx_lens, out_labels, *, n: int = 5, worksp
         _dev(out_labels, torch.uint8, "out_labels", (B, cap)), _dev(workspace, torch.uint8, "workspace"),
         workspace.numel(), _stream_ptr(stream))
     _check(code, "switchsd_copy_labels")
+
+
+# --- the target's side of a verification step (include/switchsd_target.h) -------------------------------------------
+def _strided(t: torch.Tensor, name: str, shape, dtypes) -> int:
+    """Checks a CUDA tensor of `shape` whose last dimension is contiguous; returns its element type's code."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return _DTYPES[t.dtype]
+
+
+def switchsd_kv_map(lens, new_lens, block_table, held, free_list, free_count, slots, *, page: int, T: int | None = None,
+                    lens_add: int = 0, new_add: int = 0, status=None, stream=None) -> None:
+    """switchsd_kv_map of include/switchsd_target.h: block tables and slot maps from the rows' device lengths.
+
+    lens, new_lens, held int32 [B]; block_table int32 [B, blocks]; free_list int32 [pages]; free_count int32 [1];
+    slots int32 [B, T] (or None, with T); status int32 [B] or None.
+    """
+    B, blocks = block_table.shape
+    p = switchsd_kv_map_params()
+    p.B, p.T, p.page, p.blocks = B, slots.shape[1] if slots is not None else int(T or 1), page, blocks
+    p.pages = free_list.shape[0]
+    p.lens, p.new_lens = _dev(lens, torch.int32, "lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,))
+    p.lens_add, p.new_add = lens_add, new_add
+    p.block_table = _dev(block_table, torch.int32, "block_table")
+    p.held = _dev(held, torch.int32, "held", (B,))
+    p.free_list = _dev(free_list, torch.int32, "free_list", (p.pages,))
+    p.free_count = _dev(free_count, torch.int32, "free_count", (1,))
+    p.slots = _dev(slots, torch.int32, "slots", (B, p.T))
+    p.status = _dev(status, torch.int32, "status", (B,))
+    p.stream = _stream_ptr(stream)
+    _check(load().switchsd_kv_map(ctypes.byref(p)), "switchsd_kv_map")
+
+
+def switchsd_kv4_bytes(page: int, D: int) -> int:
+    """Bytes of one (page, head) of the 4-bit cache; 0 for sizes that it does not have."""
+    return int(load().switchsd_kv4_bytes(page, D))
+
+
+def _cache_shape(cache, page: int, D: int):
+    if cache.dim() != 3 or cache.shape[2] != switchsd_kv4_bytes(page, D):
+        raise ValueError(f"the cache has shape {tuple(cache.shape)}, expected [pages, Hkv, {switchsd_kv4_bytes(page, D)}]")
+    return cache.shape[0], cache.shape[1]
+
+
+def switchsd_kv4_append(k, v, slots, cache, *, page: int, stream=None) -> None:
+    """switchsd_kv4_append of include/switchsd_target.h: k, v bf16 or f16 [B, T, Hkv, D] (views whose last dimension is
+    contiguous), slots int32 [B, T], cache uint8 [pages, Hkv, switchsd_kv4_bytes(page, D)]."""
+    B, T, H, D = k.shape
+    p = switchsd_kv4_append_params()
+    p.pages, heads = _cache_shape(cache, page, D)
+    if heads != H:
+        raise ValueError(f"the cache has {heads} heads, k has {H}")
+    p.B, p.T, p.Hkv, p.D, p.page = B, T, H, D, page
+    p.dtype = _strided(k, "k", (B, T, H, D), (torch.bfloat16, torch.float16))
+    _strided(v, "v", (B, T, H, D), (k.dtype,))
+    p.k, p.v = k.data_ptr(), v.data_ptr()
+    p.k_stride, p.v_stride = _c_i64x3(*k.stride()[:3]), _c_i64x3(*v.stride()[:3])
+    p.slots = _dev(slots, torch.int32, "slots", (B, T))
+    p.cache = _dev(cache, torch.uint8, "cache")
+    p.stream = _stream_ptr(stream)
+    _check(load().switchsd_kv4_append(ctypes.byref(p)), "switchsd_kv4_append")
+
+
+def switchsd_kv4_read(cache, slots, out_k, out_v, *, page: int, stream=None) -> None:
+    """switchsd_kv4_read of include/switchsd_target.h: what the cache holds for slots int32 [B, T], into out_k and out_v
+    f16 [B, T, Hkv, D]."""
+    B, T, H, D = out_k.shape
+    p = switchsd_kv4_read_params()
+    p.pages, heads = _cache_shape(cache, page, D)
+    if heads != H:
+        raise ValueError(f"the cache has {heads} heads, out_k has {H}")
+    p.B, p.T, p.Hkv, p.D, p.page = B, T, H, D, page
+    p.cache = _dev(cache, torch.uint8, "cache")
+    p.slots = _dev(slots, torch.int32, "slots", (B, T))
+    p.out_k = _dev(out_k, torch.float16, "out_k", (B, T, H, D))
+    p.out_v = _dev(out_v, torch.float16, "out_v", (B, T, H, D))
+    p.stream = _stream_ptr(stream)
+    _check(load().switchsd_kv4_read(ctypes.byref(p)), "switchsd_kv4_read")
+
+
+def switchsd_kv4_attention_workspace(q, cache, block_table, *, page: int) -> int:
+    """switchsd_kv4_attention_workspace_bytes for these arguments of switchsd_kv4_attention."""
+    p = switchsd_kv4_attention_params()
+    p.B, p.T, p.Hq, p.D = q.shape
+    p.pages, p.Hkv = _cache_shape(cache, page, p.D)
+    p.page, p.blocks = page, block_table.shape[1]
+    p.dtype = _DTYPES[q.dtype]
+    return int(load().switchsd_kv4_attention_workspace_bytes(ctypes.byref(p)))
+
+
+def switchsd_kv4_attention(q, cache, block_table, lens, new_lens, out, *, page: int, scale: float | None = None,
+                           lens_add: int = 0, new_add: int = 0, workspace=None, status=None, stream=None) -> None:
+    """switchsd_kv4_attention of include/switchsd_target.h: q bf16 or f16 [B, T, Hq, D] (a view whose last dimension is
+    contiguous), cache uint8 [pages, Hkv, bytes], block_table int32 [B, blocks], lens, new_lens int32 [B], out
+    [B, T, Hq, D] of q's type.  scale: 1 / sqrt(D) when None.  Allocates the workspace from torch when none is given."""
+    B, T, Hq, D = q.shape
+    p = switchsd_kv4_attention_params()
+    p.pages, p.Hkv = _cache_shape(cache, page, D)
+    p.B, p.T, p.Hq, p.D, p.page, p.blocks = B, T, Hq, D, page, block_table.shape[1]
+    p.dtype = _strided(q, "q", (B, T, Hq, D), (torch.bfloat16, torch.float16))
+    p.q, p.q_stride = q.data_ptr(), _c_i64x3(*q.stride()[:3])
+    p.cache = _dev(cache, torch.uint8, "cache")
+    p.block_table = _dev(block_table, torch.int32, "block_table", (B, p.blocks))
+    p.lens, p.new_lens = _dev(lens, torch.int32, "lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,))
+    p.lens_add, p.new_add = lens_add, new_add
+    p.scale = D ** -0.5 if scale is None else scale
+    p.out = _dev(out, q.dtype, "out", (B, T, Hq, D))
+    p.status = _dev(status, torch.int32, "status", (B,))
+    p.stream = _stream_ptr(stream)
+    need = int(load().switchsd_kv4_attention_workspace_bytes(ctypes.byref(p)))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
+    _check(load().switchsd_kv4_attention(ctypes.byref(p)), "switchsd_kv4_attention")
+
+
+def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_lens=None, new=None, new_add: int = 0,
+                    rep=None, freq=None, pres=None, prompt_lens=None, bias_ids=None, bias=None, mask=None, out=None,
+                    argmax=None, status=None, stream=None) -> None:
+    """switchsd_logits of include/switchsd_target.h: logits bf16, f16 or float32 [B, T, V] (a view whose last dimension
+    is contiguous); ctx_tokens int32 [B, cap], ctx_lens int32 [B]; draft int32 [B, >= T - 1]; new_lens (or new) int32
+    [B]; rep, freq, pres float32 [B]; prompt_lens int32 [B]; bias_ids int32, bias float32 [B, n]; mask int32
+    [B, T, >= V / 32]; out of logits' type and shape (or logits itself), argmax int32 [B, T]: one of the two at least."""
+    B, T, V = logits.shape
+    new_lens = new if new_lens is None else new_lens
+    p = switchsd_logits_params()
+    p.B, p.T, p.V = B, T, V
+    p.dtype = _strided(logits, "logits", (B, T, V), tuple(_DTYPES))
+    p.logits, p.stride_b, p.stride_t = logits.data_ptr(), logits.stride(0), logits.stride(1)
+    if (ctx_tokens is None) != (ctx_lens is None):
+        raise ValueError("ctx_tokens and ctx_lens go together")
+    if ctx_tokens is not None:
+        p.cap = ctx_tokens.shape[1]
+        p.ctx_tokens = _dev(ctx_tokens, torch.int32, "ctx_tokens", (B, p.cap))
+        p.ctx_lens = _dev(ctx_lens, torch.int32, "ctx_lens", (B,))
+    if draft is not None:
+        p.draft_stride = draft.shape[1]
+        p.draft = _dev(draft, torch.int32, "draft", (B, p.draft_stride))
+    p.new_lens, p.new_add = _dev(new_lens, torch.int32, "new_lens", (B,)), new_add
+    p.rep, p.freq = _dev(rep, torch.float32, "rep", (B,)), _dev(freq, torch.float32, "freq", (B,))
+    p.pres = _dev(pres, torch.float32, "pres", (B,))
+    p.prompt_lens = _dev(prompt_lens, torch.int32, "prompt_lens", (B,))
+    if (bias_ids is None) != (bias is None):
+        raise ValueError("bias_ids and bias go together")
+    if bias_ids is not None:
+        p.nbias = bias_ids.shape[1]
+        p.bias_ids = _dev(bias_ids, torch.int32, "bias_ids", (B, p.nbias))
+        p.bias = _dev(bias, torch.float32, "bias", (B, p.nbias))
+    if mask is not None:
+        p.mask_words = mask.shape[2]
+        p.mask = _dev(mask, torch.int32, "mask", (B, T, p.mask_words))
+    if out is not None:
+        _strided(out, "out", (B, T, V), (logits.dtype,))
+        p.out, p.out_stride_b, p.out_stride_t = out.data_ptr(), out.stride(0), out.stride(1)
+    p.argmax = _dev(argmax, torch.int32, "argmax", (B, T))
+    p.status = _dev(status, torch.int32, "status", (B,))
+    p.stream = _stream_ptr(stream)
+    _check(load().switchsd_logits(ctypes.byref(p)), "switchsd_logits")

@@ -1,4 +1,24 @@
 // attention.cu -- switchsd_kv4_attention: attention of a step's new tokens over the 4-bit paged cache.
+//
+// Work.  The query rows of a row and key head -- its new tokens times the query heads that share the key head -- are cut
+// into tiles of 8 or 16; an item is one such tile over its row's keys, and its unit of work is 128 keys.  The units of
+// all items, in order, are dealt out evenly over a fixed grid (the lengths are on the device; every CTA adds them up
+// itself): a CTA takes a contiguous range, which may begin and end inside an item.  An item that one CTA holds whole is
+// written out at once; the others leave partial results (maximum, sum, output) that a second kernel joins in order.
+//
+// Keys and values never leave the registers.  Per 32 keys a warp computes S^T = K Q^T and O^T += V^T W^T with
+// m16n8k16 matrix instructions, the 4-bit codes as the A operand.  The keys' are masked out of the cache's words in
+// place -- a code c in the low bits of an f16 is the (subnormal) number c 2^-24 --, so that a word of eight codes costs
+// five instructions, and their offset of 8 is the accumulators' start (-8 times the query's sum).  The values' become
+// signed numbers, four instructions a word more: taking 8 times the weights' sum off afterwards would leave an error of
+// that sum's size where the values are small.  The scales are applied outside: to the scores, and to the weights.
+//
+// Numbers.  The queries are scaled by a power of two so that they are f16 numbers exactly (a bf16 has fewer bits; what
+// lies 2^22 below the largest may lose bits); codes, and so keys and values, are exact; scores, maxima, sums and the
+// output are binary32, and each 32 keys' matrix sum starts from zero and is added with a rounded multiply-add, because
+// the matrix unit's own accumulation truncates.  The weights exp(s - M) * scale_v are rounded to f16 (11 bits): M is the
+// running maximum of the score plus the exponent of its value's scale, so that the largest weight is near 1 whatever
+// the scales, and weights below 2^-26 of it begin to lose bits.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -7,16 +27,34 @@
 
 namespace switchsd {
 
+constexpr int kAttnWarps = 4;
+constexpr int kAttnThreads = kAttnWarps * kWarp;
+constexpr int kAttnUnit = kAttnWarps * 32;  // keys of a unit: 32 a warp
+constexpr int kAttnMaxCtas = 1024;
+#ifndef ATTN_OCC
+#define ATTN_OCC 3
+#endif
+constexpr int attn_ctas_per_sm(int NT) { return NT == 1 ? ATTN_OCC : 2; }
+constexpr float kWeightUp = 4096.f;         // the weights' scale as f16 numbers: the largest is in [2^11, 2^13]
+constexpr float kSmall = 6.103515625e-5f;   // 2^-14: below it f16 loses bits
+constexpr float kLift = 16777216.f;         // 2^24: of the product of the small weights
+constexpr float kNone = 3.552713678800501e-15f;  // 2^-48, 2^-60 of the largest: too small for either
+constexpr float kFloor = -1e30f;            // the maximum of nothing
+
 struct AttnArgs {
     const uint16_t *q;
     int64_t qs[3];
     const uint8_t *cache;
     const int32_t *table, *lens, *new_lens;
     uint16_t *out;
+    float *part;        // [2 * CTAs][rows][D + 2]: output, maximum, sum
+    int4 *desc;         // [2 * CTAs]: of a partial result: item's row (-1: none), key head, tile of query rows, flags
     int32_t *status;
-    int32_t B, T, Hq, Hkv, pages, blocks, page_shift, lens_add, new_add;
+    int32_t B, T, Hq, Hkv, pages, blocks, page_shift, lens_add, new_add, group;
     float scale;
 };
+
+constexpr int kFirst = 1, kLast = 2;  // flags of a partial result: holds the item's first, last unit
 
 // A row's lengths, or false where they are bad.
 __device__ __forceinline__ bool row_lengths(const AttnArgs &a, int b, int32_t &len, int32_t &nw) {
@@ -27,59 +65,626 @@ __device__ __forceinline__ bool row_lengths(const AttnArgs &a, int b, int32_t &l
     return ok;
 }
 
-// One warp per (row, token, query head), over the keys one by one.
-template <bool F16, int D>
-__global__ void __launch_bounds__(128) attn_simple_kernel(const AttnArgs a) {
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// D = A B + C of m16n8k16, f16 operands, binary32 sums.
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
+                                         float c0, float c1, float c2, float c3) {
+    asm(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};\n"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+// A word's four pairs of codes as pairs of f16 numbers c - 8: the code under the exponent of 1024 is 1024 + c (or, four
+// bits higher, 1024 + 16 c), and one operation on the pair takes the rest off exactly.
+__device__ __forceinline__ uint32_t pair_sub(uint32_t v) {
+    uint32_t r;
+    asm("add.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0xe408e408u));  // - 1032
+    return r;
+}
+__device__ __forceinline__ uint32_t pair_sub16(uint32_t v) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0x2c002c00u), "r"(0xd480d480u));  // / 16 - 72
+    return r;
+}
+__device__ __forceinline__ void signed_codes(uint32_t w, uint32_t (&v)[4]) {
+    const uint32_t y = w >> 8;
+    v[0] = pair_sub((w & 0x000f000fu) | 0x64006400u);
+    v[1] = pair_sub16((w & 0x00f000f0u) | 0x64006400u);
+    v[2] = pair_sub((y & 0x000f000fu) | 0x64006400u);
+    v[3] = pair_sub16((y & 0x00f000f0u) | 0x64006400u);
+}
+
+__device__ __forceinline__ uint4 load16(const uint8_t *p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint2 load8(const uint8_t *p) {
+    uint2 v;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t load4(const uint8_t *p) {
+    uint32_t v;
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+
+template <bool F16>
+__device__ __forceinline__ float widen1(uint16_t v) {
+    return F16 ? __half2float(__ushort_as_half(v)) : bf16_lo(v);
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t narrow2(float a, float b) {
+    if (F16) return pack_f16(a, b);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+
+// Units of one row, and a position among the units.
+struct Place {
+    int b, hk, rt;    // item
+    int32_t unit;     // of the item
+};
+
+// The codes and scales of a thread's share of 32 keys.
+template <int D>
+struct Keys {
+    static constexpr int G = D / 64;
+    uint32_t k[4][2 * G];   // key tile j: words of the thread's token
+    uint32_t sc[4][G];      // scales of the thread's token of tile j: keys' then values', f16
+    uint32_t v[D / 32][4];  // value words: dimensions 32 i + 4 r + 0 .. 3, tokens of block c
+};
+
+template <bool F16, int D, int NT>
+__global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kernel(const AttnArgs a) {
     using L = Kv4<D>;
-    constexpr int N = D / 32;
+    constexpr int G = L::G, R = 8 * NT, MT = D / 16;  // groups, query rows of a tile, output tiles of 16 dimensions
+    extern __shared__ float s_out[];                  // [warps][R][D + 4]
+    __shared__ float s_max[kAttnWarps][R], s_sum[kAttnWarps][R];
+    __shared__ int64_t s_pre[kAttnThreads + 1];
+    __shared__ int s_place[1];
+    __shared__ int64_t s_before[1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int r = lane >> 2, c = lane & 3;
+    const int cta = blockIdx.x, ctas = int(gridDim.x);
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31;
-    const int64_t w = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    if (w >= int64_t(a.B) * a.T * a.Hq) return;
-    const int h = int(w % a.Hq), t = int(w / a.Hq % a.T), b = int(w / a.Hq / a.T);
-    int32_t len, nw;
-    const bool ok = row_lengths(a, b, len, nw);
-    if (a.status && h == 0 && t == 0 && lane == 0) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
-    const int page = 1 << a.page_shift, hk = h / (a.Hq / a.Hkv);
-    const uint16_t *q = a.q + b * a.qs[0] + t * a.qs[1] + h * a.qs[2] + N * lane;
-    float qf[N], o[N], m = -1e30f, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        qf[i] = (F16 ? __half2float(__ushort_as_half(q[i])) : bf16_lo(q[i])) * a.scale;
-        o[i] = 0.f;
+
+    // --- the CTA's range of units -------------------------------------------------------------------------------
+    const int per = (a.B + kAttnThreads - 1) / kAttnThreads;  // rows of a thread
+    auto units_of = [&](int b, int32_t &len, int32_t &nw) -> int64_t {
+        const bool ok = row_lengths(a, b, len, nw);
+        if (a.status && cta == 0) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
+        const int64_t tiles = (int64_t(nw) * a.group + R - 1) / R;
+        return nw ? tiles * a.Hkv * ((int64_t(len) + nw + kAttnUnit - 1) / kAttnUnit) : 0;
+    };
+    int64_t mine = 0;
+    for (int i = 0; i < per; ++i) {
+        const int b = tid * per + i;
+        int32_t len, nw;
+        if (b < a.B) mine += units_of(b, len, nw);
     }
-    const int dw = N * lane / 8, g = dw >> 3;
-    const int word = ((dw & 7) >> 1) * (2 * L::G) + 2 * g + (dw & 1);
-    const int32_t n = t < nw ? len + t + 1 : 0;
-    for (int32_t j = 0; j < n; ++j) {
-        const int32_t pg = __ldcg(a.table + size_t(b) * a.blocks + (j >> a.page_shift));
-        if (uint32_t(pg) >= uint32_t(a.pages)) continue;
-        const int in = j & (page - 1);
-        const uint8_t *src = a.cache + (size_t(pg) * a.Hkv + hk) * size_t(kv4_page_bytes(page, D));
-        const __half *sc = reinterpret_cast<const __half *>(src + L::scales(page) + size_t(in) * L::kScales);
-        const uint32_t kw = *reinterpret_cast<const uint32_t *>(src + size_t(in) * L::kRow + 4 * word);
-        float x = 0.f;
+    {
+        int64_t x = mine;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int e = (N * lane + i) & 7;
-            x += qf[i] * (float((kw >> (4 * ((e >> 1) + 4 * (e & 1)))) & 15u) - 8.f);
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(kFull, x, o);
+            if (lane >= o) x += y;
         }
-        x = warp_sum_f32(x * __half2float(sc[g]));
-        const float mn = fmaxf(m, x), f = __expf(m - mn), p = __expf(x - mn);
-        m = mn;
-        l = l * f + p;
-        const uint32_t *vw = reinterpret_cast<const uint32_t *>(src + L::values(page) + size_t(in >> 3) * L::kBlock) + N * lane;
-        const int shift = 4 * (((in & 7) >> 1) + 4 * (in & 1));
-        const float pv = p * __half2float(sc[L::G + g]);
-#pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = o[i] * f + pv * (float((vw[i] >> shift) & 15u) - 8.f);
+        s_pre[tid + 1] = x;
+        __syncthreads();
+        int64_t add = 0;
+        for (int w = 0; w < warp; ++w) add += s_pre[32 * w + 32];
+        __syncthreads();
+        s_pre[tid + 1] = x + add;
+        if (tid == 0) s_pre[0] = 0;
+        __syncthreads();
     }
-    const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
-    uint16_t *out = a.out + ((size_t(b) * a.T + t) * a.Hq + h) * D + N * lane;
+    const int64_t total = s_pre[kAttnThreads];
+    const int64_t takers = min(total, int64_t(ctas));  // CTAs with a range: at least one unit each
+    int64_t u = cta < takers ? total * cta / takers : total;
+    const int64_t u_end = cta < takers ? total * (cta + 1) / takers : total;
+    // zeros for the query rows of tokens that are not there
+    for (int64_t i0 = int64_t(cta) * kAttnWarps + warp; i0 * kWarp < int64_t(a.B) * a.T; i0 += int64_t(ctas) * kAttnWarps) {
+        const int64_t i = i0 * kWarp + lane;
+        bool none = false;
+        if (i < int64_t(a.B) * a.T) {
+            int32_t len, nw;
+            row_lengths(a, int(i / a.T), len, nw);
+            none = int(i % a.T) >= nw;
+        }
+        uint32_t todo = __ballot_sync(kFull, none);
+        while (todo) {
+            const int l = __ffs(int(todo)) - 1;
+            todo &= todo - 1;
+            uint4 *o = reinterpret_cast<uint4 *>(a.out + size_t(i0 * kWarp + l) * a.Hq * D);
+            for (int e = lane; e < a.Hq * D / 8; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
+        }
+    }
+    if (tid < 2) a.desc[2 * cta + tid] = make_int4(-1, 0, 0, 0);
+    __syncthreads();
+    if (u >= u_end) return;
+    // the row that unit u lies in
+    if (u >= s_pre[tid] && u < s_pre[tid + 1]) {
+        int64_t at = s_pre[tid];
+        int b = tid * per;
+        for (;; ++b) {
+            int32_t len, nw;
+            const int64_t n = units_of(b, len, nw);
+            if (u < at + n) break;
+            at += n;
+        }
+        s_place[0] = b;
+        s_before[0] = at;
+    }
+    __syncthreads();
+    int b = s_place[0];
+    int64_t base_u = s_before[0];
+    const int64_t u_begin = u;
+    const int page_mask = (1 << a.page_shift) - 1;
+    const size_t head_bytes = size_t(kv4_page_bytes(1 << a.page_shift, D));
+    const int val_off = L::values(1 << a.page_shift), sc_off = L::scales(1 << a.page_shift);
+
+    while (u < u_end) {
+        // --- the item -------------------------------------------------------------------------------------------
+        int32_t len, nw;
+        row_lengths(a, b, len, nw);
+        const int32_t total_keys = len + nw;
+        const int32_t units = (total_keys + kAttnUnit - 1) / kAttnUnit;
+        const int tiles = nw ? (nw * a.group + R - 1) / R : 0;
+        if (u >= base_u + int64_t(units) * tiles * a.Hkv) {  // the next row
+            base_u += int64_t(units) * tiles * a.Hkv;
+            ++b;
+            continue;
+        }
+        const int64_t item = (u - base_u) / units;
+        const int32_t first = int32_t((u - base_u) - item * units);
+        const int hk = int(item / tiles), rt = int(item % tiles);
+        const int32_t n = int32_t(min(int64_t(units - first), u_end - u));
+        const int rows = min(R, nw * a.group - rt * R);
+
+        // --- queries: B operand, row n = lane / 4 of each of NT tiles of 8 --------------------------------------
+        uint32_t qb[NT][G][2][4];   // [tile][group][word][step x register]
+        float start[NT][G][2];      // -8 sum of the query's group, of columns 2 c, 2 c + 1
+        float limit_f = 0.f;
+        int32_t limit[NT][2];       // last key that the column's query sees
+        {
+            uint4 raw[NT][G][2];
+            float big = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        out[i] = F16 ? __half_as_ushort(__float2half_rn(o[i] * inv)) : __bfloat16_as_ushort(__float2bfloat16_rn(o[i] * inv));
+            for (int nt = 0; nt < NT; ++nt) {
+                const int row = 8 * nt + r, rr = rt * R + row, t = rr / a.group, h = hk * a.group + rr - t * a.group;
+                const uint16_t *q = a.q + b * a.qs[0] + t * a.qs[1] + h * a.qs[2] + 16 * c;
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        raw[nt][g][i] = row < rows ? *reinterpret_cast<const uint4 *>(q + 64 * g + 8 * i) : make_uint4(0, 0, 0, 0);
+                        const uint32_t w[4] = {raw[nt][g][i].x, raw[nt][g][i].y, raw[nt][g][i].z, raw[nt][g][i].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            big = fmaxf(big, fmaxf(fabsf(widen1<F16>(uint16_t(w[e]))), fabsf(widen1<F16>(uint16_t(w[e] >> 16)))));
+                    }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int row_c = 8 * nt + 2 * c + e;
+                    limit[nt][e] = row_c < rows ? len + (rt * R + row_c) / a.group : -1;
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(kFull, big, o));
+            // the power of two that brings the largest into [2^11, 2^12)
+            int ex = 11 - (int(__float_as_uint(big) >> 23) - 127);
+            ex = big > 0.f && big < INFINITY ? max(-100, min(100, ex)) : 0;
+            const float up = __int_as_float((127 + ex) << 23);
+            limit_f = __int_as_float((127 - ex) << 23) * a.scale * 1.4426950408889634f * 16777216.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t w[4] = {raw[nt][g][i].x, raw[nt][g][i].y, raw[nt][g][i].z, raw[nt][g][i].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {  // pair e; the odd pairs' codes stand four bits higher
+                            const float x0 = widen1<F16>(uint16_t(w[e])) * up, x1 = widen1<F16>(uint16_t(w[e] >> 16)) * up;
+                            sum += x0 + x1;
+                            const float f = e & 1 ? 0.0625f : 1.f;
+                            qb[nt][g][i][e] = pack_f16(x0 * f, x1 * f);
+                        }
+                    }
+                    sum += __shfl_xor_sync(kFull, sum, 1);
+                    sum += __shfl_xor_sync(kFull, sum, 2);
+                    start[nt][g][0] = __shfl_sync(kFull, sum, 8 * c) * (-8.f / 16777216.f);
+                    start[nt][g][1] = __shfl_sync(kFull, sum, 8 * c + 4) * (-8.f / 16777216.f);
+                }
+        }
+        const float score = limit_f;  // binary logarithm's scale of a sum of products
+
+        float o[NT][MT][4], m[NT][2], l[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
+            m[nt][0] = m[nt][1] = kFloor;
+            l[nt][0] = l[nt][1] = 0.f;
+        }
+
+        // --- the keys, 32 at a time -----------------------------------------------------------------------------
+        const int32_t *table = a.table + size_t(b) * a.blocks;
+        const uint8_t *cache = a.cache + size_t(hk) * head_bytes;
+        const size_t page_bytes = head_bytes * a.Hkv;
+        Keys<D> x;
+        // groups of eight keys that this thread reads: its keys' token lies in group r / 2, its values' in group c
+        auto page_at = [&](int32_t key) -> int32_t {
+            return key < total_keys ? __ldcg(table + (key >> a.page_shift)) : -1;
+        };
+        auto load_keys = [&](int32_t key0, int32_t page) {  // key0: of the 32; page: of group r / 2
+            const int32_t at = key0 + 8 * (r >> 1);
+            if (uint32_t(page) < uint32_t(a.pages)) {
+                const int in = (at & page_mask) + (r & 1);
+                const uint8_t *p = cache + size_t(page) * page_bytes;
+                const uint8_t *pk = p + in * L::kRow + c * (8 * G), *ps = p + sc_off + in * L::kScales;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (G == 2) {
+                        const uint4 w = load16(pk + 2 * j * L::kRow);
+                        x.k[j][0] = w.x;
+                        x.k[j][1] = w.y;
+                        x.k[j][2 * G - 2] = w.z;
+                        x.k[j][2 * G - 1] = w.w;
+                        const uint2 s = load8(ps + 2 * j * L::kScales);
+                        x.sc[j][0] = s.x;
+                        x.sc[j][G - 1] = s.y;
+                    } else {
+                        const uint2 w = load8(pk + 2 * j * L::kRow);
+                        x.k[j][0] = w.x;
+                        x.k[j][1] = w.y;
+                        x.sc[j][0] = load4(ps + 2 * j * L::kScales);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                    for (int i = 0; i < 2 * G; ++i) x.k[j][i] = 0;
+#pragma unroll
+                    for (int i = 0; i < G; ++i) x.sc[j][i] = 0;
+                }
+            }
+        };
+        auto load_values = [&](int32_t key0, int32_t page) {  // page: of group c
+            const int32_t at = key0 + 8 * c;
+            if (uint32_t(page) < uint32_t(a.pages)) {
+                const uint8_t *p = cache + size_t(page) * page_bytes + val_off + ((at & page_mask) >> 3) * L::kBlock + 16 * r;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const uint4 w = load16(p + 128 * i);
+                    x.v[i][0] = w.x;
+                    x.v[i][1] = w.y;
+                    x.v[i][2] = w.z;
+                    x.v[i][3] = w.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x.v[i][e] = 0;
+            }
+        };
+        int32_t key0 = first * kAttnUnit + 32 * warp;
+        const int32_t key_end = min(total_keys, (first + n) * kAttnUnit);
+        int32_t pk = page_at(key0 + 8 * (r >> 1)), pv = page_at(key0 + 8 * c);
+        load_keys(key0, pk);
+        load_values(key0, pv);
+        int32_t pk1 = page_at(key0 + kAttnUnit + 8 * (r >> 1)), pv1 = page_at(key0 + kAttnUnit + 8 * c);
+        for (; key0 < key_end; key0 += kAttnUnit) {
+            const bool more = key0 + kAttnUnit < key_end;
+            const bool out_of_pool = uint32_t(pk) >= uint32_t(a.pages);
+            // S^T: tile j (rows r of two matrix tiles) holds keys key0 + 8 (r / 2) + 2 j + r % 2
+            float s[NT][4][2];
+            float ks[4][G], vs[4][G], lg[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    // scales of the token: G of the key, G of the value
+                    const uint16_t hk16 = G == 2 ? uint16_t(g ? x.sc[j][0] >> 16 : x.sc[j][0]) : uint16_t(x.sc[j][0]);
+                    const uint16_t hv16 = G == 2 ? uint16_t(g ? x.sc[j][G - 1] >> 16 : x.sc[j][G - 1]) : uint16_t(x.sc[j][0] >> 16);
+                    ks[j][g] = __half2float(__ushort_as_half(hk16)) * score;
+                    vs[j][g] = __half2float(__ushort_as_half(hv16));
+                }
+                const float big = G == 2 ? fmaxf(vs[j][0], vs[j][G - 1]) : vs[j][0];
+                lg[j] = fmaxf(float(int(__float_as_uint(big) >> 23) - 127), -24.f);
+            }
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        float acc[4];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t w0 = x.k[2 * mt][2 * g + i], w1 = x.k[2 * mt + 1][2 * g + i];
+                            if (i == 0)
+                                mma16816(acc, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb[nt][g][i][0], qb[nt][g][i][1],
+                                         start[nt][g][0], start[nt][g][1], start[nt][g][0], start[nt][g][1]);
+                            else
+                                mma16816(acc, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb[nt][g][i][0], qb[nt][g][i][1],
+                                         acc[0], acc[1], acc[2], acc[3]);
+                            const uint32_t x0 = w0 >> 8, x1 = w1 >> 8;
+                            mma16816(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u, qb[nt][g][i][2], qb[nt][g][i][3],
+                                     acc[0], acc[1], acc[2], acc[3]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (g == 0) {
+                                s[nt][2 * mt][e] = acc[e] * ks[2 * mt][0];
+                                s[nt][2 * mt + 1][e] = acc[2 + e] * ks[2 * mt + 1][0];
+                            } else {
+                                s[nt][2 * mt][e] = fmaf(acc[e], ks[2 * mt][g], s[nt][2 * mt][e]);
+                                s[nt][2 * mt + 1][e] = fmaf(acc[2 + e], ks[2 * mt + 1][g], s[nt][2 * mt + 1][e]);
+                            }
+                        }
+                    }
+                }
+            if (more) load_keys(key0 + kAttnUnit, pk1);
+            // keys that some query of the tile does not see: past its token, past the row's end, or without a page
+            const bool masked = __any_sync(kFull, out_of_pool) || key0 + 32 > len + 1;
+            if (masked) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int32_t key = key0 + 8 * (r >> 1) + 2 * j + (r & 1);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (out_of_pool || key > limit[nt][e]) s[nt][j][e] = -INFINITY;
+                }
+            }
+            // Weights: the softmax's times the values' scales.  f16 keeps 11 bits down to 2^-26 of the largest; smaller
+            // ones (kSmall) go into a product of their own, 2^24 higher.
+            uint32_t wb[NT][G][4], wl[NT][G][4];  // transposed: B operand of tile j
+            float corr[NT][2];
+            bool small = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = fmaxf(fmaxf(s[nt][0][e] + lg[0], s[nt][1][e] + lg[1]), fmaxf(s[nt][2][e] + lg[2], s[nt][3][e] + lg[3]));
+#pragma unroll
+                    for (int sh = 4; sh < 32; sh <<= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, sh));
+                    mx = fmaxf(mx, m[nt][e]);
+                    corr[nt][e] = exp2_approx(m[nt][e] - mx);
+                    m[nt][e] = mx;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[nt][j][e] = exp2_approx(s[nt][j][e] - mx);
+                        sum += s[nt][j][e];
+                    }
+                    l[nt][e] = fmaf(l[nt][e], corr[nt][e], sum);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const float f = vs[j][g] * kWeightUp;
+                        float w0 = s[nt][j][0] * f, w1 = s[nt][j][1] * f;
+                        if (masked) {  // a scale that a masked key left may be anything
+                            w0 = s[nt][j][0] > 0.f ? w0 : 0.f;
+                            w1 = s[nt][j][1] > 0.f ? w1 : 0.f;
+                        }
+                        small |= (w0 < kSmall && w0 > kNone) || (w1 < kSmall && w1 > kNone);
+                        wb[nt][g][j] = transpose8x8(pack_f16(w0 < kSmall ? 0.f : w0, w1 < kSmall ? 0.f : w1));
+                    }
+            }
+            const bool both = __any_sync(kFull, small);
+            if (both) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int g = 0; g < G; ++g) {
+                            const float f = vs[j][g] * kWeightUp;
+                            const float w0 = s[nt][j][0] * f, w1 = s[nt][j][1] * f;
+                            wl[nt][g][j] = transpose8x8(pack_f16(w0 < kSmall ? w0 * kLift : 0.f, w1 < kSmall ? w1 * kLift : 0.f));
+                        }
+            }
+            // O^T: the values' codes as signed f16 numbers
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t va[4], vb[4];
+                    signed_codes(x.v[i][2 * h], va);
+                    signed_codes(x.v[i][2 * h + 1], vb);
+                    constexpr int per_group = 2;  // i of a group
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint32_t(&w)[4] = wb[nt][i / per_group];
+                        float acc[4];
+                        if (both) {
+                            const uint32_t(&wo)[4] = wl[nt][i / per_group];
+                            mma16816(acc, va[0], vb[0], va[1], vb[1], wo[0], wo[1], 0.f, 0.f, 0.f, 0.f);
+                            mma16816(acc, va[2], vb[2], va[3], vb[3], wo[2], wo[3], acc[0], acc[1], acc[2], acc[3]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[e] *= 1.f / kLift;
+                        } else {
+                            acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+                        }
+                        mma16816(acc, va[0], vb[0], va[1], vb[1], w[0], w[1], acc[0], acc[1], acc[2], acc[3]);
+                        mma16816(acc, va[2], vb[2], va[3], vb[3], w[2], w[3], acc[0], acc[1], acc[2], acc[3]);
+                        float(&oo)[4] = o[nt][2 * i + h];
+                        oo[0] = fmaf(oo[0], corr[nt][0], acc[0]);
+                        oo[1] = fmaf(oo[1], corr[nt][1], acc[1]);
+                        oo[2] = fmaf(oo[2], corr[nt][0], acc[2]);
+                        oo[3] = fmaf(oo[3], corr[nt][1], acc[3]);
+                    }
+                }
+            if (more) load_values(key0 + kAttnUnit, pv1);
+            pk = pk1;
+            pv = pv1;
+            pk1 = page_at(key0 + 2 * kAttnUnit + 8 * (r >> 1));
+            pv1 = page_at(key0 + 2 * kAttnUnit + 8 * c);
+        }
+
+        // --- the four warps' results joined ---------------------------------------------------------------------
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int sh = 4; sh < 32; sh <<= 1) l[nt][e] += __shfl_xor_sync(kFull, l[nt][e], sh);
+                const int row = 8 * nt + 2 * c + e;
+                if (r == 0) {
+                    s_max[warp][row] = m[nt][e];
+                    s_sum[warp][row] = l[nt][e];
+                }
+                float *dst = s_out + (size_t(warp) * R + row) * (D + 4);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i)
+                    *reinterpret_cast<float4 *>(dst + 32 * i + 4 * r) =
+                        make_float4(o[nt][2 * i][e], o[nt][2 * i][2 + e], o[nt][2 * i + 1][e], o[nt][2 * i + 1][2 + e]);
+            }
+        __syncthreads();
+        const bool whole = first == 0 && n == units;
+        const int slot = 2 * cta + (u == u_begin ? 0 : 1);
+        for (int i = tid; i < R * (D / 4); i += kAttnThreads) {
+            const int row = i / (D / 4), d = 4 * (i % (D / 4));
+            float mx = kFloor;
+#pragma unroll
+            for (int w = 0; w < kAttnWarps; ++w) mx = fmaxf(mx, s_max[w][row]);
+            float sum = 0.f;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kAttnWarps; ++w) {
+                const float f = exp2_approx(s_max[w][row] - mx);
+                const float4 z = *reinterpret_cast<const float4 *>(s_out + (size_t(w) * R + row) * (D + 4) + d);
+                sum = fmaf(s_sum[w][row], f, sum);
+                y.x = fmaf(z.x, f, y.x);
+                y.y = fmaf(z.y, f, y.y);
+                y.z = fmaf(z.z, f, y.z);
+                y.w = fmaf(z.w, f, y.w);
+            }
+            if (whole) {
+                if (row < rows) {
+                    const int rr = rt * R + row, t = rr / a.group, h = hk * a.group + rr - t * a.group;
+                    const float inv = sum == 0.f ? 0.f : (1.f / kWeightUp) / sum;
+                    uint2 w = make_uint2(narrow2<F16>(y.x * inv, y.y * inv), narrow2<F16>(y.z * inv, y.w * inv));
+                    *reinterpret_cast<uint2 *>(a.out + ((size_t(b) * a.T + t) * a.Hq + h) * D + d) = w;
+                }
+            } else {
+                float *dst = a.part + (size_t(slot) * R + row) * (D + 4);
+                *reinterpret_cast<float4 *>(dst + d) = y;
+                if (d == 0) {
+                    dst[D] = mx;
+                    dst[D + 1] = sum;
+                }
+            }
+        }
+        if (!whole && tid == 0)
+            a.desc[slot] = make_int4(b, hk, rt, (first == 0 ? kFirst : 0) | (first + n == units ? kLast : 0));
+        __syncthreads();
+        u += n;
+    }
+}
+
+// Joins the partial results of the items that several CTAs hold: CTA (i, row) looks after the item whose first part is
+// the i-th CTA's, adding the parts in order.
+template <bool F16, int D, int NT>
+__global__ void __launch_bounds__(D) attn_join_kernel(const AttnArgs a) {
+    constexpr int R = 8 * NT;
+    const int i = blockIdx.x, row = blockIdx.y, d = threadIdx.x, ctas = int(gridDim.x);
+    pdl_wait();
+    pdl_trigger();
+    int slot = 2 * i + 1;
+    int4 de = __ldcg(a.desc + slot);
+    if (de.x < 0 || !(de.w & kFirst)) {
+        slot = 2 * i;
+        de = __ldcg(a.desc + slot);
+        if (de.x < 0 || !(de.w & kFirst)) return;
+    }
+    int32_t len, nw;
+    row_lengths(a, de.x, len, nw);
+    const int rr = de.z * R + row, t = rr / a.group;
+    if (t >= nw) return;
+    float mx = kFloor, sum = 0.f, y = 0.f;
+    int next = i;
+    for (int flags = de.w;;) {
+        const float *src = a.part + (size_t(slot) * R + row) * (D + 4);
+        const float pm = __ldcg(src + D), ps = __ldcg(src + D + 1), py = __ldcg(src + d);
+        const float mn = fmaxf(mx, pm), f0 = exp2_approx(mx - mn), f1 = exp2_approx(pm - mn);
+        y = y * f0 + py * f1;
+        sum = sum * f0 + ps * f1;
+        mx = mn;
+        if ((flags & kLast) || ++next >= ctas) break;
+        slot = 2 * next;
+        flags = __ldcg(&a.desc[slot].w);
+    }
+    const int h = de.y * a.group + rr - t * a.group;
+    const float inv = sum == 0.f ? 0.f : (1.f / kWeightUp) / sum;
+    const uint32_t w = narrow2<F16>(y * inv, 0.f);
+    a.out[((size_t(de.x) * a.T + t) * a.Hq + h) * D + d] = uint16_t(w);
+}
+
+static int attn_sms() {
+    static int count[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (count[dev] == 0 && cudaDeviceGetAttribute(&count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return count[dev];
+}
+
+static size_t attn_workspace(int D, int NT) {
+    return size_t(2 * kAttnMaxCtas) * (sizeof(int4) + size_t(8 * NT) * (D + 4) * sizeof(float));
+}
+
+template <bool F16, int D, int NT>
+static cudaError_t launch_attn(AttnArgs a, int sms, cudaStream_t s) {
+    static bool attr_done[64] = {false};
+    const size_t smem = size_t(kAttnWarps) * 8 * NT * (D + 4) * sizeof(float);
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+        e = cudaFuncSetAttribute(attn_kernel<F16, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_done[dev] = true;
+    }
+    const unsigned ctas = unsigned(std::min(kAttnMaxCtas, sms * attn_ctas_per_sm(NT)));
+    e = launch_pdl(attn_kernel<F16, D, NT>, dim3(ctas), dim3(kAttnThreads), smem, s, 0u, a);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(attn_join_kernel<F16, D, NT>, dim3(ctas, 8 * NT), dim3(D), 0, s, 0u, a);
+}
+
+template <bool F16, int D>
+static cudaError_t launch_attn_rows(const AttnArgs &a, int sms, cudaStream_t s) {
+    return a.T * a.group <= 8 ? launch_attn<F16, D, 1>(a, sms, s) : launch_attn<F16, D, 2>(a, sms, s);
 }
 
 }  // namespace switchsd
@@ -87,7 +692,7 @@ __global__ void __launch_bounds__(128) attn_simple_kernel(const AttnArgs a) {
 using namespace switchsd;
 
 extern "C" size_t switchsd_kv4_attention_workspace_bytes(const switchsd_kv4_attention_params *p) {
-    return p ? 16 : 0;
+    return p && kv4_dim_ok(p->D) ? attn_workspace(p->D, 2) : 0;
 }
 
 extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
@@ -99,7 +704,8 @@ extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
     if (p->B < 1 || p->T < 1 || p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv != 0 || p->Hq / p->Hkv > 64 || p->blocks < 1 || p->pages < 1 ||
         !kv4_page_ok(p->page) || !kv4_dim_ok(p->D))
         return SWITCHSD_ERR_SHAPE;
-    if (int64_t(p->pages) * p->page > 0x7fffffff || int64_t(p->blocks) * p->page > 0x7fffffff || int64_t(p->B) * p->T > 0x7fffffff)
+    if (int64_t(p->pages) * p->page > 0x7fffffff || int64_t(p->blocks) * p->page > 0x7fffffff - 1024 || int64_t(p->B) * p->T > 0x7fffffff ||
+        int64_t(p->T) * (p->Hq / p->Hkv) > 0x7fffffff)
         return SWITCHSD_ERR_SHAPE;
     if (p->workspace_bytes < switchsd_kv4_attention_workspace_bytes(p)) return SWITCHSD_ERR_ARG;
     AttnArgs a;
@@ -111,6 +717,8 @@ extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
     a.new_lens = p->new_lens;
     a.out = static_cast<uint16_t *>(p->out);
     a.status = p->status;
+    a.desc = static_cast<int4 *>(p->workspace);
+    a.part = reinterpret_cast<float *>(a.desc + 2 * kAttnMaxCtas);
     a.B = p->B;
     a.T = p->T;
     a.Hq = p->Hq;
@@ -120,15 +728,15 @@ extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
     a.page_shift = log2_of(p->page);
     a.lens_add = p->lens_add;
     a.new_add = p->new_add;
+    a.group = p->Hq / p->Hkv;
     a.scale = p->scale;
-    const int64_t ctas = (int64_t(p->B) * p->T * p->Hq + 3) / 4;
-    if (ctas > 0x7fffffff) return SWITCHSD_ERR_SHAPE;
+    const int sms = attn_sms();
+    if (sms == 0) return SWITCHSD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);
-    const dim3 grid{unsigned(ctas)}, block{128u};
     cudaError_t e;
     if (p->dtype == SWITCHSD_F16)
-        e = p->D == 128 ? launch_pdl(attn_simple_kernel<true, 128>, grid, block, 0, s, 0u, a) : launch_pdl(attn_simple_kernel<true, 64>, grid, block, 0, s, 0u, a);
+        e = p->D == 128 ? launch_attn_rows<true, 128>(a, sms, s) : launch_attn_rows<true, 64>(a, sms, s);
     else
-        e = p->D == 128 ? launch_pdl(attn_simple_kernel<false, 128>, grid, block, 0, s, 0u, a) : launch_pdl(attn_simple_kernel<false, 64>, grid, block, 0, s, 0u, a);
+        e = p->D == 128 ? launch_attn_rows<false, 128>(a, sms, s) : launch_attn_rows<false, 64>(a, sms, s);
     return e == cudaSuccess ? SWITCHSD_OK : SWITCHSD_ERR_CUDA;
 }

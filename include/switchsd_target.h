@@ -178,7 +178,7 @@ int switchsd_kv4_attention(const switchsd_kv4_attention_params *params);
  *
  *   logits        dtype (SWITCHSD_BF16, SWITCHSD_F16, SWITCHSD_F32) [B, T, V], strides in elements between rows and
  *                 positions (V values are contiguous), aligned to its elements
- *   ctx_tokens    int32 [B, cap] (16-byte aligned, cap a multiple of 4), ctx_lens int32 [B]; NULL (both): no context
+ *   ctx_tokens    int32 [B, cap] (16-byte aligned, cap a multiple of 4 below 2^28), ctx_lens int32 [B]; NULL (both): no context
  *   draft         int32 [B, draft_stride]: entries 0 .. new - 2 are read; NULL for T = 1 or to leave the draft out
  *   new_lens      int32 [B] or NULL: positions of each row, T when NULL.  new_add is added.
  *   rep, freq, pres  float [B] or NULL (1, 0, 0); rep > 0
@@ -188,6 +188,9 @@ int switchsd_kv4_attention(const switchsd_kv4_attention_params *params);
  *   out           dtype [B, T, V] with its own strides, or NULL; may be `logits` itself (with its strides); positions
  *                 t >= new are not written
  *   argmax        int32 [B, T] or NULL (not both); -1 for t >= new
+ *   workspace     at least switchsd_logits_workspace_bytes(params) bytes, 16-byte aligned, caller-owned: the tokens that
+ *                 penalties and biases name, and the positions' best so far.  Calls that share one must not overlap on
+ *                 the GPU.  (The size goes by B, T, V, cap, nbias and which of the inputs are given.)
  *   status        int32 [B] or NULL: SWITCHSD_ROW_BAD_LEN for a context length outside [0, cap] or new outside [0, T]
  *                 (the row is left out: argmax -1)
  * Tokens of the context and the draft outside [0, V) count for nothing.
@@ -212,9 +215,12 @@ typedef struct {
     int64_t out_stride_b, out_stride_t;
     int32_t *argmax;
     int32_t *status;
+    void *workspace;
+    size_t workspace_bytes;
     void *stream;
 } switchsd_logits_params;
 
+size_t switchsd_logits_workspace_bytes(const switchsd_logits_params *params);
 int switchsd_logits(const switchsd_logits_params *params);
 
 #ifdef __cplusplus

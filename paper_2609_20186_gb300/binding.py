@@ -156,7 +156,7 @@ class switchsd_logits_params(ctypes.Structure):
         ("bias", ctypes.c_void_p), ("nbias", ctypes.c_int32), ("mask", ctypes.c_void_p),
         ("mask_words", ctypes.c_int32), ("out", ctypes.c_void_p), ("out_stride_b", ctypes.c_int64),
         ("out_stride_t", ctypes.c_int64), ("argmax", ctypes.c_void_p), ("status", ctypes.c_void_p),
-        ("stream", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p),
     ]
 
 
@@ -222,6 +222,7 @@ _SIGNATURES = {
     "switchsd_kv4_read": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_read_params)]),
     "switchsd_kv4_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(switchsd_kv4_attention_params)]),
     "switchsd_kv4_attention": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_attention_params)]),
+    "switchsd_logits_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(switchsd_logits_params)]),
     "switchsd_logits": (ctypes.c_int, [ctypes.POINTER(switchsd_logits_params)]),
 }
 
@@ -233,6 +234,8 @@ def library_path() -> str:
 def load(path: str | None = None):
     """Loads (once) and returns the ctypes handle.  Raises if the library was not built."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
@@ -267,6 +270,8 @@ def _check(code: int, what: str):
 def _dev(t: torch.Tensor | None, dtype, name: str, shape=None):
     if t is None:
         return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()  # the usual case, without a message to choose
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
@@ -278,9 +283,16 @@ def _dev(t: torch.Tensor | None, dtype, name: str, shape=None):
     return t.data_ptr()
 
 
+# the current stream's handle without a Stream object around it, where this torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_ptr(stream) -> int:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _bf16(t: torch.Tensor, name: str, shape=None):
@@ -632,11 +644,12 @@ def switchsd_kv4_attention(q, cache, block_table, lens, new_lens, out, *, page: 
 
 def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_lens=None, new=None, new_add: int = 0,
                     rep=None, freq=None, pres=None, prompt_lens=None, bias_ids=None, bias=None, mask=None, out=None,
-                    argmax=None, status=None, stream=None) -> None:
+                    argmax=None, status=None, workspace=None, stream=None) -> None:
     """switchsd_logits of include/switchsd_target.h: logits bf16, f16 or float32 [B, T, V] (a view whose last dimension
     is contiguous); ctx_tokens int32 [B, cap], ctx_lens int32 [B]; draft int32 [B, >= T - 1]; new_lens (or new) int32
     [B]; rep, freq, pres float32 [B]; prompt_lens int32 [B]; bias_ids int32, bias float32 [B, n]; mask int32
-    [B, T, >= V / 32]; out of logits' type and shape (or logits itself), argmax int32 [B, T]: one of the two at least."""
+    [B, T, >= V / 32]; out of logits' type and shape (or logits itself), argmax int32 [B, T]: one of the two at least.
+    Allocates the workspace from torch when none is given."""
     B, T, V = logits.shape
     new_lens = new if new_lens is None else new_lens
     p = switchsd_logits_params()
@@ -671,4 +684,7 @@ def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_l
     p.argmax = _dev(argmax, torch.int32, "argmax", (B, T))
     p.status = _dev(status, torch.int32, "status", (B,))
     p.stream = _stream_ptr(stream)
+    if workspace is None:
+        workspace = torch.empty(int(load().switchsd_logits_workspace_bytes(ctypes.byref(p))), dtype=torch.uint8, device=logits.device)
+    p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
     _check(load().switchsd_logits(ctypes.byref(p)), "switchsd_logits")

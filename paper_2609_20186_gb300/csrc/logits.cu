@@ -1,27 +1,40 @@
 // logits.cu -- switchsd_logits: penalties for repeated tokens, biases and grammar masks on the logits of B rows and T
 // positions, and every position's greedy token.
 //
-// A cluster of kLogitParts CTAs takes one row and a range of its positions, each CTA a slice of the vocabulary.  It
-// counts the row's context for its slice in shared memory (one word a token: output occurrences, and flags), marks the
-// tokens that need more than a comparison in a bit map -- seen, biased or in the draft --, and then streams the slice
-// of every position once.  The CTAs' best tokens meet in the first one's shared memory.
+// Two kernels.  The first counts: CTA (part, row) reads the row's context and counts its part of the vocabulary in shared
+// memory (one word a token: output occurrences, and flags).  A token that is seen, biased or in the draft is special: a
+// bit in the part's map, and an entry of its list, go to the workspace.  Chunks of 256 tokens go round the parts, because a
+// tokenizer's low ids are the frequent ones.  The second streams: CTA (part, positions, row) reads its part of a few
+// positions once, where everything but the specials meets the mask and a maximum; then goes through the part's list, 32
+// lanes on 32 specials however they lie, each over those positions (the cache still has what is read again).  The parts'
+// best tokens meet in a word of the workspace a position, and the last CTA of a group of positions writes the tokens.
+//
+// Each value is worked out in binary32, one rounding an operation, in the header's order, and the best is a maximum of
+// (value, token), so nothing depends on the split or on who comes first.
+//
+// What bounds it: the second kernel reads the logits once (and writes them once), 2 or 4 bytes an element; the first
+// reads the context once a part.  One kernel that counted and then streamed all positions of a row and part took 126 us
+// where the two take 104 us (64 rows of 8K to 32K tokens, 1 to 17 positions, 128,256 tokens, masks and biases): it counted
+// while nothing streamed, and the rows' uneven positions left SMs idle at its end.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
 
-#include "common.cuh"
-#include "switchsd_target.h"
+#include "kv4.cuh"
 
 namespace switchsd {
 
-constexpr int kLogitParts = 8;
-constexpr int kLogitThreads = 512;
+constexpr int kCountThreads = 512;
+constexpr int kLogitThreads = 256;
 constexpr int kLogitWarps = kLogitThreads / kWarp;
-constexpr int kLogitRange = 64;             // most positions of a cluster
+constexpr int kLogitGroup = 4;              // positions of a CTA
+constexpr int kLogitUnits = 4;              // units (32 vectors of 16 bytes) of a warp in flight
+constexpr int kChunk = 256;                 // tokens that lie together in a part
 constexpr uint32_t kSeen = 1u << 31;        // in a token's word: occurs in the context
 constexpr uint32_t kInDraft = 1u << 30;     // occurs in the draft
-constexpr uint32_t kCount = kInDraft - 1;   // output occurrences in the context
+constexpr uint32_t kBiased = 1u << 29;      // is named by the biases
+constexpr uint32_t kCount = kBiased - 1;    // output occurrences in the context and in the draft so far
 
 struct LogitArgs {
     const uint8_t *logits;
@@ -32,10 +45,45 @@ struct LogitArgs {
     const uint32_t *mask;
     int32_t *argmax, *status;
     int32_t T, V, cap, draft_stride, new_add, nbias, mask_words;
-    int32_t slice;           // tokens of a CTA, a multiple of 64
-    int32_t range;           // positions of a cluster
+    int32_t slice;           // places for tokens of a part, a multiple of kChunk
+    int32_t parts_log;       // log2 of the parts
+    int32_t groups;          // of positions
+    int32_t entries;         // places of a part's list
+    uint32_t hash_mask;      // places of the bias table less one
+    int32_t marks;           // whether there are specials at all: penalties or biases
+    // workspace
+    unsigned long long *best;  // [B][T]
+    uint32_t *done;            // [B][groups]
+    int32_t *count;            // [B][parts]: entries of the lists
+    uint32_t *bits;            // [B][parts][slice / 32]
+    uint2 *list;               // [B][parts][entries]: place and bias entry + 1 (16 bits each), word
 };
 
+// Which tokens a part has: token v is in chunk v / kChunk, chunk c in part c % parts.
+struct Part {
+    int32_t V, part, log;
+    __device__ int place_of(int32_t v) const {  // -1: outside the vocabulary or another part's
+        const uint32_t ch = uint32_t(v) / kChunk;
+        return uint32_t(v) < uint32_t(V) && (ch & ((1u << log) - 1)) == uint32_t(part) ? int(((ch >> log) * kChunk) | (uint32_t(v) & (kChunk - 1))) : -1;
+    }
+    __device__ int32_t token_at(int l) const { return ((((l / kChunk) << log) + part) * kChunk) | (l & (kChunk - 1)); }
+    // places in use: every one below it names a token, but for the vocabulary's last chunk
+    __device__ int used() const {
+        const int chunks = (V + kChunk - 1) / kChunk;
+        return (chunks > part ? ((chunks - part - 1) >> log) + 1 : 0) * kChunk;
+    }
+};
+
+// A row's positions, and whether its lengths are good.
+__device__ __forceinline__ int row_positions(const LogitArgs &a, int b, int32_t &L, bool &ok) {
+    const int64_t n = a.new_lens ? int64_t(__ldcg(a.new_lens + b)) + a.new_add : a.T;
+    L = a.lens ? __ldcg(a.lens + b) : 0;
+    ok = n >= 0 && n <= a.T && L >= 0 && L <= a.cap;
+    return ok ? int(n) : 0;
+}
+
+// An element type: widening, narrowing, a vector whose elements without their bit become -inf (lut: for every byte of
+// bits, the mask of four words of two 16-bit elements), and a vector's largest element.
 template <int DT>
 struct Elem;
 template <>
@@ -43,242 +91,447 @@ struct Elem<SWITCHSD_BF16> {
     using type = uint16_t;
     __device__ static float get(uint16_t v) { return bf16_lo(v); }
     __device__ static uint16_t put(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
+    __device__ static uint4 keep(uint4 w, uint32_t open, const uint4 *lut) {
+        const uint4 m = lut[open & 255u];
+        constexpr uint32_t none = 0xff80ff80u;
+        return make_uint4((w.x & m.x) | (none & ~m.x), (w.y & m.y) | (none & ~m.y), (w.z & m.z) | (none & ~m.z), (w.w & m.w) | (none & ~m.w));
+    }
+    __device__ static uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static float largest(uint4 w) {
+        const uint32_t m = max2(max2(w.x, w.y), max2(w.z, w.w));
+        return fmaxf(-INFINITY, fmaxf(bf16_lo(m), bf16_hi(m)));
+    }
 };
 template <>
 struct Elem<SWITCHSD_F16> {
     using type = uint16_t;
     __device__ static float get(uint16_t v) { return __half2float(__ushort_as_half(v)); }
     __device__ static uint16_t put(float f) { return __half_as_ushort(__float2half_rn(f)); }
+    __device__ static uint4 keep(uint4 w, uint32_t open, const uint4 *lut) {
+        const uint4 m = lut[open & 255u];
+        constexpr uint32_t none = 0xfc00fc00u;
+        return make_uint4((w.x & m.x) | (none & ~m.x), (w.y & m.y) | (none & ~m.y), (w.z & m.z) | (none & ~m.z), (w.w & m.w) | (none & ~m.w));
+    }
+    __device__ static uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static float largest(uint4 w) {
+        const uint32_t m = max2(max2(w.x, w.y), max2(w.z, w.w));
+        return fmaxf(-INFINITY, fmaxf(get(uint16_t(m)), get(uint16_t(m >> 16))));
+    }
 };
 template <>
 struct Elem<SWITCHSD_F32> {
     using type = float;
     __device__ static float get(float v) { return v; }
     __device__ static float put(float f) { return f; }
+    __device__ static uint4 keep(uint4 w, uint32_t open, const uint4 *) {
+        constexpr uint32_t none = 0xff800000u;
+        return make_uint4(open & 1 ? w.x : none, open & 2 ? w.y : none, open & 4 ? w.z : none, open & 8 ? w.w : none);
+    }
+    __device__ static float largest(uint4 w) {
+        return fmaxf(-INFINITY, fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w))));
+    }
 };
 
+// A value's place in the order of values; -0 and 0 share one.  That of -inf is kNothing.
+__device__ __forceinline__ uint32_t order_of(float v) {
+    const uint32_t u = __float_as_uint(v + 0.f);
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+constexpr uint32_t kNothing = 0x007fffffu;
 // (value, token) as a word whose order is larger value first, then smaller token; 0 is nothing.
-__device__ __forceinline__ uint64_t best_key(float v, int32_t id) {
-    if (id < 0) return 0;
-    const uint32_t u = __float_as_uint(v);
-    const uint32_t o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-    return (uint64_t(o) << 32) | uint32_t(~uint32_t(id));
-}
+__device__ __forceinline__ uint64_t best_key(uint32_t order, uint32_t id) { return (uint64_t(order) << 32) | uint32_t(~id); }
 
-__device__ __forceinline__ uint64_t warp_max_u64(uint64_t k) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const uint64_t y = __shfl_xor_sync(kFull, k, o);
-        k = y > k ? y : k;
-    }
-    return k;
-}
+__device__ __forceinline__ uint32_t bias_hash(uint32_t id) { return (id * 0x9E3779B1u) >> 15; }
 
-template <int DT>
-__global__ void __launch_bounds__(kLogitThreads) logits_kernel(const LogitArgs a) {
-    using E = Elem<DT>;
-    using elem = typename E::type;
-    constexpr int N = 16 / int(sizeof(elem));  // elements of a vector
-    extern __shared__ uint32_t smem[];
-    __shared__ uint64_t s_best[kLogitRange][kLogitWarps];
-    __shared__ uint64_t s_part[kLogitParts][kLogitRange];
-    uint32_t *cnt = smem;                                                   // [slice]
-    uint32_t *bits = smem + a.slice;                                        // [1 + slice / 32 + 1]: bit of token i at 32 + i
-    uint32_t *bidx = bits + a.slice / 32 + 2;                               // [slice / 2]: 16 bits a token, list entry + 1
+// Shared memory of the counting kernel, in words.
+static size_t count_words(int32_t slice, uint32_t hash_places) { return size_t(slice) + size_t(slice) / 32 + 2 * size_t(hash_places); }
+
+__global__ void __launch_bounds__(kCountThreads) logits_count_kernel(const LogitArgs a) {
+    extern __shared__ __align__(16) uint32_t smem[];
+    __shared__ int32_t s_warp[kCountThreads / kWarp];
+    const uint32_t places = a.nbias ? a.hash_mask + 1 : 0;
+    uint32_t *cnt = smem, *bits = cnt + a.slice;                       // [slice], [slice / 32]
+    int32_t *keys = reinterpret_cast<int32_t *>(bits + a.slice / 32);  // [places]: biased tokens, -1
+    int32_t *vals = keys + places;                                     // [places]: last entry + 1
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = int(cluster_ctarank());
-    const int b = blockIdx.y, t0 = int(blockIdx.z) * a.range;
-    cluster_arrive_relaxed();  // waited for before the first store into another CTA's memory
-    pdl_wait();
-    pdl_trigger();
-
-    const int64_t nw64 = a.new_lens ? int64_t(__ldcg(a.new_lens + b)) + a.new_add : a.T;
-    const int32_t L0 = a.lens ? __ldcg(a.lens + b) : 0;
-    const bool ok = nw64 >= 0 && nw64 <= a.T && L0 >= 0 && L0 <= a.cap;
-    const int nw = ok ? int(nw64) : 0;
-    const int t1 = min(min(t0 + a.range, a.T), nw);  // positions of this cluster that have logits
-    if (rank == 0 && tid == 0 && t0 == 0 && a.status) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
-    const float rep = a.rep ? __ldcg(a.rep + b) : 1.f, freq = a.freq ? __ldcg(a.freq + b) : 0.f, pres = a.pres ? __ldcg(a.pres + b) : 0.f;
-    const bool penal = rep != 1.f || freq != 0.f || pres != 0.f;
-    const int32_t v0 = rank * a.slice, v1 = min(a.V, v0 + a.slice);
-    const int nv = max(0, v1 - v0);
-
-    if (t0 < t1) {
-        // --- counts, biases, the map of what is special ---------------------------------------------------------
-        for (int i = tid; i < a.slice + a.slice / 32 + 2 + (a.nbias ? a.slice / 2 : 0); i += kLogitThreads) smem[i] = 0;
-        const int ndraft = a.draft ? t1 - 1 : 0;  // draft tokens that some position here has behind it
-        __syncthreads();
-        if (penal) {
-            const int32_t *x = a.ctx + size_t(b) * size_t(a.cap);
-            const int32_t first = a.prompt ? __ldcg(a.prompt + b) : 0;
-            for (int i = 4 * tid; i < L0; i += 4 * kLogitThreads) {
-                const int4 r = __ldcg(reinterpret_cast<const int4 *>(x + i));
-                const int32_t id[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t at = uint32_t(id[e]) - uint32_t(v0);
-                    if (i + e < L0 && id[e] >= 0 && at < uint32_t(nv)) {
-                        if (i + e >= first)
-                            atomicAdd(&cnt[at], 1u);
-                        else
-                            atomicOr(&cnt[at], kSeen);
-                    }
-                }
-            }
-            for (int i = tid; i < ndraft; i += kLogitThreads) {
-                const int32_t id = __ldcg(a.draft + size_t(b) * a.draft_stride + i);
-                const uint32_t at = uint32_t(id) - uint32_t(v0);
-                if (id >= 0 && at < uint32_t(nv)) atomicOr(&cnt[at], kInDraft);
-            }
-        }
-        for (int i = tid; i < a.nbias; i += kLogitThreads) {
-            const int32_t id = __ldcg(a.bias_ids + size_t(b) * a.nbias + i);
-            const uint32_t at = uint32_t(id) - uint32_t(v0);
-            if (id < 0 || at >= uint32_t(nv)) continue;
-            // the last entry that names the token: a maximum of 16 bits, whatever the order of the threads
-            const int sh = 16 * int(at & 1);
-            uint32_t old = bidx[at >> 1];
-            while (((old >> sh) & 0xffffu) < uint32_t(i + 1)) {
-                const uint32_t seen = atomicCAS(&bidx[at >> 1], old, (old & ~(0xffffu << sh)) | (uint32_t(i + 1) << sh));
-                if (seen == old) break;
-                old = seen;
-            }
-        }
-        __syncthreads();
-        for (int i = warp; i < a.slice / 32; i += kLogitWarps) {
-            const int at = 32 * i + lane;
-            const bool sp = cnt[at] != 0 || (a.nbias && ((bidx[at >> 1] >> (16 * (at & 1))) & 0xffffu));
-            const uint32_t m = __ballot_sync(kFull, sp);
-            if (lane == 0) bits[1 + i] = m;
-        }
-        __syncthreads();
-
-        // --- the positions --------------------------------------------------------------------------------------
-        for (int t = t0; t < t1; ++t) {
-            const elem *row = reinterpret_cast<const elem *>(a.logits) + int64_t(b) * a.sb + int64_t(t) * a.st + v0;
-            elem *out = a.out ? reinterpret_cast<elem *>(a.out) + int64_t(b) * a.ob + int64_t(t) * a.ot + v0 : nullptr;
-            const uint32_t *mask = a.mask ? a.mask + (size_t(b) * a.T + t) * a.mask_words : nullptr;
-            const int mis = int((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(elem));
-            const bool vec_out = out && ((reinterpret_cast<uintptr_t>(out) & 15) / sizeof(elem)) == size_t(mis);
-            float best = -INFINITY;
-            int32_t best_id = -1;
-            const int nq = (nv + mis + N - 1) / N;
-            for (int q = tid; q < nq; q += kLogitThreads) {
-                const int e0 = q * N - mis;  // first element's place in the slice, negative in the first vector
-                const bool whole = e0 >= 0 && e0 + N <= nv;
-                elem v[N];
-                if (whole) {
-                    *reinterpret_cast<uint4 *>(v) = *reinterpret_cast<const uint4 *>(row + e0);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) v[i] = e0 + i >= 0 && e0 + i < nv ? row[e0 + i] : elem(0);
-                }
-                const int bit = e0 + 32;
-                const uint32_t sp = __funnelshift_r(bits[bit >> 5], bits[min((bit >> 5) + 1, a.slice / 32 + 1)], bit & 31);
-                uint32_t allow = 0xffffffffu;
-                if (mask) {
-                    const int ab = v0 + max(e0, 0), w = ab >> 5;
-                    allow = __funnelshift_r(mask[w], mask[min(w + 1, a.mask_words - 1)], ab & 31) << (max(e0, 0) - e0);
-                }
-                float x[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    x[i] = E::get(v[i]);
-                    if ((sp >> i) & 1) {
-                        const int at = e0 + i;
-                        if (at >= 0 && at < nv) {
-                            const uint32_t c = cnt[at];
-                            uint32_t extra = 0;
-                            if (c & kInDraft)
-                                for (int d = 0; d < t; ++d) extra += __ldcg(a.draft + size_t(b) * a.draft_stride + d) == v0 + at;
-                            const uint32_t m = (c & kCount) + extra;
-                            if ((c & kSeen) || m) x[i] = x[i] > 0.f ? __fdiv_rn(x[i], rep) : __fmul_rn(x[i], rep);
-                            if (m) x[i] = __fsub_rn(__fsub_rn(x[i], __fmul_rn(freq, float(m))), pres);
-                            if (a.nbias) {
-                                const uint32_t k = (bidx[at >> 1] >> (16 * (at & 1))) & 0xffffu;
-                                if (k) x[i] = __fadd_rn(x[i], __ldcg(a.bias + size_t(b) * a.nbias + k - 1));
-                            }
-                        }
-                    }
-                    if (!((allow >> i) & 1)) x[i] = -INFINITY;
-                    if (x[i] > best && e0 + i >= 0 && e0 + i < nv) {
-                        best = x[i];
-                        best_id = v0 + e0 + i;
-                    }
-                }
-                if (out) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) v[i] = E::put(x[i]);
-                    if (whole && vec_out) {
-                        *reinterpret_cast<uint4 *>(out + e0) = *reinterpret_cast<uint4 *>(v);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < N; ++i)
-                            if (e0 + i >= 0 && e0 + i < nv) out[e0 + i] = v[i];
-                    }
-                }
-            }
-            const uint64_t key = warp_max_u64(best_key(best, best_id));
-            if (lane == 0) s_best[t - t0][warp] = key;
-        }
+    const int b = blockIdx.y, parts = int(gridDim.x);
+    const Part part{a.V, int(blockIdx.x), a.parts_log};
+    // everything here but the inputs: before the kernel ahead has finished
+    for (int i = tid; i < a.slice / 4; i += kCountThreads) reinterpret_cast<uint4 *>(cnt)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < int(places); i += kCountThreads) {
+        keys[i] = -1;
+        vals[i] = 0;
     }
     __syncthreads();
-    cluster_wait_acquire();
-    if (t0 < t1) {
-        for (int i = tid; i < t1 - t0; i += kLogitThreads) {
-            uint64_t key = 0;
-#pragma unroll
-            for (int w = 0; w < kLogitWarps; ++w) key = s_best[i][w] > key ? s_best[i][w] : key;
-            asm volatile("st.shared::cluster.u64 [%0], %1;\n" ::"r"(map_to_rank(&s_part[rank][i], 0)), "l"(key) : "memory");
+    pdl_wait();
+    pdl_trigger();
+    int32_t L;
+    bool ok;
+    const int nw = row_positions(a, b, L, ok);
+    if (part.part == 0) {
+        if (tid == 0 && a.status) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
+        for (int t = tid; t < a.T; t += kCountThreads) {
+            a.best[size_t(b) * a.T + t] = 0;
+            if (t >= nw && a.argmax) a.argmax[size_t(b) * a.T + t] = -1;
         }
+        for (int g = tid; g < a.groups; g += kCountThreads) a.done[size_t(b) * a.groups + g] = 0;
     }
-    cluster_arrive_release();
-    cluster_wait_acquire();
-    if (rank == 0 && a.argmax) {
-        for (int t = t0 + tid; t < min(t0 + a.range, a.T); t += kLogitThreads) {
-            uint64_t key = 0;
-            if (t < t1)
+    if (!a.marks || nw == 0) return;
+    const float rep = a.rep ? __ldcg(a.rep + b) : 1.f, freq = a.freq ? __ldcg(a.freq + b) : 0.f, pres = a.pres ? __ldcg(a.pres + b) : 0.f;
+    if (rep != 1.f || freq != 0.f || pres != 0.f) {
+        const int32_t *x = a.ctx + size_t(b) * size_t(a.cap);
+        const int32_t first = a.prompt ? __ldcg(a.prompt + b) : 0;
+#pragma unroll 4
+        for (int i = 4 * tid; i < L; i += 4 * kCountThreads) {
+            const int4 r = __ldcg(reinterpret_cast<const int4 *>(x + i));
+            const int32_t id[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-                for (int p = 0; p < kLogitParts; ++p) key = s_part[p][t - t0] > key ? s_part[p][t - t0] : key;
-            a.argmax[size_t(b) * a.T + t] = key ? int32_t(~uint32_t(key)) : -1;
+            for (int e = 0; e < 4; ++e) {
+                const int at = part.place_of(id[e]);
+                if (at >= 0 && i + e < L) {
+                    if (i + e < first)
+                        atomicOr(&cnt[at], kSeen);
+                    else
+                        atomicAdd(&cnt[at], 1u);
+                }
+            }
         }
+        if (a.draft)
+            for (int i = tid; i < nw - 1; i += kCountThreads) {
+                const int at = part.place_of(__ldcg(a.draft + size_t(b) * a.draft_stride + i));
+                if (at >= 0) atomicOr(&cnt[at], kInDraft);
+            }
     }
-}
-
-// Rows of the mask, padded: bytes of shared memory for a slice.
-static size_t logits_smem(int32_t slice, int32_t nbias) {
-    return (size_t(slice) + size_t(slice / 32) + 2 + (nbias ? size_t(slice) / 2 : 0)) * 4;
+    for (int i = tid; i < a.nbias; i += kCountThreads) {
+        const int32_t id = __ldcg(a.bias_ids + size_t(b) * a.nbias + i);
+        const int at = part.place_of(id);
+        if (at < 0) continue;
+        // at most half of the places are taken, so the search ends; the last entry that names the token stays
+        for (uint32_t p = bias_hash(uint32_t(id)) & a.hash_mask;; p = (p + 1) & a.hash_mask) {
+            const int32_t was = atomicCAS(&keys[p], -1, id);
+            if (was == -1 || was == id) {
+                atomicMax(&vals[p], i + 1);
+                break;
+            }
+        }
+        atomicOr(&cnt[at], kBiased);
+    }
+    __syncthreads();
+    // The map, and every warp's number of specials in its share of it: words [warp per, + per).
+    const int words = a.slice / 32, per = (words + kCountThreads / kWarp - 1) / (kCountThreads / kWarp);
+    const int w0 = min(words, warp * per), w1 = min(words, w0 + per);
+    uint32_t *out_bits = a.bits + (size_t(b) * parts + part.part) * words;
+    int mine = 0;
+#pragma unroll 4
+    for (int i = w0; i < w1; ++i) {
+        const uint32_t m = __ballot_sync(kFull, cnt[32 * i + lane] != 0);
+        if (lane == 0) {
+            bits[i] = m;
+            out_bits[i] = m;
+        }
+        mine += __popc(m);
+    }
+    if (lane == 0) s_warp[warp] = mine;
+    __syncthreads();
+    int at = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kCountThreads / kWarp; ++w) {
+        if (w < warp) at += s_warp[w];
+        all += s_warp[w];
+    }
+    if (tid == 0) a.count[size_t(b) * parts + part.part] = all;
+    uint2 *list = a.list + (size_t(b) * parts + part.part) * a.entries;
+    for (int i = w0; i < w1; ++i) {
+        const uint32_t m = bits[i];
+        if ((m >> lane) & 1) {
+            const uint32_t w = cnt[32 * i + lane];
+            uint32_t bias = 0;
+            if (w & kBiased) {
+                const int32_t v = part.token_at(32 * i + lane);
+                uint32_t p = bias_hash(uint32_t(v)) & a.hash_mask;
+                while (keys[p] != v) p = (p + 1) & a.hash_mask;
+                bias = uint32_t(vals[p]);
+            }
+            const int k = at + __popc(m & ((1u << lane) - 1));
+            if (k < a.entries) list[k] = make_uint2(uint32_t(32 * i + lane) | (bias << 16), w);
+        }
+        at += __popc(m);
+    }
 }
 
 template <int DT>
-static cudaError_t launch_logits(const LogitArgs &a, int B, int ranges, cudaStream_t s) {
+__global__ void __launch_bounds__(kLogitThreads, 4) logits_kernel(const LogitArgs a) {
+    using E = Elem<DT>;
+    using elem = typename E::type;
+    constexpr int N = 16 / int(sizeof(elem));             // elements of a vector
+    constexpr int kUnit = kWarp * N;                      // tokens of a unit
+    __shared__ unsigned long long s_best[kLogitGroup];
+    __shared__ uint4 s_lut[DT == SWITCHSD_F32 ? 1 : 256];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int b = blockIdx.z, t0 = int(blockIdx.y) * kLogitGroup, parts = int(gridDim.x);
+    const Part part{a.V, int(blockIdx.x), a.parts_log};
+    auto token_at = [&](int l) { return part.token_at(l); };
+    if (tid < kLogitGroup) s_best[tid] = 0;
+    if (DT != SWITCHSD_F32 && tid < 256) {
+        auto pair = [&](int i) { return ((tid >> i) & 1 ? 0xffffu : 0u) | ((tid >> (i + 1)) & 1 ? 0xffff0000u : 0u); };
+        s_lut[tid] = make_uint4(pair(0), pair(2), pair(4), pair(6));
+    }
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    int32_t L;
+    bool ok;
+    const int t1 = min(t0 + kLogitGroup, row_positions(a, b, L, ok));
+    if (t0 >= t1) return;
+    const elem *rows = reinterpret_cast<const elem *>(a.logits) + int64_t(b) * a.sb;
+    elem *outs = a.out ? reinterpret_cast<elem *>(a.out) + int64_t(b) * a.ob : nullptr;
+    const uint32_t *masks = a.mask ? a.mask + size_t(b) * a.T * a.mask_words : nullptr;
+    const uint32_t *bits = a.bits + (size_t(b) * parts + part.part) * (a.slice / 32);
+    const int units = part.used() / kUnit;                // of a position
+    for (int t = t0; t < t1; ++t) {
+        const elem *row = rows + int64_t(t) * a.st;
+        elem *out = outs ? outs + int64_t(t) * a.ot : nullptr;
+        const uint32_t *mask = masks ? masks + size_t(t) * a.mask_words : nullptr;
+        // whether a unit is read (and written) by vectors; else 32 neighbours at a time
+        const bool vectors = ((reinterpret_cast<uintptr_t>(row) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+        uint32_t top = kNothing, top_id = 0;  // the warp's best so far
+        for (int u0 = warp; u0 < units; u0 += kLogitUnits * kLogitWarps) {
+            auto whole = [&](int u) { return vectors && u < units && token_at(u * kUnit) + kUnit <= a.V; };
+            {
+                // lane l of unit i: N tokens from token_at(u kUnit) + l N on
+                uint4 w[kLogitUnits];
+                uint32_t allow[kLogitUnits];
+                float mx[kLogitUnits];
+#pragma unroll
+                for (int i = 0; i < kLogitUnits; ++i) {
+                    const int u = u0 + i * kLogitWarps;
+                    const int32_t v = token_at(u * kUnit) + lane * N;
+                    w[i] = make_uint4(0, 0, 0, 0);
+                    allow[i] = 0;
+                    if (whole(u)) {
+                        w[i] = *reinterpret_cast<const uint4 *>(row + v);
+                        allow[i] = mask ? uint32_t(reinterpret_cast<const uint8_t *>(mask)[v >> 3]) >> (v & 7) : 0xffu;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kLogitUnits; ++i) {
+                    mx[i] = -INFINITY;
+                    if (!whole(u0 + i * kLogitWarps)) continue;
+                    const int l = (u0 + i * kLogitWarps) * kUnit + lane * N;
+                    const uint32_t special = a.marks ? uint32_t(reinterpret_cast<const uint8_t *>(bits)[l >> 3]) >> (l & 7) : 0u;
+                    if (out) {
+                        const uint4 y = mask ? E::keep(w[i], allow[i], s_lut) : w[i];
+                        *reinterpret_cast<uint4 *>(out + token_at((u0 + i * kLogitWarps) * kUnit) + lane * N) = y;
+                    }
+                    w[i] = E::keep(w[i], allow[i] & ~special, s_lut);
+                    mx[i] = E::largest(w[i]);
+                }
+                float most = mx[0];
+#pragma unroll
+                for (int i = 1; i < kLogitUnits; ++i) most = fmaxf(most, mx[i]);
+                const uint32_t mine = order_of(most), all = __reduce_max_sync(kFull, mine);
+                if (all > top) {  // a warp's tokens come in order, so only a larger value is better
+                    uint32_t id = 0xffffffffu;
+                    if (mine == all) {
+#pragma unroll
+                        for (int i = kLogitUnits - 1; i >= 0; --i)
+                            if (mx[i] == most) {
+                                elem y[N];
+                                *reinterpret_cast<uint4 *>(y) = w[i];
+                                const int32_t v = token_at((u0 + i * kLogitWarps) * kUnit) + lane * N;
+#pragma unroll
+                                for (int j = N - 1; j >= 0; --j)
+                                    if (E::get(y[j]) == most) id = uint32_t(v + j);
+                            }
+                    }
+                    top = all;
+                    top_id = __reduce_min_sync(kFull, id);
+                }
+            }
+            if (!whole(min(units - 1, u0 + (kLogitUnits - 1) * kLogitWarps))) {
+                // a row off the 16-byte boundaries, or the vocabulary's last tokens: lane l has tokens v0 + 32 j + l
+                for (int u = u0; u < min(units, u0 + kLogitUnits * kLogitWarps); u += kLogitWarps) {
+                    if (whole(u)) continue;
+                    const int32_t v0 = token_at(u * kUnit);
+                    elem y[N];
+                    uint32_t allow[N];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const int32_t v = v0 + 32 * j + lane;
+                        y[j] = v < a.V ? row[v] : elem(0);
+                        allow[j] = v0 + 32 * j >= a.V ? 0u : mask ? mask[(v0 >> 5) + j] : 0xffffffffu;
+                    }
+                    float best = -INFINITY;
+                    uint32_t best_id = 0xffffffffu;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const int32_t v = v0 + 32 * j + lane;
+                        const bool in = v < a.V, may = (allow[j] >> lane) & 1;
+                        const float x = in && may && !(a.marks && ((bits[u * (kUnit / 32) + j] >> lane) & 1)) ? E::get(y[j]) : -INFINITY;
+                        if (x > best) {
+                            best = x;
+                            best_id = uint32_t(v);
+                        }
+                        if (out && in) out[v] = may ? y[j] : E::put(-INFINITY);
+                    }
+                    const uint32_t mine = order_of(best), all = __reduce_max_sync(kFull, mine);
+                    if (all > top) {
+                        top = all;
+                        top_id = __reduce_min_sync(kFull, mine == all ? best_id : 0xffffffffu);
+                    }
+                }
+            }
+        }
+        if (lane == 0 && top > kNothing) atomicMax(&s_best[t - t0], static_cast<unsigned long long>(best_key(top, top_id)));
+    }
+    if (a.marks) {
+        if (outs) __syncthreads();  // the specials' results go over what the vectors wrote in their places
+        const float rep = a.rep ? __ldcg(a.rep + b) : 1.f, freq = a.freq ? __ldcg(a.freq + b) : 0.f, pres = a.pres ? __ldcg(a.pres + b) : 0.f;
+        const int specials = min(__ldcg(a.count + size_t(b) * parts + part.part), a.entries);
+        const uint2 *list = a.list + (size_t(b) * parts + part.part) * a.entries;
+        const int32_t *draft = a.draft + size_t(b) * a.draft_stride;
+        for (int s = tid; s < specials; s += kLogitThreads) {
+            const uint2 entry = __ldcg(list + s);
+            const uint32_t w = entry.y;
+            const int32_t v = part.token_at(int(entry.x & 0xffffu));
+            const elem *p = rows + int64_t(t0) * a.st + v;
+            float x[kLogitGroup];
+            uint32_t may[kLogitGroup];
+#pragma unroll
+            for (int i = 0; i < kLogitGroup; ++i) {
+                x[i] = t0 + i < t1 ? E::get(p[i * a.st]) : 0.f;
+                may[i] = masks && t0 + i < t1 ? masks[size_t(t0 + i) * a.mask_words + (v >> 5)] >> (v & 31) : 1u;
+            }
+            const float bias = w & kBiased ? __ldcg(a.bias + size_t(b) * a.nbias + (entry.x >> 16) - 1) : 0.f;
+            uint32_t m = w & kCount;
+            if (w & kInDraft)  // the draft's tokens behind the group's first position
+                for (int d = 0; d < t0; ++d) m += __ldcg(draft + d) == v;
+#pragma unroll
+            for (int i = 0; i < kLogitGroup; ++i) {
+                if (t0 + i >= t1) break;
+                float y = x[i];
+                if ((w & kSeen) || m) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+                if (m) y = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, float(m))), pres);
+                if (w & kBiased) y = __fadd_rn(y, bias);
+                if (!(may[i] & 1)) y = -INFINITY;
+                if (y > -INFINITY) {
+                    const uint64_t key = best_key(order_of(y), uint32_t(v));
+                    if (key > s_best[i]) atomicMax(&s_best[i], static_cast<unsigned long long>(key));
+                }
+                if (outs) outs[int64_t(t0 + i) * a.ot + v] = E::put(y);
+                if ((w & kInDraft) && t0 + i + 1 < t1) m += __ldcg(draft + t0 + i) == v;
+            }
+        }
+    }
+    if (!a.argmax) return;
+    __syncthreads();
+    // the parts' best; the last part of these positions writes the tokens
+    if (tid < t1 - t0) {
+        if (s_best[tid]) atomicMax(&a.best[size_t(b) * a.T + t0 + tid], s_best[tid]);
+        __threadfence();
+    }
+    __syncthreads();
+    if (tid == 0) s_last = atomicAdd(&a.done[size_t(b) * a.groups + blockIdx.y], 1u) == uint32_t(parts - 1);
+    __syncthreads();
+    if (s_last && tid < t1 - t0) {
+        __threadfence();
+        const uint64_t key = __ldcg(&a.best[size_t(b) * a.T + t0 + tid]);
+        a.argmax[size_t(b) * a.T + t0 + tid] = key ? int32_t(~uint32_t(key)) : -1;
+    }
+}
+
+// The parts: two CTAs of the counting kernel an SM by shared memory, at least.
+static int parts_log_of(int32_t V) { return V > 131072 ? 4 : V > 8192 ? 3 : 2; }
+static int32_t slice_of(int32_t V) {
+    const int parts = 1 << parts_log_of(V);
+    return ((V + kChunk - 1) / kChunk + parts - 1) / parts * kChunk;
+}
+
+// The workspace: sizes of its arrays, and their places after `base`.
+static size_t logits_layout(const switchsd_logits_params *p, LogitArgs *a) {
+    const size_t B = size_t(p->B), parts = size_t(1) << parts_log_of(p->V), slice = size_t(slice_of(p->V));
+    const size_t groups = (size_t(p->T) + kLogitGroup - 1) / kLogitGroup;
+    const bool marks = p->rep || p->freq || p->pres || p->nbias;
+    // a part has no more specials than tokens, nor than the context, the draft and the biases name
+    const size_t named = (p->ctx_tokens ? size_t(p->cap) : 0) + (p->draft ? size_t(p->T) : 0) + size_t(p->nbias);
+    const size_t entries = marks ? std::min(slice, named) : 0;
+    uint8_t *at = nullptr;
+    if (a) {
+        a->groups = int32_t(groups);
+        a->entries = int32_t(entries);
+        a->marks = marks && entries > 0;
+        at = static_cast<uint8_t *>(p->workspace);
+    }
+    size_t size = 0;
+    auto take = [&](size_t bytes) {
+        uint8_t *q = at + size;
+        size += (bytes + 15) / 16 * 16;
+        return q;
+    };
+    uint8_t *best = take(B * size_t(p->T) * 8), *done = take(B * groups * 4), *count = take(B * parts * 4);
+    uint8_t *bits = take(marks ? B * parts * (slice / 32) * 4 : 0), *list = take(B * parts * entries * 8);
+    if (a) {
+        a->best = reinterpret_cast<unsigned long long *>(best);
+        a->done = reinterpret_cast<uint32_t *>(done);
+        a->count = reinterpret_cast<int32_t *>(count);
+        a->bits = reinterpret_cast<uint32_t *>(bits);
+        a->list = reinterpret_cast<uint2 *>(list);
+    }
+    return size;
+}
+
+template <int DT>
+static cudaError_t launch_logits(const LogitArgs &a, int B, cudaStream_t s) {
     static bool attr_done[64] = {false};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64 || !attr_done[dev]) {
-        e = cudaFuncSetAttribute(logits_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 int(logits_smem((SWITCHSD_VMAX / kLogitParts + 63) / 64 * 64, 1)));
+        // the widest part and the largest bias table
+        e = cudaFuncSetAttribute(logits_count_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(4 * count_words(16384, 2 * SWITCHSD_BIAS_MAX)));
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_done[dev] = true;
     }
-    return launch_pdl(logits_kernel<DT>, dim3(kLogitParts, unsigned(B), unsigned(ranges)), dim3(kLogitThreads), logits_smem(a.slice, a.nbias), s,
-                      unsigned(kLogitParts), a);
+    const unsigned parts = 1u << a.parts_log;
+    // without specials the counting kernel only clears the positions' words
+    const size_t smem = 4 * count_words(a.marks ? a.slice : 0, a.nbias ? a.hash_mask + 1 : 0);
+    LogitArgs c = a;
+    if (!a.marks) {
+        c.slice = 0;
+        c.nbias = 0;
+    }
+    e = launch_pdl(logits_count_kernel, dim3(a.marks ? parts : 1u, unsigned(B)), dim3(kCountThreads), smem, s, 0u, c);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(logits_kernel<DT>, dim3(parts, unsigned(a.groups), unsigned(B)), dim3(kLogitThreads), 0, s, 0u, a);
 }
 
 }  // namespace switchsd
 
 using namespace switchsd;
 
+extern "C" size_t switchsd_logits_workspace_bytes(const switchsd_logits_params *p) {
+    if (!p || p->B < 1 || p->T < 1 || p->V < 1 || p->V > SWITCHSD_VMAX || p->cap < 0 || p->nbias < 0) return 0;
+    return logits_layout(p, nullptr);
+}
+
 extern "C" int switchsd_logits(const switchsd_logits_params *p) {
-    if (!p || !p->logits || (!p->out && !p->argmax)) return SWITCHSD_ERR_ARG;
+    if (!p || !p->logits || (!p->out && !p->argmax) || !p->workspace || !aligned16(p->workspace)) return SWITCHSD_ERR_ARG;
     if (p->dtype != SWITCHSD_BF16 && p->dtype != SWITCHSD_F16 && p->dtype != SWITCHSD_F32) return SWITCHSD_ERR_ARG;
     const uintptr_t size = p->dtype == SWITCHSD_F32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(p->logits) % size || reinterpret_cast<uintptr_t>(p->out) % size) return SWITCHSD_ERR_ARG;
     if ((p->ctx_tokens == nullptr) != (p->ctx_lens == nullptr) || (reinterpret_cast<uintptr_t>(p->ctx_tokens) & 15)) return SWITCHSD_ERR_ARG;
     if (p->nbias < 0 || (p->nbias > 0 && (!p->bias_ids || !p->bias))) return SWITCHSD_ERR_ARG;
     if (p->B < 1 || p->B > 65535 || p->T < 1 || p->V < 1 || p->V > SWITCHSD_VMAX || p->nbias > SWITCHSD_BIAS_MAX) return SWITCHSD_ERR_SHAPE;
-    if (p->ctx_tokens && (p->cap < 4 || p->cap % 4 != 0 || p->cap >= (1 << 30))) return SWITCHSD_ERR_SHAPE;
+    if (p->ctx_tokens && (p->cap < 4 || p->cap % 4 != 0 || p->cap >= (1 << 28))) return SWITCHSD_ERR_SHAPE;
     if (p->draft && p->T > 1 && p->draft_stride < p->T - 1) return SWITCHSD_ERR_SHAPE;
     if (p->mask && p->mask_words < (p->V + 31) / 32) return SWITCHSD_ERR_SHAPE;
     if (p->stride_b < 0 || p->stride_t < 0 || p->out_stride_b < 0 || p->out_stride_t < 0) return SWITCHSD_ERR_ARG;
@@ -309,15 +562,19 @@ extern "C" int switchsd_logits(const switchsd_logits_params *p) {
     a.new_add = p->new_add;
     a.nbias = p->nbias;
     a.mask_words = p->mask_words;
-    a.slice = ((p->V + kLogitParts - 1) / kLogitParts + 63) / 64 * 64;
-    // enough clusters for the chip, as few positions each as that takes (every cluster counts its row's context)
-    const int want = std::max(1, 152 * 2 / (kLogitParts * p->B));
-    a.range = std::min(kLogitRange, std::max(1, (p->T + want - 1) / want));
-    const int ranges = (p->T + a.range - 1) / a.range;
-    if (ranges > 65535) return SWITCHSD_ERR_SHAPE;
+    if (p->workspace_bytes < logits_layout(p, &a)) return SWITCHSD_ERR_ARG;
+    if (a.groups > 65535) return SWITCHSD_ERR_SHAPE;
+    a.parts_log = parts_log_of(p->V);
+    a.slice = slice_of(p->V);
+    a.hash_mask = 0;
+    if (p->nbias) {
+        uint32_t places = 2;
+        while (places < 2u * uint32_t(p->nbias)) places *= 2;
+        a.hash_mask = places - 1;
+    }
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);
-    const cudaError_t e = p->dtype == SWITCHSD_F32    ? launch_logits<SWITCHSD_F32>(a, p->B, ranges, s)
-                          : p->dtype == SWITCHSD_F16 ? launch_logits<SWITCHSD_F16>(a, p->B, ranges, s)
-                                                     : launch_logits<SWITCHSD_BF16>(a, p->B, ranges, s);
+    const cudaError_t e = p->dtype == SWITCHSD_F32    ? launch_logits<SWITCHSD_F32>(a, p->B, s)
+                          : p->dtype == SWITCHSD_F16 ? launch_logits<SWITCHSD_F16>(a, p->B, s)
+                                                     : launch_logits<SWITCHSD_BF16>(a, p->B, s);
     return e == cudaSuccess ? SWITCHSD_OK : SWITCHSD_ERR_CUDA;
 }

@@ -30,7 +30,8 @@ APPEND = dict(B=2, T=3, Hkv=2, D=64, page=16, pages=9, dtype=0, k=FAKE, v=FAKE, 
 READ = dict(B=2, T=3, Hkv=2, D=64, page=16, pages=9, cache=FAKE, slots=FAKE, out_k=FAKE, out_v=FAKE)
 ATTN = dict(B=2, T=3, Hq=4, Hkv=2, D=64, page=16, pages=9, blocks=4, dtype=0, q=FAKE, q_stride=(768, 256, 64), cache=FAKE, block_table=FAKE, lens=FAKE,
             new_lens=FAKE, scale=0.1, out=FAKE, workspace=FAKE, workspace_bytes=1 << 40)
-LOGITS = dict(B=2, T=3, V=100, cap=8, dtype=0, logits=FAKE, stride_b=300, stride_t=100, ctx_tokens=FAKE, ctx_lens=FAKE, draft=FAKE, draft_stride=2, argmax=FAKE)
+LOGITS = dict(B=2, T=3, V=100, cap=8, dtype=0, logits=FAKE, stride_b=300, stride_t=100, ctx_tokens=FAKE, ctx_lens=FAKE, draft=FAKE, draft_stride=2, argmax=FAKE,
+              workspace=FAKE, workspace_bytes=1 << 40)
 
 
 @pytest.mark.parametrize("code,kw", [(ARG, dict(lens=None)), (ARG, dict(new_lens=None)), (ARG, dict(block_table=None)), (ARG, dict(held=None)),
@@ -65,7 +66,7 @@ def test_attention_refuses(bd, code, kw):
 
 
 @pytest.mark.parametrize("code,kw", [(ARG, dict(logits=None)), (ARG, dict(argmax=None)), (ARG, dict(dtype=3)), (ARG, dict(logits=FAKE + 1)), (ARG, dict(ctx_lens=None)),
-                                     (ARG, dict(ctx_tokens=FAKE + 4)), (ARG, dict(nbias=3)), (ARG, dict(nbias=-1)), (ARG, dict(stride_t=-100)), (SHAPE, dict(B=0)),
+                                     (ARG, dict(ctx_tokens=FAKE + 4)), (ARG, dict(nbias=3)), (ARG, dict(workspace=None)), (ARG, dict(workspace=FAKE + 4)), (ARG, dict(workspace_bytes=8)), (ARG, dict(nbias=-1)), (ARG, dict(stride_t=-100)), (SHAPE, dict(B=0)),
                                      (SHAPE, dict(B=65536)), (SHAPE, dict(T=0)), (SHAPE, dict(V=0)), (SHAPE, dict(V=262145)), (SHAPE, dict(cap=6)),
                                      (SHAPE, dict(draft_stride=1)), (SHAPE, dict(mask=FAKE, mask_words=3)), (SHAPE, dict(nbias=4097, bias_ids=FAKE, bias=FAKE))])
 def test_logits_refuses(bd, code, kw):

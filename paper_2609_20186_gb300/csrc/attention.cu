@@ -19,18 +19,15 @@
 // the matrix unit's own accumulation truncates.  The weights exp(s - M) * scale_v are rounded to f16 (11 bits): M is the
 // running maximum of the score plus the exponent of its value's scale, so that the largest weight is near 1 whatever
 // the scales, and weights below 2^-26 of it begin to lose bits.
-#include <cuda_bf16.h>
-
 #include <algorithm>
 
-#include "kv4.cuh"
+#include "attention.cuh"
 
 namespace switchsd {
 
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = kAttnWarps * kWarp;
 constexpr int kAttnUnit = kAttnWarps * 32;  // keys of a unit: 32 a warp
-constexpr int kAttnMaxCtas = 1024;
 #ifndef ATTN_OCC
 #define ATTN_OCC 3
 #endif
@@ -39,43 +36,6 @@ constexpr float kWeightUp = 4096.f;         // the weights' scale as f16 numbers
 constexpr float kSmall = 6.103515625e-5f;   // 2^-14: below it f16 loses bits
 constexpr float kLift = 16777216.f;         // 2^24: of the product of the small weights
 constexpr float kNone = 3.552713678800501e-15f;  // 2^-48, 2^-60 of the largest: too small for either
-constexpr float kFloor = -1e30f;            // the maximum of nothing
-
-struct AttnArgs {
-    const uint16_t *q;
-    int64_t qs[3];
-    const uint8_t *cache;
-    const int32_t *table, *lens, *new_lens;
-    uint16_t *out;
-    float *part;        // [2 * CTAs][rows][D + 2]: output, maximum, sum
-    int4 *desc;         // [2 * CTAs]: of a partial result: item's row (-1: none), key head, tile of query rows, flags
-    int32_t *status;
-    int32_t B, T, Hq, Hkv, pages, blocks, page_shift, lens_add, new_add, group;
-    float scale;
-};
-
-constexpr int kFirst = 1, kLast = 2;  // flags of a partial result: holds the item's first, last unit
-
-// A row's lengths, or false where they are bad.
-__device__ __forceinline__ bool row_lengths(const AttnArgs &a, int b, int32_t &len, int32_t &nw) {
-    const int64_t l = int64_t(__ldcg(a.lens + b)) + a.lens_add, n = int64_t(__ldcg(a.new_lens + b)) + a.new_add;
-    const bool ok = l >= 0 && n >= 0 && n <= a.T && l + n <= (int64_t(a.blocks) << a.page_shift);
-    len = ok ? int32_t(l) : 0;
-    nw = ok ? int32_t(n) : 0;
-    return ok;
-}
-
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 
 // D = A B + C of m16n8k16, f16 operands, binary32 sums.
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
@@ -92,59 +52,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     return r;
 }
 
-// A word's four pairs of codes as pairs of f16 numbers c - 8: the code under the exponent of 1024 is 1024 + c (or, four
-// bits higher, 1024 + 16 c), and one operation on the pair takes the rest off exactly.
-__device__ __forceinline__ uint32_t pair_sub(uint32_t v) {
-    uint32_t r;
-    asm("add.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0xe408e408u));  // - 1032
-    return r;
-}
-__device__ __forceinline__ uint32_t pair_sub16(uint32_t v) {
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0x2c002c00u), "r"(0xd480d480u));  // / 16 - 72
-    return r;
-}
-__device__ __forceinline__ void signed_codes(uint32_t w, uint32_t (&v)[4]) {
-    const uint32_t y = w >> 8;
-    v[0] = pair_sub((w & 0x000f000fu) | 0x64006400u);
-    v[1] = pair_sub16((w & 0x00f000f0u) | 0x64006400u);
-    v[2] = pair_sub((y & 0x000f000fu) | 0x64006400u);
-    v[3] = pair_sub16((y & 0x00f000f0u) | 0x64006400u);
-}
-
-__device__ __forceinline__ uint4 load16(const uint8_t *p) {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
-__device__ __forceinline__ uint2 load8(const uint8_t *p) {
-    uint2 v;
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-    return v;
-}
-__device__ __forceinline__ uint32_t load4(const uint8_t *p) {
-    uint32_t v;
-    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
-    return v;
-}
-
-template <bool F16>
-__device__ __forceinline__ float widen1(uint16_t v) {
-    return F16 ? __half2float(__ushort_as_half(v)) : bf16_lo(v);
-}
-template <bool F16>
-__device__ __forceinline__ uint32_t narrow2(float a, float b) {
-    if (F16) return pack_f16(a, b);
-    const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-
-// Units of one row, and a position among the units.
-struct Place {
-    int b, hk, rt;    // item
-    int32_t unit;     // of the item
-};
-
 // The codes and scales of a thread's share of 32 keys.
 template <int D>
 struct Keys {
@@ -160,85 +67,17 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
     constexpr int G = L::G, R = 8 * NT, MT = D / 16;  // groups, query rows of a tile, output tiles of 16 dimensions
     extern __shared__ float s_out[];                  // [warps][R][D + 4]
     __shared__ float s_max[kAttnWarps][R], s_sum[kAttnWarps][R];
-    __shared__ int64_t s_pre[kAttnThreads + 1];
-    __shared__ int s_place[1];
-    __shared__ int64_t s_before[1];
+    __shared__ int64_t s_pre[kAttnThreads + 2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r = lane >> 2, c = lane & 3;
     const int cta = blockIdx.x, ctas = int(gridDim.x);
     pdl_wait();
     pdl_trigger();
 
-    // --- the CTA's range of units -------------------------------------------------------------------------------
-    const int per = (a.B + kAttnThreads - 1) / kAttnThreads;  // rows of a thread
-    auto units_of = [&](int b, int32_t &len, int32_t &nw) -> int64_t {
-        const bool ok = row_lengths(a, b, len, nw);
-        if (a.status && cta == 0) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
-        const int64_t tiles = (int64_t(nw) * a.group + R - 1) / R;
-        return nw ? tiles * a.Hkv * ((int64_t(len) + nw + kAttnUnit - 1) / kAttnUnit) : 0;
-    };
-    int64_t mine = 0;
-    for (int i = 0; i < per; ++i) {
-        const int b = tid * per + i;
-        int32_t len, nw;
-        if (b < a.B) mine += units_of(b, len, nw);
-    }
-    {
-        int64_t x = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(kFull, x, o);
-            if (lane >= o) x += y;
-        }
-        s_pre[tid + 1] = x;
-        __syncthreads();
-        int64_t add = 0;
-        for (int w = 0; w < warp; ++w) add += s_pre[32 * w + 32];
-        __syncthreads();
-        s_pre[tid + 1] = x + add;
-        if (tid == 0) s_pre[0] = 0;
-        __syncthreads();
-    }
-    const int64_t total = s_pre[kAttnThreads];
-    const int64_t takers = min(total, int64_t(ctas));  // CTAs with a range: at least one unit each
-    int64_t u = cta < takers ? total * cta / takers : total;
-    const int64_t u_end = cta < takers ? total * (cta + 1) / takers : total;
-    // zeros for the query rows of tokens that are not there
-    for (int64_t i0 = int64_t(cta) * kAttnWarps + warp; i0 * kWarp < int64_t(a.B) * a.T; i0 += int64_t(ctas) * kAttnWarps) {
-        const int64_t i = i0 * kWarp + lane;
-        bool none = false;
-        if (i < int64_t(a.B) * a.T) {
-            int32_t len, nw;
-            row_lengths(a, int(i / a.T), len, nw);
-            none = int(i % a.T) >= nw;
-        }
-        uint32_t todo = __ballot_sync(kFull, none);
-        while (todo) {
-            const int l = __ffs(int(todo)) - 1;
-            todo &= todo - 1;
-            uint4 *o = reinterpret_cast<uint4 *>(a.out + size_t(i0 * kWarp + l) * a.Hq * D);
-            for (int e = lane; e < a.Hq * D / 8; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
-        }
-    }
-    if (tid < 2) a.desc[2 * cta + tid] = make_int4(-1, 0, 0, 0);
-    __syncthreads();
+    int b;
+    int64_t u, u_end, base_u;
+    deal_units<kAttnThreads>(a, R, kAttnUnit, cta, ctas, s_pre, u, u_end, b, base_u);
     if (u >= u_end) return;
-    // the row that unit u lies in
-    if (u >= s_pre[tid] && u < s_pre[tid + 1]) {
-        int64_t at = s_pre[tid];
-        int b = tid * per;
-        for (;; ++b) {
-            int32_t len, nw;
-            const int64_t n = units_of(b, len, nw);
-            if (u < at + n) break;
-            at += n;
-        }
-        s_place[0] = b;
-        s_before[0] = at;
-    }
-    __syncthreads();
-    int b = s_place[0];
-    int64_t base_u = s_before[0];
     const int64_t u_begin = u;
     const int page_mask = (1 << a.page_shift) - 1;
     const size_t head_bytes = size_t(kv4_page_bytes(1 << a.page_shift, D));
@@ -614,44 +453,6 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
     }
 }
 
-// Joins the partial results of the items that several CTAs hold: CTA (i, row) looks after the item whose first part is
-// the i-th CTA's, adding the parts in order.
-template <bool F16, int D, int NT>
-__global__ void __launch_bounds__(D) attn_join_kernel(const AttnArgs a) {
-    constexpr int R = 8 * NT;
-    const int i = blockIdx.x, row = blockIdx.y, d = threadIdx.x, ctas = int(gridDim.x);
-    pdl_wait();
-    pdl_trigger();
-    int slot = 2 * i + 1;
-    int4 de = __ldcg(a.desc + slot);
-    if (de.x < 0 || !(de.w & kFirst)) {
-        slot = 2 * i;
-        de = __ldcg(a.desc + slot);
-        if (de.x < 0 || !(de.w & kFirst)) return;
-    }
-    int32_t len, nw;
-    row_lengths(a, de.x, len, nw);
-    const int rr = de.z * R + row, t = rr / a.group;
-    if (t >= nw) return;
-    float mx = kFloor, sum = 0.f, y = 0.f;
-    int next = i;
-    for (int flags = de.w;;) {
-        const float *src = a.part + (size_t(slot) * R + row) * (D + 4);
-        const float pm = __ldcg(src + D), ps = __ldcg(src + D + 1), py = __ldcg(src + d);
-        const float mn = fmaxf(mx, pm), f0 = exp2_approx(mx - mn), f1 = exp2_approx(pm - mn);
-        y = y * f0 + py * f1;
-        sum = sum * f0 + ps * f1;
-        mx = mn;
-        if ((flags & kLast) || ++next >= ctas) break;
-        slot = 2 * next;
-        flags = __ldcg(&a.desc[slot].w);
-    }
-    const int h = de.y * a.group + rr - t * a.group;
-    const float inv = sum == 0.f ? 0.f : (1.f / kWeightUp) / sum;
-    const uint32_t w = narrow2<F16>(y * inv, 0.f);
-    a.out[((size_t(de.x) * a.T + t) * a.Hq + h) * D + d] = uint16_t(w);
-}
-
 static int attn_sms() {
     static int count[64] = {0};
     int dev = 0;
@@ -661,7 +462,7 @@ static int attn_sms() {
 }
 
 static size_t attn_workspace(int D, int NT) {
-    return size_t(2 * kAttnMaxCtas) * (sizeof(int4) + size_t(8 * NT) * (D + 4) * sizeof(float));
+    return std::max(size_t(2 * kAttnMaxCtas) * (sizeof(int4) + size_t(8 * NT) * (D + 4) * sizeof(float)), attn_tc_workspace(D));
 }
 
 template <bool F16, int D, int NT>
@@ -679,11 +480,14 @@ static cudaError_t launch_attn(AttnArgs a, int sms, cudaStream_t s) {
     const unsigned ctas = unsigned(std::min(kAttnMaxCtas, sms * attn_ctas_per_sm(NT)));
     e = launch_pdl(attn_kernel<F16, D, NT>, dim3(ctas), dim3(kAttnThreads), smem, s, 0u, a);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attn_join_kernel<F16, D, NT>, dim3(ctas, 8 * NT), dim3(D), 0, s, 0u, a);
+    return launch_pdl(attn_join_kernel<F16, D>, dim3(ctas, 8 * NT), dim3(D), 0, s, 0u, a, 8 * NT, 1.f / kWeightUp);
 }
+
+constexpr int kTensorRows = 16;
 
 template <bool F16, int D>
 static cudaError_t launch_attn_rows(const AttnArgs &a, int sms, cudaStream_t s) {
+    if (a.T * a.group > kTensorRows) return launch_attn_tc(a, F16, D, sms, s);
     return a.T * a.group <= 8 ? launch_attn<F16, D, 1>(a, sms, s) : launch_attn<F16, D, 2>(a, sms, s);
 }
 
@@ -729,6 +533,7 @@ extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
     a.lens_add = p->lens_add;
     a.new_add = p->new_add;
     a.group = p->Hq / p->Hkv;
+    a.dim = p->D;
     a.scale = p->scale;
     const int sms = attn_sms();
     if (sms == 0) return SWITCHSD_ERR_CUDA;

@@ -1,0 +1,569 @@
+// attention_tc.cu -- attention over the 4-bit paged cache for many query rows: the verification of drafts.
+//
+// Same work, units (128 keys) and partial results as attention.cu, with tiles of 128 query rows, on tcgen05.  One CTA an
+// SM, with roles for its warps:
+//   4 warps unpack: codes from memory to f16 numbers (c - 8) * scale, which are exact, into shared memory -- K as [key][d]
+//     and V transposed as [d][key], both the K-major, 128-byte swizzled form, which the cache's word order gives for one
+//     16-byte store a word --, two stages;
+//   1 thread issues S = Q K^T (into one of two buffers of tensor memory) and O = P V (P from tensor memory, in S's place);
+//   8 warps hold the query rows, two threads a row, half of the keys each: maximum, weights, the weights' sum.
+// S of a unit is computed while the weights of the one before it are.  O stays in tensor memory over a CTA's units of an
+// item: the weights are taken relative to a maximum that may lag the true one by 2^kTcLag, and only a larger rise makes
+// the rows' threads scale O (seldom after the first units).
+//
+// Numbers: as in attention.cu, but that O's sums over the units are the tensor core's (binary32, truncated): a chain of
+// 8 additions a unit.  The weights are 2^11 exp(s - M) in f16, 11 bits down to 2^-25 of the reference; where a unit has
+// smaller ones they go into a product of their own, 2^24 higher (kTcLift).  The values' scales are in V here, so a NaN
+// among them would reach tokens that do not see it through 0 * NaN: of the new tokens, whose keys not every query row
+// sees, a NaN in the value's scale becomes one in the key's, which the mask takes out.
+#include <algorithm>
+
+#include "attention.cuh"
+#include "tc.cuh"
+
+namespace switchsd {
+
+constexpr int kTcRows = 128;                // query rows of a tile: the MMA's M
+constexpr int kTcKeys = 128;                // keys of a unit
+constexpr int kRowWarps = 8, kUnpackWarps = 4;
+constexpr int kRowThreads = kRowWarps * kWarp, kUnpackThreads = kUnpackWarps * kWarp;
+constexpr int kTcThreads = kRowThreads + kUnpackThreads + kWarp;
+constexpr int kBlockBytes = 128 * 128;      // 128 rows of one swizzle row: an operand's 64 elements
+constexpr float kTcUp = 11.f;               // log2 of the weight of a score at the reference
+constexpr float kTcLag = 4.f;               // log2 of how far a weight may lie above: 2^15 is f16's
+constexpr float kTcSmall = 6.103515625e-5f; // 2^-14
+constexpr float kTcLift = 16777216.f;       // 2^24
+constexpr int kTcColumns = 512;             // tensor memory: S 2 x 128, O 128, O of the small weights 128
+
+template <int D>
+struct TcSmem {
+    static constexpr int kQ = (D / 64) * kBlockBytes;    // [D / 64][128 rows][128 bytes]
+    static constexpr int kK = (D / 64) * kBlockBytes;    // a stage
+    static constexpr int kV = 2 * D * 128;               // a stage: [2 blocks of 64 keys][D rows][128 bytes]
+    static constexpr int bytes = 1024 + kQ + 2 * (kK + kV);
+};
+
+__device__ __forceinline__ void pair_barrier(int pair) { asm volatile("bar.sync %0, 64;\n" ::"r"(1 + pair) : "memory"); }
+// Whether any of the row warps' threads says so.
+__device__ __forceinline__ bool rows_any(bool v) {
+    uint32_t r;
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.u32 p, %1, 0;\n"
+        "bar.red.or.pred q, 5, 256, p;\n"
+        "selp.u32 %0, 1, 0, q;\n"
+        "}\n"
+        : "=r"(r)
+        : "r"(uint32_t(v))
+        : "memory");
+    return r != 0;
+}
+
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// The segments of a CTA's range: runs of units of one item.
+struct Segment {
+    int b, hk, rt;
+    int32_t len, nw, first, n, units;
+};
+struct Segments {
+    int b;
+    int64_t u, u_end, base;
+    __device__ bool next(const AttnArgs &a, Segment &s) {
+        while (u < u_end) {
+            row_lengths(a, b, s.len, s.nw);
+            s.units = (s.len + s.nw + kTcKeys - 1) / kTcKeys;
+            const int tiles = s.nw ? (s.nw * a.group + kTcRows - 1) / kTcRows : 0;
+            const int64_t all = int64_t(s.units) * tiles * a.Hkv;
+            if (u >= base + all) {
+                base += all;
+                ++b;
+                continue;
+            }
+            const int64_t item = (u - base) / s.units;
+            s.first = int32_t((u - base) - item * s.units);
+            s.b = b;
+            s.hk = int(item / tiles);
+            s.rt = int(item % tiles);
+            s.n = int32_t(min(int64_t(s.units - s.first), u_end - u));
+            u += s.n;
+            return true;
+        }
+        return false;
+    }
+};
+
+template <bool F16, int D>
+__global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a) {
+    using L = Kv4<D>;
+    using S = TcSmem<D>;
+    constexpr int G = L::G;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int64_t s_pre[kTcThreads + 2];
+    __shared__ __align__(8) uint64_t full[2], empty[2], s_full[2], p_full[2], o_full, q_full, stopped;
+    __shared__ uint32_t s_tmem, s_small[2], s_lo;  // s_lo: whether the item's small weights have a product so far
+    __shared__ __align__(16) uint32_t s_valid[2][4];   // of a stage: keys that exist and whose page does
+    __shared__ float s_x[2][kTcRows];                  // what the two threads of a row tell each other
+    __shared__ int s_bad;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int cta = blockIdx.x, ctas = int(gridDim.x);
+    uint8_t *base = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    uint8_t *sm_q = base, *sm_k = base + S::kQ, *sm_v = sm_k + 2 * S::kK;
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&full[i], kUnpackThreads);
+            mbar_init(&empty[i], 1);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], kRowThreads);
+        }
+        mbar_init(&o_full, 1);
+        mbar_init(&q_full, kRowThreads);
+        mbar_init(&stopped, 1);
+        fence_mbar_init();
+        s_bad = 0;
+    }
+    if (warp == kTcThreads / kWarp - 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_addr(&s_tmem)), "r"(kTcColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    pdl_wait();
+    pdl_trigger();
+    Segments seg;
+    deal_units<kTcThreads>(a, kTcRows, kTcKeys, cta, ctas, s_pre, seg.u, seg.u_end, seg.b, seg.base);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    const int page_mask = (1 << a.page_shift) - 1;
+    const size_t head_bytes = size_t(kv4_page_bytes(1 << a.page_shift, D)), page_bytes = head_bytes * a.Hkv;
+    const int val_off = L::values(1 << a.page_shift), sc_off = L::scales(1 << a.page_shift);
+    // Every wait of this thread has ended in time.  After one that has not, no further wait is begun and no result counts;
+    // the row warps still go through their loops, because their barriers want all of them.
+    bool ok = true;
+    Segment s;
+
+    if (warp < kRowWarps) {
+        // ------------------------------------------------------------------------------------------- query rows
+        const int half = warp >> 2, row = 32 * (warp & 3) + lane;
+        const uint32_t lanes = tmem + (uint32_t(32 * (warp & 3)) << 16);
+        const int64_t u_begin = seg.u;
+        uint32_t i = 0;  // units so far
+        for (int64_t u0 = seg.u; seg.next(a, s); u0 = seg.u) {
+            const int rows = min(kTcRows, s.nw * a.group - s.rt * kTcRows);
+            const bool mine = row < rows, warp_mine = 32 * (warp & 3) < rows;
+            const int rr = s.rt * kTcRows + row, t = rr / a.group, h = s.hk * a.group + rr - t * a.group;
+            const int32_t limit = mine ? s.len + t : -1;
+            float scale;  // of a sum of products, for the binary logarithm
+            {
+                // the row's half of the query, scaled by the power of two that brings the row's largest into [2^11, 2^12)
+                const uint16_t *q = a.q + s.b * a.qs[0] + int64_t(t) * a.qs[1] + int64_t(h) * a.qs[2] + half * (D / 2);
+                uint4 raw[D / 16];
+                float big = 0.f;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    raw[k] = mine ? *reinterpret_cast<const uint4 *>(q + 8 * k) : make_uint4(0, 0, 0, 0);
+                    const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) big = fmaxf(big, fmaxf(fabsf(widen1<F16>(uint16_t(w[e]))), fabsf(widen1<F16>(uint16_t(w[e] >> 16)))));
+                }
+                s_x[half][row] = big;
+                pair_barrier(warp & 3);
+                big = fmaxf(big, s_x[half ^ 1][row]);
+                int ex = 11 - (int(__float_as_uint(big) >> 23) - 127);
+                ex = big > 0.f && big < INFINITY ? max(-100, min(100, ex)) : 0;
+                const float up = __int_as_float((127 + ex) << 23);
+                scale = __int_as_float((127 - ex) << 23) * a.scale * 1.4426950408889634f;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+                    uint32_t y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = pack_f16(widen1<F16>(uint16_t(w[e])) * up, widen1<F16>(uint16_t(w[e] >> 16)) * up);
+                    const int d = half * (D / 2) + 8 * k;
+                    *reinterpret_cast<uint4 *>(sm_q + (d / 64) * kBlockBytes + row * 128 + ((((d % 64) / 8) ^ (row & 7)) * 16)) = make_uint4(y[0], y[1], y[2], y[3]);
+                }
+                fence_proxy_async();
+                mbar_arrive(&q_full);
+            }
+            float m = kFloor, l = 0.f;
+            for (int32_t k = 0; k < s.n; ++k, ++i) {
+                const int buf = int(i & 1);
+                const int32_t key0 = (s.first + k) * kTcKeys;
+                ok = ok && mbar_wait(&full[buf], (i >> 1) & 1) && mbar_wait(&s_full[buf], (i >> 1) & 1);
+                tc_fence_after();
+                const uint32_t sa = lanes + buf * 128 + half * 64;  // this thread's scores; its weights take their place
+                const uint4 valid4 = *reinterpret_cast<const uint4 *>(s_valid[buf]);
+                const bool masked = key0 + kTcKeys > s.len + 1 || (valid4.x & valid4.y & valid4.z & valid4.w) != 0xffffffffu;
+                uint32_t see[2] = {0xffffffffu, 0xffffffffu};       // of this thread's keys, those that the row sees
+                if (masked) {
+                    const uint32_t valid[2] = {half ? valid4.z : valid4.x, half ? valid4.w : valid4.y};
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const int32_t ahead = limit - (key0 + half * 64 + w * 32);  // the last visible key's place
+                        see[w] = valid[w] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
+                    }
+                }
+                float mx = kFloor, mn = INFINITY;
+                if (warp_mine) {
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        float v[32];
+                        tmem_ld32(sa + 32 * w, v);
+                        tmem_wait_ld();
+                        if (masked) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const bool in = (see[w] >> e) & 1;
+                                mx = fmaxf(mx, in ? v[e] * scale : kFloor);
+                                mn = fminf(mn, in ? v[e] * scale : INFINITY);
+                            }
+                        } else {
+                            float top = v[0], low = v[0];
+#pragma unroll
+                            for (int e = 1; e < 32; ++e) {
+                                top = fmaxf(top, v[e]);
+                                low = fminf(low, v[e]);
+                            }
+                            mx = fmaxf(mx, fmaxf(top * scale, low * scale));  // the scale may be negative
+                            mn = fminf(mn, fminf(top * scale, low * scale));
+                        }
+                    }
+                }
+                s_x[half][row] = mx;
+                pair_barrier(warp & 3);
+                mx = fmaxf(mx, s_x[half ^ 1][row]);
+                float corr = 1.f;
+                if (mx > m + kTcLag) {
+                    corr = exp2_approx(m - mx);
+                    m = mx;
+                    l *= corr;
+                }
+                const float off = kTcUp - m;
+                const bool any = rows_any(warp_mine && mn + off < -14.f);  // weights below 2^-14
+                if (warp_mine) {
+                    if (k > 0 && __any_sync(kFull, corr != 1.f)) {  // the units' sums so far, to the new reference
+                        ok = ok && mbar_wait(&o_full, (i - 1) & 1);
+                        tc_fence_after();
+                        const bool lo = s_lo != 0;
+#pragma unroll 1
+                        for (int e = 0; e < (lo ? D : D / 2); e += 16) {
+                            const uint32_t at = lanes + (e < D / 2 ? 256 + e : 384 + e - D / 2) + half * (D / 2);
+                            uint32_t w[16];
+                            tmem_ld16(at, w);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(__uint_as_float(w[j]) * corr);
+                            tmem_st16(at, w);
+                        }
+                    }
+                    float sum = 0.f;
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {  // 32 keys: 16 words of weights in the first 16 of their scores' columns
+                        float v[32];
+                        uint32_t y[16];
+                        tmem_ld32(sa + 32 * w, v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = exp2_approx(fmaf(v[e], scale, off));
+                        if (masked) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = (see[w] >> e) & 1 ? v[e] : 0.f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) sum += v[e];
+                        if (any) {  // the small ones in the other 16
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                float &x0 = v[2 * e], &x1 = v[2 * e + 1];
+                                y[e] = pack_f16(x0 < kTcSmall ? x0 * kTcLift : 0.f, x1 < kTcSmall ? x1 * kTcLift : 0.f);
+                                x0 = x0 < kTcSmall ? 0.f : x0;
+                                x1 = x1 < kTcSmall ? 0.f : x1;
+                            }
+                            tmem_st16(sa + 32 * w + 16, y);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+                        tmem_st16(sa + 32 * w, y);
+                    }
+                    l += sum;
+                    tmem_wait_st();
+                }
+                if (tid == 0) {
+                    s_small[buf] = any;
+                    if (k == 0 || any) s_lo = any;  // (the threads that scale O have read it: they wait for the next unit's product)
+                }
+                tc_fence_before();
+                mbar_arrive(&p_full[buf]);
+                // The product of the unit before: every one is waited for in turn (a barrier tells only neighbouring phases
+                // apart).  The next unit's scores come after it anyway.
+                if (k > 0) ok = ok && mbar_wait(&o_full, (i - 1) & 1);
+            }
+            // --- the segment's result ---------------------------------------------------------------------------
+            ok = ok && mbar_wait(&o_full, (i - 1) & 1);
+            tc_fence_after();
+            const bool lo = s_lo != 0;
+            s_x[half][row] = l;
+            pair_barrier(warp & 3);
+            l += s_x[half ^ 1][row];
+            const bool whole = s.first == 0 && s.n == s.units;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const int slot = 2 * cta + (u0 == u_begin ? 0 : 1);
+            float *part = a.part + (size_t(slot) * kTcRows + row) * (D + 4);
+            if (warp_mine) {
+#pragma unroll
+                for (int e = 0; e < D / 2; e += 32) {
+                    float v[32];
+                    const int d = half * (D / 2) + e;
+                    tmem_ld32(lanes + 256 + d, v);
+                    tmem_wait_ld();
+                    if (lo) {
+                        float w[32];
+                        tmem_ld32(lanes + 384 + d, w);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(w[j], 1.f / kTcLift, v[j]);
+                    }
+                    if (mine && whole) {
+                        uint4 *dst = reinterpret_cast<uint4 *>(a.out + ((size_t(s.b) * a.T + t) * a.Hq + h) * D + d);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8)
+                            dst[j / 8] = make_uint4(narrow2<F16>(v[j] * inv, v[j + 1] * inv), narrow2<F16>(v[j + 2] * inv, v[j + 3] * inv),
+                                                    narrow2<F16>(v[j + 4] * inv, v[j + 5] * inv), narrow2<F16>(v[j + 6] * inv, v[j + 7] * inv));
+                    } else if (mine) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4 *>(part + d + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    }
+                }
+            }
+            if (!whole && mine && half == 0) {
+                part[D] = m;
+                part[D + 1] = l;
+                if (row == 0) a.desc[slot] = make_int4(s.b, s.hk, s.rt, (s.first == 0 ? kFirst : 0) | (s.first + s.n == s.units ? kLast : 0));
+            }
+            tc_fence_before();
+            (void)rows_any(false);  // everything of this segment is read before the next one's queries and flags are written
+        }
+    } else if (warp < kRowWarps + kUnpackWarps) {
+        // ------------------------------------------------------------------------------------------- codes to f16
+        const int uw = warp - kRowWarps, r = lane >> 2, c = lane & 3;  // this warp's keys of a unit: 32 uw .. + 31
+        uint32_t i = 0;
+        uint32_t kw[4][2 * G], vw[4][D / 32], sc[4][G];  // of group j of eight keys
+        uint32_t exists = 0;                             // bits of the warp's 32 keys
+        Segments ahead = seg;
+        Segment sa;
+        int32_t ka = 0;          // the next unit to load, of segment sa
+        bool more = ahead.next(a, sa);
+        auto load = [&]() {      // unit ka of segment sa into the registers
+            const int32_t key0 = (sa.first + ka) * kTcKeys + 32 * uw, total = sa.len + sa.nw;
+            const int32_t *table = a.table + size_t(sa.b) * a.blocks;
+            const int32_t at = key0 + 8 * (lane & 3);
+            const int32_t page = at < total ? __ldcg(table + (at >> a.page_shift)) : -1;
+            const bool good = uint32_t(page) < uint32_t(a.pages);
+            exists = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int32_t pg = __shfl_sync(kFull, page, j), first = key0 + 8 * j;
+                if (__shfl_sync(kFull, int(good), j)) {
+                    exists |= (total - first >= 8 ? 0xffu : (1u << (total - first)) - 1u) << (8 * j);
+                    const uint8_t *p = a.cache + size_t(sa.hk) * head_bytes + size_t(pg) * page_bytes;
+                    const int in = (first & page_mask) + r;
+                    if (G == 2) {
+                        const uint4 w = load16(p + in * L::kRow + 16 * c);
+                        kw[j][0] = w.x;
+                        kw[j][1] = w.y;
+                        kw[j][2 * G - 2] = w.z;
+                        kw[j][2 * G - 1] = w.w;
+                        const uint2 x = load8(p + sc_off + in * L::kScales);
+                        sc[j][0] = x.x;
+                        sc[j][G - 1] = x.y;
+                    } else {
+                        const uint2 w = load8(p + in * L::kRow + 8 * c);
+                        kw[j][0] = w.x;
+                        kw[j][1] = w.y;
+                        sc[j][0] = load4(p + sc_off + in * L::kScales);
+                    }
+                    const uint8_t *pv = p + val_off + ((first & page_mask) >> 3) * L::kBlock + 4 * lane;
+#pragma unroll
+                    for (int e = 0; e < D / 32; ++e) vw[j][e] = load4(pv + 128 * e);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2 * G; ++e) kw[j][e] = 0;
+#pragma unroll
+                    for (int e = 0; e < G; ++e) sc[j][e] = 0;
+#pragma unroll
+                    for (int e = 0; e < D / 32; ++e) vw[j][e] = 0;
+                }
+            }
+        };
+        if (more) load();
+        while (more && ok) {
+            const int st = int(i & 1);
+            if (i >= 2) ok = __all_sync(kFull, mbar_wait(&empty[st], ((i >> 1) - 1) & 1));
+            if (!ok) break;
+            // scales of the warp's tokens: zero where the key does not exist, and a NaN in the value's scale of a new token
+            // moved to its key's
+            const int32_t key0 = (sa.first + ka) * kTcKeys + 32 * uw;
+            const bool fresh = key0 + 32 > sa.len + 1;
+            uint8_t *dk = sm_k + st * S::kK, *dv = sm_v + st * S::kV;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t ks[G], vs[G];  // f16, in the low half
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    ks[g] = G == 2 ? (g ? sc[j][0] >> 16 : sc[j][0] & 0xffffu) : sc[j][0] & 0xffffu;
+                    vs[g] = G == 2 ? (g ? sc[j][G - 1] >> 16 : sc[j][G - 1] & 0xffffu) : sc[j][0] >> 16;
+                }
+                if (fresh) {
+                    const int32_t key = key0 + 8 * j + r;
+                    bool nan = false;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) nan |= (vs[g] & 0x7fffu) > 0x7c00u;
+                    const bool gone = !((exists >> (8 * j + r)) & 1);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        if (gone || (nan && key > sa.len)) vs[g] = 0;
+                        if (gone) ks[g] = 0;
+                        else if (nan && key > sa.len) ks[g] = 0x7e00u;
+                    }
+                }
+                const int key = 32 * uw + 8 * j + r;  // of the unit
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const uint32_t k2 = ks[g] | (ks[g] << 16);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t y[4];
+                        signed_codes(kw[j][2 * g + e], y);
+                        *reinterpret_cast<uint4 *>(dk + g * kBlockBytes + key * 128 + (((2 * c + e) ^ (key & 7)) * 16)) =
+                            make_uint4(mul_f16x2(y[0], k2), mul_f16x2(y[1], k2), mul_f16x2(y[2], k2), mul_f16x2(y[3], k2));
+                    }
+                }
+                // the eight tokens' value scales in pairs, of each group
+                uint32_t v2[G][4];
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        v2[g][p] = (__shfl_sync(kFull, vs[g], 8 * p) & 0xffffu) | (__shfl_sync(kFull, vs[g], 8 * p + 4) << 16);
+                const int block = 4 * uw + j;  // of eight keys, of the unit
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) {
+                    const int d = lane + 32 * e;
+                    uint32_t y[4];
+                    signed_codes(vw[j][e], y);
+                    const uint32_t(&w)[4] = v2[e / 2];
+                    *reinterpret_cast<uint4 *>(dv + (block >> 3) * (D * 128) + d * 128 + (((block & 7) ^ (d & 7)) * 16)) =
+                        make_uint4(mul_f16x2(y[0], w[0]), mul_f16x2(y[1], w[1]), mul_f16x2(y[2], w[2]), mul_f16x2(y[3], w[3]));
+                }
+            }
+            if (lane == 0) s_valid[st][uw] = exists;
+            fence_proxy_async();
+            mbar_arrive(&full[st]);
+            ++i;
+            if (++ka == sa.n) {
+                ka = 0;
+                more = ahead.next(a, sa);
+            }
+            if (more) load();
+        }
+    } else if (lane == 0) {
+        // ------------------------------------------------------------------------------------------- the MMAs
+        uint32_t i = 0, nseg = 0;
+        bool fresh = false, lo = false;        // O of the item: nothing added yet, the small weights' product begun
+        auto product = [&](uint32_t j) {       // O += P V of unit j
+            const int buf = int(j & 1);
+            ok = ok && mbar_wait(&p_full[buf], (j >> 1) & 1);
+            if (!ok) return;
+            tc_fence_after();
+            const uint64_t dv = sw128_desc(smem_addr(sm_v + buf * S::kV));
+            // the weights of 32 keys are in 16 columns of their scores' 32, the small ones in the other 16
+            auto keys16 = [&](int k) { return dv + uint64_t(((k >> 2) * (D * 128) + (k & 3) * 32) >> 4); };
+#pragma unroll
+            for (int k = 0; k < kTcKeys / 16; ++k)
+                mma_ts(tmem + 256, tmem + buf * 128 + (k >> 1) * 32 + 8 * (k & 1), keys16(k), f16_idesc(D), !fresh || k != 0);
+            if (s_small[buf]) {
+#pragma unroll
+                for (int k = 0; k < kTcKeys / 16; ++k)
+                    mma_ts(tmem + 384, tmem + buf * 128 + (k >> 1) * 32 + 16 + 8 * (k & 1), keys16(k), f16_idesc(D), lo || k != 0);
+                lo = true;
+            }
+            fresh = false;
+            tc_commit(&empty[buf]);
+            tc_commit(&o_full);
+        };
+        while (ok && seg.next(a, s)) {
+            for (int32_t k = 0; ok && k < s.n; ++k, ++i) {
+                const int buf = int(i & 1);
+                if (k == 0) {
+                    // the rows' threads write the next queries when they have read the last O
+                    if (i > 0) product(i - 1);
+                    ok = ok && mbar_wait(&q_full, nseg & 1);
+                    fresh = true;
+                    lo = false;
+                }
+                ok = ok && mbar_wait(&full[buf], (i >> 1) & 1);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t dq = sw128_desc(smem_addr(sm_q)), dk = sw128_desc(smem_addr(sm_k + buf * S::kK));
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e) {
+                    const uint64_t step = uint64_t(((e >> 2) * kBlockBytes + (e & 3) * 32) >> 4);
+                    mma_ss(tmem + buf * 128, dq + step, dk + step, f16_idesc(kTcKeys), e != 0);
+                }
+                tc_commit(&s_full[buf]);
+                if (k > 0) product(i - 1);
+            }
+            ++nseg;
+        }
+        if (ok && i > 0) product(i - 1);
+        // what is in flight reads shared and tensor memory; the rows' threads have waited for the last product, unless a
+        // wait gave up
+        if (!ok) {
+            tc_commit(&stopped);
+            (void)mbar_wait(&stopped, 0);
+        }
+    }
+    if (!ok) s_bad = 1;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kTcThreads / kWarp - 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kTcColumns) : "memory");
+    if (s_bad && a.status) {
+        // a wait ran out: some rows of this launch are not done; which ones the CTA does not know
+        for (int b = tid; b < a.B; b += kTcThreads) a.status[b] = SWITCHSD_ROW_TIMEOUT;
+    }
+}
+
+size_t attn_tc_workspace(int D) { return size_t(2 * kAttnMaxCtas) * sizeof(int4) + size_t(2 * 256) * kTcRows * (D + 4) * sizeof(float); }
+
+template <bool F16, int D>
+static cudaError_t launch(const AttnArgs &a, int sms, cudaStream_t s) {
+    static bool attr_done[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+        e = cudaFuncSetAttribute(attn_tc_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcSmem<D>::bytes);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_done[dev] = true;
+    }
+    const unsigned ctas = unsigned(std::min(256, sms));
+    // an explicit one-CTA cluster: the MMA commit addresses shared::cluster
+    e = launch_pdl(attn_tc_kernel<F16, D>, dim3(ctas), dim3(kTcThreads), size_t(TcSmem<D>::bytes), s, 1u, a);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(attn_join_kernel<F16, D>, dim3(ctas, 16), dim3(D), 0, s, 0u, a, kTcRows, 1.f);
+}
+
+cudaError_t launch_attn_tc(const AttnArgs &a, bool f16, int D, int sms, cudaStream_t s) {
+    if (f16) return D == 128 ? launch<true, 128>(a, sms, s) : launch<true, 64>(a, sms, s);
+    return D == 128 ? launch<false, 128>(a, sms, s) : launch<false, 64>(a, sms, s);
+}
+
+}  // namespace switchsd

@@ -2,9 +2,10 @@
 //
 // Same work, units (128 keys) and partial results as attention.cu, with tiles of 128 query rows, on tcgen05.  One CTA an
 // SM, with roles for its warps:
-//   4 warps unpack: codes from memory to f16 numbers (c - 8) * scale, which are exact, into shared memory -- K as [key][d]
-//     and V transposed as [d][key], both the K-major, 128-byte swizzled form, which the cache's word order gives for one
-//     16-byte store a word --, two stages;
+//   1 warp fetches: a unit's key codes, value codes and scales, three bulk copies a page, into a ring of three;
+//   4 warps unpack: codes to f16 numbers (c - 8) * scale, which are exact, into shared memory -- K as [key][d] and V
+//     transposed as [d][key], both the K-major, 128-byte swizzled form, which the cache's word order gives for one 16-byte
+//     store a word --, two stages of each, the keys one unit ahead of the values;
 //   1 thread issues S = Q K^T (into one of two buffers of tensor memory) and O = P V (P from tensor memory, in S's place);
 //   8 warps hold the query rows, two threads a row, half of the keys each: maximum, weights, the weights' sum.
 // S of a unit is computed while the weights of the one before it are.  O stays in tensor memory over a CTA's units of an
@@ -27,7 +28,12 @@ constexpr int kTcRows = 128;                // query rows of a tile: the MMA's M
 constexpr int kTcKeys = 128;                // keys of a unit
 constexpr int kRowWarps = 8, kUnpackWarps = 4;
 constexpr int kRowThreads = kRowWarps * kWarp, kUnpackThreads = kUnpackWarps * kWarp;
-constexpr int kTcThreads = kRowThreads + kUnpackThreads + kWarp;
+constexpr int kTcThreads = kRowThreads + kUnpackThreads + 4 * kWarp;  // (two of the last four have no work)
+constexpr int kFetchWarp = kRowWarps + kUnpackWarps, kMmaWarp = kFetchWarp + 1;
+// Registers a thread of each warpgroup: 512 threads are launched with 128 each, and the shares add up to the same.
+constexpr int kRowRegs = 168, kUnpackRegs = 104, kOtherRegs = 72;
+static_assert(2 * kRowRegs + kUnpackRegs + kOtherRegs == 4 * 128, "what one warpgroup gains the others give");
+constexpr int kRing = 3;                    // units of codes on their way
 constexpr int kBlockBytes = 128 * 128;      // 128 rows of one swizzle row: an operand's 64 elements
 constexpr float kTcUp = 11.f;               // log2 of the weight of a score at the reference
 constexpr float kTcLag = 4.f;               // log2 of how far a weight may lie above: 2^15 is f16's
@@ -40,26 +46,16 @@ struct TcSmem {
     static constexpr int kQ = (D / 64) * kBlockBytes;    // [D / 64][128 rows][128 bytes]
     static constexpr int kK = (D / 64) * kBlockBytes;    // a stage
     static constexpr int kV = 2 * D * 128;               // a stage: [2 blocks of 64 keys][D rows][128 bytes]
-    static constexpr int bytes = 1024 + kQ + 2 * (kK + kV);
+    static constexpr int kRawV = kTcKeys * Kv4<D>::kRow;             // codes of a unit: the keys', then
+    static constexpr int kRawS = kRawV + kTcKeys / 8 * Kv4<D>::kBlock;
+    static constexpr int kRaw = kRawS + kTcKeys * Kv4<D>::kScales;
+    static constexpr int bytes = 1024 + kQ + 2 * (kK + kV) + kRing * kRaw;
 };
 
-__device__ __forceinline__ void pair_barrier(int pair) { asm volatile("bar.sync %0, 64;\n" ::"r"(1 + pair) : "memory"); }
-// Whether any of the row warps' threads says so.
-__device__ __forceinline__ bool rows_any(bool v) {
-    uint32_t r;
-    asm volatile(
-        "{\n"
-        ".reg .pred p, q;\n"
-        "setp.ne.u32 p, %1, 0;\n"
-        "bar.red.or.pred q, 5, 256, p;\n"
-        "selp.u32 %0, 1, 0, q;\n"
-        "}\n"
-        : "=r"(r)
-        : "r"(uint32_t(v))
-        : "memory");
-    return r != 0;
-}
+// A wait that gives up after a while (every one here is for this CTA's own work: some microseconds).
+__device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity) { return mbar_wait_polls(bar, parity, 1u << 17); }
 
+__device__ __forceinline__ void pair_barrier(int pair) { asm volatile("bar.sync %0, 64;\n" ::"r"(1 + pair) : "memory"); }
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("mul.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -105,30 +101,39 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
     constexpr int G = L::G;
     extern __shared__ uint8_t smem_raw[];
     __shared__ int64_t s_pre[kTcThreads + 2];
-    __shared__ __align__(8) uint64_t full[2], empty[2], s_full[2], p_full[2], o_full, q_full, stopped;
-    __shared__ uint32_t s_tmem, s_small[2], s_lo;  // s_lo: whether the item's small weights have a product so far
-    __shared__ __align__(16) uint32_t s_valid[2][4];   // of a stage: keys that exist and whose page does
+    __shared__ __align__(8) uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full, q_full, stopped, raw_full[kRing], raw_empty[kRing];
+    __shared__ uint32_t s_tmem;
+    __shared__ uint32_t s_small[2], s_pair[4];         // unit + 1, and segment + 1, that had small weights: of a buffer, of a pair of warps
+    __shared__ __align__(16) uint32_t s_valid[4][4], s_exist[kRing][4];  // of a unit (mod 4, mod 3): keys that exist and whose page does
     __shared__ float s_x[2][kTcRows];                  // what the two threads of a row tell each other
     __shared__ int s_bad;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int cta = blockIdx.x, ctas = int(gridDim.x);
     uint8_t *base = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
-    uint8_t *sm_q = base, *sm_k = base + S::kQ, *sm_v = sm_k + 2 * S::kK;
+    uint8_t *sm_q = base, *sm_k = base + S::kQ, *sm_v = sm_k + 2 * S::kK, *sm_raw = sm_v + 2 * S::kV;
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&full[i], kUnpackThreads);
-            mbar_init(&empty[i], 1);
-            mbar_init(&s_full[i], 1);
+            mbar_init(&k_full[i], kUnpackThreads);
+            mbar_init(&v_full[i], kUnpackThreads);
+            mbar_init(&k_empty[i], 1);
+            mbar_init(&v_empty[i], 1);
+            mbar_init(&s_full[i], 2);  // the scores, and the MMA thread: what it has seen of the unpacking warps
             mbar_init(&p_full[i], kRowThreads);
         }
         mbar_init(&o_full, 1);
         mbar_init(&q_full, kRowThreads);
         mbar_init(&stopped, 1);
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&raw_full[i], 1);
+            mbar_init(&raw_empty[i], kUnpackThreads);
+        }
         fence_mbar_init();
         s_bad = 0;
+        s_small[0] = s_small[1] = 0;
+        s_pair[0] = s_pair[1] = s_pair[2] = s_pair[3] = 0;
     }
-    if (warp == kTcThreads / kWarp - 1) {
+    if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_addr(&s_tmem)), "r"(kTcColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
@@ -149,17 +154,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
     Segment s;
 
     if (warp < kRowWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRowRegs));
         // ------------------------------------------------------------------------------------------- query rows
         const int half = warp >> 2, row = 32 * (warp & 3) + lane;
         const uint32_t lanes = tmem + (uint32_t(32 * (warp & 3)) << 16);
         const int64_t u_begin = seg.u;
-        uint32_t i = 0;  // units so far
+        uint32_t i = 0, nseg = 0;  // units and segments so far
         for (int64_t u0 = seg.u; seg.next(a, s); u0 = seg.u) {
             const int rows = min(kTcRows, s.nw * a.group - s.rt * kTcRows);
             const bool mine = row < rows, warp_mine = 32 * (warp & 3) < rows;
             const int rr = s.rt * kTcRows + row, t = rr / a.group, h = s.hk * a.group + rr - t * a.group;
             const int32_t limit = mine ? s.len + t : -1;
-            float scale;  // of a sum of products, for the binary logarithm
+            float scale;   // of a sum of products, for the binary logarithm
+            float hidden;  // a sum of products whose weight is 0
             {
                 // the row's half of the query, scaled by the power of two that brings the row's largest into [2^11, 2^12)
                 const uint16_t *q = a.q + s.b * a.qs[0] + int64_t(t) * a.qs[1] + int64_t(h) * a.qs[2] + half * (D / 2);
@@ -179,6 +186,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 ex = big > 0.f && big < INFINITY ? max(-100, min(100, ex)) : 0;
                 const float up = __int_as_float((127 + ex) << 23);
                 scale = __int_as_float((127 - ex) << 23) * a.scale * 1.4426950408889634f;
+                if (scale == 0.f) scale = 1e-37f;  // (hidden * 0 would be NaN)
+                hidden = scale < 0.f ? INFINITY : -INFINITY;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
@@ -192,47 +201,46 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 mbar_arrive(&q_full);
             }
             float m = kFloor, l = 0.f;
+            ++nseg;
             for (int32_t k = 0; k < s.n; ++k, ++i) {
                 const int buf = int(i & 1);
                 const int32_t key0 = (s.first + k) * kTcKeys;
-                ok = ok && mbar_wait(&full[buf], (i >> 1) & 1) && mbar_wait(&s_full[buf], (i >> 1) & 1);
+                ok = ok && tc_wait(&s_full[buf], (i >> 1) & 1);
                 tc_fence_after();
                 const uint32_t sa = lanes + buf * 128 + half * 64;  // this thread's scores; its weights take their place
-                const uint4 valid4 = *reinterpret_cast<const uint4 *>(s_valid[buf]);
+                const uint4 valid4 = *reinterpret_cast<const uint4 *>(s_valid[i & 3]);
                 const bool masked = key0 + kTcKeys > s.len + 1 || (valid4.x & valid4.y & valid4.z & valid4.w) != 0xffffffffu;
-                uint32_t see[2] = {0xffffffffu, 0xffffffffu};       // of this thread's keys, those that the row sees
-                if (masked) {
-                    const uint32_t valid[2] = {half ? valid4.z : valid4.x, half ? valid4.w : valid4.y};
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const int32_t ahead = limit - (key0 + half * 64 + w * 32);  // the last visible key's place
-                        see[w] = valid[w] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
-                    }
-                }
-                float mx = kFloor, mn = INFINITY;
+                float v[64], mx = kFloor, mn = INFINITY;
                 if (warp_mine) {
+                    tmem_ld32(sa, v);
+                    tmem_ld32(sa + 32, v + 32);
+                    tmem_wait_ld();
+                    if (masked) {
+                        // the scores to the logarithms' size, and to -inf where the row does not see the key
+                        const uint32_t valid[2] = {half ? valid4.z : valid4.x, half ? valid4.w : valid4.y};
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        float v[32];
-                        tmem_ld32(sa + 32 * w, v);
-                        tmem_wait_ld();
-                        if (masked) {
+                        for (int w = 0; w < 2; ++w) {
+                            const int32_t ahead = limit - (key0 + half * 64 + w * 32);  // the last visible key's place
+                            const uint32_t see = valid[w] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
-                                const bool in = (see[w] >> e) & 1;
-                                mx = fmaxf(mx, in ? v[e] * scale : kFloor);
-                                mn = fminf(mn, in ? v[e] * scale : INFINITY);
+                                float &x = v[32 * w + e];
+                                const bool in = (see >> e) & 1;
+                                mx = fmaxf(mx, in ? x * scale : kFloor);
+                                mn = fminf(mn, in ? x * scale : INFINITY);
+                                x = in ? x : hidden;
                             }
-                        } else {
-                            float top = v[0], low = v[0];
-#pragma unroll
-                            for (int e = 1; e < 32; ++e) {
-                                top = fmaxf(top, v[e]);
-                                low = fminf(low, v[e]);
-                            }
-                            mx = fmaxf(mx, fmaxf(top * scale, low * scale));  // the scale may be negative
-                            mn = fminf(mn, fminf(top * scale, low * scale));
                         }
+                    } else {
+                        float top[2] = {v[0], v[1]}, low[2] = {v[0], v[1]};
+#pragma unroll
+                        for (int e = 2; e < 64; ++e) {
+                            top[e & 1] = fmaxf(top[e & 1], v[e]);
+                            low[e & 1] = fminf(low[e & 1], v[e]);
+                        }
+                        const float t2 = fmaxf(top[0], top[1]) * scale, l2 = fminf(low[0], low[1]) * scale;
+                        mx = fmaxf(mx, fmaxf(t2, l2));  // the scale may be negative
+                        mn = fminf(t2, l2);
                     }
                 }
                 s_x[half][row] = mx;
@@ -245,12 +253,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                     l *= corr;
                 }
                 const float off = kTcUp - m;
-                const bool any = rows_any(warp_mine && mn + off < -14.f);  // weights below 2^-14
+                // The product of the unit before, every one in turn and before this thread's arrival below, without which
+                // the next one does not begin: a barrier tells only neighbouring phases apart.
+                if (k > 0) {
+                    ok = ok && tc_wait(&o_full, (i - 1) & 1);
+                    tc_fence_after();
+                }
                 if (warp_mine) {
                     if (k > 0 && __any_sync(kFull, corr != 1.f)) {  // the units' sums so far, to the new reference
-                        ok = ok && mbar_wait(&o_full, (i - 1) & 1);
-                        tc_fence_after();
-                        const bool lo = s_lo != 0;
+                        const bool lo = s_pair[warp & 3] == nseg;
 #pragma unroll 1
                         for (int e = 0; e < (lo ? D : D / 2); e += 16) {
                             const uint32_t at = lanes + (e < D / 2 ? 256 + e : 384 + e - D / 2) + half * (D / 2);
@@ -262,55 +273,52 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                             tmem_st16(at, w);
                         }
                     }
-                    float sum = 0.f;
+                    // some weight below 2^-14?  Its warp says so; the others' small weights are zeros.
+                    const bool small = __any_sync(kFull, mn + off < -14.f);
+                    if (small && lane == 0) {
+                        s_small[buf] = i + 1;
+                        s_pair[warp & 3] = nseg;  // (read behind the pair's next barrier)
+                    }
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {  // 32 keys: 16 words of weights in the first 16 of their scores' columns
-                        float v[32];
                         uint32_t y[16];
-                        tmem_ld32(sa + 32 * w, v);
-                        tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = exp2_approx(fmaf(v[e], scale, off));
-                        if (masked) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = (see[w] >> e) & 1 ? v[e] : 0.f;
+                        for (int e = 0; e < 32; ++e) {
+                            float &x = v[32 * w + e];
+                            x = exp2_approx(fmaf(x, scale, off));
+                            sum[e & 3] += x;
                         }
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) sum += v[e];
-                        if (any) {  // the small ones in the other 16
+                        if (small) {  // the small ones in the other 16
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
-                                float &x0 = v[2 * e], &x1 = v[2 * e + 1];
+                                float &x0 = v[32 * w + 2 * e], &x1 = v[32 * w + 2 * e + 1];
                                 y[e] = pack_f16(x0 < kTcSmall ? x0 * kTcLift : 0.f, x1 < kTcSmall ? x1 * kTcLift : 0.f);
                                 x0 = x0 < kTcSmall ? 0.f : x0;
                                 x1 = x1 < kTcSmall ? 0.f : x1;
                             }
-                            tmem_st16(sa + 32 * w + 16, y);
-                        }
+                        } else {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+                            for (int e = 0; e < 16; ++e) y[e] = 0;
+                        }
+                        tmem_st16(sa + 32 * w + 16, y);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[32 * w + 2 * e], v[32 * w + 2 * e + 1]);
                         tmem_st16(sa + 32 * w, y);
                     }
-                    l += sum;
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     tmem_wait_st();
-                }
-                if (tid == 0) {
-                    s_small[buf] = any;
-                    if (k == 0 || any) s_lo = any;  // (the threads that scale O have read it: they wait for the next unit's product)
                 }
                 tc_fence_before();
                 mbar_arrive(&p_full[buf]);
-                // The product of the unit before: every one is waited for in turn (a barrier tells only neighbouring phases
-                // apart).  The next unit's scores come after it anyway.
-                if (k > 0) ok = ok && mbar_wait(&o_full, (i - 1) & 1);
             }
             // --- the segment's result ---------------------------------------------------------------------------
-            ok = ok && mbar_wait(&o_full, (i - 1) & 1);
+            ok = ok && tc_wait(&o_full, (i - 1) & 1);
             tc_fence_after();
-            const bool lo = s_lo != 0;
             s_x[half][row] = l;
             pair_barrier(warp & 3);
             l += s_x[half ^ 1][row];
+            const bool lo = s_pair[warp & 3] == nseg;
             const bool whole = s.first == 0 && s.n == s.units;
             const float inv = l == 0.f ? 0.f : 1.f / l;
             const int slot = 2 * cta + (u0 == u_begin ? 0 : 1);
@@ -347,95 +355,71 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 if (row == 0) a.desc[slot] = make_int4(s.b, s.hk, s.rt, (s.first == 0 ? kFirst : 0) | (s.first + s.n == s.units ? kLast : 0));
             }
             tc_fence_before();
-            (void)rows_any(false);  // everything of this segment is read before the next one's queries and flags are written
+            pair_barrier(warp & 3);  // both threads of a row have read s_x
         }
-    } else if (warp < kRowWarps + kUnpackWarps) {
+    } else if (warp < kFetchWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kUnpackRegs));
         // ------------------------------------------------------------------------------------------- codes to f16
         const int uw = warp - kRowWarps, r = lane >> 2, c = lane & 3;  // this warp's keys of a unit: 32 uw .. + 31
-        uint32_t i = 0;
-        uint32_t kw[4][2 * G], vw[4][D / 32], sc[4][G];  // of group j of eight keys
-        uint32_t exists = 0;                             // bits of the warp's 32 keys
-        Segments ahead = seg;
-        Segment sa;
-        int32_t ka = 0;          // the next unit to load, of segment sa
-        bool more = ahead.next(a, sa);
-        auto load = [&]() {      // unit ka of segment sa into the registers
-            const int32_t key0 = (sa.first + ka) * kTcKeys + 32 * uw, total = sa.len + sa.nw;
-            const int32_t *table = a.table + size_t(sa.b) * a.blocks;
-            const int32_t at = key0 + 8 * (lane & 3);
-            const int32_t page = at < total ? __ldcg(table + (at >> a.page_shift)) : -1;
-            const bool good = uint32_t(page) < uint32_t(a.pages);
-            exists = 0;
+        // Scales of the warp's keys of a unit: f16 in the low half, zero where the key does not exist; a NaN in the value's
+        // scale of a new token goes to its key's.
+        auto scales = [&](const uint8_t *raw, int j, uint32_t exists, int32_t key0, int32_t len, uint32_t (&ks)[G], uint32_t (&vs)[G]) {
+            const uint32_t *scale = reinterpret_cast<const uint32_t *>(raw + S::kRawS + (32 * uw + 8 * j + r) * L::kScales);
+            if (G == 2) {
+                const uint2 x = *reinterpret_cast<const uint2 *>(scale);
+                ks[0] = x.x & 0xffffu;
+                ks[G - 1] = x.x >> 16;
+                vs[0] = x.y & 0xffffu;
+                vs[G - 1] = x.y >> 16;
+            } else {
+                const uint32_t x = *scale;
+                ks[0] = x & 0xffffu;
+                vs[0] = x >> 16;
+            }
+            if (exists != 0xffffffffu || key0 + 32 > len + 1) {
+                const bool gone = !((exists >> (8 * j + r)) & 1), fresh = key0 + 8 * j + r > len;
+                bool nan = false;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int32_t pg = __shfl_sync(kFull, page, j), first = key0 + 8 * j;
-                if (__shfl_sync(kFull, int(good), j)) {
-                    exists |= (total - first >= 8 ? 0xffu : (1u << (total - first)) - 1u) << (8 * j);
-                    const uint8_t *p = a.cache + size_t(sa.hk) * head_bytes + size_t(pg) * page_bytes;
-                    const int in = (first & page_mask) + r;
-                    if (G == 2) {
-                        const uint4 w = load16(p + in * L::kRow + 16 * c);
-                        kw[j][0] = w.x;
-                        kw[j][1] = w.y;
-                        kw[j][2 * G - 2] = w.z;
-                        kw[j][2 * G - 1] = w.w;
-                        const uint2 x = load8(p + sc_off + in * L::kScales);
-                        sc[j][0] = x.x;
-                        sc[j][G - 1] = x.y;
-                    } else {
-                        const uint2 w = load8(p + in * L::kRow + 8 * c);
-                        kw[j][0] = w.x;
-                        kw[j][1] = w.y;
-                        sc[j][0] = load4(p + sc_off + in * L::kScales);
-                    }
-                    const uint8_t *pv = p + val_off + ((first & page_mask) >> 3) * L::kBlock + 4 * lane;
+                for (int g = 0; g < G; ++g) nan |= (vs[g] & 0x7fffu) > 0x7c00u;
 #pragma unroll
-                    for (int e = 0; e < D / 32; ++e) vw[j][e] = load4(pv + 128 * e);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 2 * G; ++e) kw[j][e] = 0;
-#pragma unroll
-                    for (int e = 0; e < G; ++e) sc[j][e] = 0;
-#pragma unroll
-                    for (int e = 0; e < D / 32; ++e) vw[j][e] = 0;
+                for (int g = 0; g < G; ++g) {
+                    if (gone || (nan && fresh)) vs[g] = 0;
+                    ks[g] = gone ? 0u : nan && fresh ? 0x7e00u : ks[g];
                 }
             }
         };
-        if (more) load();
-        while (more && ok) {
-            const int st = int(i & 1);
-            if (i >= 2) ok = __all_sync(kFull, mbar_wait(&empty[st], ((i >> 1) - 1) & 1));
-            if (!ok) break;
-            // scales of the warp's tokens: zero where the key does not exist, and a NaN in the value's scale of a new token
-            // moved to its key's
-            const int32_t key0 = (sa.first + ka) * kTcKeys + 32 * uw;
-            const bool fresh = key0 + 32 > sa.len + 1;
-            uint8_t *dk = sm_k + st * S::kK, *dv = sm_v + st * S::kV;
+        auto keys = [&](uint32_t i, int32_t key0, int32_t len) {
+            const int st = int(i & 1), rs = int(i % kRing);
+            bool in_time = tc_wait(&raw_full[rs], (i / kRing) & 1);
+            if (i >= 2) in_time = in_time && tc_wait(&k_empty[st], ((i >> 1) - 1) & 1);
+            ok = __all_sync(kFull, in_time);
+            if (!ok) return;
+            const uint32_t exists = s_exist[rs][uw];
+            const uint8_t *raw = sm_raw + rs * S::kRaw;
+            uint8_t *dk = sm_k + st * S::kK;
+            uint32_t kw[4][2 * G], ks[4][G], vs[G];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                uint32_t ks[G], vs[G];  // f16, in the low half
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    ks[g] = G == 2 ? (g ? sc[j][0] >> 16 : sc[j][0] & 0xffffu) : sc[j][0] & 0xffffu;
-                    vs[g] = G == 2 ? (g ? sc[j][G - 1] >> 16 : sc[j][G - 1] & 0xffffu) : sc[j][0] >> 16;
-                }
-                if (fresh) {
-                    const int32_t key = key0 + 8 * j + r;
-                    bool nan = false;
-#pragma unroll
-                    for (int g = 0; g < G; ++g) nan |= (vs[g] & 0x7fffu) > 0x7c00u;
-                    const bool gone = !((exists >> (8 * j + r)) & 1);
-#pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        if (gone || (nan && key > sa.len)) vs[g] = 0;
-                        if (gone) ks[g] = 0;
-                        else if (nan && key > sa.len) ks[g] = 0x7e00u;
-                    }
-                }
                 const int key = 32 * uw + 8 * j + r;  // of the unit
+                if (G == 2) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(raw + key * L::kRow + 16 * c);
+                    kw[j][0] = w.x;
+                    kw[j][1] = w.y;
+                    kw[j][2 * G - 2] = w.z;
+                    kw[j][2 * G - 1] = w.w;
+                } else {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(raw + key * L::kRow + 8 * c);
+                    kw[j][0] = w.x;
+                    kw[j][1] = w.y;
+                }
+                scales(raw, j, exists, key0, len, ks[j], vs);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = 32 * uw + 8 * j + r;
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    const uint32_t k2 = ks[g] | (ks[g] << 16);
+                    const uint32_t k2 = ks[j][g] | (ks[j][g] << 16);
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         uint32_t y[4];
@@ -444,41 +428,121 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                             make_uint4(mul_f16x2(y[0], k2), mul_f16x2(y[1], k2), mul_f16x2(y[2], k2), mul_f16x2(y[3], k2));
                     }
                 }
+            }
+            if (lane == 0) s_valid[i & 3][uw] = exists;  // (unit i + 4's keys come after unit i's weights)
+            fence_proxy_async();
+            mbar_arrive(&k_full[st]);
+        };
+        auto values = [&](uint32_t i, int32_t key0, int32_t len) {
+            const int st = int(i & 1), rs = int(i % kRing);
+            if (i >= 2) ok = __all_sync(kFull, tc_wait(&v_empty[st], ((i >> 1) - 1) & 1));
+            if (!ok) return;
+            const uint32_t exists = s_exist[rs][uw];
+            const uint8_t *raw = sm_raw + rs * S::kRaw;
+            uint8_t *dv = sm_v + st * S::kV;
+            uint32_t vw[4][D / 32], v2[4][G][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t ks[G], vs[G];
+                scales(raw, j, exists, key0, len, ks, vs);
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) vw[j][e] = *reinterpret_cast<const uint32_t *>(raw + S::kRawV + (4 * uw + j) * L::kBlock + 4 * (lane + 32 * e));
                 // the eight tokens' value scales in pairs, of each group
-                uint32_t v2[G][4];
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
-                        v2[g][p] = (__shfl_sync(kFull, vs[g], 8 * p) & 0xffffu) | (__shfl_sync(kFull, vs[g], 8 * p + 4) << 16);
+                        v2[j][g][p] = (__shfl_sync(kFull, vs[g], 8 * p) & 0xffffu) | (__shfl_sync(kFull, vs[g], 8 * p + 4) << 16);
+            }
+            mbar_arrive(&raw_empty[rs]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
                 const int block = 4 * uw + j;  // of eight keys, of the unit
 #pragma unroll
                 for (int e = 0; e < D / 32; ++e) {
                     const int d = lane + 32 * e;
                     uint32_t y[4];
                     signed_codes(vw[j][e], y);
-                    const uint32_t(&w)[4] = v2[e / 2];
+                    const uint32_t(&w)[4] = v2[j][e / 2];
                     *reinterpret_cast<uint4 *>(dv + (block >> 3) * (D * 128) + d * 128 + (((block & 7) ^ (d & 7)) * 16)) =
                         make_uint4(mul_f16x2(y[0], w[0]), mul_f16x2(y[1], w[1]), mul_f16x2(y[2], w[2]), mul_f16x2(y[3], w[3]));
                 }
             }
-            if (lane == 0) s_valid[st][uw] = exists;
             fence_proxy_async();
-            mbar_arrive(&full[st]);
-            ++i;
-            if (++ka == sa.n) {
-                ka = 0;
-                more = ahead.next(a, sa);
+            mbar_arrive(&v_full[st]);
+        };
+        uint32_t i = 0;                  // units whose keys are done; the values are one behind
+        int32_t last_key0 = 0, last_len = 0;
+        while (ok && seg.next(a, s)) {
+            for (int32_t k = 0; ok && k < s.n; ++k, ++i) {
+                const int32_t key0 = (s.first + k) * kTcKeys + 32 * uw;
+                keys(i, key0, s.len);
+                if (ok && i > 0) values(i - 1, last_key0, last_len);
+                last_key0 = key0;
+                last_len = s.len;
             }
-            if (more) load();
         }
-    } else if (lane == 0) {
+        if (ok && i > 0) values(i - 1, last_key0, last_len);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kOtherRegs));
+        if (warp == kFetchWarp) {
+        // ------------------------------------------------------------------------------------------- fetching
+        // Lane 3 q + p copies part p (key codes, value codes, scales) of the unit's q-th run of keys inside a page.
+        const int run = min(kTcKeys, 1 << a.page_shift), runs = kTcKeys / run;
+        const int q = lane / 3, part = lane - 3 * q;
+        const uint32_t bytes = uint32_t(run) * (part < 2 ? L::kRow : L::kScales);  // (8 tokens' value codes are 8 rows' bytes)
+        const int from = part == 0 ? 0 : part == 1 ? val_off : sc_off, to = part == 0 ? 0 : part == 1 ? S::kRawV : S::kRawS;
+        uint32_t i = 0;
+        int32_t k = 0, page = -1;
+        auto find = [&]() {  // the page of this lane's run in unit k of the segment
+            const int32_t key = (s.first + k) * kTcKeys + q * run;
+            page = q < runs && key < s.len + s.nw ? __ldcg(a.table + size_t(s.b) * a.blocks + (key >> a.page_shift)) : -1;
+        };
+        bool more = seg.next(a, s);
+        if (more) find();
+        while (more) {
+            const int rs = int(i % kRing);
+            if (i >= kRing) ok = __all_sync(kFull, tc_wait(&raw_empty[rs], (i / kRing - 1) & 1));
+            if (!ok) break;
+            const int32_t key0 = (s.first + k) * kTcKeys, total = s.len + s.nw;
+            const bool good = uint32_t(page) < uint32_t(a.pages);
+            const uint32_t goods = __ballot_sync(kFull, good);
+            // the keys that exist: lane w has word w
+            uint32_t word = 0;
+            if (lane < 4) {
+                for (int x = 0; x < 32; x += 16) {  // runs are multiples of 16 keys
+                    const int key = 32 * lane + x;
+                    const int left = total - (key0 + key);
+                    if ((goods >> (3 * (key / run))) & 1) word |= (left >= 16 ? 0xffffu : left > 0 ? (1u << left) - 1u : 0u) << x;
+                }
+                s_exist[rs][lane] = word;
+            }
+            __syncwarp();
+            if (lane == 0) {
+                const int n = __popc(goods & 0x9249249u);  // runs: every third lane
+                mbar_arrive_expect_tx(&raw_full[rs], uint32_t(n * run) * (2 * L::kRow + L::kScales));
+            }
+            __syncwarp();
+            if (good)
+                bulk_g2s(sm_raw + rs * S::kRaw + to + q * bytes,
+                         a.cache + size_t(s.hk) * head_bytes + size_t(page) * page_bytes + from + uint32_t(key0 & page_mask) / run * bytes, bytes, &raw_full[rs]);
+            ++i;
+            if (++k == s.n) {
+                k = 0;
+                more = seg.next(a, s);
+            }
+            if (more) find();
+        }
+        // copies in flight write shared memory: the unpacking warps have waited for all of them, unless a wait gave up
+        if (!ok)
+            for (uint32_t j = i > kRing ? i - kRing : 0; j < i; ++j) (void)tc_wait(&raw_full[j % kRing], (j / kRing) & 1);
+        } else if (warp == kMmaWarp && lane == 0) {
         // ------------------------------------------------------------------------------------------- the MMAs
         uint32_t i = 0, nseg = 0;
         bool fresh = false, lo = false;        // O of the item: nothing added yet, the small weights' product begun
         auto product = [&](uint32_t j) {       // O += P V of unit j
             const int buf = int(j & 1);
-            ok = ok && mbar_wait(&p_full[buf], (j >> 1) & 1);
+            ok = ok && tc_wait(&v_full[buf], (j >> 1) & 1) && tc_wait(&p_full[buf], (j >> 1) & 1);
             if (!ok) return;
             tc_fence_after();
             const uint64_t dv = sw128_desc(smem_addr(sm_v + buf * S::kV));
@@ -487,14 +551,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
 #pragma unroll
             for (int k = 0; k < kTcKeys / 16; ++k)
                 mma_ts(tmem + 256, tmem + buf * 128 + (k >> 1) * 32 + 8 * (k & 1), keys16(k), f16_idesc(D), !fresh || k != 0);
-            if (s_small[buf]) {
+            if (s_small[buf] == j + 1) {
 #pragma unroll
                 for (int k = 0; k < kTcKeys / 16; ++k)
                     mma_ts(tmem + 384, tmem + buf * 128 + (k >> 1) * 32 + 16 + 8 * (k & 1), keys16(k), f16_idesc(D), lo || k != 0);
                 lo = true;
             }
             fresh = false;
-            tc_commit(&empty[buf]);
+            tc_commit(&v_empty[buf]);
             tc_commit(&o_full);
         };
         while (ok && seg.next(a, s)) {
@@ -503,12 +567,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 if (k == 0) {
                     // the rows' threads write the next queries when they have read the last O
                     if (i > 0) product(i - 1);
-                    ok = ok && mbar_wait(&q_full, nseg & 1);
+                    ok = ok && tc_wait(&q_full, nseg & 1);
                     fresh = true;
                     lo = false;
                 }
-                ok = ok && mbar_wait(&full[buf], (i >> 1) & 1);
+                ok = ok && tc_wait(&k_full[buf], (i >> 1) & 1);
                 if (!ok) break;
+                mbar_arrive(&s_full[buf]);
                 tc_fence_after();
                 const uint64_t dq = sw128_desc(smem_addr(sm_q)), dk = sw128_desc(smem_addr(sm_k + buf * S::kK));
 #pragma unroll
@@ -517,6 +582,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                     mma_ss(tmem + buf * 128, dq + step, dk + step, f16_idesc(kTcKeys), e != 0);
                 }
                 tc_commit(&s_full[buf]);
+                tc_commit(&k_empty[buf]);
                 if (k > 0) product(i - 1);
             }
             ++nseg;
@@ -526,14 +592,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
         // wait gave up
         if (!ok) {
             tc_commit(&stopped);
-            (void)mbar_wait(&stopped, 0);
+            (void)tc_wait(&stopped, 0);
+        }
         }
     }
     if (!ok) s_bad = 1;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == kTcThreads / kWarp - 1)
+    if (warp == kMmaWarp)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kTcColumns) : "memory");
     if (s_bad && a.status) {
         // a wait ran out: some rows of this launch are not done; which ones the CTA does not know

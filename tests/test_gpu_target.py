@@ -226,6 +226,22 @@ def test_attention(case, f16):
     _check(_attend(q, cache, table, lens, new, page, f16, scale), want, mag, f16)
 
 
+@pytest.mark.parametrize("Hq,Hkv,T,spread", [(4, 4, 1, 1.0), (12, 4, 3, 1.0), (8, 4, 9, 1.0), (8, 4, 9, 6.0), (20, 4, 33, 1.0)])
+def test_attention_of_many_units_a_cta(Hq, Hkv, T, spread):
+    """Enough keys that a CTA goes over many of an item's units and over several items; with spread queries the running maximum
+    keeps rising by more than the kernel lets its reference lag, and weights get small.  (The spread scores carry up to
+    2^-24 * 128 of their products' size in error: see the next test.)"""
+    rng = np.random.default_rng(T + Hq)
+    B, D, page = 6, 64, 32
+    lens = np.array([9000, 4100, 7777, 130, 8192, 6001])
+    new = np.minimum(np.array([T, max(1, T - 2), T, 1, T, T]), T)
+    cache, table, ks, vs = _cache_of(rng, B, Hkv, D, page, lens, new, 300)
+    q = ref.bf16_round(rng.standard_normal((B, T, Hq, D)) * 0.7 * spread)
+    want, mag = ref.attention(q, ks, vs, lens, new, 0.125)
+    big = np.abs(q).sum(-1).max() * max(np.abs(k).max() for k in ks) * 0.125
+    _check(_attend(q, cache, table, lens, new, page, False, 0.125), want, mag * (1 + 2 ** 10 * big * 2.0 ** -23 * (spread > 1)), False)
+
+
 def test_attention_shifted_lengths_strides_and_status():
     """Lengths with lens_add and new_add, queries as a view of a fused projection, and rows with bad lengths among good ones."""
     import torch

@@ -3,9 +3,9 @@
 // Same work, units (128 keys) and partial results as attention.cu, with tiles of 128 query rows, on tcgen05.  One CTA an
 // SM, with roles for its warps:
 //   1 warp fetches: a unit's key codes, value codes and scales, three bulk copies a page, into a ring of three;
-//   4 warps unpack: codes to f16 numbers (c - 8) * scale, which are exact, into shared memory -- K as [key][d] and V
-//     transposed as [d][key], both the K-major, 128-byte swizzled form, which the cache's word order gives for one 16-byte
-//     store a word --, two stages of each, the keys one unit ahead of the values;
+//   4 warps unpack the keys and 4 the values: codes to f16 numbers (c - 8) * scale, which are exact, into shared memory -- K
+//     as [key][d] and V transposed as [d][key], both the K-major, 128-byte swizzled form, which the cache's word order gives
+//     for one 16-byte store a word --, two stages of each;
 //   1 thread issues S = Q K^T (into one of two buffers of tensor memory) and O = P V (P from tensor memory, in S's place);
 //   8 warps hold the query rows, two threads a row, half of the keys each: maximum, weights, the weights' sum.
 // S of a unit is computed while the weights of the one before it are.  O stays in tensor memory over a CTA's units of an
@@ -26,13 +26,15 @@ namespace switchsd {
 
 constexpr int kTcRows = 128;                // query rows of a tile: the MMA's M
 constexpr int kTcKeys = 128;                // keys of a unit
-constexpr int kRowWarps = 8, kUnpackWarps = 4;
+constexpr int kSplit = 2;                   // threads of a row
+constexpr int kRowWarps = 4 * kSplit, kUnpackWarps = 4;  // (of each: keys, values)
 constexpr int kRowThreads = kRowWarps * kWarp, kUnpackThreads = kUnpackWarps * kWarp;
-constexpr int kTcThreads = kRowThreads + kUnpackThreads + 4 * kWarp;  // (two of the last four have no work)
-constexpr int kFetchWarp = kRowWarps + kUnpackWarps, kMmaWarp = kFetchWarp + 1;
-// Registers a thread of each warpgroup: 512 threads are launched with 128 each, and the shares add up to the same.
-constexpr int kRowRegs = 168, kUnpackRegs = 104, kOtherRegs = 72;
-static_assert(2 * kRowRegs + kUnpackRegs + kOtherRegs == 4 * 128, "what one warpgroup gains the others give");
+constexpr int kTcThreads = kRowThreads + 2 * kUnpackThreads + 4 * kWarp;  // (two of the last four warps have no work)
+constexpr int kValueWarp = kRowWarps + kUnpackWarps, kFetchWarp = kValueWarp + kUnpackWarps, kMmaWarp = kFetchWarp + 1;
+// Registers a thread of each warpgroup: 640 threads are launched with 96 each, and the shares add up to the same.  (Local
+// memory would cost much: little of the L1 is left beside the shared memory.)
+constexpr int kRowRegs = 120, kUnpackRegs = 80, kOtherRegs = 80;
+static_assert(2 * kRowRegs + 2 * kUnpackRegs + kOtherRegs == 5 * 96, "what one warpgroup gains the others give");
 constexpr int kRing = 3;                    // units of codes on their way
 constexpr int kBlockBytes = 128 * 128;      // 128 rows of one swizzle row: an operand's 64 elements
 constexpr float kTcUp = 11.f;               // log2 of the weight of a score at the reference
@@ -55,7 +57,14 @@ struct TcSmem {
 // A wait that gives up after a while (every one here is for this CTA's own work: some microseconds).
 __device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity) { return mbar_wait_polls(bar, parity, 1u << 17); }
 
-__device__ __forceinline__ void pair_barrier(int pair) { asm volatile("bar.sync %0, 64;\n" ::"r"(1 + pair) : "memory"); }
+// The warps of 32 rows.
+__device__ __forceinline__ void rows_barrier(int quarter) { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + quarter), "n"(kSplit * kWarp) : "memory"); }
+// One arrival for a warp, behind all of its threads' work (and their fences).
+__device__ __forceinline__ void warp_arrive(uint64_t *bar) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
+
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("mul.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -103,9 +112,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
     __shared__ int64_t s_pre[kTcThreads + 2];
     __shared__ __align__(8) uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full, q_full, stopped, raw_full[kRing], raw_empty[kRing];
     __shared__ uint32_t s_tmem;
-    __shared__ uint32_t s_small[2], s_pair[4];         // unit + 1, and segment + 1, that had small weights: of a buffer, of a pair of warps
+    __shared__ uint32_t s_small[2], s_rows[4];         // unit + 1, and segment + 1, that had small weights: of a buffer, of 32 rows
     __shared__ __align__(16) uint32_t s_valid[4][4], s_exist[kRing][4];  // of a unit (mod 4, mod 3): keys that exist and whose page does
-    __shared__ float s_x[2][kTcRows];                  // what the two threads of a row tell each other
+    __shared__ float s_x[kSplit][kTcRows];             // what the threads of a row tell each other
     __shared__ int s_bad;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int cta = blockIdx.x, ctas = int(gridDim.x);
@@ -114,24 +123,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&k_full[i], kUnpackThreads);
-            mbar_init(&v_full[i], kUnpackThreads);
+            mbar_init(&k_full[i], kUnpackWarps);
+            mbar_init(&v_full[i], kUnpackWarps);
             mbar_init(&k_empty[i], 1);
             mbar_init(&v_empty[i], 1);
             mbar_init(&s_full[i], 2);  // the scores, and the MMA thread: what it has seen of the unpacking warps
-            mbar_init(&p_full[i], kRowThreads);
+            mbar_init(&p_full[i], kRowWarps);
         }
         mbar_init(&o_full, 1);
-        mbar_init(&q_full, kRowThreads);
+        mbar_init(&q_full, kRowWarps);
         mbar_init(&stopped, 1);
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&raw_full[i], 1);
-            mbar_init(&raw_empty[i], kUnpackThreads);
+            mbar_init(&raw_empty[i], 2 * kUnpackWarps);
         }
         fence_mbar_init();
         s_bad = 0;
         s_small[0] = s_small[1] = 0;
-        s_pair[0] = s_pair[1] = s_pair[2] = s_pair[3] = 0;
+        s_rows[0] = s_rows[1] = s_rows[2] = s_rows[3] = 0;
     }
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_addr(&s_tmem)), "r"(kTcColumns) : "memory");
@@ -156,32 +165,40 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
     if (warp < kRowWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRowRegs));
         // ------------------------------------------------------------------------------------------- query rows
-        const int half = warp >> 2, row = 32 * (warp & 3) + lane;
-        const uint32_t lanes = tmem + (uint32_t(32 * (warp & 3)) << 16);
+        const int part = warp >> 2, quarter = warp & 3, row = 32 * quarter + lane;
+        constexpr int KT = kTcKeys / kSplit, DT = D / kSplit;  // a thread's keys of a unit, and dimensions
+        static_assert(KT % 32 == 0 && DT % 16 == 0, "whole words of keys, whole loads of dimensions");
+        const uint32_t lanes = tmem + (uint32_t(32 * quarter) << 16);
         const int64_t u_begin = seg.u;
         uint32_t i = 0, nseg = 0;  // units and segments so far
+        auto of_row = [&](auto op) {  // over what the row's threads have put down
+            float x = s_x[0][row];
+#pragma unroll
+            for (int p = 1; p < kSplit; ++p) x = op(x, s_x[p][row]);
+            return x;
+        };
         for (int64_t u0 = seg.u; seg.next(a, s); u0 = seg.u) {
             const int rows = min(kTcRows, s.nw * a.group - s.rt * kTcRows);
-            const bool mine = row < rows, warp_mine = 32 * (warp & 3) < rows;
+            const bool mine = row < rows, warp_mine = 32 * quarter < rows;
             const int rr = s.rt * kTcRows + row, t = rr / a.group, h = s.hk * a.group + rr - t * a.group;
             const int32_t limit = mine ? s.len + t : -1;
             float scale;   // of a sum of products, for the binary logarithm
             float hidden;  // a sum of products whose weight is 0
             {
-                // the row's half of the query, scaled by the power of two that brings the row's largest into [2^11, 2^12)
-                const uint16_t *q = a.q + s.b * a.qs[0] + int64_t(t) * a.qs[1] + int64_t(h) * a.qs[2] + half * (D / 2);
-                uint4 raw[D / 16];
+                // the thread's part of the query, scaled by the power of two that brings the row's largest into [2^11, 2^12)
+                const uint16_t *q = a.q + s.b * a.qs[0] + int64_t(t) * a.qs[1] + int64_t(h) * a.qs[2] + part * DT;
+                uint4 raw[DT / 8];
                 float big = 0.f;
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
+                for (int k = 0; k < DT / 8; ++k) {
                     raw[k] = mine ? *reinterpret_cast<const uint4 *>(q + 8 * k) : make_uint4(0, 0, 0, 0);
                     const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) big = fmaxf(big, fmaxf(fabsf(widen1<F16>(uint16_t(w[e]))), fabsf(widen1<F16>(uint16_t(w[e] >> 16)))));
                 }
-                s_x[half][row] = big;
-                pair_barrier(warp & 3);
-                big = fmaxf(big, s_x[half ^ 1][row]);
+                s_x[part][row] = big;
+                rows_barrier(quarter);
+                big = of_row([](float x, float y) { return fmaxf(x, y); });
                 int ex = 11 - (int(__float_as_uint(big) >> 23) - 127);
                 ex = big > 0.f && big < INFINITY ? max(-100, min(100, ex)) : 0;
                 const float up = __int_as_float((127 + ex) << 23);
@@ -189,16 +206,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 if (scale == 0.f) scale = 1e-37f;  // (hidden * 0 would be NaN)
                 hidden = scale < 0.f ? INFINITY : -INFINITY;
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
+                for (int k = 0; k < DT / 8; ++k) {
                     const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
                     uint32_t y[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[e] = pack_f16(widen1<F16>(uint16_t(w[e])) * up, widen1<F16>(uint16_t(w[e] >> 16)) * up);
-                    const int d = half * (D / 2) + 8 * k;
+                    const int d = part * DT + 8 * k;
                     *reinterpret_cast<uint4 *>(sm_q + (d / 64) * kBlockBytes + row * 128 + ((((d % 64) / 8) ^ (row & 7)) * 16)) = make_uint4(y[0], y[1], y[2], y[3]);
                 }
                 fence_proxy_async();
-                mbar_arrive(&q_full);
+                warp_arrive(&q_full);
             }
             float m = kFloor, l = 0.f;
             ++nseg;
@@ -207,45 +224,44 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 const int32_t key0 = (s.first + k) * kTcKeys;
                 ok = ok && tc_wait(&s_full[buf], (i >> 1) & 1);
                 tc_fence_after();
-                const uint32_t sa = lanes + buf * 128 + half * 64;  // this thread's scores; its weights take their place
+                const uint32_t sa = lanes + buf * 128 + part * KT;  // this thread's scores; its weights take their place
                 const uint4 valid4 = *reinterpret_cast<const uint4 *>(s_valid[i & 3]);
                 const bool masked = key0 + kTcKeys > s.len + 1 || (valid4.x & valid4.y & valid4.z & valid4.w) != 0xffffffffu;
-                float v[64], mx = kFloor, mn = INFINITY;
+                float top = -INFINITY, low = INFINITY;
                 if (warp_mine) {
-                    tmem_ld32(sa, v);
-                    tmem_ld32(sa + 32, v + 32);
-                    tmem_wait_ld();
-                    if (masked) {
-                        // the scores to the logarithms' size, and to -inf where the row does not see the key
-                        const uint32_t valid[2] = {half ? valid4.z : valid4.x, half ? valid4.w : valid4.y};
-#pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            const int32_t ahead = limit - (key0 + half * 64 + w * 32);  // the last visible key's place
-                            const uint32_t see = valid[w] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
+#pragma unroll 1
+                    for (int w = 0; w < KT / 32; ++w) {  // (a loop: the roles' code has to fit the instruction cache together)
+                        float v[32];
+                        tmem_ld32(sa + 32 * w, v);
+                        tmem_wait_ld();
+                        if (masked) {  // `hidden` in the place of the scores that the row does not see
+                            const int place = part * KT + 32 * w;
+                            const int32_t ahead = limit - (key0 + place);  // the last visible key's place
+                            const uint32_t see = s_valid[i & 3][place / 32] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
+                            uint32_t y[16];
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
-                                float &x = v[32 * w + e];
-                                const bool in = (see >> e) & 1;
-                                mx = fmaxf(mx, in ? x * scale : kFloor);
-                                mn = fminf(mn, in ? x * scale : INFINITY);
-                                x = in ? x : hidden;
+                                v[e] = (see >> e) & 1 ? v[e] : hidden;
+                                y[e & 15] = __float_as_uint(v[e]);
+                                if ((e & 15) == 15) tmem_st16(sa + 32 * w + (e & 16), y);
                             }
                         }
-                    } else {
-                        float top[2] = {v[0], v[1]}, low[2] = {v[0], v[1]};
+                        float t2[2] = {-INFINITY, -INFINITY}, l2[2] = {INFINITY, INFINITY};
 #pragma unroll
-                        for (int e = 2; e < 64; ++e) {
-                            top[e & 1] = fmaxf(top[e & 1], v[e]);
-                            low[e & 1] = fminf(low[e & 1], v[e]);
+                        for (int e = 0; e < 32; ++e) {
+                            t2[e & 1] = fmaxf(t2[e & 1], v[e]);
+                            l2[e & 1] = fminf(l2[e & 1], v[e]);
                         }
-                        const float t2 = fmaxf(top[0], top[1]) * scale, l2 = fminf(low[0], low[1]) * scale;
-                        mx = fmaxf(mx, fmaxf(t2, l2));  // the scale may be negative
-                        mn = fminf(t2, l2);
+                        top = fmaxf(top, fmaxf(t2[0], t2[1]));
+                        low = fminf(low, fminf(l2[0], l2[1]));
                     }
+                    if (masked) tmem_wait_st();
                 }
-                s_x[half][row] = mx;
-                pair_barrier(warp & 3);
-                mx = fmaxf(mx, s_x[half ^ 1][row]);
+                // the scale may be negative; a row that sees nothing has infinities
+                const float mn = fminf(top * scale, low * scale);
+                s_x[part][row] = fmaxf(kFloor, fmaxf(top * scale, low * scale));
+                rows_barrier(quarter);
+                const float mx = of_row([](float x, float y) { return fmaxf(x, y); });
                 float corr = 1.f;
                 if (mx > m + kTcLag) {
                     corr = exp2_approx(m - mx);
@@ -253,18 +269,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                     l *= corr;
                 }
                 const float off = kTcUp - m;
-                // The product of the unit before, every one in turn and before this thread's arrival below, without which
-                // the next one does not begin: a barrier tells only neighbouring phases apart.
-                if (k > 0) {
-                    ok = ok && tc_wait(&o_full, (i - 1) & 1);
-                    tc_fence_after();
-                }
                 if (warp_mine) {
                     if (k > 0 && __any_sync(kFull, corr != 1.f)) {  // the units' sums so far, to the new reference
-                        const bool lo = s_pair[warp & 3] == nseg;
+                        ok = ok && tc_wait(&o_full, (i - 1) & 1);
+                        tc_fence_after();
+                        const bool lo = s_rows[quarter] == nseg;
 #pragma unroll 1
-                        for (int e = 0; e < (lo ? D : D / 2); e += 16) {
-                            const uint32_t at = lanes + (e < D / 2 ? 256 + e : 384 + e - D / 2) + half * (D / 2);
+                        for (int e = 0; e < (lo ? 2 * DT : DT); e += 16) {
+                            const uint32_t at = lanes + (e < DT ? 256 + e : 384 + e - DT) + part * DT;
                             uint32_t w[16];
                             tmem_ld16(at, w);
                             tmem_wait_ld();
@@ -273,94 +285,100 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                             tmem_st16(at, w);
                         }
                     }
-                    // some weight below 2^-14?  Its warp says so; the others' small weights are zeros.
+                    // Some weight below 2^-14?  Its warp says so, and what rounding to f16 leaves of such weights goes into the
+                    // other 16 columns of 32 keys; else zeros do, for another warp's sake.
                     const bool small = __any_sync(kFull, mn + off < -14.f);
                     if (small && lane == 0) {
                         s_small[buf] = i + 1;
-                        s_pair[warp & 3] = nseg;  // (read behind the pair's next barrier)
+                        s_rows[quarter] = nseg;  // (read behind the rows' next barrier)
                     }
                     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {  // 32 keys: 16 words of weights in the first 16 of their scores' columns
+#pragma unroll 1
+                    for (int w = 0; w < KT / 32; ++w) {  // 32 keys: 16 words of weights in the first 16 of their scores' columns
+                        float v[32];
                         uint32_t y[16];
+                        tmem_ld32(sa + 32 * w, v);
+                        tmem_wait_ld();
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
-                            float &x = v[32 * w + e];
-                            x = exp2_approx(fmaf(x, scale, off));
-                            sum[e & 3] += x;
+                            v[e] = exp2_approx(fmaf(v[e], scale, off));
+                            sum[e & 3] += v[e];
                         }
-                        if (small) {  // the small ones in the other 16
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                float &x0 = v[32 * w + 2 * e], &x1 = v[32 * w + 2 * e + 1];
-                                y[e] = pack_f16(x0 < kTcSmall ? x0 * kTcLift : 0.f, x1 < kTcSmall ? x1 * kTcLift : 0.f);
-                                x0 = x0 < kTcSmall ? 0.f : x0;
-                                x1 = x1 < kTcSmall ? 0.f : x1;
-                            }
+                        for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+                        tmem_st16(sa + 32 * w, y);
+                        if (small) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = v[e] < kTcSmall ? (v[e] - __half2float(__float2half_rn(v[e]))) * kTcLift : 0.f;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
                         } else {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) y[e] = 0;
                         }
                         tmem_st16(sa + 32 * w + 16, y);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[32 * w + 2 * e], v[32 * w + 2 * e + 1]);
-                        tmem_st16(sa + 32 * w, y);
                     }
                     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     tmem_wait_st();
                 }
+                // The product of the unit before, every one in turn and before this warp's arrival, without which the next one
+                // does not begin: a barrier tells only neighbouring phases apart.
+                if (k > 0) ok = ok && tc_wait(&o_full, (i - 1) & 1);
                 tc_fence_before();
-                mbar_arrive(&p_full[buf]);
+                warp_arrive(&p_full[buf]);
             }
             // --- the segment's result ---------------------------------------------------------------------------
+            s_x[part][row] = l;
+            rows_barrier(quarter);
+            l = of_row([](float x, float y) { return x + y; });
             ok = ok && tc_wait(&o_full, (i - 1) & 1);
             tc_fence_after();
-            s_x[half][row] = l;
-            pair_barrier(warp & 3);
-            l += s_x[half ^ 1][row];
-            const bool lo = s_pair[warp & 3] == nseg;
+            const bool lo = s_rows[quarter] == nseg;
             const bool whole = s.first == 0 && s.n == s.units;
             const float inv = l == 0.f ? 0.f : 1.f / l;
             const int slot = 2 * cta + (u0 == u_begin ? 0 : 1);
-            float *part = a.part + (size_t(slot) * kTcRows + row) * (D + 4);
+            float *partial = a.part + (size_t(slot) * kTcRows + row) * (D + 4);
             if (warp_mine) {
-#pragma unroll
-                for (int e = 0; e < D / 2; e += 32) {
-                    float v[32];
-                    const int d = half * (D / 2) + e;
-                    tmem_ld32(lanes + 256 + d, v);
+#pragma unroll 1
+                for (int e = 0; e < DT; e += 16) {
+                    float v[16];
+                    uint32_t w[16];
+                    const int d = part * DT + e;
+                    tmem_ld16(lanes + 256 + d, w);
                     tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(w[j]);
                     if (lo) {
-                        float w[32];
-                        tmem_ld32(lanes + 384 + d, w);
+                        tmem_ld16(lanes + 384 + d, w);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(w[j], 1.f / kTcLift, v[j]);
+                        for (int j = 0; j < 16; ++j) v[j] = fmaf(__uint_as_float(w[j]), 1.f / kTcLift, v[j]);
                     }
                     if (mine && whole) {
                         uint4 *dst = reinterpret_cast<uint4 *>(a.out + ((size_t(s.b) * a.T + t) * a.Hq + h) * D + d);
 #pragma unroll
-                        for (int j = 0; j < 32; j += 8)
+                        for (int j = 0; j < 16; j += 8)
                             dst[j / 8] = make_uint4(narrow2<F16>(v[j] * inv, v[j + 1] * inv), narrow2<F16>(v[j + 2] * inv, v[j + 3] * inv),
                                                     narrow2<F16>(v[j + 4] * inv, v[j + 5] * inv), narrow2<F16>(v[j + 6] * inv, v[j + 7] * inv));
                     } else if (mine) {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4 *>(part + d + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4 *>(partial + d + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                     }
                 }
             }
-            if (!whole && mine && half == 0) {
-                part[D] = m;
-                part[D + 1] = l;
+            if (!whole && mine && part == 0) {
+                partial[D] = m;
+                partial[D + 1] = l;
                 if (row == 0) a.desc[slot] = make_int4(s.b, s.hk, s.rt, (s.first == 0 ? kFirst : 0) | (s.first + s.n == s.units ? kLast : 0));
             }
             tc_fence_before();
-            pair_barrier(warp & 3);  // both threads of a row have read s_x
+            rows_barrier(quarter);  // all threads of a row have read s_x
         }
     } else if (warp < kFetchWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kUnpackRegs));
         // ------------------------------------------------------------------------------------------- codes to f16
-        const int uw = warp - kRowWarps, r = lane >> 2, c = lane & 3;  // this warp's keys of a unit: 32 uw .. + 31
+        const bool of_keys = warp < kValueWarp;
+        const int uw = warp & (kUnpackWarps - 1), r = lane >> 2, c = lane & 3;  // this warp's keys of a unit: 32 uw .. + 31
         // Scales of the warp's keys of a unit: f16 in the low half, zero where the key does not exist; a NaN in the value's
         // scale of a new token goes to its key's.
         auto scales = [&](const uint8_t *raw, int j, uint32_t exists, int32_t key0, int32_t len, uint32_t (&ks)[G], uint32_t (&vs)[G]) {
@@ -397,92 +415,89 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             const uint32_t exists = s_exist[rs][uw];
             const uint8_t *raw = sm_raw + rs * S::kRaw;
             uint8_t *dk = sm_k + st * S::kK;
-            uint32_t kw[4][2 * G], ks[4][G], vs[G];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
+#pragma unroll 1
+            for (int j = 0; j < 4; ++j) {  // (a loop: the roles' code has to fit the instruction cache together)
                 const int key = 32 * uw + 8 * j + r;  // of the unit
+                uint32_t kw[2 * G], ks[G], vs[G];
                 if (G == 2) {
                     const uint4 w = *reinterpret_cast<const uint4 *>(raw + key * L::kRow + 16 * c);
-                    kw[j][0] = w.x;
-                    kw[j][1] = w.y;
-                    kw[j][2 * G - 2] = w.z;
-                    kw[j][2 * G - 1] = w.w;
+                    kw[0] = w.x;
+                    kw[1] = w.y;
+                    kw[2 * G - 2] = w.z;
+                    kw[2 * G - 1] = w.w;
                 } else {
                     const uint2 w = *reinterpret_cast<const uint2 *>(raw + key * L::kRow + 8 * c);
-                    kw[j][0] = w.x;
-                    kw[j][1] = w.y;
+                    kw[0] = w.x;
+                    kw[1] = w.y;
                 }
-                scales(raw, j, exists, key0, len, ks[j], vs);
-            }
+                scales(raw, j, exists, key0, len, ks, vs);
+                uint4 y4[2 * G];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int key = 32 * uw + 8 * j + r;
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const uint32_t k2 = ks[j][g] | (ks[j][g] << 16);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        uint32_t y[4];
-                        signed_codes(kw[j][2 * g + e], y);
-                        *reinterpret_cast<uint4 *>(dk + g * kBlockBytes + key * 128 + (((2 * c + e) ^ (key & 7)) * 16)) =
-                            make_uint4(mul_f16x2(y[0], k2), mul_f16x2(y[1], k2), mul_f16x2(y[2], k2), mul_f16x2(y[3], k2));
-                    }
+                for (int e = 0; e < 2 * G; ++e) {
+                    const uint32_t k2 = ks[e >> 1] | (ks[e >> 1] << 16);
+                    uint32_t y[4];
+                    signed_codes(kw[e], y);
+                    y4[e] = make_uint4(mul_f16x2(y[0], k2), mul_f16x2(y[1], k2), mul_f16x2(y[2], k2), mul_f16x2(y[3], k2));
                 }
+#pragma unroll
+                for (int e = 0; e < 2 * G; ++e)
+                    *reinterpret_cast<uint4 *>(dk + (e >> 1) * kBlockBytes + key * 128 + (((2 * c + (e & 1)) ^ (key & 7)) * 16)) = y4[e];
             }
+            warp_arrive(&raw_empty[rs]);
             if (lane == 0) s_valid[i & 3][uw] = exists;  // (unit i + 4's keys come after unit i's weights)
             fence_proxy_async();
-            mbar_arrive(&k_full[st]);
+            warp_arrive(&k_full[st]);
         };
         auto values = [&](uint32_t i, int32_t key0, int32_t len) {
             const int st = int(i & 1), rs = int(i % kRing);
-            if (i >= 2) ok = __all_sync(kFull, tc_wait(&v_empty[st], ((i >> 1) - 1) & 1));
+            bool in_time = tc_wait(&raw_full[rs], (i / kRing) & 1);
+            if (i >= 2) in_time = in_time && tc_wait(&v_empty[st], ((i >> 1) - 1) & 1);
+            ok = __all_sync(kFull, in_time);
             if (!ok) return;
             const uint32_t exists = s_exist[rs][uw];
             const uint8_t *raw = sm_raw + rs * S::kRaw;
             uint8_t *dv = sm_v + st * S::kV;
-            uint32_t vw[4][D / 32], v2[4][G][4];
-#pragma unroll
+#pragma unroll 1
             for (int j = 0; j < 4; ++j) {
-                uint32_t ks[G], vs[G];
-                scales(raw, j, exists, key0, len, ks, vs);
+                const int block = 4 * uw + j;  // of eight keys, of the unit
+                uint32_t ks[G], vs[G], vw[D / 32], v2[G][4];
 #pragma unroll
-                for (int e = 0; e < D / 32; ++e) vw[j][e] = *reinterpret_cast<const uint32_t *>(raw + S::kRawV + (4 * uw + j) * L::kBlock + 4 * (lane + 32 * e));
+                for (int e = 0; e < D / 32; ++e) vw[e] = *reinterpret_cast<const uint32_t *>(raw + S::kRawV + block * L::kBlock + 4 * (lane + 32 * e));
+                scales(raw, j, exists, key0, len, ks, vs);
                 // the eight tokens' value scales in pairs, of each group
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
-                        v2[j][g][p] = (__shfl_sync(kFull, vs[g], 8 * p) & 0xffffu) | (__shfl_sync(kFull, vs[g], 8 * p + 4) << 16);
-            }
-            mbar_arrive(&raw_empty[rs]);
+                        v2[g][p] = (__shfl_sync(kFull, vs[g], 8 * p) & 0xffffu) | (__shfl_sync(kFull, vs[g], 8 * p + 4) << 16);
+                uint4 y4[D / 32];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int block = 4 * uw + j;  // of eight keys, of the unit
+                for (int e = 0; e < D / 32; ++e) {
+                    uint32_t y[4];
+                    signed_codes(vw[e], y);
+                    const uint32_t(&w)[4] = v2[e / 2];
+                    y4[e] = make_uint4(mul_f16x2(y[0], w[0]), mul_f16x2(y[1], w[1]), mul_f16x2(y[2], w[2]), mul_f16x2(y[3], w[3]));
+                }
 #pragma unroll
                 for (int e = 0; e < D / 32; ++e) {
                     const int d = lane + 32 * e;
-                    uint32_t y[4];
-                    signed_codes(vw[j][e], y);
-                    const uint32_t(&w)[4] = v2[j][e / 2];
-                    *reinterpret_cast<uint4 *>(dv + (block >> 3) * (D * 128) + d * 128 + (((block & 7) ^ (d & 7)) * 16)) =
-                        make_uint4(mul_f16x2(y[0], w[0]), mul_f16x2(y[1], w[1]), mul_f16x2(y[2], w[2]), mul_f16x2(y[3], w[3]));
+                    *reinterpret_cast<uint4 *>(dv + (block >> 3) * (D * 128) + d * 128 + (((block & 7) ^ (d & 7)) * 16)) = y4[e];
                 }
             }
+            warp_arrive(&raw_empty[rs]);
             fence_proxy_async();
-            mbar_arrive(&v_full[st]);
+            warp_arrive(&v_full[st]);
         };
-        uint32_t i = 0;                  // units whose keys are done; the values are one behind
-        int32_t last_key0 = 0, last_len = 0;
+        uint32_t i = 0;
         while (ok && seg.next(a, s)) {
             for (int32_t k = 0; ok && k < s.n; ++k, ++i) {
                 const int32_t key0 = (s.first + k) * kTcKeys + 32 * uw;
-                keys(i, key0, s.len);
-                if (ok && i > 0) values(i - 1, last_key0, last_len);
-                last_key0 = key0;
-                last_len = s.len;
+                if (of_keys)
+                    keys(i, key0, s.len);
+                else
+                    values(i, key0, s.len);
             }
         }
-        if (ok && i > 0) values(i - 1, last_key0, last_len);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kOtherRegs));
         if (warp == kFetchWarp) {

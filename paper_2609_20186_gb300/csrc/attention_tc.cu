@@ -54,11 +54,39 @@ struct TcSmem {
     static constexpr int bytes = 1024 + kQ + 2 * (kK + kV) + kRing * kRaw;
 };
 
-// A wait that gives up after a while (every one here is for this CTA's own work: some microseconds).
-__device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity) { return mbar_wait_polls(bar, parity, 1u << 17); }
+// A wait that gives up after a while (every one here is for this CTA's own work: some microseconds).  The thread may sleep
+// for up to 20 us a poll: a spinning warp takes its scheduler's issue slots from the rows' warps.
+__device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity) {
+    const uint32_t addr = smem_addr(bar);
+    for (uint32_t it = 0; it < 1u << 15; ++it) {
+        uint32_t done;
+        asm volatile(
+            "{\n"
+            ".reg .pred p;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n"
+            "selp.u32 %0, 1, 0, p;\n"
+            "}\n"
+            : "=r"(done)
+            : "r"(addr), "r"(parity)
+            : "memory");
+        if (done) return true;
+    }
+    return false;
+}
 
 // The warps of 32 rows.
 __device__ __forceinline__ void rows_barrier(int quarter) { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + quarter), "n"(kSplit * kWarp) : "memory"); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // One arrival for a warp, behind all of its threads' work (and their fences).
 __device__ __forceinline__ void warp_arrive(uint64_t *bar) {
     __syncwarp();
@@ -69,6 +97,13 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("mul.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
+}
+// The eight elements of a word of codes times their scales, of pairs.  (The offset and the scale in one multiply-add, which
+// is exact too, wants a second path for the scales whose 72-fold f16 does not have, and was slower.)
+__device__ __forceinline__ uint4 scaled_word(uint32_t w, uint4 s) {
+    uint32_t y[4];
+    signed_codes(w, y);
+    return make_uint4(mul_f16x2(y[0], s.x), mul_f16x2(y[1], s.y), mul_f16x2(y[2], s.z), mul_f16x2(y[3], s.w));
 }
 
 // The segments of a CTA's range: runs of units of one item.
@@ -115,6 +150,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
     __shared__ uint32_t s_small[2], s_rows[4];         // unit + 1, and segment + 1, that had small weights: of a buffer, of 32 rows
     __shared__ __align__(16) uint32_t s_valid[4][4], s_exist[kRing][4];  // of a unit (mod 4, mod 3): keys that exist and whose page does
     __shared__ float s_x[kSplit][kTcRows];             // what the threads of a row tell each other
+    __shared__ __align__(16) uint32_t s_scale[kUnpackWarps][16 * G];  // of the values' warps: scales of pairs of tokens
     __shared__ int s_bad;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int cta = blockIdx.x, ctas = int(gridDim.x);
@@ -246,14 +282,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                                 if ((e & 15) == 15) tmem_st16(sa + 32 * w + (e & 16), y);
                             }
                         }
-                        float t2[2] = {-INFINITY, -INFINITY}, l2[2] = {INFINITY, INFINITY};
+                        float t2[2] = {v[0], v[1]}, l2[2] = {v[0], v[1]};
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            t2[e & 1] = fmaxf(t2[e & 1], v[e]);
-                            l2[e & 1] = fminf(l2[e & 1], v[e]);
+                        for (int e = 2; e < 32; e += 2) {
+                            t2[(e >> 1) & 1] = max3(t2[(e >> 1) & 1], v[e], v[e + 1]);
+                            l2[(e >> 1) & 1] = min3(l2[(e >> 1) & 1], v[e], v[e + 1]);
                         }
-                        top = fmaxf(top, fmaxf(t2[0], t2[1]));
-                        low = fminf(low, fminf(l2[0], l2[1]));
+                        top = max3(top, t2[0], t2[1]);
+                        low = min3(low, l2[0], l2[1]);
                     }
                     if (masked) tmem_wait_st();
                 }
@@ -379,32 +415,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
         // ------------------------------------------------------------------------------------------- codes to f16
         const bool of_keys = warp < kValueWarp;
         const int uw = warp & (kUnpackWarps - 1), r = lane >> 2, c = lane & 3;  // this warp's keys of a unit: 32 uw .. + 31
-        // Scales of the warp's keys of a unit: f16 in the low half, zero where the key does not exist; a NaN in the value's
-        // scale of a new token goes to its key's.
-        auto scales = [&](const uint8_t *raw, int j, uint32_t exists, int32_t key0, int32_t len, uint32_t (&ks)[G], uint32_t (&vs)[G]) {
-            const uint32_t *scale = reinterpret_cast<const uint32_t *>(raw + S::kRawS + (32 * uw + 8 * j + r) * L::kScales);
-            if (G == 2) {
-                const uint2 x = *reinterpret_cast<const uint2 *>(scale);
-                ks[0] = x.x & 0xffffu;
-                ks[G - 1] = x.x >> 16;
-                vs[0] = x.y & 0xffffu;
-                vs[G - 1] = x.y >> 16;
-            } else {
-                const uint32_t x = *scale;
-                ks[0] = x & 0xffffu;
-                vs[0] = x >> 16;
-            }
-            if (exists != 0xffffffffu || key0 + 32 > len + 1) {
-                const bool gone = !((exists >> (8 * j + r)) & 1), fresh = key0 + 8 * j + r > len;
-                bool nan = false;
+        // The 16 bits of a key's or a value's scale, of the warp's key `place`, group g: zero where the key does not exist; a
+        // NaN in the value's scale of a new token goes to its key's.  `plain`: all exist, and none is new.
+        auto scale_of = [&](const uint8_t *raw, int place, int g, bool of_value, bool plain, uint32_t exists, int32_t key0, int32_t len) -> uint32_t {
+            const uint16_t *x = reinterpret_cast<const uint16_t *>(raw + S::kRawS + (32 * uw + place) * L::kScales);
+            const uint32_t it = x[(of_value ? G : 0) + g];
+            if (plain) return it;
+            bool nan = false;
 #pragma unroll
-                for (int g = 0; g < G; ++g) nan |= (vs[g] & 0x7fffu) > 0x7c00u;
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    if (gone || (nan && fresh)) vs[g] = 0;
-                    ks[g] = gone ? 0u : nan && fresh ? 0x7e00u : ks[g];
-                }
-            }
+            for (int e = 0; e < G; ++e) nan |= (x[G + e] & 0x7fffu) > 0x7c00u;
+            const bool gone = !((exists >> place) & 1), moved = nan && key0 + place > len;
+            return gone || (moved && of_value) ? 0u : moved ? 0x7e00u : it;
         };
         auto keys = [&](uint32_t i, int32_t key0, int32_t len) {
             const int st = int(i & 1), rs = int(i % kRing);
@@ -413,35 +434,33 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             ok = __all_sync(kFull, in_time);
             if (!ok) return;
             const uint32_t exists = s_exist[rs][uw];
+            const bool plain = exists == 0xffffffffu && key0 + 32 <= len + 1;
             const uint8_t *raw = sm_raw + rs * S::kRaw;
-            uint8_t *dk = sm_k + st * S::kK;
+            // lane (r, c): words 4 c .. of key 8 j + r; the row's place in its swizzled block does not depend on j
+            uint8_t *dk = sm_k + st * S::kK + (32 * uw + r) * 128;
+            const int at0 = ((2 * c) ^ r) * 16, at1 = ((2 * c + 1) ^ r) * 16;
 #pragma unroll 1
-            for (int j = 0; j < 4; ++j) {  // (a loop: the roles' code has to fit the instruction cache together)
-                const int key = 32 * uw + 8 * j + r;  // of the unit
-                uint32_t kw[2 * G], ks[G], vs[G];
+            for (int j = 0; j < 4; ++j, dk += 1024) {  // (a loop: the roles' code has to fit the instruction cache together)
+                const uint8_t *src = raw + (32 * uw + 8 * j + r) * L::kRow + 8 * G * c;
+                uint32_t kw[2 * G];
                 if (G == 2) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(raw + key * L::kRow + 16 * c);
+                    const uint4 w = *reinterpret_cast<const uint4 *>(src);
                     kw[0] = w.x;
                     kw[1] = w.y;
                     kw[2 * G - 2] = w.z;
                     kw[2 * G - 1] = w.w;
                 } else {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(raw + key * L::kRow + 8 * c);
+                    const uint2 w = *reinterpret_cast<const uint2 *>(src);
                     kw[0] = w.x;
                     kw[1] = w.y;
                 }
-                scales(raw, j, exists, key0, len, ks, vs);
-                uint4 y4[2 * G];
 #pragma unroll
-                for (int e = 0; e < 2 * G; ++e) {
-                    const uint32_t k2 = ks[e >> 1] | (ks[e >> 1] << 16);
-                    uint32_t y[4];
-                    signed_codes(kw[e], y);
-                    y4[e] = make_uint4(mul_f16x2(y[0], k2), mul_f16x2(y[1], k2), mul_f16x2(y[2], k2), mul_f16x2(y[3], k2));
+                for (int g = 0; g < G; ++g) {
+                    const uint32_t x = scale_of(raw, 8 * j + r, g, false, plain, exists, key0, len), x2 = x | (x << 16);
+                    const uint4 k4 = make_uint4(x2, x2, x2, x2);
+                    *reinterpret_cast<uint4 *>(dk + g * kBlockBytes + at0) = scaled_word(kw[2 * g], k4);
+                    *reinterpret_cast<uint4 *>(dk + g * kBlockBytes + at1) = scaled_word(kw[2 * g + 1], k4);
                 }
-#pragma unroll
-                for (int e = 0; e < 2 * G; ++e)
-                    *reinterpret_cast<uint4 *>(dk + (e >> 1) * kBlockBytes + key * 128 + (((2 * c + (e & 1)) ^ (key & 7)) * 16)) = y4[e];
             }
             warp_arrive(&raw_empty[rs]);
             if (lane == 0) s_valid[i & 3][uw] = exists;  // (unit i + 4's keys come after unit i's weights)
@@ -455,34 +474,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             ok = __all_sync(kFull, in_time);
             if (!ok) return;
             const uint32_t exists = s_exist[rs][uw];
+            const bool plain = exists == 0xffffffffu && key0 + 32 <= len + 1;
             const uint8_t *raw = sm_raw + rs * S::kRaw;
-            uint8_t *dv = sm_v + st * S::kV;
+            // the scales of tokens 2 p and 2 p + 1 of block j, group g, in a word: lane 4 (G j + g) + p makes it
+            if (lane < 16 * G) {
+                const int j = lane / (4 * G), g = (lane / 4) % G, p = lane & 3;
+                s_scale[uw][lane] = scale_of(raw, 8 * j + 2 * p, g, true, plain, exists, key0, len) |
+                                    (scale_of(raw, 8 * j + 2 * p + 1, g, true, plain, exists, key0, len) << 16);
+            }
+            __syncwarp();
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(raw + S::kRawV + 4 * uw * L::kBlock) + lane;
+            uint8_t *dv = sm_v + st * S::kV + (uw >> 1) * (D * 128) + lane * 128;
 #pragma unroll 1
-            for (int j = 0; j < 4; ++j) {
-                const int block = 4 * uw + j;  // of eight keys, of the unit
-                uint32_t ks[G], vs[G], vw[D / 32], v2[G][4];
+            for (int j = 0; j < 4; ++j, src += L::kBlock / 4) {
+                const int at = ((4 * (uw & 1) + j) ^ (lane & 7)) * 16;  // of the block's 16 bytes in dimension lane's row
 #pragma unroll
-                for (int e = 0; e < D / 32; ++e) vw[e] = *reinterpret_cast<const uint32_t *>(raw + S::kRawV + block * L::kBlock + 4 * (lane + 32 * e));
-                scales(raw, j, exists, key0, len, ks, vs);
-                // the eight tokens' value scales in pairs, of each group
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-#pragma unroll
-                    for (int p = 0; p < 4; ++p)
-                        v2[g][p] = (__shfl_sync(kFull, vs[g], 8 * p) & 0xffffu) | (__shfl_sync(kFull, vs[g], 8 * p + 4) << 16);
-                uint4 y4[D / 32];
-#pragma unroll
-                for (int e = 0; e < D / 32; ++e) {
-                    uint32_t y[4];
-                    signed_codes(vw[e], y);
-                    const uint32_t(&w)[4] = v2[e / 2];
-                    y4[e] = make_uint4(mul_f16x2(y[0], w[0]), mul_f16x2(y[1], w[1]), mul_f16x2(y[2], w[2]), mul_f16x2(y[3], w[3]));
-                }
-#pragma unroll
-                for (int e = 0; e < D / 32; ++e) {
-                    const int d = lane + 32 * e;
-                    *reinterpret_cast<uint4 *>(dv + (block >> 3) * (D * 128) + d * 128 + (((block & 7) ^ (d & 7)) * 16)) = y4[e];
-                }
+                for (int e = 0; e < D / 32; ++e)
+                    *reinterpret_cast<uint4 *>(dv + e * 4096 + at) =
+                        scaled_word(src[32 * e], *reinterpret_cast<const uint4 *>(&s_scale[uw][4 * (G * j + e / 2)]));
             }
             warp_arrive(&raw_empty[rs]);
             fence_proxy_async();

@@ -315,6 +315,28 @@ def test_attention_of_extreme_values(T, Hq):
     _check(got[:, :T - 1], want[:, :T - 1], mag[:, :T - 1], False)
 
 
+@pytest.mark.parametrize("T,Hq", [(1, 4), (9, 4)])
+def test_attention_of_the_largest_scales(T, Hq):
+    """Values and keys at every size of a scale up to the largest (8128), 2^-12 apart from key to key in the scores."""
+    import torch
+    fw = _fw()
+    rng = np.random.default_rng(9)
+    Hkv, D, page, n = 1, 128, 32, 100
+    k, v = rng.standard_normal((n, Hkv, D)), rng.standard_normal((n, Hkv, D))
+    size = np.exp2(np.arange(n) % 15)[:, None, None]
+    k, v = ref.bf16_round(k * size), ref.bf16_round(v * size)
+    k[n // 2], v[n // 3] = 60000, -64000
+    k, v = ref.bf16_round(k), ref.bf16_round(v)
+    cache = torch.zeros(4, Hkv, fw.switchsd_kv4_bytes(page, D), dtype=torch.uint8, device="cuda")
+    fw.switchsd_kv4_append(_tensor(k[None], False), _tensor(v[None], False), _i32(np.arange(n)[None]), cache, page=page)
+    kd, vd = ref.dequantise(*ref.quantise(k)), ref.dequantise(*ref.quantise(v))
+    lens, new = np.array([n - T]), np.array([T])
+    q = ref.bf16_round(rng.standard_normal((1, T, Hq, D)))
+    scale = 2.0 ** -20
+    want, mag = ref.attention(q, [kd], [vd], lens, new, scale)
+    _check(_attend(q, cache, np.arange(4)[None], lens, new, page, False, scale), want, mag, False)
+
+
 def test_attention_past_32_bit_offsets():
     """The pool's last pages of a cache of more than 4 GiB."""
     import torch

@@ -131,22 +131,13 @@ __device__ __forceinline__ void deal_units(const AttnArgs &a, int R, int unit, i
     const int64_t takers = min(total, int64_t(ctas));  // CTAs with a range: at least one unit each
     u = cta < takers ? total * cta / takers : total;
     u_end = cta < takers ? total * (cta + 1) / takers : total;
-    for (int64_t i0 = int64_t(cta) * kWarps + warp; i0 * kWarp < int64_t(a.B) * a.T; i0 += int64_t(ctas) * kWarps) {
-        const int64_t i = i0 * kWarp + lane;
-        bool none = false;
-        if (i < int64_t(a.B) * a.T) {
-            int32_t len, nw;
-            row_lengths(a, int(i / a.T), len, nw);
-            none = int(i % a.T) >= nw;
-        }
-        uint32_t todo = __ballot_sync(kFull, none);
-        const int row16 = a.Hq * a.dim / 8;  // 16-byte pieces of a token's output
-        while (todo) {
-            const int l = __ffs(int(todo)) - 1;
-            todo &= todo - 1;
-            uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(i0 * kWarp + l) * row16;
-            for (int e = lane; e < row16; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
-        }
+    const int row16 = a.Hq * a.dim / 8;  // 16-byte pieces of a token's output
+    for (int64_t i = int64_t(warp) * ctas + cta; i < int64_t(a.B) * a.T; i += int64_t(ctas) * kWarps) {
+        int32_t len, nw;
+        row_lengths(a, int(i / a.T), len, nw);
+        if (int(i % a.T) < nw) continue;
+        uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(i) * row16;
+        for (int e = lane; e < row16; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
     }
     if (tid < 2) a.desc[2 * cta + tid] = make_int4(-1, 0, 0, 0);
     const bool here = u < u_end && u >= s_pre[tid] && u < s_pre[tid + 1];

@@ -218,8 +218,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             const bool mine = row < rows, warp_mine = 32 * quarter < rows;
             const int rr = s.rt * kTcRows + row, t = rr / a.group, h = s.hk * a.group + rr - t * a.group;
             const int32_t limit = mine ? s.len + t : -1;
-            float scale;   // of a sum of products, for the binary logarithm
-            float hidden;  // a sum of products whose weight is 0
+            float scale;  // of a sum of products, for the binary logarithm: positive (the sign is in the queries)
             {
                 // the thread's part of the query, scaled by the power of two that brings the row's largest into [2^11, 2^12)
                 const uint16_t *q = a.q + s.b * a.qs[0] + int64_t(t) * a.qs[1] + int64_t(h) * a.qs[2] + part * DT;
@@ -237,10 +236,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 big = of_row([](float x, float y) { return fmaxf(x, y); });
                 int ex = 11 - (int(__float_as_uint(big) >> 23) - 127);
                 ex = big > 0.f && big < INFINITY ? max(-100, min(100, ex)) : 0;
-                const float up = __int_as_float((127 + ex) << 23);
-                scale = __int_as_float((127 - ex) << 23) * a.scale * 1.4426950408889634f;
-                if (scale == 0.f) scale = 1e-37f;  // (hidden * 0 would be NaN)
-                hidden = scale < 0.f ? INFINITY : -INFINITY;
+                const float up = copysignf(__int_as_float((127 + ex) << 23), a.scale);
+                scale = __int_as_float((127 - ex) << 23) * fabsf(a.scale) * 1.4426950408889634f;
+                if (scale == 0.f) scale = 1e-37f;  // (-inf * 0 would be NaN)
 #pragma unroll
                 for (int k = 0; k < DT / 8; ++k) {
                     const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
@@ -270,32 +268,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                         float v[32];
                         tmem_ld32(sa + 32 * w, v);
                         tmem_wait_ld();
-                        if (masked) {  // `hidden` in the place of the scores that the row does not see
+                        if (masked) {  // -inf in the place of the scores that the row does not see
                             const int place = part * KT + 32 * w;
                             const int32_t ahead = limit - (key0 + place);  // the last visible key's place
                             const uint32_t see = s_valid[i & 3][place / 32] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
                             uint32_t y[16];
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
-                                v[e] = (see >> e) & 1 ? v[e] : hidden;
+                                const bool in = (see >> e) & 1;
+                                low = in ? fminf(low, v[e]) : low;
+                                v[e] = in ? v[e] : -INFINITY;
                                 y[e & 15] = __float_as_uint(v[e]);
                                 if ((e & 15) == 15) tmem_st16(sa + 32 * w + (e & 16), y);
                             }
-                        }
-                        float t2[2] = {v[0], v[1]}, l2[2] = {v[0], v[1]};
+                        } else {
+                            float l2[2] = {v[0], v[1]};
 #pragma unroll
-                        for (int e = 2; e < 32; e += 2) {
-                            t2[(e >> 1) & 1] = max3(t2[(e >> 1) & 1], v[e], v[e + 1]);
-                            l2[(e >> 1) & 1] = min3(l2[(e >> 1) & 1], v[e], v[e + 1]);
+                            for (int e = 2; e < 32; e += 2) l2[(e >> 1) & 1] = min3(l2[(e >> 1) & 1], v[e], v[e + 1]);
+                            low = min3(low, l2[0], l2[1]);
                         }
+                        float t2[2] = {v[0], v[1]};
+#pragma unroll
+                        for (int e = 2; e < 32; e += 2) t2[(e >> 1) & 1] = max3(t2[(e >> 1) & 1], v[e], v[e + 1]);
                         top = max3(top, t2[0], t2[1]);
-                        low = min3(low, l2[0], l2[1]);
                     }
                     if (masked) tmem_wait_st();
                 }
-                // the scale may be negative; a row that sees nothing has infinities
-                const float mn = fminf(top * scale, low * scale);
-                s_x[part][row] = fmaxf(kFloor, fmaxf(top * scale, low * scale));
+                const float mn = low * scale;
+                s_x[part][row] = fmaxf(kFloor, top * scale);
                 rows_barrier(quarter);
                 const float mx = of_row([](float x, float y) { return fmaxf(x, y); });
                 float corr = 1.f;
@@ -589,8 +589,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             for (int32_t k = 0; ok && k < s.n; ++k, ++i) {
                 const int buf = int(i & 1);
                 if (k == 0) {
-                    // the rows' threads write the next queries when they have read the last O
-                    if (i > 0) product(i - 1);
+                    // (the rows' threads write the queries when they have read the last O)
                     ok = ok && tc_wait(&q_full, nseg & 1);
                     fresh = true;
                     lo = false;
@@ -609,9 +608,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 tc_commit(&k_empty[buf]);
                 if (k > 0) product(i - 1);
             }
+            if (ok) product(i - 1);  // before the next segment is looked up
             ++nseg;
         }
-        if (ok && i > 0) product(i - 1);
         // what is in flight reads shared and tensor memory; the rows' threads have waited for the last product, unless a
         // wait gave up
         if (!ok) {

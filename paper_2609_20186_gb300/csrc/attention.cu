@@ -32,10 +32,16 @@ constexpr int kAttnUnit = kAttnWarps * 32;  // keys of a unit: 32 a warp
 #define ATTN_OCC 3
 #endif
 constexpr int attn_ctas_per_sm(int NT) { return NT == 1 ? ATTN_OCC : 2; }
-constexpr float kWeightUp = 4096.f;         // the weights' scale as f16 numbers: the largest is in [2^11, 2^13]
+constexpr float kWeightLog = 12.f;          // log2 of the weight of a score (with its value's scale) at the reference
+constexpr float kLag = 3.f;                 // log2 of how far one may lie above: 2^15 is f16's
 constexpr float kSmall = 6.103515625e-5f;   // 2^-14: below it f16 loses bits
-constexpr float kLift = 16777216.f;         // 2^24: of the product of the small weights
-constexpr float kNone = 3.552713678800501e-15f;  // 2^-48, 2^-60 of the largest: too small for either
+constexpr float kLift = 16777216.f;         // 2^24: of the product of what rounding leaves of small weights
+
+__device__ __forceinline__ float log2_approx(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 // D = A B + C of m16n8k16, f16 operands, binary32 sums.
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
@@ -244,19 +250,15 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
             const bool out_of_pool = uint32_t(pk) >= uint32_t(a.pages);
             // S^T: tile j (rows r of two matrix tiles) holds keys key0 + 8 (r / 2) + 2 j + r % 2
             float s[NT][4][2];
-            float ks[4][G], vs[4][G], lg[4];
+            float ks[4][G];
+            uint32_t value_scales[4];  // (the next keys' scales are loaded before they are used)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    // scales of the token: G of the key, G of the value
-                    const uint16_t hk16 = G == 2 ? uint16_t(g ? x.sc[j][0] >> 16 : x.sc[j][0]) : uint16_t(x.sc[j][0]);
-                    const uint16_t hv16 = G == 2 ? uint16_t(g ? x.sc[j][G - 1] >> 16 : x.sc[j][G - 1]) : uint16_t(x.sc[j][0] >> 16);
-                    ks[j][g] = __half2float(__ushort_as_half(hk16)) * score;
-                    vs[j][g] = __half2float(__ushort_as_half(hv16));
-                }
-                const float big = G == 2 ? fmaxf(vs[j][0], vs[j][G - 1]) : vs[j][0];
-                lg[j] = fmaxf(float(int(__float_as_uint(big) >> 23) - 127), -24.f);
+                // scales of the token: G of the key, G of the value
+                const float2 k2 = __half22float2(*reinterpret_cast<const __half2 *>(&x.sc[j][0]));
+                ks[j][0] = k2.x * score;
+                if (G == 2) ks[j][G - 1] = k2.y * score;
+                value_scales[j] = x.sc[j][G - 1];
             }
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
@@ -304,54 +306,88 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
                             if (out_of_pool || key > limit[nt][e]) s[nt][j][e] = -INFINITY;
                 }
             }
-            // Weights: the softmax's times the values' scales.  f16 keeps 11 bits down to 2^-26 of the largest; smaller
-            // ones (kSmall) go into a product of their own, 2^24 higher.
-            uint32_t wb[NT][G][4], wl[NT][G][4];  // transposed: B operand of tile j
-            float corr[NT][2];
-            bool small = false;
+            // Weights: the softmax's times the values' scales.
+            float vs[4][G], lg[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 v2 = __half22float2(*reinterpret_cast<const __half2 *>(&value_scales[j]));
+                vs[j][0] = G == 2 ? v2.x : v2.y;
+                vs[j][G - 1] = v2.y;
+                lg[j] = fmaxf(log2_approx(G == 2 ? fmaxf(v2.x, v2.y) : v2.y), -24.f);
+            }
+            // The reference m may lag the largest score and scale by 2^kLag; only where one lies further above do the columns
+            // find their maxima and bring O to the new reference.
+            bool beyond = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    beyond |= fmaxf(fmaxf(s[nt][0][e] + lg[0], s[nt][1][e] + lg[1]), fmaxf(s[nt][2][e] + lg[2], s[nt][3][e] + lg[3])) > m[nt][e] + kLag;
+            if (__any_sync(kFull, beyond)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float corr[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(fmaxf(s[nt][0][e] + lg[0], s[nt][1][e] + lg[1]), fmaxf(s[nt][2][e] + lg[2], s[nt][3][e] + lg[3]));
+#pragma unroll
+                        for (int sh = 4; sh < 32; sh <<= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, sh));
+                        mx = fmaxf(mx, m[nt][e]);
+                        corr[e] = exp2_approx(m[nt][e] - mx);
+                        m[nt][e] = mx;
+                        l[nt][e] *= corr[e];
+                    }
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[nt][i][e] *= corr[e & 1];
+                }
+            }
+            uint32_t wb[NT][G][4];  // transposed: B operand of tile j
+            float least = INFINITY;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(fmaxf(s[nt][0][e] + lg[0], s[nt][1][e] + lg[1]), fmaxf(s[nt][2][e] + lg[2], s[nt][3][e] + lg[3]));
-#pragma unroll
-                    for (int sh = 4; sh < 32; sh <<= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, sh));
-                    mx = fmaxf(mx, m[nt][e]);
-                    corr[nt][e] = exp2_approx(m[nt][e] - mx);
-                    m[nt][e] = mx;
-                    float sum = 0.f;
+                    const float off = kWeightLog - m[nt][e];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        s[nt][j][e] = exp2_approx(s[nt][j][e] - mx);
-                        sum += s[nt][j][e];
+                        s[nt][j][e] = exp2_approx(s[nt][j][e] + off);
+                        l[nt][e] += s[nt][j][e];
                     }
-                    l[nt][e] = fmaf(l[nt][e], corr[nt][e], sum);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float f = vs[j][g] * kWeightUp;
-                        float w0 = s[nt][j][0] * f, w1 = s[nt][j][1] * f;
+                        float w0 = s[nt][j][0] * vs[j][g], w1 = s[nt][j][1] * vs[j][g];
                         if (masked) {  // a scale that a masked key left may be anything
                             w0 = s[nt][j][0] > 0.f ? w0 : 0.f;
                             w1 = s[nt][j][1] > 0.f ? w1 : 0.f;
+                            least = fminf(least, fminf(w0 > 0.f ? w0 : INFINITY, w1 > 0.f ? w1 : INFINITY));
+                        } else {
+                            least = fminf(least, fminf(w0, w1));
                         }
-                        small |= (w0 < kSmall && w0 > kNone) || (w1 < kSmall && w1 > kNone);
-                        wb[nt][g][j] = transpose8x8(pack_f16(w0 < kSmall ? 0.f : w0, w1 < kSmall ? 0.f : w1));
+                        wb[nt][g][j] = transpose8x8(pack_f16(w0, w1));
                     }
             }
-            const bool both = __any_sync(kFull, small);
-            if (both) {
+            // f16 keeps 11 bits down to 2^-14; what rounding leaves of smaller weights is multiplied apart, 2^24 higher
+            uint32_t wl[NT][G][4];
+            const bool small = __any_sync(kFull, least < kSmall);
+            if (small) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
                         for (int g = 0; g < G; ++g) {
-                            const float f = vs[j][g] * kWeightUp;
-                            const float w0 = s[nt][j][0] * f, w1 = s[nt][j][1] * f;
-                            wl[nt][g][j] = transpose8x8(pack_f16(w0 < kSmall ? w0 * kLift : 0.f, w1 < kSmall ? w1 * kLift : 0.f));
+                            float w[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float p = s[nt][j][e], y = p * vs[j][g];
+                                w[e] = p > 0.f && y < kSmall ? (y - __half2float(__float2half_rn(y))) * kLift : 0.f;
+                            }
+                            wl[nt][g][j] = transpose8x8(pack_f16(w[0], w[1]));
                         }
             }
             // O^T: the values' codes as signed f16 numbers
@@ -362,27 +398,22 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
                     uint32_t va[4], vb[4];
                     signed_codes(x.v[i][2 * h], va);
                     signed_codes(x.v[i][2 * h + 1], vb);
-                    constexpr int per_group = 2;  // i of a group
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        const uint32_t(&w)[4] = wb[nt][i / per_group];
-                        float acc[4];
-                        if (both) {
-                            const uint32_t(&wo)[4] = wl[nt][i / per_group];
-                            mma16816(acc, va[0], vb[0], va[1], vb[1], wo[0], wo[1], 0.f, 0.f, 0.f, 0.f);
-                            mma16816(acc, va[2], vb[2], va[3], vb[3], wo[2], wo[3], acc[0], acc[1], acc[2], acc[3]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[e] *= 1.f / kLift;
-                        } else {
-                            acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-                        }
-                        mma16816(acc, va[0], vb[0], va[1], vb[1], w[0], w[1], acc[0], acc[1], acc[2], acc[3]);
-                        mma16816(acc, va[2], vb[2], va[3], vb[3], w[2], w[3], acc[0], acc[1], acc[2], acc[3]);
+                        const uint32_t(&w)[4] = wb[nt][i / 2];  // (two i a group)
                         float(&oo)[4] = o[nt][2 * i + h];
-                        oo[0] = fmaf(oo[0], corr[nt][0], acc[0]);
-                        oo[1] = fmaf(oo[1], corr[nt][1], acc[1]);
-                        oo[2] = fmaf(oo[2], corr[nt][0], acc[2]);
-                        oo[3] = fmaf(oo[3], corr[nt][1], acc[3]);
+                        float acc[4];
+                        mma16816(acc, va[0], vb[0], va[1], vb[1], w[0], w[1], 0.f, 0.f, 0.f, 0.f);
+                        mma16816(acc, va[2], vb[2], va[3], vb[3], w[2], w[3], acc[0], acc[1], acc[2], acc[3]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) oo[e] += acc[e];
+                        if (small) {
+                            const uint32_t(&z)[4] = wl[nt][i / 2];
+                            mma16816(acc, va[0], vb[0], va[1], vb[1], z[0], z[1], 0.f, 0.f, 0.f, 0.f);
+                            mma16816(acc, va[2], vb[2], va[3], vb[3], z[2], z[3], acc[0], acc[1], acc[2], acc[3]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) oo[e] = fmaf(acc[e], 1.f / kLift, oo[e]);
+                        }
                     }
                 }
             if (more) load_values(key0 + kAttnUnit, pv1);
@@ -433,7 +464,7 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
             if (whole) {
                 if (row < rows) {
                     const int rr = rt * R + row, t = rr / a.group, h = hk * a.group + rr - t * a.group;
-                    const float inv = sum == 0.f ? 0.f : (1.f / kWeightUp) / sum;
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
                     uint2 w = make_uint2(narrow2<F16>(y.x * inv, y.y * inv), narrow2<F16>(y.z * inv, y.w * inv));
                     *reinterpret_cast<uint2 *>(a.out + ((size_t(b) * a.T + t) * a.Hq + h) * D + d) = w;
                 }
@@ -480,7 +511,7 @@ static cudaError_t launch_attn(AttnArgs a, int sms, cudaStream_t s) {
     const unsigned ctas = unsigned(std::min(kAttnMaxCtas, sms * attn_ctas_per_sm(NT)));
     e = launch_pdl(attn_kernel<F16, D, NT>, dim3(ctas), dim3(kAttnThreads), smem, s, 0u, a);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attn_join_kernel<F16, D>, dim3(ctas, 8 * NT), dim3(D), 0, s, 0u, a, 8 * NT, 1.f / kWeightUp);
+    return launch_pdl(attn_join_kernel<F16, D>, dim3(ctas, 8 * NT), dim3(D), 0, s, 0u, a, 8 * NT);
 }
 
 constexpr int kTensorRows = 16;

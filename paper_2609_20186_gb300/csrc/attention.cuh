@@ -167,9 +167,9 @@ __device__ __forceinline__ uint16_t narrow1(float a) {
 }
 
 // Joins the partial results of the items that several CTAs hold: CTAs (i, .) look after the item whose first part is the
-// i-th CTA's, adding the parts in order.  R query rows a tile; the outputs are `up` times what the sums' size says.
+// i-th CTA's, adding the parts in order.  R query rows a tile.
 template <bool F16, int D>
-__global__ void __launch_bounds__(D) attn_join_kernel(const AttnArgs a, int R, float up) {
+__global__ void __launch_bounds__(D) attn_join_kernel(const AttnArgs a, int R) {
     const int i = blockIdx.x, d = threadIdx.x, ctas = int(gridDim.x);
     pdl_wait();
     pdl_trigger();
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(D) attn_join_kernel(const AttnArgs a, int R, f
             flags = __ldcg(&a.desc[slot].w);
         }
         const int h = de.y * a.group + rr - t * a.group;
-        const float inv = sum == 0.f ? 0.f : up / sum;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
         a.out[((size_t(de.x) * a.T + t) * a.Hq + h) * D + d] = narrow1<F16>(y * inv);
     }
 }

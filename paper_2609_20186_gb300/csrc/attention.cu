@@ -15,10 +15,11 @@
 //
 // Numbers.  The queries are scaled by a power of two so that they are f16 numbers exactly (a bf16 has fewer bits; what
 // lies 2^22 below the largest may lose bits); codes, and so keys and values, are exact; scores, maxima, sums and the
-// output are binary32, and each 32 keys' matrix sum starts from zero and is added with a rounded multiply-add, because
-// the matrix unit's own accumulation truncates.  The weights exp(s - M) * scale_v are rounded to f16 (11 bits): M is the
-// running maximum of the score plus the exponent of its value's scale, so that the largest weight is near 1 whatever
-// the scales, and weights below 2^-26 of it begin to lose bits.
+// output are binary32.  (The output's sums over the keys are the matrix unit's, which truncates: two additions for 32 keys
+// of a warp, a bias below 2^-23 of the sum each.)  The weights 2^12 exp(s - M) * scale_v are rounded to f16 (11 bits): M,
+// the reference, is at most 2^kLag below the running maximum of the score plus the logarithm of its value's scale, so
+// that the largest weight fits whatever the scales; what rounding leaves of weights below 2^-26 of the reference, where
+// f16 has fewer bits, is multiplied apart, 2^24 higher.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -58,6 +59,13 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     return r;
 }
 
+// From shared memory at every use: kept in registers, the queries would leave room for fewer warps.
+__device__ __forceinline__ uint4 load_shared(const uint4 *p) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem_addr(p)));
+    return v;
+}
+
 // The codes and scales of a thread's share of 32 keys.
 template <int D>
 struct Keys {
@@ -73,6 +81,7 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
     constexpr int G = L::G, R = 8 * NT, MT = D / 16;  // groups, query rows of a tile, output tiles of 16 dimensions
     extern __shared__ float s_out[];                  // [warps][R][D + 4]
     __shared__ float s_max[kAttnWarps][R], s_sum[kAttnWarps][R];
+    __shared__ uint4 s_q[NT][G][2][kWarp];            // queries: B operands of each lane, the same for all warps
     __shared__ int64_t s_pre[kAttnThreads + 2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r = lane >> 2, c = lane & 3;
@@ -108,7 +117,6 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
         const int rows = min(R, nw * a.group - rt * R);
 
         // --- queries: B operand, row n = lane / 4 of each of NT tiles of 8 --------------------------------------
-        uint32_t qb[NT][G][2][4];   // [tile][group][word][step x register]
         float start[NT][G][2];      // -8 sum of the query's group, of columns 2 c, 2 c + 1
         float limit_f = 0.f;
         int32_t limit[NT][2];       // last key that the column's query sees
@@ -150,13 +158,15 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const uint32_t w[4] = {raw[nt][g][i].x, raw[nt][g][i].y, raw[nt][g][i].z, raw[nt][g][i].w};
+                        uint32_t qb[4];            // [step x register]
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {  // pair e; the odd pairs' codes stand four bits higher
                             const float x0 = widen1<F16>(uint16_t(w[e])) * up, x1 = widen1<F16>(uint16_t(w[e] >> 16)) * up;
                             sum += x0 + x1;
                             const float f = e & 1 ? 0.0625f : 1.f;
-                            qb[nt][g][i][e] = pack_f16(x0 * f, x1 * f);
+                            qb[e] = pack_f16(x0 * f, x1 * f);
                         }
+                        if (warp == 0) s_q[nt][g][i][lane] = make_uint4(qb[0], qb[1], qb[2], qb[3]);
                     }
                     sum += __shfl_xor_sync(kFull, sum, 1);
                     sum += __shfl_xor_sync(kFull, sum, 2);
@@ -165,6 +175,7 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
                 }
         }
         const float score = limit_f;  // binary logarithm's scale of a sum of products
+        __syncthreads();  // (every item ends with one too, behind which the next one's queries are written)
 
         float o[NT][MT][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -270,14 +281,15 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const uint32_t w0 = x.k[2 * mt][2 * g + i], w1 = x.k[2 * mt + 1][2 * g + i];
+                            const uint4 qb = load_shared(&s_q[nt][g][i][lane]);
                             if (i == 0)
-                                mma16816(acc, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb[nt][g][i][0], qb[nt][g][i][1],
+                                mma16816(acc, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb.x, qb.y,
                                          start[nt][g][0], start[nt][g][1], start[nt][g][0], start[nt][g][1]);
                             else
-                                mma16816(acc, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb[nt][g][i][0], qb[nt][g][i][1],
+                                mma16816(acc, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qb.x, qb.y,
                                          acc[0], acc[1], acc[2], acc[3]);
                             const uint32_t x0 = w0 >> 8, x1 = w1 >> 8;
-                            mma16816(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u, qb[nt][g][i][2], qb[nt][g][i][3],
+                            mma16816(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u, qb.z, qb.w,
                                      acc[0], acc[1], acc[2], acc[3]);
                         }
 #pragma unroll
@@ -402,13 +414,11 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
                     for (int nt = 0; nt < NT; ++nt) {
                         const uint32_t(&w)[4] = wb[nt][i / 2];  // (two i a group)
                         float(&oo)[4] = o[nt][2 * i + h];
-                        float acc[4];
-                        mma16816(acc, va[0], vb[0], va[1], vb[1], w[0], w[1], 0.f, 0.f, 0.f, 0.f);
-                        mma16816(acc, va[2], vb[2], va[3], vb[3], w[2], w[3], acc[0], acc[1], acc[2], acc[3]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) oo[e] += acc[e];
+                        mma16816(oo, va[0], vb[0], va[1], vb[1], w[0], w[1], oo[0], oo[1], oo[2], oo[3]);
+                        mma16816(oo, va[2], vb[2], va[3], vb[3], w[2], w[3], oo[0], oo[1], oo[2], oo[3]);
                         if (small) {
                             const uint32_t(&z)[4] = wl[nt][i / 2];
+                            float acc[4];
                             mma16816(acc, va[0], vb[0], va[1], vb[1], z[0], z[1], 0.f, 0.f, 0.f, 0.f);
                             mma16816(acc, va[2], vb[2], va[3], vb[3], z[2], z[3], acc[0], acc[1], acc[2], acc[3]);
 #pragma unroll

@@ -1,16 +1,24 @@
 // kv4.cu -- switchsd_kv4_append and switchsd_kv4_read: tokens into and out of the 4-bit paged cache.
 //
-// A warp takes one head's tokens of one block of eight cache positions (a value word holds eight tokens, so one warp
-// writes each word).  For the keys lane 4 t + c holds token t's dimensions 16 c .. 16 c + 15 of every group, which are
-// the 4 G words it stores; a group's extremes go over the quad.  For the values lane i holds D / 32 neighbouring
-// dimensions of all eight tokens, which are its words; a group's extremes go over 16 or 32 lanes.
+// A warp takes the keys, another the values, of one head's tokens in one block of eight cache positions (a value word
+// holds eight tokens, so one warp writes each word).  For the keys lane 4 t + c holds token t's dimensions 16 c ..
+// 16 c + 15 of every group, which are the 2 G words it stores; a group's extreme goes over the quad.  For the values lane
+// i holds D / 32 neighbouring dimensions of all eight tokens, which are its words; the eight tokens' extremes go over 16 or
+// 32 lanes by halves -- a lane hands on the half of the tokens that it does not keep --, so that each lane ends with one
+// token's and works out one scale.
+//
+// One extreme is enough for a scale: max(pos / 7, neg / 8) is max(8 pos, 7 neg) / 56, where the products are exact.  A
+// code is the rounded quotient x / s: x times the reciprocal, corrected once by its remainder (x has at most 11 bits and s
+// 7, so the remainder is exact, and a quotient that lies half-way between two codes comes out as it is).
+//
+// What bounds it: memory, 2 bytes read and 0.53 written a value, with about 10 instructions a value.
 #include <cuda_bf16.h>
 
 #include "kv4.cuh"
 
 namespace switchsd {
 
-constexpr int kAppendThreads = 128;
+constexpr int kUnitThreads = 128;
 
 struct AppendArgs {
     const uint8_t *k, *v;
@@ -21,180 +29,238 @@ struct AppendArgs {
     int32_t T, Hkv, units_per_row, page_shift, total;  // total: pages * page slots
 };
 
+struct ReadArgs {
+    const uint8_t *cache;
+    const int32_t *slots;
+    uint8_t *k, *v;        // f16 [B][T][Hkv][D]
+    int64_t units;
+    int32_t T, Hkv, units_per_row, page_shift, total;
+};
+
+// The unit of a warp: eight tokens from t0 on (some before the row's first or after its last), one head.
+struct Unit {
+    int64_t b;
+    int32_t h, t0;
+};
+template <class Args>
+__device__ __forceinline__ Unit unit_of(const Args &a, int64_t unit) {
+    Unit u;
+    u.h = int32_t(unit % a.Hkv);
+    const int64_t rest = unit / a.Hkv;
+    u.b = rest / a.units_per_row;
+    // Blocks begin where the first token's does: unit i has tokens [8 i - a0, 8 i - a0 + 8), a0 its place in the block.
+    u.t0 = 8 * int32_t(rest % a.units_per_row) - (__ldcg(a.slots + u.b * a.T) & 7);
+    return u;
+}
+// The slot of token t, -1 where there is none.
+template <class Args>
+__device__ __forceinline__ int32_t slot_of(const Args &a, int64_t b, int32_t t) {
+    const int32_t slot = t >= 0 && t < a.T ? __ldcg(a.slots + b * a.T + t) : -1;
+    return slot < a.total ? slot : -1;
+}
+
 // Two 16-bit values of the caller's type, widened.
 template <bool F16>
 __device__ __forceinline__ float2 widen(uint32_t w) {
-    if (F16) {
-        return __half22float2(*reinterpret_cast<const __half2 *>(&w));
-    }
+    if (F16) return __half22float2(*reinterpret_cast<const __half2 *>(&w));
     return make_float2(bf16_lo(w), bf16_hi(w));
 }
 
 // max that keeps a NaN.
-__device__ __forceinline__ float max_nan(float a, float b) { return (a > b || a != a) ? a : b; }
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 
-// The group's stored scale from its extremes: max(pos / 7, neg / 8) rounded up to 7 significant bits.  pos, neg >= 0
-// or NaN.  The divisions are exact where the quotient has 7 bits, so that the rounding never lifts such a scale.
-__device__ __forceinline__ __half group_scale(float pos, float neg) {
-    float s = max_nan(__fdiv_rn(pos, 7.f), neg * 0.125f);
-    if (s != s) return __ushort_as_half(0x7e00);
-    s = fminf(s, kScaleMax);
+// What x adds to its group's extreme: max(8 x, -7 x).
+__device__ __forceinline__ float extreme_of(float m, float x) { return max_nan(max_nan(m, 8.f * x), -7.f * x); }
+
+// The group's stored scale from its extreme (>= 0 or NaN): rounded up to 7 significant bits.  The division is exact where
+// the quotient has 7 bits, so that the rounding never lifts such a scale.
+__device__ __forceinline__ __half group_scale(float m) {
+    if (m != m) return __ushort_as_half(0x7e00);
+    const float s = fminf(__fdiv_rn(m, 56.f), kScaleMax);
     return __float2half_rn(__uint_as_float((__float_as_uint(s) + 0x1ffffu) & ~0x1ffffu));
 }
 
-// The code of x under scale s: round(x / s) to even, in 0 .. 15; 8 where s is 0 or NaN.
-__device__ __forceinline__ uint32_t code_of(float x, float s) {
-    if (!(s > 0.f)) return 8u;
-    const float q = fminf(fmaxf(rintf(__fdiv_rn(x, s)), -8.f), 7.f);
-    return uint32_t(int(q) + 8);
+// A group's scale and its reciprocal for the codes: zeros, and so codes of 8, where it is 0 or NaN.  Only a group that
+// is `wide` can hold an infinity, a NaN or a value beyond the largest scale's reach.
+struct Scale {
+    float s, r;
+    bool wide;
+    __device__ explicit Scale(__half h) : s(__half2float(h)), r(0.f) {
+        wide = !(s < kScaleMax);
+        if (s > 0.f)
+            r = __frcp_rn(s);
+        else
+            s = 0.f;
+    }
+};
+
+// The code of x in bits 0 .. 3 (the bits above are not clean).
+__device__ __forceinline__ uint32_t code_of(float x, const Scale &k) {
+    const float q = x * k.r;
+    const float t = fmaf(fmaf(-q, k.s, x), k.r, q);
+    return __float_as_uint(fminf(fmaxf(t, -8.f), 7.f) + 12582920.f);  // 1.5 * 2^23 + 8: rounds to even, code in the low bits
 }
+// An infinity has no remainder: a wide group's values are cut to finite ones first, beyond the largest scale's reach.
+__device__ __forceinline__ float within(float x) { return fminf(fmaxf(x, -65536.f), 65536.f); }
 
 __device__ __forceinline__ constexpr int nibble_of(int j) { return (j >> 1) + 4 * (j & 1); }
+// `w` with code c (its low 4 bits) as element j.
+__device__ __forceinline__ uint32_t put_code(uint32_t w, uint32_t c, int j) { return w | ((c & 15u) << (4 * nibble_of(j))); }
 
 template <bool F16, int D>
-__global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kUnitThreads) kv4_append_kernel(const AppendArgs a) {
     using L = Kv4<D>;
     constexpr int G = L::G;
     const int lane = threadIdx.x & 31;
-    const int64_t unit = int64_t(blockIdx.x) * (kAppendThreads / kWarp) + (threadIdx.x >> 5);
+    const int64_t job = int64_t(blockIdx.x) * (kUnitThreads / kWarp) + (threadIdx.x >> 5);
     pdl_wait();
     pdl_trigger();
-    if (unit >= a.units) return;
-    const int h = int(unit % a.Hkv);
-    const int u = int((unit / a.Hkv) % a.units_per_row);
-    const int64_t b = unit / a.Hkv / a.units_per_row;
-    const int32_t *slots = a.slots + b * a.T;
-    // Blocks begin where the first token's does: unit u has tokens [8 u - a0, 8 u - a0 + 8), a0 its place in the block.
-    const int32_t a0 = __ldcg(slots) & 7;
-    const int32_t t0 = 8 * u - a0;
-    const int tq = lane >> 2, c = lane & 3;
-    // lane 4 t + c looks at token t0 + t
-    const int32_t t = t0 + tq;
-    const int32_t slot = t >= 0 && t < a.T ? __ldcg(slots + t) : -1;
-    const bool live = slot >= 0 && slot < a.total;
-    const uint32_t any = __ballot_sync(kFull, live);
-    if (any == 0) return;
+    if (job >= 2 * a.units) return;
+    const Unit u = unit_of(a, job >> 1);
     const int page = 1 << a.page_shift;
     const size_t head_bytes = size_t(kv4_page_bytes(page, D));
-    // --- keys -------------------------------------------------------------------------------------------------
-    uint8_t *mine = a.cache + (size_t(live ? slot >> a.page_shift : 0) * a.Hkv + h) * head_bytes;
-    const int in_page = slot & (page - 1);
-    {
-        uint32_t words[2 * G];
-        __half scales[G];
-        const uint8_t *src = a.k + 2 * (b * a.ks[0] + int64_t(t) * a.ks[1] + int64_t(h) * a.ks[2]);
+    auto head_of = [&](int32_t slot) { return a.cache + (size_t(slot >> a.page_shift) * a.Hkv + u.h) * head_bytes; };
+    if ((job & 1) == 0) {
+        // --- keys ---------------------------------------------------------------------------------------------
+        const int tq = lane >> 2, c = lane & 3;
+        const int32_t t = u.t0 + tq, slot = slot_of(a, u.b, t);
+        if (__ballot_sync(kFull, slot >= 0) == 0) return;
+        const uint8_t *src = a.k + 2 * (u.b * a.ks[0] + int64_t(t) * a.ks[1] + int64_t(u.h) * a.ks[2]);
+        uint4 raw[G][2];
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            float x[16];
-            float pos = 0.f, neg = 0.f;
+        for (int g = 0; g < G; ++g)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                uint4 r = make_uint4(0, 0, 0, 0);
-                if (live) r = *reinterpret_cast<const uint4 *>(src + 2 * (64 * g + 16 * c + 8 * i));
-                const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+                raw[g][i] = make_uint4(0, 0, 0, 0);
+                if (slot >= 0) raw[g][i] = *reinterpret_cast<const uint4 *>(src + 2 * (64 * g + 16 * c + 8 * i));
+            }
+        uint32_t words[2 * G];
+        __half scales[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float x[16], m = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t w[4] = {raw[g][i].x, raw[g][i].y, raw[g][i].z, raw[g][i].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 f = widen<F16>(w[e]);
                     x[8 * i + 2 * e] = f.x;
                     x[8 * i + 2 * e + 1] = f.y;
+                    m = extreme_of(extreme_of(m, f.x), f.y);
                 }
             }
+            m = max_nan(m, __shfl_xor_sync(kFull, m, 1));
+            m = max_nan(m, __shfl_xor_sync(kFull, m, 2));
+            scales[g] = group_scale(m);
+            const Scale k(scales[g]);
+            if (__any_sync(kFull, k.wide)) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                pos = max_nan(x[e], pos);
-                neg = max_nan(-x[e], neg);
+                for (int e = 0; e < 16; ++e) x[e] = within(x[e]);
             }
-#pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                pos = max_nan(pos, __shfl_xor_sync(kFull, pos, o));
-                neg = max_nan(neg, __shfl_xor_sync(kFull, neg, o));
-            }
-            scales[g] = group_scale(pos, neg);
-            const float s = __half2float(scales[g]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 uint32_t w = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w |= code_of(x[8 * i + e], s) << (4 * nibble_of(e));
+                for (int e = 0; e < 8; ++e) w = put_code(w, code_of(x[8 * i + e], k), e);
                 words[2 * g + i] = w;
             }
         }
-        if (live) {
-            uint8_t *dst = mine + size_t(in_page) * L::kRow + c * (8 * G);
-            if (G == 2)
-                *reinterpret_cast<uint4 *>(dst) = make_uint4(words[0], words[1], words[2 * G - 2], words[2 * G - 1]);
-            else
-                *reinterpret_cast<uint2 *>(dst) = make_uint2(words[0], words[1]);
-            if (c == 0) {
-                __half *sc = reinterpret_cast<__half *>(mine + L::scales(page) + size_t(in_page) * L::kScales);
+        if (slot < 0) return;
+        uint8_t *head = head_of(slot);
+        const int in_page = slot & (page - 1);
+        uint8_t *dst = head + size_t(in_page) * L::kRow + c * (8 * G);
+        if (G == 2)
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(words[0], words[1], words[2 * G - 2], words[2 * G - 1]);
+        else
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(words[0], words[1]);
+        if (c == 0) {
+            __half *sc = reinterpret_cast<__half *>(head + L::scales(page) + size_t(in_page) * L::kScales);
 #pragma unroll
-                for (int g = 0; g < G; ++g) sc[g] = scales[g];
-            }
+            for (int g = 0; g < G; ++g) sc[g] = scales[g];
         }
+        return;
     }
     // --- values -----------------------------------------------------------------------------------------------
-    constexpr int N = D / 32;  // dimensions of a lane
+    constexpr int N = D / 32;       // dimensions of a lane
+    constexpr int kLanes = 64 / N;  // lanes of a group
+    const int32_t slot = slot_of(a, u.b, u.t0 + (lane & 7));  // lane e (mod 8): token t0 + e
+    // The block: the slot of its first token.  Tokens that do not stand in their place of it (slots that no map wrote) are
+    // left out: their words are another warp's.
+    const int32_t begin = slot >= (lane & 7) && ((slot - (lane & 7)) & 7) == 0 ? slot - (lane & 7) : -1;
+    const uint32_t can = __ballot_sync(kFull, begin >= 0) & 255u;
+    if (can == 0) return;
+    const int32_t base = __shfl_sync(kFull, begin, __ffs(int(can)) - 1);
+    const uint32_t in = __ballot_sync(kFull, slot >= 0 && slot == base + (lane & 7)) & 255u;  // bit e: token t0 + e
+    const uint8_t *src = a.v + 2 * (u.b * a.vs[0] + int64_t(u.t0) * a.vs[1] + int64_t(u.h) * a.vs[2]) + 2 * N * lane;
+    uint2 raw[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        raw[e] = make_uint2(0, 0);
+        if ((in >> e) & 1) {
+            const uint8_t *p = src + 2 * int64_t(e) * a.vs[1];
+            if (N == 4)
+                raw[e] = *reinterpret_cast<const uint2 *>(p);
+            else
+                raw[e].x = *reinterpret_cast<const uint32_t *>(p);
+        }
+    }
+    float m[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float2 f = widen<F16>(raw[e].x);
+        m[e] = extreme_of(extreme_of(0.f, f.x), f.y);
+        if (N == 4) {
+            const float2 f2 = widen<F16>(raw[e].y);
+            m[e] = extreme_of(extreme_of(m[e], f2.x), f2.y);
+        }
+    }
+    // by halves: after the three exchanges a lane has the token of its three highest bits in the group
+#pragma unroll
+    for (int half = 4, bit = kLanes / 2; half > 0; half >>= 1, bit >>= 1) {
+        const bool upper = (lane & bit) != 0;
+#pragma unroll
+        for (int e = 0; e < half; ++e) {
+            const float keep = upper ? m[e + half] : m[e], give = upper ? m[e] : m[e + half];
+            m[e] = max_nan(keep, __shfl_xor_sync(kFull, give, bit));
+        }
+    }
+#pragma unroll
+    for (int bit = kLanes / 16; bit > 0; bit >>= 1) m[0] = max_nan(m[0], __shfl_xor_sync(kFull, m[0], bit));
+    const __half mine = group_scale(m[0]);
+    const int token = (lane / (kLanes / 8)) & 7;  // whose scale this lane has
+    if (lane % (kLanes / 8) == 0 && ((in >> token) & 1)) {
+        const int32_t at = base + token;
+        reinterpret_cast<__half *>(head_of(at) + L::scales(page) + size_t(at & (page - 1)) * L::kScales)[G + lane / kLanes] = mine;
+    }
+    const Scale own(mine);
+    const bool wide = __any_sync(kFull, own.wide);
     uint32_t words[N], keep = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) words[i] = 0;
-    int32_t base = -1;         // the block: slot of its first token
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int32_t se = __shfl_sync(kFull, slot, 4 * e);
-        const bool le = se >= 0 && se < a.total;
-        // A token that does not stand e places into the first one's block (slots that no map wrote) is left out: its
-        // word is another warp's.
-        if (le && base < 0 && se >= e && ((se - e) & 7) == 0) base = se - e;
-        const bool in = le && se == base + e;
-        float x[N];
-        float pos = 0.f, neg = 0.f;
-        const uint8_t *src = a.v + 2 * (b * a.vs[0] + int64_t(t0 + e) * a.vs[1] + int64_t(h) * a.vs[2]) + 2 * N * lane;
-        uint2 r = make_uint2(0, 0);
-        if (in) {
-            if (N == 4)
-                r = *reinterpret_cast<const uint2 *>(src);
-            else
-                r.x = *reinterpret_cast<const uint32_t *>(src);
-        }
-        {
-            const float2 f = widen<F16>(r.x);
-            x[0] = f.x;
-            x[1] = f.y;
-            if (N == 4) {
-                const float2 f2 = widen<F16>(r.y);
-                x[N - 2] = f2.x;
-                x[N - 1] = f2.y;
-            }
-        }
+        Scale k = own;
+        const int from = (lane & ~(kLanes - 1)) | (e * (kLanes / 8));
+        k.s = __shfl_sync(kFull, own.s, from);
+        k.r = __shfl_sync(kFull, own.r, from);
+        const float2 f = widen<F16>(raw[e].x), f2 = widen<F16>(raw[e].y);
+        float x[4] = {f.x, f.y, f2.x, f2.y};
+        if ((in >> e) & 1) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            pos = max_nan(x[i], pos);
-            neg = max_nan(-x[i], neg);
-        }
-#pragma unroll
-        for (int o = 1; o < 64 / N; o <<= 1) {
-            pos = max_nan(pos, __shfl_xor_sync(kFull, pos, o));
-            neg = max_nan(neg, __shfl_xor_sync(kFull, neg, o));
-        }
-        const __half sh = group_scale(pos, neg);
-        const float s = __half2float(sh);
-        if (in) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) words[i] |= code_of(x[i], s) << (4 * nibble_of(e));
-            if ((lane & (64 / N - 1)) == 0) {
-                uint8_t *at = a.cache + (size_t(se >> a.page_shift) * a.Hkv + h) * head_bytes;
-                reinterpret_cast<__half *>(at + L::scales(page) + size_t(se & (page - 1)) * L::kScales)[G + lane / (64 / N)] = sh;
-            }
+            for (int i = 0; i < N; ++i) words[i] = put_code(words[i], code_of(wide ? within(x[i]) : x[i], k), e);
         } else {
             keep |= 0xfu << (4 * nibble_of(e));
         }
     }
-    if (base < 0) return;
-    uint8_t *dst = a.cache + (size_t(base >> a.page_shift) * a.Hkv + h) * head_bytes + L::values(page) +
-                   size_t((base & (page - 1)) >> 3) * L::kBlock + 4 * N * lane;
+    uint8_t *dst = head_of(base) + L::values(page) + size_t((base & (page - 1)) >> 3) * L::kBlock + 4 * N * lane;
     if (N == 4) {
         uint4 w = make_uint4(words[0], words[1], words[N - 2], words[N - 1]);
-        if (keep) {
+        if (keep) {  // tokens of earlier calls in the same words
             const uint4 old = *reinterpret_cast<const uint4 *>(dst);
             w.x |= old.x & keep;
             w.y |= old.y & keep;
@@ -213,47 +279,86 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const Append
     }
 }
 
-struct ReadArgs {
-    const uint8_t *cache;
-    const int32_t *slots;
-    uint8_t *k, *v;   // f16 [tokens][Hkv][D]
-    int64_t n;        // tokens * Hkv * D / 8
-    int32_t Hkv, page_shift, total;
-};
+// (c - 8) * scale of a pair of codes in bits 0 .. 3 and 16 .. 19, as f16 numbers: exact.
+__device__ __forceinline__ uint32_t pair_value(uint32_t w, __half2 s) {
+    const uint32_t magic = (w & 0x000f000fu) | 0x64006400u;  // 1024 + c
+    const __half2 c = __hsub2(*reinterpret_cast<const __half2 *>(&magic), __float2half2_rn(1032.f));
+    const __half2 v = __hmul2(c, s);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
 
-// A thread reads eight dimensions of one token's key and value.
+// The same units as the append's; tokens without a slot get zeros.
 template <int D>
-__global__ void __launch_bounds__(256) kv4_read_kernel(const ReadArgs a) {
+__global__ void __launch_bounds__(kUnitThreads) kv4_read_kernel(const ReadArgs a) {
     using L = Kv4<D>;
+    constexpr int G = L::G;
+    const int lane = threadIdx.x & 31;
+    const int64_t job = int64_t(blockIdx.x) * (kUnitThreads / kWarp) + (threadIdx.x >> 5);
     pdl_wait();
     pdl_trigger();
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= a.n) return;
-    const int dw = int(i % (D / 8));
-    const int64_t th = i / (D / 8);
-    const int h = int(th % a.Hkv);
-    const int32_t slot = __ldcg(a.slots + th / a.Hkv);
-    __half ok[8], ov[8];
-    if (slot >= 0 && slot < a.total) {
-        const int page = 1 << a.page_shift, in = slot & (page - 1), g = dw >> 3;
-        const uint8_t *src = a.cache + (size_t(slot >> a.page_shift) * a.Hkv + h) * size_t(kv4_page_bytes(page, D));
-        const __half *sc = reinterpret_cast<const __half *>(src + L::scales(page) + size_t(in) * L::kScales);
-        const int word = ((dw & 7) >> 1) * (2 * L::G) + 2 * g + (dw & 1);
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(src + size_t(in) * L::kRow + 4 * word);
-        const uint32_t *vw = reinterpret_cast<const uint32_t *>(src + L::values(page) + size_t(in >> 3) * L::kBlock) + 8 * dw;
-        const float ks = __half2float(sc[g]), vs = __half2float(sc[L::G + g]);
-        const int shift = 4 * (((in & 7) >> 1) + 4 * (in & 1));
+    if (job >= 2 * a.units) return;
+    const Unit u = unit_of(a, job >> 1);
+    const int page = 1 << a.page_shift;
+    const size_t head_bytes = size_t(kv4_page_bytes(page, D));
+    auto head_of = [&](int32_t slot) { return a.cache + (size_t(slot >> a.page_shift) * a.Hkv + u.h) * head_bytes; };
+    auto out_of = [&](uint8_t *out, int32_t t) { return out + ((size_t(u.b) * a.T + t) * a.Hkv + u.h) * (2 * D); };
+    if ((job & 1) == 0) {
+        const int c = lane & 3;
+        const int32_t t = u.t0 + (lane >> 2), slot = slot_of(a, u.b, t);
+        if (t < 0 || t >= a.T) return;
+        uint32_t words[2 * G];
+        __half2 s[G];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            ok[j] = __float2half_rn((float((w >> (4 * nibble_of(j))) & 15u) - 8.f) * ks);
-            ov[j] = __float2half_rn((float((vw[j] >> shift) & 15u) - 8.f) * vs);
+        for (int g = 0; g < G; ++g) {
+            words[2 * g] = words[2 * g + 1] = 0x88888888u;  // zeros
+            s[g] = __float2half2_rn(0.f);
         }
-    } else {
+        if (slot >= 0) {
+            const uint8_t *head = head_of(slot);
+            const int in_page = slot & (page - 1);
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(head + size_t(in_page) * L::kRow + c * (8 * G));
+            const __half *sc = reinterpret_cast<const __half *>(head + L::scales(page) + size_t(in_page) * L::kScales);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) ok[j] = ov[j] = __ushort_as_half(0);
+            for (int i = 0; i < 2 * G; ++i) words[i] = w[i];
+#pragma unroll
+            for (int g = 0; g < G; ++g) s[g] = __half2half2(sc[g]);
+        }
+        uint8_t *out = out_of(a.k, t);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t w = words[2 * g + i];
+                *reinterpret_cast<uint4 *>(out + 2 * (64 * g + 16 * c + 8 * i)) =
+                    make_uint4(pair_value(w, s[g]), pair_value(w >> 4, s[g]), pair_value(w >> 8, s[g]), pair_value(w >> 12, s[g]));
+            }
+        return;
     }
-    *reinterpret_cast<uint4 *>(a.k + 16 * i) = *reinterpret_cast<uint4 *>(ok);
-    *reinterpret_cast<uint4 *>(a.v + 16 * i) = *reinterpret_cast<uint4 *>(ov);
+    constexpr int N = D / 32;  // dimensions of a lane
+    const int32_t slot = slot_of(a, u.b, u.t0 + (lane & 7));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int32_t se = __shfl_sync(kFull, slot, e), t = u.t0 + e;
+        if (t < 0 || t >= a.T) continue;
+        uint32_t v[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) v[i] = 0;
+        if (se >= 0) {
+            // a token's codes stand in its block's words, eight tokens' together: the same line for the unit's other tokens
+            const uint8_t *head = head_of(se);
+            const int in_page = se & (page - 1), sh = 4 * ((in_page & 7) >> 1) + 16 * (in_page & 1);
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(head + L::values(page) + size_t(in_page >> 3) * L::kBlock) + N * lane;
+            const __half *sc = reinterpret_cast<const __half *>(head + L::scales(page) + size_t(in_page) * L::kScales);
+            const __half2 s = __half2half2(sc[G + N * lane / 64]);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) v[i] = pair_value(((w[2 * i] >> sh) & 15u) | (((w[2 * i + 1] >> sh) & 15u) << 16), s);
+        }
+        uint8_t *out = out_of(a.v, t) + 2 * N * lane;
+        if (N == 4)
+            *reinterpret_cast<uint2 *>(out) = make_uint2(v[0], v[N / 2 - 1]);
+        else
+            *reinterpret_cast<uint32_t *>(out) = v[0];
+    }
 }
 
 }  // namespace switchsd
@@ -287,10 +392,10 @@ extern "C" int switchsd_kv4_append(const switchsd_kv4_append_params *p) {
     a.units = int64_t(p->B) * a.units_per_row * p->Hkv;
     a.page_shift = log2_of(p->page);
     a.total = p->pages * p->page;
-    const int64_t ctas = (a.units + kAppendThreads / kWarp - 1) / (kAppendThreads / kWarp);
+    const int64_t ctas = (2 * a.units + kUnitThreads / kWarp - 1) / (kUnitThreads / kWarp);
     if (ctas > 0x7fffffff) return SWITCHSD_ERR_SHAPE;
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);
-    const dim3 grid{unsigned(ctas)}, block{unsigned(kAppendThreads)};
+    const dim3 grid{unsigned(ctas)}, block{unsigned(kUnitThreads)};
     cudaError_t e;
     if (p->dtype == SWITCHSD_F16)
         e = p->D == 128 ? launch_pdl(kv4_append_kernel<true, 128>, grid, block, 0, s, 0u, a)
@@ -311,14 +416,16 @@ extern "C" int switchsd_kv4_read(const switchsd_kv4_read_params *p) {
     a.slots = p->slots;
     a.k = static_cast<uint8_t *>(p->out_k);
     a.v = static_cast<uint8_t *>(p->out_v);
-    a.n = int64_t(p->B) * p->T * p->Hkv * (p->D / 8);
+    a.T = p->T;
     a.Hkv = p->Hkv;
+    a.units_per_row = (p->T - 1 + 7) / 8 + 1;
+    a.units = int64_t(p->B) * a.units_per_row * p->Hkv;
     a.page_shift = log2_of(p->page);
     a.total = p->pages * p->page;
-    const int64_t ctas = (a.n + 255) / 256;
+    const int64_t ctas = (2 * a.units + kUnitThreads / kWarp - 1) / (kUnitThreads / kWarp);
     if (ctas > 0x7fffffff) return SWITCHSD_ERR_SHAPE;
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);
-    const cudaError_t e = p->D == 128 ? launch_pdl(kv4_read_kernel<128>, dim3(unsigned(ctas)), dim3(256u), 0, s, 0u, a)
-                                      : launch_pdl(kv4_read_kernel<64>, dim3(unsigned(ctas)), dim3(256u), 0, s, 0u, a);
+    const dim3 grid{unsigned(ctas)}, block{unsigned(kUnitThreads)};
+    const cudaError_t e = p->D == 128 ? launch_pdl(kv4_read_kernel<128>, grid, block, 0, s, 0u, a) : launch_pdl(kv4_read_kernel<64>, grid, block, 0, s, 0u, a);
     return e == cudaSuccess ? SWITCHSD_OK : SWITCHSD_ERR_CUDA;
 }

@@ -29,7 +29,7 @@ constexpr int kCountThreads = 512;
 constexpr int kLogitThreads = 256;
 constexpr int kLogitWarps = kLogitThreads / kWarp;
 constexpr int kLogitGroup = 4;              // positions of a CTA
-constexpr int kLogitUnits = 4;              // units (32 vectors of 16 bytes) of a warp in flight
+constexpr int kLogitFlight = 4;             // units (32 vectors of 16 bytes) of a warp in flight, over its positions
 constexpr int kChunk = 256;                 // tokens that lie together in a part
 constexpr uint32_t kSeen = 1u << 31;        // in a token's word: occurs in the context
 constexpr uint32_t kInDraft = 1u << 30;     // occurs in the draft
@@ -83,7 +83,8 @@ __device__ __forceinline__ int row_positions(const LogitArgs &a, int b, int32_t 
 }
 
 // An element type: widening, narrowing, a vector whose elements without their bit become -inf (lut: for every byte of
-// bits, the mask of four words of two 16-bit elements), and a vector's largest element.
+// bits, the mask of four words of two 16-bit elements), and a vector's largest
+// element (NaN if they all are).
 template <int DT>
 struct Elem;
 template <>
@@ -103,7 +104,7 @@ struct Elem<SWITCHSD_BF16> {
     }
     __device__ static float largest(uint4 w) {
         const uint32_t m = max2(max2(w.x, w.y), max2(w.z, w.w));
-        return fmaxf(-INFINITY, fmaxf(bf16_lo(m), bf16_hi(m)));
+        return fmaxf(bf16_lo(m), bf16_hi(m));
     }
 };
 template <>
@@ -123,7 +124,7 @@ struct Elem<SWITCHSD_F16> {
     }
     __device__ static float largest(uint4 w) {
         const uint32_t m = max2(max2(w.x, w.y), max2(w.z, w.w));
-        return fmaxf(-INFINITY, fmaxf(get(uint16_t(m)), get(uint16_t(m >> 16))));
+        return fmaxf(get(uint16_t(m)), get(uint16_t(m >> 16)));
     }
 };
 template <>
@@ -136,7 +137,7 @@ struct Elem<SWITCHSD_F32> {
         return make_uint4(open & 1 ? w.x : none, open & 2 ? w.y : none, open & 4 ? w.z : none, open & 8 ? w.w : none);
     }
     __device__ static float largest(uint4 w) {
-        return fmaxf(-INFINITY, fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w))));
+        return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
     }
 };
 
@@ -165,6 +166,7 @@ __global__ void __launch_bounds__(kCountThreads) logits_count_kernel(const Logit
     const int b = blockIdx.y, parts = int(gridDim.x);
     const Part part{a.V, int(blockIdx.x), a.parts_log};
     // everything here but the inputs: before the kernel ahead has finished
+    const int words = a.slice / 32;
     for (int i = tid; i < a.slice / 4; i += kCountThreads) reinterpret_cast<uint4 *>(cnt)[i] = make_uint4(0, 0, 0, 0);
     for (int i = tid; i < int(places); i += kCountThreads) {
         keys[i] = -1;
@@ -225,45 +227,174 @@ __global__ void __launch_bounds__(kCountThreads) logits_count_kernel(const Logit
         atomicOr(&cnt[at], kBiased);
     }
     __syncthreads();
-    // The map, and every warp's number of specials in its share of it: words [warp per, + per).
-    const int words = a.slice / 32, per = (words + kCountThreads / kWarp - 1) / (kCountThreads / kWarp);
-    const int w0 = min(words, warp * per), w1 = min(words, w0 + per);
     uint32_t *out_bits = a.bits + (size_t(b) * parts + part.part) * words;
-    int mine = 0;
-#pragma unroll 4
-    for (int i = w0; i < w1; ++i) {
+    for (int i = warp; i < words; i += kCountThreads / kWarp) {
         const uint32_t m = __ballot_sync(kFull, cnt[32 * i + lane] != 0);
-        if (lane == 0) {
-            bits[i] = m;
-            out_bits[i] = m;
-        }
-        mine += __popc(m);
+        if (lane == 0) bits[i] = m;
     }
+    __syncthreads();
+    // The map goes out.  A warp lists the specials of words [warp per, + per), a lane those of a word, all in the order of
+    // their places, so that neighbours in the list are near each other in the logits.
+    const int per = (words + kCountThreads / kWarp - 1) / (kCountThreads / kWarp);
+    const int w0 = min(words, warp * per), w1 = min(words, w0 + per);
+    int mine = 0;
+    for (int i = w0 + lane; i < w1; i += kWarp) {
+        out_bits[i] = bits[i];
+        mine += __popc(bits[i]);
+    }
+    mine = __reduce_add_sync(kFull, mine);
     if (lane == 0) s_warp[warp] = mine;
     __syncthreads();
-    int at = 0, all = 0;
+    int before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < kCountThreads / kWarp; ++w) {
-        if (w < warp) at += s_warp[w];
+        if (w < warp) before += s_warp[w];
         all += s_warp[w];
     }
     if (tid == 0) a.count[size_t(b) * parts + part.part] = all;
     uint2 *list = a.list + (size_t(b) * parts + part.part) * a.entries;
-    for (int i = w0; i < w1; ++i) {
-        const uint32_t m = bits[i];
-        if ((m >> lane) & 1) {
-            const uint32_t w = cnt[32 * i + lane];
+    for (int i0 = w0; i0 < w1; i0 += kWarp) {
+        const int i = i0 + lane;
+        uint32_t m = i < w1 ? bits[i] : 0u;
+        const int n = __popc(m);
+        int k = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(kFull, k, o);
+            if (lane >= o) k += y;
+        }
+        const int sum = __shfl_sync(kFull, k, 31);
+        for (k += before - n; m; m &= m - 1, ++k) {
+            const int at = 32 * i + __ffs(int(m)) - 1;
+            const uint32_t w = cnt[at];
             uint32_t bias = 0;
             if (w & kBiased) {
-                const int32_t v = part.token_at(32 * i + lane);
+                const int32_t v = part.token_at(at);
                 uint32_t p = bias_hash(uint32_t(v)) & a.hash_mask;
                 while (keys[p] != v) p = (p + 1) & a.hash_mask;
                 bias = uint32_t(vals[p]);
             }
-            const int k = at + __popc(m & ((1u << lane) - 1));
-            if (k < a.entries) list[k] = make_uint2(uint32_t(32 * i + lane) | (bias << 16), w);
+            if (k < a.entries) list[k] = make_uint2(uint32_t(at) | (bias << 16), w);
         }
-        at += __popc(m);
+        before += sum;
+    }
+}
+
+// The positions of a CTA that the streaming pass takes together, P of them (the last ones may not be there), and what they
+// have in common: rows begin at `row`, results at `out`, masks at `mask`, each its own stride apart.
+template <int DT, int P>
+__device__ __forceinline__ void stream_part(const LogitArgs &a, const Part &part, int positions, const typename Elem<DT>::type *row,
+                                            typename Elem<DT>::type *out, const uint32_t *mask, const uint32_t *bits, const uint4 *lut,
+                                            unsigned long long *s_best) {
+    using E = Elem<DT>;
+    using elem = typename E::type;
+    constexpr int N = 16 / int(sizeof(elem));     // elements of a vector
+    constexpr int kUnit = kWarp * N;              // tokens of a unit
+    constexpr int kUnits = kLogitFlight / P;      // units of a warp in flight
+    constexpr uint32_t kExact = 1u << 31;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int units = part.used() / kUnit;
+    // The units that are read (and written) by vectors: all but the vocabulary's last tokens, where every row begins on a
+    // 16-byte boundary; the rest 32 neighbours at a time.
+    int whole = units;
+    while (whole > 0 && part.token_at((whole - 1) * kUnit) + kUnit > a.V) --whole;
+    {
+        uintptr_t low = reinterpret_cast<uintptr_t>(row) | reinterpret_cast<uintptr_t>(out);
+        if (positions > 1) low |= (uintptr_t(a.st) | (out ? uintptr_t(a.ot) : 0)) * sizeof(elem);
+        if (low & 15) whole = 0;
+    }
+    // Per position, a lane's best value, and its token (kExact) or the first token of the vector that has it.
+    float best[P];
+    uint32_t where[P];
+#pragma unroll
+    for (int t = 0; t < P; ++t) {
+        best[t] = -INFINITY;
+        where[t] = 0;
+    }
+    const int step = (kLogitWarps * kUnit) << part.log;  // tokens between a warp's units: whole chunks
+    auto open_of = [&](int t, int32_t v) { return uint32_t(__ldcg(reinterpret_cast<const uint8_t *>(mask + size_t(t) * a.mask_words) + (v >> 3))) >> (v & 7 & -N); };
+    auto special_of = [&](int l) { return uint32_t(__ldcg(reinterpret_cast<const uint8_t *>(bits) + (l >> 3))) >> (l & 7 & -N); };
+    for (int u0 = warp; u0 < whole; u0 += kUnits * kLogitWarps) {
+        const int32_t v0 = part.token_at(u0 * kUnit) + lane * N;
+        uint4 w[kUnits][P];
+        uint32_t open[kUnits][P], special[kUnits];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const bool in = u0 + i * kLogitWarps < whole;
+            special[i] = a.marks && in ? special_of((u0 + i * kLogitWarps) * kUnit + lane * N) : 0u;
+#pragma unroll
+            for (int t = 0; t < P; ++t) {
+                const int32_t v = v0 + i * step;
+                open[i][t] = 0;
+                w[i][t] = make_uint4(0, 0, 0, 0);
+                if (in && t < positions) {
+                    w[i][t] = *reinterpret_cast<const uint4 *>(row + t * a.st + v);
+                    open[i][t] = mask ? open_of(t, v) : 0xffu;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+            for (int t = 0; t < P; ++t) {
+                const int32_t v = v0 + i * step;
+                if (out && u0 + i * kLogitWarps < whole && t < positions)
+                    *reinterpret_cast<uint4 *>(out + t * a.ot + v) = mask ? E::keep(w[i][t], open[i][t], lut) : w[i][t];
+                const float m = E::largest(E::keep(w[i][t], open[i][t] & ~special[i], lut));
+                if (m > best[t]) {  // a lane's tokens come in order, so only a larger value is better
+                    best[t] = m;
+                    where[t] = uint32_t(v);
+                }
+            }
+    }
+    for (int u = whole + (warp - whole % kLogitWarps + kLogitWarps) % kLogitWarps; u < units; u += kLogitWarps) {
+        const int32_t v0 = part.token_at(u * kUnit);
+        uint32_t special[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) special[j] = a.marks ? __ldcg(bits + u * (kUnit / 32) + j) : 0u;
+#pragma unroll
+        for (int t = 0; t < P; ++t) {
+            if (t >= positions) break;
+            elem y[N];
+            uint32_t open[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int32_t v = v0 + 32 * j + lane;
+                y[j] = v < a.V ? row[t * a.st + v] : elem(0);
+                open[j] = v0 + 32 * j >= a.V ? 0u : mask ? __ldcg(mask + size_t(t) * a.mask_words + (v0 >> 5) + j) : 0xffffffffu;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int32_t v = v0 + 32 * j + lane;
+                const bool in = v < a.V, may = (open[j] >> lane) & 1;
+                const float x = in && may && !((special[j] >> lane) & 1) ? E::get(y[j]) : -INFINITY;
+                if (x > best[t]) {
+                    best[t] = x;
+                    where[t] = uint32_t(v) | kExact;
+                }
+                if (out && in) out[t * a.ot + v] = may ? y[j] : E::put(-INFINITY);
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < P; ++t) {
+        const uint32_t mine = order_of(best[t]), all = __reduce_max_sync(kFull, mine);
+        if (all <= kNothing) continue;
+        uint32_t id = 0xffffffffu;
+        if (mine == all) {
+            id = where[t] & ~kExact;
+            if (!(where[t] & kExact)) {  // which of the vector: it is read again
+                const int32_t v = int32_t(where[t]);
+                const uint32_t may = (mask ? open_of(t, v) : 0xffu) & ~(a.marks ? special_of(part.place_of(v)) : 0u);
+                elem y[N];
+                *reinterpret_cast<uint4 *>(y) = *reinterpret_cast<const uint4 *>(row + t * a.st + v);
+#pragma unroll
+                for (int j = N - 1; j >= 0; --j)
+                    if (((may >> j) & 1) && E::get(y[j]) == best[t]) id = uint32_t(v + j);
+            }
+        }
+        id = __reduce_min_sync(kFull, id);
+        if (lane == 0) atomicMax(&s_best[t], static_cast<unsigned long long>(best_key(all, id)));
     }
 }
 
@@ -271,15 +402,12 @@ template <int DT>
 __global__ void __launch_bounds__(kLogitThreads, 4) logits_kernel(const LogitArgs a) {
     using E = Elem<DT>;
     using elem = typename E::type;
-    constexpr int N = 16 / int(sizeof(elem));             // elements of a vector
-    constexpr int kUnit = kWarp * N;                      // tokens of a unit
     __shared__ unsigned long long s_best[kLogitGroup];
     __shared__ uint4 s_lut[DT == SWITCHSD_F32 ? 1 : 256];
     __shared__ int s_last;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     const int b = blockIdx.z, t0 = int(blockIdx.y) * kLogitGroup, parts = int(gridDim.x);
     const Part part{a.V, int(blockIdx.x), a.parts_log};
-    auto token_at = [&](int l) { return part.token_at(l); };
     if (tid < kLogitGroup) s_best[tid] = 0;
     if (DT != SWITCHSD_F32 && tid < 256) {
         auto pair = [&](int i) { return ((tid >> i) & 1 ? 0xffffu : 0u) | ((tid >> (i + 1)) & 1 ? 0xffff0000u : 0u); };
@@ -295,103 +423,17 @@ __global__ void __launch_bounds__(kLogitThreads, 4) logits_kernel(const LogitArg
     const elem *rows = reinterpret_cast<const elem *>(a.logits) + int64_t(b) * a.sb;
     elem *outs = a.out ? reinterpret_cast<elem *>(a.out) + int64_t(b) * a.ob : nullptr;
     const uint32_t *masks = a.mask ? a.mask + size_t(b) * a.T * a.mask_words : nullptr;
-    const uint32_t *bits = a.bits + (size_t(b) * parts + part.part) * (a.slice / 32);
-    const int units = part.used() / kUnit;                // of a position
-    for (int t = t0; t < t1; ++t) {
-        const elem *row = rows + int64_t(t) * a.st;
-        elem *out = outs ? outs + int64_t(t) * a.ot : nullptr;
-        const uint32_t *mask = masks ? masks + size_t(t) * a.mask_words : nullptr;
-        // whether a unit is read (and written) by vectors; else 32 neighbours at a time
-        const bool vectors = ((reinterpret_cast<uintptr_t>(row) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-        uint32_t top = kNothing, top_id = 0;  // the warp's best so far
-        for (int u0 = warp; u0 < units; u0 += kLogitUnits * kLogitWarps) {
-            auto whole = [&](int u) { return vectors && u < units && token_at(u * kUnit) + kUnit <= a.V; };
-            {
-                // lane l of unit i: N tokens from token_at(u kUnit) + l N on
-                uint4 w[kLogitUnits];
-                uint32_t allow[kLogitUnits];
-                float mx[kLogitUnits];
-#pragma unroll
-                for (int i = 0; i < kLogitUnits; ++i) {
-                    const int u = u0 + i * kLogitWarps;
-                    const int32_t v = token_at(u * kUnit) + lane * N;
-                    w[i] = make_uint4(0, 0, 0, 0);
-                    allow[i] = 0;
-                    if (whole(u)) {
-                        w[i] = *reinterpret_cast<const uint4 *>(row + v);
-                        allow[i] = mask ? uint32_t(reinterpret_cast<const uint8_t *>(mask)[v >> 3]) >> (v & 7) : 0xffu;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < kLogitUnits; ++i) {
-                    mx[i] = -INFINITY;
-                    if (!whole(u0 + i * kLogitWarps)) continue;
-                    const int l = (u0 + i * kLogitWarps) * kUnit + lane * N;
-                    const uint32_t special = a.marks ? uint32_t(reinterpret_cast<const uint8_t *>(bits)[l >> 3]) >> (l & 7) : 0u;
-                    if (out) {
-                        const uint4 y = mask ? E::keep(w[i], allow[i], s_lut) : w[i];
-                        *reinterpret_cast<uint4 *>(out + token_at((u0 + i * kLogitWarps) * kUnit) + lane * N) = y;
-                    }
-                    w[i] = E::keep(w[i], allow[i] & ~special, s_lut);
-                    mx[i] = E::largest(w[i]);
-                }
-                float most = mx[0];
-#pragma unroll
-                for (int i = 1; i < kLogitUnits; ++i) most = fmaxf(most, mx[i]);
-                const uint32_t mine = order_of(most), all = __reduce_max_sync(kFull, mine);
-                if (all > top) {  // a warp's tokens come in order, so only a larger value is better
-                    uint32_t id = 0xffffffffu;
-                    if (mine == all) {
-#pragma unroll
-                        for (int i = kLogitUnits - 1; i >= 0; --i)
-                            if (mx[i] == most) {
-                                elem y[N];
-                                *reinterpret_cast<uint4 *>(y) = w[i];
-                                const int32_t v = token_at((u0 + i * kLogitWarps) * kUnit) + lane * N;
-#pragma unroll
-                                for (int j = N - 1; j >= 0; --j)
-                                    if (E::get(y[j]) == most) id = uint32_t(v + j);
-                            }
-                    }
-                    top = all;
-                    top_id = __reduce_min_sync(kFull, id);
-                }
-            }
-            if (!whole(min(units - 1, u0 + (kLogitUnits - 1) * kLogitWarps))) {
-                // a row off the 16-byte boundaries, or the vocabulary's last tokens: lane l has tokens v0 + 32 j + l
-                for (int u = u0; u < min(units, u0 + kLogitUnits * kLogitWarps); u += kLogitWarps) {
-                    if (whole(u)) continue;
-                    const int32_t v0 = token_at(u * kUnit);
-                    elem y[N];
-                    uint32_t allow[N];
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const int32_t v = v0 + 32 * j + lane;
-                        y[j] = v < a.V ? row[v] : elem(0);
-                        allow[j] = v0 + 32 * j >= a.V ? 0u : mask ? mask[(v0 >> 5) + j] : 0xffffffffu;
-                    }
-                    float best = -INFINITY;
-                    uint32_t best_id = 0xffffffffu;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const int32_t v = v0 + 32 * j + lane;
-                        const bool in = v < a.V, may = (allow[j] >> lane) & 1;
-                        const float x = in && may && !(a.marks && ((bits[u * (kUnit / 32) + j] >> lane) & 1)) ? E::get(y[j]) : -INFINITY;
-                        if (x > best) {
-                            best = x;
-                            best_id = uint32_t(v);
-                        }
-                        if (out && in) out[v] = may ? y[j] : E::put(-INFINITY);
-                    }
-                    const uint32_t mine = order_of(best), all = __reduce_max_sync(kFull, mine);
-                    if (all > top) {
-                        top = all;
-                        top_id = __reduce_min_sync(kFull, mine == all ? best_id : 0xffffffffu);
-                    }
-                }
-            }
-        }
-        if (lane == 0 && top > kNothing) atomicMax(&s_best[t - t0], static_cast<unsigned long long>(best_key(top, top_id)));
+    {
+        const uint32_t *bits = a.bits + (size_t(b) * parts + part.part) * (a.slice / 32);
+        const elem *row = rows + t0 * a.st;
+        elem *out = outs ? outs + t0 * a.ot : nullptr;
+        const uint32_t *mask = masks ? masks + size_t(t0) * a.mask_words : nullptr;
+        if (t1 - t0 > 2)
+            stream_part<DT, 4>(a, part, t1 - t0, row, out, mask, bits, s_lut, s_best);
+        else if (t1 - t0 == 2)
+            stream_part<DT, 2>(a, part, 2, row, out, mask, bits, s_lut, s_best);
+        else
+            stream_part<DT, 1>(a, part, 1, row, out, mask, bits, s_lut, s_best);
     }
     if (a.marks) {
         if (outs) __syncthreads();  // the specials' results go over what the vectors wrote in their places
@@ -449,16 +491,22 @@ __global__ void __launch_bounds__(kLogitThreads, 4) logits_kernel(const LogitArg
     }
 }
 
-// The parts: two CTAs of the counting kernel an SM by shared memory, at least.
-static int parts_log_of(int32_t V) { return V > 131072 ? 4 : V > 8192 ? 3 : 2; }
-static int32_t slice_of(int32_t V) {
-    const int parts = 1 << parts_log_of(V);
-    return ((V + kChunk - 1) / kChunk + parts - 1) / parts * kChunk;
+#ifndef PT
+#define PT 128
+#endif
+// log2 of the parts: enough that the shared memory of a part of the vocabulary leaves an SM two counting CTAs, and, where
+// rows are few, more -- as long as each part has a chunk.
+static int parts_log_of(int32_t V, int32_t B) {
+    int log = V > 131072 ? 4 : V > 8192 ? 3 : 2;
+    while ((int64_t(B) << (log + 1)) <= PT && (kChunk << (log + 1)) <= V) ++log;
+    return log;
 }
+static int32_t slice_of(int32_t V, int log) { return (((V + kChunk - 1) / kChunk + (1 << log) - 1) >> log) * kChunk; }
 
 // The workspace: sizes of its arrays, and their places after `base`.
 static size_t logits_layout(const switchsd_logits_params *p, LogitArgs *a) {
-    const size_t B = size_t(p->B), parts = size_t(1) << parts_log_of(p->V), slice = size_t(slice_of(p->V));
+    const int log = parts_log_of(p->V, p->B);
+    const size_t B = size_t(p->B), parts = size_t(1) << log, slice = size_t(slice_of(p->V, log));
     const size_t groups = (size_t(p->T) + kLogitGroup - 1) / kLogitGroup;
     const bool marks = p->rep || p->freq || p->pres || p->nbias;
     // a part has no more specials than tokens, nor than the context, the draft and the biases name
@@ -466,6 +514,8 @@ static size_t logits_layout(const switchsd_logits_params *p, LogitArgs *a) {
     const size_t entries = marks ? std::min(slice, named) : 0;
     uint8_t *at = nullptr;
     if (a) {
+        a->parts_log = log;
+        a->slice = int32_t(slice);
         a->groups = int32_t(groups);
         a->entries = int32_t(entries);
         a->marks = marks && entries > 0;
@@ -564,8 +614,6 @@ extern "C" int switchsd_logits(const switchsd_logits_params *p) {
     a.mask_words = p->mask_words;
     if (p->workspace_bytes < logits_layout(p, &a)) return SWITCHSD_ERR_ARG;
     if (a.groups > 65535) return SWITCHSD_ERR_SHAPE;
-    a.parts_log = parts_log_of(p->V);
-    a.slice = slice_of(p->V);
     a.hash_mask = 0;
     if (p->nbias) {
         uint32_t places = 2;

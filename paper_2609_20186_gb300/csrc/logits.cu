@@ -26,6 +26,7 @@
 namespace switchsd {
 
 constexpr int kCountThreads = 512;
+constexpr int kCountFlight = 4;             // vectors of four tokens of a thread in flight
 constexpr int kLogitThreads = 256;
 constexpr int kLogitWarps = kLogitThreads / kWarp;
 constexpr int kLogitGroup = 4;              // positions of a CTA
@@ -62,10 +63,9 @@ struct LogitArgs {
 // Which tokens a part has: token v is in chunk v / kChunk, chunk c in part c % parts.
 struct Part {
     int32_t V, part, log;
-    __device__ int place_of(int32_t v) const {  // -1: outside the vocabulary or another part's
-        const uint32_t ch = uint32_t(v) / kChunk;
-        return uint32_t(v) < uint32_t(V) && (ch & ((1u << log) - 1)) == uint32_t(part) ? int(((ch >> log) * kChunk) | (uint32_t(v) & (kChunk - 1))) : -1;
-    }
+    __device__ bool has(int32_t v) const { return ((uint32_t(v) / kChunk) & ((1u << log) - 1)) == uint32_t(part); }
+    __device__ int place_of(int32_t v) const { return int(((uint32_t(v) / kChunk) >> log) * kChunk | (uint32_t(v) & (kChunk - 1))); }
+    __device__ int find(int32_t v) const { return uint32_t(v) < uint32_t(V) && has(v) ? place_of(v) : -1; }  // -1: not here
     __device__ int32_t token_at(int l) const { return ((((l / kChunk) << log) + part) * kChunk) | (l & (kChunk - 1)); }
     // places in use: every one below it names a token, but for the vocabulary's last chunk
     __device__ int used() const {
@@ -155,7 +155,7 @@ __device__ __forceinline__ uint32_t bias_hash(uint32_t id) { return (id * 0x9E37
 // Shared memory of the counting kernel, in words.
 static size_t count_words(int32_t slice, uint32_t hash_places) { return size_t(slice) + size_t(slice) / 32 + 2 * size_t(hash_places); }
 
-__global__ void __launch_bounds__(kCountThreads) logits_count_kernel(const LogitArgs a) {
+__global__ void __launch_bounds__(kCountThreads, 3) logits_count_kernel(const LogitArgs a) {
     extern __shared__ __align__(16) uint32_t smem[];
     __shared__ int32_t s_warp[kCountThreads / kWarp];
     const uint32_t places = a.nbias ? a.hash_mask + 1 : 0;
@@ -175,9 +175,19 @@ __global__ void __launch_bounds__(kCountThreads) logits_count_kernel(const Logit
     __syncthreads();
     pdl_wait();
     pdl_trigger();
+    // What a row needs to know is read together, and its first tokens with it (the places are the row's, filled or not).
     int32_t L;
     bool ok;
     const int nw = row_positions(a, b, L, ok);
+    const float rep = a.rep ? __ldcg(a.rep + b) : 1.f, freq = a.freq ? __ldcg(a.freq + b) : 0.f, pres = a.pres ? __ldcg(a.pres + b) : 0.f;
+    const int32_t first = a.prompt ? __ldcg(a.prompt + b) : 0;
+    const int32_t *ctx = a.ctx + size_t(b) * size_t(a.cap);
+    auto fetch = [&](int i, int end) { return i < end ? __ldcg(reinterpret_cast<const int4 *>(ctx + i)) : make_int4(-1, -1, -1, -1); };
+    int4 next[kCountFlight];
+#pragma unroll
+    for (int k = 0; k < kCountFlight; ++k) next[k] = fetch(4 * (tid + k * kCountThreads), a.marks ? a.cap : 0);
+    int32_t draft = a.draft && tid < a.T - 1 ? __ldcg(a.draft + size_t(b) * a.draft_stride + tid) : -1;
+    int32_t biased = tid < a.nbias ? __ldcg(a.bias_ids + size_t(b) * a.nbias + tid) : -1;
     if (part.part == 0) {
         if (tid == 0 && a.status) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
         for (int t = tid; t < a.T; t += kCountThreads) {
@@ -187,39 +197,43 @@ __global__ void __launch_bounds__(kCountThreads) logits_count_kernel(const Logit
         for (int g = tid; g < a.groups; g += kCountThreads) a.done[size_t(b) * a.groups + g] = 0;
     }
     if (!a.marks || nw == 0) return;
-    const float rep = a.rep ? __ldcg(a.rep + b) : 1.f, freq = a.freq ? __ldcg(a.freq + b) : 0.f, pres = a.pres ? __ldcg(a.pres + b) : 0.f;
     if (rep != 1.f || freq != 0.f || pres != 0.f) {
-        const int32_t *x = a.ctx + size_t(b) * size_t(a.cap);
-        const int32_t first = a.prompt ? __ldcg(a.prompt + b) : 0;
-#pragma unroll 4
-        for (int i = 4 * tid; i < L; i += 4 * kCountThreads) {
-            const int4 r = __ldcg(reinterpret_cast<const int4 *>(x + i));
-            const int32_t id[4] = {r.x, r.y, r.z, r.w};
+        for (int i0 = 4 * tid; i0 < L; i0 += 4 * kCountThreads * kCountFlight) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int at = part.place_of(id[e]);
-                if (at >= 0 && i + e < L) {
-                    if (i + e < first)
-                        atomicOr(&cnt[at], kSeen);
-                    else
-                        atomicAdd(&cnt[at], 1u);
+            for (int k = 0; k < kCountFlight; ++k) {
+                const int i = i0 + 4 * k * kCountThreads;
+                if (i >= L) break;
+                const int32_t id[4] = {next[k].x, next[k].y, next[k].z, next[k].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (!part.has(id[e])) continue;
+                    const int at = part.place_of(id[e]);
+                    if (uint32_t(id[e]) < uint32_t(a.V) && i + e < L) {
+                        if (i + e < first)
+                            atomicOr(&cnt[at], kSeen);
+                        else
+                            atomicAdd(&cnt[at], 1u);
+                    }
                 }
             }
+#pragma unroll
+            for (int k = 0; k < kCountFlight; ++k) next[k] = fetch(i0 + 4 * kCountThreads * (kCountFlight + k), L);
         }
         if (a.draft)
             for (int i = tid; i < nw - 1; i += kCountThreads) {
-                const int at = part.place_of(__ldcg(a.draft + size_t(b) * a.draft_stride + i));
+                if (i != tid) draft = __ldcg(a.draft + size_t(b) * a.draft_stride + i);
+                const int at = part.find(draft);
                 if (at >= 0) atomicOr(&cnt[at], kInDraft);
             }
     }
     for (int i = tid; i < a.nbias; i += kCountThreads) {
-        const int32_t id = __ldcg(a.bias_ids + size_t(b) * a.nbias + i);
-        const int at = part.place_of(id);
+        if (i != tid) biased = __ldcg(a.bias_ids + size_t(b) * a.nbias + i);
+        const int at = part.find(biased);
         if (at < 0) continue;
         // at most half of the places are taken, so the search ends; the last entry that names the token stays
-        for (uint32_t p = bias_hash(uint32_t(id)) & a.hash_mask;; p = (p + 1) & a.hash_mask) {
-            const int32_t was = atomicCAS(&keys[p], -1, id);
-            if (was == -1 || was == id) {
+        for (uint32_t p = bias_hash(uint32_t(biased)) & a.hash_mask;; p = (p + 1) & a.hash_mask) {
+            const int32_t was = atomicCAS(&keys[p], -1, biased);
+            if (was == -1 || was == biased) {
                 atomicMax(&vals[p], i + 1);
                 break;
             }

@@ -98,6 +98,7 @@ size_t switchsd_kv4_bytes(int32_t page, int32_t D);
  *   slots       int32 [B, T]: as switchsd_kv_map writes them -- a row's slots are consecutive inside a page and begin
  *               a page at its first slot, and -1 past the row's new tokens.  Slots outside [0, pages * page) are
  *               skipped.
+ *   B * T < 2^31, B * (T / 8 + 2) * Hkv < 2^30 (here and for the read)
  * Calls that write into one page must not overlap on the GPU (eight tokens share a word).
  */
 typedef struct {

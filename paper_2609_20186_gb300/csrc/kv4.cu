@@ -7,11 +7,18 @@
 // 32 lanes by halves -- a lane hands on the half of the tokens that it does not keep --, so that each lane ends with one
 // token's and works out one scale.
 //
-// One extreme is enough for a scale: max(pos / 7, neg / 8) is max(8 pos, 7 neg) / 56, where the products are exact.  A
-// code is the rounded quotient x / s: x times the reciprocal, corrected once by its remainder (x has at most 11 bits and s
-// 7, so the remainder is exact, and a quotient that lies half-way between two codes comes out as it is).
+// A scale goes by one number a group, max(8 pos, 7 neg) / 56 = max(pos / 7, neg / 8), where the products are exact; the
+// maximum and minimum are taken of packed pairs, as they come.
 //
-// What bounds it: memory, 2 bytes read and 0.53 written a value, with about 10 instructions a value.
+// A code is x / s rounded half to even, from x times the reciprocal.  x has at most 11 significant bits and s 7, so a
+// quotient that is not half-way between two codes is 2^-12 or more off: rounded to a multiple of 2^-15 first, which takes
+// the reciprocal's error away, it stays on its side, and one that is half-way comes out as it is.  Both roundings are
+// additions, of 1.5 * 2^8 in the product's instruction and of 1.5 * 2^23 in one more, which leaves the code in the low
+// bits; eight of those words times powers of 16 add up to a cache word and a known constant.
+//
+// What bounds it: memory, 2 bytes read and 0.53 written a value (and the other way round for the read), and instructions,
+// about 10 a value.  16 rows of 2048 tokens, 8 heads of 128 dimensions: append and read take 84 us, where the bytes alone
+// would take 50; of 1 to 2048 tokens each 60 us.  A divided quotient and its comparisons took 94 us for the latter.
 #include <cuda_bf16.h>
 
 #include "kv4.cuh"
@@ -25,7 +32,7 @@ struct AppendArgs {
     int64_t ks[3], vs[3];  // strides in elements: row, token, head
     const int32_t *slots;
     uint8_t *cache;
-    int64_t units;         // B * units_per_row * Hkv
+    uint32_t units;        // B * units_per_row * Hkv, below 2^30
     int32_t T, Hkv, units_per_row, page_shift, total;  // total: pages * page slots
 };
 
@@ -33,7 +40,7 @@ struct ReadArgs {
     const uint8_t *cache;
     const int32_t *slots;
     uint8_t *k, *v;        // f16 [B][T][Hkv][D]
-    int64_t units;
+    uint32_t units;
     int32_t T, Hkv, units_per_row, page_shift, total;
 };
 
@@ -43,13 +50,13 @@ struct Unit {
     int32_t h, t0;
 };
 template <class Args>
-__device__ __forceinline__ Unit unit_of(const Args &a, int64_t unit) {
+__device__ __forceinline__ Unit unit_of(const Args &a, uint32_t unit) {
     Unit u;
-    u.h = int32_t(unit % a.Hkv);
-    const int64_t rest = unit / a.Hkv;
-    u.b = rest / a.units_per_row;
+    const uint32_t rest = unit / uint32_t(a.Hkv);
+    u.h = int32_t(unit - rest * uint32_t(a.Hkv));
+    u.b = rest / uint32_t(a.units_per_row);
     // Blocks begin where the first token's does: unit i has tokens [8 i - a0, 8 i - a0 + 8), a0 its place in the block.
-    u.t0 = 8 * int32_t(rest % a.units_per_row) - (__ldcg(a.slots + u.b * a.T) & 7);
+    u.t0 = 8 * int32_t(rest - uint32_t(u.b) * uint32_t(a.units_per_row)) - (__ldcg(a.slots + u.b * a.T) & 7);
     return u;
 }
 // The slot of token t, -1 where there is none.
@@ -66,15 +73,37 @@ __device__ __forceinline__ float2 widen(uint32_t w) {
     return make_float2(bf16_lo(w), bf16_hi(w));
 }
 
-// max that keeps a NaN.
+// The larger and the smaller of two pairs; a NaN stays.
+template <bool F16>
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if (F16)
+        asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if (F16)
+        asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else
+        asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 
-// What x adds to its group's extreme: max(8 x, -7 x).
-__device__ __forceinline__ float extreme_of(float m, float x) { return max_nan(max_nan(m, 8.f * x), -7.f * x); }
+// max(8 pos, 7 neg) of values whose pairs' maximum and minimum are hi and lo.
+template <bool F16>
+__device__ __forceinline__ float extreme_of(uint32_t hi, uint32_t lo) {
+    const float2 h = widen<F16>(hi), l = widen<F16>(lo);
+    return max_nan(max_nan(8.f * max_nan(h.x, h.y), 7.f * max_nan(-l.x, -l.y)), 0.f);
+}
 
 // The group's stored scale from its extreme (>= 0 or NaN): rounded up to 7 significant bits.  The division is exact where
 // the quotient has 7 bits, so that the rounding never lifts such a scale.
@@ -84,39 +113,36 @@ __device__ __forceinline__ __half group_scale(float m) {
     return __float2half_rn(__uint_as_float((__float_as_uint(s) + 0x1ffffu) & ~0x1ffffu));
 }
 
-// A group's scale and its reciprocal for the codes: zeros, and so codes of 8, where it is 0 or NaN.  Only a group that
-// is `wide` can hold an infinity, a NaN or a value beyond the largest scale's reach.
+// A group's scale and its reciprocal for the codes: zeros, and so codes of 8, where it is 0 or NaN.  Only in a group whose
+// scale was cut off at the largest, lost bits among f16's smallest, or is NaN can a quotient lie outside [-8, 7]: `wide`.
 struct Scale {
     float s, r;
     bool wide;
     __device__ explicit Scale(__half h) : s(__half2float(h)), r(0.f) {
-        wide = !(s < kScaleMax);
+        wide = !(s < kScaleMax && (s >= 0x1p-17f || s == 0.f));
         if (s > 0.f)
             r = __frcp_rn(s);
         else
             s = 0.f;
     }
+    // x inside what the codes reach, for a wide group
+    __device__ float within(float x) const { return fminf(fmaxf(x, -8.f * s), 7.f * s); }
 };
 
-// The code of x in bits 0 .. 3 (the bits above are not clean).
-__device__ __forceinline__ uint32_t code_of(float x, const Scale &k) {
-    const float q = x * k.r;
-    const float t = fmaf(fmaf(-q, k.s, x), k.r, q);
-    return __float_as_uint(fminf(fmaxf(t, -8.f), 7.f) + 12582920.f);  // 1.5 * 2^23 + 8: rounds to even, code in the low bits
-}
-// An infinity has no remainder: a wide group's values are cut to finite ones first, beyond the largest scale's reach.
-__device__ __forceinline__ float within(float x) { return fminf(fmaxf(x, -65536.f), 65536.f); }
-
+// A word of codes from the scaled values, an element at a time: nibble_of(j) is element j's.
 __device__ __forceinline__ constexpr int nibble_of(int j) { return (j >> 1) + 4 * (j & 1); }
-// `w` with code c (its low 4 bits) as element j.
-__device__ __forceinline__ uint32_t put_code(uint32_t w, uint32_t c, int j) { return w | ((c & 15u) << (4 * nibble_of(j))); }
+constexpr uint32_t kCodeBits = 0x4b400000u;  // 1.5 * 2^23: the bits of 1.5 * 2^23 + c are kCodeBits + c
+// x's code, its bits on top of kCodeBits
+__device__ __forceinline__ uint32_t code_of(float x, float r) { return __float_as_uint(fmaf(x, r, 384.f) + (12582912.f + 8.f - 384.f)); }
+__device__ __forceinline__ uint32_t put_code(uint32_t w, uint32_t c, int j) { return w + c * (1u << (4 * nibble_of(j))); }
+constexpr uint32_t kNoBits = 0u - kCodeBits * 0x11111111u;  // a word of eight codes begins with it
 
 template <bool F16, int D>
 __global__ void __launch_bounds__(kUnitThreads) kv4_append_kernel(const AppendArgs a) {
     using L = Kv4<D>;
     constexpr int G = L::G;
     const int lane = threadIdx.x & 31;
-    const int64_t job = int64_t(blockIdx.x) * (kUnitThreads / kWarp) + (threadIdx.x >> 5);
+    const uint32_t job = blockIdx.x * (kUnitThreads / kWarp) + (threadIdx.x >> 5);
     pdl_wait();
     pdl_trigger();
     if (job >= 2 * a.units) return;
@@ -142,31 +168,28 @@ __global__ void __launch_bounds__(kUnitThreads) kv4_append_kernel(const AppendAr
         __half scales[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            float x[16], m = 0.f;
+            const uint32_t v[8] = {raw[g][0].x, raw[g][0].y, raw[g][0].z, raw[g][0].w, raw[g][1].x, raw[g][1].y, raw[g][1].z, raw[g][1].w};
+            uint32_t hi = v[0], lo = v[0];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t w[4] = {raw[g][i].x, raw[g][i].y, raw[g][i].z, raw[g][i].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = widen<F16>(w[e]);
-                    x[8 * i + 2 * e] = f.x;
-                    x[8 * i + 2 * e + 1] = f.y;
-                    m = extreme_of(extreme_of(m, f.x), f.y);
-                }
+            for (int e = 1; e < 8; ++e) {
+                hi = max_pair<F16>(hi, v[e]);
+                lo = min_pair<F16>(lo, v[e]);
             }
+            float m = extreme_of<F16>(hi, lo);
             m = max_nan(m, __shfl_xor_sync(kFull, m, 1));
             m = max_nan(m, __shfl_xor_sync(kFull, m, 2));
             scales[g] = group_scale(m);
             const Scale k(scales[g]);
-            if (__any_sync(kFull, k.wide)) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = within(x[e]);
-            }
+            const bool wide = __any_sync(kFull, k.wide);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                uint32_t w = 0;
+                uint32_t w = kNoBits;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w = put_code(w, code_of(x[8 * i + e], k), e);
+                for (int e = 0; e < 4; ++e) {
+                    float2 f = widen<F16>(v[4 * i + e]);
+                    if (wide) f = make_float2(k.within(f.x), k.within(f.y));
+                    w = put_code(put_code(w, code_of(f.x, k.r), 2 * e), code_of(f.y, k.r), 2 * e + 1);
+                }
                 words[2 * g + i] = w;
             }
         }
@@ -212,12 +235,8 @@ __global__ void __launch_bounds__(kUnitThreads) kv4_append_kernel(const AppendAr
     float m[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float2 f = widen<F16>(raw[e].x);
-        m[e] = extreme_of(extreme_of(0.f, f.x), f.y);
-        if (N == 4) {
-            const float2 f2 = widen<F16>(raw[e].y);
-            m[e] = extreme_of(extreme_of(m[e], f2.x), f2.y);
-        }
+        m[e] = N == 4 ? extreme_of<F16>(max_pair<F16>(raw[e].x, raw[e].y), min_pair<F16>(raw[e].x, raw[e].y))
+                      : extreme_of<F16>(raw[e].x, raw[e].x);
     }
     // by halves: after the three exchanges a lane has the token of its three highest bits in the group
 #pragma unroll
@@ -239,9 +258,10 @@ __global__ void __launch_bounds__(kUnitThreads) kv4_append_kernel(const AppendAr
     }
     const Scale own(mine);
     const bool wide = __any_sync(kFull, own.wide);
+    // Tokens that are not in get codes of 0 here: what is there stays.
     uint32_t words[N], keep = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) words[i] = 0;
+    for (int i = 0; i < N; ++i) words[i] = kNoBits;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         Scale k = own;
@@ -249,13 +269,11 @@ __global__ void __launch_bounds__(kUnitThreads) kv4_append_kernel(const AppendAr
         k.s = __shfl_sync(kFull, own.s, from);
         k.r = __shfl_sync(kFull, own.r, from);
         const float2 f = widen<F16>(raw[e].x), f2 = widen<F16>(raw[e].y);
-        float x[4] = {f.x, f.y, f2.x, f2.y};
-        if ((in >> e) & 1) {
+        const float x[4] = {f.x, f.y, f2.x, f2.y};
+        const bool is_in = (in >> e) & 1;
+        if (!is_in) keep |= 0xfu << (4 * nibble_of(e));
 #pragma unroll
-            for (int i = 0; i < N; ++i) words[i] = put_code(words[i], code_of(wide ? within(x[i]) : x[i], k), e);
-        } else {
-            keep |= 0xfu << (4 * nibble_of(e));
-        }
+        for (int i = 0; i < N; ++i) words[i] = put_code(words[i], is_in ? code_of(wide ? k.within(x[i]) : x[i], k.r) : kCodeBits, e);
     }
     uint8_t *dst = head_of(base) + L::values(page) + size_t((base & (page - 1)) >> 3) * L::kBlock + 4 * N * lane;
     if (N == 4) {
@@ -293,7 +311,7 @@ __global__ void __launch_bounds__(kUnitThreads) kv4_read_kernel(const ReadArgs a
     using L = Kv4<D>;
     constexpr int G = L::G;
     const int lane = threadIdx.x & 31;
-    const int64_t job = int64_t(blockIdx.x) * (kUnitThreads / kWarp) + (threadIdx.x >> 5);
+    const uint32_t job = blockIdx.x * (kUnitThreads / kWarp) + (threadIdx.x >> 5);
     pdl_wait();
     pdl_trigger();
     if (job >= 2 * a.units) return;
@@ -388,14 +406,15 @@ extern "C" int switchsd_kv4_append(const switchsd_kv4_append_params *p) {
     a.cache = static_cast<uint8_t *>(p->cache);
     a.T = p->T;
     a.Hkv = p->Hkv;
-    a.units_per_row = (p->T - 1 + 7) / 8 + 1;  // the first block may hold one of the row's tokens only
-    a.units = int64_t(p->B) * a.units_per_row * p->Hkv;
+    a.units_per_row = int32_t((int64_t(p->T) + 6) / 8 + 1);  // the first block may hold one of the row's tokens only
+    const int64_t units = int64_t(p->B) * a.units_per_row;
+    if (units >= (int64_t(1) << 30) || units * p->Hkv >= (int64_t(1) << 30)) return SWITCHSD_ERR_SHAPE;
+    a.units = uint32_t(units) * uint32_t(p->Hkv);
     a.page_shift = log2_of(p->page);
     a.total = p->pages * p->page;
-    const int64_t ctas = (2 * a.units + kUnitThreads / kWarp - 1) / (kUnitThreads / kWarp);
-    if (ctas > 0x7fffffff) return SWITCHSD_ERR_SHAPE;
+    const uint32_t ctas = (2 * a.units + kUnitThreads / kWarp - 1) / (kUnitThreads / kWarp);
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);
-    const dim3 grid{unsigned(ctas)}, block{unsigned(kUnitThreads)};
+    const dim3 grid{ctas}, block{unsigned(kUnitThreads)};
     cudaError_t e;
     if (p->dtype == SWITCHSD_F16)
         e = p->D == 128 ? launch_pdl(kv4_append_kernel<true, 128>, grid, block, 0, s, 0u, a)
@@ -418,14 +437,15 @@ extern "C" int switchsd_kv4_read(const switchsd_kv4_read_params *p) {
     a.v = static_cast<uint8_t *>(p->out_v);
     a.T = p->T;
     a.Hkv = p->Hkv;
-    a.units_per_row = (p->T - 1 + 7) / 8 + 1;
-    a.units = int64_t(p->B) * a.units_per_row * p->Hkv;
+    a.units_per_row = int32_t((int64_t(p->T) + 6) / 8 + 1);
+    const int64_t units = int64_t(p->B) * a.units_per_row;
+    if (units >= (int64_t(1) << 30) || units * p->Hkv >= (int64_t(1) << 30)) return SWITCHSD_ERR_SHAPE;
+    a.units = uint32_t(units) * uint32_t(p->Hkv);
     a.page_shift = log2_of(p->page);
     a.total = p->pages * p->page;
-    const int64_t ctas = (2 * a.units + kUnitThreads / kWarp - 1) / (kUnitThreads / kWarp);
-    if (ctas > 0x7fffffff) return SWITCHSD_ERR_SHAPE;
+    const uint32_t ctas = (2 * a.units + kUnitThreads / kWarp - 1) / (kUnitThreads / kWarp);
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);
-    const dim3 grid{unsigned(ctas)}, block{unsigned(kUnitThreads)};
+    const dim3 grid{ctas}, block{unsigned(kUnitThreads)};
     const cudaError_t e = p->D == 128 ? launch_pdl(kv4_read_kernel<128>, grid, block, 0, s, 0u, a) : launch_pdl(kv4_read_kernel<64>, grid, block, 0, s, 0u, a);
     return e == cudaSuccess ? SWITCHSD_OK : SWITCHSD_ERR_CUDA;
 }

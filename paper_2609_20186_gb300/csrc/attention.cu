@@ -29,10 +29,7 @@ namespace switchsd {
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = kAttnWarps * kWarp;
 constexpr int kAttnUnit = kAttnWarps * 32;  // keys of a unit: 32 a warp
-#ifndef ATTN_OCC
-#define ATTN_OCC 3
-#endif
-constexpr int attn_ctas_per_sm(int NT) { return NT == 1 ? ATTN_OCC : 2; }
+constexpr int attn_ctas_per_sm(int NT) { return NT == 1 ? 3 : 2; }
 constexpr float kWeightLog = 12.f;          // log2 of the weight of a score (with its value's scale) at the reference
 constexpr float kLag = 3.f;                 // log2 of how far one may lie above: 2^15 is f16's
 constexpr float kSmall = 6.103515625e-5f;   // 2^-14: below it f16 loses bits

@@ -518,7 +518,7 @@ static cudaError_t launch_attn(AttnArgs a, int sms, cudaStream_t s) {
     const unsigned ctas = unsigned(std::min(kAttnMaxCtas, sms * attn_ctas_per_sm(NT)));
     e = launch_pdl(attn_kernel<F16, D, NT>, dim3(ctas), dim3(kAttnThreads), smem, s, 0u, a);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attn_join_kernel<F16, D>, dim3(ctas, 8 * NT), dim3(D), 0, s, 0u, a, 8 * NT);
+    return launch_join<F16, D>(a, int(ctas), 8 * NT, s);
 }
 
 constexpr int kTensorRows = 16;

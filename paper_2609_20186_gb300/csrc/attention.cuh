@@ -3,11 +3,14 @@
 
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "kv4.cuh"
 
 namespace switchsd {
 
 constexpr int kAttnMaxCtas = 1024;
+constexpr int kJoinParts = 4;     // partial results whose numbers are on their way together
 constexpr float kFloor = -1e30f;  // the maximum of nothing
 
 struct AttnArgs {
@@ -167,41 +170,77 @@ __device__ __forceinline__ uint16_t narrow1(float a) {
 }
 
 // Joins the partial results of the items that several CTAs hold: CTAs (i, .) look after the item whose first part is the
-// i-th CTA's, adding the parts in order.  R query rows a tile.
+// i-th CTA's, a CTA a query row and a thread a dimension, adding the parts in order.  R query rows a tile.  What bounds it:
+// latency, so the parts' number comes from their flags 32 at a time and their numbers kJoinParts at a time (one after the
+// other, with 16 CTAs for an item's rows, 68 rows of 17 parts each took 50 us with their attention; now 21 us).  CTAs of
+// 128 threads and 32 registers fit beside the attention's last ones; wider ones did not and cost 10 us of 280.
 template <bool F16, int D>
-__global__ void __launch_bounds__(D) attn_join_kernel(const AttnArgs a, int R) {
-    const int i = blockIdx.x, d = threadIdx.x, ctas = int(gridDim.x);
+__global__ void __launch_bounds__(D, 2048 / D) attn_join_kernel(const AttnArgs a, int R) {
+    const int i = blockIdx.x, d = threadIdx.x, lane = threadIdx.x & 31, ctas = int(gridDim.x);
     pdl_wait();
     pdl_trigger();
     int from = 2 * i + 1;
     int4 de = __ldcg(a.desc + from);
+    const int4 other = __ldcg(a.desc + 2 * i);
     if (de.x < 0 || !(de.w & kFirst)) {
         from = 2 * i;
-        de = __ldcg(a.desc + from);
+        de = other;
         if (de.x < 0 || !(de.w & kFirst)) return;
+    }
+    int n = 1;  // partial results of the item: this CTA's and the next ones' first, up to the one that holds the last unit
+    for (int c0 = i + 1; !(de.w & kLast);) {
+        const int c = c0 + lane;
+        const uint32_t last = __ballot_sync(kFull, c >= ctas || (__ldcg(&a.desc[2 * min(c, ctas - 1)].w) & kLast));
+        if (last) {
+            n = min(c0 + __ffs(int(last)), ctas) - i;
+            break;
+        }
+        c0 += 32;
     }
     int32_t len, nw;
     row_lengths(a, de.x, len, nw);
-    for (int row = blockIdx.y; row < R; row += int(gridDim.y)) {
+    for (int row = int(blockIdx.y); row < R; row += int(gridDim.y)) {
         const int rr = de.z * R + row, t = rr / a.group;
         if (t >= nw) return;
         float mx = kFloor, sum = 0.f, y = 0.f;
-        int next = i, slot = from;
-        for (int flags = de.w;;) {
-            const float *src = a.part + (size_t(slot) * R + row) * (D + 4);
-            const float pm = __ldcg(src + D), ps = __ldcg(src + D + 1), py = __ldcg(src + d);
-            const float mn = fmaxf(mx, pm), f0 = exp2_approx(mx - mn), f1 = exp2_approx(pm - mn);
-            y = y * f0 + py * f1;
-            sum = sum * f0 + ps * f1;
-            mx = mn;
-            if ((flags & kLast) || ++next >= ctas) break;
-            slot = 2 * next;
-            flags = __ldcg(&a.desc[slot].w);
+        for (int j0 = 0; j0 < n; j0 += kJoinParts) {
+            float pm[kJoinParts], ps[kJoinParts], py[kJoinParts], top = mx;
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) {
+                pm[j] = kFloor;
+                ps[j] = py[j] = 0.f;
+                if (j0 + j < n) {
+                    const float *src = a.part + (size_t(j0 + j ? 2 * (i + j0 + j) : from) * R + row) * (D + 4);
+                    pm[j] = __ldcg(src + D);
+                    ps[j] = __ldcg(src + D + 1);
+                    py[j] = __ldcg(src + d);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) top = fmaxf(top, pm[j]);
+            const float f0 = exp2_approx(mx - top);
+            y *= f0;
+            sum *= f0;
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) {
+                const float f = exp2_approx(pm[j] - top);
+                y = fmaf(py[j], f, y);
+                sum = fmaf(ps[j], f, sum);
+            }
+            mx = top;
         }
         const int h = de.y * a.group + rr - t * a.group;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         a.out[((size_t(de.x) * a.T + t) * a.Hq + h) * D + d] = narrow1<F16>(y * inv);
     }
+}
+
+// Joins the partial results of a grid of `ctas`, tiles of R query rows.
+template <bool F16, int D>
+inline cudaError_t launch_join(const AttnArgs &a, int ctas, int R, cudaStream_t s) {
+    const int64_t rows = std::min(int64_t(R), int64_t(a.T) * a.group);
+    const unsigned y = unsigned(std::min(int64_t(32), rows));
+    return launch_pdl(attn_join_kernel<F16, D>, dim3(unsigned(ctas), y), dim3(D), 0, s, 0u, a, R);
 }
 
 // The kernel for many query rows (attention_tc.cu): bytes of partial results, and the launch of it and of its join.

@@ -648,7 +648,7 @@ static cudaError_t launch(const AttnArgs &a, int sms, cudaStream_t s) {
     // an explicit one-CTA cluster: the MMA commit addresses shared::cluster
     e = launch_pdl(attn_tc_kernel<F16, D>, dim3(ctas), dim3(kTcThreads), size_t(TcSmem<D>::bytes), s, 1u, a);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attn_join_kernel<F16, D>, dim3(ctas, 16), dim3(D), 0, s, 0u, a, kTcRows);
+    return launch_join<F16, D>(a, int(ctas), kTcRows, s);
 }
 
 cudaError_t launch_attn_tc(const AttnArgs &a, bool f16, int D, int sms, cudaStream_t s) {

@@ -135,8 +135,9 @@ int switchsd_kv4_read(const switchsd_kv4_read_params *params);
  * Tokens t >= new, rows with bad lengths (negative, new outside [0, T], len + new > blocks * page: status
  * SWITCHSD_ROW_BAD_LEN) and tokens that see nothing get zeros.  The tokens of a page whose table entry lies outside
  * [0, pages) are not seen.  What the cache holds in places that a token does not see never reaches its result, NaN
- * among it.  Scores, the softmax's maximum and sum and the output's sum are held in binary32; the weights that multiply
- * the values are rounded to 11 bits.
+ * among it; a NaN that it does see makes its result NaN, in the value's 64 dimensions or, where a call has many query
+ * rows, in all of the head's.  Scores, the softmax's maximum and sum and the output's sum are held in binary32; the
+ * weights that multiply the values are rounded to 11 bits.
  *
  *   q             dtype (SWITCHSD_BF16 or SWITCHSD_F16) [B, T, Hq, D], strides in elements between rows, tokens and
  *                 heads (multiples of 8; a head's values are contiguous), 16-byte aligned

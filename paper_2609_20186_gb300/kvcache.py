@@ -23,7 +23,8 @@ class KVCache:
     def __init__(self, B: int, T: int, *, layers: int, heads: int, dim: int, pages: int, max_len: int, page: int = 64,
                  lens_add: int = 0, new_add: int = 0, device="cuda", stream: torch.cuda.Stream | None = None):
         """B rows of at most max_len tokens, T new tokens a step, `pages` pages of `page` tokens shared by the rows;
-        lens_add and new_add are added to the lengths that the calls take."""
+        lens_add and new_add are added to the lengths that the calls take.  `stream` (the current one of each call when
+        None) is the stream of the calls; what fills the buffers here is behind it."""
         size = bd.switchsd_kv4_bytes(page, dim)
         if size == 0:
             raise ValueError(f"no 4-bit cache has pages of {page} tokens and heads of {dim} dimensions")
@@ -38,6 +39,8 @@ class KVCache:
         self.slots = torch.full((B, T), -1, **i32)
         self.status = torch.zeros(B, **i32)
         self.workspace = None
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream(self.data.device))
         self._lens = self._new = None
 
     def map(self, lens: torch.Tensor, new: torch.Tensor) -> None:
@@ -55,7 +58,7 @@ class KVCache:
         """Attention of the new tokens' queries [B, T, query heads, dim] over `layer`, into `out`."""
         if self._lens is None:
             raise RuntimeError("map() comes before attend()")
-        if self.workspace is None:
+        if self.workspace is None:  # its size goes by the heads' dimensions alone
             self.workspace = torch.empty(bd.switchsd_kv4_attention_workspace(q, self.data[layer], self.table, page=self.page),
                                          dtype=torch.uint8, device=q.device)
         bd.switchsd_kv4_attention(q, self.data[layer], self.table, self._lens, self._new, out, page=self.page, scale=scale,

@@ -20,6 +20,11 @@
 // the reference, is at most 2^kLag below the running maximum of the score plus the logarithm of its value's scale, so
 // that the largest weight fits whatever the scales; what rounding leaves of weights below 2^-26 of the reference, where
 // f16 has fewer bits, is multiplied apart, 2^24 higher.
+//
+// What bounds it: the instructions that unpack codes and weigh scores, at 12 warps an SM, about 60 % of the issue slots.
+// Measured: 64 contexts of 8K to 32K tokens, 8 key heads of 128 dimensions, 4 query heads each, one token a row: 362 us,
+// 58 % of the time that the 1.4 GB of cache need alone; 4 contexts of 32K to 128K, 8 query heads each: 100 us (53 %); one
+// context of 2K: 11 us, with its join.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -29,6 +34,8 @@ namespace switchsd {
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = kAttnWarps * kWarp;
 constexpr int kAttnUnit = kAttnWarps * 32;  // keys of a unit: 32 a warp
+// As many CTAs an SM as leave a warp its registers (168; 8 query rows: 2 CTAs 451, 3 CTAs 362, 4 CTAs, which spill, 468 us
+// for the first figures above; 16 rows of 64 contexts of 8K: 1 CTA 558, 2 CTAs 295, 3 CTAs 459 us).
 constexpr int attn_ctas_per_sm(int NT) { return NT == 1 ? 3 : 2; }
 constexpr float kWeightLog = 12.f;          // log2 of the weight of a score (with its value's scale) at the reference
 constexpr float kLag = 3.f;                 // log2 of how far one may lie above: 2^15 is f16's
@@ -521,6 +528,10 @@ static cudaError_t launch_attn(AttnArgs a, int sms, cudaStream_t s) {
     return launch_join<F16, D>(a, int(ctas), 8 * NT, s);
 }
 
+// Query rows of a key head up to which the tiles of 8 or 16 are faster than those of 128, whose time does not depend on
+// how many are filled.  Measured on 64 contexts of 8K: 16 rows 295 us here and 385 us there, 20 rows (two tiles here) 571
+// and 387 us, 48 rows 851 and 396 us.  A tile of 8 rather than 16 for 8 rows and fewer: 4 rows, 64 contexts of 8K to 32K
+// tokens, 362 and 713 us.  The contexts' lengths are on the device, so the choice goes by the rows alone.
 constexpr int kTensorRows = 16;
 
 template <bool F16, int D>

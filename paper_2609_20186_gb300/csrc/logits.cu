@@ -12,10 +12,13 @@
 // Each value is worked out in binary32, one rounding an operation, in the header's order, and the best is a maximum of
 // (value, token), so nothing depends on the split or on who comes first.
 //
-// What bounds it: the second kernel reads the logits once (and writes them once), 2 or 4 bytes an element; the first
-// reads the context once a part.  One kernel that counted and then streamed all positions of a row and part took 126 us
-// where the two take 104 us (64 rows of 8K to 32K tokens, 1 to 17 positions, 128,256 tokens, masks and biases): it counted
-// while nothing streamed, and the rows' uneven positions left SMs idle at its end.
+// What bounds it: the instructions and latencies of both: the first looks at every token of the context once a part and
+// adds up in shared memory, the second has 2 or 4 bytes an element to read (and write).  Measured: 64 rows of 8K to 32K
+// tokens, 1 to 17 positions, 128,256 tokens, masks and biases: 92 us, 31 of them the counting (148 MB of logits are 22 us);
+// 16 rows of 32K to 128K, 1 to 33 positions, 152,064 tokens, written: 109 us; one row and position: 12 us.  Measured and
+// not kept: one kernel that counted and then streamed (126 us where the two took 104); the context cut over a cluster of
+// the parts, with remote additions (118 us where each part reading it whole takes 94); sending for the first logits while
+// the tokens are counted (no change).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -505,14 +508,13 @@ __global__ void __launch_bounds__(kLogitThreads, 4) logits_kernel(const LogitArg
     }
 }
 
-#ifndef PT
-#define PT 128
-#endif
 // log2 of the parts: enough that the shared memory of a part of the vocabulary leaves an SM two counting CTAs, and, where
-// rows are few, more -- as long as each part has a chunk.
+// rows are few, more, up to about a CTA an SM -- as long as each part has a chunk.  Measured with and without the latter:
+// one row and position 12 and 20 us (with 64K tokens of context 25 and 40 us), 4 rows of 1 to 17 positions 31 and 38 us.
+constexpr int kFewCtas = 128;
 static int parts_log_of(int32_t V, int32_t B) {
     int log = V > 131072 ? 4 : V > 8192 ? 3 : 2;
-    while ((int64_t(B) << (log + 1)) <= PT && (kChunk << (log + 1)) <= V) ++log;
+    while ((int64_t(B) << (log + 1)) <= kFewCtas && (kChunk << (log + 1)) <= V) ++log;
     return log;
 }
 static int32_t slice_of(int32_t V, int log) { return (((V + kChunk - 1) / kChunk + (1 << log) - 1) >> log) * kChunk; }

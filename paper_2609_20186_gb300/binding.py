@@ -8,6 +8,7 @@ the library's kernels.  If the library is missing the first call raises; there i
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 
@@ -525,6 +526,8 @@ def switchsd_copy_labels(ctx_tokens, ctx_lens, out_labels, *, n: int = 5, worksp
 # --- the target's side of a verification step (include/switchsd_target.h) -------------------------------------------
 def _strided(t: torch.Tensor, name: str, shape, dtypes) -> int:
     """Checks a CUDA tensor of `shape` whose last dimension is contiguous; returns its element type's code."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes and t.shape == shape and t.stride(-1) == 1:
+        return _DTYPES[t.dtype]  # the usual case, without a message to choose
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype not in dtypes:
@@ -544,21 +547,17 @@ def switchsd_kv_map(lens, new_lens, block_table, held, free_list, free_count, sl
     slots int32 [B, T] (or None, with T); status int32 [B] or None.
     """
     B, blocks = block_table.shape
-    p = switchsd_kv_map_params()
-    p.B, p.T, p.page, p.blocks = B, slots.shape[1] if slots is not None else int(T or 1), page, blocks
-    p.pages = free_list.shape[0]
-    p.lens, p.new_lens = _dev(lens, torch.int32, "lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,))
-    p.lens_add, p.new_add = lens_add, new_add
-    p.block_table = _dev(block_table, torch.int32, "block_table")
-    p.held = _dev(held, torch.int32, "held", (B,))
-    p.free_list = _dev(free_list, torch.int32, "free_list", (p.pages,))
-    p.free_count = _dev(free_count, torch.int32, "free_count", (1,))
-    p.slots = _dev(slots, torch.int32, "slots", (B, p.T))
-    p.status = _dev(status, torch.int32, "status", (B,))
-    p.stream = _stream_ptr(stream)
+    T, pages = slots.shape[1] if slots is not None else int(T or 1), free_list.shape[0]
+    i32, row = torch.int32, (B,)
+    p = switchsd_kv_map_params(
+        B, T, page, blocks, pages, _dev(lens, i32, "lens", row), _dev(new_lens, i32, "new_lens", row), lens_add, new_add,
+        _dev(block_table, i32, "block_table"), _dev(held, i32, "held", row), _dev(free_list, i32, "free_list", (pages,)),
+        _dev(free_count, i32, "free_count", (1,)), _dev(slots, i32, "slots", (B, T)), _dev(status, i32, "status", row),
+        _stream_ptr(stream))
     _check(load().switchsd_kv_map(ctypes.byref(p)), "switchsd_kv_map")
 
 
+@functools.lru_cache(maxsize=64)
 def switchsd_kv4_bytes(page: int, D: int) -> int:
     """Bytes of one (page, head) of the 4-bit cache; 0 for sizes that it does not have."""
     return int(load().switchsd_kv4_bytes(page, D))
@@ -574,18 +573,14 @@ def switchsd_kv4_append(k, v, slots, cache, *, page: int, stream=None) -> None:
     """switchsd_kv4_append of include/switchsd_target.h: k, v bf16 or f16 [B, T, Hkv, D] (views whose last dimension is
     contiguous), slots int32 [B, T], cache uint8 [pages, Hkv, switchsd_kv4_bytes(page, D)]."""
     B, T, H, D = k.shape
-    p = switchsd_kv4_append_params()
-    p.pages, heads = _cache_shape(cache, page, D)
+    pages, heads = _cache_shape(cache, page, D)
     if heads != H:
         raise ValueError(f"the cache has {heads} heads, k has {H}")
-    p.B, p.T, p.Hkv, p.D, p.page = B, T, H, D, page
-    p.dtype = _strided(k, "k", (B, T, H, D), (torch.bfloat16, torch.float16))
+    dtype = _strided(k, "k", (B, T, H, D), (torch.bfloat16, torch.float16))
     _strided(v, "v", (B, T, H, D), (k.dtype,))
-    p.k, p.v = k.data_ptr(), v.data_ptr()
-    p.k_stride, p.v_stride = _c_i64x3(*k.stride()[:3]), _c_i64x3(*v.stride()[:3])
-    p.slots = _dev(slots, torch.int32, "slots", (B, T))
-    p.cache = _dev(cache, torch.uint8, "cache")
-    p.stream = _stream_ptr(stream)
+    p = switchsd_kv4_append_params(
+        B, T, H, D, page, pages, dtype, k.data_ptr(), v.data_ptr(), k.stride()[:3], v.stride()[:3],
+        _dev(slots, torch.int32, "slots", (B, T)), _dev(cache, torch.uint8, "cache"), _stream_ptr(stream))
     _check(load().switchsd_kv4_append(ctypes.byref(p)), "switchsd_kv4_append")
 
 
@@ -593,16 +588,12 @@ def switchsd_kv4_read(cache, slots, out_k, out_v, *, page: int, stream=None) -> 
     """switchsd_kv4_read of include/switchsd_target.h: what the cache holds for slots int32 [B, T], into out_k and out_v
     f16 [B, T, Hkv, D]."""
     B, T, H, D = out_k.shape
-    p = switchsd_kv4_read_params()
-    p.pages, heads = _cache_shape(cache, page, D)
+    pages, heads = _cache_shape(cache, page, D)
     if heads != H:
         raise ValueError(f"the cache has {heads} heads, out_k has {H}")
-    p.B, p.T, p.Hkv, p.D, p.page = B, T, H, D, page
-    p.cache = _dev(cache, torch.uint8, "cache")
-    p.slots = _dev(slots, torch.int32, "slots", (B, T))
-    p.out_k = _dev(out_k, torch.float16, "out_k", (B, T, H, D))
-    p.out_v = _dev(out_v, torch.float16, "out_v", (B, T, H, D))
-    p.stream = _stream_ptr(stream)
+    p = switchsd_kv4_read_params(
+        B, T, H, D, page, pages, _dev(cache, torch.uint8, "cache"), _dev(slots, torch.int32, "slots", (B, T)),
+        _dev(out_k, torch.float16, "out_k", (B, T, H, D)), _dev(out_v, torch.float16, "out_v", (B, T, H, D)), _stream_ptr(stream))
     _check(load().switchsd_kv4_read(ctypes.byref(p)), "switchsd_kv4_read")
 
 
@@ -622,22 +613,15 @@ def switchsd_kv4_attention(q, cache, block_table, lens, new_lens, out, *, page: 
     contiguous), cache uint8 [pages, Hkv, bytes], block_table int32 [B, blocks], lens, new_lens int32 [B], out
     [B, T, Hq, D] of q's type.  scale: 1 / sqrt(D) when None.  Allocates the workspace from torch when none is given."""
     B, T, Hq, D = q.shape
-    p = switchsd_kv4_attention_params()
-    p.pages, p.Hkv = _cache_shape(cache, page, D)
-    p.B, p.T, p.Hq, p.D, p.page, p.blocks = B, T, Hq, D, page, block_table.shape[1]
-    p.dtype = _strided(q, "q", (B, T, Hq, D), (torch.bfloat16, torch.float16))
-    p.q, p.q_stride = q.data_ptr(), _c_i64x3(*q.stride()[:3])
-    p.cache = _dev(cache, torch.uint8, "cache")
-    p.block_table = _dev(block_table, torch.int32, "block_table", (B, p.blocks))
-    p.lens, p.new_lens = _dev(lens, torch.int32, "lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,))
-    p.lens_add, p.new_add = lens_add, new_add
-    p.scale = D ** -0.5 if scale is None else scale
-    p.out = _dev(out, q.dtype, "out", (B, T, Hq, D))
-    p.status = _dev(status, torch.int32, "status", (B,))
-    p.stream = _stream_ptr(stream)
-    need = int(load().switchsd_kv4_attention_workspace_bytes(ctypes.byref(p)))
+    (pages, Hkv), blocks, row = _cache_shape(cache, page, D), block_table.shape[1], (B,)
+    dtype = _strided(q, "q", (B, T, Hq, D), (torch.bfloat16, torch.float16))
+    p = switchsd_kv4_attention_params(
+        B, T, Hq, Hkv, D, page, pages, blocks, dtype, q.data_ptr(), q.stride()[:3], _dev(cache, torch.uint8, "cache"),
+        _dev(block_table, torch.int32, "block_table", (B, blocks)), _dev(lens, torch.int32, "lens", row),
+        _dev(new_lens, torch.int32, "new_lens", row), lens_add, new_add, D ** -0.5 if scale is None else scale,
+        _dev(out, q.dtype, "out", (B, T, Hq, D)), None, 0, _dev(status, torch.int32, "status", row), _stream_ptr(stream))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(load().switchsd_kv4_attention_workspace_bytes(ctypes.byref(p)), dtype=torch.uint8, device=q.device)
     p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
     _check(load().switchsd_kv4_attention(ctypes.byref(p)), "switchsd_kv4_attention")
 
@@ -652,39 +636,28 @@ def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_l
     Allocates the workspace from torch when none is given."""
     B, T, V = logits.shape
     new_lens = new if new_lens is None else new_lens
-    p = switchsd_logits_params()
-    p.B, p.T, p.V = B, T, V
-    p.dtype = _strided(logits, "logits", (B, T, V), tuple(_DTYPES))
-    p.logits, p.stride_b, p.stride_t = logits.data_ptr(), logits.stride(0), logits.stride(1)
+    dtype = _strided(logits, "logits", (B, T, V), tuple(_DTYPES))
     if (ctx_tokens is None) != (ctx_lens is None):
         raise ValueError("ctx_tokens and ctx_lens go together")
-    if ctx_tokens is not None:
-        p.cap = ctx_tokens.shape[1]
-        p.ctx_tokens = _dev(ctx_tokens, torch.int32, "ctx_tokens", (B, p.cap))
-        p.ctx_lens = _dev(ctx_lens, torch.int32, "ctx_lens", (B,))
-    if draft is not None:
-        p.draft_stride = draft.shape[1]
-        p.draft = _dev(draft, torch.int32, "draft", (B, p.draft_stride))
-    p.new_lens, p.new_add = _dev(new_lens, torch.int32, "new_lens", (B,)), new_add
-    p.rep, p.freq = _dev(rep, torch.float32, "rep", (B,)), _dev(freq, torch.float32, "freq", (B,))
-    p.pres = _dev(pres, torch.float32, "pres", (B,))
-    p.prompt_lens = _dev(prompt_lens, torch.int32, "prompt_lens", (B,))
     if (bias_ids is None) != (bias is None):
         raise ValueError("bias_ids and bias go together")
-    if bias_ids is not None:
-        p.nbias = bias_ids.shape[1]
-        p.bias_ids = _dev(bias_ids, torch.int32, "bias_ids", (B, p.nbias))
-        p.bias = _dev(bias, torch.float32, "bias", (B, p.nbias))
-    if mask is not None:
-        p.mask_words = mask.shape[2]
-        p.mask = _dev(mask, torch.int32, "mask", (B, T, p.mask_words))
+    cap = ctx_tokens.shape[1] if ctx_tokens is not None else 0
+    draft_stride = draft.shape[1] if draft is not None else 0
+    nbias = bias_ids.shape[1] if bias_ids is not None else 0
+    words = mask.shape[2] if mask is not None else 0
+    out_ptr, out_strides = None, (0, 0)
     if out is not None:
         _strided(out, "out", (B, T, V), (logits.dtype,))
-        p.out, p.out_stride_b, p.out_stride_t = out.data_ptr(), out.stride(0), out.stride(1)
-    p.argmax = _dev(argmax, torch.int32, "argmax", (B, T))
-    p.status = _dev(status, torch.int32, "status", (B,))
-    p.stream = _stream_ptr(stream)
+        out_ptr, out_strides = out.data_ptr(), out.stride()
+    i32, f32, row, strides = torch.int32, torch.float32, (B,), logits.stride()
+    p = switchsd_logits_params(
+        B, T, V, cap, dtype, logits.data_ptr(), strides[0], strides[1], _dev(ctx_tokens, i32, "ctx_tokens", (B, cap)),
+        _dev(ctx_lens, i32, "ctx_lens", row), _dev(draft, i32, "draft", (B, draft_stride)), draft_stride,
+        _dev(new_lens, i32, "new_lens", row), new_add, _dev(rep, f32, "rep", row), _dev(freq, f32, "freq", row),
+        _dev(pres, f32, "pres", row), _dev(prompt_lens, i32, "prompt_lens", row), _dev(bias_ids, i32, "bias_ids", (B, nbias)),
+        _dev(bias, f32, "bias", (B, nbias)), nbias, _dev(mask, i32, "mask", (B, T, words)), words, out_ptr, out_strides[0],
+        out_strides[1], _dev(argmax, i32, "argmax", (B, T)), _dev(status, i32, "status", row), None, 0, _stream_ptr(stream))
     if workspace is None:
-        workspace = torch.empty(int(load().switchsd_logits_workspace_bytes(ctypes.byref(p))), dtype=torch.uint8, device=logits.device)
+        workspace = torch.empty(load().switchsd_logits_workspace_bytes(ctypes.byref(p)), dtype=torch.uint8, device=logits.device)
     p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
     _check(load().switchsd_logits(ctypes.byref(p)), "switchsd_logits")

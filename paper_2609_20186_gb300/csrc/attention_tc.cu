@@ -22,8 +22,9 @@
 // over a row's threads, weights (whose exponentials alone are 1,000 cycles), weights into tensor memory, a barrier each --
 // where its two products take 500 and its codes 500.  Measured: 64 contexts of 2K to 8K tokens, drafts of up to 16, 4
 // query heads a key head: 281 us; 16 contexts of 8K to 32K, drafts of up to 32, 5 query heads a key head: 289 us (with the
-// tiles of 16 rows 407 and 801 us).  Two groups of row warps on units in turn, 16 row warps, and one pass over the scores
-// that starts again where the maximum rose were slower.
+// tiles of 16 rows 407 and 801 us); half of the issue slots, 17 % of the memory.  Slower were two groups of row warps on
+// units in turn, 16 row warps, one pass over the scores that starts again where the maximum rose, and all of a thread's
+// scores loaded at once (325 us: the unrolled code of the roles no longer fits the instruction cache together).
 #include <algorithm>
 
 #include "attention.cuh"

@@ -16,9 +16,10 @@
 // additions, of 1.5 * 2^8 in the product's instruction and of 1.5 * 2^23 in one more, which leaves the code in the low
 // bits; eight of those words times powers of 16 add up to a cache word and a known constant.
 //
-// What bounds it: memory, 2 bytes read and 0.53 written a value (and the other way round for the read), and instructions,
-// about 10 a value.  16 rows of 2048 tokens, 8 heads of 128 dimensions: append and read take 84 us, where the bytes alone
-// would take 50; of 1 to 2048 tokens each 60 us.  A divided quotient and its comparisons took 94 us for the latter.
+// What bounds it: instructions (about 20 a value, 70 % of the issue slots) more than memory, 2 bytes read and 0.53 written
+// a value (and the other way round for the read).  16 rows of 2048 tokens, 8 heads of 128 dimensions: append and read take
+// 73 us, where the bytes alone would take 50; of 1 to 2048 tokens each 55 us (35).  A divided quotient and its comparisons
+// took 94 us for the latter, limits on every code, not only those of wide groups, and words read token by token 60 us.
 #include <cuda_bf16.h>
 
 #include "kv4.cuh"
@@ -126,7 +127,7 @@ struct Scale {
             s = 0.f;
     }
     // x inside what the codes reach, for a wide group
-    __device__ float within(float x) const { return fminf(fmaxf(x, -8.f * s), 7.f * s); }
+    __device__ static float within(float x, float s) { return fminf(fmaxf(x, -8.f * s), 7.f * s); }
 };
 
 // A word of codes from the scaled values, an element at a time: nibble_of(j) is element j's.
@@ -180,18 +181,22 @@ __global__ void __launch_bounds__(kUnitThreads) kv4_append_kernel(const AppendAr
             m = max_nan(m, __shfl_xor_sync(kFull, m, 2));
             scales[g] = group_scale(m);
             const Scale k(scales[g]);
-            const bool wide = __any_sync(kFull, k.wide);
+            auto code = [&](auto value) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                uint32_t w = kNoBits;
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t w = kNoBits;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float2 f = widen<F16>(v[4 * i + e]);
-                    if (wide) f = make_float2(k.within(f.x), k.within(f.y));
-                    w = put_code(put_code(w, code_of(f.x, k.r), 2 * e), code_of(f.y, k.r), 2 * e + 1);
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 f = widen<F16>(v[4 * i + e]);
+                        w = put_code(put_code(w, code_of(value(f.x), k.r), 2 * e), code_of(value(f.y), k.r), 2 * e + 1);
+                    }
+                    words[2 * g + i] = w;
                 }
-                words[2 * g + i] = w;
-            }
+            };
+            if (__any_sync(kFull, k.wide))
+                code([&](float x) { return Scale::within(x, k.s); });
+            else
+                code([](float x) { return x; });
         }
         if (slot < 0) return;
         uint8_t *head = head_of(slot);
@@ -257,24 +262,30 @@ __global__ void __launch_bounds__(kUnitThreads) kv4_append_kernel(const AppendAr
         reinterpret_cast<__half *>(head_of(at) + L::scales(page) + size_t(at & (page - 1)) * L::kScales)[G + lane / kLanes] = mine;
     }
     const Scale own(mine);
-    const bool wide = __any_sync(kFull, own.wide);
-    // Tokens that are not in get codes of 0 here: what is there stays.
+    // Tokens that are not in have no bits here: what is there stays.
     uint32_t words[N], keep = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) words[i] = kNoBits;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        Scale k = own;
-        const int from = (lane & ~(kLanes - 1)) | (e * (kLanes / 8));
-        k.s = __shfl_sync(kFull, own.s, from);
-        k.r = __shfl_sync(kFull, own.r, from);
-        const float2 f = widen<F16>(raw[e].x), f2 = widen<F16>(raw[e].y);
-        const float x[4] = {f.x, f.y, f2.x, f2.y};
-        const bool is_in = (in >> e) & 1;
-        if (!is_in) keep |= 0xfu << (4 * nibble_of(e));
+    for (int e = 0; e < 8; ++e)
+        if (!((in >> e) & 1)) keep |= 0xfu << (4 * nibble_of(e));
+    auto code = [&](auto value) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) words[i] = put_code(words[i], is_in ? code_of(wide ? k.within(x[i]) : x[i], k.r) : kCodeBits, e);
-    }
+        for (int e = 0; e < 8; ++e) {
+            const int from = (lane & ~(kLanes - 1)) | (e * (kLanes / 8));
+            const float s = __shfl_sync(kFull, own.s, from), r = __shfl_sync(kFull, own.r, from);
+            const float2 f = widen<F16>(raw[e].x), f2 = widen<F16>(raw[e].y);
+            const float x[4] = {f.x, f.y, f2.x, f2.y};
+#pragma unroll
+            for (int i = 0; i < N; ++i) words[i] = put_code(words[i], code_of(value(x[i], s), r), e);
+        }
+    };
+    if (__any_sync(kFull, own.wide))
+        code([](float x, float s) { return Scale::within(x, s); });
+    else
+        code([](float x, float) { return x; });
+#pragma unroll
+    for (int i = 0; i < N; ++i) words[i] &= ~keep;
     uint8_t *dst = head_of(base) + L::values(page) + size_t((base & (page - 1)) >> 3) * L::kBlock + 4 * N * lane;
     if (N == 4) {
         uint4 w = make_uint4(words[0], words[1], words[N - 2], words[N - 1]);
@@ -353,29 +364,62 @@ __global__ void __launch_bounds__(kUnitThreads) kv4_read_kernel(const ReadArgs a
         return;
     }
     constexpr int N = D / 32;  // dimensions of a lane
-    const int32_t slot = slot_of(a, u.b, u.t0 + (lane & 7));
+    const int32_t slot = slot_of(a, u.b, u.t0 + (lane & 7));  // lane e (mod 8): token t0 + e
+    const int first = max(0, -u.t0), last = min(8, a.T - u.t0);  // the unit's tokens that there are
+    if (first >= last) return;
+    const uint32_t filled = __ballot_sync(kFull, slot >= 0) & 255u;
+    const int32_t begin = __shfl_sync(kFull, slot - (lane & 7), filled ? __ffs(int(filled)) - 1 : 0);
+    const bool block = filled && begin >= 0 && (begin & 7) == 0 && __all_sync(kFull, slot < 0 || slot == begin + (lane & 7));
+    uint8_t *out = out_of(a.v, u.t0) + 2 * N * lane;
+    const size_t token = size_t(a.Hkv) * (2 * D);
+    auto store = [&](int e, const uint32_t (&v)[N / 2]) {
+        if (N == 4)
+            *reinterpret_cast<uint2 *>(out + int64_t(e) * token) = make_uint2(v[0], v[N / 2 - 1]);
+        else
+            *reinterpret_cast<uint32_t *>(out + int64_t(e) * token) = v[0];
+    };
+    if (block) {
+        // all in their places of one block: its words and scales are read once
+        const uint8_t *head = head_of(begin);
+        const int in_page = begin & (page - 1);
+        const uint32_t *src = reinterpret_cast<const uint32_t *>(head + L::values(page) + size_t(in_page >> 3) * L::kBlock) + N * lane;
+        const __half *sc = reinterpret_cast<const __half *>(head + L::scales(page) + size_t(in_page) * L::kScales) + G + N * lane / 64;
+        uint32_t w[N];
+        __half s[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int32_t se = __shfl_sync(kFull, slot, e), t = u.t0 + e;
-        if (t < 0 || t >= a.T) continue;
+        for (int i = 0; i < N; ++i) w[i] = src[i];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = sc[2 * G * e];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e < first || e >= last) continue;
+            const __half2 s2 = __half2half2(s[e]);
+            uint32_t v[N / 2];
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const int sh = 4 * nibble_of(e);
+                v[i] = (filled >> e) & 1 ? pair_value(((w[2 * i] >> sh) & 15u) | (((w[2 * i + 1] >> sh) & 15u) << 16), s2) : 0u;
+            }
+            store(e, v);
+        }
+        return;
+    }
+#pragma unroll 1
+    for (int e = first; e < last; ++e) {
+        const int32_t se = __shfl_sync(kFull, slot, e);
         uint32_t v[N / 2];
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) v[i] = 0;
         if (se >= 0) {
-            // a token's codes stand in its block's words, eight tokens' together: the same line for the unit's other tokens
             const uint8_t *head = head_of(se);
-            const int in_page = se & (page - 1), sh = 4 * ((in_page & 7) >> 1) + 16 * (in_page & 1);
+            const int in_page = se & (page - 1), sh = 4 * nibble_of(in_page & 7);
             const uint32_t *w = reinterpret_cast<const uint32_t *>(head + L::values(page) + size_t(in_page >> 3) * L::kBlock) + N * lane;
             const __half *sc = reinterpret_cast<const __half *>(head + L::scales(page) + size_t(in_page) * L::kScales);
             const __half2 s = __half2half2(sc[G + N * lane / 64]);
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) v[i] = pair_value(((w[2 * i] >> sh) & 15u) | (((w[2 * i + 1] >> sh) & 15u) << 16), s);
         }
-        uint8_t *out = out_of(a.v, t) + 2 * N * lane;
-        if (N == 4)
-            *reinterpret_cast<uint2 *>(out) = make_uint2(v[0], v[N / 2 - 1]);
-        else
-            *reinterpret_cast<uint32_t *>(out) = v[0];
+        store(e, v);
     }
 }
 

@@ -146,7 +146,8 @@ int switchsd_kv4_read(const switchsd_kv4_read_params *params);
  *   block_table   int32 [B, blocks]
  *   workspace     at least switchsd_kv4_attention_workspace_bytes(params) bytes, 16-byte aligned, caller-owned: partial
  *                 results between the call's two kernels.  Calls that share one must not overlap on the GPU.
- *   status        int32 [B] or NULL
+ *   status        int32 [B] or NULL.  SWITCHSD_ROW_TIMEOUT in all rows: an on-chip wait ran out, and what the call wrote
+ *                 does not count.
  */
 typedef struct {
     int32_t B, T, Hq, Hkv, D, page, pages, blocks, dtype;

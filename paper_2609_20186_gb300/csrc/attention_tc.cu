@@ -37,8 +37,10 @@ constexpr int kTcKeys = 128;                // keys of a unit
 constexpr int kSplit = 2;                   // threads of a row
 constexpr int kRowWarps = 4 * kSplit, kUnpackWarps = 4;  // (of each: keys, values)
 constexpr int kRowThreads = kRowWarps * kWarp, kUnpackThreads = kUnpackWarps * kWarp;
-constexpr int kTcThreads = kRowThreads + 2 * kUnpackThreads + 4 * kWarp;  // (two of the last four warps have no work)
-constexpr int kValueWarp = kRowWarps + kUnpackWarps, kFetchWarp = kValueWarp + kUnpackWarps, kMmaWarp = kFetchWarp + 1;
+constexpr int kTcThreads = kRowThreads + 2 * kUnpackThreads + 4 * kWarp;
+// The last four warps: two without work, then the fetching and the MMAs' one, beside the rows 64 .. 127 on their schedulers,
+// which not every tile fills (beside the first rows: 288 us where it takes 282).
+constexpr int kValueWarp = kRowWarps + kUnpackWarps, kFetchWarp = kValueWarp + kUnpackWarps + 2, kMmaWarp = kFetchWarp + 1;
 // Registers a thread of each warpgroup: 640 threads are launched with 96 each, and the shares add up to the same.  (Local
 // memory would cost much: little of the L1 is left beside the shared memory.)
 constexpr int kRowRegs = 120, kUnpackRegs = 80, kOtherRegs = 80;
@@ -418,7 +420,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             tc_fence_before();
             rows_barrier(quarter);  // all threads of a row have read s_x
         }
-    } else if (warp < kFetchWarp) {
+    } else if (warp < kValueWarp + kUnpackWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kUnpackRegs));
         // ------------------------------------------------------------------------------------------- codes to f16
         const bool of_keys = warp < kValueWarp;
@@ -571,13 +573,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
         } else if (warp == kMmaWarp && lane == 0) {
         // ------------------------------------------------------------------------------------------- the MMAs
         uint32_t i = 0, nseg = 0;
+        const uint64_t dq = sw128_desc(smem_addr(sm_q)), dk0 = sw128_desc(smem_addr(sm_k)), dv0 = sw128_desc(smem_addr(sm_v));
         bool fresh = false, lo = false;        // O of the item: nothing added yet, the small weights' product begun
         auto product = [&](uint32_t j) {       // O += P V of unit j
             const int buf = int(j & 1);
             ok = ok && tc_wait(&v_full[buf], (j >> 1) & 1) && tc_wait(&p_full[buf], (j >> 1) & 1);
             if (!ok) return;
             tc_fence_after();
-            const uint64_t dv = sw128_desc(smem_addr(sm_v + buf * S::kV));
+            const uint64_t dv = dv0 + (buf ? uint64_t(S::kV >> 4) : 0);
             // the weights of 32 keys are in 16 columns of their scores' 32, the small ones in the other 16
             auto keys16 = [&](int k) { return dv + uint64_t(((k >> 2) * (D * 128) + (k & 3) * 32) >> 4); };
 #pragma unroll
@@ -606,7 +609,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 if (!ok) break;
                 mbar_arrive(&s_full[buf]);
                 tc_fence_after();
-                const uint64_t dq = sw128_desc(smem_addr(sm_q)), dk = sw128_desc(smem_addr(sm_k + buf * S::kK));
+                const uint64_t dk = dk0 + (buf ? uint64_t(S::kK >> 4) : 0);
 #pragma unroll
                 for (int e = 0; e < D / 16; ++e) {
                     const uint64_t step = uint64_t(((e >> 2) * kBlockBytes + (e & 3) * 32) >> 4);

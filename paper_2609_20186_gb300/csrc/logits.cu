@@ -14,8 +14,8 @@
 //
 // What bounds it: the instructions and latencies of both: the first looks at every token of the context once a part and
 // adds up in shared memory, the second has 2 or 4 bytes an element to read (and write).  Measured: 64 rows of 8K to 32K
-// tokens, 1 to 17 positions, 128,256 tokens, masks and biases: 92 us, 31 of them the counting (148 MB of logits are 22 us);
-// 16 rows of 32K to 128K, 1 to 33 positions, 152,064 tokens, written: 109 us; one row and position: 12 us.  Measured and
+// tokens, 1 to 17 positions, 128,256 tokens, masks and biases: 88 us, 28 of them the counting (148 MB of logits are 22 us);
+// 16 rows of 32K to 128K, 1 to 33 positions, 152,064 tokens, written: 106 us; one row and position: 12 us.  Measured and
 // not kept: one kernel that counted and then streamed (126 us where the two took 104); the context cut over a cluster of
 // the parts, with remote additions (118 us where each part reading it whole takes 94); sending for the first logits while
 // the tokens are counted (no change).
@@ -458,37 +458,43 @@ __global__ void __launch_bounds__(kLogitThreads, 4) logits_kernel(const LogitArg
         const int specials = min(__ldcg(a.count + size_t(b) * parts + part.part), a.entries);
         const uint2 *list = a.list + (size_t(b) * parts + part.part) * a.entries;
         const int32_t *draft = a.draft + size_t(b) * a.draft_stride;
+        uint64_t top[kLogitGroup] = {};
+        uint2 next = tid < specials ? __ldcg(list + tid) : make_uint2(0, 0);
         for (int s = tid; s < specials; s += kLogitThreads) {
-            const uint2 entry = __ldcg(list + s);
+            const uint2 entry = next;
+            if (s + kLogitThreads < specials) next = __ldcg(list + s + kLogitThreads);
             const uint32_t w = entry.y;
             const int32_t v = part.token_at(int(entry.x & 0xffffu));
             const elem *p = rows + int64_t(t0) * a.st + v;
-            float x[kLogitGroup];
-            uint32_t may[kLogitGroup];
+            bool may[kLogitGroup];
 #pragma unroll
-            for (int i = 0; i < kLogitGroup; ++i) {
-                x[i] = t0 + i < t1 ? E::get(p[i * a.st]) : 0.f;
-                may[i] = masks && t0 + i < t1 ? masks[size_t(t0 + i) * a.mask_words + (v >> 5)] >> (v & 31) : 1u;
-            }
+            for (int i = 0; i < kLogitGroup; ++i)
+                may[i] = t0 + i < t1 && (!masks || ((__ldcg(masks + size_t(t0 + i) * a.mask_words + (v >> 5)) >> (v & 31)) & 1));
+            float x[kLogitGroup];
+#pragma unroll
+            for (int i = 0; i < kLogitGroup; ++i) x[i] = may[i] ? E::get(p[i * a.st]) : 0.f;
             const float bias = w & kBiased ? __ldcg(a.bias + size_t(b) * a.nbias + (entry.x >> 16) - 1) : 0.f;
             uint32_t m = w & kCount;
             if (w & kInDraft)  // the draft's tokens behind the group's first position
                 for (int d = 0; d < t0; ++d) m += __ldcg(draft + d) == v;
 #pragma unroll
             for (int i = 0; i < kLogitGroup; ++i) {
-                if (t0 + i >= t1) break;
-                float y = x[i];
-                if ((w & kSeen) || m) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
-                if (m) y = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, float(m))), pres);
-                if (w & kBiased) y = __fadd_rn(y, bias);
-                if (!(may[i] & 1)) y = -INFINITY;
-                if (y > -INFINITY) {
-                    const uint64_t key = best_key(order_of(y), uint32_t(v));
-                    if (key > s_best[i]) atomicMax(&s_best[i], static_cast<unsigned long long>(key));
+                if (may[i]) {  // (what the mask leaves out has its -inf from the vectors)
+                    float y = x[i];
+                    if ((w & kSeen) || m) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+                    if (m) y = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, float(m))), pres);
+                    if (w & kBiased) y = __fadd_rn(y, bias);
+                    if (y > -INFINITY) top[i] = max(top[i], best_key(order_of(y), uint32_t(v)));
+                    if (outs) outs[int64_t(t0 + i) * a.ot + v] = E::put(y);
                 }
-                if (outs) outs[int64_t(t0 + i) * a.ot + v] = E::put(y);
                 if ((w & kInDraft) && t0 + i + 1 < t1) m += __ldcg(draft + t0 + i) == v;
             }
+        }
+#pragma unroll
+        for (int i = 0; i < kLogitGroup; ++i) {
+            const uint32_t high = __reduce_max_sync(kFull, uint32_t(top[i] >> 32));
+            const uint32_t low = __reduce_max_sync(kFull, uint32_t(top[i] >> 32) == high ? uint32_t(top[i]) : 0u);
+            if ((tid & 31) == 0 && high) atomicMax(&s_best[i], static_cast<unsigned long long>((uint64_t(high) << 32) | low));
         }
     }
     if (!a.argmax) return;

@@ -159,7 +159,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
     __shared__ uint32_t s_tmem;
     __shared__ uint32_t s_small[2], s_rows[4];         // unit + 1, and segment + 1, that had small weights: of a buffer, of 32 rows
     __shared__ __align__(16) uint32_t s_valid[4][4], s_exist[kRing][4];  // of a unit (mod 4, mod 3): keys that exist and whose page does
-    __shared__ float s_x[kSplit][kTcRows];             // what the threads of a row tell each other
+    __shared__ Segments s_seg[kRowWarps];              // what a row warp needs again when its segment is done
+    __shared__ Segment s_item[kRowWarps];
+    __shared__ float s_x[2][kSplit][kTcRows];          // what the threads of a row tell each other, of a unit (mod 2)
     __shared__ __align__(16) uint32_t s_scale[kUnpackWarps][16 * G];  // of the values' warps: scales of pairs of tokens
     __shared__ int s_bad;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -215,15 +217,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
         constexpr int KT = kTcKeys / kSplit, DT = D / kSplit;  // a thread's keys of a unit, and dimensions
         static_assert(KT % 32 == 0 && DT % 16 == 0, "whole words of keys, whole loads of dimensions");
         const uint32_t lanes = tmem + (uint32_t(32 * quarter) << 16);
-        const int64_t u_begin = seg.u;
         uint32_t i = 0, nseg = 0;  // units and segments so far
         auto of_row = [&](auto op) {  // over what the row's threads have put down
-            float x = s_x[0][row];
+            float x = s_x[i & 1][0][row];
 #pragma unroll
-            for (int p = 1; p < kSplit; ++p) x = op(x, s_x[p][row]);
+            for (int p = 1; p < kSplit; ++p) x = op(x, s_x[i & 1][p][row]);
             return x;
         };
-        for (int64_t u0 = seg.u; seg.next(a, s); u0 = seg.u) {
+        while (seg.next(a, s)) {
+            if (lane == 0) {  // (registers are short)
+                s_seg[warp] = seg;
+                s_item[warp] = s;
+            }
             const int rows = min(kTcRows, s.nw * a.group - s.rt * kTcRows);
             const bool mine = row < rows, warp_mine = 32 * quarter < rows;
             const int rr = s.rt * kTcRows + row, t = rr / a.group, h = s.hk * a.group + rr - t * a.group;
@@ -241,7 +246,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
 #pragma unroll
                     for (int e = 0; e < 4; ++e) big = fmaxf(big, fmaxf(fabsf(widen1<F16>(uint16_t(w[e]))), fabsf(widen1<F16>(uint16_t(w[e] >> 16)))));
                 }
-                s_x[part][row] = big;
+                s_x[i & 1][part][row] = big;
                 rows_barrier(quarter);
                 big = of_row([](float x, float y) { return fmaxf(x, y); });
                 int ex = 11 - (int(__float_as_uint(big) >> 23) - 127);
@@ -273,12 +278,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 const bool masked = key0 + kTcKeys > s.len + 1 || (valid4.x & valid4.y & valid4.z & valid4.w) != 0xffffffffu;
                 float top = -INFINITY, low = INFINITY;
                 if (warp_mine) {
+                    if (masked) {  // -inf in the place of the scores that the row does not see
 #pragma unroll 1
-                    for (int w = 0; w < KT / 32; ++w) {  // (a loop: the roles' code has to fit the instruction cache together)
-                        float v[32];
-                        tmem_ld32(sa + 32 * w, v);
-                        tmem_wait_ld();
-                        if (masked) {  // -inf in the place of the scores that the row does not see
+                        for (int w = 0; w < KT / 32; ++w) {
+                            float v[32];
+                            tmem_ld32(sa + 32 * w, v);
+                            tmem_wait_ld();
                             const int place = part * KT + 32 * w;
                             const int32_t ahead = limit - (key0 + place);  // the last visible key's place
                             const uint32_t see = s_valid[i & 3][place / 32] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
@@ -288,24 +293,29 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                                 const bool in = (see >> e) & 1;
                                 low = in ? fminf(low, v[e]) : low;
                                 v[e] = in ? v[e] : -INFINITY;
+                                top = fmaxf(top, v[e]);
                                 y[e & 15] = __float_as_uint(v[e]);
                                 if ((e & 15) == 15) tmem_st16(sa + 32 * w + (e & 16), y);
                             }
-                        } else {
-                            float l2[2] = {v[0], v[1]};
-#pragma unroll
-                            for (int e = 2; e < 32; e += 2) l2[(e >> 1) & 1] = min3(l2[(e >> 1) & 1], v[e], v[e + 1]);
-                            low = min3(low, l2[0], l2[1]);
                         }
-                        float t2[2] = {v[0], v[1]};
+                        tmem_wait_st();
+                    } else {
+                        float v[KT];  // loaded together: a load's latency is most of what this pass takes
 #pragma unroll
-                        for (int e = 2; e < 32; e += 2) t2[(e >> 1) & 1] = max3(t2[(e >> 1) & 1], v[e], v[e + 1]);
-                        top = max3(top, t2[0], t2[1]);
+                        for (int w = 0; w < KT / 32; ++w) tmem_ld32(sa + 32 * w, v + 32 * w);
+                        tmem_wait_ld();
+                        float t2[4] = {v[0], v[1], v[2], v[3]}, l2[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                        for (int e = 4; e < KT; e += 2) {
+                            t2[(e >> 1) & 3] = max3(t2[(e >> 1) & 3], v[e], v[e + 1]);
+                            l2[(e >> 1) & 3] = min3(l2[(e >> 1) & 3], v[e], v[e + 1]);
+                        }
+                        top = fmaxf(max3(t2[0], t2[1], t2[2]), t2[3]);
+                        low = fminf(min3(l2[0], l2[1], l2[2]), l2[3]);
                     }
-                    if (masked) tmem_wait_st();
                 }
                 const float mn = low * scale;
-                s_x[part][row] = fmaxf(kFloor, top * scale);
+                s_x[i & 1][part][row] = fmaxf(kFloor, top * scale);
                 rows_barrier(quarter);
                 const float mx = of_row([](float x, float y) { return fmaxf(x, y); });
                 float corr = 1.f;
@@ -374,17 +384,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 warp_arrive(&p_full[buf]);
             }
             // --- the segment's result ---------------------------------------------------------------------------
-            s_x[part][row] = l;
+            s_x[i & 1][part][row] = l;
             rows_barrier(quarter);
             l = of_row([](float x, float y) { return x + y; });
             ok = ok && tc_wait(&o_full, (i - 1) & 1);
             tc_fence_after();
+            seg = s_seg[warp];
+            s = s_item[warp];
             const bool lo = s_rows[quarter] == nseg;
             const bool whole = s.first == 0 && s.n == s.units;
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            const int slot = 2 * cta + (u0 == u_begin ? 0 : 1);
+            const int slot = 2 * cta + (nseg == 1 ? 0 : 1);
             float *partial = a.part + (size_t(slot) * kTcRows + row) * (D + 4);
-            if (warp_mine) {
+            const int rows_now = min(kTcRows, s.nw * a.group - s.rt * kTcRows), r0 = s.rt * kTcRows + row, t0 = r0 / a.group;
+            const bool out_mine = row < rows_now;
+            uint16_t *out = a.out + ((size_t(s.b) * a.T + t0) * a.Hq + s.hk * a.group + r0 - t0 * a.group) * D;
+            if (32 * quarter < rows_now) {
 #pragma unroll 1
                 for (int e = 0; e < DT; e += 16) {
                     float v[16];
@@ -400,19 +415,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[j] = fmaf(__uint_as_float(w[j]), 1.f / kTcLift, v[j]);
                     }
-                    if (mine && whole) {
-                        uint4 *dst = reinterpret_cast<uint4 *>(a.out + ((size_t(s.b) * a.T + t) * a.Hq + h) * D + d);
+                    if (out_mine && whole) {
+                        uint4 *dst = reinterpret_cast<uint4 *>(out + d);
 #pragma unroll
                         for (int j = 0; j < 16; j += 8)
                             dst[j / 8] = make_uint4(narrow2<F16>(v[j] * inv, v[j + 1] * inv), narrow2<F16>(v[j + 2] * inv, v[j + 3] * inv),
                                                     narrow2<F16>(v[j + 4] * inv, v[j + 5] * inv), narrow2<F16>(v[j + 6] * inv, v[j + 7] * inv));
-                    } else if (mine) {
+                    } else if (out_mine) {
 #pragma unroll
                         for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4 *>(partial + d + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                     }
                 }
             }
-            if (!whole && mine && part == 0) {
+            if (!whole && out_mine && part == 0) {
                 partial[D] = m;
                 partial[D + 1] = l;
                 if (row == 0) a.desc[slot] = make_int4(s.b, s.hk, s.rt, (s.first == 0 ? kFirst : 0) | (s.first + s.n == s.units ? kLast : 0));

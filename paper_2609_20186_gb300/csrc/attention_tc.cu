@@ -18,13 +18,14 @@
 // among them would reach tokens that do not see it through 0 * NaN: of the new tokens, whose keys not every query row
 // sees, a NaN in the value's scale becomes one in the key's, which the mask takes out.
 //
-// What bounds it: latency.  A unit takes the rows' warps about 3,400 cycles -- scores out of tensor memory, the maximum
-// over a row's threads, weights (whose exponentials alone are 1,000 cycles), weights into tensor memory, a barrier each --
-// where its two products take 500 and its codes 500.  Measured: 64 contexts of 2K to 8K tokens, drafts of up to 16, 4
-// query heads a key head: 281 us; 16 contexts of 8K to 32K, drafts of up to 32, 5 query heads a key head: 289 us (with the
-// tiles of 16 rows 407 and 801 us); half of the issue slots, 17 % of the memory.  Slower were two groups of row warps on
-// units in turn, 16 row warps, one pass over the scores that starts again where the maximum rose, and all of a thread's
-// scores loaded at once (325 us: the unrolled code of the roles no longer fits the instruction cache together).
+// What bounds it: the latencies of the rows' warps, and the instructions of the schedulers that hold the tile's first rows.
+// A unit takes about 3,300 cycles -- scores out of tensor memory, the maximum over a row's threads, weights (whose
+// exponentials alone are 1,000 cycles of a full tile), weights into tensor memory, a barrier each -- where its two products
+// take 500; half of the issue slots and 17 % of the memory's rate are used.  Measured: 64 contexts of 2K to 8K tokens, drafts
+// of up to 16, 4 query heads a key head: 268 us; 16 contexts of 8K to 32K, drafts of up to 32, 5 query heads a key head: 278
+// us (with the tiles of 16 rows 407 and 801 us).  Two numbers an instruction where weights are made and added took 6 us of
+// that.  Slower were two groups of row warps on units in turn, 16 row warps, one pass over the scores that starts again where
+// the maximum rose, and all of a thread's scores loaded together for the weights too (303 us).
 #include <algorithm>
 
 #include "attention.cuh"
@@ -39,7 +40,7 @@ constexpr int kRowWarps = 4 * kSplit, kUnpackWarps = 4;  // (of each: keys, valu
 constexpr int kRowThreads = kRowWarps * kWarp, kUnpackThreads = kUnpackWarps * kWarp;
 constexpr int kTcThreads = kRowThreads + 2 * kUnpackThreads + 4 * kWarp;
 // The last four warps: two without work, then the fetching and the MMAs' one, beside the rows 64 .. 127 on their schedulers,
-// which not every tile fills (beside the first rows: 288 us where it takes 282).
+// which not every tile fills (beside the first rows: 288 us where that took 282).
 constexpr int kValueWarp = kRowWarps + kUnpackWarps, kFetchWarp = kValueWarp + kUnpackWarps + 2, kMmaWarp = kFetchWarp + 1;
 // Registers a thread of each warpgroup: 640 threads are launched with 96 each, and the shares add up to the same.  (Local
 // memory would cost much: little of the L1 is left beside the shared memory.)
@@ -94,6 +95,28 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ float min3(float a, float b, float c) {
     float r;
     asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// Two binary32 numbers an instruction.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 halves_of(uint64_t p) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 
@@ -348,7 +371,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                         s_small[buf] = i + 1;
                         s_rows[quarter] = nseg;  // (read behind the rows' next barrier)
                     }
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    const uint64_t scale2 = pair_of(scale, scale), off2 = pair_of(off, off);
+                    uint64_t sum[2] = {0, 0};
 #pragma unroll 1
                     for (int w = 0; w < KT / 32; ++w) {  // 32 keys: 16 words of weights in the first 16 of their scores' columns
                         float v[32];
@@ -356,12 +380,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                         tmem_ld32(sa + 32 * w, v);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            v[e] = exp2_approx(fmaf(v[e], scale, off));
-                            sum[e & 3] += v[e];
+                        for (int e = 0; e < 16; ++e) {
+                            const float2 x = halves_of(fma_pair(pair_of(v[2 * e], v[2 * e + 1]), scale2, off2));
+                            v[2 * e] = exp2_approx(x.x);
+                            v[2 * e + 1] = exp2_approx(x.y);
+                            sum[e & 1] = add_pair(sum[e & 1], pair_of(v[2 * e], v[2 * e + 1]));
+                            y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
                         }
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
                         tmem_st16(sa + 32 * w, y);
                         if (small) {
 #pragma unroll
@@ -374,7 +399,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                         }
                         tmem_st16(sa + 32 * w + 16, y);
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    const float2 both = halves_of(add_pair(sum[0], sum[1]));
+                    l += both.x + both.y;
                     tmem_wait_st();
                 }
                 // The product of the unit before, every one in turn and before this warp's arrival, without which the next one

@@ -529,8 +529,8 @@ static cudaError_t launch_attn(AttnArgs a, int sms, cudaStream_t s) {
 }
 
 // Query rows of a key head up to which the tiles of 8 or 16 are faster than those of 128, whose time does not depend on
-// how many are filled.  Measured on 64 contexts of 8K: 16 rows 295 us here and 385 us there, 20 rows (two tiles here) 571
-// and 387 us, 48 rows 851 and 396 us.  A tile of 8 rather than 16 for 8 rows and fewer: 4 rows, 64 contexts of 8K to 32K
+// how many are filled.  Measured on 64 contexts of 8K: 16 rows 295 us here and 352 us there, 20 rows (two tiles here) 571
+// and 354 us, 48 rows 851 and 358 us.  A tile of 8 rather than 16 for 8 rows and fewer: 4 rows, 64 contexts of 8K to 32K
 // tokens, 362 and 713 us.  The contexts' lengths are on the device, so the choice goes by the rows alone.
 constexpr int kTensorRows = 16;
 

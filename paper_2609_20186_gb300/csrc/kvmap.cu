@@ -115,8 +115,9 @@ __global__ void __launch_bounds__(kMapThreads) kv_map_kernel(const MapArgs a) {
     if (cta == 0) {
         int32_t taken = 0;
         for (int b = tid; b < a.B; b += kMapThreads) {
+            if (s_need[b] <= s_held[b] || s_need[b] < 0) continue;  // (a bad row's held may be anything)
             const int64_t end = int64_t(s_off[b]) + (s_need[b] - s_held[b]);
-            if (s_need[b] > s_held[b] && end <= n) taken = max(taken, int32_t(end));
+            if (end <= n) taken = max(taken, int32_t(end));
         }
         taken = __reduce_max_sync(kFull, taken);
         if (lane == 0 && taken > 0) atomicMax(&s_taken, taken);

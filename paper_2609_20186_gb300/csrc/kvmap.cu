@@ -169,8 +169,8 @@ __global__ void __launch_bounds__(kMapThreads) kv_map_kernel(const MapArgs a) {
     if (cta == 0 && tid == 0) *a.free_count = n - s_taken;
     // 3. Slots of this CTA's rows.
     if (a.slots) {
-        for (int k = tid; k < mine * a.T; k += kMapThreads) {
-            const int i = k / a.T, t = k - i * a.T, b = row_of(i);
+        for (int64_t k = tid; k < int64_t(mine) * a.T; k += kMapThreads) {  // (k passes 2^31 with a step of nearly as many tokens)
+            const int i = int(uint32_t(k) / uint32_t(a.T)), t = int(uint32_t(k) - uint32_t(i) * uint32_t(a.T)), b = row_of(i);
             const int32_t need = s_need[b], held = s_held[b];
             int32_t slot = -1;
             if (need >= 0 && (need <= held || int64_t(s_off[b]) + (need - held) <= n) && t < __ldcg(a.new_lens + b) + a.new_add) {

@@ -57,3 +57,20 @@ def test_map_leaves_rows_with_a_bad_count_of_pages_alone(B, bad):
         assert np.array_equal(held.cpu().numpy(), wh)
     everything = np.concatenate([wf[:wc], wt[wt >= 0]])
     assert np.array_equal(np.sort(everything), np.arange(pages))  # no page lost, none held twice
+
+
+@pytest.mark.parametrize("B,T", [(1, 2**31 - 1), (33, (2**31 - 1) // 33)])
+def test_map_of_the_longest_step(B, T):
+    """B * T just below 2^31: the slots' last places."""
+    import torch
+    fw = _fw()
+    page, blocks, n = 256, 4, 700
+    table, held = torch.full((B, blocks), -1, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    fl, fc = _i32(np.arange(B * blocks)), _i32([B * blocks])
+    slots, status = torch.full((B, T), 7, dtype=torch.int32, device="cuda"), torch.full((B,), 7, dtype=torch.int32, device="cuda")
+    fw.switchsd_kv_map(_i32(np.full(B, 100)), _i32(np.full(B, n)), table, held, fl, fc, slots, page=page, status=status)
+    assert not status.any() and (held == 4).all()
+    p = torch.arange(100, 100 + n, device="cuda")
+    assert torch.equal(slots[:, :n].long(), table.long()[:, p // page] * page + p % page)
+    for b in range(B):
+        assert (slots[b, n:] == -1).all()

@@ -296,6 +296,15 @@ def _stream_ptr(stream) -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _scratch(nbytes: int, device, stream) -> torch.Tensor:
+    """Bytes for one call on `stream` (None: the current one), in that stream's order: torch hands them out only behind
+    what used them there before, and takes them back, once dropped, behind the call."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _bf16(t: torch.Tensor, name: str, shape=None):
     return _dev(t, torch.bfloat16, name, shape)
 
@@ -326,7 +335,7 @@ def switchsd_step(ctx_tokens, ctx_lens, hidden, probe_w, out_draft, out_len, out
     p.stream = _stream_ptr(stream)
     p.prefetch = int(prefetch)  # PREFETCH_* bits (see the header for the caller's guarantee)
     nw = d if probe_kind == PROBE_LINEAR else probe_hidden * d + probe_hidden
-    ws = _attach_workspace(p, workspace, ctx_tokens.device)  # noqa: F841 (kept alive for the call)
+    ws = _attach_workspace(p, workspace, ctx_tokens.device, stream)  # noqa: F841 (kept alive for the call)
     code = load().switchsd_step(
         _dev(ctx_tokens, torch.int32, "ctx_tokens"), _dev(ctx_lens, torch.int32, "ctx_lens", (B,)),
         _bf16(hidden, "hidden", (B, d)), _bf16(probe_w, "probe_w", (nw,)), ctypes.byref(p),
@@ -377,14 +386,14 @@ class NgramIndex:
             pass
 
 
-def _attach_workspace(p: switchsd_params, workspace, device) -> torch.Tensor | None:
-    """Points p at `workspace` (a CUDA uint8 tensor), allocating one from torch when the probe needs it
-    and none was given.  Returns the tensor so the caller keeps it alive for the call."""
+def _attach_workspace(p: switchsd_params, workspace, device, stream) -> torch.Tensor | None:
+    """Points p at `workspace` (a CUDA uint8 tensor), allocating one from torch (for a call on `stream`) when the
+    probe needs it and none was given.  Returns the tensor so the caller keeps it alive for the call."""
     need = int(load().switchsd_workspace_bytes(ctypes.byref(p)))
     if need == 0 and workspace is None:
         return None
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = _scratch(need, device, stream)
     if not workspace.is_cuda or workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"workspace must be a CUDA tensor of at least {need} bytes")
     p.workspace = workspace.data_ptr()
@@ -416,7 +425,7 @@ def switchsd_verify_step(draft, target_argmax, draft_len, out_accept, ctx_tokens
     p.stream = _stream_ptr(stream)
     p.prefetch = int(prefetch)  # PREFETCH_* bits (see the header for the caller's guarantee)
     nw = d if probe_kind == PROBE_LINEAR else probe_hidden * d + probe_hidden
-    ws = _attach_workspace(p, workspace, ctx_tokens.device)  # noqa: F841 (kept alive for the call)
+    ws = _attach_workspace(p, workspace, ctx_tokens.device, stream)  # noqa: F841 (kept alive for the call)
     code = load().switchsd_verify_step(
         _dev(draft, torch.int32, "draft", (B, k)),
         _dev(target_argmax, torch.int32, "target_argmax", (B, k + 1)),
@@ -511,11 +520,11 @@ def switchsd_harness_sampled(ctx_lens, mode, draft, draft_len, future, vdraft, v
 
 def switchsd_copy_labels(ctx_tokens, ctx_lens, out_labels, *, n: int = 5, workspace=None, stream=None) -> None:
     """switchsd_copy_labels of include/switchsd.h (§3.2 copy-mode labels): ctx_tokens int32 [B, cap],
-    ctx_lens int32 [B], out_labels uint8 [B, cap].  Allocates the workspace from torch when none is given."""
+    ctx_lens int32 [B], out_labels uint8 [B, cap].  Takes its workspace from torch, in the order of the call's stream, when none is given."""
     B, cap = ctx_tokens.shape
     need = int(load().switchsd_labels_workspace_bytes(B, cap))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=ctx_tokens.device)
+        workspace = _scratch(need, ctx_tokens.device, stream)
     code = load().switchsd_copy_labels(
         _dev(ctx_tokens, torch.int32, "ctx_tokens"), _dev(ctx_lens, torch.int32, "ctx_lens", (B,)), B, cap, n,
         _dev(out_labels, torch.uint8, "out_labels", (B, cap)), _dev(workspace, torch.uint8, "workspace"),
@@ -607,11 +616,18 @@ def switchsd_kv4_attention_workspace(q, cache, block_table, *, page: int) -> int
     return int(load().switchsd_kv4_attention_workspace_bytes(ctypes.byref(p)))
 
 
+def switchsd_kv4_attention_workspace_of(D: int) -> int:
+    """The same for any call on heads of D dimensions: the size goes by them alone."""
+    p = switchsd_kv4_attention_params()
+    p.D = D
+    return int(load().switchsd_kv4_attention_workspace_bytes(ctypes.byref(p)))
+
+
 def switchsd_kv4_attention(q, cache, block_table, lens, new_lens, out, *, page: int, scale: float | None = None,
                            lens_add: int = 0, new_add: int = 0, workspace=None, status=None, stream=None) -> None:
     """switchsd_kv4_attention of include/switchsd_target.h: q bf16 or f16 [B, T, Hq, D] (a view whose last dimension is
     contiguous), cache uint8 [pages, Hkv, bytes], block_table int32 [B, blocks], lens, new_lens int32 [B], out
-    [B, T, Hq, D] of q's type.  scale: 1 / sqrt(D) when None.  Allocates the workspace from torch when none is given."""
+    [B, T, Hq, D] of q's type.  scale: 1 / sqrt(D) when None.  Takes its workspace from torch, in the order of the call's stream, when none is given."""
     B, T, Hq, D = q.shape
     (pages, Hkv), blocks, row = _cache_shape(cache, page, D), block_table.shape[1], (B,)
     dtype = _strided(q, "q", (B, T, Hq, D), (torch.bfloat16, torch.float16))
@@ -621,7 +637,7 @@ def switchsd_kv4_attention(q, cache, block_table, lens, new_lens, out, *, page: 
         _dev(new_lens, torch.int32, "new_lens", row), lens_add, new_add, D ** -0.5 if scale is None else scale,
         _dev(out, q.dtype, "out", (B, T, Hq, D)), None, 0, _dev(status, torch.int32, "status", row), _stream_ptr(stream))
     if workspace is None:
-        workspace = torch.empty(load().switchsd_kv4_attention_workspace_bytes(ctypes.byref(p)), dtype=torch.uint8, device=q.device)
+        workspace = _scratch(load().switchsd_kv4_attention_workspace_bytes(ctypes.byref(p)), q.device, stream)
     p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
     _check(load().switchsd_kv4_attention(ctypes.byref(p)), "switchsd_kv4_attention")
 
@@ -633,7 +649,7 @@ def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_l
     is contiguous); ctx_tokens int32 [B, cap], ctx_lens int32 [B]; draft int32 [B, >= T - 1]; new_lens (or new) int32
     [B]; rep, freq, pres float32 [B]; prompt_lens int32 [B]; bias_ids int32, bias float32 [B, n]; mask int32
     [B, T, >= V / 32]; out of logits' type and shape (or logits itself), argmax int32 [B, T]: one of the two at least.
-    Allocates the workspace from torch when none is given."""
+    Takes its workspace from torch, in the order of the call's stream, when none is given."""
     B, T, V = logits.shape
     new_lens = new if new_lens is None else new_lens
     dtype = _strided(logits, "logits", (B, T, V), tuple(_DTYPES))
@@ -658,6 +674,6 @@ def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_l
         _dev(bias, f32, "bias", (B, nbias)), nbias, _dev(mask, i32, "mask", (B, T, words)), words, out_ptr, out_strides[0],
         out_strides[1], _dev(argmax, i32, "argmax", (B, T)), _dev(status, i32, "status", row), None, 0, _stream_ptr(stream))
     if workspace is None:
-        workspace = torch.empty(load().switchsd_logits_workspace_bytes(ctypes.byref(p)), dtype=torch.uint8, device=logits.device)
+        workspace = _scratch(load().switchsd_logits_workspace_bytes(ctypes.byref(p)), logits.device, stream)
     p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
     _check(load().switchsd_logits(ctypes.byref(p)), "switchsd_logits")

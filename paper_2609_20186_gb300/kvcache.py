@@ -11,6 +11,9 @@ With a ``Session`` whose draft is in ``sess.vdraft`` / ``sess.vlen``, ``lens`` i
 (the context's last token is the first one of the step) and ``new`` is ``sess.vlen`` with ``new_add = 1``.  The next
 step's ``map`` gives back the pages of rejected tokens; a row with length 0 and no new tokens gives back all of its pages.
 Nothing here computes any part of the operators.
+
+With a stream of its own (``stream=``) a cache's calls run there, whatever the current stream is: what fills their inputs
+has to be ahead of them on that stream, and the inputs live until the calls are done.
 """
 from __future__ import annotations
 
@@ -24,7 +27,7 @@ class KVCache:
                  lens_add: int = 0, new_add: int = 0, device="cuda", stream: torch.cuda.Stream | None = None):
         """B rows of at most max_len tokens, T new tokens a step, `pages` pages of `page` tokens shared by the rows;
         lens_add and new_add are added to the lengths that the calls take.  `stream` (the current one of each call when
-        None) is the stream of the calls; what fills the buffers here is behind it."""
+        None) is the stream of the calls; it waits for what fills the buffers here."""
         size = bd.switchsd_kv4_bytes(page, dim)
         if size == 0:
             raise ValueError(f"no 4-bit cache has pages of {page} tokens and heads of {dim} dimensions")
@@ -38,9 +41,11 @@ class KVCache:
         self.free_count = torch.full((1,), pages, **i32)
         self.slots = torch.full((B, T), -1, **i32)
         self.status = torch.zeros(B, **i32)
-        self.workspace = None
+        self.workspace = torch.empty(bd.switchsd_kv4_attention_workspace_of(dim), dtype=torch.uint8, device=device)
         if stream is not None:
             stream.wait_stream(torch.cuda.current_stream(self.data.device))
+            for t in (self.data, self.table, self.held, self.free_list, self.free_count, self.slots, self.status, self.workspace):
+                t.record_stream(stream)  # freed behind the calls
         self._lens = self._new = None
 
     def map(self, lens: torch.Tensor, new: torch.Tensor) -> None:
@@ -58,18 +63,20 @@ class KVCache:
         """Attention of the new tokens' queries [B, T, query heads, dim] over `layer`, into `out`."""
         if self._lens is None:
             raise RuntimeError("map() comes before attend()")
-        if self.workspace is None:  # its size goes by the heads' dimensions alone
-            self.workspace = torch.empty(bd.switchsd_kv4_attention_workspace(q, self.data[layer], self.table, page=self.page),
-                                         dtype=torch.uint8, device=q.device)
         bd.switchsd_kv4_attention(q, self.data[layer], self.table, self._lens, self._new, out, page=self.page, scale=scale,
                                   lens_add=self.lens_add, new_add=self.new_add, workspace=self.workspace,
                                   stream=self.stream)
         return out
 
     def read(self, layer: int, slots: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
-        """What `layer` holds for slots int32 [B, n]: keys and values, f16 [B, n, heads, dim]."""
+        """What `layer` holds for slots int32 [B, n]: keys and values, f16 [B, n, heads, dim].  They belong to the current
+        stream, which a cache's own stream waits for here, and which has to wait for that one before it uses them."""
         shape = (*slots.shape, self.heads, self.dim)
         k = torch.empty(shape, dtype=torch.float16, device=slots.device)
         v = torch.empty_like(k)
+        if self.stream is not None:
+            self.stream.wait_stream(torch.cuda.current_stream(slots.device))
+            for t in (k, v):
+                t.record_stream(self.stream)
         bd.switchsd_kv4_read(self.data[layer], slots, k, v, page=self.page, stream=self.stream)
         return k, v

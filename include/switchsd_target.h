@@ -53,12 +53,18 @@ extern "C" {
  * tokens outside [0, T] or with held[b] outside [0, blocks] is left alone with SWITCHSD_ROW_BAD_LEN.  Both get no
  * slots.
  *
+ * Such a row has no place for its new tokens, so the step has to leave it out altogether: switchsd_kv_map_granted also
+ * writes granted[b] = new_lens[b] for the other rows and -1 - new_add for these.  Given as new_lens to the attention and
+ * the logits, and as draft_len to the verification (with new_add >= 0), it is a bad length there: the row gets zeros, no
+ * greedy token, and a context that stays as it is, until a later map has pages for it.
+ *
  *   lens, new_lens  int32 [B];  lens_add, new_add  see above
  *   block_table     int32 [B, blocks] (modified; entries that no page backs are -1 after the call that freed them)
  *   held            int32 [B] (modified)
  *   free_list       int32 [pages] (modified; entries taken become -1);  free_count  int32 [1] (modified)
  *   slots           int32 [B, T] or NULL: out, -1 for t >= new and for rows without slots
  *   status          int32 [B] or NULL: out
+ *   granted         int32 [B] or NULL: out; may be new_lens itself
  *   B 1 .. SWITCHSD_MAP_ROWS, T >= 1, blocks >= 1, pages >= 1, pages * page <= 2^31 - 1, B * T and B * blocks < 2^31
  */
 typedef struct {
@@ -72,6 +78,7 @@ typedef struct {
 } switchsd_kv_map_params;
 
 int switchsd_kv_map(const switchsd_kv_map_params *params);
+int switchsd_kv_map_granted(const switchsd_kv_map_params *params, int32_t *granted);
 
 /*
  * The 4-bit cache of one layer: uint8 [pages][Hkv][switchsd_kv4_bytes(page, D)], 16-byte aligned, D = 64 or 128.  With
@@ -128,7 +135,8 @@ int switchsd_kv4_read(const switchsd_kv4_read_params *params);
 
 /*
  * Attention over the 4-bit cache.  New token t of row b (t < new) stands at position len + t and sees the keys of the
- * positions 0 .. len + t, its own among them (append first):
+ * positions 0 .. len + t, its own among them (append first; a row that the map left without slots is left out here by
+ * switchsd_kv_map_granted's lengths, or it would see what earlier steps left behind its last token):
  *
  *   out[b, t, h] = sum_j softmax_j(scale * q[b, t, h] . k_j) v_j,   k, v of the key head h / (Hq / Hkv)
  *
@@ -177,7 +185,8 @@ int switchsd_kv4_attention(const switchsd_kv4_attention_params *params);
  *   l = l + bias_v                                 (the last entry of bias_ids that names v)
  *   l = -inf where the position's mask has a 0 bit
  *
- * argmax is the smallest v with the largest l; l = -inf and NaN are never chosen, and it is -1 where nothing is.
+ * argmax is the smallest v with the largest l; l = -inf and NaN are never chosen, and it is -1 where nothing is.  (The
+ * verification appends the token that it is given: a grammar that leaves a position nothing is the caller's to see to.)
  *
  *   logits        dtype (SWITCHSD_BF16, SWITCHSD_F16, SWITCHSD_F32) [B, T, V], strides in elements between rows and
  *                 positions (V values are contiguous), aligned to its elements

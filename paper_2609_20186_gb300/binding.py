@@ -218,6 +218,7 @@ _SIGNATURES = {
     "switchsd_harness_sampled": (ctypes.c_int, [ctypes.c_void_p] * 11
                                  + [ctypes.POINTER(switchsd_harness_params)]),
     "switchsd_kv_map": (ctypes.c_int, [ctypes.POINTER(switchsd_kv_map_params)]),
+    "switchsd_kv_map_granted": (ctypes.c_int, [ctypes.POINTER(switchsd_kv_map_params), ctypes.c_void_p]),
     "switchsd_kv4_bytes": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32]),
     "switchsd_kv4_append": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_append_params)]),
     "switchsd_kv4_read": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_read_params)]),
@@ -549,11 +550,13 @@ def _strided(t: torch.Tensor, name: str, shape, dtypes) -> int:
 
 
 def switchsd_kv_map(lens, new_lens, block_table, held, free_list, free_count, slots, *, page: int, T: int | None = None,
-                    lens_add: int = 0, new_add: int = 0, status=None, stream=None) -> None:
-    """switchsd_kv_map of include/switchsd_target.h: block tables and slot maps from the rows' device lengths.
+                    lens_add: int = 0, new_add: int = 0, status=None, granted=None, stream=None) -> None:
+    """switchsd_kv_map of include/switchsd_target.h (switchsd_kv_map_granted with `granted`): block tables and slot maps
+    from the rows' device lengths.
 
     lens, new_lens, held int32 [B]; block_table int32 [B, blocks]; free_list int32 [pages]; free_count int32 [1];
-    slots int32 [B, T] (or None, with T); status int32 [B] or None.
+    slots int32 [B, T] (or None, with T); status int32 [B] or None; granted int32 [B] or None: new_lens, but for rows
+    without slots -1 - new_add (new_lens itself will do).
     """
     B, blocks = block_table.shape
     T, pages = slots.shape[1] if slots is not None else int(T or 1), free_list.shape[0]
@@ -563,7 +566,7 @@ def switchsd_kv_map(lens, new_lens, block_table, held, free_list, free_count, sl
         _dev(block_table, i32, "block_table"), _dev(held, i32, "held", row), _dev(free_list, i32, "free_list", (pages,)),
         _dev(free_count, i32, "free_count", (1,)), _dev(slots, i32, "slots", (B, T)), _dev(status, i32, "status", row),
         _stream_ptr(stream))
-    _check(load().switchsd_kv_map(ctypes.byref(p)), "switchsd_kv_map")
+    _check(load().switchsd_kv_map_granted(ctypes.byref(p), _dev(granted, i32, "granted", row)), "switchsd_kv_map")
 
 
 @functools.lru_cache(maxsize=64)

@@ -22,7 +22,7 @@ constexpr int kMapCtas = 8;  // of the cluster at most: the size that every devi
 
 struct MapArgs {
     const int32_t *lens, *new_lens;
-    int32_t *table, *held, *free_list, *free_count, *slots, *status;
+    int32_t *table, *held, *free_list, *free_count, *slots, *status, *granted;
     int32_t B, T, blocks, pages, page_shift, lens_add, new_add;
 };
 
@@ -148,9 +148,12 @@ __global__ void __launch_bounds__(kMapThreads) kv_map_kernel(const MapArgs a) {
     for (int i = first; i < mine; i += rows_step) {
         const int b = row_of(i);
         const int32_t need = s_need[b], held = s_held[b];
+        const bool fits = need >= 0 && (need <= held || int64_t(s_off[b]) + (need - held) <= n);
+        // (over new_lens itself, perhaps: every CTA has read it, and the slots read the rows' that keep it)
+        if (a.granted && part == 0 && lane == 0) a.granted[b] = fits ? __ldcg(a.new_lens + b) : -1 - a.new_add;
         if (need < 0) continue;
         if (need > held) {
-            if (int64_t(s_off[b]) + (need - held) > n) {
+            if (!fits) {
                 if (part == 0 && lane == 0 && a.status) a.status[b] = SWITCHSD_ROW_CAPACITY;
                 continue;
             }
@@ -187,7 +190,9 @@ __global__ void __launch_bounds__(kMapThreads) kv_map_kernel(const MapArgs a) {
 
 using namespace switchsd;
 
-extern "C" int switchsd_kv_map(const switchsd_kv_map_params *p) {
+extern "C" int switchsd_kv_map(const switchsd_kv_map_params *p) { return switchsd_kv_map_granted(p, nullptr); }
+
+extern "C" int switchsd_kv_map_granted(const switchsd_kv_map_params *p, int32_t *granted) {
     if (!p || !p->lens || !p->new_lens || !p->block_table || !p->held || !p->free_list || !p->free_count) return SWITCHSD_ERR_ARG;
     if (p->B < 1 || p->B > SWITCHSD_MAP_ROWS || p->T < 1 || p->blocks < 1 || p->pages < 1 || !kv4_page_ok(p->page)) return SWITCHSD_ERR_SHAPE;
     if (int64_t(p->pages) * p->page > 0x7fffffff || int64_t(p->B) * p->T > 0x7fffffff || int64_t(p->B) * p->blocks > 0x7fffffff)
@@ -201,6 +206,7 @@ extern "C" int switchsd_kv_map(const switchsd_kv_map_params *p) {
     a.free_count = p->free_count;
     a.slots = p->slots;
     a.status = p->status;
+    a.granted = granted;
     a.B = p->B;
     a.T = p->T;
     a.blocks = p->blocks;

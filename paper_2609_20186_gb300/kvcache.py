@@ -10,6 +10,10 @@ of a verification step on device-resident lengths:
 With a ``Session`` whose draft is in ``sess.vdraft`` / ``sess.vlen``, ``lens`` is ``sess.lens`` with ``lens_add = -1``
 (the context's last token is the first one of the step) and ``new`` is ``sess.vlen`` with ``new_add = 1``.  The next
 step's ``map`` gives back the pages of rejected tokens; a row with length 0 and no new tokens gives back all of its pages.
+
+A row that the pool has no pages for has to sit the step out, or it would go on without its tokens' keys and values:
+``map`` puts the step's new tokens into ``cache.new``, -1 - new_add for such a row.  ``attend`` goes by it; give it to the
+logits (``new_lens=cache.new``) and to the verification (``sess.vlen.copy_(cache.new)``), and the row stays as it is.
 Nothing here computes any part of the operators.
 
 With a stream of its own (``stream=``) a cache's calls run there, whatever the current stream is: what fills their inputs
@@ -41,19 +45,20 @@ class KVCache:
         self.free_count = torch.full((1,), pages, **i32)
         self.slots = torch.full((B, T), -1, **i32)
         self.status = torch.zeros(B, **i32)
+        self.new = torch.zeros(B, **i32)
         self.workspace = torch.empty(bd.switchsd_kv4_attention_workspace_of(dim), dtype=torch.uint8, device=device)
         if stream is not None:
             stream.wait_stream(torch.cuda.current_stream(self.data.device))
-            for t in (self.data, self.table, self.held, self.free_list, self.free_count, self.slots, self.status, self.workspace):
+            for t in (self.data, self.table, self.held, self.free_list, self.free_count, self.slots, self.status, self.new, self.workspace):
                 t.record_stream(stream)  # freed behind the calls
-        self._lens = self._new = None
+        self._lens = None
 
     def map(self, lens: torch.Tensor, new: torch.Tensor) -> None:
-        """Pages for lens[b] + lens_add cached and new[b] + new_add new tokens of each row; fills slots and status.  The
-        calls that follow use the same lengths."""
-        self._lens, self._new = lens, new
+        """Pages for lens[b] + lens_add cached and new[b] + new_add new tokens of each row; fills slots, status and
+        cache.new.  The calls that follow use the same `lens`, and cache.new."""
+        self._lens = lens
         bd.switchsd_kv_map(lens, new, self.table, self.held, self.free_list, self.free_count, self.slots, page=self.page,
-                           lens_add=self.lens_add, new_add=self.new_add, status=self.status, stream=self.stream)
+                           lens_add=self.lens_add, new_add=self.new_add, status=self.status, granted=self.new, stream=self.stream)
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor) -> None:
         """The new tokens' keys and values [B, T, heads, dim] into `layer`."""
@@ -63,7 +68,7 @@ class KVCache:
         """Attention of the new tokens' queries [B, T, query heads, dim] over `layer`, into `out`."""
         if self._lens is None:
             raise RuntimeError("map() comes before attend()")
-        bd.switchsd_kv4_attention(q, self.data[layer], self.table, self._lens, self._new, out, page=self.page, scale=scale,
+        bd.switchsd_kv4_attention(q, self.data[layer], self.table, self._lens, self.new, out, page=self.page, scale=scale,
                                   lens_add=self.lens_add, new_add=self.new_add, workspace=self.workspace,
                                   stream=self.stream)
         return out

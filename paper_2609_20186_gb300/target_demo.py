@@ -3,9 +3,9 @@
     python -m paper_2609_20186_gb300.target_demo [--rows 8] [--steps 64] [--no-drafts]
 
 Every step, with nothing read back by the host: pages and slots for the step's tokens (the context's last one and the
-draft), their keys and values into the 4-bit cache and their attention over it, penalties and biases on the logits and
-the greedy token of every position, then the controller's verification, append and next draft.  The target here is
-attention layers without positions and a head that prefers, by far, the token that follows in a fixed cycle of tokens,
+draft; a row that the pool has no pages for sits the step out), their keys and values into the 4-bit cache and their
+attention over it, penalties and biases on the logits and the greedy token of every position, then the controller's
+verification, append and next draft.  The target here is attention layers without positions and a head that prefers, by far, the token that follows in a fixed cycle of tokens,
 so that its text repeats and copied drafts are accepted; its products are torch's.
 """
 from __future__ import annotations
@@ -57,7 +57,8 @@ class Decoder:
     """A batch of sequences between a SmallTarget, a KVCache and a Session."""
 
     def __init__(self, target: SmallTarget, prompts: np.ndarray, lens: np.ndarray, *, k: int = 8, room: int = 256, page: int = 16,
-                 drafts: bool = True):
+                 drafts: bool = True, pages: int | None = None):
+        """`pages` pages for all rows: enough for every row's whole context when None."""
         B = prompts.shape[0]
         self.target, self.k, self.drafts = target, k, drafts
         cap = -(-(prompts.shape[1] + room) // 4) * 4
@@ -67,8 +68,8 @@ class Decoder:
         self.sess = Session(ctx, lens, probe, k=k, n_min=2, n_max=4, logit_tau=-1.0, d=target.dim, hidden_rows=k + 1)
         dev = self.sess.ctx.device
         # lengths as the context's: its last token is the first of the step
-        self.cache = KVCache(B, k + 1, layers=target.layers, heads=target.kv_heads, dim=target.head_dim, pages=B * -(-cap // page), max_len=cap,
-                             page=page, lens_add=-1, new_add=1, device=dev)
+        self.cache = KVCache(B, k + 1, layers=target.layers, heads=target.kv_heads, dim=target.head_dim, pages=pages or B * -(-cap // page),
+                             max_len=cap, page=page, lens_add=-1, new_add=1, device=dev)
         f32 = dict(dtype=torch.float32, device=dev)
         self.rep, self.freq, self.pres = torch.full((B,), 1.02, **f32), torch.full((B,), 0.01, **f32), torch.full((B,), 0.1, **f32)
         self.prompt_lens = self.sess.lens.clone()
@@ -82,6 +83,8 @@ class Decoder:
         for start in range(0, longest - 1, T):
             cached = torch.clamp(self.sess.lens - 1, max=start)
             self.cache.map(cached + 1, torch.clamp(self.sess.lens - 1 - cached, max=T) - 1)
+            if self.cache.status.any():
+                raise RuntimeError("the cache has too few pages for the prompts")
             # (places past a row's new tokens get tokens too, which no slot and no result has)
             at = torch.clamp(cached[:, None] + torch.arange(T, device=cached.device), max=self.sess.ctx.shape[1] - 1)
             self.target.hidden(self.sess.ctx.gather(1, at.long()), self.cache)
@@ -90,6 +93,7 @@ class Decoder:
         """One verification step: the target on the last token and the draft, then the controller."""
         s = self.sess
         self.cache.map(s.lens, s.vlen)
+        s.vlen.copy_(self.cache.new)  # rows without pages: no logits, nothing appended, and another try in the next step
         tokens = torch.cat([s.ctx.gather(1, (s.lens - 1).long()[:, None]), s.vdraft], 1)
         x = self.target.hidden(tokens, self.cache)
         bd.switchsd_logits(x @ self.target.head.T, ctx_tokens=s.ctx, ctx_lens=s.lens, draft=s.vdraft, new_lens=s.vlen, new_add=1,
@@ -98,7 +102,10 @@ class Decoder:
         s.verify_step(x)
         if self.drafts:
             s.vdraft.copy_(s.draft)
-            s.vlen.copy_(torch.where(s.mode == bd.MODE_COPY, s.len, 0))
+            # (a row that sat the step out tries the next one with its one token)
+            s.vlen.copy_(torch.where((s.mode == bd.MODE_COPY) & (s.accept >= 0), s.len, 0))
+        else:
+            s.vlen.zero_()
 
 
 def prompts_of(rows: int, target: SmallTarget, longest: int = 40, seed: int = 0) -> tuple[np.ndarray, np.ndarray]:

@@ -74,3 +74,87 @@ def test_map_of_the_longest_step(B, T):
     assert torch.equal(slots[:, :n].long(), table.long()[:, p // page] * page + p % page)
     for b in range(B):
         assert (slots[b, n:] == -1).all()
+
+
+@pytest.mark.parametrize("B,add,alias", [(5, 0, False), (40, 1, False), (300, 1, True), (1030, -2, False)])
+def test_map_says_what_it_granted(B, add, alias):
+    """granted is new_lens for the rows with slots and -1 - new_add for the others: bad lengths, too many blocks, no pages."""
+    import torch
+    fw = _fw()
+    rng = np.random.default_rng(B)
+    T, page, blocks = 9, 16, 10
+    pages = max(2, int(B * blocks * 0.35))
+    free = rng.permutation(pages).astype(np.int32)
+    st = ref.MapState(B, blocks, free)
+    table, held = torch.full((B, blocks), -1, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    fl, fc = _i32(free), _i32([pages])
+    refused = 0
+    for step in range(4):
+        lens, new = rng.integers(0, page * blocks - T, B), rng.integers(0, T + 1, B)
+        lens[1], new[2], lens[3] = -4, T + 1, page * blocks
+        new[3] = max(new[3], 1)
+        given, status = _i32(new - add), torch.full((B,), 7, dtype=torch.int32, device="cuda")
+        granted = given if alias else torch.full((B,), 77, dtype=torch.int32, device="cuda")
+        slots = torch.full((B, T), 7, dtype=torch.int32, device="cuda")
+        fw.switchsd_kv_map(_i32(lens), given, table, held, fl, fc, slots, page=page, new_add=add, status=status, granted=granted)
+        want_slots, want_status = st.step(lens.tolist(), new.tolist(), T, page)
+        assert np.array_equal(slots.cpu().numpy(), want_slots) and np.array_equal(status.cpu().numpy(), want_status)
+        assert np.array_equal(granted.cpu().numpy(), np.where(want_status == 0, new - add, -1 - add))
+        assert np.array_equal(table.cpu().numpy(), st.arrays()[0])
+        refused += int((want_status == 1).sum())
+    assert refused > 4 or B < 40  # (more than the row whose blocks are too few: the pool was short too)
+
+
+@pytest.mark.parametrize("T", [3, 9])  # 12 and 36 query rows a key head
+def test_a_row_without_pages_sits_the_step_out(T):
+    """The pool is short of pages for one row, in whose last page an earlier step left a rejected draft: its attention is
+    zeros and not those tokens', its logits name no token, the verification leaves its context; the other row goes on, and
+    so does the first once the pool has pages."""
+    import torch
+    fw = _fw()
+    torch.manual_seed(T)
+    B, H, Hq, D, page, V, k = 2, 1, 4, 128, 16, 50, T - 1
+    cache = fw.KVCache(B, T, layers=1, heads=H, dim=D, pages=4, max_len=200, page=page, lens_add=-1, new_add=1)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    ctx = torch.randint(0, V, (B, 200), **i32)
+    hist = [[], []]
+
+    def step(lens, vlen):
+        """One step; the rows' keys and values join `hist` where they got slots."""
+        x = torch.randn(B, T, Hq + 2 * H, D, device="cuda").to(torch.bfloat16)
+        cl, vl = _i32(lens), _i32(vlen)
+        cache.map(cl, vl)
+        vl.copy_(cache.new)
+        cache.append(0, x[:, :, Hq:Hq + H], x[:, :, Hq + H:])
+        out = cache.attend(0, x[:, :, :Hq], torch.full((B, T, Hq, D), 9.0, dtype=torch.bfloat16, device="cuda"))
+        best = torch.full((B, T), 77, **i32)
+        fw.switchsd_logits(torch.randn(B, T, V, device="cuda"), ctx_tokens=ctx, ctx_lens=cl, new_lens=vl, new_add=1, argmax=best)
+        acc, status = torch.full((B,), 77, **i32), torch.full((B,), 77, **i32)
+        before = ctx.clone()
+        fw.switchsd_verify(torch.zeros(B, k, **i32), best, acc, draft_len=vl, ctx_tokens=ctx, ctx_lens=cl, status=status)
+        xs = x.double().cpu().numpy()
+        got = out.double().cpu().numpy()
+        for b in range(B):
+            n = lens[b] - 1
+            del hist[b][n:]
+            if cache.status[b] != 0:
+                assert cache.new[b] == -2 and (got[b] == 0).all()
+                assert (best[b] == -1).all() and acc[b] == -1 and status[b] == 2
+                assert torch.equal(ctx[b], before[b]) and cl[b] == lens[b]
+                continue
+            assert cache.new[b] == vlen[b] and acc[b] >= 0 and status[b] == 0 and cl[b] == lens[b] + acc[b] + 1
+            for t in range(vlen[b] + 1):
+                hist[b].append([ref.dequantise(*ref.quantise(xs[b, t, lo:lo + H])) for lo in (Hq, Hq + H)])
+            ks, vs = (np.array([h[i] for h in hist[b]]) for i in range(2))
+            want, mag = ref.attention(xs[b:b + 1, :, :Hq], [ks], [vs], [n], [vlen[b] + 1], float(np.float32(D ** -0.5)))
+            tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * mag
+            assert np.all(np.abs(got[b:b + 1] - want) <= tol)
+        return cache.status.cpu().tolist()
+    goal = (14, 40)
+    while [len(h) for h in hist] != list(goal):      # (a row that is there already writes its last token again)
+        have = [len(h) for h in hist]
+        assert step([min(n, g - 1) + 1 for n, g in zip(have, goal)], [max(0, min(k, g - n - 1)) for n, g in zip(have, goal)]) == [0, 0]
+    assert int(cache.free_count) == 0
+    assert step([15, 40], [1, 0]) == [0, 0]          # the first row's one page is full; its last token is rejected
+    assert step([16, 40], [1, 0]) == [1, 0]          # and needs a second page, which there is not
+    assert step([16, 31], [1, 0]) == [0, 0]          # the second row gave one back

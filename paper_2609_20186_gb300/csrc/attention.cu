@@ -584,6 +584,7 @@ extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
     a.group = p->Hq / p->Hkv;
     a.dim = p->D;
     a.scale = p->scale;
+    a.give_up = 0;
     const int sms = attn_sms();
     if (sms == 0) return SWITCHSD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);

@@ -21,12 +21,15 @@ struct AttnArgs {
     uint16_t *out;
     float *part;        // [2 * CTAs][rows][D + 4]: output, maximum, sum
     int4 *desc;         // [2 * CTAs]: of a partial result: item's row (-1: none), key head, tile of query rows, flags
+                        // (kLate: of the CTA, in its first one)
     int32_t *status;
     int32_t B, T, Hq, Hkv, pages, blocks, page_shift, lens_add, new_add, group, dim;
     float scale;
+    int32_t give_up;  // attention_tc.cu: a diagnostic, see tc_give_up()
 };
 
-constexpr int kFirst = 1, kLast = 2;  // flags of a partial result: holds the item's first, last unit
+// Flags of a partial result: holds the item's first, last unit; a wait of the CTA ran out.
+constexpr int kFirst = 1, kLast = 2, kLate = 4;
 
 // A row's lengths, or false where they are bad.
 __device__ __forceinline__ bool row_lengths(const AttnArgs &a, int b, int32_t &len, int32_t &nw) {
@@ -169,7 +172,8 @@ __device__ __forceinline__ uint16_t narrow1(float a) {
     return F16 ? __half_as_ushort(__float2half_rn(a)) : __bfloat16_as_ushort(__float2bfloat16_rn(a));
 }
 
-// Joins the partial results of the items that several CTAs hold: CTAs (i, .) look after the item whose first part is the
+// Joins the partial results of the items that several CTAs hold, and writes the statuses of a launch that a CTA gave up
+// (here, behind all of its CTAs: the first of them writes the others, at a time of its own).  The join: CTAs (i, .) look after the item whose first part is the
 // i-th CTA's, a CTA a query row and a thread a dimension, adding the parts in order.  R query rows a tile.  What bounds it:
 // latency, so the parts' number comes from their flags 32 at a time and their numbers kJoinParts at a time (one after the
 // other, with 16 CTAs for an item's rows, 68 rows of 17 parts each took 50 us with their attention; now 21 us).  CTAs of
@@ -182,6 +186,8 @@ __global__ void __launch_bounds__(D, 2048 / D) attn_join_kernel(const AttnArgs a
     int from = 2 * i + 1;
     int4 de = __ldcg(a.desc + from);
     const int4 other = __ldcg(a.desc + 2 * i);
+    if ((other.w & kLate) && blockIdx.y == 0 && a.status)
+        for (int b = d; b < a.B; b += D) a.status[b] = SWITCHSD_ROW_TIMEOUT;  // some row is not done; which ones, the CTA does not know
     if (de.x < 0 || !(de.w & kFirst)) {
         from = 2 * i;
         de = other;
@@ -245,6 +251,6 @@ inline cudaError_t launch_join(const AttnArgs &a, int ctas, int R, cudaStream_t 
 
 // The kernel for many query rows (attention_tc.cu): bytes of partial results, and the launch of it and of its join.
 size_t attn_tc_workspace(int D);
-cudaError_t launch_attn_tc(const AttnArgs &a, bool f16, int D, int sms, cudaStream_t s);
+cudaError_t launch_attn_tc(AttnArgs a, bool f16, int D, int sms, cudaStream_t s);
 
 }  // namespace switchsd

@@ -27,6 +27,7 @@
 // that.  Slower were two groups of row warps on units in turn, 16 row warps, one pass over the scores that starts again where
 // the maximum rose, and all of a thread's scores loaded together for the weights too (303 us).
 #include <algorithm>
+#include <cstdlib>
 
 #include "attention.cuh"
 #include "tc.cuh"
@@ -65,8 +66,8 @@ struct TcSmem {
     static constexpr int bytes = 1024 + kQ + 2 * (kK + kV) + kRing * kRaw;
 };
 
-// A wait that gives up after a while (every one here is for this CTA's own work: some microseconds).  The thread may sleep
-// for up to 20 us a poll: a spinning warp takes its scheduler's issue slots from the rows' warps.
+// A wait that gives up after a number of polls (every one here is for this CTA's own work: some microseconds).  The thread may
+// sleep for up to 20 us a poll: a spinning warp takes its scheduler's issue slots from the rows' warps.
 __device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity) {
     const uint32_t addr = smem_addr(bar);
     for (uint32_t it = 0; it < 1u << 15; ++it) {
@@ -84,6 +85,8 @@ __device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity) {
     }
     return false;
 }
+// The same for all of a warp, whose threads go on together.
+__device__ __forceinline__ bool tc_wait_warp(uint64_t *bar, uint32_t parity) { return __all_sync(kFull, tc_wait(bar, parity)); }
 
 // The warps of 32 rows.
 __device__ __forceinline__ void rows_barrier(int quarter) { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + quarter), "n"(kSplit * kWarp) : "memory"); }
@@ -230,7 +233,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
     const int val_off = L::values(1 << a.page_shift), sc_off = L::scales(1 << a.page_shift);
     // Every wait of this thread has ended in time.  After one that has not, no further wait is begun and no result counts;
     // the row warps still go through their loops, because their barriers want all of them.
-    bool ok = true;
+    bool ok = !a.give_up || warp == kFetchWarp;
     Segment s;
 
     if (warp < kRowWarps) {
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             for (int32_t k = 0; k < s.n; ++k, ++i) {
                 const int buf = int(i & 1);
                 const int32_t key0 = (s.first + k) * kTcKeys;
-                ok = ok && tc_wait(&s_full[buf], (i >> 1) & 1);
+                ok = ok && tc_wait_warp(&s_full[buf], (i >> 1) & 1);
                 tc_fence_after();
                 const uint32_t sa = lanes + buf * 128 + part * KT;  // this thread's scores; its weights take their place
                 const uint4 valid4 = *reinterpret_cast<const uint4 *>(s_valid[i & 3]);
@@ -350,7 +353,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 const float off = kTcUp - m;
                 if (warp_mine) {
                     if (k > 0 && __any_sync(kFull, corr != 1.f)) {  // the units' sums so far, to the new reference
-                        ok = ok && tc_wait(&o_full, (i - 1) & 1);
+                        ok = ok && tc_wait_warp(&o_full, (i - 1) & 1);
                         tc_fence_after();
                         const bool lo = s_rows[quarter] == nseg;
 #pragma unroll 1
@@ -405,7 +408,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                 }
                 // The product of the unit before, every one in turn and before this warp's arrival, without which the next one
                 // does not begin: a barrier tells only neighbouring phases apart.
-                if (k > 0) ok = ok && tc_wait(&o_full, (i - 1) & 1);
+                if (k > 0) ok = ok && tc_wait_warp(&o_full, (i - 1) & 1);
                 tc_fence_before();
                 warp_arrive(&p_full[buf]);
             }
@@ -413,7 +416,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             s_x[i & 1][part][row] = l;
             rows_barrier(quarter);
             l = of_row([](float x, float y) { return x + y; });
-            ok = ok && tc_wait(&o_full, (i - 1) & 1);
+            ok = ok && tc_wait_warp(&o_full, (i - 1) & 1);
             tc_fence_after();
             seg = s_seg[warp];
             s = s_item[warp];
@@ -480,9 +483,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
         };
         auto keys = [&](uint32_t i, int32_t key0, int32_t len) {
             const int st = int(i & 1), rs = int(i % kRing);
-            bool in_time = tc_wait(&raw_full[rs], (i / kRing) & 1);
-            if (i >= 2) in_time = in_time && tc_wait(&k_empty[st], ((i >> 1) - 1) & 1);
-            ok = __all_sync(kFull, in_time);
+            ok = tc_wait_warp(&raw_full[rs], (i / kRing) & 1);
+            if (i >= 2) ok = ok && tc_wait_warp(&k_empty[st], ((i >> 1) - 1) & 1);
             if (!ok) return;
             const uint32_t exists = s_exist[rs][uw];
             const bool plain = exists == 0xffffffffu && key0 + 32 <= len + 1;
@@ -520,9 +522,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
         };
         auto values = [&](uint32_t i, int32_t key0, int32_t len) {
             const int st = int(i & 1), rs = int(i % kRing);
-            bool in_time = tc_wait(&raw_full[rs], (i / kRing) & 1);
-            if (i >= 2) in_time = in_time && tc_wait(&v_empty[st], ((i >> 1) - 1) & 1);
-            ok = __all_sync(kFull, in_time);
+            ok = tc_wait_warp(&raw_full[rs], (i / kRing) & 1);
+            if (i >= 2) ok = ok && tc_wait_warp(&v_empty[st], ((i >> 1) - 1) & 1);
             if (!ok) return;
             const uint32_t exists = s_exist[rs][uw];
             const bool plain = exists == 0xffffffffu && key0 + 32 <= len + 1;
@@ -577,7 +578,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
         if (more) find();
         while (more) {
             const int rs = int(i % kRing);
-            if (i >= kRing) ok = __all_sync(kFull, tc_wait(&raw_empty[rs], (i / kRing - 1) & 1));
+            if (i >= kRing) ok = tc_wait_warp(&raw_empty[rs], (i / kRing - 1) & 1);
             if (!ok) break;
             const int32_t key0 = (s.first + k) * kTcKeys, total = s.len + s.nw;
             const bool good = uint32_t(page) < uint32_t(a.pages);
@@ -608,9 +609,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             }
             if (more) find();
         }
-        // copies in flight write shared memory: the unpacking warps have waited for all of them, unless a wait gave up
-        if (!ok)
-            for (uint32_t j = i > kRing ? i - kRing : 0; j < i; ++j) (void)tc_wait(&raw_full[j % kRing], (j / kRing) & 1);
+        // copies in flight write shared memory: it stays the CTA's until they have come (also where another warp gave up on them)
+        for (uint32_t j = i > kRing ? i - kRing : 0; j < i; ++j) (void)tc_wait(&raw_full[j % kRing], (j / kRing) & 1);
         } else if (warp == kMmaWarp && lane == 0) {
         // ------------------------------------------------------------------------------------------- the MMAs
         uint32_t i = 0, nseg = 0;
@@ -663,12 +663,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
             if (ok) product(i - 1);  // before the next segment is looked up
             ++nseg;
         }
-        // what is in flight reads shared and tensor memory; the rows' threads have waited for the last product, unless a
-        // wait gave up
-        if (!ok) {
-            tc_commit(&stopped);
-            (void)tc_wait(&stopped, 0);
-        }
+        // what is in flight reads shared and tensor memory (the rows' threads wait for the last product too, unless they gave up)
+        tc_commit(&stopped);
+        (void)tc_wait(&stopped, 0);
         }
     }
     if (!ok) s_bad = 1;
@@ -677,10 +674,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
     tc_fence_after();
     if (warp == kMmaWarp)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kTcColumns) : "memory");
-    if (s_bad && a.status) {
-        // a wait ran out: some rows of this launch are not done; which ones the CTA does not know
-        for (int b = tid; b < a.B; b += kTcThreads) a.status[b] = SWITCHSD_ROW_TIMEOUT;
-    }
+    if (s_bad && tid == 0) a.desc[2 * cta].w |= kLate;  // (the thread that wrote it; the join writes the statuses)
+}
+
+// Whether the environment variable SWITCHSD_DIAG_ATTENTION_GIVE_UP is 1 (read once per process).  A diagnostic of the path
+// behind a wait that ran out: the rows', the unpacking and the MMAs' warps give up before their first wait, and the fetching
+// one once the ring that nobody empties is full and its own wait has run out; the statuses then say SWITCHSD_ROW_TIMEOUT.
+static bool tc_give_up() {
+    static const bool set = [] {
+        const char *v = std::getenv("SWITCHSD_DIAG_ATTENTION_GIVE_UP");
+        return v != nullptr && v[0] == '1' && v[1] == '\0';
+    }();
+    return set;
 }
 
 size_t attn_tc_workspace(int D) { return size_t(2 * kAttnMaxCtas) * sizeof(int4) + size_t(2 * 256) * kTcRows * (D + 4) * sizeof(float); }
@@ -703,7 +708,8 @@ static cudaError_t launch(const AttnArgs &a, int sms, cudaStream_t s) {
     return launch_join<F16, D>(a, int(ctas), kTcRows, s);
 }
 
-cudaError_t launch_attn_tc(const AttnArgs &a, bool f16, int D, int sms, cudaStream_t s) {
+cudaError_t launch_attn_tc(AttnArgs a, bool f16, int D, int sms, cudaStream_t s) {
+    a.give_up = tc_give_up();
     if (f16) return D == 128 ? launch<true, 128>(a, sms, s) : launch<true, 64>(a, sms, s);
     return D == 128 ? launch<false, 128>(a, sms, s) : launch<false, 64>(a, sms, s);
 }

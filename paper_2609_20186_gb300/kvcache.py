@@ -46,10 +46,12 @@ class KVCache:
         self.slots = torch.full((B, T), -1, **i32)
         self.status = torch.zeros(B, **i32)
         self.new = torch.zeros(B, **i32)
+        self.attend_status = torch.zeros(layers, B, **i32)
         self.workspace = torch.empty(bd.switchsd_kv4_attention_workspace_of(dim), dtype=torch.uint8, device=device)
         if stream is not None:
             stream.wait_stream(torch.cuda.current_stream(self.data.device))
-            for t in (self.data, self.table, self.held, self.free_list, self.free_count, self.slots, self.status, self.new, self.workspace):
+            for t in (self.data, self.table, self.held, self.free_list, self.free_count, self.slots, self.status, self.new, self.attend_status,
+                      self.workspace):
                 t.record_stream(stream)  # freed behind the calls
         self._lens = None
 
@@ -65,12 +67,14 @@ class KVCache:
         bd.switchsd_kv4_append(k, v, self.slots, self.data[layer], page=self.page, stream=self.stream)
 
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float | None = None) -> torch.Tensor:
-        """Attention of the new tokens' queries [B, T, query heads, dim] over `layer`, into `out`."""
+        """Attention of the new tokens' queries [B, T, query heads, dim] over `layer`, into `out`.  The rows' statuses go
+        to attend_status[layer]: other than 0 where the row was left out or, ROW_TIMEOUT in all rows, where `out` does not
+        count."""
         if self._lens is None:
             raise RuntimeError("map() comes before attend()")
         bd.switchsd_kv4_attention(q, self.data[layer], self.table, self._lens, self.new, out, page=self.page, scale=scale,
                                   lens_add=self.lens_add, new_add=self.new_add, workspace=self.workspace,
-                                  stream=self.stream)
+                                  status=self.attend_status[layer], stream=self.stream)
         return out
 
     def read(self, layer: int, slots: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:

@@ -63,3 +63,32 @@ def test_waits_that_run_out_say_so_in_every_row():
             for leg in out[name]["status"]:
                 assert [s for s in leg] == [2 if b == 1 else 0 for b in range(len(leg))]
     assert late["one token"] == plain["one token"]
+
+
+CACHE = r"""
+import json, sys
+sys.path.insert(0, sys.argv[1])
+import torch
+import paper_2609_20186_gb300 as fw
+torch.manual_seed(0)
+B, T, H, Hq, D = 3, 9, 1, 4, 64
+i32 = dict(dtype=torch.int32, device="cuda")
+c = fw.KVCache(B, T, layers=3, heads=H, dim=D, pages=5, max_len=64, page=16)
+x = torch.randn(B, T, Hq + 2 * H, D, device="cuda").to(torch.bfloat16)
+o = torch.empty(B, T, Hq, D, dtype=x.dtype, device="cuda")
+c.map(torch.tensor([3, 60, 0], **i32), torch.tensor([9, 9, 1], **i32))  # the second row asks for five pages: one too many
+for layer in (0, 2):
+    c.append(layer, x[:, :, Hq:Hq + H], x[:, :, Hq + H:])
+    c.attend(layer, x[:, :, :Hq], o)
+print(json.dumps(dict(map=c.status.tolist(), attend=c.attend_status.tolist())))
+"""
+
+
+def test_a_caches_layers_keep_their_statuses():
+    def child(env_extra):
+        env = {k: v for k, v in os.environ.items() if k != "SWITCHSD_DIAG_ATTENTION_GIVE_UP"}
+        r = subprocess.run([sys.executable, "-c", CACHE, ROOT], env={**env, **env_extra}, capture_output=True, text=True, timeout=600, cwd=ROOT)
+        assert r.returncode == 0, r.stderr[-2000:]
+        return json.loads(r.stdout.strip().splitlines()[-1])
+    assert child({}) == dict(map=[0, 1, 0], attend=[[0, 2, 0], [0, 0, 0], [0, 2, 0]])
+    assert child({"SWITCHSD_DIAG_ATTENTION_GIVE_UP": "1"}) == dict(map=[0, 1, 0], attend=[[3, 3, 3], [0, 0, 0], [3, 3, 3]])

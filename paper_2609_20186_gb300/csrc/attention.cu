@@ -13,8 +13,8 @@
 // signed numbers, four instructions a word more: taking 8 times the weights' sum off afterwards would leave an error of
 // that sum's size where the values are small.  The scales are applied outside: to the scores, and to the weights.
 //
-// Numbers.  The queries are scaled by a power of two so that they are f16 numbers exactly (a bf16 has fewer bits; what
-// lies 2^22 below the largest may lose bits); codes, and so keys and values, are exact; scores, maxima, sums and the
+// Numbers.  Each query is scaled by a power of two of its own so that it is f16 numbers exactly (a bf16 has fewer bits; what
+// lies 2^22 below its largest may lose bits, less than the binary32 sums do), and its scores by the inverse; codes, and so keys and values, are exact; scores, maxima, sums and the
 // output are binary32.  (The output's sums over the keys are the matrix unit's, which truncates: two additions for 32 keys
 // of a warp, a bias below 2^-23 of the sum each.)  The weights 2^12 exp(s - M) * scale_v are rounded to f16 (11 bits): M,
 // the reference, is at most 2^kLag below the running maximum of the score plus the logarithm of its value's scale, so
@@ -122,13 +122,14 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
 
         // --- queries: B operand, row n = lane / 4 of each of NT tiles of 8 --------------------------------------
         float start[NT][G][2];      // -8 sum of the query's group, of columns 2 c, 2 c + 1
-        float limit_f = 0.f;
+        float score[NT][2];         // of the column's query: the binary logarithm's scale of a sum of products
         int32_t limit[NT][2];       // last key that the column's query sees
         {
             uint4 raw[NT][G][2];
-            float big = 0.f;
+            float up[NT];           // of row r's query
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
+                float big = 0.f;
                 const int row = 8 * nt + r, rr = rt * R + row, t = rr / a.group, h = hk * a.group + rr - t * a.group;
                 const uint16_t *q = a.q + b * a.qs[0] + t * a.qs[1] + h * a.qs[2] + 16 * c;
 #pragma unroll
@@ -146,14 +147,16 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
                     const int row_c = 8 * nt + 2 * c + e;
                     limit[nt][e] = row_c < rows ? len + (rt * R + row_c) / a.group : -1;
                 }
-            }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(kFull, big, o));
-            // the power of two that brings the largest into [2^11, 2^12)
-            int ex = 11 - (int(__float_as_uint(big) >> 23) - 127);
-            ex = big > 0.f && big < INFINITY ? max(-100, min(100, ex)) : 0;
-            const float up = __int_as_float((127 + ex) << 23);
-            limit_f = __int_as_float((127 - ex) << 23) * a.scale * 1.4426950408889634f * 16777216.f;
+                for (int o = 1; o < 4; o <<= 1) big = fmaxf(big, __shfl_xor_sync(kFull, big, o));  // a row's four lanes
+                // the power of two that brings the row's largest into [2^11, 2^12)
+                int ex = 11 - (int(__float_as_uint(big) >> 23) - 127);
+                ex = big > 0.f && big < INFINITY ? max(-100, min(100, ex)) : 0;
+                up[nt] = __int_as_float((127 + ex) << 23);
+                const float down = __int_as_float((127 - ex) << 23) * a.scale * 1.4426950408889634f * 16777216.f;
+                score[nt][0] = __shfl_sync(kFull, down, 8 * c);
+                score[nt][1] = __shfl_sync(kFull, down, 8 * c + 4);
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -165,7 +168,7 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
                         uint32_t qb[4];            // [step x register]
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {  // pair e; the odd pairs' codes stand four bits higher
-                            const float x0 = widen1<F16>(uint16_t(w[e])) * up, x1 = widen1<F16>(uint16_t(w[e] >> 16)) * up;
+                            const float x0 = widen1<F16>(uint16_t(w[e])) * up[nt], x1 = widen1<F16>(uint16_t(w[e] >> 16)) * up[nt];
                             sum += x0 + x1;
                             const float f = e & 1 ? 0.0625f : 1.f;
                             qb[e] = pack_f16(x0 * f, x1 * f);
@@ -178,7 +181,6 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
                     start[nt][g][1] = __shfl_sync(kFull, sum, 8 * c + 4) * (-8.f / 16777216.f);
                 }
         }
-        const float score = limit_f;  // binary logarithm's scale of a sum of products
         __syncthreads();  // (every item ends with one too, behind which the next one's queries are written)
 
         float o[NT][MT][4], m[NT][2], l[NT][2];
@@ -271,8 +273,8 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
             for (int j = 0; j < 4; ++j) {
                 // scales of the token: G of the key, G of the value
                 const float2 k2 = __half22float2(*reinterpret_cast<const __half2 *>(&x.sc[j][0]));
-                ks[j][0] = k2.x * score;
-                if (G == 2) ks[j][G - 1] = k2.y * score;
+                ks[j][0] = k2.x;
+                if (G == 2) ks[j][G - 1] = k2.y;
                 value_scales[j] = x.sc[j][G - 1];
             }
 #pragma unroll
@@ -304,6 +306,10 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
                             } else {
                                 s[nt][2 * mt][e] = fmaf(acc[e], ks[2 * mt][g], s[nt][2 * mt][e]);
                                 s[nt][2 * mt + 1][e] = fmaf(acc[2 + e], ks[2 * mt + 1][g], s[nt][2 * mt + 1][e]);
+                            }
+                            if (g == G - 1) {
+                                s[nt][2 * mt][e] *= score[nt][e];
+                                s[nt][2 * mt + 1][e] *= score[nt][e];
                             }
                         }
                     }

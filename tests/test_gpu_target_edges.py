@@ -158,3 +158,62 @@ def test_a_row_without_pages_sits_the_step_out(T):
     assert step([15, 40], [1, 0]) == [0, 0]          # the first row's one page is full; its last token is rejected
     assert step([16, 40], [1, 0]) == [1, 0]          # and needs a second page, which there is not
     assert step([16, 31], [1, 0]) == [0, 0]          # the second row gave one back
+
+
+# --- attention ----------------------------------------------------------------------------------------------------
+def _bf16(x):
+    import torch
+    return torch.from_numpy(np.asarray(x, np.float64)).to(torch.bfloat16).cuda()
+
+
+def _filled(rng, n, Hkv, D, page):
+    """A cache with n random tokens of one row in order of its pages; its table, and the keys and values it holds."""
+    import torch
+    fw = _fw()
+    blocks = -(-n // page)
+    cache = torch.full((blocks, Hkv, fw.switchsd_kv4_bytes(page, D)), 0xff, dtype=torch.uint8, device="cuda")
+    k, v = ref.bf16_round(rng.standard_normal((n, Hkv, D))), ref.bf16_round(rng.standard_normal((n, Hkv, D)))
+    fw.switchsd_kv4_append(_bf16(k[None]), _bf16(v[None]), _i32(np.arange(n)[None]), cache, page=page)
+    return cache, _i32(np.arange(blocks)[None]), ref.dequantise(*ref.quantise(k)), ref.dequantise(*ref.quantise(v))
+
+
+def _near(got, want, mag):
+    """bf16's rounding, 2^-8 of the result, and the weights' and the scores', 2^-10 of sum p |v|: as in test_gpu_target.py."""
+    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * mag
+    assert np.all(np.abs(got - want) <= tol), float(np.nanmax(np.abs(got - want) / tol))
+
+
+@pytest.mark.parametrize("T", [1, 2, 5])  # tiles of 8, 16 and 128 query rows
+@pytest.mark.parametrize("up,odd", [(0, 24), (0, -30), (20, "inf"), (20, "nan")])
+def test_attention_of_a_head_goes_by_its_own_queries(T, up, odd):
+    """One head's queries 2^24 above, and 2^30 below, the others' of its tile, or with an infinity or a NaN among
+    them: the others' results are what they are without it."""
+    import torch
+    fw = _fw()
+    rng = np.random.default_rng(T)
+    Hq, D, page, n = 8, 128, 32, 200
+    cache, table, k, v = _filled(rng, n, 1, D, page)
+    q = ref.bf16_round(rng.standard_normal((1, T, Hq, D))) * 2.0 ** up
+    if isinstance(odd, int):
+        q[:, :, 3] *= 2.0 ** odd
+    else:
+        q[:, :, 3, 17] = float(odd)
+    scale = float(np.float32(D ** -0.5 * 2.0 ** -up))
+    out = torch.empty(1, T, Hq, D, dtype=torch.bfloat16, device="cuda")
+    fw.switchsd_kv4_attention(_bf16(q), cache, table, _i32([n - T]), _i32([T]), out, page=page, scale=scale)
+    got = out.double().cpu().numpy()
+    rest = [h for h in range(Hq) if h != 3]
+    want, mag = ref.attention(q[:, :, rest], [k], [v], [n - T], [T], scale)
+    _near(got[:, :, rest], want, mag)
+    if isinstance(odd, str):
+        assert np.isnan(got[:, :, 3]).all()
+    elif odd < 0:  # its scores are all but equal
+        want, mag = ref.attention(q[:, :, 3:4], [k], [v], [n - T], [T], scale)
+        _near(got[:, :, 3:4], want, mag)
+    else:          # one key has all of the weight: the largest score's, far above every rounding of the scores
+        x = np.einsum("td,nd->tn", q[0, :, 3], k[:, 0])
+        for t in range(T):
+            x[t, n - T + t + 1:] = -np.inf
+            best = np.sort(x[t])
+            if best[-1] - best[-2] > 2.0 ** -14 * np.abs(q[0, t, 3]).sum() * np.abs(k).max():
+                assert np.all(np.abs(got[0, t, 3] - v[np.argmax(x[t]), 0]) <= 2.0 ** -8 * np.abs(v[np.argmax(x[t]), 0]))

@@ -146,7 +146,7 @@ int switchsd_kv4_read(const switchsd_kv4_read_params *params);
  * among it; a NaN that it does see makes its result NaN, in the value's 64 dimensions or, where a call has many query
  * rows, in all of the head's.  Scores, the softmax's maximum and sum and the output's sum are held in binary32; the
  * weights that multiply the values are rounded to 11 bits.  The elements of a query that lie 2^22 and more below its own
- * largest may lose bits; magnitudes from 2^112 on, which only bf16 has, count as infinite.
+ * largest may lose bits; magnitudes from 2^116 on, which only bf16 has, count as infinite.
  *
  *   q             dtype (SWITCHSD_BF16 or SWITCHSD_F16) [B, T, Hq, D], strides in elements between rows, tokens and
  *                 heads (multiples of 8; a head's values are contiguous), 16-byte aligned

@@ -22,8 +22,8 @@
 // f16 has fewer bits, is multiplied apart, 2^24 higher.
 //
 // What bounds it: the instructions that unpack codes and weigh scores, at 12 warps an SM, about 60 % of the issue slots.
-// Measured: 64 contexts of 8K to 32K tokens, 8 key heads of 128 dimensions, 4 query heads each, one token a row: 362 us,
-// 58 % of the time that the 1.4 GB of cache need alone; 4 contexts of 32K to 128K, 8 query heads each: 100 us (53 %); one
+// Measured: 64 contexts of 8K to 32K tokens, 8 key heads of 128 dimensions, 4 query heads each, one token a row: 353 us,
+// of which the 1.4 GB of cache need 60 % alone; 4 contexts of 32K to 128K, 8 query heads each: 98 us (54 %); one
 // context of 2K: 11 us, with its join.
 #include <algorithm>
 

@@ -371,7 +371,9 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float off = kWeightLog - m[nt][e];
+                    // (rounded down: to nearest, a reference from 2^26 on, whose neighbours are 8 and more apart, would let
+                    // weights through that f16 does not have)
+                    const float off = __fsub_rd(kWeightLog, m[nt][e]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         s[nt][j][e] = exp2_approx(s[nt][j][e] + off);

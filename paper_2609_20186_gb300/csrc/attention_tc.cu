@@ -51,6 +51,7 @@ constexpr int kRing = 3;                    // units of codes on their way
 constexpr int kBlockBytes = 128 * 128;      // 128 rows of one swizzle row: an operand's 64 elements
 constexpr float kTcUp = 11.f;               // log2 of the weight of a score at the reference
 constexpr float kTcLag = 4.f;               // log2 of how far a weight may lie above: 2^15 is f16's
+constexpr float kTcFar = 4194304.f;         // 2^22: the rounding of references of this size and more would show in the weights
 constexpr float kTcSmall = 6.103515625e-5f; // 2^-14
 constexpr float kTcLift = 16777216.f;       // 2^24
 constexpr int kTcColumns = 512;             // tensor memory: S 2 x 128, O 128, O of the small weights 128
@@ -376,32 +377,40 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const AttnArgs a
                     }
                     const uint64_t scale2 = pair_of(scale, scale), off2 = pair_of(off, off);
                     uint64_t sum[2] = {0, 0};
+                    auto weigh = [&](auto exponents) {
 #pragma unroll 1
-                    for (int w = 0; w < KT / 32; ++w) {  // 32 keys: 16 words of weights in the first 16 of their scores' columns
-                        float v[32];
-                        uint32_t y[16];
-                        tmem_ld32(sa + 32 * w, v);
-                        tmem_wait_ld();
+                        for (int w = 0; w < KT / 32; ++w) {  // 32 keys: 16 words of weights in the first 16 of their scores' columns
+                            float v[32];
+                            uint32_t y[16];
+                            tmem_ld32(sa + 32 * w, v);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float2 x = halves_of(fma_pair(pair_of(v[2 * e], v[2 * e + 1]), scale2, off2));
-                            v[2 * e] = exp2_approx(x.x);
-                            v[2 * e + 1] = exp2_approx(x.y);
-                            sum[e & 1] = add_pair(sum[e & 1], pair_of(v[2 * e], v[2 * e + 1]));
-                            y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+                            for (int e = 0; e < 16; ++e) {
+                                const float2 x = exponents(v[2 * e], v[2 * e + 1]);
+                                v[2 * e] = exp2_approx(x.x);
+                                v[2 * e + 1] = exp2_approx(x.y);
+                                sum[e & 1] = add_pair(sum[e & 1], pair_of(v[2 * e], v[2 * e + 1]));
+                                y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+                            }
+                            tmem_st16(sa + 32 * w, y);
+                            if (small) {
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) v[e] = v[e] < kTcSmall ? (v[e] - __half2float(__float2half_rn(v[e]))) * kTcLift : 0.f;
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) y[e] = 0;
+                            }
+                            tmem_st16(sa + 32 * w + 16, y);
                         }
-                        tmem_st16(sa + 32 * w, y);
-                        if (small) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = v[e] < kTcSmall ? (v[e] - __half2float(__float2half_rn(v[e]))) * kTcLift : 0.f;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) y[e] = pack_f16(v[2 * e], v[2 * e + 1]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) y[e] = 0;
-                        }
-                        tmem_st16(sa + 32 * w + 16, y);
-                    }
+                    };
+                    // (a form of its own for references that large: in one, with what is seldom put in the scores' places first, drafts
+                    // took 1 to 5 % more)
+                    if (__any_sync(kFull, fabsf(m) > kTcFar && m > kFloor))  // the products rounded as the reference's was
+                        weigh([&](float x, float y) { return make_float2(__fsub_rn(__fmul_rn(x, scale), m) + kTcUp, __fsub_rn(__fmul_rn(y, scale), m) + kTcUp); });
+                    else
+                        weigh([&](float x, float y) { return halves_of(fma_pair(pair_of(x, y), scale2, off2)); });
                     const float2 both = halves_of(add_pair(sum[0], sum[1]));
                     l += both.x + both.y;
                     tmem_wait_st();

@@ -217,3 +217,34 @@ def test_attention_of_a_head_goes_by_its_own_queries(T, up, odd):
             best = np.sort(x[t])
             if best[-1] - best[-2] > 2.0 ** -14 * np.abs(q[0, t, 3]).sum() * np.abs(k).max():
                 assert np.all(np.abs(got[0, t, 3] - v[np.argmax(x[t]), 0]) <= 2.0 ** -8 * np.abs(v[np.argmax(x[t]), 0]))
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("T", [1, 2, 5])  # tiles of 8, 16 and 128 query rows
+def test_attention_of_scores_of_any_size(T, sign):
+    """Scores of 2^20 to 2^90, where binary32 numbers lie up to 2^66 apart: where the largest is the largest by far more than
+    the sums' rounding, its value is the result.  (A score's error is below 2^-14 sum |q| max |k|: 128 products, 2^-23 each.)"""
+    import torch
+    fw = _fw()
+    rng = np.random.default_rng(T)
+    Hq, D, page, n = 8, 128, 32, 600
+    cache = torch.full((-(-n // page), 1, fw.switchsd_kv4_bytes(page, D)), 0xff, dtype=torch.uint8, device="cuda")
+    k, v = ref.bf16_round(rng.standard_normal((n, 1, D)) + 0.5), ref.bf16_round(rng.standard_normal((n, 1, D)) * 40)
+    fw.switchsd_kv4_append(_bf16(k[None]), _bf16(v[None]), _i32(np.arange(n)[None]), cache, page=page)
+    table, k, v = _i32(np.arange(-(-n // page))[None]), ref.dequantise(*ref.quantise(k)), ref.dequantise(*ref.quantise(v))
+    for up in (18, 22, 23, 24, 25, 26, 28, 30, 40, 90):
+        # (the largest of many scores that are all positive, or all negative)
+        q = ref.bf16_round(sign * np.abs(rng.standard_normal((1, T, Hq, D)))) * 2.0 ** up
+        out = torch.empty(1, T, Hq, D, dtype=torch.bfloat16, device="cuda")
+        fw.switchsd_kv4_attention(_bf16(q), cache, table, _i32([n - T]), _i32([T]), out, page=page, scale=0.09)
+        got, sure = out.double().cpu().numpy(), 0
+        assert np.isfinite(got).all()
+        for t in range(T):
+            for h in range(Hq):
+                x = k[:n - T + t + 1, 0] @ q[0, t, h]
+                order = np.argsort(x)
+                if x[order[-1]] - x[order[-2]] > 2.0 ** -14 * np.abs(q[0, t, h]).sum() * np.abs(k).max() + 2.0 ** 9:
+                    want = v[order[-1], 0]
+                    _near(got[0, t, h], want, np.abs(want))
+                    sure += 1
+        assert sure >= T * Hq // 2

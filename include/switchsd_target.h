@@ -101,7 +101,7 @@ size_t switchsd_kv4_bytes(int32_t page, int32_t D);
  * the group's scale NaN; values beyond what the largest scale reaches saturate.
  *
  *   k, v        dtype (SWITCHSD_BF16 or SWITCHSD_F16) [B, T, Hkv, D], strides in elements between rows, tokens and
- *               heads (multiples of 8; a head's values are contiguous), 16-byte aligned
+ *               heads (multiples of 8, but for a dimension of one; a head's values are contiguous), 16-byte aligned
  *   slots       int32 [B, T]: as switchsd_kv_map writes them -- a row's slots are consecutive inside a page and begin
  *               a page at its first slot, and -1 past the row's new tokens.  Slots outside [0, pages * page) are
  *               skipped.
@@ -149,7 +149,7 @@ int switchsd_kv4_read(const switchsd_kv4_read_params *params);
  * largest may lose bits; magnitudes from 2^116 on, which only bf16 has, count as infinite.
  *
  *   q             dtype (SWITCHSD_BF16 or SWITCHSD_F16) [B, T, Hq, D], strides in elements between rows, tokens and
- *                 heads (multiples of 8; a head's values are contiguous), 16-byte aligned
+ *                 heads (multiples of 8, but for a dimension of one; a head's values are contiguous), 16-byte aligned
  *   out           dtype [B, T, Hq, D] contiguous, 16-byte aligned
  *   Hq            a multiple of Hkv, at most 64 times it
  *   block_table   int32 [B, blocks]

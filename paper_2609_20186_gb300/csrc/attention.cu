@@ -560,8 +560,9 @@ extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
     if (!p || !p->q || !p->cache || !p->block_table || !p->lens || !p->new_lens || !p->out || !p->workspace) return SWITCHSD_ERR_ARG;
     if (p->dtype != SWITCHSD_BF16 && p->dtype != SWITCHSD_F16) return SWITCHSD_ERR_ARG;
     if (!aligned16(p->q) || !aligned16(p->cache) || !aligned16(p->out) || !aligned16(p->workspace)) return SWITCHSD_ERR_ARG;
+    const int32_t sizes[3] = {p->B, p->T, p->Hq};
     for (int i = 0; i < 3; ++i)
-        if (p->q_stride[i] % 8 != 0 || p->q_stride[i] < 0) return SWITCHSD_ERR_ARG;
+        if (!stride_ok(p->q_stride[i], sizes[i])) return SWITCHSD_ERR_ARG;
     if (p->B < 1 || p->T < 1 || p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv != 0 || p->Hq / p->Hkv > 64 || p->blocks < 1 || p->pages < 1 ||
         !kv4_page_ok(p->page) || !kv4_dim_ok(p->D))
         return SWITCHSD_ERR_SHAPE;
@@ -571,7 +572,7 @@ extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
     if (p->workspace_bytes < switchsd_kv4_attention_workspace_bytes(p)) return SWITCHSD_ERR_ARG;
     AttnArgs a;
     a.q = static_cast<const uint16_t *>(p->q);
-    for (int i = 0; i < 3; ++i) a.qs[i] = p->q_stride[i];
+    for (int i = 0; i < 3; ++i) a.qs[i] = stride_of(p->q_stride[i], sizes[i]);
     a.cache = static_cast<const uint8_t *>(p->cache);
     a.table = p->block_table;
     a.lens = p->lens;

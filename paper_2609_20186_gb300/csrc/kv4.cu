@@ -435,16 +435,17 @@ extern "C" int switchsd_kv4_append(const switchsd_kv4_append_params *p) {
     if (!p || !p->k || !p->v || !p->slots || !p->cache) return SWITCHSD_ERR_ARG;
     if (p->dtype != SWITCHSD_BF16 && p->dtype != SWITCHSD_F16) return SWITCHSD_ERR_ARG;
     if (!aligned16(p->k) || !aligned16(p->v) || !aligned16(p->cache)) return SWITCHSD_ERR_ARG;
+    const int32_t sizes[3] = {p->B, p->T, p->Hkv};
     for (int i = 0; i < 3; ++i)
-        if (p->k_stride[i] % 8 != 0 || p->v_stride[i] % 8 != 0 || p->k_stride[i] < 0 || p->v_stride[i] < 0) return SWITCHSD_ERR_ARG;
+        if (!stride_ok(p->k_stride[i], sizes[i]) || !stride_ok(p->v_stride[i], sizes[i])) return SWITCHSD_ERR_ARG;
     if (p->B < 1 || p->T < 1 || p->Hkv < 1 || p->pages < 1 || !kv4_page_ok(p->page) || !kv4_dim_ok(p->D)) return SWITCHSD_ERR_SHAPE;
     if (int64_t(p->pages) * p->page > 0x7fffffff || int64_t(p->B) * p->T > 0x7fffffff) return SWITCHSD_ERR_SHAPE;
     AppendArgs a;
     a.k = static_cast<const uint8_t *>(p->k);
     a.v = static_cast<const uint8_t *>(p->v);
     for (int i = 0; i < 3; ++i) {
-        a.ks[i] = p->k_stride[i];
-        a.vs[i] = p->v_stride[i];
+        a.ks[i] = stride_of(p->k_stride[i], sizes[i]);
+        a.vs[i] = stride_of(p->v_stride[i], sizes[i]);
     }
     a.slots = p->slots;
     a.cache = static_cast<uint8_t *>(p->cache);

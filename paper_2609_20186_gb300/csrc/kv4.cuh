@@ -28,6 +28,9 @@ inline bool kv4_page_ok(int32_t page) {
 inline bool kv4_dim_ok(int32_t D) { return D == 64 || D == 128; }
 __host__ __device__ inline constexpr int kv4_page_bytes(int page, int D) { return page * (D + (D / 64) * 4); }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+// A stride of a dimension of n: no address goes by that of a dimension of one.
+inline bool stride_ok(int64_t stride, int32_t n) { return n == 1 || (stride >= 0 && stride % 8 == 0); }
+inline int64_t stride_of(int64_t stride, int32_t n) { return n == 1 ? 0 : stride; }
 inline int log2_of(int32_t pow2) {
     int s = 0;
     while ((1 << s) < pow2) ++s;

@@ -248,3 +248,24 @@ def test_attention_of_scores_of_any_size(T, sign):
                     _near(got[0, t, h], want, np.abs(want))
                     sure += 1
         assert sure >= T * Hq // 2
+
+
+def test_a_dimension_of_one_may_have_any_stride():
+    """Strides that no address goes by: of a batch, a step or a head count of one."""
+    import torch
+    fw = _fw()
+    rng = np.random.default_rng(3)
+    D, page, n = 64, 16, 20
+    cache, table, k, v = _filled(rng, n, 1, D, page)
+    q = ref.bf16_round(rng.standard_normal((1, 1, 1, D)))
+    flat = _bf16(q).reshape(-1)
+    x = flat.as_strided((1, 1, 1, D), (D + 1, 3 * D + 5, 7, 1))
+    out = torch.empty(1, 1, 1, D, dtype=torch.bfloat16, device="cuda")
+    fw.switchsd_kv4_attention(x, cache, table, _i32([n - 1]), _i32([1]), out, page=page, scale=0.125)
+    want, mag = ref.attention(q, [k], [v], [n - 1], [1], 0.125)
+    _near(out.double().cpu().numpy(), want, mag)
+    fw.switchsd_kv4_append(x, x, _i32([[3]]), cache, page=page)
+    ok, ov = (torch.empty(1, 1, 1, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    fw.switchsd_kv4_read(cache, _i32([[3]]), ok, ov, page=page)
+    held = ref.dequantise(*ref.quantise(q))
+    assert np.array_equal(ok.double().cpu().numpy(), held) and np.array_equal(ov.double().cpu().numpy(), held)

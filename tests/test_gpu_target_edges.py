@@ -269,3 +269,68 @@ def test_a_dimension_of_one_may_have_any_stride():
     fw.switchsd_kv4_read(cache, _i32([[3]]), ok, ov, page=page)
     held = ref.dequantise(*ref.quantise(q))
     assert np.array_equal(ok.double().cpu().numpy(), held) and np.array_equal(ov.double().cpu().numpy(), held)
+
+
+@pytest.mark.parametrize("of", ["key", "value"])
+@pytest.mark.parametrize("T,Hq,at", [(1, 4, 0), (2, 8, 1), (9, 4, 8), (9, 4, 3), (40, 4, 17), (9, 4, -5)])  # tiles of 8, 16 and 128 rows, two tiles
+def test_attention_of_a_nan_reaches_those_who_see_it(T, Hq, at, of):
+    """A NaN in the second group of 64 of the key or the value of new token `at` (-5: of a cached one): the tokens before it
+    are as without it, it and those after it get NaN -- a value's in its 64 dimensions at least."""
+    import torch
+    fw = _fw()
+    rng = np.random.default_rng(T + at)
+    D, page, n = 128, 16, 300
+    blocks = -(-n // page)
+    cache = torch.full((blocks, 1, fw.switchsd_kv4_bytes(page, D)), 0xff, dtype=torch.uint8, device="cuda")
+    k, v = ref.bf16_round(rng.standard_normal((n, 1, D))), ref.bf16_round(rng.standard_normal((n, 1, D)))
+    kn, vn = k.copy(), v.copy()
+    (kn if of == "key" else vn)[n - T + at, 0, 70] = np.nan
+    fw.switchsd_kv4_append(_bf16(kn[None]), _bf16(vn[None]), _i32(np.arange(n)[None]), cache, page=page)
+    k, v = ref.dequantise(*ref.quantise(k)), ref.dequantise(*ref.quantise(v))
+    q = ref.bf16_round(rng.standard_normal((1, T, Hq, D)))
+    out = torch.empty(1, T, Hq, D, dtype=torch.bfloat16, device="cuda")
+    fw.switchsd_kv4_attention(_bf16(q), cache, _i32(np.arange(blocks)[None]), _i32([n - T]), _i32([T]), out, page=page, scale=0.09)
+    got = out.double().cpu().numpy()
+    want, mag = ref.attention(q, [k], [v], [n - T], [T], 0.09)
+    first = max(at, 0)
+    _near(got[:, :first], want[:, :first], mag[:, :first])
+    assert np.isnan(got[:, first:, :, 64 if of == "value" else 0:]).all()
+    if of == "value" and T * Hq <= 16:
+        _near(got[:, first:, :, :64], want[:, first:, :, :64], mag[:, first:, :, :64])
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,D", [(1, 4, 2, 64), (5, 8, 2, 128)])
+def test_attention_of_more_rows_than_threads(T, Hq, Hkv, D):
+    """1500 ragged rows, some without new tokens, some of bad lengths: a thread looks up several; and twice the same, bit for
+    bit."""
+    import torch
+    fw = _fw()
+    rng = np.random.default_rng(D)
+    B, page = 1500, 16
+    lens, new = rng.integers(0, 70, B), rng.integers(0, T + 1, B)
+    lens[::7] = 0
+    need = -(-(lens + new) // page)
+    blocks, pages = int(need.max()), int(need.sum())
+    table, ids, at = np.full((B, blocks), -1), rng.permutation(pages), 0
+    for b in range(B):
+        table[b, :need[b]] = ids[at:at + need[b]]
+        at += need[b]
+    most = int((lens + new).max())
+    k, v = ref.bf16_round(rng.standard_normal((B, most, Hkv, D))), ref.bf16_round(rng.standard_normal((B, most, Hkv, D)))
+    p = np.arange(most)
+    slots = np.where(p < (lens + new)[:, None], np.take_along_axis(table, np.minimum(p // page, blocks - 1)[None].repeat(B, 0), 1) * page + p % page, -1)
+    cache = torch.full((pages, Hkv, fw.switchsd_kv4_bytes(page, D)), 0xff, dtype=torch.uint8, device="cuda")
+    fw.switchsd_kv4_append(_bf16(k), _bf16(v), _i32(slots), cache, page=page)
+    k, v = ref.dequantise(*ref.quantise(k)), ref.dequantise(*ref.quantise(v))
+    q = ref.bf16_round(rng.standard_normal((B, T, Hq, D)))
+    given = lens.copy()
+    given[5::50] = -1
+    outs = []
+    for _ in range(2):
+        out, status = torch.full((B, T, Hq, D), 9.0, dtype=torch.bfloat16, device="cuda"), torch.full((B,), 9, dtype=torch.int32, device="cuda")
+        fw.switchsd_kv4_attention(_bf16(q), cache, _i32(table), _i32(given), _i32(new), out, page=page, scale=0.1, status=status)
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1])
+    assert np.array_equal(status.cpu().numpy(), np.where(given < 0, 2, 0))
+    want, mag = ref.attention(q, [x[:n] for x, n in zip(k, lens + new)], [x[:n] for x, n in zip(v, lens + new)], lens, np.where(given < 0, 0, new), 0.1)
+    _near(outs[0].double().cpu().numpy(), want, mag)

@@ -47,6 +47,7 @@ class KVCache:
         self.status = torch.zeros(B, **i32)
         self.new = torch.zeros(B, **i32)
         self.attend_status = torch.zeros(layers, B, **i32)
+        self._layers = list(zip(self.data, self.attend_status))  # (a view made anew costs a call a microsecond)
         self.workspace = torch.empty(bd.switchsd_kv4_attention_workspace_of(dim), dtype=torch.uint8, device=device)
         if stream is not None:
             stream.wait_stream(torch.cuda.current_stream(self.data.device))
@@ -64,7 +65,7 @@ class KVCache:
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor) -> None:
         """The new tokens' keys and values [B, T, heads, dim] into `layer`."""
-        bd.switchsd_kv4_append(k, v, self.slots, self.data[layer], page=self.page, stream=self.stream)
+        bd.switchsd_kv4_append(k, v, self.slots, self._layers[layer][0], page=self.page, stream=self.stream)
 
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float | None = None) -> torch.Tensor:
         """Attention of the new tokens' queries [B, T, query heads, dim] over `layer`, into `out`.  The rows' statuses go
@@ -72,9 +73,10 @@ class KVCache:
         count."""
         if self._lens is None:
             raise RuntimeError("map() comes before attend()")
-        bd.switchsd_kv4_attention(q, self.data[layer], self.table, self._lens, self.new, out, page=self.page, scale=scale,
-                                  lens_add=self.lens_add, new_add=self.new_add, workspace=self.workspace,
-                                  status=self.attend_status[layer], stream=self.stream)
+        data, status = self._layers[layer]
+        bd.switchsd_kv4_attention(q, data, self.table, self._lens, self.new, out, page=self.page, scale=scale,
+                                  lens_add=self.lens_add, new_add=self.new_add, workspace=self.workspace, status=status,
+                                  stream=self.stream)
         return out
 
     def read(self, layer: int, slots: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
@@ -87,5 +89,5 @@ class KVCache:
             self.stream.wait_stream(torch.cuda.current_stream(slots.device))
             for t in (k, v):
                 t.record_stream(self.stream)
-        bd.switchsd_kv4_read(self.data[layer], slots, k, v, page=self.page, stream=self.stream)
+        bd.switchsd_kv4_read(self._layers[layer][0], slots, k, v, page=self.page, stream=self.stream)
         return k, v

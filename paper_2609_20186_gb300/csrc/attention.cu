@@ -14,17 +14,22 @@
 // that sum's size where the values are small.  The scales are applied outside: to the scores, and to the weights.
 //
 // Numbers.  Each query is scaled by a power of two of its own so that it is f16 numbers exactly (a bf16 has fewer bits; what
-// lies 2^22 below its largest may lose bits, less than the binary32 sums do), and its scores by the inverse; codes, and so keys and values, are exact; scores, maxima, sums and the
-// output are binary32.  (The output's sums over the keys are the matrix unit's, which truncates: two additions for 32 keys
-// of a warp, a bias below 2^-23 of the sum each.)  The weights 2^12 exp(s - M) * scale_v are rounded to f16 (11 bits): M,
-// the reference, is at most 2^kLag below the running maximum of the score plus the logarithm of its value's scale, so
-// that the largest weight fits whatever the scales; what rounding leaves of weights below 2^-26 of the reference, where
-// f16 has fewer bits, is multiplied apart, 2^24 higher.
+// lies 2^22 below its largest may lose bits, less than the binary32 sums do), and its scores by the inverse; codes, and so
+// keys and values, are exact; scores, maxima, sums and the output are binary32.  (The output's sums over the keys are the
+// matrix unit's, which truncates: two additions for 32 keys of a warp, a bias below 2^-23 of the sum each.)  The weights
+// 2^12 exp(s - M) * scale_v are rounded to f16 (11 bits): M, the reference, is at most 2^kLag below the running maximum of
+// the score plus the logarithm of its value's scale, so that the largest weight fits whatever the scales; what rounding
+// leaves of weights below 2^-26 of the reference, where f16 has fewer bits, is multiplied apart, 2^24 higher.
 //
-// What bounds it: the instructions that unpack codes and weigh scores, at 12 warps an SM, about 60 % of the issue slots.
+// Why the weights are f16: the matrix instructions take them so, and what their rounding leaves of every weight, multiplied
+// apart too, would double the values' instructions.  It disappears in a bf16 result; an f16 result over 32K to 128K keys is
+// 2.9e-4 off (relative to the result, over all of it) where binary32 weights leave it 2.1e-4 off, its own rounding.
+//
+// What bounds it: the instructions that unpack codes and weigh scores, at 12 warps an SM, about 56 % of the issue slots.
 // Measured: 64 contexts of 8K to 32K tokens, 8 key heads of 128 dimensions, 4 query heads each, one token a row: 353 us,
 // of which the 1.4 GB of cache need 60 % alone; 4 contexts of 32K to 128K, 8 query heads each: 98 us (54 %); one
-// context of 2K: 11 us, with its join.
+// context of 2K: 11 us, with its join.  Where many weights are small (eight times these queries), the first two take 386 and
+// 108 us.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -34,8 +39,8 @@ namespace switchsd {
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = kAttnWarps * kWarp;
 constexpr int kAttnUnit = kAttnWarps * 32;  // keys of a unit: 32 a warp
-// As many CTAs an SM as leave a warp its registers (168; 8 query rows: 2 CTAs 451, 3 CTAs 362, 4 CTAs, which spill, 468 us
-// for the first figures above; 16 rows of 64 contexts of 8K: 1 CTA 558, 2 CTAs 295, 3 CTAs 459 us).
+// As many CTAs an SM as leave a warp its registers (168; 8 query rows: 2 CTAs 453, 3 CTAs 353, 4 CTAs, which spill, 469 us
+// for the first figures above; 16 rows of 64 contexts of 8K: 1 CTA 438, 2 CTAs 235, 3 CTAs 545 us).
 constexpr int attn_ctas_per_sm(int NT) { return NT == 1 ? 3 : 2; }
 constexpr float kWeightLog = 12.f;          // log2 of the weight of a score (with its value's scale) at the reference
 constexpr float kLag = 3.f;                 // log2 of how far one may lie above: 2^15 is f16's
@@ -537,9 +542,9 @@ static cudaError_t launch_attn(AttnArgs a, int sms, cudaStream_t s) {
 }
 
 // Query rows of a key head up to which the tiles of 8 or 16 are faster than those of 128, whose time does not depend on
-// how many are filled.  Measured on 64 contexts of 8K: 16 rows 295 us here and 352 us there, 20 rows (two tiles here) 571
-// and 354 us, 48 rows 851 and 358 us.  A tile of 8 rather than 16 for 8 rows and fewer: 4 rows, 64 contexts of 8K to 32K
-// tokens, 362 and 713 us.  The contexts' lengths are on the device, so the choice goes by the rows alone.
+// how many are filled.  Measured on 64 contexts of 8K: 16 rows 235 us here and 356 us there, 20 rows (two tiles here) 449
+// and 359 us, 48 rows 663 and 364 us.  A tile of 8 rather than 16 for 8 rows and fewer: 4 rows, 64 contexts of 8K to 32K
+// tokens, 353 and 537 us.  The contexts' lengths are on the device, so the choice goes by the rows alone.
 constexpr int kTensorRows = 16;
 
 template <bool F16, int D>

@@ -21,11 +21,12 @@
 // What bounds it: the latencies of the rows' warps, and the instructions of the schedulers that hold the tile's first rows.
 // A unit takes about 3,200 cycles -- scores out of tensor memory, the maximum over a row's threads, weights (whose
 // exponentials alone are 1,000 cycles of a full tile), weights into tensor memory, a barrier each -- where its two products
-// take 500; half of the issue slots and 17 % of the memory's rate are used.  Measured: 64 contexts of 2K to 8K tokens, drafts
-// of up to 16, 4 query heads a key head: 258 us; 16 contexts of 8K to 32K, drafts of up to 32, 5 query heads a key head: 274
-// us (with the tiles of 16 rows 407 and 801 us).  Two numbers an instruction where weights are made and added took 6 us of
-// that.  Slower were two groups of row warps on units in turn, 16 row warps, one pass over the scores that starts again where
-// the maximum rose, and all of a thread's scores loaded together for the weights too (303 us).
+// take 500; half of the issue slots and 18 % of the memory's rate are used.  Measured: 64 contexts of 2K to 8K tokens, drafts
+// of up to 16, 4 query heads a key head: 256 us; 16 contexts of 8K to 32K, drafts of up to 32, 5 query heads a key head: 274
+// us (with the tiles of 16 rows 328 and 611 us).  Where many weights are small, with eight times these queries, they take 420
+// and 442 us.  Two numbers an instruction where weights are made and added saved 6 us.  Slower were two groups of row warps on
+// units in turn, 16 row warps, one pass over the scores that starts again where the maximum rose, and all of a thread's
+// scores loaded together for the weights too (303 us).
 #include <algorithm>
 #include <cstdlib>
 

@@ -16,9 +16,9 @@
 // additions, of 1.5 * 2^8 in the product's instruction and of 1.5 * 2^23 in one more, which leaves the code in the low
 // bits; eight of those words times powers of 16 add up to a cache word and a known constant.
 //
-// What bounds it: instructions (about 20 a value, 70 % of the issue slots) more than memory, 2 bytes read and 0.53 written
-// a value (and the other way round for the read).  16 rows of 2048 tokens, 8 heads of 128 dimensions: append and read take
-// 73 us, where the bytes alone would take 50; of 1 to 2048 tokens each 55 us (35).  A divided quotient and its comparisons
+// What bounds it: instructions (about 20 a value, the read 16; 65 and 60 % of the issue slots) more than memory, 2 bytes
+// read and 0.53 written a value (and the other way round for the read).  16 rows of 2048 tokens, 8 heads of 128 dimensions:
+// append and read take 74 us, where the bytes alone would take 50; of 1 to 2048 tokens each 56 us (35).  A divided quotient and its comparisons
 // took 94 us for the latter, limits on every code, not only those of wide groups, and words read token by token 60 us.
 #include <cuda_bf16.h>
 

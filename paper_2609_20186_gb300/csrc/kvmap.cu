@@ -7,8 +7,8 @@
 // One cluster of CTAs, each with 32 rows of every 32 * CTAs in turn (a warp a row, more where rows are few); every CTA
 // works out all rows' sums for itself, which costs less than handing them round, and cluster barriers stand between the
 // gives, the takes and the slots.  As many CTAs as there are 32s of rows, 8 at most.  Measured, two calls of which a third
-// of the rows begin or end (up to 512 pages each), one CTA against that rule: 128 rows 39 and 25 us, 1024 rows 175 and
-// 46 us, 8192 rows 1145 and 210 us; a second CTA for 16 rows only waits (17.4 and 18 us).
+// of the rows begin or end (up to 512 pages each), one CTA against that rule: 128 rows 37 and 24 us, 1024 rows 171 and
+// 45 us, 8192 rows 1147 and 214 us; a second CTA for 16 rows only waits (in a graph 14.2 us with one and 16.1 with two).
 //
 // What bounds it: latency -- the launch, and about four dependent trips to L2 (lengths, stack, table, slots); two calls
 // on 64 rows take 13 us in a graph.  With many rows, the scattered 4-byte moves of pages, 128 of a row in flight.

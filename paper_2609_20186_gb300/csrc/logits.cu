@@ -14,8 +14,8 @@
 //
 // What bounds it: the instructions and latencies of both: the first looks at every token of the context once a part and
 // adds up in shared memory, the second has 2 or 4 bytes an element to read (and write).  Measured: 64 rows of 8K to 32K
-// tokens, 1 to 17 positions, 128,256 tokens, masks and biases: 88 us, 28 of them the counting (148 MB of logits are 22 us);
-// 16 rows of 32K to 128K, 1 to 33 positions, 152,064 tokens, written: 106 us; one row and position: 12 us.  Measured and
+// tokens, 1 to 17 positions, 128,256 tokens, masks and biases: 89 us, 28 of them the counting (148 MB of logits are 22 us);
+// 16 rows of 32K to 128K, 1 to 33 positions, 152,064 tokens, written: 108 us; one row and position: 12 us.  Measured and
 // not kept: one kernel that counted and then streamed (126 us where the two took 104); the context cut over a cluster of
 // the parts, with remote additions (118 us where each part reading it whole takes 94); sending for the first logits while
 // the tokens are counted (no change).
@@ -515,8 +515,9 @@ __global__ void __launch_bounds__(kLogitThreads, 4) logits_kernel(const LogitArg
 }
 
 // log2 of the parts: enough that the shared memory of a part of the vocabulary leaves an SM two counting CTAs, and, where
-// rows are few, more, up to about a CTA an SM -- as long as each part has a chunk.  Measured with and without the latter:
-// one row and position 12 and 20 us (with 64K tokens of context 25 and 40 us), 4 rows of 1 to 17 positions 31 and 38 us.
+// rows are few, more, up to about a CTA an SM -- as long as each part has a chunk.  Measured with and without the latter, in a
+// graph: one row and position 12 and 16 us (with 64K tokens of context 25 and 34 us), 4 rows of 1 to 17 positions, masks and
+// biases 26 and 31 us.
 constexpr int kFewCtas = 128;
 static int parts_log_of(int32_t V, int32_t B) {
     int log = V > 131072 ? 4 : V > 8192 ? 3 : 2;

@@ -11,7 +11,7 @@ namespace switchsd {
 
 constexpr int kAttnMaxCtas = 1024;
 constexpr int kJoinParts = 4;     // partial results whose numbers are on their way together
-constexpr float kFloor = -1e30f;  // the maximum of nothing
+constexpr float kFloor = -3e38f;  // the maximum of nothing: below every score
 
 struct AttnArgs {
     const uint16_t *q;

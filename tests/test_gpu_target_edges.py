@@ -334,3 +334,29 @@ def test_attention_of_more_rows_than_threads(T, Hq, Hkv, D):
     assert np.array_equal(status.cpu().numpy(), np.where(given < 0, 2, 0))
     want, mag = ref.attention(q, [x[:n] for x, n in zip(k, lens + new)], [x[:n] for x, n in zip(v, lens + new)], lens, np.where(given < 0, 0, new), 0.1)
     _near(outs[0].double().cpu().numpy(), want, mag)
+
+
+@pytest.mark.parametrize("T", [1, 2, 5])  # tiles of 8, 16 and 128 query rows
+def test_attention_of_scores_far_below_zero(T):
+    """All scores near -2^115, which is still a score: the largest takes it all."""
+    import torch
+    fw = _fw()
+    rng = np.random.default_rng(T)
+    Hq, D, page, n = 4, 64, 16, 500
+    cache = torch.full((-(-n // page), 1, fw.switchsd_kv4_bytes(page, D)), 0xff, dtype=torch.uint8, device="cuda")
+    k, v = ref.bf16_round(np.abs(rng.standard_normal((n, 1, D))) + 1), ref.bf16_round(rng.standard_normal((n, 1, D)))
+    fw.switchsd_kv4_append(_bf16(k[None]), _bf16(v[None]), _i32(np.arange(n)[None]), cache, page=page)
+    k, v = ref.dequantise(*ref.quantise(k)), ref.dequantise(*ref.quantise(v))
+    q = ref.bf16_round(-np.abs(rng.standard_normal((1, T, Hq, D))) - 0.5) * 2.0 ** 108
+    out = torch.empty(1, T, Hq, D, dtype=torch.bfloat16, device="cuda")
+    fw.switchsd_kv4_attention(_bf16(q), cache, _i32(np.arange(-(-n // page))[None]), _i32([n - T]), _i32([T]), out, page=page, scale=1.0)
+    got, sure = out.double().cpu().numpy(), 0
+    for t in range(T):
+        for h in range(Hq):
+            x = k[:n - T + t + 1, 0] @ q[0, t, h]
+            assert -2.0 ** 117 < x.min() and x.max() < -2.0 ** 113
+            order = np.argsort(x)
+            if x[order[-1]] - x[order[-2]] > 2.0 ** -14 * np.abs(q[0, t, h]).sum() * np.abs(k).max():
+                _near(got[0, t, h], v[order[-1], 0], np.abs(v[order[-1], 0]))
+                sure += 1
+    assert sure >= T * Hq // 2

@@ -206,7 +206,8 @@ int switchsd_kv4_attention(const switchsd_kv4_attention_params *params);
  *                 the GPU.  (The size goes by B, T, V, cap, nbias and which of the inputs are given.)
  *   status        int32 [B] or NULL: SWITCHSD_ROW_BAD_LEN for a context length outside [0, cap] or new outside [0, T]
  *                 (the row is left out: argmax -1)
- * Tokens of the context and the draft outside [0, V) count for nothing.
+ * Tokens of the context and the draft outside [0, V) count for nothing.  B 1 .. 65535, T 1 .. 262140, V 1 .. SWITCHSD_VMAX,
+ * nbias up to SWITCHSD_BIAS_MAX.
  */
 typedef struct {
     int32_t B, T, V, cap, dtype;

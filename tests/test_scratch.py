@@ -5,9 +5,11 @@ import inspect
 import torch
 
 from paper_2609_20186_gb300 import binding as bd
+from paper_2609_20186_gb300 import build
 
 
 def test_scratch_is_taken_under_the_calls_stream(monkeypatch):
+    build.build()
     under, seen = [], []
     real = torch.empty
 

@@ -12,6 +12,16 @@
  *                           position's greedy token: the target_argmax of switchsd_verify;
  *   switchsd_kv4_read       the values that the cache holds for some tokens.
  *
+ * The same cache in 16 bits, for a target whose own distribution counts, and for the prompts' chunks:
+ *
+ *   switchsd_kv16_append, switchsd_kv16_read, switchsd_kv16_attention
+ *
+ * And what the verification at temperature > 0 (switchsd_verify_sampled) takes, from logits:
+ *
+ *   switchsd_logprobs       log probabilities of given tokens (the drafts' p_draft and q_draft among them), the entropy
+ *                           and the top alternatives of every position;
+ *   switchsd_resample       the token that the verification will append: its `resample`.
+ *
  * The conventions of switchsd.h hold: caller-owned device pointers, asynchronous on `stream`, host codes before
  * anything is enqueued, per-row device status, capture into CUDA graphs, no allocation.
  *
@@ -35,8 +45,9 @@ extern "C" {
 #define SWITCHSD_F32 2
 
 #define SWITCHSD_MAP_ROWS 8192  /* largest B of switchsd_kv_map */
-#define SWITCHSD_VMAX 262144    /* largest vocabulary of switchsd_logits */
+#define SWITCHSD_VMAX 262144    /* largest vocabulary */
 #define SWITCHSD_BIAS_MAX 4096  /* largest number of biases a row */
+#define SWITCHSD_TOP_MAX 32     /* largest number of top alternatives */
 
 /*
  * Block tables and slot maps.  A pool of `pages` pages of `page` tokens (16, 32, 64, 128 or 256) serves B rows.
@@ -177,6 +188,35 @@ size_t switchsd_kv4_attention_workspace_bytes(const switchsd_kv4_attention_param
 int switchsd_kv4_attention(const switchsd_kv4_attention_params *params);
 
 /*
+ * The 16-bit cache of one layer: dtype [pages][2][Hkv][page][D], the keys (0) and the values (1), 16-byte aligned; D = 64
+ * or 128, pages of 16, 32, 64, 128 or 256 tokens.  Parameters as those of the 4-bit cache, dtype (SWITCHSD_BF16 or
+ * SWITCHSD_F16) being the cache's type too.
+ *
+ * Append: the new tokens' keys and values into the cache, as they are.  Strides, alignment and slots as
+ * switchsd_kv4_append; the slots may come in any order (where two tokens name one slot, which of them it holds, 8 elements
+ * at a time, is not defined), and calls that write different slots may overlap.  B * T * Hkv < 2^30 (here and for the read).
+ * Read: what the cache holds for given slots, as it is; zeros for slots outside [0, pages * page).
+ */
+typedef switchsd_kv4_append_params switchsd_kv16_append_params;
+typedef switchsd_kv4_read_params switchsd_kv16_read_params;
+
+int switchsd_kv16_append(const switchsd_kv16_append_params *params);
+int switchsd_kv16_read(const switchsd_kv16_read_params *params);
+
+/*
+ * Attention over the 16-bit cache: what switchsd_kv4_attention computes, for one new token to a prompt's chunk, with the
+ * same rules for lengths, pages, statuses and places that a token does not see (a token's result is what it would be if
+ * they held zeros).  Products are exact, and scores, the softmax's maximum and sum and the output's sum are held in
+ * binary32; the weights that multiply the values are rounded to dtype.  (f16 weights lose bits where they are below 2^-25
+ * of their row's largest, and are 0 below 2^-36 of it.)  A NaN that a token sees in a value makes its result NaN in that
+ * dimension, a NaN score in all of the head's.
+ */
+typedef switchsd_kv4_attention_params switchsd_kv16_attention_params;
+
+size_t switchsd_kv16_attention_workspace_bytes(const switchsd_kv16_attention_params *params);
+int switchsd_kv16_attention(const switchsd_kv16_attention_params *params);
+
+/*
  * Logits of B rows and T positions.  Position t of row b (t < new) follows the row's context x[0 .. L-1] and the
  * draft's first t tokens.  With n_v the number of times that token v occurs there, m_v the same without the context's
  * first prompt_lens[b] tokens, and every operation rounded to binary32,
@@ -236,6 +276,106 @@ typedef struct {
 
 size_t switchsd_logits_workspace_bytes(const switchsd_logits_params *params);
 int switchsd_logits(const switchsd_logits_params *params);
+
+/*
+ * Log probabilities.  With l the logits of position t < new of row b, z = l / temperature[b] and v a token,
+ *
+ *   lse = ln sum_v e^z_v      logprob_v = z_v - lse      entropy = - sum_v e^logprob_v logprob_v
+ *
+ * A temperature of 0 is the limit: logprob is 0 for the smallest v with the largest l and -inf for the others, entropy 0,
+ * and lse = max l (which is what switchsd_resample takes).  l = -inf and NaN have no weight (logprob -inf), as for
+ * switchsd_logits.  Where nothing has any: logprob -inf, entropy 0, lse -inf.  A logit of +inf makes lse +inf, and the
+ * position's other numbers NaN (but at temperature 0).  Everything is worked out in binary32.
+ *
+ *   logits        dtype (SWITCHSD_BF16, SWITCHSD_F16, SWITCHSD_F32) [B, T, V], strides in elements between rows and
+ *                 positions (V values are contiguous), aligned to its elements
+ *   new_lens      int32 [B] or NULL: positions of each row, T when NULL.  new_add is added.
+ *   temperature   float [B] or NULL (1): finite and >= 0; others make the row's lse, entropy and log probabilities NaN
+ *   tokens        int32 [B, tokens_stride], of which entries 0 .. K - 1 of a row are read (K <= T); NULL with K = 0
+ *   logprob, prob float [B, K] or NULL: of tokens[b, t] at position t, and its exponential (p_draft, or the drafter's
+ *                 q_draft, where tokens is the draft): -inf and 0 for tokens outside [0, V) and for t >= new
+ *   entropy, lse  float [B, T] or NULL: 0 and -inf for t >= new
+ *   top_ids       int32 [B, T, top] or NULL: the tokens with the largest l, largest first, of equal ones the smallest first;
+ *                 -1 where there are no more with a weight, and for t >= new
+ *   top_logprobs  float [B, T, top] or NULL: theirs; -inf at the -1
+ *   status        int32 [B] or NULL: SWITCHSD_ROW_BAD_LEN for new outside [0, T] (the row has no positions then)
+ * At least one output besides status.  B 1 .. 65535, T 1 .. 262140, V 1 .. SWITCHSD_VMAX, top 0 .. SWITCHSD_TOP_MAX.
+ */
+typedef struct {
+    int32_t B, T, V, K, top, dtype;
+    const void *logits;
+    int64_t stride_b, stride_t;
+    const int32_t *new_lens;
+    int32_t new_add;
+    int32_t tokens_stride;
+    const float *temperature;
+    const int32_t *tokens;
+    float *logprob, *prob, *entropy, *lse;
+    int32_t *top_ids;
+    float *top_logprobs;
+    int32_t *status;
+    void *stream;
+} switchsd_logprobs_params;
+
+int switchsd_logprobs(const switchsd_logprobs_params *params);
+
+/*
+ * The token that switchsd_verify_sampled appends: `resample` for the one entry that it will take.  With a the accepted
+ * length (draft token i < draft_len is accepted iff u_i * q_i < p_i, as there), l the target's logits at position a and
+ * p_v = e^(l_v / temperature - lse),
+ *
+ *   a = draft_len                          w = p                            the target's own distribution
+ *   a < draft_len, copied draft            w = p, but 0 for draft[a]        max(0, p - q) with q one-hot
+ *   a < draft_len, a drafter's             w = max(0, p - q)                q_v = e^(q_logits_v / temperature - q_lse)
+ *
+ * (w = p where that leaves nothing), and the token is the v with the largest
+ *
+ *   ln w_v - ln E_v,   E_v = -ln(1 - x_v),   x_v = (r_v + 1/2) / 2^32
+ *
+ * the smallest of equal ones, -1 where no token has a weight (l = -inf and NaN have none).  The E_v are exponential, so
+ * the token is v with probability w_v / sum w.  r_v is a 32-bit number from the row's seed and the appended token's place
+ * in the context: with g = 0x9E3779B97F4A7C15 and mix the output function of splitmix64, in 64 bits,
+ *
+ *   key = mix(seed + (ctx_len + a + 1) g),   r_2n + 2^32 r_2n+1 = mix(key + (n + 1) g)
+ *
+ * so a row's draws depend on its own seed and length only, and a call that is made again draws the same.  What decides is
+ * compared in binary32 where that is enough and else in binary64, as if all were.  A temperature of 0: the smallest v with
+ * the largest l, whatever the draft.
+ *
+ *   T             positions: drafts have up to T - 1 tokens
+ *   logits        dtype [B, T, V] as for switchsd_logprobs
+ *   lse           float [B, T] of the logits (at least for positions that a drafter's draft is rejected at), or NULL
+ *                 without q_logits
+ *   temperature   float [B] or NULL (1), finite and >= 0 (others, and a NaN lse that is looked at: -1)
+ *   draft         int32 [B, T - 1];  draft_len  int32 [B]
+ *   p_draft, u    float [B, T - 1];  q_draft  float [B, T - 1] or NULL (1)
+ *   q_logits      dtype [B, T - 1, V] with its own strides, or NULL: every draft is a copied one;  q_lse  float [B, T - 1]
+ *   mode          int32 [B] or NULL: rows of SWITCHSD_MODE_COPY hold copied drafts beside q_logits
+ *   seeds         int64 [B];  ctx_lens  int32 [B]
+ *   out           int32 [B, T]: the token at entry a, -1 elsewhere
+ *   status        int32 [B] or NULL: SWITCHSD_ROW_BAD_LEN for draft_len outside [0, T - 1] or a negative ctx_len (all of
+ *                 the row's entries are -1)
+ * The inputs of T - 1 columns may be NULL for T = 1.  B 1 .. 65535, T 1 .. 262140, V 1 .. SWITCHSD_VMAX.
+ */
+typedef struct {
+    int32_t B, T, V, dtype;
+    const void *logits;
+    int64_t stride_b, stride_t;
+    const float *lse, *temperature;
+    const int32_t *draft, *draft_len;
+    const float *p_draft, *q_draft, *u;
+    const void *q_logits;
+    int64_t q_stride_b, q_stride_t;
+    const float *q_lse;
+    const int32_t *mode;
+    const int64_t *seeds;
+    const int32_t *ctx_lens;
+    int32_t *out;
+    int32_t *status;
+    void *stream;
+} switchsd_resample_params;
+
+int switchsd_resample(const switchsd_resample_params *params);
 
 #ifdef __cplusplus
 }

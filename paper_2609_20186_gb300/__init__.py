@@ -12,6 +12,7 @@ from .binding import (  # noqa: F401
     switchsd_verify_params, switchsd_harness_params, NgramIndex, load, strerror, abi_version,
     MODE_NO_REP, MODE_COPY, MODE_REP_NO_COPY, PROBE_LINEAR, PROBE_MLP,
     switchsd_kv_map, switchsd_kv4_bytes, switchsd_kv4_append, switchsd_kv4_read, switchsd_kv4_attention, switchsd_logits,
+    switchsd_kv16_append, switchsd_kv16_read, switchsd_kv16_attention, switchsd_kv16_attention_workspace, switchsd_logprobs, switchsd_resample,
 )
 from .kvcache import KVCache  # noqa: F401
 from .session import HostPlan, Session, bf16_tensor  # noqa: F401

@@ -161,6 +161,35 @@ class switchsd_logits_params(ctypes.Structure):
     ]
 
 
+switchsd_kv16_append_params, switchsd_kv16_read_params = switchsd_kv4_append_params, switchsd_kv4_read_params
+switchsd_kv16_attention_params = switchsd_kv4_attention_params
+
+
+class switchsd_logprobs_params(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("K", ctypes.c_int32),
+        ("top", ctypes.c_int32), ("dtype", ctypes.c_int32), ("logits", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+        ("stride_t", ctypes.c_int64), ("new_lens", ctypes.c_void_p), ("new_add", ctypes.c_int32),
+        ("tokens_stride", ctypes.c_int32), ("temperature", ctypes.c_void_p), ("tokens", ctypes.c_void_p),
+        ("logprob", ctypes.c_void_p), ("prob", ctypes.c_void_p), ("entropy", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+        ("top_ids", ctypes.c_void_p), ("top_logprobs", ctypes.c_void_p), ("status", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class switchsd_resample_params(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("logits", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64),
+        ("lse", ctypes.c_void_p), ("temperature", ctypes.c_void_p), ("draft", ctypes.c_void_p),
+        ("draft_len", ctypes.c_void_p), ("p_draft", ctypes.c_void_p), ("q_draft", ctypes.c_void_p),
+        ("u", ctypes.c_void_p), ("q_logits", ctypes.c_void_p), ("q_stride_b", ctypes.c_int64),
+        ("q_stride_t", ctypes.c_int64), ("q_lse", ctypes.c_void_p), ("mode", ctypes.c_void_p),
+        ("seeds", ctypes.c_void_p), ("ctx_lens", ctypes.c_void_p), ("out", ctypes.c_void_p), ("status", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
 _lock = threading.Lock()
 _lib = None
 
@@ -226,6 +255,12 @@ _SIGNATURES = {
     "switchsd_kv4_attention": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_attention_params)]),
     "switchsd_logits_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(switchsd_logits_params)]),
     "switchsd_logits": (ctypes.c_int, [ctypes.POINTER(switchsd_logits_params)]),
+    "switchsd_kv16_append": (ctypes.c_int, [ctypes.POINTER(switchsd_kv16_append_params)]),
+    "switchsd_kv16_read": (ctypes.c_int, [ctypes.POINTER(switchsd_kv16_read_params)]),
+    "switchsd_kv16_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(switchsd_kv16_attention_params)]),
+    "switchsd_kv16_attention": (ctypes.c_int, [ctypes.POINTER(switchsd_kv16_attention_params)]),
+    "switchsd_logprobs": (ctypes.c_int, [ctypes.POINTER(switchsd_logprobs_params)]),
+    "switchsd_resample": (ctypes.c_int, [ctypes.POINTER(switchsd_resample_params)]),
 }
 
 
@@ -680,3 +715,111 @@ def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_l
         workspace = _scratch(load().switchsd_logits_workspace_bytes(ctypes.byref(p)), logits.device, stream)
     p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
     _check(load().switchsd_logits(ctypes.byref(p)), "switchsd_logits")
+
+
+def _cache16_shape(cache, H: int, D: int):
+    """pages and tokens a page of a 16-bit cache [pages, 2, H, page, D] of one layer."""
+    if not isinstance(cache, torch.Tensor) or cache.dim() != 5 or cache.shape[1] != 2 or cache.shape[4] != D or (H and cache.shape[2] != H):
+        raise ValueError(f"the cache has shape {tuple(getattr(cache, 'shape', ()))}, expected [pages, 2, {H or 'Hkv'}, page, {D}]")
+    if cache.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError(f"the cache must be bfloat16 or float16, got {cache.dtype}")
+    return cache.shape[0], cache.shape[3]
+
+
+def switchsd_kv16_append(k, v, slots, cache, *, stream=None) -> None:
+    """switchsd_kv16_append of include/switchsd_target.h: k, v [B, T, Hkv, D] (views whose last dimension is contiguous)
+    of the cache's type, slots int32 [B, T], cache bf16 or f16 [pages, 2, Hkv, page, D]."""
+    B, T, H, D = k.shape
+    pages, page = _cache16_shape(cache, H, D)
+    dtype = _strided(k, "k", (B, T, H, D), (cache.dtype,))
+    _strided(v, "v", (B, T, H, D), (cache.dtype,))
+    p = switchsd_kv16_append_params(
+        B, T, H, D, page, pages, dtype, k.data_ptr(), v.data_ptr(), k.stride()[:3], v.stride()[:3],
+        _dev(slots, torch.int32, "slots", (B, T)), _dev(cache, cache.dtype, "cache"), _stream_ptr(stream))
+    _check(load().switchsd_kv16_append(ctypes.byref(p)), "switchsd_kv16_append")
+
+
+def switchsd_kv16_read(cache, slots, out_k, out_v, *, stream=None) -> None:
+    """switchsd_kv16_read of include/switchsd_target.h: what the cache holds for slots int32 [B, T], into out_k and out_v
+    [B, T, Hkv, D] of its type."""
+    B, T, H, D = out_k.shape
+    pages, page = _cache16_shape(cache, H, D)
+    p = switchsd_kv16_read_params(
+        B, T, H, D, page, pages, _dev(cache, cache.dtype, "cache"), _dev(slots, torch.int32, "slots", (B, T)),
+        _dev(out_k, cache.dtype, "out_k", (B, T, H, D)), _dev(out_v, cache.dtype, "out_v", (B, T, H, D)), _stream_ptr(stream))
+    _check(load().switchsd_kv16_read(ctypes.byref(p)), "switchsd_kv16_read")
+
+
+@functools.lru_cache(maxsize=64)
+def switchsd_kv16_attention_workspace(D: int) -> int:
+    """Bytes of the workspace of any switchsd_kv16_attention on heads of D dimensions; 0 for sizes that it does not have."""
+    p = switchsd_kv16_attention_params()
+    p.D = D
+    return int(load().switchsd_kv16_attention_workspace_bytes(ctypes.byref(p)))
+
+
+def switchsd_kv16_attention(q, cache, block_table, lens, new_lens, out, *, scale: float | None = None, lens_add: int = 0,
+                            new_add: int = 0, workspace=None, status=None, stream=None) -> None:
+    """switchsd_kv16_attention of include/switchsd_target.h: q [B, T, Hq, D] (a view whose last dimension is contiguous) of
+    the cache's type, cache bf16 or f16 [pages, 2, Hkv, page, D], block_table int32 [B, blocks], lens, new_lens int32 [B],
+    out [B, T, Hq, D] of q's type.  scale: 1 / sqrt(D) when None.  Takes its workspace from torch, in the order of the
+    call's stream, when none is given."""
+    B, T, Hq, D = q.shape
+    (pages, page), Hkv, blocks, row = _cache16_shape(cache, 0, D), cache.shape[2], block_table.shape[1], (B,)
+    dtype = _strided(q, "q", (B, T, Hq, D), (cache.dtype,))
+    p = switchsd_kv16_attention_params(
+        B, T, Hq, Hkv, D, page, pages, blocks, dtype, q.data_ptr(), q.stride()[:3], _dev(cache, cache.dtype, "cache"),
+        _dev(block_table, torch.int32, "block_table", (B, blocks)), _dev(lens, torch.int32, "lens", row),
+        _dev(new_lens, torch.int32, "new_lens", row), lens_add, new_add, D ** -0.5 if scale is None else scale,
+        _dev(out, q.dtype, "out", (B, T, Hq, D)), None, 0, _dev(status, torch.int32, "status", row), _stream_ptr(stream))
+    if workspace is None:
+        workspace = _scratch(switchsd_kv16_attention_workspace(D), q.device, stream)
+    p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
+    _check(load().switchsd_kv16_attention(ctypes.byref(p)), "switchsd_kv16_attention")
+
+
+def switchsd_logprobs(logits, *, tokens=None, new_lens=None, new_add: int = 0, temperature=None, logprob=None, prob=None,
+                      entropy=None, lse=None, top_ids=None, top_logprobs=None, status=None, stream=None) -> None:
+    """switchsd_logprobs of include/switchsd_target.h: logits bf16, f16 or float32 [B, T, V] (a view whose last dimension is
+    contiguous); tokens int32 [B, K], K <= T, with logprob and / or prob float32 [B, K]; new_lens int32 [B]; temperature
+    float32 [B]; entropy, lse float32 [B, T]; top_ids int32, top_logprobs float32 [B, T, n]; one output at least."""
+    B, T, V = logits.shape
+    dtype = _strided(logits, "logits", (B, T, V), tuple(_DTYPES))
+    if tokens is None and (logprob is not None or prob is not None):
+        raise ValueError("logprob and prob are of tokens")
+    K = tokens.shape[1] if tokens is not None else 0
+    of_top = top_ids if top_ids is not None else top_logprobs
+    top = of_top.shape[2] if of_top is not None else 0
+    i32, f32, row, strides = torch.int32, torch.float32, (B,), logits.stride()
+    p = switchsd_logprobs_params(
+        B, T, V, K, top, dtype, logits.data_ptr(), strides[0], strides[1], _dev(new_lens, i32, "new_lens", row), new_add, K,
+        _dev(temperature, f32, "temperature", row), _dev(tokens, i32, "tokens", (B, K)), _dev(logprob, f32, "logprob", (B, K)),
+        _dev(prob, f32, "prob", (B, K)), _dev(entropy, f32, "entropy", (B, T)), _dev(lse, f32, "lse", (B, T)),
+        _dev(top_ids, i32, "top_ids", (B, T, top)), _dev(top_logprobs, f32, "top_logprobs", (B, T, top)),
+        _dev(status, i32, "status", row), _stream_ptr(stream))
+    _check(load().switchsd_logprobs(ctypes.byref(p)), "switchsd_logprobs")
+
+
+def switchsd_resample(logits, draft, draft_len, p_draft, u, out, *, seeds, ctx_lens, temperature=None, lse=None, q_draft=None,
+                      q_logits=None, q_lse=None, mode=None, status=None, stream=None) -> None:
+    """switchsd_resample of include/switchsd_target.h: logits bf16, f16 or float32 [B, T, V] and q_logits [B, T - 1, V] of
+    the same type (views whose last dimension is contiguous); draft int32, p_draft, q_draft, u float32 [B, T - 1];
+    draft_len, ctx_lens, mode int32 [B]; seeds int64 [B]; temperature float32 [B]; lse float32 [B, T], q_lse float32
+    [B, T - 1]; out int32 [B, T]: the `resample` of switchsd_verify_sampled at the entry that it takes, -1 elsewhere."""
+    B, T, V = logits.shape
+    dtype = _strided(logits, "logits", (B, T, V), tuple(_DTYPES))
+    q_ptr, q_strides = None, (0, 0)
+    if q_logits is not None:
+        _strided(q_logits, "q_logits", (B, T - 1, V), (logits.dtype,))
+        q_ptr, q_strides = q_logits.data_ptr(), q_logits.stride()
+        if T > 1 and (lse is None or q_lse is None):
+            raise ValueError("q_logits go with lse and q_lse")
+    i32, f32, row, k, strides = torch.int32, torch.float32, (B,), (B, T - 1), logits.stride()
+    p = switchsd_resample_params(
+        B, T, V, dtype, logits.data_ptr(), strides[0], strides[1], _dev(lse, f32, "lse", (B, T)),
+        _dev(temperature, f32, "temperature", row), _dev(draft, i32, "draft", k), _dev(draft_len, i32, "draft_len", row),
+        _dev(p_draft, f32, "p_draft", k), _dev(q_draft, f32, "q_draft", k), _dev(u, f32, "u", k), q_ptr, q_strides[0],
+        q_strides[1], _dev(q_lse, f32, "q_lse", k), _dev(mode, i32, "mode", row), _dev(seeds, torch.int64, "seeds", row),
+        _dev(ctx_lens, i32, "ctx_lens", row), _dev(out, i32, "out", (B, T)), _dev(status, i32, "status", row),
+        _stream_ptr(stream))
+    _check(load().switchsd_resample(ctypes.byref(p)), "switchsd_resample")

@@ -1,0 +1,343 @@
+// logprobs.cu -- switchsd_logprobs: log probabilities of given tokens, entropies and top alternatives.
+//
+// One pass.  A CTA (or a cluster of up to 8 where there are few positions) reads a position's logits once.  A thread keeps,
+// relative to its running maximum m and with z = (l - m) / temperature, S = sum e^z and W = sum e^z z; a larger m scales both
+// (W also loses what z gained).  The threads' meet in a tree; then lse = m / temperature + ln S, and the entropy is
+// ln S - W / S.
+//
+// Top alternatives.  Of the first batch of loads every half warp's largest logit is known, and the k-th largest of those 32
+// is a bound that k of the CTA's logits reach: what lies below is no alternative.  The few that do not go, one by one, into
+// their warp's list, sorted over its lanes, whose k-th raises the warp's own bound.  The lists (of all CTAs) are ranked by
+// counting at the end.  A batch is looked at again only where its largest logit, which the sums want anyway, reaches the
+// bound.
+#include "sampling.cuh"
+
+#include <algorithm>
+
+namespace switchsd {
+
+constexpr int kProbThreads = 512;
+constexpr int kProbWarps = kProbThreads / kWarp;
+constexpr int kProbFlight = 8;          // vectors of a thread in flight
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kGone = -200.f;         // binary logarithm of a weight that binary32 does not have
+
+struct ProbArgs {
+    const void *logits;
+    int64_t sb, st;
+    const int32_t *new_lens, *tokens;
+    const float *temperature;
+    float *logprob, *prob, *entropy, *lse;
+    int32_t *top_ids;
+    float *top_logprobs;
+    int32_t *status;
+    int32_t T, V, K, top, new_add, tokens_stride;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// max, sum of weights, sum of weights times their binary logarithms
+struct Sums {
+    float m, s, w;
+    __device__ void scale_to(float top, float c2) {  // top >= m
+        const float d = fmaxf((m - top) * c2, kGone), f = exp2_fast(d);  // (the clamp also takes -inf - -inf)
+        w = f * fmaf(s, d, w);
+        s *= f;
+        m = top;
+    }
+    __device__ void add(Sums o, float c2) {
+        const float top = fmaxf(m, o.m);
+        scale_to(top, c2);
+        o.scale_to(top, c2);
+        s += o.s;
+        w += o.w;
+    }
+};
+
+__device__ __forceinline__ bool before(float v, int32_t i, float w, int32_t j) { return v > w || (v == w && i < j); }
+
+// The first k of n (value, token) pairs in `v`, `id`, in order, to `out_v`, `out_id` (the same for all threads of the CTA).
+__device__ __forceinline__ void rank_pairs(const float *v, const int32_t *id, int n, int k, float *out_v, int32_t *out_id) {
+    for (int i = threadIdx.x; i < n; i += kProbThreads) {
+        const float x = v[i];
+        const int32_t t = id[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += before(v[j], id[j], x, t);
+        if (rank < k) {
+            out_v[rank] = x;
+            out_id[rank] = t;
+        }
+    }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArgs a, int parts) {
+    using Row = LogitRow<DT>;
+    constexpr int P = Row::P, F = kProbFlight;
+    __shared__ float s_group[2 * kProbWarps];
+    __shared__ Sums s_sums[kProbWarps], s_all;
+    __shared__ float s_value[kProbWarps * 32], s_top[32];
+    __shared__ int32_t s_id[kProbWarps * 32], s_top_id[32];
+    __shared__ int s_n, s_n_top;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int t = int(blockIdx.x) / parts, part = int(blockIdx.x) - t * parts, b = blockIdx.y;
+    pdl_wait();
+    pdl_trigger();
+    const int64_t nw64 = a.new_lens ? int64_t(__ldcg(a.new_lens + b)) + a.new_add : a.T;
+    const bool ok = nw64 >= 0 && nw64 <= a.T;
+    if (a.status && t == 0 && part == 0 && tid == 0) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
+    const int64_t at = int64_t(b) * a.T + t;
+    if (!ok || t >= nw64) {
+        if (part == 0) {
+            if (tid == 0) {
+                if (a.entropy) a.entropy[at] = 0.f;
+                if (a.lse) a.lse[at] = -INFINITY;
+                if (t < a.K) {
+                    if (a.logprob) a.logprob[int64_t(b) * a.K + t] = -INFINITY;
+                    if (a.prob) a.prob[int64_t(b) * a.K + t] = 0.f;
+                }
+            }
+            if (tid < a.top) {
+                if (a.top_ids) a.top_ids[at * a.top + tid] = -1;
+                if (a.top_logprobs) a.top_logprobs[at * a.top + tid] = -INFINITY;
+            }
+        }
+        return;
+    }
+    const float temperature = a.temperature ? __ldcg(a.temperature + b) : 1.f;
+    const bool greedy = temperature == 0.f;
+    const float c2 = greedy ? 1.f : fminf(kLog2e / temperature, 3e38f);
+    const int k = a.top > 0 ? a.top : greedy ? 1 : 0;  // alternatives to find
+    const Row row(a.logits, b * a.sb + t * a.st, a.V);
+    const int32_t per = (row.vectors + parts - 1) / parts, begin = part * per, end = min(begin + per, row.vectors);
+    if (tid == 0) s_n = s_n_top = 0;
+
+    Sums sums{-INFINITY, 0.f, 0.f};
+    float bound = -INFINITY;                   // of the CTA: k logits reach it
+    float list_v = -INFINITY, list_last = -INFINITY;  // this lane's place of the warp's list, its k-th value
+    int32_t list_id = 0x7fffffff;
+    bool first = true;
+    for (int32_t base = begin; base < end; base += kProbThreads * F) {
+        uint4 x[F];
+#pragma unroll
+        for (int i = 0; i < F; ++i) x[i] = row.load(base + tid + i * kProbThreads, end);
+        const float top = Row::largest(x);
+        if (first && k > 0) {
+            float g = fmaxf(top, -INFINITY);
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(kFull, g, o));
+            if ((lane & 15) == 0) s_group[2 * warp + (lane >> 4)] = g;
+            __syncthreads();
+            g = s_group[lane];
+            int rank = 0;
+            for (int i = 0; i < 32; ++i) {
+                const float o = __shfl_sync(kFull, g, i);
+                rank += o > g || (o == g && i < lane);
+            }
+            bound = __shfl_sync(kFull, g, __ffs(int(__ballot_sync(kFull, rank == k - 1))) - 1);
+        }
+        first = false;
+        if (top > sums.m) sums.scale_to(top, c2);
+        float s2 = 0.f, w2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            float v[P];
+            Row::widen(x[i], v);
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const float y = fmaxf((v[e] - sums.m) * c2, kGone), p = exp2_fast(y);  // (NaN: no weight)
+                s2 += p;
+                w2 = fmaf(p, y, w2);
+            }
+        }
+        sums.s += s2;
+        sums.w += w2;
+        if (k > 0 && __any_sync(kFull, top >= bound && top > list_last)) {
+            uint64_t mask = 0;
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                float v[P];
+                Row::widen(x[i], v);
+#pragma unroll
+                for (int e = 0; e < P; ++e) mask |= uint64_t(v[e] >= bound && v[e] > list_last) << (i * P + e);
+            }
+            while (__any_sync(kFull, mask != 0)) {
+                float v = -INFINITY;
+                int32_t id = 0x7fffffff;
+                if (mask) {
+                    const int e = __ffsll(static_cast<long long>(mask)) - 1;
+                    mask &= mask - 1;
+                    id = row.token(base + tid + (e / P) * kProbThreads) + e % P;
+                    v = row[id];
+                }
+                uint32_t todo = __ballot_sync(kFull, v > list_last || (v == list_last && v > -INFINITY));
+                while (todo) {
+                    const int src = __ffs(int(todo)) - 1;
+                    todo &= todo - 1;
+                    const float nv = __shfl_sync(kFull, v, src);
+                    const int32_t ni = __shfl_sync(kFull, id, src);
+                    const int place = __popc(__ballot_sync(kFull, before(list_v, list_id, nv, ni)));
+                    const float uv = __shfl_up_sync(kFull, list_v, 1);
+                    const int32_t ui = __shfl_up_sync(kFull, list_id, 1);
+                    if (lane == place) {
+                        list_v = nv;
+                        list_id = ni;
+                    } else if (lane > place) {
+                        list_v = uv;
+                        list_id = ui;
+                    }
+                    list_last = __shfl_sync(kFull, list_v, k - 1);
+                }
+            }
+        }
+    }
+
+    // --- the CTA's ------------------------------------------------------------------------------------------------
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        sums.add(Sums{__shfl_xor_sync(kFull, sums.m, o), __shfl_xor_sync(kFull, sums.s, o), __shfl_xor_sync(kFull, sums.w, o)}, c2);
+    if (lane == 0) s_sums[warp] = sums;
+    __syncthreads();
+    if (k > 0) {
+        const bool has = lane < k && list_v >= bound && list_v > -INFINITY;
+        const uint32_t those = __ballot_sync(kFull, has);
+        int from = 0;
+        if (lane == 0 && those) from = atomicAdd(&s_n, __popc(those));
+        from = __shfl_sync(kFull, from, 0) + __popc(those & ((1u << lane) - 1));
+        if (has) {
+            s_value[from] = list_v;
+            s_id[from] = list_id;
+        }
+        __syncthreads();
+        rank_pairs(s_value, s_id, s_n, k, s_top, s_top_id);
+    }
+    if (warp == 0) {
+        sums = lane < kProbWarps ? s_sums[lane] : Sums{-INFINITY, 0.f, 0.f};
+#pragma unroll
+        for (int o = kProbWarps / 2; o > 0; o >>= 1)
+            sums.add(Sums{__shfl_xor_sync(kFull, sums.m, o), __shfl_xor_sync(kFull, sums.s, o), __shfl_xor_sync(kFull, sums.w, o)}, c2);
+        if (lane == 0) {
+            s_all = sums;
+            s_n_top = min(s_n, k);
+        }
+    }
+    __syncthreads();
+
+    // --- the cluster's --------------------------------------------------------------------------------------------
+    if (parts > 1) {
+        cluster_arrive_release();
+        cluster_wait_acquire();
+        if (part == 0) {
+            if (warp == 0) {
+                sums = Sums{-INFINITY, 0.f, 0.f};
+                if (lane < parts) sums = Sums{remote_float(&s_all.m, lane), remote_float(&s_all.s, lane), remote_float(&s_all.w, lane)};
+#pragma unroll
+                for (int o = 4; o > 0; o >>= 1)
+                    sums.add(Sums{__shfl_xor_sync(kFull, sums.m, o), __shfl_xor_sync(kFull, sums.s, o), __shfl_xor_sync(kFull, sums.w, o)}, c2);
+            }
+            if (k > 0) {  // part tid / 32's list, place tid % 32
+                __syncthreads();
+                if (tid == 0) s_n = 0;
+                __syncthreads();
+                if (warp < parts && lane < int(remote_word(&s_n_top, warp))) {
+                    const int i = atomicAdd(&s_n, 1);
+                    s_value[i] = remote_float(&s_top[lane], warp);
+                    s_id[i] = int32_t(remote_word(&s_top_id[lane], warp));
+                }
+                __syncthreads();
+                rank_pairs(s_value, s_id, s_n, k, s_top, s_top_id);  // (all have read this CTA's list)
+            }
+            __syncthreads();
+            if (tid == 0) {
+                s_all = sums;
+                s_n_top = min(s_n, k);
+            }
+            __syncthreads();
+        }
+        cluster_arrive_release();  // the others' shared memory is read until here
+        cluster_wait_acquire();
+        if (part != 0) return;
+    }
+    const float m = s_all.m, log_s = logf(s_all.s);
+    const bool bad = !(temperature >= 0.f && temperature < INFINITY) || (m == INFINITY && !greedy), none = m == -INFINITY;
+    const float nan = __int_as_float(0x7fc00000);
+    auto logprob_of = [&](float l, int32_t id) {
+        if (!(l > -INFINITY)) return -INFINITY;
+        if (bad) return nan;
+        if (greedy) return id == s_top_id[0] ? 0.f : -INFINITY;
+        return (l - m) / temperature - log_s;
+    };
+    if (tid == 0) {
+        const bool bad_t = !(temperature >= 0.f && temperature < INFINITY);
+        if (a.lse) a.lse[at] = bad_t ? nan : none || greedy || m == INFINITY ? m : m / temperature + log_s;
+        if (a.entropy) a.entropy[at] = none || greedy ? 0.f : bad ? nan : fmaxf(0.f, log_s - s_all.w / s_all.s * kLn2);
+        if (t < a.K) {
+            const int32_t token = __ldcg(a.tokens + int64_t(b) * a.tokens_stride + t);
+            const float lp = uint32_t(token) < uint32_t(a.V) ? logprob_of(row[token], token) : -INFINITY;
+            if (a.logprob) a.logprob[int64_t(b) * a.K + t] = lp;
+            if (a.prob) a.prob[int64_t(b) * a.K + t] = expf(lp);
+        }
+    }
+    if (tid < a.top) {
+        const bool there = tid < s_n_top;
+        if (a.top_ids) a.top_ids[at * a.top + tid] = there ? s_top_id[tid] : -1;
+        if (a.top_logprobs) a.top_logprobs[at * a.top + tid] = there ? logprob_of(s_top[tid], s_top_id[tid]) : -INFINITY;
+    }
+}
+
+template <int DT>
+static cudaError_t launch_logprobs(const ProbArgs &a, int32_t B, cudaStream_t s) {
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    const int parts = parts_of(int64_t(B) * a.T, (int64_t(a.V) + LogitRow<DT>::P - 1) / LogitRow<DT>::P, kProbThreads, 2 * sms);
+    return launch_pdl(logprobs_kernel<DT>, dim3(unsigned(parts) * unsigned(a.T), unsigned(B)), dim3(kProbThreads), 0, s, parts > 1 ? unsigned(parts) : 0u, a, parts);
+}
+
+}  // namespace switchsd
+
+using namespace switchsd;
+
+extern "C" int switchsd_logprobs(const switchsd_logprobs_params *p) {
+    if (!p || !p->logits) return SWITCHSD_ERR_ARG;
+    if (p->dtype != SWITCHSD_BF16 && p->dtype != SWITCHSD_F16 && p->dtype != SWITCHSD_F32) return SWITCHSD_ERR_ARG;
+    if (reinterpret_cast<uintptr_t>(p->logits) % (p->dtype == SWITCHSD_F32 ? 4 : 2)) return SWITCHSD_ERR_ARG;
+    const bool of_tokens = p->logprob || p->prob, of_top = p->top_ids || p->top_logprobs;
+    if (!of_tokens && !of_top && !p->entropy && !p->lse) return SWITCHSD_ERR_ARG;
+    if (of_tokens && (p->K < 1 || !p->tokens)) return SWITCHSD_ERR_ARG;
+    if (of_top && p->top < 1) return SWITCHSD_ERR_ARG;
+    if ((p->stride_b < 0 && p->B > 1) || (p->stride_t < 0 && p->T > 1)) return SWITCHSD_ERR_ARG;
+    if (p->B < 1 || p->B > 65535 || p->T < 1 || p->T > 262140 || p->V < 1 || p->V > SWITCHSD_VMAX || p->K < 0 || p->K > p->T || p->top < 0 ||
+        p->top > SWITCHSD_TOP_MAX || (of_tokens && p->tokens_stride < p->K))
+        return SWITCHSD_ERR_SHAPE;
+    ProbArgs a;
+    a.logits = p->logits;
+    a.sb = stride_of(p->stride_b, p->B);
+    a.st = stride_of(p->stride_t, p->T);
+    a.new_lens = p->new_lens;
+    a.tokens = p->tokens;
+    a.temperature = p->temperature;
+    a.logprob = p->logprob;
+    a.prob = p->prob;
+    a.entropy = p->entropy;
+    a.lse = p->lse;
+    a.top_ids = p->top_ids;
+    a.top_logprobs = p->top_logprobs;
+    a.status = p->status;
+    a.T = p->T;
+    a.V = p->V;
+    a.K = of_tokens ? p->K : 0;
+    a.top = of_top ? p->top : 0;
+    a.new_add = p->new_add;
+    a.tokens_stride = p->tokens_stride;
+    cudaStream_t s = static_cast<cudaStream_t>(p->stream);
+    const cudaError_t e = p->dtype == SWITCHSD_F32   ? launch_logprobs<SWITCHSD_F32>(a, p->B, s)
+                          : p->dtype == SWITCHSD_F16 ? launch_logprobs<SWITCHSD_F16>(a, p->B, s)
+                                                     : launch_logprobs<SWITCHSD_BF16>(a, p->B, s);
+    return e == cudaSuccess ? SWITCHSD_OK : SWITCHSD_ERR_CUDA;
+}

@@ -1,56 +1,739 @@
-// attention16.cu -- switchsd_kv16_attention: attention of a step's new tokens over the 16-bit paged cache.
+// attention16.cu -- switchsd_kv16_attention: attention of a step's new tokens over the 16-bit paged cache, on tcgen05.
 //
-// The plain form: a warp a (token, query head), lane i holding D / 32 dimensions, one pass over the keys with the running
-// maximum and sum.
+// Work.  The query rows of a row and key head -- its new tokens times the query heads that share the key head -- are cut
+// into tiles of whole tokens, up to 256 rows; an item is one such tile over the keys that its last token sees, and its unit
+// of work is 128 keys.  The units of all items, in order of rows, key heads and tiles, are dealt out evenly over a CTA an
+// SM (the lengths are on the device; every CTA adds them up itself): a CTA takes a contiguous range, which may begin and
+// end inside an item.  An item that one CTA holds whole is written out at once; the others leave partial results that a
+// second kernel joins in order.
+//
+// A CTA has two slots, each with four warps for 128 query rows (a thread a row), its scores S = Q K^T and its output
+// O = P V in tensor memory.  A tile of more than 128 rows has half of them in each slot, and both slots take every unit; a
+// smaller one is in both slots, which take units in turn and join at the end.  While one slot's warps turn scores into
+// weights, the tensor cores work for the other.  Further warps: one fetches tiles of keys and values through a ring (TMA,
+// 128-byte swizzle, a box a page), one issues the products, two look after the values' tiles.
+//
+// Numbers.  The operands are the cache's and the queries' own numbers, products exact, S and O in binary32.  P takes S's
+// place in tensor memory, in the cache's type, since both operands of a product have one: weights are relative to a
+// reference that may lag the largest score (kLagUp), so that O is scaled seldom, f16 weights 2^11 higher so that few are
+// below its normal numbers.  Their sum is of the unrounded weights, in binary32.
+//
+// What a token does not see: scores are replaced before their maximum is taken.  Of the values, what no row of the tile sees
+// (past its last token, without a page) is cleared in shared memory; among the values that some rows see and others do
+// not, numbers that are not finite would reach the others as 0 * inf: they are cleared too, and added to the rows that see
+// them at the end.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <cstdlib>
+
 #include "attention.cuh"
+#include "tc.cuh"
 
 namespace switchsd {
 
-constexpr int kPlainThreads = 128;
+constexpr int kSlotRows = 128;              // query rows of a slot: the MMA's M
+constexpr int kTileRows = 2 * kSlotRows;
+constexpr int kUnitKeys = 128;
+constexpr int kSlotThreads = kSlotRows, kSlotWarps = kSlotThreads / kWarp;
+constexpr int kValueWarps = 2;
+constexpr int kMmaWarp16 = 2 * kSlotWarps, kFetchWarp16 = kMmaWarp16 + 1, kFirstValueWarp = kFetchWarp16 + 1;
+constexpr int kThreads16 = (2 * kSlotWarps + 4) * kWarp;
+// Registers a thread of the two slots' warpgroups and of the third: 384 threads are launched with 168 each, and the shares
+// add up to the same.
+constexpr int kSlotRegs = 208, kOtherRegs16 = 88;
+static_assert(2 * kSlotRegs + kOtherRegs16 == 3 * 168, "what two warpgroups gain the third gives");
+constexpr int kMaxCtas16 = 160;
+constexpr int kReady = 8;                   // units whose values are on their way, at most (a ring's tiles are fewer)
+constexpr int kBlock16 = 128 * 128;         // 128 rows of one swizzle row: an operand's 64 elements
+constexpr int kColumns16 = 512;             // tensor memory: S 2 x 128, O 2 x 128
+// log2 of the weight of a score at the reference, and of one that is as large as can be without a new reference.
+template <bool F16>
+constexpr float kUp = F16 ? 11.f : 0.f;
+template <bool F16>
+constexpr float kLagUp = F16 ? 15.f : 8.f;
+
+struct Attn16Args : AttnArgs {
+    int32_t tokens;  // of a tile: kTileRows / group
+};
+
+template <int D>
+struct Smem16 {
+    static constexpr int kQ = (D / 64) * kBlock16;      // a slot's queries: [D / 64][128 rows][128 bytes]
+    static constexpr int kTile = (D / 64) * kBlock16;   // 128 keys or values: [D / 64][128 tokens][128 bytes]
+    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr int bytes = 1024 + 2 * kQ + kStages * kTile;
+};
+
+// K-major operands (sw128_desc), and V: [D / 64][token][64], the contracted axis outermost; groups of eight tokens are 1024
+// bytes apart, the other 64 dimensions kBlock16.
+__device__ __forceinline__ uint64_t value_desc(uint32_t saddr) {
+    return uint64_t((saddr & 0x3FFFFu) >> 4) | (uint64_t(kBlock16 >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+// Instruction descriptor: binary32 sums, M = 128; `values`: B with the contracted axis outermost.
+template <bool F16>
+__device__ constexpr uint32_t idesc16(int N, bool values) {
+    return f16_idesc(N) | (F16 ? 0u : (1u << 7) | (1u << 10)) | (values ? 1u << 16 : 0u);
+}
+
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, int32_t w, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n" ::"r"(smem_addr(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_addr(bar))
+        : "memory");
+}
+
+// sum over i < n of floor((c + a i) / 128): the sum of the numbers less that of their remainders, which repeat.
+__device__ __forceinline__ int64_t sum_of_units(int64_t c, int32_t a, int64_t n) {
+    const int32_t g = min(128, a & -a), period = 128 / g, some = int32_t(n % period);
+    int64_t rest = n / period * (int64_t(period) * (c % g) + int64_t(g) * period * (period - 1) / 2);
+    int32_t r = int32_t(c & 127);
+    for (int32_t i = 0; i < some; ++i, r = (r + a) & 127) rest += r;
+    return (n * c + a * (n * (n - 1) / 2) - rest) >> 7;
+}
+
+// A run of units of one item.
+struct Run {
+    int b, hk, rt;
+    int32_t len, token0, tokens, keys;  // of the tile: its first token, tokens, and keys that its last one sees
+    int32_t first, n, units, part;      // part: which of the CTA's two partial results it may leave
+};
+// The runs of a CTA's range, in order, but that one which begins inside an item comes last: the CTAs that share an item's
+// keys then go through them side by side, and what one has fetched the others find in L2.
+struct Runs {
+    int b, hk, rt;
+    int32_t skip;        // of the first item: units before the range
+    int64_t left;        // units
+    int32_t len, nw;     // of row b
+    bool begun, held;
+    Run late;
+    __device__ bool take(const Attn16Args &a, Run &s) {
+        while (left > 0) {
+            const int tiles = (nw + a.tokens - 1) / a.tokens;
+            if (rt >= tiles) {
+                rt = 0;
+                if (nw == 0 || ++hk == a.Hkv) {
+                    hk = 0;
+                    ++b;
+                    row_lengths(a, b, len, nw);
+                }
+                continue;
+            }
+            s.b = b;
+            s.hk = hk;
+            s.rt = rt++;
+            s.len = len;
+            s.token0 = s.rt * a.tokens;
+            s.tokens = min(a.tokens, nw - s.token0);
+            s.keys = len + s.token0 + s.tokens;
+            s.units = (s.keys + kUnitKeys - 1) / kUnitKeys;
+            s.first = skip;
+            s.n = int32_t(min(int64_t(s.units - skip), left));
+            s.part = 1;
+            skip = 0;
+            left -= s.n;
+            return true;
+        }
+        return false;
+    }
+    __device__ bool next(const Attn16Args &a, Run &s) {
+        if (!begun) {
+            begun = true;
+            if (left == 0) return false;
+            row_lengths(a, b, len, nw);
+            if (!take(a, s)) return false;
+            s.part = 0;
+            if (s.first == 0 || left == 0) return true;
+            late = s;
+            held = true;
+        }
+        if (take(a, s)) return true;
+        if (!held) return false;
+        held = false;
+        s = late;
+        return true;
+    }
+};
+
+// The CTA's range.  Also: statuses (CTA 0), zeros for the query rows of tokens that are not there, and the CTA's partial
+// results marked as none.  All threads call it.  s_pre: kThreads16 + 2 numbers.
+__device__ __forceinline__ void deal_runs(const Attn16Args &a, int64_t *s_pre, Runs &runs) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, ctas = int(gridDim.x);
+    constexpr int kWarps = kThreads16 / kWarp;
+    const int per = (a.B + kThreads16 - 1) / kThreads16;  // rows of a thread
+    auto before_tile = [&](int32_t len, int32_t nw, int rt) -> int64_t {  // units of a key head's tiles before rt
+        const int whole = nw / a.tokens;
+        const int64_t c = int64_t(len) + a.tokens + kUnitKeys - 1;
+        return sum_of_units(c, a.tokens, min(rt, whole)) + (rt > whole ? (int64_t(len) + nw + kUnitKeys - 1) / kUnitKeys : 0);
+    };
+    auto units_of = [&](int row) -> int64_t {  // of a key head
+        int32_t len, nw;
+        const bool ok = row_lengths(a, row, len, nw);
+        if (a.status && cta == 0) a.status[row] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
+        return nw ? before_tile(len, nw, (nw + a.tokens - 1) / a.tokens) : 0;
+    };
+    int64_t mine = 0;
+    for (int i = 0; i < per; ++i)
+        if (tid * per + i < a.B) mine += units_of(tid * per + i) * a.Hkv;
+    int64_t x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(kFull, x, o);
+        if (lane >= o) x += y;
+    }
+    s_pre[tid + 1] = x;
+    __syncthreads();
+    int64_t add = 0;
+    for (int w = 0; w < warp; ++w) add += s_pre[32 * w + 32];
+    __syncthreads();
+    s_pre[tid + 1] = x + add;
+    if (tid == 0) s_pre[0] = 0;
+    __syncthreads();
+    const int64_t total = s_pre[kThreads16];
+    const int64_t takers = min(total, int64_t(ctas));  // CTAs with a range: at least one unit each
+    const int64_t u = cta < takers ? total * cta / takers : total, u_end = cta < takers ? total * (cta + 1) / takers : total;
+    const int row16 = a.Hq * a.dim / 8;  // 16-byte pieces of a token's output
+    for (int64_t i = int64_t(warp) * ctas + cta; i < int64_t(a.B) * a.T; i += int64_t(ctas) * kWarps) {
+        int32_t len, nw;
+        row_lengths(a, int(i / a.T), len, nw);
+        if (int(i % a.T) < nw) continue;
+        uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(i) * row16;
+        for (int e = lane; e < row16; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
+    }
+    if (tid < 2) a.desc[2 * cta + tid] = make_int4(-1, 0, 0, 0);
+    const bool here = u < u_end && u >= s_pre[tid] && u < s_pre[tid + 1];
+    const int64_t at0 = s_pre[tid];
+    __syncthreads();
+    if (here) {
+        int64_t at = at0, n;
+        int row = tid * per;
+        for (;; ++row) {
+            n = units_of(row);
+            if (u < at + n * a.Hkv) break;
+            at += n * a.Hkv;
+        }
+        int32_t len, nw;
+        row_lengths(a, row, len, nw);
+        const int64_t off = (u - at) % n;
+        int lo = 0, hi = (nw + a.tokens - 1) / a.tokens;  // the last tile with no more than `off` units before it
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            (before_tile(len, nw, mid) <= off ? lo : hi) = mid;
+        }
+        s_pre[0] = row;
+        s_pre[1] = (u - at) / n;
+        s_pre[2] = lo;
+        s_pre[3] = off - before_tile(len, nw, lo);
+    }
+    __syncthreads();
+    runs.b = int(s_pre[0]);
+    runs.hk = int(s_pre[1]);
+    runs.rt = int(s_pre[2]);
+    runs.skip = int32_t(s_pre[3]);
+    runs.left = u < u_end ? u_end - u : 0;
+    runs.begun = runs.held = false;
+}
+
+__device__ __forceinline__ void both_slots() { asm volatile("bar.sync 1, %0;\n" ::"n"(2 * kSlotThreads) : "memory"); }
 
 template <bool F16, int D>
-__global__ void __launch_bounds__(kPlainThreads) attn16_plain_kernel(const AttnArgs a) {
-    constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_constant__ CUtensorMap map, const Attn16Args a) {
+    using S = Smem16<D>;
+    constexpr int N = S::kStages, G = D / 64;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t full[N], empty[N], ready[kReady], s_full[2], p_full[2], o_done[2], q_full, stopped;
+    __shared__ __align__(16) uint32_t s_exist[kReady][4];  // of a unit: its keys that exist and whose page does
+    __shared__ uint32_t s_tmem, s_cleared[kReady];         // s_cleared: a run (+ 1) with values that were not finite, by the run
+    __shared__ int s_bad;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+    uint8_t *base = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    uint8_t *sm_q = base, *sm_kv = base + 2 * S::kQ;
+    float2 *s_ml = reinterpret_cast<float2 *>(sm_q + S::kQ);  // [2][128], of a tile that is in both slots: reference, sum
+
+    if (tid == 0) {
+        for (int i = 0; i < N; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < kReady; ++i) mbar_init(&ready[i], kValueWarps);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s_full[i], 2);  // the products, and the MMA thread: what it has seen of the other warps
+            mbar_init(&o_done[i], 2);
+            mbar_init(&p_full[i], kSlotWarps);
+        }
+        mbar_init(&q_full, 2 * kSlotWarps);
+        mbar_init(&stopped, 1);
+        fence_mbar_init();
+        s_bad = 0;
+        for (int i = 0; i < kReady; ++i) s_cleared[i] = 0;
+    }
+    if (warp == kMmaWarp16) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_addr(&s_tmem)), "r"(kColumns16) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
     pdl_wait();
     pdl_trigger();
-    const int64_t warps = int64_t(gridDim.x) * (kPlainThreads / kWarp), first = (int64_t(blockIdx.x) * kPlainThreads + threadIdx.x) / kWarp;
-    if (a.status && blockIdx.x == 0)
-        for (int b = threadIdx.x; b < a.B; b += kPlainThreads) {
-            int32_t len, nw;
-            a.status[b] = row_lengths(a, b, len, nw) ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
-        }
-    for (int64_t i = first; i < int64_t(a.B) * a.T * a.Hq; i += warps) {
-        const int h = int(i % a.Hq), t = int(i / a.Hq % a.T), b = int(i / a.Hq / a.T), hk = h / a.group;
-        int32_t len, nw;
-        row_lengths(a, b, len, nw);
-        float m = -INFINITY, l = 0.f, o[E], q[E];
-        for (int e = 0; e < E; ++e) {
-            o[e] = 0.f;
-            q[e] = t < nw ? widen1<F16>(a.q[b * a.qs[0] + t * a.qs[1] + h * a.qs[2] + lane * E + e]) : 0.f;
-        }
-        const int32_t end = t < nw ? len + t + 1 : 0, mask = (1 << a.page_shift) - 1;
-        for (int32_t j = 0; j < end; ++j) {
-            const int32_t page = __ldcg(a.table + size_t(b) * a.blocks + (j >> a.page_shift));
-            if (uint32_t(page) >= uint32_t(a.pages)) continue;
-            const uint16_t *k = reinterpret_cast<const uint16_t *>(a.cache) + (((size_t(page) * 2 * a.Hkv + hk) << a.page_shift) + (j & mask)) * D + lane * E;
-            const uint16_t *v = k + (size_t(a.Hkv) << a.page_shift) * D;
-            float s = 0.f;
-            for (int e = 0; e < E; ++e) s = fmaf(q[e], widen1<F16>(k[e]), s);
-            s = warp_sum_f32(s) * a.scale;
-            if (!(s <= m)) {
-                const float f = expf(m - s);
-                m = s;
-                l *= f;
-                for (int e = 0; e < E; ++e) o[e] *= f;
+    Runs runs;
+    deal_runs(a, reinterpret_cast<int64_t *>(sm_kv), runs);
+    fence_proxy_async();  // (the ring's memory was just used)
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    // Every wait of this thread has ended in time.  After one that has not, no further wait is begun and no result counts;
+    // the slots' warps still go through their loops, because their barriers want all of them.
+    bool ok = !a.give_up || warp == kFetchWarp16;
+    Run s;
+
+    if (warp < 2 * kSlotWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kSlotRegs));
+        // ------------------------------------------------------------------------------------------- query rows
+        const int slot = warp / kSlotWarps, quarter = warp % kSlotWarps, place = tid % kSlotThreads;
+        const uint32_t lanes = tmem + (uint32_t(32 * quarter) << 16), scores = lanes + uint32_t(slot * 128);
+        const bool flip = a.scale < 0.f;
+        // of a sum of products, for the binary logarithm; positive, so that what is masked stays -inf
+        const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
+        uint32_t i = 0, done = 0, nrun = 0, unit0 = 0;  // this slot's units and runs so far, the CTA's runs and units
+        for (; runs.next(a, s); ++nrun, unit0 += uint32_t(s.n)) {
+            const int rows = s.tokens * a.group;
+            const bool split = rows <= kSlotRows;  // the tile is in both slots, which take units in turn
+            const int row = split ? place : slot * kSlotRows + place, t = row / a.group, h = s.hk * a.group + row - t * a.group;
+            const bool mine = row < rows, warp_mine = row - lane < rows;
+            const int32_t limit = mine ? s.len + s.token0 + t : -1;
+            {
+                const uint16_t *q = a.q + s.b * a.qs[0] + int64_t(s.token0 + t) * a.qs[1] + int64_t(h) * a.qs[2];
+                uint8_t *dst = sm_q + (split ? 0 : slot * S::kQ) + place * 128;
+                const int c0 = split ? slot * (D / 16) : 0, c1 = split ? c0 + D / 16 : D / 8;
+#pragma unroll 8
+                for (int c = c0; c < c1; ++c) {
+                    const uint4 x = mine ? *reinterpret_cast<const uint4 *>(q + 8 * c) : make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(dst + (c / 8) * kBlock16 + (((c & 7) ^ (place & 7)) * 16)) = x;
+                }
+                fence_proxy_async();
+                tc_fence_before();
+                warp_arrive(&q_full);
             }
-            const float p = expf(s - m);
-            l += p;
-            for (int e = 0; e < E; ++e) o[e] = fmaf(p, widen1<F16>(v[e]), o[e]);
+            float ref = kFloor, l = 0.f;
+            const int step = split ? 2 : 1, k0 = split ? slot : 0;
+            const uint32_t out = lanes + 256 + uint32_t(slot * 128);
+            for (int32_t k = k0; k < s.n; k += step, ++i) {
+                const int32_t key0 = (s.first + k) * kUnitKeys;
+                ok = ok && tc_wait_warp(&s_full[slot], i & 1);
+                tc_fence_after();
+                if (warp_mine) {
+                    float v[kUnitKeys];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) tmem_ld32(scores + 32 * w, v + 32 * w);
+                    const uint4 there = *reinterpret_cast<const uint4 *>(s_exist[(unit0 + uint32_t(k)) % kReady]);
+                    tmem_wait_ld();
+                    if (flip)
+#pragma unroll
+                        for (int e = 0; e < kUnitKeys; ++e) v[e] = -v[e];
+                    if (key0 + kUnitKeys > s.len + s.token0 + 1 || (there.x & there.y & there.z & there.w) != 0xffffffffu) {
+                        const uint32_t word[4] = {there.x, there.y, there.z, there.w};
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const int32_t ahead = limit - (key0 + 32 * w);  // the last visible key's place
+                            const uint32_t see = word[w] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[32 * w + e] = (see >> e) & 1 ? v[32 * w + e] : -INFINITY;
+                        }
+                    }
+                    float t4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                    for (int e = 4; e < kUnitKeys; e += 2) t4[(e >> 1) & 3] = max3(t4[(e >> 1) & 3], v[e], v[e + 1]);
+                    const float mx = fmaxf(max3(t4[0], t4[1], t4[2]), t4[3]) * scale;
+                    float corr = 1.f;
+                    if (mx > ref + kLagUp<F16>) {
+                        const float to = __fsub_ru(mx, kUp<F16>);  // (rounded up: f16 has no weights beyond 2^15)
+                        corr = exp2_approx(ref - to);
+                        ref = to;
+                        l *= corr;
+                    }
+                    if (k != k0 && __any_sync(kFull, corr != 1.f)) {  // (the scores' product came behind the last one of O)
+#pragma unroll 1
+                        for (int e = 0; e < D; e += 16) {
+                            uint32_t w[16];
+                            tmem_ld16(out + e, w);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(__uint_as_float(w[j]) * corr);
+                            tmem_st16(out + e, w);
+                        }
+                    }
+                    const uint64_t scale2 = pair_of(scale, scale), ref2 = pair_of(-ref, -ref);
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {  // 32 keys, in 16 columns
+                        uint32_t y[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float2 x = halves_of(fma_pair(pair_of(v[32 * w + 2 * e], v[32 * w + 2 * e + 1]), scale2, ref2));
+                            const float p0 = exp2_approx(x.x), p1 = exp2_approx(x.y);
+                            sum[e & 1] = add_pair(sum[e & 1], pair_of(p0, p1));
+                            y[e] = narrow2<F16>(p0, p1);
+                        }
+                        tmem_st16(scores + 16 * w, y);
+                    }
+                    const float2 both = halves_of(add_pair(sum[0], sum[1]));
+                    l += both.x + both.y;
+                    tmem_wait_st();
+                }
+                tc_fence_before();
+                warp_arrive(&p_full[slot]);
+            }
+            // --- the run's result -------------------------------------------------------------------------------
+            if (k0 < s.n) {
+                ok = ok && tc_wait_warp(&o_done[slot], done & 1);
+                ++done;
+            }
+            tc_fence_after();
+            float f = 1.f, f1 = 0.f;          // of this slot's output (or the first one's), and the second one's
+            const bool two = split && s.n > 1;  // the second slot has an output too
+            if (split) {
+                s_ml[slot * kSlotRows + place] = make_float2(ref, l);
+                tc_fence_before();
+                both_slots();
+                tc_fence_after();
+                const float2 x = s_ml[place], y = s_ml[kSlotRows + place];
+                both_slots();  // (the next queries may take the numbers' place)
+                ref = fmaxf(x.x, y.x);
+                f = exp2_approx(x.x - ref);
+                f1 = exp2_approx(y.x - ref);
+                l = x.y * f + y.y * f1;
+            }
+            const bool whole = s.first == 0 && s.n == s.units;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            if (warp_mine) {
+                const uint32_t from = split ? lanes + 256 : out;
+                const int part = 2 * cta + s.part, d0 = split ? slot * (D / 2) : 0, d1 = split ? d0 + D / 2 : D;
+                float *partial = a.part + (size_t(part) * kTileRows + row) * (D + 4);
+                uint16_t *result = a.out + ((size_t(s.b) * a.T + s.token0 + t) * a.Hq + h) * D;
+                const int32_t cleared = s_cleared[nrun % kReady] == nrun + 1 ? min(limit + 1, (s.first + s.n) * kUnitKeys) : 0;
+#pragma unroll 1
+                for (int d = d0; d < d1; d += 16) {
+                    float v[16];
+                    uint32_t w[16];
+                    tmem_ld16(from + d, w);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(w[j]) * f;
+                    if (two) {
+                        tmem_ld16(from + 128 + d, w);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[j] = fmaf(__uint_as_float(w[j]), f1, v[j]);
+                    }
+                    for (int32_t key = max(s.first * kUnitKeys, s.len + s.token0 + 1); key < cleared; ++key) {  // (seldom)
+                        const int32_t page = __ldcg(a.table + size_t(s.b) * a.blocks + (key >> a.page_shift));
+                        if (uint32_t(page) >= uint32_t(a.pages)) continue;
+                        const size_t line = (((size_t(page) * 2 + 1) * a.Hkv + s.hk) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+                        const uint16_t *src = reinterpret_cast<const uint16_t *>(a.cache) + line * D + d;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const float x = widen1<F16>(__ldcg(src + j));
+                            if (!(fabsf(x) < INFINITY)) v[j] += x;
+                        }
+                    }
+                    if (mine && whole) {
+                        uint4 *dst = reinterpret_cast<uint4 *>(result + d);
+#pragma unroll
+                        for (int j = 0; j < 16; j += 8)
+                            dst[j / 8] = make_uint4(narrow2<F16>(v[j] * inv, v[j + 1] * inv), narrow2<F16>(v[j + 2] * inv, v[j + 3] * inv),
+                                                    narrow2<F16>(v[j + 4] * inv, v[j + 5] * inv), narrow2<F16>(v[j + 6] * inv, v[j + 7] * inv));
+                    } else if (mine) {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4 *>(partial + d + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    }
+                }
+                if (!whole && mine && d0 == 0) {
+                    partial[D] = ref;
+                    partial[D + 1] = l;
+                    if (tid == 0) a.desc[part] = make_int4(s.b, s.hk, s.rt, (s.first == 0 ? kFirst : 0) | (s.first + s.n == s.units ? kLast : 0));
+                }
+            }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        for (int e = 0; e < E; ++e) a.out[i * D + lane * E + e] = narrow1<F16>(o[e] * inv);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kOtherRegs16));
+        if (warp == kFetchWarp16) {
+            // --------------------------------------------------------------------------------------- fetching
+            // Lane G q + g copies the 64 dimensions g of the unit's q-th run of tokens inside a page.
+            const int run = min(kUnitKeys, 1 << a.page_shift), nruns = kUnitKeys / run, page_mask = (1 << a.page_shift) - 1;
+            const int q = lane / G, g = lane - G * q;
+            uint32_t unit = 0, issued = 0;  // units, tiles
+            while (ok && runs.next(a, s)) {
+                auto find = [&](int32_t k) {  // the page of this lane's tokens in unit k of the run
+                    const int32_t key = (s.first + k) * kUnitKeys + q * run;
+                    return q < nruns && k < s.n && key < s.keys ? __ldcg(a.table + size_t(s.b) * a.blocks + (key >> a.page_shift)) : -1;
+                };
+                int32_t page = find(0);
+                for (int32_t k = 0; ok && k < s.n; ++k, ++unit) {
+                    const int32_t key0 = (s.first + k) * kUnitKeys, next = find(k + 1);
+                    const bool good = uint32_t(page) < uint32_t(a.pages);
+                    const uint32_t goods = __ballot_sync(kFull, good);
+                    const uint32_t bytes = uint32_t(__popc(goods)) * uint32_t(run) * 128u;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t x = 2 * unit + half, st = x % N;
+                        if (x >= N) ok = ok && tc_wait_warp(&empty[st], (x / N - 1) & 1);
+                        if (!ok) break;
+                        if (half == 0 && lane < 4) {
+                            uint32_t word = 0;
+                            for (int e = 0; e < 32; e += 16) {  // runs are multiples of 16 tokens
+                                const int at = 32 * lane + e, left = s.keys - (key0 + at);
+                                if ((goods >> (G * (at / run))) & 1) word |= (left >= 16 ? 0xffffu : left > 0 ? (1u << left) - 1u : 0u) << e;
+                            }
+                            s_exist[unit % kReady][lane] = word;
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
+                        __syncwarp();
+                        if (good)
+                            tma_load_4d(sm_kv + st * S::kTile + g * kBlock16 + q * run * 128, &map, 64 * g, (key0 + q * run) & page_mask, half * a.Hkv + s.hk, page, &full[st]);
+                        issued = x + 1;
+                    }
+                    page = next;
+                }
+            }
+            // copies in flight write shared memory: it stays the CTA's until they have come (also where another warp gave up on them)
+            for (uint32_t x = issued > N ? issued - N : 0; x < issued; ++x) (void)tc_wait(&full[x % N], (x / N) & 1);
+        } else if (warp == kMmaWarp16 && lane == 0) {
+            // --------------------------------------------------------------------------------------- the products
+            uint32_t unit0 = 0, nrun = 0, weights[2] = {0, 0};  // units and runs so far, units whose weights a slot's product took
+            const uint64_t dq0 = sw128_desc(smem_addr(sm_q)), dk0 = sw128_desc(smem_addr(sm_kv)), dv0 = value_desc(smem_addr(sm_kv));
+            auto stage_of = [&](uint32_t x) { return uint64_t(x % N) * (S::kTile >> 4); };
+            auto score = [&](int slot, bool split, uint32_t unit) {  // S = Q K^T
+                const uint32_t x = 2 * unit;
+                ok = ok && tc_wait(&full[x % N], (x / N) & 1);
+                if (!ok) return;
+                mbar_arrive(&s_full[slot]);
+                tc_fence_after();
+                const uint64_t dq = dq0 + (split ? 0 : uint64_t(slot) * (S::kQ >> 4)), dk = dk0 + stage_of(x);
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e) {
+                    const uint64_t step = uint64_t(((e >> 2) * kBlock16 + (e & 3) * 32) >> 4);
+                    mma_ss(tmem + slot * 128, dq + step, dk + step, idesc16<F16>(kUnitKeys, false), e != 0);
+                }
+                tc_commit(&s_full[slot]);
+            };
+            auto product = [&](int slot, uint32_t unit, bool fresh) {  // O += P V
+                ok = ok && tc_wait(&p_full[slot], weights[slot] & 1) && tc_wait(&ready[unit % kReady], (unit / kReady) & 1);
+                if (!ok) return;
+                ++weights[slot];
+                tc_fence_after();
+                const uint64_t dv = dv0 + stage_of(2 * unit + 1);
+#pragma unroll
+                for (int e = 0; e < kUnitKeys / 16; ++e)
+                    mma_ts(tmem + 256 + slot * 128, tmem + slot * 128 + 8 * e, dv + uint64_t((e * 16 * 128) >> 4), idesc16<F16>(D, true), !fresh || e != 0);
+            };
+            auto release = [&](uint32_t x) {
+                if (ok) tc_commit(&empty[x % N]);
+            };
+            auto finish = [&](int slot) {
+                if (!ok) return;
+                mbar_arrive(&o_done[slot]);
+                tc_commit(&o_done[slot]);
+            };
+            while (ok && runs.next(a, s)) {
+                const bool split = s.tokens * a.group <= kSlotRows;
+                ok = ok && tc_wait(&q_full, nrun & 1);  // (the rows' threads write the queries when they have read the last O)
+                if (split) {
+                    for (int32_t k = 0; ok && k < s.n + 2; ++k) {
+                        const int slot = k & 1;
+                        if (k >= 2) {
+                            product(slot, unit0 + k - 2, k < 4);
+                            release(2 * (unit0 + k - 2) + 1);
+                            if (k >= s.n) finish(slot);
+                        }
+                        if (k < s.n) {
+                            score(slot, true, unit0 + k);
+                            release(2 * (unit0 + k));
+                        }
+                    }
+                } else {
+                    for (int32_t k = 0; ok && k <= s.n; ++k)
+#pragma unroll
+                        for (int slot = 0; slot < 2; ++slot) {
+                            if (k > 0) {
+                                product(slot, unit0 + k - 1, k == 1);
+                                if (slot == 1) release(2 * (unit0 + k - 1) + 1);
+                                if (k == s.n) finish(slot);
+                            }
+                            if (k < s.n) {
+                                score(slot, false, unit0 + k);
+                                if (slot == 1) release(2 * (unit0 + k));
+                            }
+                        }
+                }
+                unit0 += uint32_t(s.n);
+                ++nrun;
+            }
+            // what is in flight reads shared and tensor memory (the rows' threads wait for the last product too, unless they gave up)
+            tc_commit(&stopped);
+            (void)tc_wait(&stopped, 0);
+        } else if (warp >= kFirstValueWarp) {
+            // --------------------------------------------------------------------------------------- values that not every row sees
+            const int first_place = (warp - kFirstValueWarp) * (kUnitKeys / kValueWarps) + lane;
+            uint32_t unit = 0;
+            for (uint32_t nrun = 0; ok && runs.next(a, s); ++nrun) {
+                const int32_t all_see = s.len + s.token0;  // the last key that all rows see
+                for (int32_t k = 0; ok && k < s.n; ++k, ++unit) {
+                    const uint32_t x = 2 * unit + 1, st = x % N;
+                    ok = tc_wait_warp(&full[st], (x / N) & 1);
+                    if (!ok) break;
+                    const int32_t key0 = (s.first + k) * kUnitKeys;
+                    const uint4 there = *reinterpret_cast<const uint4 *>(s_exist[unit % kReady]);
+                    if (key0 + kUnitKeys > all_see + 1 || (there.x & there.y & there.z & there.w) != 0xffffffffu) {
+                        bool found = false;
+#pragma unroll 1
+                        for (int at = first_place; at < first_place + kUnitKeys / kValueWarps; at += kWarp) {
+                            uint8_t *line = sm_kv + st * S::kTile + at * 128;
+                            const bool gone = !((s_exist[unit % kReady][at / 32] >> (at & 31)) & 1);
+                            if (!gone && key0 + at <= all_see) continue;
+#pragma unroll 1
+                            for (int c = 0; c < D / 8; ++c) {  // (in an order that spreads the lanes over the banks)
+                                uint4 *piece = reinterpret_cast<uint4 *>(line + (c / 8) * kBlock16 + ((c ^ at) & 7) * 16);
+                                uint4 v = make_uint4(0, 0, 0, 0);
+                                if (!gone) {
+                                    v = *piece;
+                                    uint32_t *w[4] = {&v.x, &v.y, &v.z, &v.w};
+                                    constexpr uint32_t kMax = F16 ? 0x7c00u : 0x7f80u;
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        uint32_t keep = 0xffffffffu;
+                                        if ((*w[e] & kMax) == kMax) keep &= 0xffff0000u;
+                                        if ((*w[e] >> 16 & kMax) == kMax) keep &= 0x0000ffffu;
+                                        found |= keep != 0xffffffffu;
+                                        *w[e] &= keep;
+                                    }
+                                }
+                                *piece = v;
+                            }
+                        }
+                        if (found) s_cleared[nrun % kReady] = nrun + 1;
+                        fence_proxy_async();
+                    }
+                    warp_arrive(&ready[unit % kReady]);
+                }
+            }
+        }
     }
+    if (!ok) s_bad = 1;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kMmaWarp16)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kColumns16) : "memory");
+    if (s_bad && tid == 0) a.desc[2 * cta].w |= kLate;  // (the thread that wrote it; the join writes the statuses)
+}
+
+// Joins the partial results of the items that several CTAs hold, and writes the statuses of a launch that a CTA gave up:
+// CTAs (i, .) look after the item whose first part is the i-th CTA's, a CTA a query row and a thread a dimension, adding
+// the parts in order, kJoinParts on their way together.
+template <bool F16, int D>
+__global__ void __launch_bounds__(D, 2048 / D) attn16_join_kernel(const Attn16Args a) {
+    const int i = blockIdx.x, d = threadIdx.x, lane = threadIdx.x & 31, ctas = int(gridDim.x);
+    pdl_wait();
+    pdl_trigger();
+    int from = 2 * i + 1;
+    int4 de = __ldcg(a.desc + from);
+    const int4 other = __ldcg(a.desc + 2 * i);
+    if ((other.w & kLate) && blockIdx.y == 0 && a.status)
+        for (int b = d; b < a.B; b += D) a.status[b] = SWITCHSD_ROW_TIMEOUT;
+    if (de.x < 0 || !(de.w & kFirst)) {
+        from = 2 * i;
+        de = other;
+        if (de.x < 0 || !(de.w & kFirst)) return;
+    }
+    int n = 1;  // partial results of the item: this CTA's and the next ones' first, up to the one that holds the last unit
+    for (int c0 = i + 1; !(de.w & kLast);) {
+        const int c = c0 + lane;
+        const uint32_t last = __ballot_sync(kFull, c >= ctas || (__ldcg(&a.desc[2 * min(c, ctas - 1)].w) & kLast));
+        if (last) {
+            n = min(c0 + __ffs(int(last)), ctas) - i;
+            break;
+        }
+        c0 += 32;
+    }
+    int32_t len, nw;
+    row_lengths(a, de.x, len, nw);
+    const int token0 = de.z * a.tokens, rows = min(a.tokens, nw - token0) * a.group;
+    for (int row = int(blockIdx.y); row < rows; row += int(gridDim.y)) {
+        float mx = kFloor, sum = 0.f, y = 0.f;
+        for (int j0 = 0; j0 < n; j0 += kJoinParts) {
+            float pm[kJoinParts], ps[kJoinParts], py[kJoinParts], top = mx;
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) {
+                pm[j] = kFloor;
+                ps[j] = py[j] = 0.f;
+                if (j0 + j < n) {
+                    const float *src = a.part + (size_t(j0 + j ? 2 * (i + j0 + j) : from) * kTileRows + row) * (D + 4);
+                    pm[j] = __ldcg(src + D);
+                    ps[j] = __ldcg(src + D + 1);
+                    py[j] = __ldcg(src + d);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) top = fmaxf(top, pm[j]);
+            const float f0 = exp2_approx(mx - top);
+            y *= f0;
+            sum *= f0;
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) {
+                const float f = exp2_approx(pm[j] - top);
+                y = fmaf(py[j], f, y);
+                sum = fmaf(ps[j], f, sum);
+            }
+            mx = top;
+        }
+        const int t = token0 + row / a.group, h = de.y * a.group + row % a.group;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        a.out[((size_t(de.x) * a.T + t) * a.Hq + h) * D + d] = narrow1<F16>(y * inv);
+    }
+}
+
+// Whether the environment variable SWITCHSD_DIAG_ATTENTION_GIVE_UP is 1 (read once per process): a diagnostic of the path
+// behind a wait that ran out, as in attention_tc.cu.  The fetching warp alone waits, on the ring that nobody empties.
+static bool give_up16() {
+    static const bool set = [] {
+        const char *v = std::getenv("SWITCHSD_DIAG_ATTENTION_GIVE_UP");
+        return v != nullptr && v[0] == '1' && v[1] == '\0';
+    }();
+    return set;
+}
+
+static size_t workspace16(int D) { return size_t(2 * kMaxCtas16) * (sizeof(int4) + size_t(kTileRows) * (D + 4) * sizeof(float)); }
+
+// The cache as [pages][2 Hkv][page][D], a box of 64 dimensions of the tokens of a unit that lie in one page.
+static bool encode_cache(CUtensorMap *map, const switchsd_kv16_attention_params *p) {
+    PFN_cuTensorMapEncodeTiled_v12000 fn = tensor_map_encoder();
+    if (fn == nullptr) return false;
+    const cuuint64_t D = cuuint64_t(p->D), P = cuuint64_t(p->page), H2 = 2 * cuuint64_t(p->Hkv);
+    const cuuint64_t dims[4] = {D, P, H2, cuuint64_t(p->pages)}, strides[3] = {2 * D, 2 * D * P, 2 * D * P * H2};
+    const cuuint32_t box[4] = {64, cuuint32_t(std::min(kUnitKeys, int(p->page))), 1, 1}, one[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void *>(p->cache), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool F16, int D>
+static cudaError_t launch16(const CUtensorMap &map, const Attn16Args &a, cudaStream_t s) {
+    static bool attr_done[64] = {false};
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+        e = cudaFuncSetAttribute(attn16_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem16<D>::bytes);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_done[dev] = true;
+    }
+    const unsigned ctas = unsigned(std::min(kMaxCtas16, sms));
+    // an explicit one-CTA cluster: the MMA commit addresses shared::cluster
+    e = launch_pdl(attn16_kernel<F16, D>, dim3(ctas), dim3(kThreads16), size_t(Smem16<D>::bytes), s, 1u, map, a);
+    if (e != cudaSuccess) return e;
+    const unsigned y = unsigned(std::min(int64_t(32), std::min(int64_t(a.tokens), int64_t(a.T)) * a.group));
+    return launch_pdl(attn16_join_kernel<F16, D>, dim3(ctas, y), dim3(D), 0, s, 0u, a);
 }
 
 }  // namespace switchsd
@@ -58,7 +741,7 @@ __global__ void __launch_bounds__(kPlainThreads) attn16_plain_kernel(const AttnA
 using namespace switchsd;
 
 extern "C" size_t switchsd_kv16_attention_workspace_bytes(const switchsd_kv16_attention_params *p) {
-    return p && kv4_dim_ok(p->D) ? 16 : 0;
+    return p && kv4_dim_ok(p->D) ? workspace16(p->D) : 0;
 }
 
 extern "C" int switchsd_kv16_attention(const switchsd_kv16_attention_params *p) {
@@ -75,7 +758,7 @@ extern "C" int switchsd_kv16_attention(const switchsd_kv16_attention_params *p) 
         int64_t(p->T) * (p->Hq / p->Hkv) > 0x7fffffff)
         return SWITCHSD_ERR_SHAPE;
     if (p->workspace_bytes < switchsd_kv16_attention_workspace_bytes(p)) return SWITCHSD_ERR_ARG;
-    AttnArgs a = {};
+    Attn16Args a = {};
     a.q = static_cast<const uint16_t *>(p->q);
     for (int i = 0; i < 3; ++i) a.qs[i] = stride_of(p->q_stride[i], sizes[i]);
     a.cache = static_cast<const uint8_t *>(p->cache);
@@ -84,6 +767,8 @@ extern "C" int switchsd_kv16_attention(const switchsd_kv16_attention_params *p) 
     a.new_lens = p->new_lens;
     a.out = static_cast<uint16_t *>(p->out);
     a.status = p->status;
+    a.desc = static_cast<int4 *>(p->workspace);
+    a.part = reinterpret_cast<float *>(a.desc + 2 * kMaxCtas16);
     a.B = p->B;
     a.T = p->T;
     a.Hq = p->Hq;
@@ -96,12 +781,15 @@ extern "C" int switchsd_kv16_attention(const switchsd_kv16_attention_params *p) 
     a.group = p->Hq / p->Hkv;
     a.dim = p->D;
     a.scale = p->scale;
+    a.give_up = give_up16();
+    a.tokens = kTileRows / a.group;
+    CUtensorMap map;
+    if (!encode_cache(&map, p)) return SWITCHSD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);
-    const dim3 grid(unsigned(std::min<int64_t>(int64_t(1) << 20, (int64_t(p->B) * p->T * p->Hq + 3) / 4))), block(kPlainThreads);
     cudaError_t e;
     if (p->dtype == SWITCHSD_F16)
-        e = p->D == 128 ? launch_pdl(attn16_plain_kernel<true, 128>, grid, block, 0, s, 0u, a) : launch_pdl(attn16_plain_kernel<true, 64>, grid, block, 0, s, 0u, a);
+        e = p->D == 128 ? launch16<true, 128>(map, a, s) : launch16<true, 64>(map, a, s);
     else
-        e = p->D == 128 ? launch_pdl(attn16_plain_kernel<false, 128>, grid, block, 0, s, 0u, a) : launch_pdl(attn16_plain_kernel<false, 64>, grid, block, 0, s, 0u, a);
+        e = p->D == 128 ? launch16<false, 128>(map, a, s) : launch16<false, 64>(map, a, s);
     return e == cudaSuccess ? SWITCHSD_OK : SWITCHSD_ERR_CUDA;
 }

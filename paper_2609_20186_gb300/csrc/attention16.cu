@@ -579,8 +579,10 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
             for (uint32_t nrun = 0; ok && runs.next(a, s); ++nrun) {
                 const int32_t all_see = s.len + s.token0;  // the last key that all rows see
                 for (int32_t k = 0; ok && k < s.n; ++k, ++unit) {
+                    // (the keys too: where a stage has keys and values in turn, a phase of either that was not waited for would
+                    // let the next but one be taken for complete)
                     const uint32_t x = 2 * unit + 1, st = x % N;
-                    ok = tc_wait_warp(&full[st], (x / N) & 1);
+                    ok = tc_wait_warp(&full[(x - 1) % N], ((x - 1) / N) & 1) && tc_wait_warp(&full[st], (x / N) & 1);
                     if (!ok) break;
                     const int32_t key0 = (s.first + k) * kUnitKeys;
                     const uint4 there = *reinterpret_cast<const uint4 *>(s_exist[unit % kReady]);

@@ -178,6 +178,37 @@ def test_many_units_a_cta(T, G, D, f16):
     assert not status.any()
 
 
+@pytest.mark.parametrize("T,G,D,page", [(17, 4, 128, 32), (1, 8, 128, 16), (130, 2, 128, 64), (40, 4, 64, 256)])
+def test_long_ranges(T, G, D, page):
+    """Some hundred units a CTA, again and again: tiles of keys and values that arrive in any order.  (The reference by torch,
+    in 64 bits.)"""
+    import torch
+    fw = _fw()
+    torch.manual_seed(T)
+    B, H, L = 40, 8, 9000 if T < 100 else 3000
+    i32 = dict(dtype=torch.int32, device="cuda")
+    blocks = -(-(L + T) // page)
+    table = torch.randperm(B * blocks, device="cuda").to(torch.int32).view(B, blocks)
+    cache = torch.randn(B * blocks, 2, H, page, D, device="cuda").to(torch.bfloat16)
+    lens = torch.linspace(L // 3, L, B, device="cuda").to(torch.int32)
+    new = (torch.arange(B, **i32) * 7 % T) + 1
+    q = torch.randn(B, T, H * G, D, device="cuda").to(torch.bfloat16)
+    out, first, status = torch.empty_like(q), torch.empty_like(q), torch.zeros(B, **i32)
+    for i in range(60):
+        fw.switchsd_kv16_attention(q, cache, table, lens, new, out, status=status)
+        if i == 0:
+            first.copy_(out)
+        assert torch.equal(out, first) and not status.any()
+    for b in range(0, B, 3):
+        n, m = int(lens[b]), int(new[b])
+        kv = cache[table[b].long()].permute(1, 2, 0, 3, 4).reshape(2, H, -1, D)[:, :, :n + m].double()
+        x = torch.einsum("thgd,hjd->htgj", q[b, :m].double().view(m, H, G, D), kv[0]) * D ** -0.5
+        p = torch.softmax(x.masked_fill((torch.arange(n + m, device="cuda") > n + torch.arange(m, device="cuda")[:, None])[None, :, None], float("-inf")), -1)
+        want, mag = (torch.einsum("htgj,hjd->thgd", p, v).reshape(m, H * G, D) for v in (kv[1], kv[1].abs()))
+        off = (out[b, :m].double() - want).abs() - (2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -10) * mag)
+        assert off.max() <= 0 and not out[b, m:].any()
+
+
 def test_many_rows():
     """More rows than threads of a CTA, most of them short."""
     rng = np.random.default_rng(5)

@@ -77,6 +77,61 @@ __device__ constexpr uint32_t idesc16(int N, bool values) {
     return f16_idesc(N) | (F16 ? 0u : (1u << 7) | (1u << 10)) | (values ? 1u << 16 : 0u);
 }
 
+// The products and commits of a warp that stays together: its threads run the same loop on the same numbers, and the leader's
+// instructions alone take effect.  A loop of one thread's has its descriptors in ordinary registers, from where each product
+// moves them at 100 cycles a product.
+__device__ __forceinline__ uint32_t elect_leader() {
+    uint32_t leader;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "elect.sync _|p, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(leader));
+    return leader;
+}
+__device__ __forceinline__ void lead_mma_ss(uint32_t leader, uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "setp.ne.b32 q, %5, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(d),
+        "l"(da), "l"(db), "r"(idesc), "r"(uint32_t(acc)), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void lead_mma_ts(uint32_t leader, uint32_t d, uint32_t ta, uint64_t db, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "setp.ne.b32 q, %5, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+        "}\n" ::"r"(d),
+        "r"(ta), "l"(db), "r"(idesc), "r"(uint32_t(acc)), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void lead_commit(uint32_t leader, uint64_t *bar) {
+    asm volatile(
+        "{\n"
+        ".reg .pred q;\n"
+        "setp.ne.b32 q, %1, 0;\n"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n"
+        "}\n" ::"r"(smem_addr(bar)), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void lead_arrive(uint32_t leader, uint64_t *bar) {
+    asm volatile(
+        "{\n"
+        ".reg .pred q;\n"
+        "setp.ne.b32 q, %1, 0;\n"
+        "@q mbarrier.arrive.shared::cta.b64 _, [%0];\n"
+        "}\n" ::"r"(smem_addr(bar)), "r"(leader)
+        : "memory");
+}
+
 __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, int32_t w, uint64_t *bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n" ::"r"(smem_addr(dst)),
@@ -242,7 +297,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     using S = Smem16<D>;
     constexpr int N = S::kStages, G = D / 64;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full[N], empty[N], ready[kReady], s_full[2], p_full[2], o_done[2], q_full, stopped;
+    __shared__ __align__(8) uint64_t full[2][kReady], empty[N], ready[kReady], s_full[2], p_full[2], o_done[2], q_full, stopped;
     __shared__ __align__(16) uint32_t s_exist[kReady][4];  // of a unit: its keys that exist and whose page does
     __shared__ uint32_t s_tmem, s_cleared[kReady];         // s_cleared: a run (+ 1) with values that were not finite, by the run
     __shared__ int s_bad;
@@ -252,11 +307,15 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     float2 *s_ml = reinterpret_cast<float2 *>(sm_q + S::kQ);  // [2][128], of a tile that is in both slots: reference, sum
 
     if (tid == 0) {
-        for (int i = 0; i < N; ++i) {
-            mbar_init(&full[i], 1);
-            mbar_init(&empty[i], 1);
+        for (int i = 0; i < N; ++i) mbar_init(&empty[i], 1);
+        // A tile's arrival has a barrier by its unit and kind, not by its stage: a phase is then waited for by everyone who waits
+        // on that barrier at all, before its next one can begin.  (A stage has keys and values in turn, and who waits for the values
+        // only would take a phase of the keys that is still to come, or is over, for another.)
+        for (int i = 0; i < kReady; ++i) {
+            mbar_init(&full[0][i], 1);
+            mbar_init(&full[1][i], 1);
+            mbar_init(&ready[i], kValueWarps);
         }
-        for (int i = 0; i < kReady; ++i) mbar_init(&ready[i], kValueWarps);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s_full[i], 2);  // the products, and the MMA thread: what it has seen of the other warps
             mbar_init(&o_done[i], 2);
@@ -487,57 +546,58 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                             s_exist[unit % kReady][lane] = word;
                         }
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
+                        if (lane == 0) mbar_arrive_expect_tx(&full[half][unit % kReady], bytes);
                         __syncwarp();
                         if (good)
-                            tma_load_4d(sm_kv + st * S::kTile + g * kBlock16 + q * run * 128, &map, 64 * g, (key0 + q * run) & page_mask, half * a.Hkv + s.hk, page, &full[st]);
+                            tma_load_4d(sm_kv + st * S::kTile + g * kBlock16 + q * run * 128, &map, 64 * g, (key0 + q * run) & page_mask, half * a.Hkv + s.hk, page, &full[half][unit % kReady]);
                         issued = x + 1;
                     }
                     page = next;
                 }
             }
             // copies in flight write shared memory: it stays the CTA's until they have come (also where another warp gave up on them)
-            for (uint32_t x = issued > N ? issued - N : 0; x < issued; ++x) (void)tc_wait(&full[x % N], (x / N) & 1);
-        } else if (warp == kMmaWarp16 && lane == 0) {
+            for (uint32_t x = issued > N ? issued - N : 0; x < issued; ++x) (void)tc_wait(&full[x & 1][x / 2 % kReady], (x / 2 / kReady) & 1);
+        } else if (warp == kMmaWarp16) {
             // --------------------------------------------------------------------------------------- the products
             uint32_t unit0 = 0, nrun = 0, weights[2] = {0, 0};  // units and runs so far, units whose weights a slot's product took
+            const uint32_t leader = elect_leader(), tm = __shfl_sync(kFull, tmem, 0);
             const uint64_t dq0 = sw128_desc(smem_addr(sm_q)), dk0 = sw128_desc(smem_addr(sm_kv)), dv0 = value_desc(smem_addr(sm_kv));
             auto stage_of = [&](uint32_t x) { return uint64_t(x % N) * (S::kTile >> 4); };
             auto score = [&](int slot, bool split, uint32_t unit) {  // S = Q K^T
-                const uint32_t x = 2 * unit;
-                ok = ok && tc_wait(&full[x % N], (x / N) & 1);
+                ok = ok && tc_wait_warp(&full[0][unit % kReady], (unit / kReady) & 1);
                 if (!ok) return;
-                mbar_arrive(&s_full[slot]);
+                lead_arrive(leader, &s_full[slot]);
                 tc_fence_after();
-                const uint64_t dq = dq0 + (split ? 0 : uint64_t(slot) * (S::kQ >> 4)), dk = dk0 + stage_of(x);
+                const uint64_t dq = dq0 + (split ? 0 : uint64_t(slot) * (S::kQ >> 4)), dk = dk0 + stage_of(2 * unit);
 #pragma unroll
                 for (int e = 0; e < D / 16; ++e) {
                     const uint64_t step = uint64_t(((e >> 2) * kBlock16 + (e & 3) * 32) >> 4);
-                    mma_ss(tmem + slot * 128, dq + step, dk + step, idesc16<F16>(kUnitKeys, false), e != 0);
+                    lead_mma_ss(leader, tm + slot * 128, dq + step, dk + step, idesc16<F16>(kUnitKeys, false), e != 0);
                 }
-                tc_commit(&s_full[slot]);
+                lead_commit(leader, &s_full[slot]);
             };
             auto product = [&](int slot, uint32_t unit, bool fresh) {  // O += P V
-                ok = ok && tc_wait(&p_full[slot], weights[slot] & 1) && tc_wait(&ready[unit % kReady], (unit / kReady) & 1);
+                ok = ok && tc_wait_warp(&p_full[slot], weights[slot] & 1) && tc_wait_warp(&ready[unit % kReady], (unit / kReady) & 1);
                 if (!ok) return;
                 ++weights[slot];
                 tc_fence_after();
                 const uint64_t dv = dv0 + stage_of(2 * unit + 1);
 #pragma unroll
                 for (int e = 0; e < kUnitKeys / 16; ++e)
-                    mma_ts(tmem + 256 + slot * 128, tmem + slot * 128 + 8 * e, dv + uint64_t((e * 16 * 128) >> 4), idesc16<F16>(D, true), !fresh || e != 0);
+                    lead_mma_ts(leader, tm + 256 + slot * 128, tm + slot * 128 + 8 * e, dv + uint64_t((e * 16 * 128) >> 4), idesc16<F16>(D, true), !fresh || e != 0);
             };
             auto release = [&](uint32_t x) {
-                if (ok) tc_commit(&empty[x % N]);
+                if (ok) lead_commit(leader, &empty[x % N]);
             };
             auto finish = [&](int slot) {
                 if (!ok) return;
-                mbar_arrive(&o_done[slot]);
-                tc_commit(&o_done[slot]);
+                lead_arrive(leader, &o_done[slot]);
+                lead_commit(leader, &o_done[slot]);
             };
-            while (ok && runs.next(a, s)) {
-                const bool split = s.tokens * a.group <= kSlotRows;
-                ok = ok && tc_wait(&q_full, nrun & 1);  // (the rows' threads write the queries when they have read the last O)
+            while (ok && __any_sync(kFull, runs.next(a, s))) {
+                const bool split = __any_sync(kFull, s.tokens * a.group <= kSlotRows);
+                s.n = __shfl_sync(kFull, s.n, 0);
+                ok = tc_wait_warp(&q_full, nrun & 1);  // (the rows' threads write the queries when they have read the last O)
                 if (split) {
                     for (int32_t k = 0; ok && k < s.n + 2; ++k) {
                         const int slot = k & 1;
@@ -570,7 +630,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 ++nrun;
             }
             // what is in flight reads shared and tensor memory (the rows' threads wait for the last product too, unless they gave up)
-            tc_commit(&stopped);
+            lead_commit(leader, &stopped);
             (void)tc_wait(&stopped, 0);
         } else if (warp >= kFirstValueWarp) {
             // --------------------------------------------------------------------------------------- values that not every row sees
@@ -579,10 +639,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
             for (uint32_t nrun = 0; ok && runs.next(a, s); ++nrun) {
                 const int32_t all_see = s.len + s.token0;  // the last key that all rows see
                 for (int32_t k = 0; ok && k < s.n; ++k, ++unit) {
-                    // (the keys too: where a stage has keys and values in turn, a phase of either that was not waited for would
-                    // let the next but one be taken for complete)
-                    const uint32_t x = 2 * unit + 1, st = x % N;
-                    ok = tc_wait_warp(&full[(x - 1) % N], ((x - 1) / N) & 1) && tc_wait_warp(&full[st], (x / N) & 1);
+                    const uint32_t st = (2 * unit + 1) % N;
+                    ok = tc_wait_warp(&full[1][unit % kReady], (unit / kReady) & 1);
                     if (!ok) break;
                     const int32_t key0 = (s.first + k) * kUnitKeys;
                     const uint4 there = *reinterpret_cast<const uint4 *>(s_exist[unit % kReady]);

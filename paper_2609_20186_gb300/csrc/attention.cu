@@ -511,14 +511,6 @@ __global__ void __launch_bounds__(kAttnThreads, attn_ctas_per_sm(NT)) attn_kerne
     }
 }
 
-static int attn_sms() {
-    static int count[64] = {0};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    if (count[dev] == 0 && cudaDeviceGetAttribute(&count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return count[dev];
-}
-
 static size_t attn_workspace(int D, int NT) {
     return std::max(size_t(2 * kAttnMaxCtas) * (sizeof(int4) + size_t(8 * NT) * (D + 4) * sizeof(float)), attn_tc_workspace(D));
 }
@@ -599,7 +591,7 @@ extern "C" int switchsd_kv4_attention(const switchsd_kv4_attention_params *p) {
     a.dim = p->D;
     a.scale = p->scale;
     a.give_up = 0;
-    const int sms = attn_sms();
+    const int sms = sm_count();
     if (sms == 0) return SWITCHSD_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(p->stream);
     cudaError_t e;

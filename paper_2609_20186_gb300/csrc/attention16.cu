@@ -779,9 +779,9 @@ static bool encode_cache(CUtensorMap *map, const switchsd_kv16_attention_params 
 template <bool F16, int D>
 static cudaError_t launch16(const CUtensorMap &map, const Attn16Args &a, cudaStream_t s) {
     static bool attr_done[64] = {false};
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    const int sms = sm_count();
+    int dev = 0;
+    cudaError_t e = sms ? cudaGetDevice(&dev) : cudaErrorInvalidDevice;
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64 || !attr_done[dev]) {
         e = cudaFuncSetAttribute(attn16_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem16<D>::bytes);

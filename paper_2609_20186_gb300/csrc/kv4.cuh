@@ -31,6 +31,14 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 // A stride of a dimension of n: no address goes by that of a dimension of one.
 inline bool stride_ok(int64_t stride, int32_t n) { return n == 1 || (stride >= 0 && stride % 8 == 0); }
 inline int64_t stride_of(int64_t stride, int32_t n) { return n == 1 ? 0 : stride; }
+// SMs of the current device; 0: no device.
+inline int sm_count() {
+    static int count[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (count[dev] == 0 && cudaDeviceGetAttribute(&count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return count[dev];
+}
 inline int log2_of(int32_t pow2) {
     int s = 0;
     while ((1 << s) < pow2) ++s;

@@ -5,11 +5,11 @@
 // (W also loses what z gained).  The threads' meet in a tree; then lse = m / temperature + ln S, and the entropy is
 // ln S - W / S.
 //
-// Top alternatives.  Of the first batch of loads every half warp's largest logit is known, and the k-th largest of those 32
-// is a bound that k of the CTA's logits reach: what lies below is no alternative.  The few that do not go, one by one, into
-// their warp's list, sorted over its lanes, whose k-th raises the warp's own bound.  The lists (of all CTAs) are ranked by
-// counting at the end.  A batch is looked at again only where its largest logit, which the sums want anyway, reaches the
-// bound.
+// Top alternatives.  Of the first batch of loads the largest logit of every four threads is known, and the k-th largest of
+// those 128 is a bound that k of the CTA's logits reach: what lies below is no alternative.  The few that do not go, one by
+// one, into their warp's list, sorted over its lanes, whose k-th raises the warp's own bound.  The lists (of all CTAs) are
+// ranked by counting at the end.  A batch is looked at again only where its largest logit, which the sums want anyway,
+// reaches the bound.
 #include "sampling.cuh"
 
 #include <algorithm>
@@ -18,7 +18,7 @@ namespace switchsd {
 
 constexpr int kProbThreads = 512;
 constexpr int kProbWarps = kProbThreads / kWarp;
-constexpr int kProbFlight = 8;          // vectors of a thread in flight
+constexpr int kProbFlight = 4;          // vectors of a thread that are worked on, and as many in flight
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kGone = -200.f;         // binary logarithm of a weight that binary32 does not have
 
@@ -33,12 +33,6 @@ struct ProbArgs {
     int32_t *status;
     int32_t T, V, K, top, new_add, tokens_stride;
 };
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 // max, sum of weights, sum of weights times their binary logarithms
 struct Sums {
@@ -58,7 +52,54 @@ struct Sums {
     }
 };
 
+// Places in the order of floats (0 of what is not a number, -inf and what is not there come first); -0 and 0 share one.
+__device__ __forceinline__ uint32_t place_of(float v) {
+    const uint32_t u = __float_as_uint(v + 0.f);
+    return v == v ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float at_place(uint32_t p) {
+    return p == 0 ? -INFINITY : __uint_as_float(p & 0x80000000u ? p & 0x7fffffffu : ~p);
+}
+// A bound that k of a warp's 128 numbers (four a lane, by their places) reach, as large as 20 bits can say; the same for all.
+__device__ __forceinline__ float kth_largest(const uint32_t (&p)[4], int k) {
+    uint32_t bound = 0;
+#pragma unroll 1
+    for (uint32_t bit = 0x80000000u; bit >= 0x1000u; bit >>= 1) {
+        const uint32_t trial = bound | bit;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += __popc(__ballot_sync(kFull, p[i] >= trial));
+        if (n >= k) bound = trial;
+    }
+    return bound > 0x007fffffu ? at_place(bound) : -INFINITY;  // (the place of -inf)
+}
+
 __device__ __forceinline__ bool before(float v, int32_t i, float w, int32_t j) { return v > w || (v == w && i < j); }
+
+// A warp's 32 best (value, token) pairs, a lane each, in order.
+struct WarpList {
+    float v = -INFINITY, last = -INFINITY;  // this lane's, and the k-th
+    int32_t id = 0x7fffffff;
+    // The lanes' pairs, those with x > last (or the first of equal ones).
+    __device__ __forceinline__ void insert(float x, int32_t token, int k) {
+        uint32_t todo = __ballot_sync(kFull, x > last || (x == last && x > -INFINITY));
+        const int lane = threadIdx.x & 31;
+        while (todo) {
+            const int src = __ffs(int(todo)) - 1;
+            todo &= todo - 1;
+            const float nv = __shfl_sync(kFull, x, src);
+            const int32_t ni = __shfl_sync(kFull, token, src);
+            const int place = __popc(__ballot_sync(kFull, before(v, id, nv, ni)));
+            const float uv = __shfl_up_sync(kFull, v, 1);
+            const int32_t ui = __shfl_up_sync(kFull, id, 1);
+            if (lane >= place) {
+                v = lane == place ? nv : uv;
+                id = lane == place ? ni : ui;
+            }
+        }
+        last = __shfl_sync(kFull, v, k - 1);
+    }
+};
 
 // The first k of n (value, token) pairs in `v`, `id`, in order, to `out_v`, `out_id` (the same for all threads of the CTA).
 __device__ __forceinline__ void rank_pairs(const float *v, const int32_t *id, int n, int k, float *out_v, int32_t *out_id) {
@@ -78,7 +119,8 @@ template <int DT>
 __global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArgs a, int parts) {
     using Row = LogitRow<DT>;
     constexpr int P = Row::P, F = kProbFlight;
-    __shared__ float s_group[2 * kProbWarps];
+    __shared__ float s_group[4 * 32];  // largest of four threads each
+    __shared__ float s_bound;
     __shared__ Sums s_sums[kProbWarps], s_all;
     __shared__ float s_value[kProbWarps * 32], s_top[32];
     __shared__ int32_t s_id[kProbWarps * 32], s_top_id[32];
@@ -118,79 +160,91 @@ __global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArg
 
     Sums sums{-INFINITY, 0.f, 0.f};
     float bound = -INFINITY;                   // of the CTA: k logits reach it
-    float list_v = -INFINITY, list_last = -INFINITY;  // this lane's place of the warp's list, its k-th value
-    int32_t list_id = 0x7fffffff;
+    WarpList list;
     bool first = true;
+    uint4 x[F], next[F];
+    row.load(next, begin + tid, kProbThreads, end);
     for (int32_t base = begin; base < end; base += kProbThreads * F) {
-        uint4 x[F];
 #pragma unroll
-        for (int i = 0; i < F; ++i) x[i] = row.load(base + tid + i * kProbThreads, end);
+        for (int i = 0; i < F; ++i) x[i] = next[i];
+        row.load(next, base + tid + kProbThreads * F, kProbThreads, end);
         const float top = Row::largest(x);
         if (first && k > 0) {
             float g = fmaxf(top, -INFINITY);
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(kFull, g, o));
-            if ((lane & 15) == 0) s_group[2 * warp + (lane >> 4)] = g;
+            g = fmaxf(g, __shfl_xor_sync(kFull, g, 1));
+            g = fmaxf(g, __shfl_xor_sync(kFull, g, 2));
+            if ((lane & 3) == 0) s_group[tid >> 2] = g;
             __syncthreads();
-            g = s_group[lane];
-            int rank = 0;
-            for (int i = 0; i < 32; ++i) {
-                const float o = __shfl_sync(kFull, g, i);
-                rank += o > g || (o == g && i < lane);
+            if (warp == 0) {
+                const uint32_t p[4] = {place_of(s_group[lane]), place_of(s_group[lane + 32]), place_of(s_group[lane + 64]), place_of(s_group[lane + 96])};
+                g = kth_largest(p, k);
+                if (lane == 0) s_bound = g;
             }
-            bound = __shfl_sync(kFull, g, __ffs(int(__ballot_sync(kFull, rank == k - 1))) - 1);
+            __syncthreads();
+            bound = s_bound;
         }
         first = false;
         if (top > sums.m) sums.scale_to(top, c2);
-        float s2 = 0.f, w2 = 0.f;
+        // Where a logit at kLow has no weight, what lies below (-inf, NaN) is taken for it, and z is one multiply-add off the
+        // reference m c2, whose rounding is put right at the batch's end.
+        const float ref = sums.m * c2;
+        if ((sums.m - Row::kLow) * c2 >= -kGone && fabsf(ref) < 1e30f && c2 < 1e6f) {
+            const float off = fmaf(sums.m, c2, -ref);
+            const uint64_t c = pair_of(c2, c2), r = pair_of(-ref, -ref);
+            uint64_t s2[2] = {0, 0}, w2[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < F; ++i) {
-            float v[P];
-            Row::widen(x[i], v);
+            for (int i = 0; i < F; ++i) {
+                float v[P];
+                Row::widen(Row::raised(x[i]), v);
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const float y = fmaxf((v[e] - sums.m) * c2, kGone), p = exp2_fast(y);  // (NaN: no weight)
-                s2 += p;
-                w2 = fmaf(p, y, w2);
+                for (int e = 0; e < P; e += 2) {
+                    const uint64_t z = fma_pair(pair_of(v[e], v[e + 1]), c, r);
+                    const float2 y = halves_of(z);
+                    const uint64_t p = pair_of(exp2_fast(y.x), exp2_fast(y.y));
+                    s2[(e >> 1) & 1] = add_pair(s2[(e >> 1) & 1], p);
+                    w2[(e >> 1) & 1] = fma_pair(p, z, w2[(e >> 1) & 1]);
+                }
             }
-        }
-        sums.s += s2;
-        sums.w += w2;
-        if (k > 0 && __any_sync(kFull, top >= bound && top > list_last)) {
-            uint64_t mask = 0;
+            const float2 sp = halves_of(add_pair(s2[0], s2[1])), wp = halves_of(add_pair(w2[0], w2[1]));
+            const float f = exp2_fast(-off), part_s = sp.x + sp.y;
+            sums.s = fmaf(part_s, f, sums.s);
+            sums.w = fmaf(fmaf(-off, part_s, wp.x + wp.y), f, sums.w);
+        } else {
+            float s2 = 0.f, w2 = 0.f;
 #pragma unroll
             for (int i = 0; i < F; ++i) {
                 float v[P];
                 Row::widen(x[i], v);
 #pragma unroll
-                for (int e = 0; e < P; ++e) mask |= uint64_t(v[e] >= bound && v[e] > list_last) << (i * P + e);
-            }
-            while (__any_sync(kFull, mask != 0)) {
-                float v = -INFINITY;
-                int32_t id = 0x7fffffff;
-                if (mask) {
-                    const int e = __ffsll(static_cast<long long>(mask)) - 1;
-                    mask &= mask - 1;
-                    id = row.token(base + tid + (e / P) * kProbThreads) + e % P;
-                    v = row[id];
+                for (int e = 0; e < P; ++e) {
+                    const float y = fmaxf((v[e] - sums.m) * c2, kGone), p = exp2_fast(y);  // (NaN: no weight)
+                    s2 += p;
+                    w2 = fmaf(p, y, w2);
                 }
-                uint32_t todo = __ballot_sync(kFull, v > list_last || (v == list_last && v > -INFINITY));
-                while (todo) {
-                    const int src = __ffs(int(todo)) - 1;
-                    todo &= todo - 1;
-                    const float nv = __shfl_sync(kFull, v, src);
-                    const int32_t ni = __shfl_sync(kFull, id, src);
-                    const int place = __popc(__ballot_sync(kFull, before(list_v, list_id, nv, ni)));
-                    const float uv = __shfl_up_sync(kFull, list_v, 1);
-                    const int32_t ui = __shfl_up_sync(kFull, list_id, 1);
-                    if (lane == place) {
-                        list_v = nv;
-                        list_id = ni;
-                    } else if (lane > place) {
-                        list_v = uv;
-                        list_id = ui;
-                    }
-                    list_last = __shfl_sync(kFull, list_v, k - 1);
+            }
+            sums.s += s2;
+            sums.w += w2;
+        }
+        if (k > 0 && __any_sync(kFull, top >= bound && top > list.last)) {
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                const uint4 one[1] = {x[i]};
+                const float best = Row::largest(one);
+                if (!__any_sync(kFull, best >= bound && best > list.last)) continue;
+                float v[P];
+                Row::widen(x[i], v);
+                uint32_t mask = 0;
+#pragma unroll
+                for (int e = 0; e < P; ++e) mask |= uint32_t(v[e] >= bound && v[e] > list.last) << e;
+                const int32_t from = row.token(base + tid + i * kProbThreads);
+#pragma unroll 1
+                while (__any_sync(kFull, mask != 0)) {
+                    const int e = __ffs(int(mask)) - 1;  // (-1: nothing)
+                    mask &= mask - 1;
+                    float y = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < P; ++j) y = e == j ? v[j] : y;
+                    list.insert(y, from + e, k);
                 }
             }
         }
@@ -203,14 +257,14 @@ __global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArg
     if (lane == 0) s_sums[warp] = sums;
     __syncthreads();
     if (k > 0) {
-        const bool has = lane < k && list_v >= bound && list_v > -INFINITY;
+        const bool has = lane < k && list.v >= bound && list.v > -INFINITY;
         const uint32_t those = __ballot_sync(kFull, has);
         int from = 0;
         if (lane == 0 && those) from = atomicAdd(&s_n, __popc(those));
         from = __shfl_sync(kFull, from, 0) + __popc(those & ((1u << lane) - 1));
         if (has) {
-            s_value[from] = list_v;
-            s_id[from] = list_id;
+            s_value[from] = list.v;
+            s_id[from] = list.id;
         }
         __syncthreads();
         rank_pairs(s_value, s_id, s_n, k, s_top, s_top_id);
@@ -291,10 +345,8 @@ __global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArg
 
 template <int DT>
 static cudaError_t launch_logprobs(const ProbArgs &a, int32_t B, cudaStream_t s) {
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
+    const int sms = sm_count();
+    if (sms == 0) return cudaErrorInvalidDevice;
     const int parts = parts_of(int64_t(B) * a.T, (int64_t(a.V) + LogitRow<DT>::P - 1) / LogitRow<DT>::P, kProbThreads, 2 * sms);
     return launch_pdl(logprobs_kernel<DT>, dim3(unsigned(parts) * unsigned(a.T), unsigned(B)), dim3(kProbThreads), 0, s, parts > 1 ? unsigned(parts) : 0u, a, parts);
 }

@@ -5,9 +5,8 @@
 // the row's seed, the token's place in the context and v.
 //
 // Screening.  E = -ln(1 - x) is at least x, so v beats a score s only where x < w_v e^-s: a binary exponential and a
-// comparison of the number's upper 23 bits, beside the bits themselves (two 64-bit products for two tokens).  s is the
-// best score of the CTA so far, to begin with of one logit a thread; few tokens pass, and they alone are worked out, in
-// binary32.  Where two scores are closer than its error, both are worked out in binary64, so the answer is that of
+// comparison of the number's upper 23 bits, beside the bits themselves (two 64-bit products for two tokens).  s is what a
+// vector of logits a thread reaches at least; few tokens pass, and they alone are worked out, a thread each, in binary32.  Where two scores are closer than its error, both are worked out in binary64, so the answer is that of
 // binary64 throughout.  A drafter's distribution is read for the few only: w = max(0, p - q) is at most p.
 #include "sampling.cuh"
 
@@ -15,6 +14,7 @@ namespace switchsd {
 
 constexpr int kRaceThreads = 512;
 constexpr int kRaceFlight = 4;          // vectors of a thread in flight
+constexpr int kRaceList = 1024;         // tokens of a CTA that passed the test
 constexpr float kRaceLog2e = 1.4426950408889634f;
 
 struct RaceArgs {
@@ -66,24 +66,28 @@ struct Race {
         }
         return y - log(-log1p(-(double(bits(v)) + 0.5) * 0x1p-32));
     }
-    // ln w - ln E of token v with logit z, -inf where it has no weight.
-    __device__ float score(int32_t v, float z) const {
+    // ln w - ln E of token v with logit z, -inf where it has no weight, or where it stays below `floor`.
+    __device__ float score(int32_t v, float z, float floor) const {
         if (!(z > -INFINITY) || v == skip) return -INFINITY;
         if (greedy) return z;
-        float y = z / temperature;
-        if (residual) {
-            const float zq = q[v];
-            if (zq > -INFINITY) {
-                const float a = (zq - z) / temperature, b = q_lse - lse, d = a - b;  // ln(q / p)
-                if (d > 0.0078125f + 1e-4f * (fabsf(a) + fabsf(b))) return -INFINITY;
-                if (!(d < -0.0078125f - 1e-4f * (fabsf(a) + fabsf(b)))) return float(exact(v));  // p - q nearly cancels
-                y += logf(-expm1f(d));
-            }
-            y -= lse;
-        }
         const uint32_t r = bits(v);
         const float e = r < 0x80000000u ? -log1pf(-(float(r) + 0.5f) * 0x1p-32f) : -logf((float(~r) + 0.5f) * 0x1p-32f);
-        return y - logf(e);
+        float y = z / temperature - logf(e);
+        if (residual) {
+            y -= lse;
+            const float zq = q[v];
+            if (zq > -INFINITY) {
+                const float a = (zq - z) / temperature, b = q_lse - lse, d = a - b;  // ln(q / p), and how far it may be off
+                const float off = 4e-7f * (fabsf(a) + fabsf(b));
+                if (d > off) return -INFINITY;
+                if (!(-d > 1e3f * off)) {  // p - q nearly cancels
+                    if (y + logf(off - d) + margin(y) < floor) return -INFINITY;
+                    return float(exact(v));
+                }
+                y += logf(-expm1f(d));
+            }
+        }
+        return y;
     }
     // How far binary32's score may be off, and binary64's of what is compared with it.
     __device__ float margin(float s) const { return greedy || fabsf(s) == INFINITY ? 0.f : (residual ? 4e-3f : 2e-5f) + 1e-6f * fabsf(s); }
@@ -93,8 +97,8 @@ template <int DT>
 struct Best {
     float s = -INFINITY;
     int32_t v = -1;
-    __device__ void consider(const Race<DT> &race, int32_t token, float z) {
-        const float x = race.score(token, z);
+    __device__ void consider(const Race<DT> &race, int32_t token, float z, float floor) {
+        const float x = race.score(token, z, floor);
         if (!(x > -INFINITY) || token == v) return;
         const float margin = race.margin(x);
         bool take = v < 0 || x > s + margin;
@@ -113,7 +117,8 @@ template <int DT>
 __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArgs a, int parts) {
     using Row = LogitRow<DT>;
     constexpr int P = Row::P, F = kRaceFlight;
-    __shared__ int32_t s_first, s_best, s_n;
+    __shared__ int32_t s_first, s_best, s_n, s_few, s_token;
+    __shared__ int32_t s_tokens[kRaceList];
     __shared__ int32_t s_list[kRaceThreads];
     __shared__ double s_exact[kRaceThreads];
     const int tid = threadIdx.x, part = blockIdx.x, b = blockIdx.y, k = a.T - 1;
@@ -130,7 +135,7 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
     // --- the accepted length --------------------------------------------------------------------------------------
     if (tid == 0) {
         s_first = len;
-        s_n = 0;
+        s_n = s_few = 0;
         s_best = float_order(-INFINITY);
     }
     __syncthreads();
@@ -162,12 +167,15 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
     const int32_t per = (row.vectors + parts - 1) / parts, begin = part * per, end = min(begin + per, row.vectors);
     const float c2 = fminf(kRaceLog2e / race.temperature, 3e38f);
     Best<DT> best;
-    float top = -INFINITY;
-    for (int round = 0; !none; ++round) {
+    int32_t token = -1;
+    bool again = race.residual || race.skip >= 0;  // where w leaves nothing
+    while (!none) {
         if (race.greedy) {
             for (int32_t j = begin + tid; j < end; j += kRaceThreads) {
+                uint4 w[1];
                 float x[P];
-                Row::widen(row.load(j, end), x);
+                row.load(w, j, 0, end);
+                Row::widen(w[0], x);
 #pragma unroll
                 for (int e = 0; e < P; ++e)
                     if (x[e] > best.s) {  // (ascending tokens)
@@ -176,19 +184,48 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
                     }
             }
         } else {
-            const int32_t v0 = row.token(begin + tid) + (tid & (P - 1));
-            if (begin + tid < end && uint32_t(v0) < uint32_t(a.V)) best.consider(race, v0, row[v0]);
-            atomicMax(&s_best, float_order(best.s));
-            __syncthreads();
-            const float lse2 = race.lse * kRaceLog2e;
-            for (int32_t base = begin + tid; base < end; base += kRaceThreads * F) {
-                uint4 w[F];
+            uint4 w[F];
+            row.load(w, begin + tid, kRaceThreads, end);
+            // --- a bound: what a vector a thread reaches at least, in binary logarithms ---------------------------
+            // E <= x (1 + x) for x <= 1/2, and ln(1 + x) <= x
+            const float lse2 = race.lse * kRaceLog2e, q_lse2 = race.q_lse * kRaceLog2e;
+            float low = -INFINITY;
+            if (begin + tid < end && (!race.residual || (race.q.lead == race.l.lead && race.l.inside(begin + tid)))) {
+                float x[P], y[P];
+                Row::widen(w[0], x);
+                if (race.residual) {
+                    uint4 qw[1];
+                    race.q.load(qw, begin + tid, 0, end);
+                    Row::widen(qw[0], y);
+                }
+                const int32_t from = row.token(begin + tid);
+                const float c = kRaceLog2e / race.temperature, eps = 1e-4f + 1e-6f * (fabsf(lse2) + fabsf(q_lse2));
 #pragma unroll
-                for (int i = 0; i < F; ++i) w[i] = row.load(base + i * kRaceThreads, end);
-                // A lower bound of the best score, in binary logarithms, less what the test's own roundings may take.
-                const float s = order_float(*static_cast<volatile int32_t *>(&s_best));
-                const float s2 = (s - race.margin(s)) * kRaceLog2e;
-                const float off = fabsf(s) < 1e30f ? 1e-3f + 4e-7f * (fabsf(s2) + fabsf(lse2)) - s2 - lse2 : INFINITY;
+                for (int e = 0; e < P; ++e) {
+                    const int32_t v = from + e;
+                    const float r = (float(race.bits(v)) + 0.5f) * 0x1p-32f;
+                    float z = fmaf(x[e], c, -lse2);
+                    if (race.residual) {  // p - q less what their roundings may take
+                        const float p = exp2_fast(z);
+                        z = log2_fast(fmaf(-1.f - eps, exp2_fast(fmaf(y[e] > -INFINITY ? y[e] : -1e30f, c, -q_lse2)), (1.f - eps) * p));
+                    }
+                    z -= log2_fast(r) + 1.4427f * r;
+                    if (uint32_t(v) < uint32_t(a.V) && v != race.skip && r <= 0.5f && x[e] > -INFINITY && fabsf(z) < 1e30f) low = fmaxf(low, z);
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) low = fmaxf(low, __shfl_xor_sync(kFull, low, o));
+            if ((tid & 31) == 0) atomicMax(&s_best, float_order(low));
+            __syncthreads();
+            low = order_float(s_best);
+            // less what the roundings of the bound and of the test may take
+            const float off = fabsf(low) < 1e30f ? 2e-3f + 1e-6f * (fabsf(low) + fabsf(lse2) + fabsf(q_lse2)) - low - lse2 : INFINITY;
+            const float floor = fabsf(low) < 1e30f ? (low - 2e-3f - 1e-6f * (fabsf(low) + fabsf(lse2) + fabsf(q_lse2))) * 0.69314718f : -INFINITY;
+            __syncthreads();
+            if (tid == 0) s_best = float_order(-INFINITY);
+            const uint64_t c22 = pair_of(c2, c2), off2 = pair_of(off, off), up = pair_of(1.002f, 1.002f), one = pair_of(1.0000003f, 1.0000003f);
+            // --- the tokens that may be better --------------------------------------------------------------------
+            for (int32_t base = begin + tid; base < end;) {
 #pragma unroll 1
                 for (int i = 0; i < F; ++i) {
                     const int32_t j = base + i * kRaceThreads;
@@ -198,15 +235,22 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
 #pragma unroll
                     for (int o = 0; o < F - 1; ++o) w[o] = w[o + 1];
                     const int32_t from = row.token(j);
+                    // 1 + (x rounded down to 23 bits) <= 1 + w e^-s, of the pairs that begin at an even token
+                    float most[P];
+#pragma unroll
+                    for (int e = 0; e < P; e += 2) {
+                        const float2 z = halves_of(fma_pair(pair_of(x[e], x[e + 1]), c22, off2));
+                        const float2 t = halves_of(fma_pair(pair_of(exp2_fast(z.x), exp2_fast(z.y)), up, one));
+                        most[e] = t.x;
+                        most[e + 1] = t.y;
+                    }
                     uint64_t n = race.key + (uint64_t(int64_t(from >> 1)) + 1) * kGolden;  // of the pair that `from` lies in
-                    uint64_t z = splitmix(n);
                     uint32_t mask = 0;
                     auto test = [&](int e, uint32_t r) {
-                        // 1 + (x rounded down to 23 bits) <= 1 + w e^-s
-                        const float t = exp2f(fmaf(x[e], c2, off));
-                        mask |= uint32_t(__uint_as_float(0x3f800000u | (r >> 9)) <= fmaf(t, 1.002f, 1.0000003f)) << e;
+                        if (__uint_as_float(0x3f800000u | (r >> 9)) <= most[e]) mask |= 1u << e;
                     };
                     if (from & 1) {
+                        uint64_t z = splitmix(n);
 #pragma unroll
                         for (int e = 0; e < P; e += 2) {
                             test(e, uint32_t(z >> 32));
@@ -215,77 +259,110 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
                         }
                     } else {
 #pragma unroll
-                        for (int e = 0; e < P; e += 2) {
-                            if (e) z = splitmix(n += kGolden);
+                        for (int e = 0; e < P; e += 2, n += kGolden) {
+                            const uint64_t z = splitmix(n);
                             test(e, uint32_t(z));
                             test(e + 1, uint32_t(z >> 32));
                         }
                     }
                     while (mask) {
-                        const int e = __ffs(int(mask)) - 1;
+                        const int32_t v = from + __ffs(int(mask)) - 1;
                         mask &= mask - 1;
-                        const int32_t v = from + e;
                         if (uint32_t(v) >= uint32_t(a.V)) continue;
-                        best.consider(race, v, row[v]);
-                        atomicMax(&s_best, float_order(best.s));
+                        const int at = atomicAdd(&s_few, 1);
+                        if (at < kRaceList)
+                            s_tokens[at] = v;
+                        else
+                            best.consider(race, v, row[v], floor);
                     }
                 }
+                base += kRaceThreads * F;
+                if (base < end) row.load(w, base, kRaceThreads, end);
             }
+            // --- their scores -------------------------------------------------------------------------------------
+            __syncthreads();
+            for (int i = tid; i < min(s_few, kRaceList); i += kRaceThreads) best.consider(race, s_tokens[i], row[s_tokens[i]], floor);
         }
-        // --- the best of all: those that binary32 does not tell from it, in binary64 ------------------------------
-        if (race.greedy) atomicMax(&s_best, float_order(best.s));
+        // --- the CTA's best: among those that binary32 does not tell from it, binary64's --------------------------
+        float s = best.s;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s = fmaxf(s, __shfl_xor_sync(kFull, s, o));
+        if ((tid & 31) == 0) atomicMax(&s_best, float_order(s));
         __syncthreads();
-        top = order_float(s_best);
+        const float top = order_float(s_best);
+        if (top > -INFINITY && best.v >= 0 && best.s >= top - 2.f * race.margin(top)) s_list[atomicAdd(&s_n, 1)] = best.v;
+        __syncthreads();
+        const int n = s_n;
+        if (n > 1) {
+            if (tid < n) s_exact[tid] = race.exact(s_list[tid]);
+            __syncthreads();
+        }
+        if (tid == 0) {
+            int32_t v = n > 0 ? s_list[0] : -1;
+            double most = n > 1 ? s_exact[0] : 0.;
+            for (int i = 1; i < n; ++i)
+                if (s_exact[i] > most || (s_exact[i] == most && s_list[i] < v)) {
+                    v = s_list[i];
+                    most = s_exact[i];
+                }
+            s_token = v;
+        }
+        // --- the row's --------------------------------------------------------------------------------------------
         if (parts > 1) {
             cluster_arrive_release();
             cluster_wait_acquire();
-            for (int r = 0; r < parts; ++r) top = fmaxf(top, order_float(int32_t(remote_word(&s_best, r))));
         }
-        if (top > -INFINITY || round == 1 || (!race.residual && race.skip < 0)) break;
+        if (tid < 32 && (part == 0 || again)) {  // lane r has part r's
+            int32_t v = -1;
+            float its = -INFINITY;
+            const int lane = tid;
+            if (lane < parts) {
+                v = parts > 1 ? int32_t(remote_word(&s_token, lane)) : s_token;
+                its = parts > 1 ? order_float(int32_t(remote_word(&s_best, lane))) : top;
+            }
+            float all = its;
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(kFull, all, o));
+            all = __shfl_sync(kFull, all, 0);
+            uint32_t near = __ballot_sync(kFull, v >= 0 && its >= all - 2.f * race.margin(all));
+            if (near & (near - 1)) {  // several: binary64's best, of equal ones the first
+                double mine = -INFINITY;
+                if ((near >> lane) & 1) mine = race.exact(v);
+                int32_t best_v = -1;
+                double most = -INFINITY;
+                for (int r = 0; r < parts; ++r) {
+                    const double x = __shfl_sync(kFull, mine, r);
+                    const int32_t u = __shfl_sync(kFull, v, r);
+                    if (((near >> r) & 1) && (best_v < 0 || x > most || (x == most && u < best_v))) {
+                        best_v = u;
+                        most = x;
+                    }
+                }
+                token = best_v;
+            } else if (near) {
+                token = __shfl_sync(kFull, v, __ffs(int(near)) - 1);
+            }
+            if (lane == 0) s_first = token;  // (the accepted length is known)
+        }
+        if (!again) break;
+        __syncthreads();
+        if (s_first >= 0) break;
         // nothing is left of w: once more with p
         if (parts > 1) {
-            cluster_arrive_release();  // (all have read s_best)
+            cluster_arrive_release();  // (all have read the parts' results)
             cluster_wait_acquire();
         }
+        if (tid == 0) {
+            s_few = s_n = 0;
+            s_best = float_order(-INFINITY);
+        }
         __syncthreads();
-        race.residual = false;
+        race.residual = again = false;
         race.lse = race.q_lse = 0.f;
         race.skip = -1;
     }
-    int32_t token = -1;
-    if (top > -INFINITY) {
-        if (best.v >= 0 && best.s >= top - 2.f * race.margin(top)) s_list[atomicAdd(&s_n, 1)] = best.v;
-        __syncthreads();
-        if (parts > 1) {
-            cluster_arrive_release();
-            cluster_wait_acquire();
-        }
-        if (part == 0) {
-            double of_token = -INFINITY;
-            int all = 0;
-            for (int r = 0; r < parts; ++r) all += parts > 1 ? int(remote_word(&s_n, r)) : s_n;
-            for (int r = 0; r < parts; ++r) {
-                const int n = parts > 1 ? int(remote_word(&s_n, r)) : s_n;
-                int32_t mine = -1;
-                if (tid < n) {
-                    mine = parts > 1 ? int32_t(remote_word(&s_list[tid], r)) : s_list[tid];
-                    s_exact[tid] = all == 1 ? 0. : race.exact(mine);
-                }
-                __syncthreads();
-                if (tid == 0)
-                    for (int i = 0; i < n; ++i) {
-                        const int32_t v = parts > 1 ? int32_t(remote_word(&s_list[i], r)) : s_list[i];
-                        if (token < 0 || s_exact[i] > of_token || (s_exact[i] == of_token && v < token)) {
-                            token = v;
-                            of_token = s_exact[i];
-                        }
-                    }
-                __syncthreads();
-            }
-        }
-    }
     if (part == 0 && tid == 0) a.out[int64_t(b) * a.T + acc] = token;
-    if (parts > 1) {  // the others' shared memory is read until here
+    if (parts > 1) {  // the parts' shared memory is read until here
         cluster_arrive_release();
         cluster_wait_acquire();
     }
@@ -293,10 +370,8 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
 
 template <int DT>
 static cudaError_t launch_resample(const RaceArgs &a, int32_t B, cudaStream_t s) {
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
+    const int sms = sm_count();
+    if (sms == 0) return cudaErrorInvalidDevice;
     const int parts = parts_of(B, (int64_t(a.V) + LogitRow<DT>::P - 1) / LogitRow<DT>::P, kRaceThreads, 2 * sms);
     return launch_pdl(resample_kernel<DT>, dim3(unsigned(parts), unsigned(B)), dim3(kRaceThreads), 0, s, parts > 1 ? unsigned(parts) : 0u, a, parts);
 }

@@ -5,8 +5,21 @@
 #include <cuda_fp16.h>
 
 #include "kv4.cuh"
+#include "tc.cuh"
 
 namespace switchsd {
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float log2_fast(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 // A row of V logits in vectors of 16 aligned bytes: vector j has the tokens j * P - lead .. j * P - lead + P - 1, of which
 // the first and the last vector may lack some.
@@ -60,10 +73,28 @@ struct LogitRow {
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
     __device__ bool inside(int32_t j) const { return token(j) >= 0 && token(j) + P <= V; }
-    __device__ uint4 load(int32_t j, int32_t end) const {  // nothing from `end` on
-        if (j >= end) return nothing();
-        if (!inside(j)) return edge(row, V, token(j));
-        return __ldcs(reinterpret_cast<const uint4 *>(row + token(j)));
+    // Vectors j, j + step, ..; nothing from `end` on.  All loads are sent before the row's first or last vector is made up, for
+    // which there is a call.
+    template <int N>
+    __device__ __forceinline__ void load(uint4 (&x)[N], int32_t j, int32_t step, int32_t end) const {
+        bool edges = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int32_t k = j + i * step;
+            x[i] = nothing();
+            if (k < end) {
+                if (inside(k))
+                    x[i] = __ldcs(reinterpret_cast<const uint4 *>(row + token(k)));
+                else
+                    edges = true;
+            }
+        }
+        if (edges)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int32_t k = j + i * step;
+                if (k < end && !inside(k)) x[i] = edge(row, V, token(k));
+            }
     }
     __device__ static void widen(uint4 w, float (&x)[P]) {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -88,6 +119,17 @@ struct LogitRow {
         else
             asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         return r;
+    }
+    // A vector whose elements below kLow, and NaN, are kLow.
+    static constexpr float kLow = DT == SWITCHSD_F16 ? -65504.f : -0x1.98p99f;  // (8 bits)
+    __device__ static uint4 raised(uint4 w) {
+        if constexpr (DT == SWITCHSD_F32) {
+            return make_uint4(__float_as_uint(fmaxf(__uint_as_float(w.x), kLow)), __float_as_uint(fmaxf(__uint_as_float(w.y), kLow)),
+                              __float_as_uint(fmaxf(__uint_as_float(w.z), kLow)), __float_as_uint(fmaxf(__uint_as_float(w.w), kLow)));
+        } else {
+            constexpr uint32_t low = DT == SWITCHSD_F16 ? 0xfbfffbffu : 0xf14cf14cu;
+            return make_uint4(max2(w.x, low), max2(w.y, low), max2(w.z, low), max2(w.w, low));
+        }
     }
     // The largest of N vectors' elements, NaN aside (NaN where there is nothing else).
     template <int N>

@@ -124,7 +124,16 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
     const int tid = threadIdx.x, part = blockIdx.x, b = blockIdx.y, k = a.T - 1;
     pdl_wait();
     pdl_trigger();
-    const int32_t len = __ldcg(a.draft_len + b), ctx = __ldcg(a.ctx_lens + b);
+    // what does not depend on the accepted length is read together
+    const int32_t len = __ldcg(a.draft_len + b), ctx = __ldcg(a.ctx_lens + b), mode = a.mode ? __ldcg(a.mode + b) : SWITCHSD_MODE_COPY + 1;
+    const float temperature = a.temperature ? __ldcg(a.temperature + b) : 1.f;
+    const uint64_t seed = uint64_t(__ldcg(a.seeds + b));
+    auto rejected = [&](int i) {
+        const int64_t at = int64_t(b) * k + i;
+        const float q = a.q ? __ldcg(a.q + at) : 1.f;
+        return !(__fmul_rn(__ldcg(a.u + at), q) < __ldcg(a.p + at));
+    };
+    const bool mine = tid < k && rejected(tid);
     const bool ok = len >= 0 && len <= k && ctx >= 0;
     if (part == 0) {
         if (tid == 0 && a.status) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
@@ -139,25 +148,23 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
         s_best = float_order(-INFINITY);
     }
     __syncthreads();
-    for (int i = tid; i < len; i += kRaceThreads) {
-        const int64_t at = int64_t(b) * k + i;
-        const float q = a.q ? __ldcg(a.q + at) : 1.f;
-        if (!(__fmul_rn(__ldcg(a.u + at), q) < __ldcg(a.p + at))) {
+    if (mine && tid < len) atomicMin(&s_first, tid);
+    for (int i = tid + kRaceThreads; i < len; i += kRaceThreads)
+        if (rejected(i)) {
             atomicMin(&s_first, i);
             break;
         }
-    }
     __syncthreads();
     const int acc = s_first;
     if (part == 0)
         for (int i = tid; i < a.T; i += kRaceThreads)
             if (i != acc) a.out[int64_t(b) * a.T + i] = -1;
     // --- the weights ----------------------------------------------------------------------------------------------
-    const bool drafted = acc < len, drafter = drafted && a.q_logits && !(a.mode && __ldcg(a.mode + b) == SWITCHSD_MODE_COPY);
+    const bool drafted = acc < len, drafter = drafted && a.q_logits && mode != SWITCHSD_MODE_COPY;
     const Row row(a.logits, b * a.sb + acc * a.st, a.V);
     Race<DT> race{row, drafter ? Row(a.q_logits, b * a.qb + acc * a.qt, a.V) : row};
-    race.key = splitmix(uint64_t(__ldcg(a.seeds + b)) + (uint64_t(ctx) + uint64_t(acc) + 1) * kGolden);
-    race.temperature = a.temperature ? __ldcg(a.temperature + b) : 1.f;
+    race.key = splitmix(seed + (uint64_t(ctx) + uint64_t(acc) + 1) * kGolden);
+    race.temperature = temperature;
     race.greedy = race.temperature == 0.f;
     race.residual = drafter && !race.greedy;
     race.lse = race.residual ? __ldcg(a.lse + int64_t(b) * a.T + acc) : 0.f;
@@ -225,18 +232,15 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
             if (tid == 0) s_best = float_order(-INFINITY);
             const uint64_t c22 = pair_of(c2, c2), off2 = pair_of(off, off), up = pair_of(1.002f, 1.002f), one = pair_of(1.0000003f, 1.0000003f);
             // --- the tokens that may be better --------------------------------------------------------------------
-            for (int32_t base = begin + tid; base < end;) {
-#pragma unroll 1
-                for (int i = 0; i < F; ++i) {
-                    const int32_t j = base + i * kRaceThreads;
-                    if (j >= end) break;
-                    float x[P];
-                    Row::widen(w[0], x);
+            uint4 next[F];
+            for (int32_t base = begin + tid; base < end; base += kRaceThreads * F) {
+                row.load(next, base + kRaceThreads * F, kRaceThreads, end);
+                uint32_t mask = 0;
 #pragma unroll
-                    for (int o = 0; o < F - 1; ++o) w[o] = w[o + 1];
-                    const int32_t from = row.token(j);
-                    // 1 + (x rounded down to 23 bits) <= 1 + w e^-s, of the pairs that begin at an even token
-                    float most[P];
+                for (int i = 0; i < F; ++i) {
+                    float x[P], most[P];
+                    Row::widen(w[i], x);
+                    // 1 + (x rounded down to 23 bits) <= 1 + w e^-s
 #pragma unroll
                     for (int e = 0; e < P; e += 2) {
                         const float2 z = halves_of(fma_pair(pair_of(x[e], x[e + 1]), c22, off2));
@@ -244,12 +248,12 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
                         most[e] = t.x;
                         most[e + 1] = t.y;
                     }
+                    const int32_t from = row.token(base + i * kRaceThreads);
                     uint64_t n = race.key + (uint64_t(int64_t(from >> 1)) + 1) * kGolden;  // of the pair that `from` lies in
-                    uint32_t mask = 0;
                     auto test = [&](int e, uint32_t r) {
-                        if (__uint_as_float(0x3f800000u | (r >> 9)) <= most[e]) mask |= 1u << e;
+                        if (__uint_as_float(0x3f800000u | (r >> 9)) <= most[e]) mask |= 1u << (i * P + e);
                     };
-                    if (from & 1) {
+                    if (row.lead & 1) {
                         uint64_t z = splitmix(n);
 #pragma unroll
                         for (int e = 0; e < P; e += 2) {
@@ -265,19 +269,20 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
                             test(e + 1, uint32_t(z >> 32));
                         }
                     }
-                    while (mask) {
-                        const int32_t v = from + __ffs(int(mask)) - 1;
-                        mask &= mask - 1;
-                        if (uint32_t(v) >= uint32_t(a.V)) continue;
-                        const int at = atomicAdd(&s_few, 1);
-                        if (at < kRaceList)
-                            s_tokens[at] = v;
-                        else
-                            best.consider(race, v, row[v], floor);
-                    }
                 }
-                base += kRaceThreads * F;
-                if (base < end) row.load(w, base, kRaceThreads, end);
+                while (mask) {
+                    const int at_mask = __ffs(int(mask)) - 1;
+                    mask &= mask - 1;
+                    const int32_t j = base + at_mask / P * kRaceThreads, v = row.token(j) + at_mask % P;
+                    if (j >= end || uint32_t(v) >= uint32_t(a.V)) continue;
+                    const int at = atomicAdd(&s_few, 1);
+                    if (at < kRaceList)
+                        s_tokens[at] = v;
+                    else
+                        best.consider(race, v, row[v], floor);
+                }
+#pragma unroll
+                for (int i = 0; i < F; ++i) w[i] = next[i];
             }
             // --- their scores -------------------------------------------------------------------------------------
             __syncthreads();

@@ -10,8 +10,10 @@
 // A CTA has two slots, each with four warps for 128 query rows (a thread a row), its scores S = Q K^T and its output
 // O = P V in tensor memory.  A tile of more than 128 rows has half of them in each slot, and both slots take every unit; a
 // smaller one is in both slots, which take units in turn and join at the end.  While one slot's warps turn scores into
-// weights, the tensor cores work for the other.  Further warps: one fetches tiles of keys and values through a ring (TMA,
-// 128-byte swizzle, a box a page), one issues the products, two look after the values' tiles.
+// weights, the tensor cores work for the other.  Further warps: one goes through the CTA's runs of units ahead of the others
+// and brings their queries, one fetches tiles of keys and values through a ring (TMA, 128-byte swizzle, a box a page), one
+// issues the products, one looks after the values' tiles.  So the next run's scores are computed while a slot's warps still
+// write the last one's output.
 //
 // Numbers.  The operands are the cache's and the queries' own numbers, products exact, S and O in binary32.  P takes S's
 // place in tensor memory, in the cache's type, since both operands of a product have one: weights are relative to a
@@ -37,8 +39,7 @@ constexpr int kSlotRows = 128;              // query rows of a slot: the MMA's M
 constexpr int kTileRows = 2 * kSlotRows;
 constexpr int kUnitKeys = 128;
 constexpr int kSlotThreads = kSlotRows, kSlotWarps = kSlotThreads / kWarp;
-constexpr int kValueWarps = 2;
-constexpr int kMmaWarp16 = 2 * kSlotWarps, kFetchWarp16 = kMmaWarp16 + 1, kFirstValueWarp = kFetchWarp16 + 1;
+constexpr int kMmaWarp16 = 2 * kSlotWarps, kFetchWarp16 = kMmaWarp16 + 1, kValueWarp16 = kMmaWarp16 + 2, kRunWarp = kMmaWarp16 + 3;
 constexpr int kThreads16 = (2 * kSlotWarps + 4) * kWarp;
 // Registers a thread of the two slots' warpgroups and of the third: 384 threads are launched with 168 each, and the shares
 // add up to the same.
@@ -46,6 +47,7 @@ constexpr int kSlotRegs = 208, kOtherRegs16 = 88;
 static_assert(2 * kSlotRegs + kOtherRegs16 == 3 * 168, "what two warpgroups gain the third gives");
 constexpr int kMaxCtas16 = 160;
 constexpr int kReady = 8;                   // units whose values are on their way, at most (a ring's tiles are fewer)
+constexpr int kRuns = 8;                    // runs between the first and the last of the warps, at most
 constexpr int kBlock16 = 128 * 128;         // 128 rows of one swizzle row: an operand's 64 elements
 constexpr int kColumns16 = 512;             // tensor memory: S 2 x 128, O 2 x 128
 // log2 of the weight of a score at the reference, and of one that is as large as can be without a new reference.
@@ -62,8 +64,9 @@ template <int D>
 struct Smem16 {
     static constexpr int kQ = (D / 64) * kBlock16;      // a slot's queries: [D / 64][128 rows][128 bytes]
     static constexpr int kTile = (D / 64) * kBlock16;   // 128 keys or values: [D / 64][128 tokens][128 bytes]
+    static constexpr int kQueries = D == 128 ? 2 : 4;   // slots' queries in shared memory
     static constexpr int kStages = D == 128 ? 5 : 10;
-    static constexpr int bytes = 1024 + 2 * kQ + kStages * kTile;
+    static constexpr int bytes = 1024 + kQueries * kQ + kStages * kTile;
 };
 
 // K-major operands (sw128_desc), and V: [D / 64][token][64], the contracted axis outermost; groups of eight tokens are 1024
@@ -139,6 +142,17 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, i
         : "memory");
 }
 
+__device__ __forceinline__ void cp_async16(void *dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;\n" ::: "memory"); }
+__device__ __forceinline__ void tmem_st2(uint32_t taddr, uint32_t a, uint32_t b) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\n" ::"r"(taddr), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void tmem_ld2(uint32_t taddr, uint32_t (&r)[2]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];\n" : "=r"(r[0]), "=r"(r[1]) : "r"(taddr));
+}
+
 // sum over i < n of floor((c + a i) / 128): the sum of the numbers less that of their remainders, which repeat.
 __device__ __forceinline__ int64_t sum_of_units(int64_t c, int32_t a, int64_t n) {
     const int32_t g = min(128, a & -a), period = 128 / g, some = int32_t(n % period);
@@ -195,8 +209,6 @@ struct Runs {
     __device__ bool next(const Attn16Args &a, Run &s) {
         if (!begun) {
             begun = true;
-            if (left == 0) return false;
-            row_lengths(a, b, len, nw);
             if (!take(a, s)) return false;
             s.part = 0;
             if (s.first == 0 || left == 0) return true;
@@ -211,121 +223,126 @@ struct Runs {
     }
 };
 
-// The CTA's range.  Also: statuses (CTA 0), zeros for the query rows of tokens that are not there, and the CTA's partial
-// results marked as none.  All threads call it.  s_pre: kThreads16 + 2 numbers.
+// n / d, n below 2^63: 32 bits where they are enough.
+__device__ __forceinline__ int64_t quotient(int64_t n, int64_t d) {
+    return ((n | d) >> 32) == 0 ? int64_t(uint32_t(n) / uint32_t(d)) : n / d;
+}
+
+// The CTA's range.  Also: statuses (CTA 0), and the CTA's partial results marked as none.  All threads call it.  s_pre:
+// kThreads16 + 2 numbers.
 __device__ __forceinline__ void deal_runs(const Attn16Args &a, int64_t *s_pre, Runs &runs) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, ctas = int(gridDim.x);
-    constexpr int kWarps = kThreads16 / kWarp;
     const int per = (a.B + kThreads16 - 1) / kThreads16;  // rows of a thread
     auto before_tile = [&](int32_t len, int32_t nw, int rt) -> int64_t {  // units of a key head's tiles before rt
         const int whole = nw / a.tokens;
         const int64_t c = int64_t(len) + a.tokens + kUnitKeys - 1;
-        return sum_of_units(c, a.tokens, min(rt, whole)) + (rt > whole ? (int64_t(len) + nw + kUnitKeys - 1) / kUnitKeys : 0);
+        return (whole && rt ? sum_of_units(c, a.tokens, min(rt, whole)) : 0) + (rt > whole ? (int64_t(len) + nw + kUnitKeys - 1) / kUnitKeys : 0);
     };
+    int32_t len = 0, nw = 0;
     auto units_of = [&](int row) -> int64_t {  // of a key head
-        int32_t len, nw;
         const bool ok = row_lengths(a, row, len, nw);
         if (a.status && cta == 0) a.status[row] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
         return nw ? before_tile(len, nw, (nw + a.tokens - 1) / a.tokens) : 0;
     };
-    int64_t mine = 0;
+    int64_t mine = 0, n = 0;
     for (int i = 0; i < per; ++i)
-        if (tid * per + i < a.B) mine += units_of(tid * per + i) * a.Hkv;
+        if (tid * per + i < a.B) mine += (n = units_of(tid * per + i)) * a.Hkv;
     int64_t x = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int64_t y = __shfl_up_sync(kFull, x, o);
         if (lane >= o) x += y;
     }
-    s_pre[tid + 1] = x;
+    if (lane == 31) s_pre[warp] = x;
     __syncthreads();
-    int64_t add = 0;
-    for (int w = 0; w < warp; ++w) add += s_pre[32 * w + 32];
-    __syncthreads();
-    s_pre[tid + 1] = x + add;
-    if (tid == 0) s_pre[0] = 0;
-    __syncthreads();
-    const int64_t total = s_pre[kThreads16];
-    const int64_t takers = min(total, int64_t(ctas));  // CTAs with a range: at least one unit each
-    const int64_t u = cta < takers ? total * cta / takers : total, u_end = cta < takers ? total * (cta + 1) / takers : total;
-    const int row16 = a.Hq * a.dim / 8;  // 16-byte pieces of a token's output
-    for (int64_t i = int64_t(warp) * ctas + cta; i < int64_t(a.B) * a.T; i += int64_t(ctas) * kWarps) {
-        int32_t len, nw;
-        row_lengths(a, int(i / a.T), len, nw);
-        if (int(i % a.T) < nw) continue;
-        uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(i) * row16;
-        for (int e = lane; e < row16; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
+    int64_t total = 0, before = x - mine;  // of all rows, of those before the thread's
+#pragma unroll
+    for (int w = 0; w < kThreads16 / kWarp; ++w) {
+        const int64_t y = s_pre[w];
+        total += y;
+        if (w < warp) before += y;
     }
+    const int64_t takers = min(total, int64_t(ctas));  // CTAs with a range: at least one unit each
+    const int64_t u = cta < takers ? quotient(total * cta, takers) : total, u_end = cta < takers ? quotient(total * (cta + 1), takers) : total;
     if (tid < 2) a.desc[2 * cta + tid] = make_int4(-1, 0, 0, 0);
-    const bool here = u < u_end && u >= s_pre[tid] && u < s_pre[tid + 1];
-    const int64_t at0 = s_pre[tid];
-    __syncthreads();
-    if (here) {
-        int64_t at = at0, n;
+    int64_t *s_at = s_pre + kThreads16 / kWarp;
+    if (u < u_end && u >= before && u < before + mine) {
+        int64_t at = before;
         int row = tid * per;
-        for (;; ++row) {
-            n = units_of(row);
-            if (u < at + n * a.Hkv) break;
-            at += n * a.Hkv;
-        }
-        int32_t len, nw;
-        row_lengths(a, row, len, nw);
-        const int64_t off = (u - at) % n;
+        if (per > 1)
+            for (;; ++row) {
+                n = units_of(row);
+                if (u < at + n * a.Hkv) break;
+                at += n * a.Hkv;
+            }
+        const int64_t hk = quotient(u - at, n), off = u - at - hk * n;
         int lo = 0, hi = (nw + a.tokens - 1) / a.tokens;  // the last tile with no more than `off` units before it
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
             (before_tile(len, nw, mid) <= off ? lo : hi) = mid;
         }
-        s_pre[0] = row;
-        s_pre[1] = (u - at) / n;
-        s_pre[2] = lo;
-        s_pre[3] = off - before_tile(len, nw, lo);
+        s_at[0] = row;
+        s_at[1] = hk;
+        s_at[2] = lo;
+        s_at[3] = off - before_tile(len, nw, lo);
+        s_at[4] = (int64_t(len) << 32) | nw;
     }
     __syncthreads();
-    runs.b = int(s_pre[0]);
-    runs.hk = int(s_pre[1]);
-    runs.rt = int(s_pre[2]);
-    runs.skip = int32_t(s_pre[3]);
+    runs.b = int(s_at[0]);
+    runs.hk = int(s_at[1]);
+    runs.rt = int(s_at[2]);
+    runs.skip = int32_t(s_at[3]);
+    runs.len = int32_t(s_at[4] >> 32);
+    runs.nw = int32_t(s_at[4]);
     runs.left = u < u_end ? u_end - u : 0;
     runs.begun = runs.held = false;
 }
-
-__device__ __forceinline__ void both_slots() { asm volatile("bar.sync 1, %0;\n" ::"n"(2 * kSlotThreads) : "memory"); }
 
 template <bool F16, int D>
 __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_constant__ CUtensorMap map, const Attn16Args a) {
     using S = Smem16<D>;
     constexpr int N = S::kStages, G = D / 64;
+    constexpr int NQ = S::kQueries;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full[2][kReady], empty[N], ready[kReady], s_full[2], p_full[2], o_done[2], q_full, stopped;
+    // A tile's arrival has a barrier by its unit and kind, not by its stage: a phase is then waited for by everyone who waits
+    // on that barrier at all, before its next one can begin.  (A stage has keys and values in turn, and who waits for the values
+    // only would take a phase of the keys that is still to come, or is over, for another.)
+    __shared__ __align__(8) uint64_t full[2][kReady], ready[kReady], empty[N], run_full[kRuns], q_ready[NQ], q_free[NQ], s_full[2], p_full[2], o_done[2], met, taken, written,
+        stopped;
     __shared__ __align__(16) uint32_t s_exist[kReady][4];  // of a unit: its keys that exist and whose page does
-    __shared__ uint32_t s_tmem, s_cleared[kReady];         // s_cleared: a run (+ 1) with values that were not finite, by the run
+    __shared__ __align__(16) int4 s_run[kRuns][3];
+    __shared__ uint32_t s_tmem, s_cleared[kRuns];          // s_cleared: a run (+ 1) with values that were not finite, by the run
     __shared__ int s_bad;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
     uint8_t *base = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
-    uint8_t *sm_q = base, *sm_kv = base + 2 * S::kQ;
-    float2 *s_ml = reinterpret_cast<float2 *>(sm_q + S::kQ);  // [2][128], of a tile that is in both slots: reference, sum
+    uint8_t *sm_q = base, *sm_kv = base + NQ * S::kQ;
 
     if (tid == 0) {
         for (int i = 0; i < N; ++i) mbar_init(&empty[i], 1);
-        // A tile's arrival has a barrier by its unit and kind, not by its stage: a phase is then waited for by everyone who waits
-        // on that barrier at all, before its next one can begin.  (A stage has keys and values in turn, and who waits for the values
-        // only would take a phase of the keys that is still to come, or is over, for another.)
         for (int i = 0; i < kReady; ++i) {
             mbar_init(&full[0][i], 1);
             mbar_init(&full[1][i], 1);
-            mbar_init(&ready[i], kValueWarps);
+            mbar_init(&ready[i], 1);
+        }
+        for (int i = 0; i < kRuns; ++i) {
+            mbar_init(&run_full[i], 1);
+            s_cleared[i] = 0;
+        }
+        for (int i = 0; i < NQ; ++i) {
+            mbar_init(&q_ready[i], 1);
+            mbar_init(&q_free[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&s_full[i], 2);  // the products, and the MMA thread: what it has seen of the other warps
+            mbar_init(&s_full[i], 2);  // the products, and the MMA warp: what it has seen of the other warps
             mbar_init(&o_done[i], 2);
             mbar_init(&p_full[i], kSlotWarps);
         }
-        mbar_init(&q_full, 2 * kSlotWarps);
+        mbar_init(&met, 2 * kSlotWarps);
+        mbar_init(&taken, 2 * kSlotWarps);
+        mbar_init(&written, 2 * kSlotWarps);
         mbar_init(&stopped, 1);
         fence_mbar_init();
         s_bad = 0;
-        for (int i = 0; i < kReady; ++i) s_cleared[i] = 0;
     }
     if (warp == kMmaWarp16) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_addr(&s_tmem)), "r"(kColumns16) : "memory");
@@ -340,10 +357,16 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
-    // Every wait of this thread has ended in time.  After one that has not, no further wait is begun and no result counts;
-    // the slots' warps still go through their loops, because their barriers want all of them.
-    bool ok = !a.give_up || warp == kFetchWarp16;
+    // Every wait of this warp has ended in time.  After one that has not, the warp goes to the end, and no result counts.
+    bool ok = !a.give_up || warp == kFetchWarp16 || warp == kRunWarp;
     Run s;
+    // The CTA's r-th run; n = 0: there are no more.
+    auto read_run = [&](uint32_t r) {
+        ok = ok && tc_wait_warp(&run_full[r % kRuns], (r / kRuns) & 1);
+        const int4 x = s_run[r % kRuns][0], y = s_run[r % kRuns][1], z = s_run[r % kRuns][2];
+        s = Run{x.x, x.y, x.z, y.x, y.y, y.z, y.w, z.x, z.y, z.z, x.w};
+        return ok && s.n > 0;
+    };
 
     if (warp < 2 * kSlotWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kSlotRegs));
@@ -353,32 +376,20 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
         const bool flip = a.scale < 0.f;
         // of a sum of products, for the binary logarithm; positive, so that what is masked stays -inf
         const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
-        uint32_t i = 0, done = 0, nrun = 0, unit0 = 0;  // this slot's units and runs so far, the CTA's runs and units
-        for (; runs.next(a, s); ++nrun, unit0 += uint32_t(s.n)) {
+        uint32_t i = 0, done = 0, splits = 0, unit0 = 0;  // this slot's units and runs so far, the CTA's runs in both slots and units
+        for (uint32_t nrun = 0; read_run(nrun); ++nrun, unit0 += uint32_t(s.n)) {
             const int rows = s.tokens * a.group;
             const bool split = rows <= kSlotRows;  // the tile is in both slots, which take units in turn
             const int row = split ? place : slot * kSlotRows + place, t = row / a.group, h = s.hk * a.group + row - t * a.group;
             const bool mine = row < rows, warp_mine = row - lane < rows;
             const int32_t limit = mine ? s.len + s.token0 + t : -1;
-            {
-                const uint16_t *q = a.q + s.b * a.qs[0] + int64_t(s.token0 + t) * a.qs[1] + int64_t(h) * a.qs[2];
-                uint8_t *dst = sm_q + (split ? 0 : slot * S::kQ) + place * 128;
-                const int c0 = split ? slot * (D / 16) : 0, c1 = split ? c0 + D / 16 : D / 8;
-#pragma unroll 8
-                for (int c = c0; c < c1; ++c) {
-                    const uint4 x = mine ? *reinterpret_cast<const uint4 *>(q + 8 * c) : make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4 *>(dst + (c / 8) * kBlock16 + (((c & 7) ^ (place & 7)) * 16)) = x;
-                }
-                fence_proxy_async();
-                tc_fence_before();
-                warp_arrive(&q_full);
-            }
             float ref = kFloor, l = 0.f;
             const int step = split ? 2 : 1, k0 = split ? slot : 0;
             const uint32_t out = lanes + 256 + uint32_t(slot * 128);
             for (int32_t k = k0; k < s.n; k += step, ++i) {
                 const int32_t key0 = (s.first + k) * kUnitKeys;
                 ok = ok && tc_wait_warp(&s_full[slot], i & 1);
+                if (!ok) break;
                 tc_fence_after();
                 if (warp_mine) {
                     float v[kUnitKeys];
@@ -399,10 +410,10 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                             for (int e = 0; e < 32; ++e) v[32 * w + e] = (see >> e) & 1 ? v[32 * w + e] : -INFINITY;
                         }
                     }
-                    float t4[4] = {v[0], v[1], v[2], v[3]};
+                    float top[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
 #pragma unroll
-                    for (int e = 4; e < kUnitKeys; e += 2) t4[(e >> 1) & 3] = max3(t4[(e >> 1) & 3], v[e], v[e + 1]);
-                    const float mx = fmaxf(max3(t4[0], t4[1], t4[2]), t4[3]) * scale;
+                    for (int e = 8; e < kUnitKeys; e += 2) top[(e >> 1) & 7] = max3(top[(e >> 1) & 7], v[e], v[e + 1]);
+                    const float mx = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), fmaxf(top[6], top[7])) * scale;
                     float corr = 1.f;
                     if (mx > ref + kLagUp<F16>) {
                         const float to = __fsub_ru(mx, kUp<F16>);  // (rounded up: f16 has no weights beyond 2^15)
@@ -447,21 +458,35 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 ok = ok && tc_wait_warp(&o_done[slot], done & 1);
                 ++done;
             }
+            if (!ok) break;
             tc_fence_after();
             float f = 1.f, f1 = 0.f;          // of this slot's output (or the first one's), and the second one's
             const bool two = split && s.n > 1;  // the second slot has an output too
-            if (split) {
-                s_ml[slot * kSlotRows + place] = make_float2(ref, l);
+            if (split) {  // references and sums change hands in the scores' place
+                if (warp_mine) {
+                    tmem_st2(scores, __float_as_uint(ref), __float_as_uint(l));
+                    tmem_wait_st();
+                }
                 tc_fence_before();
-                both_slots();
+                warp_arrive(&met);
+                ok = tc_wait_warp(&met, splits & 1);
+                ++splits;
+                if (!ok) break;
                 tc_fence_after();
-                const float2 x = s_ml[place], y = s_ml[kSlotRows + place];
-                both_slots();  // (the next queries may take the numbers' place)
-                ref = fmaxf(x.x, y.x);
-                f = exp2_approx(x.x - ref);
-                f1 = exp2_approx(y.x - ref);
-                l = x.y * f + y.y * f1;
+                if (warp_mine) {
+                    uint32_t other[2];
+                    tmem_ld2(lanes + uint32_t((1 - slot) * 128), other);
+                    tmem_wait_ld();
+                    const float its_ref = __uint_as_float(other[0]), its_l = __uint_as_float(other[1]);
+                    const float top = fmaxf(ref, its_ref), own = exp2_approx(ref - top), its = exp2_approx(its_ref - top);
+                    f = slot == 0 ? own : its;
+                    f1 = slot == 0 ? its : own;
+                    l = slot == 0 ? l * f + its_l * f1 : its_l * f + l * f1;  // (the same for both)
+                    ref = top;
+                }
+                tc_fence_before();
             }
+            warp_arrive(&taken);
             const bool whole = s.first == 0 && s.n == s.units;
             const float inv = l == 0.f ? 0.f : 1.f / l;
             if (warp_mine) {
@@ -469,8 +494,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 const int part = 2 * cta + s.part, d0 = split ? slot * (D / 2) : 0, d1 = split ? d0 + D / 2 : D;
                 float *partial = a.part + (size_t(part) * kTileRows + row) * (D + 4);
                 uint16_t *result = a.out + ((size_t(s.b) * a.T + s.token0 + t) * a.Hq + h) * D;
-                const int32_t cleared = s_cleared[nrun % kReady] == nrun + 1 ? min(limit + 1, (s.first + s.n) * kUnitKeys) : 0;
-#pragma unroll 1
+                const int32_t cleared = s_cleared[nrun % kRuns] == nrun + 1 ? min(limit + 1, (s.first + s.n) * kUnitKeys) : 0;
+#pragma unroll 2
                 for (int d = d0; d < d1; d += 16) {
                     float v[16];
                     uint32_t w[16];
@@ -512,6 +537,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                     if (tid == 0) a.desc[part] = make_int4(s.b, s.hk, s.rt, (s.first == 0 ? kFirst : 0) | (s.first + s.n == s.units ? kLast : 0));
                 }
             }
+            tc_fence_before();
+            warp_arrive(&written);
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kOtherRegs16));
@@ -521,7 +548,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
             const int run = min(kUnitKeys, 1 << a.page_shift), nruns = kUnitKeys / run, page_mask = (1 << a.page_shift) - 1;
             const int q = lane / G, g = lane - G * q;
             uint32_t unit = 0, issued = 0;  // units, tiles
-            while (ok && runs.next(a, s)) {
+            for (uint32_t nrun = 0; read_run(nrun); ++nrun) {
                 auto find = [&](int32_t k) {  // the page of this lane's tokens in unit k of the run
                     const int32_t key = (s.first + k) * kUnitKeys + q * run;
                     return q < nruns && k < s.n && key < s.keys ? __ldcg(a.table + size_t(s.b) * a.blocks + (key >> a.page_shift)) : -1;
@@ -559,16 +586,16 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
             for (uint32_t x = issued > N ? issued - N : 0; x < issued; ++x) (void)tc_wait(&full[x & 1][x / 2 % kReady], (x / 2 / kReady) & 1);
         } else if (warp == kMmaWarp16) {
             // --------------------------------------------------------------------------------------- the products
-            uint32_t unit0 = 0, nrun = 0, weights[2] = {0, 0};  // units and runs so far, units whose weights a slot's product took
+            uint32_t unit0 = 0, qx = 0, weights[2] = {0, 0};  // units and slots' queries so far, units whose weights a slot's product took
             const uint32_t leader = elect_leader(), tm = __shfl_sync(kFull, tmem, 0);
             const uint64_t dq0 = sw128_desc(smem_addr(sm_q)), dk0 = sw128_desc(smem_addr(sm_kv)), dv0 = value_desc(smem_addr(sm_kv));
             auto stage_of = [&](uint32_t x) { return uint64_t(x % N) * (S::kTile >> 4); };
-            auto score = [&](int slot, bool split, uint32_t unit) {  // S = Q K^T
+            auto score = [&](int slot, uint32_t query, uint32_t unit) {  // S = Q K^T
                 ok = ok && tc_wait_warp(&full[0][unit % kReady], (unit / kReady) & 1);
                 if (!ok) return;
                 lead_arrive(leader, &s_full[slot]);
                 tc_fence_after();
-                const uint64_t dq = dq0 + (split ? 0 : uint64_t(slot) * (S::kQ >> 4)), dk = dk0 + stage_of(2 * unit);
+                const uint64_t dq = dq0 + uint64_t(query % NQ) * (S::kQ >> 4), dk = dk0 + stage_of(2 * unit);
 #pragma unroll
                 for (int e = 0; e < D / 16; ++e) {
                     const uint64_t step = uint64_t(((e >> 2) * kBlock16 + (e & 3) * 32) >> 4);
@@ -594,49 +621,44 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 lead_arrive(leader, &o_done[slot]);
                 lead_commit(leader, &o_done[slot]);
             };
-            while (ok && __any_sync(kFull, runs.next(a, s))) {
+            for (uint32_t nrun = 0; __any_sync(kFull, read_run(nrun)); ++nrun) {
                 const bool split = __any_sync(kFull, s.tokens * a.group <= kSlotRows);
-                s.n = __shfl_sync(kFull, s.n, 0);
-                ok = tc_wait_warp(&q_full, nrun & 1);  // (the rows' threads write the queries when they have read the last O)
-                if (split) {
-                    for (int32_t k = 0; ok && k < s.n + 2; ++k) {
-                        const int slot = k & 1;
-                        if (k >= 2) {
-                            product(slot, unit0 + k - 2, k < 4);
-                            release(2 * (unit0 + k - 2) + 1);
-                            if (k >= s.n) finish(slot);
+                const int32_t n = __shfl_sync(kFull, s.n, 0);
+                const uint32_t q0 = qx, q1 = split ? qx : qx + 1;
+                qx = q1 + 1;
+                ok = tc_wait_warp(&q_ready[q0 % NQ], (q0 / NQ) & 1) && (split || tc_wait_warp(&q_ready[q1 % NQ], (q1 / NQ) & 1));
+                if (nrun > 0) ok = ok && tc_wait_warp(&taken, (nrun - 1) & 1);  // the scores' place
+                const int step = split ? 2 : 1;
+                for (int32_t k = 0; ok && k < n + step; ++k) {
+                    if (k == step && nrun > 0) ok = tc_wait_warp(&written, (nrun - 1) & 1);  // the outputs' place
+#pragma unroll
+                    for (int slot = 0; slot < 2; ++slot) {
+                        if (split && slot != (k & 1)) continue;
+                        const bool frees = split || slot == 1;  // the last to use the unit's tiles
+                        if (k >= step) {
+                            product(slot, unit0 + k - step, k - step < step);
+                            if (frees) release(2 * (unit0 + k - step) + 1);
+                            if (k >= n) finish(slot);
                         }
-                        if (k < s.n) {
-                            score(slot, true, unit0 + k);
-                            release(2 * (unit0 + k));
+                        if (k < n) {
+                            score(slot, slot ? q1 : q0, unit0 + k);
+                            if (frees) release(2 * (unit0 + k));
+                            if (frees && k == n - 1 && ok) {
+                                lead_commit(leader, &q_free[q0 % NQ]);
+                                if (!split) lead_commit(leader, &q_free[q1 % NQ]);
+                            }
                         }
                     }
-                } else {
-                    for (int32_t k = 0; ok && k <= s.n; ++k)
-#pragma unroll
-                        for (int slot = 0; slot < 2; ++slot) {
-                            if (k > 0) {
-                                product(slot, unit0 + k - 1, k == 1);
-                                if (slot == 1) release(2 * (unit0 + k - 1) + 1);
-                                if (k == s.n) finish(slot);
-                            }
-                            if (k < s.n) {
-                                score(slot, false, unit0 + k);
-                                if (slot == 1) release(2 * (unit0 + k));
-                            }
-                        }
                 }
-                unit0 += uint32_t(s.n);
-                ++nrun;
+                unit0 += uint32_t(n);
             }
             // what is in flight reads shared and tensor memory (the rows' threads wait for the last product too, unless they gave up)
             lead_commit(leader, &stopped);
             (void)tc_wait(&stopped, 0);
-        } else if (warp >= kFirstValueWarp) {
+        } else if (warp == kValueWarp16) {
             // --------------------------------------------------------------------------------------- values that not every row sees
-            const int first_place = (warp - kFirstValueWarp) * (kUnitKeys / kValueWarps) + lane;
             uint32_t unit = 0;
-            for (uint32_t nrun = 0; ok && runs.next(a, s); ++nrun) {
+            for (uint32_t nrun = 0; read_run(nrun); ++nrun) {
                 const int32_t all_see = s.len + s.token0;  // the last key that all rows see
                 for (int32_t k = 0; ok && k < s.n; ++k, ++unit) {
                     const uint32_t st = (2 * unit + 1) % N;
@@ -647,7 +669,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                     if (key0 + kUnitKeys > all_see + 1 || (there.x & there.y & there.z & there.w) != 0xffffffffu) {
                         bool found = false;
 #pragma unroll 1
-                        for (int at = first_place; at < first_place + kUnitKeys / kValueWarps; at += kWarp) {
+                        for (int at = lane; at < kUnitKeys; at += kWarp) {
                             uint8_t *line = sm_kv + st * S::kTile + at * 128;
                             const bool gone = !((s_exist[unit % kReady][at / 32] >> (at & 31)) & 1);
                             if (!gone && key0 + at <= all_see) continue;
@@ -671,10 +693,42 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                                 *piece = v;
                             }
                         }
-                        if (found) s_cleared[nrun % kReady] = nrun + 1;
+                        if (found) s_cleared[nrun % kRuns] = nrun + 1;
                         fence_proxy_async();
                     }
                     warp_arrive(&ready[unit % kReady]);
+                }
+            }
+        } else {
+            // --------------------------------------------------------------------------------------- runs, and their queries
+            uint32_t qx = 0;
+            for (uint32_t nrun = 0;; ++nrun) {
+                const bool more = ok && runs.next(a, s);
+                if (lane == 0) {
+                    s_run[nrun % kRuns][0] = make_int4(s.b, s.hk, s.rt, s.part);
+                    s_run[nrun % kRuns][1] = make_int4(s.len, s.token0, s.tokens, s.keys);
+                    s_run[nrun % kRuns][2] = make_int4(s.first, more ? s.n : 0, s.units, 0);
+                    mbar_arrive(&run_full[nrun % kRuns]);
+                }
+                if (!more) break;
+                const int rows = s.tokens * a.group;
+                const uint32_t end = qx + (rows <= kSlotRows ? 1 : 2);
+                const uint16_t *q = a.q + s.b * a.qs[0] + s.token0 * a.qs[1] + int64_t(s.hk) * a.group * a.qs[2];
+                for (int row0 = 0; qx < end; ++qx, row0 += kSlotRows) {
+                    if (qx >= NQ) ok = ok && tc_wait_warp(&q_free[qx % NQ], (qx / NQ - 1) & 1);
+                    if (!ok) break;
+                    constexpr int kVec = D / 8, kStep = kWarp / kVec;  // vectors of a row, rows of a pass
+                    const int c = lane % kVec, last = min(rows - row0, kSlotRows);
+                    int row = lane / kVec, t = (row0 + row) / a.group, g = row0 + row - t * a.group;
+                    uint8_t *dst = sm_q + (qx % NQ) * S::kQ + (c / 8) * kBlock16;
+#pragma unroll 4
+                    for (; row < last; row += kStep) {
+                        cp_async16(dst + row * 128 + (((c & 7) ^ (row & 7)) * 16), q + t * a.qs[1] + g * a.qs[2] + 8 * c);
+                        for (g += kStep; g >= a.group; g -= a.group) ++t;
+                    }
+                    cp_async_wait();
+                    fence_proxy_async();
+                    warp_arrive(&q_ready[qx % NQ]);
                 }
             }
         }
@@ -688,7 +742,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     if (s_bad && tid == 0) a.desc[2 * cta].w |= kLate;  // (the thread that wrote it; the join writes the statuses)
 }
 
-// Joins the partial results of the items that several CTAs hold, and writes the statuses of a launch that a CTA gave up:
+// Joins the partial results of the items that several CTAs hold, and writes the zeros of tokens that are not there and the
+// statuses of a launch that a CTA gave up:
 // CTAs (i, .) look after the item whose first part is the i-th CTA's, a CTA a query row and a thread a dimension, adding
 // the parts in order, kJoinParts on their way together.
 template <bool F16, int D>
@@ -696,6 +751,20 @@ __global__ void __launch_bounds__(D, 2048 / D) attn16_join_kernel(const Attn16Ar
     const int i = blockIdx.x, d = threadIdx.x, lane = threadIdx.x & 31, ctas = int(gridDim.x);
     pdl_wait();
     pdl_trigger();
+    {  // zeros for the tokens that are not there: a warp looks at 32 tokens together, and fills a part of each, 512 bytes or more
+        const uint32_t warps = gridDim.x * gridDim.y * (D / kWarp), all = uint32_t(a.B) * uint32_t(a.T);  // (below 2^31)
+        const uint32_t groups = (all + kWarp - 1) / kWarp, row16 = uint32_t(a.Hq) * (D / 8);               // 16-byte pieces of a token's output
+        const uint32_t cuts = max(1u, min(warps / groups, row16 / kWarp)), cut = (row16 + cuts - 1) / cuts;
+        for (uint32_t w = (blockIdx.y * gridDim.x + i) * (D / kWarp) + d / kWarp; w < groups * cuts; w += warps) {
+            const uint32_t j0 = w / cuts * kWarp, j = j0 + lane, b = j / uint32_t(a.T), e0 = w % cuts * cut, e1 = min(e0 + cut, row16);
+            int32_t len, nw = a.T;
+            if (j < all) row_lengths(a, int(b), len, nw);
+            for (uint32_t gone = __ballot_sync(kFull, int(j - b * a.T) >= nw); gone; gone &= gone - 1) {
+                uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(j0 + __ffs(int(gone)) - 1) * row16;
+                for (uint32_t e = e0 + lane; e < e1; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
     int from = 2 * i + 1;
     int4 de = __ldcg(a.desc + from);
     const int4 other = __ldcg(a.desc + 2 * i);

@@ -162,21 +162,30 @@ __device__ __forceinline__ int64_t sum_of_units(int64_t c, int32_t a, int64_t n)
     return (n * c + a * (n * (n - 1) / 2) - rest) >> 7;
 }
 
+// n / d, n below 2^63: 32 bits where they are enough.
+__device__ __forceinline__ int64_t quotient(int64_t n, int64_t d) {
+    return ((n | d) >> 32) == 0 ? int64_t(uint32_t(n) / uint32_t(d)) : n / d;
+}
+
 // A run of units of one item.
 struct Run {
     int b, hk, rt;
     int32_t len, token0, tokens, keys;  // of the tile: its first token, tokens, and keys that its last one sees
     int32_t first, n, units, part;      // part: which of the CTA's two partial results it may leave
+    int32_t parts;                      // CTAs that hold units of the item
 };
 // The runs of a CTA's range, in order, but that one which begins inside an item comes last: the CTAs that share an item's
 // keys then go through them side by side, and what one has fetched the others find in L2.
 struct Runs {
+    int64_t u, total;    // units before the next run's first, in all
+    int32_t takers;
     int b, hk, rt;
     int32_t skip;        // of the first item: units before the range
     int64_t left;        // units
     int32_t len, nw;     // of row b
     bool begun, held;
     Run late;
+    __device__ int holder(int64_t unit) const { return int(quotient((unit + 1) * takers - 1, total)); }  // the CTA whose range has a unit
     __device__ bool take(const Attn16Args &a, Run &s) {
         while (left > 0) {
             const int tiles = (nw + a.tokens - 1) / a.tokens;
@@ -200,6 +209,9 @@ struct Runs {
             s.first = skip;
             s.n = int32_t(min(int64_t(s.units - skip), left));
             s.part = 1;
+            // CTAs that hold units of the item
+            s.parts = holder(u - s.first + s.units - 1) - holder(u - s.first) + 1;
+            u += s.n;
             skip = 0;
             left -= s.n;
             return true;
@@ -222,11 +234,6 @@ struct Runs {
         return true;
     }
 };
-
-// n / d, n below 2^63: 32 bits where they are enough.
-__device__ __forceinline__ int64_t quotient(int64_t n, int64_t d) {
-    return ((n | d) >> 32) == 0 ? int64_t(uint32_t(n) / uint32_t(d)) : n / d;
-}
 
 // The CTA's range.  Also: statuses (CTA 0), and the CTA's partial results marked as none.  All threads call it.  s_pre:
 // kThreads16 + 2 numbers.
@@ -295,6 +302,9 @@ __device__ __forceinline__ void deal_runs(const Attn16Args &a, int64_t *s_pre, R
     runs.len = int32_t(s_at[4] >> 32);
     runs.nw = int32_t(s_at[4]);
     runs.left = u < u_end ? u_end - u : 0;
+    runs.u = u;
+    runs.total = total;
+    runs.takers = int32_t(takers);
     runs.begun = runs.held = false;
 }
 
@@ -307,7 +317,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     // A tile's arrival has a barrier by its unit and kind, not by its stage: a phase is then waited for by everyone who waits
     // on that barrier at all, before its next one can begin.  (A stage has keys and values in turn, and who waits for the values
     // only would take a phase of the keys that is still to come, or is over, for another.)
-    __shared__ __align__(8) uint64_t full[2][kReady], ready[kReady], empty[N], run_full[kRuns], q_ready[NQ], q_free[NQ], s_full[2], p_full[2], o_done[2], met, taken, written,
+    __shared__ __align__(8) uint64_t full[2][kReady], ready[kReady], empty[N], run_full[kRuns], q_ready[NQ], q_free[NQ], s_full[2], p_half[2], p_full[2], o_done[2], met, taken, written,
         stopped;
     __shared__ __align__(16) uint32_t s_exist[kReady][4];  // of a unit: its keys that exist and whose page does
     __shared__ __align__(16) int4 s_run[kRuns][3];
@@ -335,6 +345,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s_full[i], 2);  // the products, and the MMA warp: what it has seen of the other warps
             mbar_init(&o_done[i], 2);
+            mbar_init(&p_half[i], kSlotWarps);
             mbar_init(&p_full[i], kSlotWarps);
         }
         mbar_init(&met, 2 * kSlotWarps);
@@ -364,7 +375,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     auto read_run = [&](uint32_t r) {
         ok = ok && tc_wait_warp(&run_full[r % kRuns], (r / kRuns) & 1);
         const int4 x = s_run[r % kRuns][0], y = s_run[r % kRuns][1], z = s_run[r % kRuns][2];
-        s = Run{x.x, x.y, x.z, y.x, y.y, y.z, y.w, z.x, z.y, z.z, x.w};
+        s = Run{x.x, x.y, x.z, y.x, y.y, y.z, y.w, z.x, z.y, z.z, x.w, z.w};
         return ok && s.n > 0;
     };
 
@@ -445,10 +456,17 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                             y[e] = narrow2<F16>(p0, p1);
                         }
                         tmem_st16(scores + 16 * w, y);
+                        if (w == 1) {  // the product of the first half may begin
+                            tmem_wait_st();
+                            tc_fence_before();
+                            warp_arrive(&p_half[slot]);
+                        }
                     }
                     const float2 both = halves_of(add_pair(sum[0], sum[1]));
                     l += both.x + both.y;
                     tmem_wait_st();
+                } else {
+                    warp_arrive(&p_half[slot]);
                 }
                 tc_fence_before();
                 warp_arrive(&p_full[slot]);
@@ -495,7 +513,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 float *partial = a.part + (size_t(part) * kTileRows + row) * (D + 4);
                 uint16_t *result = a.out + ((size_t(s.b) * a.T + s.token0 + t) * a.Hq + h) * D;
                 const int32_t cleared = s_cleared[nrun % kRuns] == nrun + 1 ? min(limit + 1, (s.first + s.n) * kUnitKeys) : 0;
-#pragma unroll 2
+#pragma unroll 4
                 for (int d = d0; d < d1; d += 16) {
                     float v[16];
                     uint32_t w[16];
@@ -534,7 +552,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 if (!whole && mine && d0 == 0) {
                     partial[D] = ref;
                     partial[D + 1] = l;
-                    if (tid == 0) a.desc[part] = make_int4(s.b, s.hk, s.rt, (s.first == 0 ? kFirst : 0) | (s.first + s.n == s.units ? kLast : 0));
+                    if (tid == 0) a.desc[part] = make_int4(s.b, s.hk, s.token0, (s.first == 0 ? kFirst : 0) | (rows << 3) | (s.parts << 16));
                 }
             }
             tc_fence_before();
@@ -603,15 +621,19 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 }
                 lead_commit(leader, &s_full[slot]);
             };
-            auto product = [&](int slot, uint32_t unit, bool fresh) {  // O += P V
-                ok = ok && tc_wait_warp(&p_full[slot], weights[slot] & 1) && tc_wait_warp(&ready[unit % kReady], (unit / kReady) & 1);
-                if (!ok) return;
-                ++weights[slot];
-                tc_fence_after();
+            auto product = [&](int slot, uint32_t unit, bool fresh) {  // O += P V, half of the keys as soon as their weights are there
+                ok = ok && tc_wait_warp(&ready[unit % kReady], (unit / kReady) & 1);
                 const uint64_t dv = dv0 + stage_of(2 * unit + 1);
 #pragma unroll
-                for (int e = 0; e < kUnitKeys / 16; ++e)
-                    lead_mma_ts(leader, tm + 256 + slot * 128, tm + slot * 128 + 8 * e, dv + uint64_t((e * 16 * 128) >> 4), idesc16<F16>(D, true), !fresh || e != 0);
+                for (int half = 0; half < 2; ++half) {
+                    ok = ok && tc_wait_warp(half ? &p_full[slot] : &p_half[slot], weights[slot] & 1);
+                    if (!ok) return;
+                    tc_fence_after();
+#pragma unroll
+                    for (int e = half * (kUnitKeys / 32); e < (half + 1) * (kUnitKeys / 32); ++e)
+                        lead_mma_ts(leader, tm + 256 + slot * 128, tm + slot * 128 + 8 * e, dv + uint64_t((e * 16 * 128) >> 4), idesc16<F16>(D, true), !fresh || e != 0);
+                }
+                ++weights[slot];
             };
             auto release = [&](uint32_t x) {
                 if (ok) lead_commit(leader, &empty[x % N]);
@@ -707,7 +729,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 if (lane == 0) {
                     s_run[nrun % kRuns][0] = make_int4(s.b, s.hk, s.rt, s.part);
                     s_run[nrun % kRuns][1] = make_int4(s.len, s.token0, s.tokens, s.keys);
-                    s_run[nrun % kRuns][2] = make_int4(s.first, more ? s.n : 0, s.units, 0);
+                    s_run[nrun % kRuns][2] = make_int4(s.first, more ? s.n : 0, s.units, s.parts);
                     mbar_arrive(&run_full[nrun % kRuns]);
                 }
                 if (!more) break;
@@ -743,82 +765,81 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
 }
 
 // Joins the partial results of the items that several CTAs hold, and writes the zeros of tokens that are not there and the
-// statuses of a launch that a CTA gave up:
-// CTAs (i, .) look after the item whose first part is the i-th CTA's, a CTA a query row and a thread a dimension, adding
-// the parts in order, kJoinParts on their way together.
+// statuses of a launch that a CTA gave up: CTAs (i, .) look after the item whose first part is the i-th CTA's, a warp a query
+// row, adding the parts in order, kJoinFlight on their way together.
+constexpr int kJoinWarps16 = 8, kJoinFlight = 8;
 template <bool F16, int D>
-__global__ void __launch_bounds__(D, 2048 / D) attn16_join_kernel(const Attn16Args a) {
-    const int i = blockIdx.x, d = threadIdx.x, lane = threadIdx.x & 31, ctas = int(gridDim.x);
+__global__ void __launch_bounds__(kJoinWarps16 *kWarp, 3) attn16_join_kernel(const Attn16Args a) {
+    constexpr int E = D / kWarp;  // dimensions of a lane
+    using Part = typename std::conditional<E == 4, float4, float2>::type;
+    const int i = blockIdx.x, lane = threadIdx.x & 31, warp = int(blockIdx.y) * kJoinWarps16 + (threadIdx.x >> 5), warps = int(gridDim.y) * kJoinWarps16;
     pdl_wait();
     pdl_trigger();
-    {  // zeros for the tokens that are not there: a warp looks at 32 tokens together, and fills a part of each, 512 bytes or more
-        const uint32_t warps = gridDim.x * gridDim.y * (D / kWarp), all = uint32_t(a.B) * uint32_t(a.T);  // (below 2^31)
-        const uint32_t groups = (all + kWarp - 1) / kWarp, row16 = uint32_t(a.Hq) * (D / 8);               // 16-byte pieces of a token's output
-        const uint32_t cuts = max(1u, min(warps / groups, row16 / kWarp)), cut = (row16 + cuts - 1) / cuts;
-        for (uint32_t w = (blockIdx.y * gridDim.x + i) * (D / kWarp) + d / kWarp; w < groups * cuts; w += warps) {
-            const uint32_t j0 = w / cuts * kWarp, j = j0 + lane, b = j / uint32_t(a.T), e0 = w % cuts * cut, e1 = min(e0 + cut, row16);
-            int32_t len, nw = a.T;
-            if (j < all) row_lengths(a, int(b), len, nw);
-            for (uint32_t gone = __ballot_sync(kFull, int(j - b * a.T) >= nw); gone; gone &= gone - 1) {
-                uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(j0 + __ffs(int(gone)) - 1) * row16;
-                for (uint32_t e = e0 + lane; e < e1; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
-            }
-        }
-    }
-    int from = 2 * i + 1;
-    int4 de = __ldcg(a.desc + from);
-    const int4 other = __ldcg(a.desc + 2 * i);
-    if ((other.w & kLate) && blockIdx.y == 0 && a.status)
-        for (int b = d; b < a.B; b += D) a.status[b] = SWITCHSD_ROW_TIMEOUT;
-    if (de.x < 0 || !(de.w & kFirst)) {
-        from = 2 * i;
-        de = other;
-        if (de.x < 0 || !(de.w & kFirst)) return;
-    }
-    int n = 1;  // partial results of the item: this CTA's and the next ones' first, up to the one that holds the last unit
-    for (int c0 = i + 1; !(de.w & kLast);) {
-        const int c = c0 + lane;
-        const uint32_t last = __ballot_sync(kFull, c >= ctas || (__ldcg(&a.desc[2 * min(c, ctas - 1)].w) & kLast));
-        if (last) {
-            n = min(c0 + __ffs(int(last)), ctas) - i;
-            break;
-        }
-        c0 += 32;
-    }
-    int32_t len, nw;
-    row_lengths(a, de.x, len, nw);
-    const int token0 = de.z * a.tokens, rows = min(a.tokens, nw - token0) * a.group;
-    for (int row = int(blockIdx.y); row < rows; row += int(gridDim.y)) {
-        float mx = kFloor, sum = 0.f, y = 0.f;
-        for (int j0 = 0; j0 < n; j0 += kJoinParts) {
-            float pm[kJoinParts], ps[kJoinParts], py[kJoinParts], top = mx;
+    // the item's first part is the CTA's second partial result, or its first one
+    const int4 first = __ldcg(a.desc + 2 * i), second = __ldcg(a.desc + 2 * i + 1);
+    if ((first.w & kLate) && blockIdx.y == 0 && a.status)
+        for (int b = threadIdx.x; b < a.B; b += kJoinWarps16 * kWarp) a.status[b] = SWITCHSD_ROW_TIMEOUT;  // some row is not done; which ones, the CTA does not know
+    const bool is_second = second.x >= 0 && (second.w & kFirst);
+    const int4 de = is_second ? second : first;
+    if (de.x >= 0 && (de.w & kFirst)) {
+        const int n = de.w >> 16, rows = (de.w >> 3) & 0x1fff, from = 2 * i + is_second;
+        for (int row = warp; row < rows; row += warps) {
+            float mx = kFloor, sum = 0.f, y[E];
 #pragma unroll
-            for (int j = 0; j < kJoinParts; ++j) {
-                pm[j] = kFloor;
-                ps[j] = py[j] = 0.f;
-                if (j0 + j < n) {
-                    const float *src = a.part + (size_t(j0 + j ? 2 * (i + j0 + j) : from) * kTileRows + row) * (D + 4);
-                    pm[j] = __ldcg(src + D);
-                    ps[j] = __ldcg(src + D + 1);
-                    py[j] = __ldcg(src + d);
+            for (int e = 0; e < E; ++e) y[e] = 0.f;
+            for (int j0 = 0; j0 < n; j0 += kJoinFlight) {
+                float pm[kJoinFlight], ps[kJoinFlight], top = mx;
+                Part py[kJoinFlight];
+#pragma unroll
+                for (int j = 0; j < kJoinFlight; ++j) {
+                    pm[j] = kFloor;
+                    ps[j] = 0.f;
+                    py[j] = Part{};
+                    if (j0 + j < n) {
+                        const float *src = a.part + (size_t(j0 + j ? 2 * (i + j0 + j) : from) * kTileRows + row) * (D + 4);
+                        const float2 ms = __ldcg(reinterpret_cast<const float2 *>(src + D));
+                        pm[j] = ms.x;
+                        ps[j] = ms.y;
+                        py[j] = __ldcg(reinterpret_cast<const Part *>(src) + lane);
+                    }
                 }
-            }
 #pragma unroll
-            for (int j = 0; j < kJoinParts; ++j) top = fmaxf(top, pm[j]);
-            const float f0 = exp2_approx(mx - top);
-            y *= f0;
-            sum *= f0;
+                for (int j = 0; j < kJoinFlight; ++j) top = fmaxf(top, pm[j]);
+                const float f0 = exp2_approx(mx - top);
+                sum *= f0;
 #pragma unroll
-            for (int j = 0; j < kJoinParts; ++j) {
-                const float f = exp2_approx(pm[j] - top);
-                y = fmaf(py[j], f, y);
-                sum = fmaf(ps[j], f, sum);
+                for (int e = 0; e < E; ++e) y[e] *= f0;
+#pragma unroll
+                for (int j = 0; j < kJoinFlight; ++j) {
+                    const float f = exp2_approx(pm[j] - top);
+                    sum = fmaf(ps[j], f, sum);
+                    const float *p = reinterpret_cast<const float *>(&py[j]);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) y[e] = fmaf(p[e], f, y[e]);
+                }
+                mx = top;
             }
-            mx = top;
+            const int t = de.z + row / a.group, h = de.y * a.group + row % a.group;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            uint32_t *out = reinterpret_cast<uint32_t *>(a.out + ((size_t(de.x) * a.T + t) * a.Hq + h) * D) + lane * (E / 2);
+            if constexpr (E == 4)
+                *reinterpret_cast<uint2 *>(out) = make_uint2(narrow2<F16>(y[0] * inv, y[1] * inv), narrow2<F16>(y[2] * inv, y[3] * inv));
+            else
+                *out = narrow2<F16>(y[0] * inv, y[1] * inv);
         }
-        const int t = token0 + row / a.group, h = de.y * a.group + row % a.group;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        a.out[((size_t(de.x) * a.T + t) * a.Hq + h) * D + d] = narrow1<F16>(y * inv);
+    }
+    // zeros for the tokens that are not there: a warp looks at 32 tokens together, and fills a part of each, 512 bytes or more
+    const uint32_t all_warps = gridDim.x * warps, all = uint32_t(a.B) * uint32_t(a.T);                          // (below 2^31)
+    const uint32_t groups = (all + kWarp - 1) / kWarp, row16 = uint32_t(a.Hq) * (D / 8);                      // 16-byte pieces of a token's output
+    const uint32_t cuts = max(1u, min(all_warps / groups, row16 / kWarp)), cut = (row16 + cuts - 1) / cuts;
+    for (uint32_t w = uint32_t(i) * warps + warp; w < groups * cuts; w += all_warps) {
+        const uint32_t j0 = w / cuts * kWarp, j = j0 + lane, b = j / uint32_t(a.T), e0 = w % cuts * cut, e1 = min(e0 + cut, row16);
+        int32_t len, nw = a.T;
+        if (j < all) row_lengths(a, int(b), len, nw);
+        for (uint32_t gone = __ballot_sync(kFull, int(j - b * a.T) >= nw); gone; gone &= gone - 1) {
+            uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(j0 + __ffs(int(gone)) - 1) * row16;
+            for (uint32_t e = e0 + lane; e < e1; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
+        }
     }
 }
 
@@ -861,8 +882,8 @@ static cudaError_t launch16(const CUtensorMap &map, const Attn16Args &a, cudaStr
     // an explicit one-CTA cluster: the MMA commit addresses shared::cluster
     e = launch_pdl(attn16_kernel<F16, D>, dim3(ctas), dim3(kThreads16), size_t(Smem16<D>::bytes), s, 1u, map, a);
     if (e != cudaSuccess) return e;
-    const unsigned y = unsigned(std::min(int64_t(32), std::min(int64_t(a.tokens), int64_t(a.T)) * a.group));
-    return launch_pdl(attn16_join_kernel<F16, D>, dim3(ctas, y), dim3(D), 0, s, 0u, a);
+    const int64_t rows = std::min(int64_t(a.tokens), int64_t(a.T)) * a.group;
+    return launch_pdl(attn16_join_kernel<F16, D>, dim3(ctas, unsigned((rows + kJoinWarps16 - 1) / kJoinWarps16)), dim3(kJoinWarps16 * kWarp), 0, s, 0u, a);
 }
 
 }  // namespace switchsd

@@ -39,7 +39,7 @@ constexpr int kSlotRows = 128;              // query rows of a slot: the MMA's M
 constexpr int kTileRows = 2 * kSlotRows;
 constexpr int kUnitKeys = 128;
 constexpr int kSlotThreads = kSlotRows, kSlotWarps = kSlotThreads / kWarp;
-constexpr int kMmaWarp16 = 2 * kSlotWarps, kFetchWarp16 = kMmaWarp16 + 1, kValueWarp16 = kMmaWarp16 + 2, kRunWarp = kMmaWarp16 + 3;
+constexpr int kMmaWarp16 = 0, kFetchWarp16 = 1, kValueWarp16 = 2, kRunWarp = 3, kFirstSlotWarp = 4;
 constexpr int kThreads16 = (2 * kSlotWarps + 4) * kWarp;
 // Registers a thread of the two slots' warpgroups and of the third: 384 threads are launched with 168 each, and the shares
 // add up to the same.
@@ -379,10 +379,10 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
         return ok && s.n > 0;
     };
 
-    if (warp < 2 * kSlotWarps) {
+    if (warp >= kFirstSlotWarp) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kSlotRegs));
         // ------------------------------------------------------------------------------------------- query rows
-        const int slot = warp / kSlotWarps, quarter = warp % kSlotWarps, place = tid % kSlotThreads;
+        const int slot = warp / kSlotWarps - 1, quarter = warp % kSlotWarps, place = tid % kSlotThreads;
         const uint32_t lanes = tmem + (uint32_t(32 * quarter) << 16), scores = lanes + uint32_t(slot * 128);
         const bool flip = a.scale < 0.f;
         // of a sum of products, for the binary logarithm; positive, so that what is masked stays -inf
@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 if (!whole && mine && d0 == 0) {
                     partial[D] = ref;
                     partial[D + 1] = l;
-                    if (tid == 0) a.desc[part] = make_int4(s.b, s.hk, s.token0, (s.first == 0 ? kFirst : 0) | (rows << 3) | (s.parts << 16));
+                    if (tid == kFirstSlotWarp * kWarp) a.desc[part] = make_int4(s.b, s.hk, s.token0, (s.first == 0 ? kFirst : 0) | (rows << 3) | (s.parts << 16));
                 }
             }
             tc_fence_before();
@@ -608,8 +608,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
             const uint32_t leader = elect_leader(), tm = __shfl_sync(kFull, tmem, 0);
             const uint64_t dq0 = sw128_desc(smem_addr(sm_q)), dk0 = sw128_desc(smem_addr(sm_kv)), dv0 = value_desc(smem_addr(sm_kv));
             auto stage_of = [&](uint32_t x) { return uint64_t(x % N) * (S::kTile >> 4); };
-            auto score = [&](int slot, uint32_t query, uint32_t unit) {  // S = Q K^T
-                ok = ok && tc_wait_warp(&full[0][unit % kReady], (unit / kReady) & 1);
+            auto score = [&](int slot, uint32_t query, uint32_t unit, bool first) {  // S = Q K^T; first: of the unit
+                if (first) ok = ok && tc_wait_warp(&full[0][unit % kReady], (unit / kReady) & 1);
                 if (!ok) return;
                 lead_arrive(leader, &s_full[slot]);
                 tc_fence_after();
@@ -621,8 +621,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 }
                 lead_commit(leader, &s_full[slot]);
             };
-            auto product = [&](int slot, uint32_t unit, bool fresh) {  // O += P V, half of the keys as soon as their weights are there
-                ok = ok && tc_wait_warp(&ready[unit % kReady], (unit / kReady) & 1);
+            auto product = [&](int slot, uint32_t unit, bool first, bool fresh) {  // O += P V, half of the keys as soon as their weights are there
+                if (first) ok = ok && tc_wait_warp(&ready[unit % kReady], (unit / kReady) & 1);
                 const uint64_t dv = dv0 + stage_of(2 * unit + 1);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
@@ -656,14 +656,14 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
 #pragma unroll
                     for (int slot = 0; slot < 2; ++slot) {
                         if (split && slot != (k & 1)) continue;
-                        const bool frees = split || slot == 1;  // the last to use the unit's tiles
+                        const bool first = split || slot == 0, frees = split || slot == 1;  // the first and the last to use the unit's tiles
                         if (k >= step) {
-                            product(slot, unit0 + k - step, k - step < step);
+                            product(slot, unit0 + k - step, first, k - step < step);
                             if (frees) release(2 * (unit0 + k - step) + 1);
                             if (k >= n) finish(slot);
                         }
                         if (k < n) {
-                            score(slot, slot ? q1 : q0, unit0 + k);
+                            score(slot, slot ? q1 : q0, unit0 + k, first);
                             if (frees) release(2 * (unit0 + k));
                             if (frees && k == n - 1 && ok) {
                                 lead_commit(leader, &q_free[q0 % NQ]);
@@ -761,7 +761,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     tc_fence_after();
     if (warp == kMmaWarp16)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kColumns16) : "memory");
-    if (s_bad && tid == 0) a.desc[2 * cta].w |= kLate;  // (the thread that wrote it; the join writes the statuses)
+    if (s_bad && tid == kFirstSlotWarp * kWarp) a.desc[2 * cta].w |= kLate;  // (the thread that wrote it last; the join writes the statuses)
 }
 
 // Joins the partial results of the items that several CTAs hold, and writes the zeros of tokens that are not there and the

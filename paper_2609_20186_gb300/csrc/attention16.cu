@@ -43,7 +43,7 @@ constexpr int kMmaWarp16 = 0, kFetchWarp16 = 1, kValueWarp16 = 2, kRunWarp = 3, 
 constexpr int kThreads16 = (2 * kSlotWarps + 4) * kWarp;
 // Registers a thread of the two slots' warpgroups and of the third: 384 threads are launched with 168 each, and the shares
 // add up to the same.
-constexpr int kSlotRegs = 208, kOtherRegs16 = 88;
+constexpr int kSlotRegs = 192, kOtherRegs16 = 120;
 static_assert(2 * kSlotRegs + kOtherRegs16 == 3 * 168, "what two warpgroups gain the third gives");
 constexpr int kMaxCtas16 = 160;
 constexpr int kReady = 8;                   // units whose values are on their way, at most (a ring's tiles are fewer)
@@ -882,8 +882,9 @@ static cudaError_t launch16(const CUtensorMap &map, const Attn16Args &a, cudaStr
     // an explicit one-CTA cluster: the MMA commit addresses shared::cluster
     e = launch_pdl(attn16_kernel<F16, D>, dim3(ctas), dim3(kThreads16), size_t(Smem16<D>::bytes), s, 1u, map, a);
     if (e != cudaSuccess) return e;
+    // (two waves of CTAs at the most)
     const int64_t rows = std::min(int64_t(a.tokens), int64_t(a.T)) * a.group;
-    return launch_pdl(attn16_join_kernel<F16, D>, dim3(ctas, unsigned((rows + kJoinWarps16 - 1) / kJoinWarps16)), dim3(kJoinWarps16 * kWarp), 0, s, 0u, a);
+    return launch_pdl(attn16_join_kernel<F16, D>, dim3(ctas, unsigned(std::min(int64_t(6), (rows + kJoinWarps16 - 1) / kJoinWarps16))), dim3(kJoinWarps16 * kWarp), 0, s, 0u, a);
 }
 
 }  // namespace switchsd

@@ -5,8 +5,8 @@
 // (W also loses what z gained).  The threads' meet in a tree; then lse = m / temperature + ln S, and the entropy is
 // ln S - W / S.
 //
-// Top alternatives.  Of the first batch of loads the largest logit of every four threads is known, and the k-th largest of
-// those 128 is a bound that k of the CTA's logits reach: what lies below is no alternative.  The few that do not go, one by
+// Top alternatives.  Of the first batch of loads (and again of the first four) the largest logit of every group of threads is
+// known, and the k-th largest of those 128 is a bound that k of the CTA's logits reach: what lies below is no alternative.  The few that do not go, one by
 // one, into their warp's list, sorted over its lanes, whose k-th raises the warp's own bound.  The lists (of all CTAs) are
 // ranked by counting at the end.  A batch is looked at again only where its largest logit, which the sums want anyway,
 // reaches the bound.
@@ -16,8 +16,9 @@
 
 namespace switchsd {
 
-constexpr int kProbThreads = 512;
-constexpr int kProbWarps = kProbThreads / kWarp;
+// Threads of a CTA: many positions are a CTA each, small ones so that some of an SM's wait for each other or for their sums
+// while others stream; few positions are clusters of large ones.
+constexpr int kProbMany = 256, kProbFew = 512;
 constexpr int kProbFlight = 4;          // vectors of a thread that are worked on, and as many in flight
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kGone = -200.f;         // binary logarithm of a weight that binary32 does not have
@@ -103,7 +104,7 @@ struct WarpList {
 
 // The first k of n (value, token) pairs in `v`, `id`, in order, to `out_v`, `out_id` (the same for all threads of the CTA).
 __device__ __forceinline__ void rank_pairs(const float *v, const int32_t *id, int n, int k, float *out_v, int32_t *out_id) {
-    for (int i = threadIdx.x; i < n; i += kProbThreads) {
+    for (int i = threadIdx.x; i < n; i += int(blockDim.x)) {
         const float x = v[i];
         const int32_t t = id[i];
         int rank = 0;
@@ -115,15 +116,17 @@ __device__ __forceinline__ void rank_pairs(const float *v, const int32_t *id, in
     }
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArgs a, int parts) {
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const ProbArgs a, int parts) {
     using Row = LogitRow<DT>;
+    constexpr int kProbThreads = THREADS, kProbWarps = THREADS / kWarp;
+    constexpr int kGroup = THREADS / 128;                   // threads whose largest logit is looked at as one
     constexpr int P = Row::P, F = kProbFlight;
-    __shared__ float s_group[4 * 32];  // largest of four threads each
+    __shared__ float s_group[128];
     __shared__ float s_bound;
     __shared__ Sums s_sums[kProbWarps], s_all;
-    __shared__ float s_value[kProbWarps * 32], s_top[32];
-    __shared__ int32_t s_id[kProbWarps * 32], s_top_id[32];
+    __shared__ float s_value[512], s_top[32];  // of the CTA's warps, or of the cluster's CTAs (8 at the most)
+    __shared__ int32_t s_id[512], s_top_id[32];
     __shared__ int s_n, s_n_top;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int t = int(blockIdx.x) / parts, part = int(blockIdx.x) - t * parts, b = blockIdx.y;
@@ -161,7 +164,8 @@ __global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArg
     Sums sums{-INFINITY, 0.f, 0.f};
     float bound = -INFINITY;                   // of the CTA: k logits reach it
     WarpList list;
-    bool first = true;
+    float most = -INFINITY;                    // this thread's largest logit
+    int batch = 0;
     uint4 x[F], next[F];
     row.load(next, begin + tid, kProbThreads, end);
     for (int32_t base = begin; base < end; base += kProbThreads * F) {
@@ -169,11 +173,13 @@ __global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArg
         for (int i = 0; i < F; ++i) x[i] = next[i];
         row.load(next, base + tid + kProbThreads * F, kProbThreads, end);
         const float top = Row::largest(x);
-        if (first && k > 0) {
-            float g = fmaxf(top, -INFINITY);
-            g = fmaxf(g, __shfl_xor_sync(kFull, g, 1));
-            g = fmaxf(g, __shfl_xor_sync(kFull, g, 2));
-            if ((lane & 3) == 0) s_group[tid >> 2] = g;
+        most = fmaxf(most, top);
+        // (again when there is four times as much to go by: half of what passed the first bound does not pass the second)
+        if (k > 0 && (batch == 0 || batch == 3)) {
+            float g = most;
+#pragma unroll
+            for (int o = 1; o < kGroup; o <<= 1) g = fmaxf(g, __shfl_xor_sync(kFull, g, o));
+            if (lane % kGroup == 0) s_group[tid / kGroup] = g;
             __syncthreads();
             if (warp == 0) {
                 const uint32_t p[4] = {place_of(s_group[lane]), place_of(s_group[lane + 32]), place_of(s_group[lane + 64]), place_of(s_group[lane + 96])};
@@ -183,7 +189,7 @@ __global__ void __launch_bounds__(kProbThreads, 2) logprobs_kernel(const ProbArg
             __syncthreads();
             bound = s_bound;
         }
-        first = false;
+        ++batch;
         if (top > sums.m) sums.scale_to(top, c2);
         // Where a logit at kLow has no weight, what lies below (-inf, NaN) is taken for it, and z is one multiply-add off the
         // reference m c2, whose rounding is put right at the batch's end.
@@ -347,8 +353,10 @@ template <int DT>
 static cudaError_t launch_logprobs(const ProbArgs &a, int32_t B, cudaStream_t s) {
     const int sms = sm_count();
     if (sms == 0) return cudaErrorInvalidDevice;
-    const int parts = parts_of(int64_t(B) * a.T, (int64_t(a.V) + LogitRow<DT>::P - 1) / LogitRow<DT>::P, kProbThreads, 2 * sms);
-    return launch_pdl(logprobs_kernel<DT>, dim3(unsigned(parts) * unsigned(a.T), unsigned(B)), dim3(kProbThreads), 0, s, parts > 1 ? unsigned(parts) : 0u, a, parts);
+    const int parts = parts_of(int64_t(B) * a.T, (int64_t(a.V) + LogitRow<DT>::P - 1) / LogitRow<DT>::P, kProbFew, 2 * sms);
+    const dim3 grid(unsigned(parts) * unsigned(a.T), unsigned(B));
+    if (parts > 1) return launch_pdl(logprobs_kernel<DT, kProbFew>, grid, dim3(kProbFew), 0, s, unsigned(parts), a, parts);
+    return launch_pdl(logprobs_kernel<DT, kProbMany>, grid, dim3(kProbMany), 0, s, 0u, a, parts);
 }
 
 }  // namespace switchsd

@@ -46,8 +46,10 @@ constexpr int kThreads16 = (2 * kSlotWarps + 4) * kWarp;
 constexpr int kSlotRegs = 192, kOtherRegs16 = 120;
 static_assert(2 * kSlotRegs + kOtherRegs16 == 3 * 168, "what two warpgroups gain the third gives");
 constexpr int kMaxCtas16 = 160;
+constexpr int kPartExtra = 8;               // of a partial result's row: reference and sum, and room for rows of whole 32 bytes
 constexpr int kReady = 8;                   // units whose values are on their way, at most (a ring's tiles are fewer)
 constexpr int kRuns = 8;                    // runs between the first and the last of the warps, at most
+constexpr int kRunCost = 1;                 // units that a run costs beside its own when the units are dealt out
 constexpr int kBlock16 = 128 * 128;         // 128 rows of one swizzle row: an operand's 64 elements
 constexpr int kColumns16 = 512;             // tensor memory: S 2 x 128, O 2 x 128
 // log2 of the weight of a score at the reference, and of one that is as large as can be without a new reference.
@@ -145,7 +147,14 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, i
 __device__ __forceinline__ void cp_async16(void *dst, const void *src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(smem_addr(dst)), "l"(src) : "memory");
 }
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;\n" ::: "memory"); }
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+// 32 bytes; p is a multiple of 32.
+__device__ __forceinline__ void store32(void *p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_st2(uint32_t taddr, uint32_t a, uint32_t b) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\n" ::"r"(taddr), "r"(a), "r"(b) : "memory");
 }
@@ -177,15 +186,15 @@ struct Run {
 // The runs of a CTA's range, in order, but that one which begins inside an item comes last: the CTAs that share an item's
 // keys then go through them side by side, and what one has fetched the others find in L2.
 struct Runs {
-    int64_t u, total;    // units before the next run's first, in all
+    int64_t u, total;    // units and runs' costs before the next run, in all
     int32_t takers;
     int b, hk, rt;
-    int32_t skip;        // of the first item: units before the range
-    int64_t left;        // units
+    int32_t skip;        // of the first item: what lies before the range
+    int64_t left;        // what is left of the range
     int32_t len, nw;     // of row b
     bool begun, held;
     Run late;
-    __device__ int holder(int64_t unit) const { return int(quotient((unit + 1) * takers - 1, total)); }  // the CTA whose range has a unit
+    __device__ int holder(int64_t at) const { return int(quotient((at + 1) * takers - 1, total)); }  // the CTA whose range has it
     __device__ bool take(const Attn16Args &a, Run &s) {
         while (left > 0) {
             const int tiles = (nw + a.tokens - 1) / a.tokens;
@@ -206,15 +215,16 @@ struct Runs {
             s.tokens = min(a.tokens, nw - s.token0);
             s.keys = len + s.token0 + s.tokens;
             s.units = (s.keys + kUnitKeys - 1) / kUnitKeys;
-            s.first = skip;
-            s.n = int32_t(min(int64_t(s.units - skip), left));
+            const int32_t taken = int32_t(min(int64_t(kRunCost + s.units - skip), left));
+            s.first = max(0, skip - kRunCost);
+            s.n = skip + taken - kRunCost - s.first;
             s.part = 1;
-            // CTAs that hold units of the item
-            s.parts = holder(u - s.first + s.units - 1) - holder(u - s.first) + 1;
-            u += s.n;
+            const int64_t unit0 = u - skip + kRunCost;  // the item's first
+            s.parts = holder(unit0 + s.units - 1) - holder(unit0) + 1;
+            u += taken;
             skip = 0;
-            left -= s.n;
-            return true;
+            left -= taken;
+            if (s.n > 0) return true;  // (else the range ends before the item's first unit)
         }
         return false;
     }
@@ -240,10 +250,10 @@ struct Runs {
 __device__ __forceinline__ void deal_runs(const Attn16Args &a, int64_t *s_pre, Runs &runs) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, ctas = int(gridDim.x);
     const int per = (a.B + kThreads16 - 1) / kThreads16;  // rows of a thread
-    auto before_tile = [&](int32_t len, int32_t nw, int rt) -> int64_t {  // units of a key head's tiles before rt
+    auto before_tile = [&](int32_t len, int32_t nw, int rt) -> int64_t {  // units and costs of a key head's tiles before rt
         const int whole = nw / a.tokens;
         const int64_t c = int64_t(len) + a.tokens + kUnitKeys - 1;
-        return (whole && rt ? sum_of_units(c, a.tokens, min(rt, whole)) : 0) + (rt > whole ? (int64_t(len) + nw + kUnitKeys - 1) / kUnitKeys : 0);
+        return int64_t(rt) * kRunCost + (whole && rt ? sum_of_units(c, a.tokens, min(rt, whole)) : 0) + (rt > whole ? (int64_t(len) + nw + kUnitKeys - 1) / kUnitKeys : 0);
     };
     int32_t len = 0, nw = 0;
     auto units_of = [&](int row) -> int64_t {  // of a key head
@@ -269,7 +279,7 @@ __device__ __forceinline__ void deal_runs(const Attn16Args &a, int64_t *s_pre, R
         total += y;
         if (w < warp) before += y;
     }
-    const int64_t takers = min(total, int64_t(ctas));  // CTAs with a range: at least one unit each
+    const int64_t takers = min(total, int64_t(ctas));  // CTAs with a range
     const int64_t u = cta < takers ? quotient(total * cta, takers) : total, u_end = cta < takers ? quotient(total * (cta + 1), takers) : total;
     if (tid < 2) a.desc[2 * cta + tid] = make_int4(-1, 0, 0, 0);
     int64_t *s_at = s_pre + kThreads16 / kWarp;
@@ -510,8 +520,9 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
             if (warp_mine) {
                 const uint32_t from = split ? lanes + 256 : out;
                 const int part = 2 * cta + s.part, d0 = split ? slot * (D / 2) : 0, d1 = split ? d0 + D / 2 : D;
-                float *partial = a.part + (size_t(part) * kTileRows + row) * (D + 4);
+                float *partial = a.part + (size_t(part) * kTileRows + row) * (D + kPartExtra);
                 uint16_t *result = a.out + ((size_t(s.b) * a.T + s.token0 + t) * a.Hq + h) * D;
+                const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
                 const int32_t cleared = s_cleared[nrun % kRuns] == nrun + 1 ? min(limit + 1, (s.first + s.n) * kUnitKeys) : 0;
 #pragma unroll 4
                 for (int d = d0; d < d1; d += 16) {
@@ -538,15 +549,21 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                             if (!(fabsf(x) < INFINITY)) v[j] += x;
                         }
                     }
+                    // (every thread has a row of its own: a store's 32 pieces are sectors of as many lines, so they are whole ones)
                     if (mine && whole) {
-                        uint4 *dst = reinterpret_cast<uint4 *>(result + d);
 #pragma unroll
-                        for (int j = 0; j < 16; j += 8)
-                            dst[j / 8] = make_uint4(narrow2<F16>(v[j] * inv, v[j + 1] * inv), narrow2<F16>(v[j + 2] * inv, v[j + 3] * inv),
-                                                    narrow2<F16>(v[j + 4] * inv, v[j + 5] * inv), narrow2<F16>(v[j + 6] * inv, v[j + 7] * inv));
+                        for (int j = 0; j < 8; ++j) w[j] = narrow2<F16>(v[2 * j] * inv, v[2 * j + 1] * inv);
+                        if (wide) {
+                            store32(result + d, *reinterpret_cast<uint32_t(*)[8]>(w));
+                        } else {
+                            reinterpret_cast<uint4 *>(result + d)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                            reinterpret_cast<uint4 *>(result + d)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                        }
                     } else if (mine) {
 #pragma unroll
-                        for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4 *>(partial + d + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(v[j]);
+                        store32(partial + d, *reinterpret_cast<uint32_t(*)[8]>(w));
+                        store32(partial + d + 8, *reinterpret_cast<uint32_t(*)[8]>(w + 8));
                     }
                 }
                 if (!whole && mine && d0 == 0) {
@@ -734,23 +751,32 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 }
                 if (!more) break;
                 const int rows = s.tokens * a.group;
-                const uint32_t end = qx + (rows <= kSlotRows ? 1 : 2);
-                const uint16_t *q = a.q + s.b * a.qs[0] + s.token0 * a.qs[1] + int64_t(s.hk) * a.group * a.qs[2];
+                const uint32_t q0 = qx, end = qx + (rows <= kSlotRows ? 1 : 2);
+                constexpr int kVec = D / 8, kStep = kWarp / kVec;  // vectors of a row, rows of a pass
+                const int c = lane % kVec, in_pass = lane / kVec;
+                int g = in_pass % a.group;  // (a row's query head in its key head's)
+                const uint16_t *q = a.q + s.b * a.qs[0] + (s.token0 + in_pass / a.group) * a.qs[1] + (int64_t(s.hk) * a.group + g) * a.qs[2] + 8 * c;
+                const int64_t next = kStep * a.qs[2], wrap = a.qs[1] - a.group * a.qs[2];
                 for (int row0 = 0; qx < end; ++qx, row0 += kSlotRows) {
                     if (qx >= NQ) ok = ok && tc_wait_warp(&q_free[qx % NQ], (qx / NQ - 1) & 1);
                     if (!ok) break;
-                    constexpr int kVec = D / 8, kStep = kWarp / kVec;  // vectors of a row, rows of a pass
-                    const int c = lane % kVec, last = min(rows - row0, kSlotRows);
-                    int row = lane / kVec, t = (row0 + row) / a.group, g = row0 + row - t * a.group;
-                    uint8_t *dst = sm_q + (qx % NQ) * S::kQ + (c / 8) * kBlock16;
+                    const int last = min(rows - row0, kSlotRows);
+                    uint8_t *dst = sm_q + (qx % NQ) * S::kQ + (c / 8) * kBlock16 + in_pass * 128;
 #pragma unroll 4
-                    for (; row < last; row += kStep) {
-                        cp_async16(dst + row * 128 + (((c & 7) ^ (row & 7)) * 16), q + t * a.qs[1] + g * a.qs[2] + 8 * c);
-                        for (g += kStep; g >= a.group; g -= a.group) ++t;
+                    for (int row = in_pass; row < last; row += kStep, dst += kStep * 128) {
+                        cp_async16(dst + (((c & 7) ^ (row & 7)) * 16), q);
+                        q += next;
+                        for (g += kStep; g >= a.group; g -= a.group) q += wrap;
                     }
-                    cp_async_wait();
+                    cp_async_commit();
+                }
+                for (uint32_t x = q0; x < qx; ++x) {
+                    if (x + 1 < qx)
+                        cp_async_wait<1>();
+                    else
+                        cp_async_wait<0>();
                     fence_proxy_async();
-                    warp_arrive(&q_ready[qx % NQ]);
+                    warp_arrive(&q_ready[x % NQ]);
                 }
             }
         }
@@ -796,7 +822,7 @@ __global__ void __launch_bounds__(kJoinWarps16 *kWarp, 3) attn16_join_kernel(con
                     ps[j] = 0.f;
                     py[j] = Part{};
                     if (j0 + j < n) {
-                        const float *src = a.part + (size_t(j0 + j ? 2 * (i + j0 + j) : from) * kTileRows + row) * (D + 4);
+                        const float *src = a.part + (size_t(j0 + j ? 2 * (i + j0 + j) : from) * kTileRows + row) * (D + kPartExtra);
                         const float2 ms = __ldcg(reinterpret_cast<const float2 *>(src + D));
                         pm[j] = ms.x;
                         ps[j] = ms.y;
@@ -853,7 +879,7 @@ static bool give_up16() {
     return set;
 }
 
-static size_t workspace16(int D) { return size_t(2 * kMaxCtas16) * (sizeof(int4) + size_t(kTileRows) * (D + 4) * sizeof(float)); }
+static size_t workspace16(int D) { return size_t(2 * kMaxCtas16) * (sizeof(int4) + size_t(kTileRows) * (D + kPartExtra) * sizeof(float)) + 32; }
 
 // The cache as [pages][2 Hkv][page][D], a box of 64 dimensions of the tokens of a unit that lie in one page.
 static bool encode_cache(CUtensorMap *map, const switchsd_kv16_attention_params *p) {
@@ -919,7 +945,7 @@ extern "C" int switchsd_kv16_attention(const switchsd_kv16_attention_params *p) 
     a.out = static_cast<uint16_t *>(p->out);
     a.status = p->status;
     a.desc = static_cast<int4 *>(p->workspace);
-    a.part = reinterpret_cast<float *>(a.desc + 2 * kMaxCtas16);
+    a.part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(a.desc + 2 * kMaxCtas16) + 31) & ~uintptr_t(31));
     a.B = p->B;
     a.T = p->T;
     a.Hq = p->Hq;

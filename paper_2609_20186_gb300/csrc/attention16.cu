@@ -318,6 +318,24 @@ __device__ __forceinline__ void deal_runs(const Attn16Args &a, int64_t *s_pre, R
     runs.begun = runs.held = false;
 }
 
+// Zeros for the tokens that are not there, by warp w of so many: it looks at 32 tokens together and fills a part of each, 512
+// bytes or more.
+__device__ __forceinline__ void fill_absent(const Attn16Args &a, uint32_t w, uint32_t warps) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t all = uint32_t(a.B) * uint32_t(a.T), groups = (all + kWarp - 1) / kWarp;  // (below 2^31)
+    const uint32_t row16 = uint32_t(a.Hq) * uint32_t(a.dim / 8);                             // 16-byte pieces of a token's output
+    const uint32_t cuts = max(1u, min(warps / groups, row16 / kWarp)), cut = (row16 + cuts - 1) / cuts;
+    for (; w < groups * cuts; w += warps) {
+        const uint32_t j0 = w / cuts * kWarp, j = j0 + lane, b = j / uint32_t(a.T), e0 = w % cuts * cut, e1 = min(e0 + cut, row16);
+        int32_t len, nw = a.T;
+        if (j < all) row_lengths(a, int(b), len, nw);
+        for (uint32_t gone = __ballot_sync(kFull, int(j - b * a.T) >= nw); gone; gone &= gone - 1) {
+            uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(j0 + __ffs(int(gone)) - 1) * row16;
+            for (uint32_t e = e0 + lane; e < e1; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
+        }
+    }
+}
+
 template <bool F16, int D>
 __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_constant__ CUtensorMap map, const Attn16Args a) {
     using S = Smem16<D>;
@@ -779,6 +797,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                     warp_arrive(&q_ready[x % NQ]);
                 }
             }
+            fill_absent(a, cta, gridDim.x);  // (the others are still at the last runs)
         }
     }
     if (!ok) s_bad = 1;
@@ -790,8 +809,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     if (s_bad && tid == kFirstSlotWarp * kWarp) a.desc[2 * cta].w |= kLate;  // (the thread that wrote it last; the join writes the statuses)
 }
 
-// Joins the partial results of the items that several CTAs hold, and writes the zeros of tokens that are not there and the
-// statuses of a launch that a CTA gave up: CTAs (i, .) look after the item whose first part is the i-th CTA's, a warp a query
+// Joins the partial results of the items that several CTAs hold, and writes the statuses of a launch that a CTA gave up: CTAs (i, .) look after the item whose first part is the i-th CTA's, a warp a query
 // row, adding the parts in order, kJoinFlight on their way together.
 constexpr int kJoinWarps16 = 8, kJoinFlight = 8;
 template <bool F16, int D>
@@ -852,19 +870,6 @@ __global__ void __launch_bounds__(kJoinWarps16 *kWarp, 3) attn16_join_kernel(con
                 *reinterpret_cast<uint2 *>(out) = make_uint2(narrow2<F16>(y[0] * inv, y[1] * inv), narrow2<F16>(y[2] * inv, y[3] * inv));
             else
                 *out = narrow2<F16>(y[0] * inv, y[1] * inv);
-        }
-    }
-    // zeros for the tokens that are not there: a warp looks at 32 tokens together, and fills a part of each, 512 bytes or more
-    const uint32_t all_warps = gridDim.x * warps, all = uint32_t(a.B) * uint32_t(a.T);                          // (below 2^31)
-    const uint32_t groups = (all + kWarp - 1) / kWarp, row16 = uint32_t(a.Hq) * (D / 8);                      // 16-byte pieces of a token's output
-    const uint32_t cuts = max(1u, min(all_warps / groups, row16 / kWarp)), cut = (row16 + cuts - 1) / cuts;
-    for (uint32_t w = uint32_t(i) * warps + warp; w < groups * cuts; w += all_warps) {
-        const uint32_t j0 = w / cuts * kWarp, j = j0 + lane, b = j / uint32_t(a.T), e0 = w % cuts * cut, e1 = min(e0 + cut, row16);
-        int32_t len, nw = a.T;
-        if (j < all) row_lengths(a, int(b), len, nw);
-        for (uint32_t gone = __ballot_sync(kFull, int(j - b * a.T) >= nw); gone; gone &= gone - 1) {
-            uint4 *o = reinterpret_cast<uint4 *>(a.out) + size_t(j0 + __ffs(int(gone)) - 1) * row16;
-            for (uint32_t e = e0 + lane; e < e1; e += kWarp) o[e] = make_uint4(0, 0, 0, 0);
         }
     }
 }

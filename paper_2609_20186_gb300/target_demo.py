@@ -1,11 +1,12 @@
 """The controller and the target's side of a verification step together, on a small target with random weights.
 
-    python -m paper_2609_20186_gb300.target_demo [--rows 8] [--steps 64] [--no-drafts]
+    python -m paper_2609_20186_gb300.target_demo [--rows 8] [--steps 64] [--no-drafts] [--temperature 0.8] [--cache16]
 
 Every step, with nothing read back by the host: pages and slots for the step's tokens (the context's last one and the
 draft; a row that the pool has no pages for sits the step out), their keys and values into the 4-bit cache and their
 attention over it, penalties and biases on the logits and the greedy token of every position, then the controller's
-verification, append and next draft.  The target here is attention layers without positions and a head that prefers, by far, the token that follows in a fixed cycle of tokens,
+verification, append and next draft.  With a temperature the drafts' probabilities and the token that is appended come from
+the same logits, and the verification is the sampled one.  The cache may be held in 16 bits.  The target here is attention layers without positions and a head that prefers, by far, the token that follows in a fixed cycle of tokens,
 so that its text repeats and copied drafts are accepted; its products are torch's.
 """
 from __future__ import annotations
@@ -57,8 +58,10 @@ class Decoder:
     """A batch of sequences between a SmallTarget, a KVCache and a Session."""
 
     def __init__(self, target: SmallTarget, prompts: np.ndarray, lens: np.ndarray, *, k: int = 8, room: int = 256, page: int = 16,
-                 drafts: bool = True, pages: int | None = None):
-        """`pages` pages for all rows: enough for every row's whole context when None."""
+                 drafts: bool = True, pages: int | None = None, temperature: float | None = None, seed: int = 0,
+                 dtype: torch.dtype | None = None):
+        """`pages` pages for all rows: enough for every row's whole context when None.  temperature None: the greedy
+        verification; else the sampled one, with draws from `seed`.  dtype: the cache's (None: 4 bits)."""
         B = prompts.shape[0]
         self.target, self.k, self.drafts = target, k, drafts
         cap = -(-(prompts.shape[1] + room) // 4) * 4
@@ -69,12 +72,18 @@ class Decoder:
         dev = self.sess.ctx.device
         # lengths as the context's: its last token is the first of the step
         self.cache = KVCache(B, k + 1, layers=target.layers, heads=target.kv_heads, dim=target.head_dim, pages=pages or B * -(-cap // page),
-                             max_len=cap, page=page, lens_add=-1, new_add=1, device=dev)
+                             max_len=cap, page=page, lens_add=-1, new_add=1, device=dev, dtype=dtype)
         f32 = dict(dtype=torch.float32, device=dev)
         self.rep, self.freq, self.pres = torch.full((B,), 1.02, **f32), torch.full((B,), 0.01, **f32), torch.full((B,), 0.1, **f32)
         self.prompt_lens = self.sess.lens.clone()
         self.banned = torch.full((B, 1), target.vocab - 1, dtype=torch.int32, device=dev)  # a token that never comes
         self.bias = torch.full((B, 1), float("-inf"), **f32)
+        self.temperature = None
+        if temperature is not None:
+            self.temperature = torch.full((B,), temperature, **f32)
+            self.seeds = torch.arange(B, dtype=torch.int64, device=dev) + (seed << 32)
+            self.draws = torch.Generator(device=dev)
+            self.draws.manual_seed(seed)
         self._prefill(prompts.shape[1])
 
     def _prefill(self, longest: int) -> None:
@@ -96,10 +105,18 @@ class Decoder:
         s.vlen.copy_(self.cache.new)  # rows without pages: no logits, nothing appended, and another try in the next step
         tokens = torch.cat([s.ctx.gather(1, (s.lens - 1).long()[:, None]), s.vdraft], 1)
         x = self.target.hidden(tokens, self.cache)
-        bd.switchsd_logits(x @ self.target.head.T, ctx_tokens=s.ctx, ctx_lens=s.lens, draft=s.vdraft, new_lens=s.vlen, new_add=1,
+        logits = x @ self.target.head.T
+        bd.switchsd_logits(logits, ctx_tokens=s.ctx, ctx_lens=s.lens, draft=s.vdraft, new_lens=s.vlen, new_add=1,
                            rep=self.rep, freq=self.freq, pres=self.pres, prompt_lens=self.prompt_lens, bias_ids=self.banned,
-                           bias=self.bias, argmax=s.target)
-        s.verify_step(x)
+                           bias=self.bias, **(dict(argmax=s.target) if self.temperature is None else dict(out=logits)))
+        if self.temperature is None:
+            s.verify_step(x)
+        else:  # (every draft is a copied one: the drafter's probabilities stay 1)
+            s.vu.uniform_(generator=self.draws)
+            bd.switchsd_logprobs(logits, tokens=s.vdraft, new_lens=s.vlen, new_add=1, temperature=self.temperature, prob=s.vp)
+            bd.switchsd_resample(logits, s.vdraft, s.vlen, s.vp, s.vu, s.target, seeds=self.seeds, ctx_lens=s.lens,
+                                 temperature=self.temperature)
+            s.verify_sampled_step(x)
         if self.drafts:
             s.vdraft.copy_(s.draft)
             # (a row that sat the step out tries the next one with its one token)
@@ -119,10 +136,13 @@ def main(argv=None) -> None:
     p.add_argument("--rows", type=int, default=8)
     p.add_argument("--steps", type=int, default=64)
     p.add_argument("--no-drafts", action="store_true")
+    p.add_argument("--temperature", type=float, default=None)
+    p.add_argument("--cache16", action="store_true")
     a = p.parse_args(argv)
     target = SmallTarget()
     prompts, lens = prompts_of(a.rows, target)
-    d = Decoder(target, prompts, lens, room=a.steps * 9, drafts=not a.no_drafts)
+    d = Decoder(target, prompts, lens, room=a.steps * 9, drafts=not a.no_drafts, temperature=a.temperature,
+                dtype=torch.bfloat16 if a.cache16 else None)
     for _ in range(a.steps):
         d.step()
     new = d.sess.lens.cpu().numpy() - lens

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 import threading
 
 import torch
@@ -190,6 +191,15 @@ class switchsd_resample_params(ctypes.Structure):
     ]
 
 
+# The parameter blocks of the 16-bit cache's and the sampling's calls as bytes, which the calls take as well: made in a third
+# of the time.
+_BLOCKS = {switchsd_kv16_append_params: "@7iPP3q3qPPP", switchsd_kv16_read_params: "@6iPPPPP", switchsd_kv16_attention_params: "@9iP3qPPPP2ifPPNPP",
+           switchsd_logprobs_params: "@6iP2qP2i10P", switchsd_resample_params: "@4iP2q8P2q7P"}
+for _params, _format in _BLOCKS.items():
+    assert struct.calcsize(_format) == ctypes.sizeof(_params), _params
+_KV16_APPEND, _KV16_READ, _KV16_ATTENTION, _LOGPROBS, _RESAMPLE = (struct.Struct(f) for f in _BLOCKS.values())
+
+
 _lock = threading.Lock()
 _lib = None
 
@@ -255,12 +265,12 @@ _SIGNATURES = {
     "switchsd_kv4_attention": (ctypes.c_int, [ctypes.POINTER(switchsd_kv4_attention_params)]),
     "switchsd_logits_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(switchsd_logits_params)]),
     "switchsd_logits": (ctypes.c_int, [ctypes.POINTER(switchsd_logits_params)]),
-    "switchsd_kv16_append": (ctypes.c_int, [ctypes.POINTER(switchsd_kv16_append_params)]),
-    "switchsd_kv16_read": (ctypes.c_int, [ctypes.POINTER(switchsd_kv16_read_params)]),
+    "switchsd_kv16_append": (ctypes.c_int, [ctypes.c_void_p]),
+    "switchsd_kv16_read": (ctypes.c_int, [ctypes.c_void_p]),
     "switchsd_kv16_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(switchsd_kv16_attention_params)]),
-    "switchsd_kv16_attention": (ctypes.c_int, [ctypes.POINTER(switchsd_kv16_attention_params)]),
-    "switchsd_logprobs": (ctypes.c_int, [ctypes.POINTER(switchsd_logprobs_params)]),
-    "switchsd_resample": (ctypes.c_int, [ctypes.POINTER(switchsd_resample_params)]),
+    "switchsd_kv16_attention": (ctypes.c_int, [ctypes.c_void_p]),
+    "switchsd_logprobs": (ctypes.c_int, [ctypes.c_void_p]),
+    "switchsd_resample": (ctypes.c_int, [ctypes.c_void_p]),
 }
 
 
@@ -717,37 +727,38 @@ def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_l
     _check(load().switchsd_logits(ctypes.byref(p)), "switchsd_logits")
 
 
-def _cache16_shape(cache, H: int, D: int):
-    """pages and tokens a page of a 16-bit cache [pages, 2, H, page, D] of one layer."""
-    if not isinstance(cache, torch.Tensor) or cache.dim() != 5 or cache.shape[1] != 2 or cache.shape[4] != D or (H and cache.shape[2] != H):
-        raise ValueError(f"the cache has shape {tuple(getattr(cache, 'shape', ()))}, expected [pages, 2, {H or 'Hkv'}, page, {D}]")
+def _cache16(cache, H: int, D: int):
+    """pages, Hkv and tokens a page of a 16-bit cache [pages, 2, Hkv, page, D] of one layer (H: Hkv, or 0 for any)."""
+    shape = cache.shape if isinstance(cache, torch.Tensor) else ()
+    if len(shape) != 5 or shape[1] != 2 or shape[4] != D or (H and shape[2] != H):
+        raise ValueError(f"the cache has shape {tuple(shape)}, expected [pages, 2, {H or 'Hkv'}, page, {D}]")
     if cache.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"the cache must be bfloat16 or float16, got {cache.dtype}")
-    return cache.shape[0], cache.shape[3]
+    return shape[0], shape[2], shape[3]
 
 
 def switchsd_kv16_append(k, v, slots, cache, *, stream=None) -> None:
     """switchsd_kv16_append of include/switchsd_target.h: k, v [B, T, Hkv, D] (views whose last dimension is contiguous)
     of the cache's type, slots int32 [B, T], cache bf16 or f16 [pages, 2, Hkv, page, D]."""
-    B, T, H, D = k.shape
-    pages, page = _cache16_shape(cache, H, D)
-    dtype = _strided(k, "k", (B, T, H, D), (cache.dtype,))
-    _strided(v, "v", (B, T, H, D), (cache.dtype,))
-    p = switchsd_kv16_append_params(
-        B, T, H, D, page, pages, dtype, k.data_ptr(), v.data_ptr(), k.stride()[:3], v.stride()[:3],
-        _dev(slots, torch.int32, "slots", (B, T)), _dev(cache, cache.dtype, "cache"), _stream_ptr(stream))
-    _check(load().switchsd_kv16_append(ctypes.byref(p)), "switchsd_kv16_append")
+    shape = k.shape
+    B, T, H, D = shape
+    pages, _, page = _cache16(cache, H, D)
+    dtype = _strided(k, "k", shape, (cache.dtype,))
+    _strided(v, "v", shape, (cache.dtype,))
+    p = _KV16_APPEND.pack(B, T, H, D, page, pages, dtype, k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3],
+                          _dev(slots, torch.int32, "slots", (B, T)) or 0, _dev(cache, cache.dtype, "cache"), _stream_ptr(stream))
+    _check(load().switchsd_kv16_append(p), "switchsd_kv16_append")
 
 
 def switchsd_kv16_read(cache, slots, out_k, out_v, *, stream=None) -> None:
     """switchsd_kv16_read of include/switchsd_target.h: what the cache holds for slots int32 [B, T], into out_k and out_v
     [B, T, Hkv, D] of its type."""
-    B, T, H, D = out_k.shape
-    pages, page = _cache16_shape(cache, H, D)
-    p = switchsd_kv16_read_params(
-        B, T, H, D, page, pages, _dev(cache, cache.dtype, "cache"), _dev(slots, torch.int32, "slots", (B, T)),
-        _dev(out_k, cache.dtype, "out_k", (B, T, H, D)), _dev(out_v, cache.dtype, "out_v", (B, T, H, D)), _stream_ptr(stream))
-    _check(load().switchsd_kv16_read(ctypes.byref(p)), "switchsd_kv16_read")
+    shape = out_k.shape
+    B, T, H, D = shape
+    pages, _, page = _cache16(cache, H, D)
+    p = _KV16_READ.pack(B, T, H, D, page, pages, _dev(cache, cache.dtype, "cache"), _dev(slots, torch.int32, "slots", (B, T)) or 0,
+                        _dev(out_k, cache.dtype, "out_k", shape), _dev(out_v, cache.dtype, "out_v", shape), _stream_ptr(stream))
+    _check(load().switchsd_kv16_read(p), "switchsd_kv16_read")
 
 
 @functools.lru_cache(maxsize=64)
@@ -764,18 +775,18 @@ def switchsd_kv16_attention(q, cache, block_table, lens, new_lens, out, *, scale
     the cache's type, cache bf16 or f16 [pages, 2, Hkv, page, D], block_table int32 [B, blocks], lens, new_lens int32 [B],
     out [B, T, Hq, D] of q's type.  scale: 1 / sqrt(D) when None.  Takes its workspace from torch, in the order of the
     call's stream, when none is given."""
-    B, T, Hq, D = q.shape
-    (pages, page), Hkv, blocks, row = _cache16_shape(cache, 0, D), cache.shape[2], block_table.shape[1], (B,)
-    dtype = _strided(q, "q", (B, T, Hq, D), (cache.dtype,))
-    p = switchsd_kv16_attention_params(
-        B, T, Hq, Hkv, D, page, pages, blocks, dtype, q.data_ptr(), q.stride()[:3], _dev(cache, cache.dtype, "cache"),
-        _dev(block_table, torch.int32, "block_table", (B, blocks)), _dev(lens, torch.int32, "lens", row),
-        _dev(new_lens, torch.int32, "new_lens", row), lens_add, new_add, D ** -0.5 if scale is None else scale,
-        _dev(out, q.dtype, "out", (B, T, Hq, D)), None, 0, _dev(status, torch.int32, "status", row), _stream_ptr(stream))
+    shape = q.shape
+    B, T, Hq, D = shape
+    (pages, Hkv, page), blocks, row, i32 = _cache16(cache, 0, D), block_table.shape[1], (B,), torch.int32
+    dtype = _strided(q, "q", shape, (cache.dtype,))
     if workspace is None:
         workspace = _scratch(switchsd_kv16_attention_workspace(D), q.device, stream)
-    p.workspace, p.workspace_bytes = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
-    _check(load().switchsd_kv16_attention(ctypes.byref(p)), "switchsd_kv16_attention")
+    p = _KV16_ATTENTION.pack(
+        B, T, Hq, Hkv, D, page, pages, blocks, dtype, q.data_ptr(), *q.stride()[:3], _dev(cache, cache.dtype, "cache"), _dev(block_table, i32, "block_table", (B, blocks)) or 0,
+        _dev(lens, i32, "lens", row) or 0, _dev(new_lens, i32, "new_lens", row) or 0, lens_add, new_add, D ** -0.5 if scale is None else scale,
+        _dev(out, q.dtype, "out", shape) or 0, _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _dev(status, i32, "status", row) or 0,
+        _stream_ptr(stream))
+    _check(load().switchsd_kv16_attention(p), "switchsd_kv16_attention")
 
 
 def switchsd_logprobs(logits, *, tokens=None, new_lens=None, new_add: int = 0, temperature=None, logprob=None, prob=None,
@@ -791,13 +802,13 @@ def switchsd_logprobs(logits, *, tokens=None, new_lens=None, new_add: int = 0, t
     of_top = top_ids if top_ids is not None else top_logprobs
     top = of_top.shape[2] if of_top is not None else 0
     i32, f32, row, strides = torch.int32, torch.float32, (B,), logits.stride()
-    p = switchsd_logprobs_params(
-        B, T, V, K, top, dtype, logits.data_ptr(), strides[0], strides[1], _dev(new_lens, i32, "new_lens", row), new_add, K,
-        _dev(temperature, f32, "temperature", row), _dev(tokens, i32, "tokens", (B, K)), _dev(logprob, f32, "logprob", (B, K)),
-        _dev(prob, f32, "prob", (B, K)), _dev(entropy, f32, "entropy", (B, T)), _dev(lse, f32, "lse", (B, T)),
-        _dev(top_ids, i32, "top_ids", (B, T, top)), _dev(top_logprobs, f32, "top_logprobs", (B, T, top)),
-        _dev(status, i32, "status", row), _stream_ptr(stream))
-    _check(load().switchsd_logprobs(ctypes.byref(p)), "switchsd_logprobs")
+    p = _LOGPROBS.pack(
+        B, T, V, K, top, dtype, logits.data_ptr(), strides[0], strides[1], _dev(new_lens, i32, "new_lens", row) or 0, new_add, K,
+        _dev(temperature, f32, "temperature", row) or 0, _dev(tokens, i32, "tokens", (B, K)) or 0, _dev(logprob, f32, "logprob", (B, K)) or 0,
+        _dev(prob, f32, "prob", (B, K)) or 0, _dev(entropy, f32, "entropy", (B, T)) or 0, _dev(lse, f32, "lse", (B, T)) or 0,
+        _dev(top_ids, i32, "top_ids", (B, T, top)) or 0, _dev(top_logprobs, f32, "top_logprobs", (B, T, top)) or 0,
+        _dev(status, i32, "status", row) or 0, _stream_ptr(stream))
+    _check(load().switchsd_logprobs(p), "switchsd_logprobs")
 
 
 def switchsd_resample(logits, draft, draft_len, p_draft, u, out, *, seeds, ctx_lens, temperature=None, lse=None, q_draft=None,
@@ -808,18 +819,18 @@ def switchsd_resample(logits, draft, draft_len, p_draft, u, out, *, seeds, ctx_l
     [B, T - 1]; out int32 [B, T]: the `resample` of switchsd_verify_sampled at the entry that it takes, -1 elsewhere."""
     B, T, V = logits.shape
     dtype = _strided(logits, "logits", (B, T, V), tuple(_DTYPES))
-    q_ptr, q_strides = None, (0, 0)
+    q_ptr, q_strides = 0, (0, 0)
     if q_logits is not None:
         _strided(q_logits, "q_logits", (B, T - 1, V), (logits.dtype,))
         q_ptr, q_strides = q_logits.data_ptr(), q_logits.stride()
         if T > 1 and (lse is None or q_lse is None):
             raise ValueError("q_logits go with lse and q_lse")
     i32, f32, row, k, strides = torch.int32, torch.float32, (B,), (B, T - 1), logits.stride()
-    p = switchsd_resample_params(
-        B, T, V, dtype, logits.data_ptr(), strides[0], strides[1], _dev(lse, f32, "lse", (B, T)),
-        _dev(temperature, f32, "temperature", row), _dev(draft, i32, "draft", k), _dev(draft_len, i32, "draft_len", row),
-        _dev(p_draft, f32, "p_draft", k), _dev(q_draft, f32, "q_draft", k), _dev(u, f32, "u", k), q_ptr, q_strides[0],
-        q_strides[1], _dev(q_lse, f32, "q_lse", k), _dev(mode, i32, "mode", row), _dev(seeds, torch.int64, "seeds", row),
-        _dev(ctx_lens, i32, "ctx_lens", row), _dev(out, i32, "out", (B, T)), _dev(status, i32, "status", row),
+    p = _RESAMPLE.pack(
+        B, T, V, dtype, logits.data_ptr(), strides[0], strides[1], _dev(lse, f32, "lse", (B, T)) or 0,
+        _dev(temperature, f32, "temperature", row) or 0, _dev(draft, i32, "draft", k) or 0, _dev(draft_len, i32, "draft_len", row) or 0,
+        _dev(p_draft, f32, "p_draft", k) or 0, _dev(q_draft, f32, "q_draft", k) or 0, _dev(u, f32, "u", k) or 0, q_ptr, q_strides[0],
+        q_strides[1], _dev(q_lse, f32, "q_lse", k) or 0, _dev(mode, i32, "mode", row) or 0, _dev(seeds, torch.int64, "seeds", row) or 0,
+        _dev(ctx_lens, i32, "ctx_lens", row) or 0, _dev(out, i32, "out", (B, T)) or 0, _dev(status, i32, "status", row) or 0,
         _stream_ptr(stream))
-    _check(load().switchsd_resample(ctypes.byref(p)), "switchsd_resample")
+    _check(load().switchsd_resample(p), "switchsd_resample")

@@ -107,3 +107,17 @@ def test_a_cache_of_another_type_is_refused(bd):
     from paper_2609_20186_gb300 import KVCache
     with pytest.raises(ValueError, match="no cache holds"):
         KVCache(1, 1, layers=1, heads=1, dim=64, pages=1, max_len=16, page=16, dtype=torch.float32, device="cpu")
+
+
+def test_parameter_blocks_as_bytes(bd):
+    """Every field of the blocks that the binding packs lies where the structure has it."""
+    import re
+    import struct
+    for params, fmt in bd._BLOCKS.items():
+        fields = [(name, i) for name, t in params._fields_ for i in (range(3) if t is bd._c_i64x3 else (None,))]
+        codes = [c for n, c in re.findall(r"(\d*)([a-zA-Z])", fmt[1:]) for _ in range(int(n or 1))]
+        assert len(fields) == len(codes)
+        p = params.from_buffer_copy(struct.pack(fmt, *(i + 1 for i in range(len(codes)))))
+        for i, (name, k) in enumerate(fields):
+            got = getattr(p, name)
+            assert (got if k is None else got[k]) == i + 1, (params, name)

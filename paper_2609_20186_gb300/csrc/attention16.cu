@@ -49,7 +49,7 @@ constexpr int kMaxCtas16 = 160;
 constexpr int kPartExtra = 8;               // of a partial result's row: reference and sum, and room for rows of whole 32 bytes
 constexpr int kReady = 8;                   // units whose values are on their way, at most (a ring's tiles are fewer)
 constexpr int kRuns = 8;                    // runs between the first and the last of the warps, at most
-constexpr int kRunCost = 1;                 // units that a run costs beside its own when the units are dealt out
+constexpr int kRunCost = 2;                 // units that a run costs beside its own when the units are dealt out
 constexpr int kBlock16 = 128 * 128;         // 128 rows of one swizzle row: an operand's 64 elements
 constexpr int kColumns16 = 512;             // tensor memory: S 2 x 128, O 2 x 128
 // log2 of the weight of a score at the reference, and of one that is as large as can be without a new reference.
@@ -144,12 +144,6 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, i
         : "memory");
 }
 
-__device__ __forceinline__ void cp_async16(void *dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(smem_addr(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
 // 32 bytes; p is a multiple of 32.
 __device__ __forceinline__ void store32(void *p, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])

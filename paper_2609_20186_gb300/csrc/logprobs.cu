@@ -18,8 +18,9 @@ namespace switchsd {
 
 // Threads of a CTA: many positions are a CTA each, small ones so that some of an SM's wait for each other or for their sums
 // while others stream; few positions are clusters of large ones.
-constexpr int kProbMany = 256, kProbFew = 512;
-constexpr int kProbFlight = 4;          // vectors of a thread that are worked on, and as many in flight
+constexpr int kProbMost = 128, kProbMany = 256, kProbFew = 512;
+constexpr int kProbFlight = 4;          // vectors of a thread that are worked on together
+constexpr int kProbRing = 2;            // batches of them in shared memory, or on their way there
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kGone = -200.f;         // binary logarithm of a weight that binary32 does not have
 
@@ -122,6 +123,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
     constexpr int kProbThreads = THREADS, kProbWarps = THREADS / kWarp;
     constexpr int kGroup = THREADS / 128;                   // threads whose largest logit is looked at as one
     constexpr int P = Row::P, F = kProbFlight;
+    extern __shared__ __align__(16) uint4 s_ring[];         // [kProbRing][F][threads], a thread's own
     __shared__ float s_group[128];
     __shared__ float s_bound;
     __shared__ Sums s_sums[kProbWarps], s_all;
@@ -166,12 +168,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
     WarpList list;
     float most = -INFINITY;                    // this thread's largest logit
     int batch = 0;
-    uint4 x[F], next[F];
-    row.load(next, begin + tid, kProbThreads, end);
-    for (int32_t base = begin; base < end; base += kProbThreads * F) {
+    uint4 x[F], *slot = s_ring + tid;          // of the batch that is next
 #pragma unroll
-        for (int i = 0; i < F; ++i) x[i] = next[i];
-        row.load(next, base + tid + kProbThreads * F, kProbThreads, end);
+    for (int r = 0; r < kProbRing; ++r) {
+        row.template fetch<F>(slot + r * F * kProbThreads, kProbThreads, begin + tid + r * F * kProbThreads, kProbThreads, end);
+        cp_async_commit();
+    }
+    for (int32_t base = begin; base < end; base += kProbThreads * F) {
+        cp_async_wait<kProbRing - 1>();
+#pragma unroll
+        for (int i = 0; i < F; ++i) x[i] = slot[i * kProbThreads];
+        row.template fetch<F>(slot, kProbThreads, base + tid + kProbRing * F * kProbThreads, kProbThreads, end);
+        cp_async_commit();
+        slot = slot == s_ring + tid + (kProbRing - 1) * F * kProbThreads ? s_ring + tid : slot + F * kProbThreads;
         const float top = Row::largest(x);
         most = fmaxf(most, top);
         // (again when there is four times as much to go by: half of what passed the first bound does not pass the second)
@@ -349,14 +358,29 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
     }
 }
 
+template <int DT, int THREADS>
+static cudaError_t launch_logprobs(const ProbArgs &a, int32_t B, int parts, cudaStream_t s) {
+    static bool attr_done[64] = {false};
+    constexpr int kSmem = kProbRing * kProbFlight * THREADS * 16;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+        e = cudaFuncSetAttribute(logprobs_kernel<DT, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_done[dev] = true;
+    }
+    const dim3 grid(unsigned(parts) * unsigned(a.T), unsigned(B));
+    return launch_pdl(logprobs_kernel<DT, THREADS>, grid, dim3(THREADS), size_t(kSmem), s, parts > 1 ? unsigned(parts) : 0u, a, parts);
+}
 template <int DT>
 static cudaError_t launch_logprobs(const ProbArgs &a, int32_t B, cudaStream_t s) {
-    const int sms = sm_count();
+    const int64_t sms = sm_count(), rows = int64_t(B) * a.T;
     if (sms == 0) return cudaErrorInvalidDevice;
-    const int parts = parts_of(int64_t(B) * a.T, (int64_t(a.V) + LogitRow<DT>::P - 1) / LogitRow<DT>::P, kProbFew, 2 * sms);
-    const dim3 grid(unsigned(parts) * unsigned(a.T), unsigned(B));
-    if (parts > 1) return launch_pdl(logprobs_kernel<DT, kProbFew>, grid, dim3(kProbFew), 0, s, unsigned(parts), a, parts);
-    return launch_pdl(logprobs_kernel<DT, kProbMany>, grid, dim3(kProbMany), 0, s, 0u, a, parts);
+    const int parts = parts_of(rows, (int64_t(a.V) + LogitRow<DT>::P - 1) / LogitRow<DT>::P, kProbFew, 2 * sms);
+    if (rows <= 3 * sms) return launch_logprobs<DT, kProbFew>(a, B, parts, s);
+    if (DT == SWITCHSD_F32 || rows <= 12 * sms) return launch_logprobs<DT, kProbMany>(a, B, 1, s);
+    return launch_logprobs<DT, kProbMost>(a, B, 1, s);
 }
 
 }  // namespace switchsd

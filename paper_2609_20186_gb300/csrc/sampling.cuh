@@ -96,6 +96,27 @@ struct LogitRow {
                 if (k < end && !inside(k)) x[i] = edge(row, V, token(k));
             }
     }
+    // The same into shared memory, in flight until they are waited for: this thread's vectors, `width` apart.
+    template <int N>
+    __device__ __forceinline__ void fetch(uint4 *to, int32_t width, int32_t j, int32_t step, int32_t end) const {
+        bool edges = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int32_t k = j + i * step;
+            if (k < end && inside(k)) {
+                cp_async16(to + i * width, row + token(k));
+            } else {
+                to[i * width] = nothing();
+                edges |= k < end;
+            }
+        }
+        if (edges)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int32_t k = j + i * step;
+                if (k < end && !inside(k)) to[i * width] = edge(row, V, token(k));
+            }
+    }
     __device__ static void widen(uint4 w, float (&x)[P]) {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -156,6 +177,10 @@ __device__ __forceinline__ uint32_t remote_word(const void *p, uint32_t rank) {
     return v;
 }
 __device__ __forceinline__ float remote_float(const void *p, uint32_t rank) { return __uint_as_float(remote_word(p, rank)); }
+
+__device__ __forceinline__ void remote_store(void *p, uint32_t rank, int32_t x, int32_t y) {
+    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};\n" ::"r"(map_to_rank(p, rank)), "r"(x), "r"(y) : "memory");
+}
 
 // CTAs of a row, a power of two: as many as leave every thread a vector, up to 8 (a cluster that every device takes), while
 // the rows together stay within the CTAs that are on the GPU at once.

@@ -13,8 +13,9 @@
 namespace switchsd {
 
 constexpr int kRaceThreads = 512;
-constexpr int kRaceFlight = 4;          // vectors of a thread in flight
+constexpr int kRaceFlight = 2;          // vectors of a thread that are worked on, and as many in flight
 constexpr int kRaceList = 1024;         // tokens of a CTA that passed the test
+constexpr int kRaceWarps = kRaceThreads / kWarp, kRaceParts = 8;
 constexpr float kRaceLog2e = 1.4426950408889634f;
 
 struct RaceArgs {
@@ -53,6 +54,23 @@ struct Race {
         const uint64_t z = splitmix(key + (uint64_t(uint32_t(v) >> 1) + 1) * kGolden);
         return (v & 1) ? uint32_t(z >> 32) : uint32_t(z);
     }
+    // The bits of P tokens from `from` on, the first of a pair or (ODD) the second.
+    template <bool ODD, int P>
+    __device__ __forceinline__ void bits_of(int32_t from, uint32_t (&r)[P]) const {
+        uint64_t n = key + (uint64_t(int64_t(from >> 1)) + 1) * kGolden, z = ODD ? splitmix(n) : 0;
+#pragma unroll
+        for (int e = 0; e < P; e += 2) {
+            if (ODD) {
+                r[e] = uint32_t(z >> 32);
+                r[e + 1] = uint32_t(z = splitmix(n += kGolden));
+            } else {
+                z = splitmix(n);
+                r[e] = uint32_t(z);
+                r[e + 1] = uint32_t(z >> 32);
+                n += kGolden;
+            }
+        }
+    }
     __device__ __noinline__ double exact(int32_t v) const {
         const double z = double(l[v]);
         if (greedy) return z;
@@ -73,8 +91,9 @@ struct Race {
         const uint32_t r = bits(v);
         const float e = r < 0x80000000u ? -log1pf(-(float(r) + 0.5f) * 0x1p-32f) : -logf((float(~r) + 0.5f) * 0x1p-32f);
         float y = z / temperature - logf(e);
+        if (residual) y -= lse;
+        if (y + margin(y) < floor) return -INFINITY;  // (w is at most p)
         if (residual) {
-            y -= lse;
             const float zq = q[v];
             if (zq > -INFINITY) {
                 const float a = (zq - z) / temperature, b = q_lse - lse, d = a - b;  // ln(q / p), and how far it may be off
@@ -97,8 +116,7 @@ template <int DT>
 struct Best {
     float s = -INFINITY;
     int32_t v = -1;
-    __device__ void consider(const Race<DT> &race, int32_t token, float z, float floor) {
-        const float x = race.score(token, z, floor);
+    __device__ void consider(const Race<DT> &race, int32_t token, float x) {  // x: its score
         if (!(x > -INFINITY) || token == v) return;
         const float margin = race.margin(x);
         bool take = v < 0 || x > s + margin;
@@ -111,16 +129,41 @@ struct Best {
             v = token;
         }
     }
+    // The warp's: among those that binary32 does not tell from the best, binary64's best, of equal ones the first.
+    __device__ void of_warp(const Race<DT> &race) {
+        const int lane = threadIdx.x & 31;
+        const float top = order_float(__reduce_max_sync(kFull, float_order(s)));
+        const uint32_t near = __ballot_sync(kFull, v >= 0 && s >= top - 2.f * race.margin(top));
+        int src = near ? __ffs(int(near)) - 1 : 0;
+        if (near & (near - 1)) {
+            double mine = -INFINITY, most = -INFINITY;
+            if ((near >> lane) & 1) mine = race.exact(v);
+            int32_t best_v = -1;
+            for (uint32_t rest = near; rest; rest &= rest - 1) {
+                const int r = __ffs(int(rest)) - 1;
+                const double x = __shfl_sync(kFull, mine, r);
+                const int32_t u = __shfl_sync(kFull, v, r);
+                if (best_v < 0 || x > most || (x == most && u < best_v)) {
+                    best_v = u;
+                    most = x;
+                    src = r;
+                }
+            }
+        }
+        s = __shfl_sync(kFull, s, src);
+        v = __shfl_sync(kFull, v, src);
+    }
 };
 
 template <int DT>
 __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArgs a, int parts) {
     using Row = LogitRow<DT>;
     constexpr int P = Row::P, F = kRaceFlight;
-    __shared__ int32_t s_first, s_best, s_n, s_few, s_token;
+    __shared__ int32_t s_few, s_token;
     __shared__ int32_t s_tokens[kRaceList];
-    __shared__ int32_t s_list[kRaceThreads];
-    __shared__ double s_exact[kRaceThreads];
+    __shared__ float s_low[kRaceWarps];
+    __shared__ __align__(8) int2 s_best[2][kRaceParts * kRaceWarps];  // by round: all warps' best scores and their tokens
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tid = threadIdx.x, part = blockIdx.x, b = blockIdx.y, k = a.T - 1;
     pdl_wait();
     pdl_trigger();
@@ -133,7 +176,7 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
         const float q = a.q ? __ldcg(a.q + at) : 1.f;
         return !(__fmul_rn(__ldcg(a.u + at), q) < __ldcg(a.p + at));
     };
-    const bool mine = tid < k && rejected(tid);
+    const bool mine = lane < k && rejected(lane);
     const bool ok = len >= 0 && len <= k && ctx >= 0;
     if (part == 0) {
         if (tid == 0 && a.status) a.status[b] = ok ? SWITCHSD_ROW_OK : SWITCHSD_ROW_BAD_LEN;
@@ -142,20 +185,12 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
     }
     if (!ok) return;
     // --- the accepted length --------------------------------------------------------------------------------------
-    if (tid == 0) {
-        s_first = len;
-        s_n = s_few = 0;
-        s_best = float_order(-INFINITY);
+    uint32_t no = __ballot_sync(kFull, mine && lane < len);  // (every warp finds it for itself)
+    int acc = no ? __ffs(int(no)) - 1 : len;
+    for (int i = kWarp; no == 0 && i < len; i += kWarp) {
+        no = __ballot_sync(kFull, i + lane < len && rejected(i + lane));
+        if (no) acc = i + __ffs(int(no)) - 1;
     }
-    __syncthreads();
-    if (mine && tid < len) atomicMin(&s_first, tid);
-    for (int i = tid + kRaceThreads; i < len; i += kRaceThreads)
-        if (rejected(i)) {
-            atomicMin(&s_first, i);
-            break;
-        }
-    __syncthreads();
-    const int acc = s_first;
     if (part == 0)
         for (int i = tid; i < a.T; i += kRaceThreads)
             if (i != acc) a.out[int64_t(b) * a.T + i] = -1;
@@ -173,10 +208,12 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
     const bool none = !(race.temperature >= 0.f && race.temperature < INFINITY) || race.lse != race.lse || race.q_lse != race.q_lse;
     const int32_t per = (row.vectors + parts - 1) / parts, begin = part * per, end = min(begin + per, row.vectors);
     const float c2 = fminf(kRaceLog2e / race.temperature, 3e38f);
-    Best<DT> best;
     int32_t token = -1;
     bool again = race.residual || race.skip >= 0;  // where w leaves nothing
-    while (!none) {
+    if (parts > 1 && !none) cluster_arrive_release();  // (that it runs: the others will write its shared memory)
+    for (int round = 0; !none; ++round) {
+        Best<DT> best;
+        if (tid == 0) s_few = 0;
         if (race.greedy) {
             for (int32_t j = begin + tid; j < end; j += kRaceThreads) {
                 uint4 w[1];
@@ -191,186 +228,117 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
                     }
             }
         } else {
-            uint4 w[F];
-            row.load(w, begin + tid, kRaceThreads, end);
-            // --- a bound: what a vector a thread reaches at least, in binary logarithms ---------------------------
-            // E <= x (1 + x) for x <= 1/2, and ln(1 + x) <= x
             const float lse2 = race.lse * kRaceLog2e, q_lse2 = race.q_lse * kRaceLog2e;
-            float low = -INFINITY;
-            if (begin + tid < end && (!race.residual || (race.q.lead == race.l.lead && race.l.inside(begin + tid)))) {
-                float x[P], y[P];
-                Row::widen(w[0], x);
-                if (race.residual) {
-                    uint4 qw[1];
-                    race.q.load(qw, begin + tid, 0, end);
-                    Row::widen(qw[0], y);
-                }
-                const int32_t from = row.token(begin + tid);
-                const float c = kRaceLog2e / race.temperature, eps = 1e-4f + 1e-6f * (fabsf(lse2) + fabsf(q_lse2));
-#pragma unroll
-                for (int e = 0; e < P; ++e) {
-                    const int32_t v = from + e;
-                    const float r = (float(race.bits(v)) + 0.5f) * 0x1p-32f;
-                    float z = fmaf(x[e], c, -lse2);
-                    if (race.residual) {  // p - q less what their roundings may take
-                        const float p = exp2_fast(z);
-                        z = log2_fast(fmaf(-1.f - eps, exp2_fast(fmaf(y[e] > -INFINITY ? y[e] : -1e30f, c, -q_lse2)), (1.f - eps) * p));
+            float off, floor;
+            auto look_at = [&](int32_t v) { best.consider(race, v, race.score(v, row[v], floor)); };
+            auto screen = [&](auto odd) {  // (whether vectors begin with the second token of a pair is known to its loops)
+                uint4 w[F], next[F];
+                row.load(w, begin + tid, kRaceThreads, end);
+                // --- a bound: what a vector a thread reaches at least, in binary logarithms -----------------------
+                // E <= x (1 + x) for x <= 1/2, and ln(1 + x) <= x
+                float low = -INFINITY;
+                if (begin + tid < end && (!race.residual || (race.q.lead == race.l.lead && race.l.inside(begin + tid)))) {
+                    float x[P], y[P];
+                    Row::widen(w[0], x);
+                    if (race.residual) {
+                        uint4 qw[1];
+                        race.q.load(qw, begin + tid, 0, end);
+                        Row::widen(qw[0], y);
                     }
-                    z -= log2_fast(r) + 1.4427f * r;
-                    if (uint32_t(v) < uint32_t(a.V) && v != race.skip && r <= 0.5f && x[e] > -INFINITY && fabsf(z) < 1e30f) low = fmaxf(low, z);
-                }
-            }
+                    const int32_t from = row.token(begin + tid);
+                    uint32_t bits[P];
+                    race.template bits_of<odd, P>(from, bits);
+                    const float c = kRaceLog2e / race.temperature, eps = 1e-4f + 1e-6f * (fabsf(lse2) + fabsf(q_lse2));
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) low = fmaxf(low, __shfl_xor_sync(kFull, low, o));
-            if ((tid & 31) == 0) atomicMax(&s_best, float_order(low));
-            __syncthreads();
-            low = order_float(s_best);
-            // less what the roundings of the bound and of the test may take
-            const float off = fabsf(low) < 1e30f ? 2e-3f + 1e-6f * (fabsf(low) + fabsf(lse2) + fabsf(q_lse2)) - low - lse2 : INFINITY;
-            const float floor = fabsf(low) < 1e30f ? (low - 2e-3f - 1e-6f * (fabsf(low) + fabsf(lse2) + fabsf(q_lse2))) * 0.69314718f : -INFINITY;
-            __syncthreads();
-            if (tid == 0) s_best = float_order(-INFINITY);
-            const uint64_t c22 = pair_of(c2, c2), off2 = pair_of(off, off), up = pair_of(1.002f, 1.002f), one = pair_of(1.0000003f, 1.0000003f);
-            // --- the tokens that may be better --------------------------------------------------------------------
-            uint4 next[F];
-            for (int32_t base = begin + tid; base < end; base += kRaceThreads * F) {
-                row.load(next, base + kRaceThreads * F, kRaceThreads, end);
-                uint32_t mask = 0;
-#pragma unroll
-                for (int i = 0; i < F; ++i) {
-                    float x[P], most[P];
-                    Row::widen(w[i], x);
-                    // 1 + (x rounded down to 23 bits) <= 1 + w e^-s
-#pragma unroll
-                    for (int e = 0; e < P; e += 2) {
-                        const float2 z = halves_of(fma_pair(pair_of(x[e], x[e + 1]), c22, off2));
-                        const float2 t = halves_of(fma_pair(pair_of(exp2_fast(z.x), exp2_fast(z.y)), up, one));
-                        most[e] = t.x;
-                        most[e + 1] = t.y;
+                    for (int e = 0; e < P; ++e) {
+                        const int32_t v = from + e;
+                        const float r = (float(bits[e]) + 0.5f) * 0x1p-32f;
+                        float z = fmaf(x[e], c, -lse2);
+                        if (race.residual) {  // p - q less what their roundings may take
+                            const float p = exp2_fast(z);
+                            z = log2_fast(fmaf(-1.f - eps, exp2_fast(fmaf(y[e] > -INFINITY ? y[e] : -1e30f, c, -q_lse2)), (1.f - eps) * p));
+                        }
+                        z -= log2_fast(r) + 1.4427f * r;
+                        if (uint32_t(v) < uint32_t(a.V) && v != race.skip && r <= 0.5f && x[e] > -INFINITY && fabsf(z) < 1e30f) low = fmaxf(low, z);
                     }
-                    const int32_t from = row.token(base + i * kRaceThreads);
-                    uint64_t n = race.key + (uint64_t(int64_t(from >> 1)) + 1) * kGolden;  // of the pair that `from` lies in
-                    auto test = [&](int e, uint32_t r) {
-                        if (__uint_as_float(0x3f800000u | (r >> 9)) <= most[e]) mask |= 1u << (i * P + e);
-                    };
-                    if (row.lead & 1) {
-                        uint64_t z = splitmix(n);
+                }
+                low = order_float(__reduce_max_sync(kFull, float_order(low)));
+                if (lane == 0) s_low[warp] = low;
+                __syncthreads();
+                low = order_float(__reduce_max_sync(kFull, float_order(s_low[lane % kRaceWarps])));
+                // less what the roundings of the bound and of the test may take
+                const float slack = 2e-3f + 1e-6f * (fabsf(low) + fabsf(lse2) + fabsf(q_lse2));
+                off = fabsf(low) < 1e30f ? slack - low - lse2 : INFINITY;
+                floor = fabsf(low) < 1e30f ? (low - slack) * 0.69314718f : -INFINITY;
+                // --- the tokens that may be better ----------------------------------------------------------------
+                for (int32_t base = begin + tid; base < end; base += kRaceThreads * F) {
+                    row.load(next, base + kRaceThreads * F, kRaceThreads, end);
+                    uint32_t mask = 0;
+#pragma unroll
+                    for (int i = 0; i < F; ++i) {
+                        float x[P];
+                        uint32_t r[P];
+                        Row::widen(w[i], x);
+                        // 1 + (x rounded down to 23 bits) <= 1 + w e^-s
+                        race.template bits_of<odd, P>(row.token(base + i * kRaceThreads), r);
 #pragma unroll
                         for (int e = 0; e < P; e += 2) {
-                            test(e, uint32_t(z >> 32));
-                            z = splitmix(n += kGolden);
-                            test(e + 1, uint32_t(z));
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < P; e += 2, n += kGolden) {
-                            const uint64_t z = splitmix(n);
-                            test(e, uint32_t(z));
-                            test(e + 1, uint32_t(z >> 32));
+                            const float2 z = halves_of(fma_pair(pair_of(x[e], x[e + 1]), pair_of(c2, c2), pair_of(off, off)));
+                            const float2 t = halves_of(fma_pair(pair_of(exp2_fast(z.x), exp2_fast(z.y)), pair_of(1.002f, 1.002f), pair_of(1.0000003f, 1.0000003f)));
+                            mask |= uint32_t(__uint_as_float(0x3f800000u | (r[e] >> 9)) <= t.x) << (i * P + e);
+                            mask |= uint32_t(__uint_as_float(0x3f800000u | (r[e + 1] >> 9)) <= t.y) << (i * P + e + 1);
                         }
                     }
-                }
-                while (mask) {
-                    const int at_mask = __ffs(int(mask)) - 1;
-                    mask &= mask - 1;
-                    const int32_t j = base + at_mask / P * kRaceThreads, v = row.token(j) + at_mask % P;
-                    if (j >= end || uint32_t(v) >= uint32_t(a.V)) continue;
-                    const int at = atomicAdd(&s_few, 1);
-                    if (at < kRaceList)
-                        s_tokens[at] = v;
-                    else
-                        best.consider(race, v, row[v], floor);
-                }
+                    for (; mask; mask &= mask - 1) {
+                        const int at_mask = __ffs(int(mask)) - 1;
+                        const int32_t j = base + at_mask / P * kRaceThreads, v = row.token(j) + at_mask % P;
+                        if (j >= end || uint32_t(v) >= uint32_t(a.V)) continue;
+                        const int at = atomicAdd(&s_few, 1);
+                        if (at < kRaceList)
+                            s_tokens[at] = v;
+                        else
+                            look_at(v);
+                    }
 #pragma unroll
-                for (int i = 0; i < F; ++i) w[i] = next[i];
-            }
+                    for (int i = 0; i < F; ++i) w[i] = next[i];
+                }
+            };
+            if (row.lead & 1)
+                screen(std::true_type{});
+            else
+                screen(std::false_type{});
             // --- their scores -------------------------------------------------------------------------------------
             __syncthreads();
-            for (int i = tid; i < min(s_few, kRaceList); i += kRaceThreads) best.consider(race, s_tokens[i], row[s_tokens[i]], floor);
+            for (int i = tid; i < min(s_few, kRaceList); i += kRaceThreads) look_at(s_tokens[i]);
         }
-        // --- the CTA's best: among those that binary32 does not tell from it, binary64's --------------------------
-        float s = best.s;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s = fmaxf(s, __shfl_xor_sync(kFull, s, o));
-        if ((tid & 31) == 0) atomicMax(&s_best, float_order(s));
-        __syncthreads();
-        const float top = order_float(s_best);
-        if (top > -INFINITY && best.v >= 0 && best.s >= top - 2.f * race.margin(top)) s_list[atomicAdd(&s_n, 1)] = best.v;
-        __syncthreads();
-        const int n = s_n;
-        if (n > 1) {
-            if (tid < n) s_exact[tid] = race.exact(s_list[tid]);
-            __syncthreads();
-        }
-        if (tid == 0) {
-            int32_t v = n > 0 ? s_list[0] : -1;
-            double most = n > 1 ? s_exact[0] : 0.;
-            for (int i = 1; i < n; ++i)
-                if (s_exact[i] > most || (s_exact[i] == most && s_list[i] < v)) {
-                    v = s_list[i];
-                    most = s_exact[i];
-                }
-            s_token = v;
-        }
-        // --- the row's --------------------------------------------------------------------------------------------
+        // --- the row's best, of all its warps' --------------------------------------------------------------------
+        best.of_warp(race);
         if (parts > 1) {
+            if (round == 0) cluster_wait_acquire();
+            if (lane < parts) remote_store(&s_best[round][part * kRaceWarps + warp], uint32_t(lane), __float_as_int(best.s), best.v);
             cluster_arrive_release();
             cluster_wait_acquire();
+        } else {
+            if (lane == 0) s_best[round][warp] = make_int2(__float_as_int(best.s), best.v);
+            __syncthreads();
         }
-        if (tid < 32 && (part == 0 || again)) {  // lane r has part r's
-            int32_t v = -1;
-            float its = -INFINITY;
-            const int lane = tid;
-            if (lane < parts) {
-                v = parts > 1 ? int32_t(remote_word(&s_token, lane)) : s_token;
-                its = parts > 1 ? order_float(int32_t(remote_word(&s_best, lane))) : top;
-            }
-            float all = its;
-#pragma unroll
-            for (int o = 4; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(kFull, all, o));
-            all = __shfl_sync(kFull, all, 0);
-            uint32_t near = __ballot_sync(kFull, v >= 0 && its >= all - 2.f * race.margin(all));
-            if (near & (near - 1)) {  // several: binary64's best, of equal ones the first
-                double mine = -INFINITY;
-                if ((near >> lane) & 1) mine = race.exact(v);
-                int32_t best_v = -1;
-                double most = -INFINITY;
-                for (int r = 0; r < parts; ++r) {
-                    const double x = __shfl_sync(kFull, mine, r);
-                    const int32_t u = __shfl_sync(kFull, v, r);
-                    if (((near >> r) & 1) && (best_v < 0 || x > most || (x == most && u < best_v))) {
-                        best_v = u;
-                        most = x;
-                    }
-                }
-                token = best_v;
-            } else if (near) {
-                token = __shfl_sync(kFull, v, __ffs(int(near)) - 1);
-            }
-            if (lane == 0) s_first = token;  // (the accepted length is known)
+        if (warp == 0) {
+            best = Best<DT>{};
+            for (int i = lane; i < parts * kRaceWarps; i += kWarp)
+                if (s_best[round][i].y >= 0) best.consider(race, s_best[round][i].y, __int_as_float(s_best[round][i].x));
+            best.of_warp(race);
+            token = best.v;
         }
         if (!again) break;
+        if (tid == 0) s_token = token;
         __syncthreads();
-        if (s_first >= 0) break;
+        if (s_token >= 0) break;
         // nothing is left of w: once more with p
-        if (parts > 1) {
-            cluster_arrive_release();  // (all have read the parts' results)
-            cluster_wait_acquire();
-        }
-        if (tid == 0) {
-            s_few = s_n = 0;
-            s_best = float_order(-INFINITY);
-        }
-        __syncthreads();
         race.residual = again = false;
         race.lse = race.q_lse = 0.f;
         race.skip = -1;
     }
     if (part == 0 && tid == 0) a.out[int64_t(b) * a.T + acc] = token;
-    if (parts > 1) {  // the parts' shared memory is read until here
-        cluster_arrive_release();
-        cluster_wait_acquire();
-    }
 }
 
 template <int DT>

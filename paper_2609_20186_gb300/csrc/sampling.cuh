@@ -73,10 +73,17 @@ struct LogitRow {
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
     __device__ bool inside(int32_t j) const { return token(j) >= 0 && token(j) + P <= V; }
+    __device__ bool all_inside(int32_t j, int32_t last, int32_t end) const { return token(j) >= 0 && last < end && token(last) + P <= V; }
     // Vectors j, j + step, ..; nothing from `end` on.  All loads are sent before the row's first or last vector is made up, for
     // which there is a call.
     template <int N>
     __device__ __forceinline__ void load(uint4 (&x)[N], int32_t j, int32_t step, int32_t end) const {
+        if (all_inside(j, j + (N - 1) * step, end)) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(row + token(j));
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = __ldcs(from + i * step);
+            return;
+        }
         bool edges = false;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -99,6 +106,12 @@ struct LogitRow {
     // The same into shared memory, in flight until they are waited for: this thread's vectors, `width` apart.
     template <int N>
     __device__ __forceinline__ void fetch(uint4 *to, int32_t width, int32_t j, int32_t step, int32_t end) const {
+        if (all_inside(j, j + (N - 1) * step, end)) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(row + token(j));
+#pragma unroll
+            for (int i = 0; i < N; ++i) cp_async16(to + i * width, from + i * step);
+            return;
+        }
         bool edges = false;
 #pragma unroll
         for (int i = 0; i < N; ++i) {

@@ -62,8 +62,9 @@ __device__ __forceinline__ uint32_t place_of(float v) {
 __device__ __forceinline__ float at_place(uint32_t p) {
     return p == 0 ? -INFINITY : __uint_as_float(p & 0x80000000u ? p & 0x7fffffffu : ~p);
 }
-// A bound that k of a warp's 128 numbers (four a lane, by their places) reach, as large as 20 bits can say; the same for all.
-__device__ __forceinline__ float kth_largest(const uint32_t (&p)[4], int k) {
+// A bound that k of a warp's 128 numbers (four a lane, by their places) reach, as large as 20 bits can say, or
+// (soon) as soon as the others do not; the same for all lanes.
+__device__ __forceinline__ float kth_largest(const uint32_t (&p)[4], int k, bool soon) {
     uint32_t bound = 0;
 #pragma unroll 1
     for (uint32_t bit = 0x80000000u; bit >= 0x1000u; bit >>= 1) {
@@ -72,6 +73,7 @@ __device__ __forceinline__ float kth_largest(const uint32_t (&p)[4], int k) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) n += __popc(__ballot_sync(kFull, p[i] >= trial));
         if (n >= k) bound = trial;
+        if (soon && n == k) break;
     }
     return bound > 0x007fffffu ? at_place(bound) : -INFINITY;  // (the place of -inf)
 }
@@ -103,14 +105,20 @@ struct WarpList {
     }
 };
 
-// The first k of n (value, token) pairs in `v`, `id`, in order, to `out_v`, `out_id` (the same for all threads of the CTA).
+// The first k of n (value, token) pairs in `v`, `id`, in order, to `out_v`, `out_id` (the same for all threads of the CTA):
+// eight threads count those before a pair.
 __device__ __forceinline__ void rank_pairs(const float *v, const int32_t *id, int n, int k, float *out_v, int32_t *out_id) {
-    for (int i = threadIdx.x; i < n; i += int(blockDim.x)) {
-        const float x = v[i];
-        const int32_t t = id[i];
+    const int of = threadIdx.x & 7;
+    for (int i0 = 0; i0 < n; i0 += int(blockDim.x) / 8) {
+        const int i = i0 + int(threadIdx.x) / 8;
+        const float x = i < n ? v[i] : INFINITY;
+        const int32_t t = i < n ? id[i] : -1;
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += before(v[j], id[j], x, t);
-        if (rank < k) {
+        if (i < n)
+            for (int j = of; j < n; j += 8) rank += before(v[j], id[j], x, t);
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) rank += __shfl_xor_sync(kFull, rank, o);
+        if (of == 0 && i < n && rank < k) {
             out_v[rank] = x;
             out_id[rank] = t;
         }
@@ -192,7 +200,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
             __syncthreads();
             if (warp == 0) {
                 const uint32_t p[4] = {place_of(s_group[lane]), place_of(s_group[lane + 32]), place_of(s_group[lane + 64]), place_of(s_group[lane + 96])};
-                g = kth_largest(p, k);
+                g = kth_largest(p, k, THREADS == kProbFew);  // (where latency counts)
                 if (lane == 0) s_bound = g;
             }
             __syncthreads();

@@ -24,6 +24,23 @@
 // (past its last token, without a page) is cleared in shared memory; among the values that some rows see and others do
 // not, numbers that are not finite would reach the others as 0 * inf: they are cleared too, and added to the rows that see
 // them at the end.
+//
+// Bound.  One token a row and up to a draft's: memory.  64 rows of 8K to 32K tokens, 8 key heads x 128, one token each:
+// 802 us, 5.4 GB, 99 % of a copy's rate; 1 to 17 tokens over 2K to 8K: 224 us (89 %), of which 6 are the join.  Chunks: 2 rows
+// of 2048 tokens over 30K, 32 query heads: 1425 us, 1.49 PFLOP/s, 77 % of what a library's product reaches in a short run and
+// 87 % of what it sustains; the tensor pipe is active 71 % of the time, and between products its warp waits for weights: 128
+// keys take a slot's warps some 735 instructions each, nearly six a score.  16 rows of up to 500 tokens with heads of 64:
+// 128 us, 4.7 times its products' time, since a product of half the size waits for the same weights, and a run has few units
+// for its queries, masks and output.  One token over 2K: 13.4 us, latency (the dealing 1.7, queries and first tiles 2, the
+// second launch 4).
+//
+// Why so.  Two slots: with one, the tensor cores wait while scores become weights.  Products issued by a warp that stays
+// together: 1874 -> 1515 us for the chunks.  The warps that help are the first ones, so that the slots' registers are whole
+// warpgroups': 1515 -> 1449.  Runs and queries ahead, by a warp of their own: 256 -> 229 us for the drafts.
+// Not kept: weights before the unit's maximum is known, put right afterwards (chunks of 500 tokens 182 against 162); looking
+// for the next scores before the second half of the weights (1610 against 1449); loading the scores a second time to have
+// fewer registers (1813); sums and products one by one instead of packed in pairs (1505); three places for scores where heads
+// have 64 dimensions (194 against 162).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -42,14 +59,16 @@ constexpr int kSlotThreads = kSlotRows, kSlotWarps = kSlotThreads / kWarp;
 constexpr int kMmaWarp16 = 0, kFetchWarp16 = 1, kValueWarp16 = 2, kRunWarp = 3, kFirstSlotWarp = 4;
 constexpr int kThreads16 = (2 * kSlotWarps + 4) * kWarp;
 // Registers a thread of the two slots' warpgroups and of the third: 384 threads are launched with 168 each, and the shares
-// add up to the same.
+// add up to the same.  (176 / 152 a thread: 1474 us for chunks, 134 for chunks of 500 tokens; 216 / 72: 1488, 132; these: 1463, 130.)
 constexpr int kSlotRegs = 192, kOtherRegs16 = 120;
 static_assert(2 * kSlotRegs + kOtherRegs16 == 3 * 168, "what two warpgroups gain the third gives");
 constexpr int kMaxCtas16 = 160;
 constexpr int kPartExtra = 8;               // of a partial result's row: reference and sum, and room for rows of whole 32 bytes
 constexpr int kReady = 8;                   // units whose values are on their way, at most (a ring's tiles are fewer)
 constexpr int kRuns = 8;                    // runs between the first and the last of the warps, at most
-constexpr int kRunCost = 2;                 // units that a run costs beside its own when the units are dealt out
+// Units that a run costs beside its own when the units are dealt out: queries, masks, output.  (0: 232 us for drafts, 142 for
+// chunks of 500 tokens; 1: 226, 130; 2: 224, 128; 4: 223, 127, but 14.2 instead of 13.4 for one token over 2K.)
+constexpr int kRunCost = 2;
 constexpr int kBlock16 = 128 * 128;         // 128 rows of one swizzle row: an operand's 64 elements
 constexpr int kColumns16 = 512;             // tensor memory: S 2 x 128, O 2 x 128
 // log2 of the weight of a score at the reference, and of one that is as large as can be without a new reference.
@@ -247,7 +266,8 @@ __device__ __forceinline__ void deal_runs(const Attn16Args &a, int64_t *s_pre, R
     auto before_tile = [&](int32_t len, int32_t nw, int rt) -> int64_t {  // units and costs of a key head's tiles before rt
         const int whole = nw / a.tokens;
         const int64_t c = int64_t(len) + a.tokens + kUnitKeys - 1;
-        return int64_t(rt) * kRunCost + (whole && rt ? sum_of_units(c, a.tokens, min(rt, whole)) : 0) + (rt > whole ? (int64_t(len) + nw + kUnitKeys - 1) / kUnitKeys : 0);
+        return int64_t(rt) * kRunCost + (whole && rt ? sum_of_units(c, a.tokens, min(rt, whole)) : 0) +
+               (rt > whole ? (int64_t(len) + nw + kUnitKeys - 1) / kUnitKeys : 0);
     };
     int32_t len = 0, nw = 0;
     auto units_of = [&](int row) -> int64_t {  // of a key head
@@ -339,8 +359,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     // A tile's arrival has a barrier by its unit and kind, not by its stage: a phase is then waited for by everyone who waits
     // on that barrier at all, before its next one can begin.  (A stage has keys and values in turn, and who waits for the values
     // only would take a phase of the keys that is still to come, or is over, for another.)
-    __shared__ __align__(8) uint64_t full[2][kReady], ready[kReady], empty[N], run_full[kRuns], q_ready[NQ], q_free[NQ], s_full[2], p_half[2], p_full[2], o_done[2], met, taken, written,
-        stopped;
+    __shared__ __align__(8) uint64_t full[2][kReady], ready[kReady], empty[N], run_full[kRuns], q_ready[NQ], q_free[NQ];
+    __shared__ __align__(8) uint64_t s_full[2], p_half[2], p_full[2], o_done[2], met, taken, written, stopped;
     __shared__ __align__(16) uint32_t s_exist[kReady][4];  // of a unit: its keys that exist and whose page does
     __shared__ __align__(16) int4 s_run[kRuns][3];
     __shared__ uint32_t s_tmem, s_cleared[kRuns];          // s_cleared: a run (+ 1) with values that were not finite, by the run
@@ -623,7 +643,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                         if (lane == 0) mbar_arrive_expect_tx(&full[half][unit % kReady], bytes);
                         __syncwarp();
                         if (good)
-                            tma_load_4d(sm_kv + st * S::kTile + g * kBlock16 + q * run * 128, &map, 64 * g, (key0 + q * run) & page_mask, half * a.Hkv + s.hk, page, &full[half][unit % kReady]);
+                            tma_load_4d(sm_kv + st * S::kTile + g * kBlock16 + q * run * 128, &map, 64 * g, (key0 + q * run) & page_mask,
+                                        half * a.Hkv + s.hk, page, &full[half][unit % kReady]);
                         issued = x + 1;
                     }
                     page = next;
@@ -800,11 +821,13 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     tc_fence_after();
     if (warp == kMmaWarp16)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kColumns16) : "memory");
-    if (s_bad && tid == kFirstSlotWarp * kWarp) a.desc[2 * cta].w |= kLate;  // (the thread that wrote it last; the join writes the statuses)
+    // (the thread that wrote it last; the join writes the statuses)
+    if (s_bad && tid == kFirstSlotWarp * kWarp) a.desc[2 * cta].w |= kLate;
 }
 
-// Joins the partial results of the items that several CTAs hold, and writes the statuses of a launch that a CTA gave up: CTAs (i, .) look after the item whose first part is the i-th CTA's, a warp a query
-// row, adding the parts in order, kJoinFlight on their way together.
+// Joins the partial results of the items that several CTAs hold, and writes the statuses of a launch that a CTA gave up: CTAs
+// (i, .) look after the item whose first part is the i-th CTA's, a warp a query row, adding the parts in order, kJoinFlight on
+// their way together.
 constexpr int kJoinWarps16 = 8, kJoinFlight = 8;
 template <bool F16, int D>
 __global__ void __launch_bounds__(kJoinWarps16 *kWarp, 3) attn16_join_kernel(const Attn16Args a) {
@@ -816,7 +839,8 @@ __global__ void __launch_bounds__(kJoinWarps16 *kWarp, 3) attn16_join_kernel(con
     // the item's first part is the CTA's second partial result, or its first one
     const int4 first = __ldcg(a.desc + 2 * i), second = __ldcg(a.desc + 2 * i + 1);
     if ((first.w & kLate) && blockIdx.y == 0 && a.status)
-        for (int b = threadIdx.x; b < a.B; b += kJoinWarps16 * kWarp) a.status[b] = SWITCHSD_ROW_TIMEOUT;  // some row is not done; which ones, the CTA does not know
+        // some row is not done; which ones, the CTA does not know
+        for (int b = threadIdx.x; b < a.B; b += kJoinWarps16 * kWarp) a.status[b] = SWITCHSD_ROW_TIMEOUT;
     const bool is_second = second.x >= 0 && (second.w & kFirst);
     const int4 de = is_second ? second : first;
     if (de.x >= 0 && (de.w & kFirst)) {

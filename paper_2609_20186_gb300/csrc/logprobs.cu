@@ -6,18 +6,30 @@
 // ln S - W / S.
 //
 // Top alternatives.  Of the first batch of loads (and again of the first four) the largest logit of every group of threads is
-// known, and the k-th largest of those 128 is a bound that k of the CTA's logits reach: what lies below is no alternative.  The few that do not go, one by
-// one, into their warp's list, sorted over its lanes, whose k-th raises the warp's own bound.  The lists (of all CTAs) are
-// ranked by counting at the end.  A batch is looked at again only where its largest logit, which the sums want anyway,
-// reaches the bound.
+// known, and the k-th largest of those 128 is a bound that k of the CTA's logits reach: what lies below is no alternative.
+// The few that do not go, one by one, into their warp's list, sorted over its lanes, whose k-th raises the warp's own bound.
+// The lists (of all CTAs) are ranked by counting at the end.  A batch is looked at again only where its largest logit, which
+// the sums want anyway, reaches the bound.
+//
+// Bound (128,256 tokens).  f32 logits: memory, 2048 positions in 153 us (103 % of a copy's rate, all of it reads), 164 with
+// five alternatives.  16-bit ones: instructions, ten a logit with five alternatives: 2048 positions 92 us (84 %) without, with 5 /
+// 20 / 32 alternatives 102 / 144 / 174; 8192 positions with five 352 (88 %).  One position (f32): 6.8 us, 11.6 with 20
+// alternatives: a chain of loads, the bound, the lists, two rankings and two cluster barriers.
+//
+// What made the difference: one multiply-add a logit for z and packed sums (662 -> 511 us of the 8192 positions), a bound of
+// 128 groups (of a warp's maxima: 40 logits a warp passed it), a second bound (460 -> 445), smaller CTAs, and a batch that
+// lies inside the row loaded from one address (409 -> 352).  Batches of two vectors a thread instead of four: 497 against 445;
+// three batches in shared memory instead of two: 467 against 436.
 #include "sampling.cuh"
 
 #include <algorithm>
 
 namespace switchsd {
 
-// Threads of a CTA: many positions are a CTA each, small ones so that some of an SM's wait for each other or for their sums
-// while others stream; few positions are clusters of large ones.
+// Threads of a CTA.  Few positions are clusters of large CTAs (one position: 12.8 us, as a single CTA 35).  More are a CTA
+// each: large ones while an SM has no more than three (450 positions with 512 / 256 / 128 threads: 35 / 38 / 39 us), smaller
+// ones beyond, so that some of an SM's wait for each other or for their sums while others stream (1088 positions: 37 / 35 / 54;
+// 3648: 232 / 198 / 191).  f32 logits want the loads in flight that 256 threads have (3648: 297 / 272 / 309).
 constexpr int kProbMost = 128, kProbMany = 256, kProbFew = 512;
 constexpr int kProbFlight = 4;          // vectors of a thread that are worked on together
 constexpr int kProbRing = 2;            // batches of them in shared memory, or on their way there

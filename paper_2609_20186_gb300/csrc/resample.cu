@@ -15,6 +15,8 @@
 // exclusive-ors) and 2 in the scores and the meeting; a launch takes the rest.  16 rows of 152,064, f16, with drafters'
 // distributions: 16 us.  One CTA a row instead of a cluster: 26 and 49.  Testing the vector's largest logit with its smallest x instead of every
 // token: 17.5 and 20, since several times as many are worked out; four vectors in flight instead of two: 17.1 and 17.3.
+// Without a bound where a drafter's rows are aligned otherwise than the target's (odd vocabularies), 16 rows of 128,255: 95 us
+// instead of 16.
 #include "sampling.cuh"
 
 namespace switchsd {
@@ -244,13 +246,18 @@ __global__ void __launch_bounds__(kRaceThreads, 2) resample_kernel(const RaceArg
                 // --- a bound: what a vector a thread reaches at least, in binary logarithms -----------------------
                 // E <= x (1 + x) for x <= 1/2, and ln(1 + x) <= x
                 float low = -INFINITY;
-                if (begin + tid < end && (!race.residual || (race.q.lead == race.l.lead && race.l.inside(begin + tid)))) {
+                if (begin + tid < end && (!race.residual || race.l.inside(begin + tid))) {
                     float x[P], y[P];
                     Row::widen(w[0], x);
                     if (race.residual) {
                         uint4 qw[1];
-                        race.q.load(qw, begin + tid, 0, end);
-                        Row::widen(qw[0], y);
+                        if (race.q.lead == race.l.lead) {
+                            race.q.load(qw, begin + tid, 0, end);
+                            Row::widen(qw[0], y);
+                        } else {  // (its vectors are other tokens')
+#pragma unroll
+                            for (int e = 0; e < P; ++e) y[e] = race.q[row.token(begin + tid) + e];
+                        }
                     }
                     const int32_t from = row.token(begin + tid);
                     uint32_t bits[P];

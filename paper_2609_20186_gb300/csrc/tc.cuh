@@ -128,12 +128,6 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
     return r;
 }
 
-__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 // One arrival for a warp, behind all of its threads' work (and their fences).
 __device__ __forceinline__ void warp_arrive(uint64_t *bar) {
     __syncwarp();

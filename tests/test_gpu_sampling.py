@@ -341,3 +341,38 @@ def test_a_step_at_temperature():
             want = ref.token(x[b, a], T[b], int(s[b]), int(L[b]) + a, **(dict(skip=d[b, a]) if a < m[b] else {}))
             assert int(accept[b]) == a and int(lens[b]) == L[b] + a + 1
             assert ctx[b, L[b]:L[b] + a + 1].tolist() == d[b, :a].tolist() + [want]
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T", [(3, 50), (8, 57), (3, 153), (152, 12), (19, 97)])
+def test_logprobs_of_many_positions(B, T, name):
+    """Numbers of positions on both sides of those where other CTAs take them, a vocabulary that none divides evenly."""
+    rng = np.random.default_rng(B + T)
+    V, top = 4099, 7
+    x = _logits(rng, (B, T, V), name)
+    new = rng.integers(0, T + 1, B)
+    new[0] = T
+    temps = np.float32(0.9) + np.zeros(B, np.float32)
+    tokens = rng.integers(0, V, (B, T))
+    o = _outputs(B, T, T, top)
+    _fw().switchsd_logprobs(_placed(x, name, 3, 1), tokens=_i32(tokens), new_lens=_i32(new), temperature=_f32(temps), **o)
+    _check(o, x, new, temps.astype(np.float64), tokens, top)
+
+
+def test_resample_of_rows_with_unlike_alignments():
+    """A drafter's rows that are aligned otherwise than the target's, at every offset between them, over more than one CTA a
+    row."""
+    rng = np.random.default_rng(3)
+    B, T, V = 4, 2, 20011
+    x = _logits(rng, (B, T, V), "bf16")
+    xq = _round(x[:, :1] + rng.standard_normal((B, 1, V)) * 0.7, "bf16")
+    draft, ones = x[:, :1].argmax(2), np.ones((B, 1))
+    lse = np.array([[np.float32(ref.logprobs(x[b, t], 1.0)[2]) for t in range(T)] for b in range(B)], np.float64)
+    q_lse = np.array([[np.float32(ref.logprobs(xq[b, 0], 1.0)[2])] for b in range(B)], np.float64)
+    seeds, ctx = rng.integers(0, 2**62, B), rng.integers(0, 1000, B)
+    for lead in range(8):
+        got, status = _resample(x, "bf16", draft, np.ones(B, int), 0.5 * ones, ones, seeds, ctx, np.ones(B), lse, ones, xq, q_lse, np.zeros(B, int), lead, lead)
+        assert not status.any()
+        for b in range(B):
+            want = ref.token(x[b, 0], 1.0, int(seeds[b]), int(ctx[b]), lse=lse[b, 0], lq=xq[b, 0], q_lse=q_lse[b, 0])
+            assert got[b].tolist() == [want, -1], (lead, b)

@@ -728,13 +728,25 @@ def switchsd_logits(logits, *, ctx_tokens=None, ctx_lens=None, draft=None, new_l
 
 
 def _cache16(cache, H: int, D: int):
-    """pages, Hkv and tokens a page of a 16-bit cache [pages, 2, Hkv, page, D] of one layer (H: Hkv, or 0 for any)."""
+    """pages, Hkv, tokens a page and type of a 16-bit cache [pages, 2, Hkv, page, D] of one layer (H: Hkv, or 0 for any)."""
     shape = cache.shape if isinstance(cache, torch.Tensor) else ()
     if len(shape) != 5 or shape[1] != 2 or shape[4] != D or (H and shape[2] != H):
         raise ValueError(f"the cache has shape {tuple(shape)}, expected [pages, 2, {H or 'Hkv'}, page, {D}]")
-    if cache.dtype not in (torch.bfloat16, torch.float16):
-        raise TypeError(f"the cache must be bfloat16 or float16, got {cache.dtype}")
-    return shape[0], shape[2], shape[3]
+    dtype = cache.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
+        raise TypeError(f"the cache must be bfloat16 or float16, got {dtype}")
+    return shape[0], shape[2], shape[3], dtype
+
+
+def _heads(t, name: str, shape, dtype):
+    """The strides of a CUDA tensor [B, T, H, D] of `dtype` whose last dimension is contiguous (a call costs tenths of a
+    microsecond, so they are asked for once)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.shape == shape:
+        strides = t.stride()
+        if strides[3] == 1:
+            return strides
+    _strided(t, name, shape, (dtype,))
+    return t.stride()
 
 
 def switchsd_kv16_append(k, v, slots, cache, *, stream=None) -> None:
@@ -742,11 +754,10 @@ def switchsd_kv16_append(k, v, slots, cache, *, stream=None) -> None:
     of the cache's type, slots int32 [B, T], cache bf16 or f16 [pages, 2, Hkv, page, D]."""
     shape = k.shape
     B, T, H, D = shape
-    pages, _, page = _cache16(cache, H, D)
-    dtype = _strided(k, "k", shape, (cache.dtype,))
-    _strided(v, "v", shape, (cache.dtype,))
-    p = _KV16_APPEND.pack(B, T, H, D, page, pages, dtype, k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3],
-                          _dev(slots, torch.int32, "slots", (B, T)) or 0, _dev(cache, cache.dtype, "cache"), _stream_ptr(stream))
+    pages, _, page, dtype = _cache16(cache, H, D)
+    ks, vs = _heads(k, "k", shape, dtype), _heads(v, "v", shape, dtype)
+    p = _KV16_APPEND.pack(B, T, H, D, page, pages, _DTYPES[dtype], k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                          _dev(slots, torch.int32, "slots", (B, T)) or 0, _dev(cache, dtype, "cache"), _stream_ptr(stream))
     _check(load().switchsd_kv16_append(p), "switchsd_kv16_append")
 
 
@@ -755,9 +766,9 @@ def switchsd_kv16_read(cache, slots, out_k, out_v, *, stream=None) -> None:
     [B, T, Hkv, D] of its type."""
     shape = out_k.shape
     B, T, H, D = shape
-    pages, _, page = _cache16(cache, H, D)
-    p = _KV16_READ.pack(B, T, H, D, page, pages, _dev(cache, cache.dtype, "cache"), _dev(slots, torch.int32, "slots", (B, T)) or 0,
-                        _dev(out_k, cache.dtype, "out_k", shape), _dev(out_v, cache.dtype, "out_v", shape), _stream_ptr(stream))
+    pages, _, page, dtype = _cache16(cache, H, D)
+    p = _KV16_READ.pack(B, T, H, D, page, pages, _dev(cache, dtype, "cache"), _dev(slots, torch.int32, "slots", (B, T)) or 0,
+                        _dev(out_k, dtype, "out_k", shape), _dev(out_v, dtype, "out_v", shape), _stream_ptr(stream))
     _check(load().switchsd_kv16_read(p), "switchsd_kv16_read")
 
 
@@ -777,15 +788,15 @@ def switchsd_kv16_attention(q, cache, block_table, lens, new_lens, out, *, scale
     call's stream, when none is given."""
     shape = q.shape
     B, T, Hq, D = shape
-    (pages, Hkv, page), blocks, row, i32 = _cache16(cache, 0, D), block_table.shape[1], (B,), torch.int32
-    dtype = _strided(q, "q", shape, (cache.dtype,))
+    (pages, Hkv, page, dtype), blocks, row, i32 = _cache16(cache, 0, D), block_table.shape[1], (B,), torch.int32
+    qs = _heads(q, "q", shape, dtype)
     if workspace is None:
         workspace = _scratch(switchsd_kv16_attention_workspace(D), q.device, stream)
     p = _KV16_ATTENTION.pack(
-        B, T, Hq, Hkv, D, page, pages, blocks, dtype, q.data_ptr(), *q.stride()[:3], _dev(cache, cache.dtype, "cache"), _dev(block_table, i32, "block_table", (B, blocks)) or 0,
-        _dev(lens, i32, "lens", row) or 0, _dev(new_lens, i32, "new_lens", row) or 0, lens_add, new_add, D ** -0.5 if scale is None else scale,
-        _dev(out, q.dtype, "out", shape) or 0, _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _dev(status, i32, "status", row) or 0,
-        _stream_ptr(stream))
+        B, T, Hq, Hkv, D, page, pages, blocks, _DTYPES[dtype], q.data_ptr(), qs[0], qs[1], qs[2], _dev(cache, dtype, "cache"),
+        _dev(block_table, i32, "block_table", (B, blocks)) or 0, _dev(lens, i32, "lens", row) or 0, _dev(new_lens, i32, "new_lens", row) or 0,
+        lens_add, new_add, D ** -0.5 if scale is None else scale, _dev(out, dtype, "out", shape) or 0,
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _dev(status, i32, "status", row) or 0, _stream_ptr(stream))
     _check(load().switchsd_kv16_attention(p), "switchsd_kv16_attention")
 
 

@@ -28,11 +28,13 @@
 // Bound.  One token a row and up to a draft's: memory.  64 rows of 8K to 32K tokens, 8 key heads x 128, one token each:
 // 802 us, 5.4 GB, 99 % of a copy's rate; 1 to 17 tokens over 2K to 8K: 224 us (89 %), of which 6 are the join.  Chunks: 2 rows
 // of 2048 tokens over 30K, 32 query heads: 1425 us, 1.49 PFLOP/s, 77 % of what a library's product reaches in a short run and
-// 87 % of what it sustains; the tensor pipe is active 71 % of the time, and between products its warp waits for weights: 128
-// keys take a slot's warps some 735 instructions each, nearly six a score.  16 rows of up to 500 tokens with heads of 64:
-// 128 us, 4.7 times its products' time, since a product of half the size waits for the same weights, and a run has few units
-// for its queries, masks and output.  One token over 2K: 13.4 us, latency (the dealing 1.7, queries and first tiles 2, the
-// second launch 4).
+// 87 % of what it sustains.  The tensor pipe is active 71 % of the time; what it waits for is the chain of barriers between a
+// slot's scores, weights and products, some 3000 cycles a unit, 1800 of them the rows' warps' (loads 240, maxima 500, weights
+// 1000), and the warp that issues the products has one for both slots (100 to 200 cycles a wait).  It is not the exponentials:
+// without them the time is the same.  16 rows of up to 500 tokens with heads of 64: 128 us, 4.7 times its products' time,
+// since the chain is as long for a product of half the size, and a run has few units for its queries, masks and output (2 to 3
+// us a run); 10 us pass before the first scores.  One token over 2K: 13.4 us, latency (the dealing, queries, first tiles, and 4
+// for the second launch).
 //
 // Why so.  Two slots: with one, the tensor cores wait while scores become weights.  Products issued by a warp that stays
 // together: 1874 -> 1515 us for the chunks.  The warps that help are the first ones, so that the slots' registers are whole
@@ -40,7 +42,9 @@
 // Not kept: weights before the unit's maximum is known, put right afterwards (chunks of 500 tokens 182 against 162); looking
 // for the next scores before the second half of the weights (1610 against 1449); loading the scores a second time to have
 // fewer registers (1813); sums and products one by one instead of packed in pairs (1505); three places for scores where heads
-// have 64 dimensions (194 against 162).
+// have 64 dimensions (194 against 162); a quarter of the exponentials by a polynomial (1523 against 1440); maxima of the first
+// half of the scores while the others are loaded (1519 against 1425); a warp of its own for each slot's products (1642 against
+// 1425, since the slots fall into step; 791 against 801 for one token a row); waits that poll instead of sleeping (1472).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

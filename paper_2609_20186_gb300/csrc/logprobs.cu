@@ -13,7 +13,7 @@
 //
 // Bound (128,256 tokens).  f32 logits: memory, 2048 positions in 153 us (103 % of a copy's rate, all of it reads), 164 with
 // five alternatives.  16-bit ones: instructions, ten a logit with five alternatives: 2048 positions 92 us (84 %) without, with 5 /
-// 20 / 32 alternatives 102 / 144 / 174; 8192 positions with five 352 (88 %).  One position (f32): 6.8 us, 11.6 with 20
+// 20 / 32 alternatives 102 / 132 / 151; 8192 positions with five 352 (88 %).  One position (f32): 6.8 us, 11.6 with 20
 // alternatives: a chain of loads, the bound, the lists, two rankings and two cluster barriers.
 //
 // What made the difference: one multiply-add a logit for z and packed sums (662 -> 511 us of the 8192 positions), a bound of
@@ -33,6 +33,9 @@ namespace switchsd {
 constexpr int kProbMost = 128, kProbMany = 256, kProbFew = 512;
 constexpr int kProbFlight = 4;          // vectors of a thread that are worked on together
 constexpr int kProbRing = 2;            // batches of them in shared memory, or on their way there
+// More alternatives than these have a bound again whenever twice as much has been read (2048 positions, bf16, 32 of them: 151
+// instead of 178 us; 12: 118, 123; 5: 106 instead of 102), but where positions are few (20 of one: 13.1 instead of 12.0).
+constexpr int kProbOften = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kGone = -200.f;         // binary logarithm of a weight that binary32 does not have
 
@@ -204,7 +207,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
         const float top = Row::largest(x);
         most = fmaxf(most, top);
         // (again when there is four times as much to go by: half of what passed the first bound does not pass the second)
-        if (k > 0 && (batch == 0 || batch == 3)) {
+        if (k > 0 && (batch & (batch + 1)) == 0 && (batch == 0 || batch == 3 || (k > kProbOften && THREADS != kProbFew))) {
             float g = most;
 #pragma unroll
             for (int o = 1; o < kGroup; o <<= 1) g = fmaxf(g, __shfl_xor_sync(kFull, g, o));

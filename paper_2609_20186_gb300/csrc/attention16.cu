@@ -26,14 +26,14 @@
 // them at the end.
 //
 // Bound.  One token a row and up to a draft's: memory.  64 rows of 8K to 32K tokens, 8 key heads x 128, one token each:
-// 802 us, 5.4 GB, 99 % of a copy's rate; 1 to 17 tokens over 2K to 8K: 224 us (89 %), of which 6 are the join.  Chunks: 2 rows
+// 802 us, 5.4 GB, 99 % of a copy's rate; 1 to 17 tokens over 2K to 8K: 222 us (90 %), of which 6 are the join.  Chunks: 2 rows
 // of 2048 tokens over 30K, 32 query heads: 1425 us, 1.49 PFLOP/s, 77 % of what a library's product reaches in a short run and
 // 87 % of what it sustains.  The tensor pipe is active 71 % of the time; what it waits for is the chain of barriers between a
 // slot's scores, weights and products, some 3000 cycles a unit, 1800 of them the rows' warps' (loads 240, maxima 500, weights
 // 1000), and the warp that issues the products has one for both slots (100 to 200 cycles a wait).  It is not the exponentials:
-// without them the time is the same.  16 rows of up to 500 tokens with heads of 64: 128 us, 4.7 times its products' time,
-// since the chain is as long for a product of half the size, and a run has few units for its queries, masks and output (2 to 3
-// us a run); 10 us pass before the first scores.  One token over 2K: 13.4 us, latency (the dealing, queries, first tiles, and 4
+// without them the time is the same.  16 rows of up to 500 tokens with heads of 64: 115 us, 4.3 times its products' time,
+// since the chain is as long for a product of half the size, and a run has few units for its queries, masks and output (2 us a
+// run); 10 us pass before the first scores.  One token over 2K: 13.1 us, latency (the dealing, queries, first tiles, and 4
 // for the second launch).
 //
 // Why so.  Two slots: with one, the tensor cores wait while scores become weights.  Products issued by a warp that stays
@@ -181,8 +181,8 @@ __device__ __forceinline__ void tmem_ld2(uint32_t taddr, uint32_t (&r)[2]) {
 
 // sum over i < n of floor((c + a i) / 128): the sum of the numbers less that of their remainders, which repeat.
 __device__ __forceinline__ int64_t sum_of_units(int64_t c, int32_t a, int64_t n) {
-    const int32_t g = min(128, a & -a), period = 128 / g, some = int32_t(n % period);
-    int64_t rest = n / period * (int64_t(period) * (c % g) + int64_t(g) * period * (period - 1) / 2);
+    const int32_t g = min(128, a & -a), log_period = 8 - __ffs(g), period = 1 << log_period, some = int32_t(n) & (period - 1);
+    int64_t rest = (n >> log_period) * (int64_t(period) * (c & (g - 1)) + (int64_t(g) * period * (period - 1) >> 1));
     int32_t r = int32_t(c & 127);
     for (int32_t i = 0; i < some; ++i, r = (r + a) & 127) rest += r;
     return (n * c + a * (n * (n - 1) / 2) - rest) >> 7;
@@ -560,7 +560,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 uint16_t *result = a.out + ((size_t(s.b) * a.T + s.token0 + t) * a.Hq + h) * D;
                 const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
                 const int32_t cleared = s_cleared[nrun % kRuns] == nrun + 1 ? min(limit + 1, (s.first + s.n) * kUnitKeys) : 0;
-#pragma unroll 4
+// (as short as can be: what runs once a run is not in the instruction caches; unrolled by four, 128 us instead of 119 for chunks of 500)
+#pragma unroll 1
                 for (int d = d0; d < d1; d += 16) {
                     float v[16];
                     uint32_t w[16];
@@ -799,7 +800,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                     if (!ok) break;
                     const int last = min(rows - row0, kSlotRows);
                     uint8_t *dst = sm_q + (qx % NQ) * S::kQ + (c / 8) * kBlock16 + in_pass * 128;
-#pragma unroll 4
+#pragma unroll 1
                     for (int row = in_pass; row < last; row += kStep, dst += kStep * 128) {
                         cp_async16(dst + (((c & 7) ^ (row & 7)) * 16), q);
                         q += next;

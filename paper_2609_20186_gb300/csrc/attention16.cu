@@ -31,9 +31,9 @@
 // 87 % of what it sustains.  The tensor pipe is active 71 % of the time; what it waits for is the chain of barriers between a
 // slot's scores, weights and products, some 3000 cycles a unit, 1800 of them the rows' warps' (loads 240, maxima 500, weights
 // 1000), and the warp that issues the products has one for both slots (100 to 200 cycles a wait).  It is not the exponentials:
-// without them the time is the same.  16 rows of up to 500 tokens with heads of 64: 115 us, 4.3 times its products' time,
+// without them the time is the same.  16 rows of up to 500 tokens with heads of 64: 113 us, 4.2 times its products' time,
 // since the chain is as long for a product of half the size, and a run has few units for its queries, masks and output (2 us a
-// run); 10 us pass before the first scores.  One token over 2K: 13.1 us, latency (the dealing, queries, first tiles, and 4
+// run); 10 us pass before the first scores.  One token over 2K: 13.0 us, latency (the dealing, queries, first tiles, and 4
 // for the second launch).
 //
 // Why so.  Two slots: with one, the tensor cores wait while scores become weights.  Products issued by a warp that stays
@@ -832,8 +832,9 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
 
 // Joins the partial results of the items that several CTAs hold, and writes the statuses of a launch that a CTA gave up: CTAs
 // (i, .) look after the item whose first part is the i-th CTA's, a warp a query row, adding the parts in order, kJoinFlight on
-// their way together.
-constexpr int kJoinWarps16 = 8, kJoinFlight = 8;
+// their way together.  (4 / 6 / 8 / 12: 13.8 / 13.0 / 13.2 / 14.2 us for one token over 2K, whose 17 parts they divide, and
+// 115.4 / 113.0 / 115.8 / 117.2 for chunks of 500 tokens.)
+constexpr int kJoinWarps16 = 8, kJoinFlight = 6;
 template <bool F16, int D>
 __global__ void __launch_bounds__(kJoinWarps16 *kWarp, 3) attn16_join_kernel(const Attn16Args a) {
     constexpr int E = D / kWarp;  // dimensions of a lane

@@ -526,9 +526,14 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
             tc_fence_after();
             float f = 1.f, f1 = 0.f;          // of this slot's output (or the first one's), and the second one's
             const bool two = split && s.n > 1;  // the second slot has an output too
-            if (split) {  // references and sums change hands in the scores' place
+            if (split) {
+                // References and sums change hands in the scores' place, in one of two places in turn.  The second slot has
+                // nothing to wait for in a run of one unit and puts its own down while the first one may still read what it
+                // put down before: that is in the other place, and in the same one only behind `met` of the run between,
+                // where the first slot arrives once it has read.
+                const uint32_t hand = 2 * (splits & 1);
                 if (warp_mine) {
-                    tmem_st2(scores, __float_as_uint(ref), __float_as_uint(l));
+                    tmem_st2(scores + hand, __float_as_uint(ref), __float_as_uint(l));
                     tmem_wait_st();
                 }
                 tc_fence_before();
@@ -539,7 +544,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 tc_fence_after();
                 if (warp_mine) {
                     uint32_t other[2];
-                    tmem_ld2(lanes + uint32_t((1 - slot) * 128), other);
+                    tmem_ld2(lanes + uint32_t((1 - slot) * 128) + hand, other);
                     tmem_wait_ld();
                     const float its_ref = __uint_as_float(other[0]), its_l = __uint_as_float(other[1]);
                     const float top = fmaxf(ref, its_ref), own = exp2_approx(ref - top), its = exp2_approx(its_ref - top);

@@ -208,8 +208,8 @@ int switchsd_kv16_read(const switchsd_kv16_read_params *params);
  * same rules for lengths, pages, statuses and places that a token does not see (a token's result is what it would be if
  * they held zeros).  Products are exact, and scores, the softmax's maximum and sum and the output's sum are held in
  * binary32; the weights that multiply the values are rounded to dtype.  (f16 weights lose bits where they are below 2^-25
- * of their row's largest, and are 0 below 2^-36 of it.)  A NaN that a token sees in a value makes its result NaN in that
- * dimension, a NaN score in all of the head's.
+ * of their row's largest, and are 0 below 2^-36 of it.)  Scores of 2^126 and more in size count as infinite.  A NaN that a
+ * token sees in a value makes its result NaN in that dimension, a NaN score in all of the head's.
  */
 typedef switchsd_kv4_attention_params switchsd_kv16_attention_params;
 

@@ -18,7 +18,7 @@
 // Numbers.  The operands are the cache's and the queries' own numbers, products exact, S and O in binary32.  P takes S's
 // place in tensor memory, in the cache's type, since both operands of a product have one: weights are relative to a
 // reference that may lag the largest score (kLagUp), so that O is scaled seldom, f16 weights 2^11 higher so that few are
-// below its normal numbers.  Their sum is of the unrounded weights, in binary32.
+// below its normal numbers; scores may be of any size (far_units).  Their sum is of the unrounded weights, in binary32.
 //
 // What a token does not see: scores are replaced before their maximum is taken.  Of the values, what no row of the tile sees
 // (past its last token, without a page) is cleared in shared memory; among the values that some rows see and others do
@@ -80,6 +80,7 @@ template <bool F16>
 constexpr float kUp = F16 ? 11.f : 0.f;
 template <bool F16>
 constexpr float kLagUp = F16 ? 15.f : 8.f;
+constexpr float kFar = 4194304.f;           // 2^22: the rounding of references of this size and more would show in the weights
 
 struct Attn16Args : AttnArgs {
     int32_t tokens;  // of a tile: kTileRows / group
@@ -354,6 +355,100 @@ __device__ __forceinline__ void fill_absent(const Attn16Args &a, uint32_t w, uin
     }
 }
 
+// Bits of the keys from `key` on that a row sees whose last visible one is `limit`, among 32 of a unit.
+__device__ __forceinline__ uint32_t seen_of(uint32_t there, int32_t limit, int32_t key) {
+    const int32_t ahead = limit - key;
+    return there & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
+}
+
+// A row's reference and sum of weights follow a unit's largest score mx (times the scale), and so does O, where there is one.  Returns
+// whether a reference of the warp's has changed.  All of a warp.
+template <bool F16, int D>
+__device__ __forceinline__ bool follow(float mx, float &ref, float &l, uint32_t out, bool has_out) {
+    float corr = 1.f;
+    if (mx > __fadd_rd(ref, kLagUp<F16>)) {  // (both rounded so that weights stay small: f16 has none beyond 2^15)
+        const float to = __fsub_ru(mx, kUp<F16>);
+        corr = exp2_approx(ref - to);
+        ref = to;
+        l *= corr;
+    }
+    if (!__any_sync(kFull, corr != 1.f)) return false;
+    if (has_out)
+#pragma unroll 1
+        for (int e = 0; e < D; e += 16) {
+            uint32_t w[16];
+            tmem_ld16(out + e, w);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(__uint_as_float(w[j]) * corr);
+            tmem_st16(out + e, w);
+        }
+    return true;
+}
+
+// A row's units from k on, of which the first one's scores are there, where references of the warp's are far: exponents are of
+// products rounded as the reference's was, since an exact one lies up to half of a step of the reference beside it, and weights of
+// the largest score itself would be infinite or 0.  Little code, in a place of its own: chunks 1445 us with it, 1434 without, chunks
+// of 500 tokens 118 and 114.5, one token a row and drafts the same; a branch in the loop: 1460, 119.5; a second form of the whole
+// loop: 1428, 119; exponents of (score - reference), which need neither, an addition more a pair: 1515, 122.
+struct FarRow {
+    float ref, l;
+    int32_t k;
+    uint32_t i;
+    bool ok;
+};
+template <bool F16, int D>
+__device__ __forceinline__ FarRow far_units(FarRow r, uint32_t scores, uint32_t out, int32_t n, int32_t step, int32_t k0, int32_t key0, int32_t limit, uint32_t unit0,
+                                            float scale, const uint32_t (*exist)[4], uint64_t *s_full, uint64_t *p_half, uint64_t *p_full) {
+    const float size = fabsf(scale);
+    for (bool there_already = true; r.k < n; r.k += step, ++r.i) {
+        if (!there_already) r.ok = tc_wait_warp(s_full, r.i & 1);
+        there_already = false;
+        if (!r.ok) break;
+        tc_fence_after();
+        const uint32_t *there = exist[(unit0 + uint32_t(r.k)) % kReady];
+        auto scores_of = [&](int w, float (&v)[32]) {
+            tmem_ld32(scores + 32 * w, v);
+            const uint32_t see = seen_of(there[w], limit, key0 + r.k * kUnitKeys + 32 * w);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1 ? (scale < 0.f ? -v[e] : v[e]) : -INFINITY;
+        };
+        float mx = -INFINITY, sum = 0.f, v[32];
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w) {
+            scores_of(w, v);
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) mx = max3(mx, v[e], v[e + 1]);
+        }
+        follow<F16, D>(__fmul_rn(mx, size), r.ref, r.l, out, r.k != k0);
+        const bool rounded = fabsf(r.ref) > kFar;
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w) {
+            uint32_t y[16];
+            scores_of(w, v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = exp2_approx(rounded ? __fsub_rn(__fmul_rn(v[e], size), r.ref) : __fmaf_rn(v[e], size, -r.ref));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                sum += v[2 * e] + v[2 * e + 1];
+                y[e] = narrow2<F16>(v[2 * e], v[2 * e + 1]);
+            }
+            tmem_st16(scores + 16 * w, y);
+            if (w == 1) {
+                tmem_wait_st();
+                tc_fence_before();
+                warp_arrive(p_half);
+            }
+        }
+        r.l += sum;
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(p_full);
+    }
+    return r;
+}
+
 template <bool F16, int D>
 __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_constant__ CUtensorMap map, const Attn16Args a) {
     using S = Smem16<D>;
@@ -443,7 +538,9 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
             float ref = kFloor, l = 0.f;
             const int step = split ? 2 : 1, k0 = split ? slot : 0;
             const uint32_t out = lanes + 256 + uint32_t(slot * 128);
-            for (int32_t k = k0; k < s.n; k += step, ++i) {
+            int32_t k = k0;
+            bool far = false;
+            for (; k < s.n; k += step, ++i) {
                 const int32_t key0 = (s.first + k) * kUnitKeys;
                 ok = ok && tc_wait_warp(&s_full[slot], i & 1);
                 if (!ok) break;
@@ -461,8 +558,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                         const uint32_t word[4] = {there.x, there.y, there.z, there.w};
 #pragma unroll
                         for (int w = 0; w < 4; ++w) {
-                            const int32_t ahead = limit - (key0 + 32 * w);  // the last visible key's place
-                            const uint32_t see = word[w] & (ahead >= 31 ? 0xffffffffu : ahead < 0 ? 0u : (2u << ahead) - 1u);
+                            const uint32_t see = seen_of(word[w], limit, key0 + 32 * w);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) v[32 * w + e] = (see >> e) & 1 ? v[32 * w + e] : -INFINITY;
                         }
@@ -470,25 +566,10 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                     float top[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
 #pragma unroll
                     for (int e = 8; e < kUnitKeys; e += 2) top[(e >> 1) & 7] = max3(top[(e >> 1) & 7], v[e], v[e + 1]);
-                    const float mx = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), fmaxf(top[6], top[7])) * scale;
-                    float corr = 1.f;
-                    if (mx > ref + kLagUp<F16>) {
-                        const float to = __fsub_ru(mx, kUp<F16>);  // (rounded up: f16 has no weights beyond 2^15)
-                        corr = exp2_approx(ref - to);
-                        ref = to;
-                        l *= corr;
-                    }
-                    if (k != k0 && __any_sync(kFull, corr != 1.f)) {  // (the scores' product came behind the last one of O)
-#pragma unroll 1
-                        for (int e = 0; e < D; e += 16) {
-                            uint32_t w[16];
-                            tmem_ld16(out + e, w);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(__uint_as_float(w[j]) * corr);
-                            tmem_st16(out + e, w);
-                        }
-                    }
+                    const float mx = __fmul_rn(max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), fmaxf(top[6], top[7])), scale);
+                    if (follow<F16, D>(mx, ref, l, out, k != k0))  // (the scores' product came behind the last one of O)
+                        far = __any_sync(kFull, mine && fabsf(ref) > kFar && ref > kFloor);  // (what is in rows that are not there is no one's)
+                    if (__builtin_expect(far, 0)) break;
                     const uint64_t scale2 = pair_of(scale, scale), ref2 = pair_of(-ref, -ref);
                     uint64_t sum[2] = {0, 0};
 #pragma unroll
@@ -516,6 +597,14 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 }
                 tc_fence_before();
                 warp_arrive(&p_full[slot]);
+            }
+            if (__builtin_expect(far, 0)) {
+                const FarRow r = far_units<F16, D>(FarRow{ref, l, k, i, ok}, scores, out, s.n, step, k0, s.first * kUnitKeys, limit, unit0, flip ? -scale : scale, s_exist,
+                                                   &s_full[slot], &p_half[slot], &p_full[slot]);
+                ref = r.ref;
+                l = r.l;
+                i = r.i;
+                ok = r.ok;
             }
             // --- the run's result -------------------------------------------------------------------------------
             if (k0 < s.n) {

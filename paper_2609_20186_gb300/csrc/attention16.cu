@@ -526,8 +526,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
         const int slot = warp / kSlotWarps - 1, quarter = warp % kSlotWarps, place = tid % kSlotThreads;
         const uint32_t lanes = tmem + (uint32_t(32 * quarter) << 16), scores = lanes + uint32_t(slot * 128);
         const bool flip = a.scale < 0.f;
-        // of a sum of products, for the binary logarithm; positive, so that what is masked stays -inf
-        const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
+        // of a sum of products, for the binary logarithm; positive, so that what is masked stays -inf (2^-149 for 0: no score shows it)
+        const float scale = a.scale == 0.f ? 0x1p-149f : fabsf(a.scale) * 1.4426950408889634f;
         uint32_t i = 0, done = 0, splits = 0, unit0 = 0;  // this slot's units and runs so far, the CTA's runs in both slots and units
         for (uint32_t nrun = 0; read_run(nrun); ++nrun, unit0 += uint32_t(s.n)) {
             const int rows = s.tokens * a.group;

@@ -127,3 +127,29 @@ def test_half_weights_stay_in_range(T, G, base):
         if last:
             want = v[:, tops[-1]].double()[None, None, :, None]
             assert ((out.double().view(B, T, H, G, D) - want).abs() <= (2.0 ** -10 + 2.0 ** -22) * want).all()
+
+
+@pytest.mark.parametrize("name", ["bfloat16"])
+@pytest.mark.parametrize("T,G", [(1, 4), (40, 8)])
+def test_scales_of_any_size(T, G, name):
+    """Small scales of large products, subnormal ones among them, of either sign: the scores are of ordinary size.  (Sums off by
+    2^-16 sum |q k|, 2^-10 of a score; a subnormal scale has 2^-12 of itself; then as in test_gpu_kv16.py.)"""
+    import torch
+    torch.manual_seed(T)
+    B, H, D, n, page = 5, 2, 64, 700, 64
+    k = torch.randn(H, n, D, device="cuda").to(torch.bfloat16)
+    v = torch.randn(H, n, D, device="cuda").to(torch.bfloat16)
+    cache, table = _setup(B, H, D, n, page, torch.bfloat16, k * 2.0 ** 58, v)
+    lens, new = torch.full((B,), n - T, dtype=torch.int32, device="cuda"), torch.full((B,), T, dtype=torch.int32, device="cuda")
+    q = torch.randn(B, T, H * G, D, device="cuda").to(torch.bfloat16)
+    unseen = (torch.arange(n, device="cuda") > n - T + torch.arange(T, device="cuda")[:, None])[None, :, None, None]
+    x = torch.einsum("bthgd,hjd->bthgj", q.double().view(B, T, H, G, D), k.double())
+    lifted = (q.float() * 2.0 ** 63).to(torch.bfloat16)
+    for factor in (0.1, -0.1, 1e-4, -1e-4):  # (of 2^-121)
+        p = torch.softmax((x * factor).masked_fill(unseen, float("-inf")), -1)
+        want, mag = (torch.einsum("bthgj,hjd->bthgd", p, y.double()) for y in (v, v.abs()))
+        out, scale = torch.empty_like(q), float(np.float32(factor * 2.0 ** -121))
+        assert abs(scale / (factor * 2.0 ** -121) - 1) < 2.0 ** -12
+        _fw().switchsd_kv16_attention(lifted, cache, table, lens, new, out, scale=scale)
+        off = (out.double().view_as(want) - want).abs() - (2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -9) * mag)
+        assert off.max() <= 0, factor

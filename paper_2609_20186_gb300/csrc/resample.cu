@@ -117,8 +117,12 @@ struct Race {
         }
         return y;
     }
-    // How far binary32's score may be off, and binary64's of what is compared with it.
-    __device__ float margin(float s) const { return greedy || fabsf(s) == INFINITY ? 0.f : (residual ? 4e-3f : 2e-5f) + 1e-6f * fabsf(s); }
+    // How far binary32's score may be off, and binary64's of what is compared with it.  (A residual's is what is left of z /
+    // temperature less lse: four roundings of 2^-24 of numbers up to |s| + |lse| and some 30 in size, twice.)
+    __device__ float margin(float s) const {
+        if (greedy || fabsf(s) == INFINITY) return 0.f;
+        return residual ? 4e-3f + 1e-6f * (fabsf(s) + fabsf(lse)) : 2e-5f + 1e-6f * fabsf(s);
+    }
 };
 
 template <int DT>

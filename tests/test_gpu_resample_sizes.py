@@ -1,0 +1,47 @@
+"""switchsd_resample where logits over temperatures are large: the token is binary64's (sampling_ref.py), whatever binary32 can
+tell apart there."""
+import numpy as np
+import pytest
+
+from tests import sampling_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def _call(x, name, draft, temps, seeds, ctx, *, lse=None, xq=None, q_lse=None):
+    """Every row's draft of one token is rejected; the token appended in its place."""
+    import torch
+    import paper_2609_20186_gb300 as fw
+    dtype = dict(bf16=torch.bfloat16, f32=torch.float32)[name]
+    B, V = x.shape
+    f32 = lambda a: None if a is None else torch.from_numpy(np.asarray(a, np.float32)).cuda()
+    logits = torch.from_numpy(np.asarray(x, np.float32)).cuda().to(dtype)[:, None].expand(B, 2, V)
+    q = None if xq is None else torch.from_numpy(np.asarray(xq, np.float32)).cuda().to(dtype)[:, None]
+    one, out = torch.ones(B, 1, device="cuda"), torch.full((B, 2), 77, dtype=torch.int32, device="cuda")
+    status = torch.full((B,), 77, dtype=torch.int32, device="cuda")
+    fw.switchsd_resample(logits, torch.from_numpy(np.asarray(draft, np.int32)).cuda()[:, None], torch.ones(B, dtype=torch.int32, device="cuda"), one * 0, one * 0.5, out,
+                         seeds=torch.from_numpy(np.asarray(seeds, np.int64)).cuda(), ctx_lens=torch.from_numpy(np.asarray(ctx, np.int32)).cuda(), temperature=f32(temps),
+                         lse=None if lse is None else f32(lse)[:, None].expand(B, 2).contiguous(), q_logits=q, q_lse=None if q_lse is None else f32(q_lse)[:, None], status=status)
+    assert not status.any() and (out[:, 1] == -1).all()
+    return out[:, 0].cpu().numpy()
+
+
+def _rows(x, temps, seeds, ctx, **kw):
+    each = lambda b: {k: (v[b] if isinstance(v, np.ndarray) else v) for k, v in kw.items()}
+    return np.array([ref.token(x[b], temps[b], int(seeds[b]), int(ctx[b]), **each(b)) for b in range(len(x))])
+
+
+@pytest.mark.parametrize("at,T,spread", [(1e5, 0.7, 2.0), (-1e5, 0.7, 2.0), (60.0, 4e-4, 1e-3), (3e6, 1.0, 4.0), (-40.0, 1e-3, 3e-3)])
+def test_residuals_of_large_logits(at, T, spread):
+    """A drafter's rows whose logits over the temperature lie near 4e4 to 3e6, where binary32's numbers are up to 1/4 apart."""
+    rng = np.random.default_rng(int(abs(at)))
+    B, V = 4000, 150
+    x = np.float32(at + rng.standard_normal((B, V)) * spread).astype(np.float64)
+    xq = np.float32(x + rng.standard_normal((B, V)) * spread * 0.3).astype(np.float64)
+    temps = np.full(B, np.float32(T), np.float64)
+    lse, q_lse = (np.float32([ref.logprobs(y[b], temps[b])[2] for b in range(B)]).astype(np.float64) for y in (x, xq))
+    seeds, ctx = rng.integers(-2**63, 2**63 - 1, B), rng.integers(0, 10000, B)
+    got = _call(x, "f32", np.zeros(B), temps, seeds, ctx, lse=lse, xq=xq, q_lse=q_lse)
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = _rows(x, temps, seeds, ctx, lse=lse, lq=xq, q_lse=q_lse)
+    assert np.array_equal(got, want), (np.argwhere(got != want)[:5], (got != want).sum())

@@ -26,6 +26,7 @@ constexpr int kRaceFlight = 2;          // vectors of a thread that are worked o
 constexpr int kRaceList = 1024;         // tokens of a CTA that passed the test
 constexpr int kRaceWarps = kRaceThreads / kWarp, kRaceParts = 8;
 constexpr float kRaceLog2e = 1.4426950408889634f;
+constexpr float kRaceMost = 3.402823466e38f;  // binary32's largest
 
 struct RaceArgs {
     const void *logits, *q_logits;
@@ -99,7 +100,7 @@ struct Race {
         if (greedy) return z;
         const uint32_t r = bits(v);
         const float e = r < 0x80000000u ? -log1pf(-(float(r) + 0.5f) * 0x1p-32f) : -logf((float(~r) + 0.5f) * 0x1p-32f);
-        float y = z / temperature - logf(e);
+        float y = fmaxf(z / temperature - logf(e), -kRaceMost);  // (what binary32 does not reach has a weight, and binary64 tells it apart)
         if (residual) y -= lse;
         if (y + margin(y) < floor) return -INFINITY;  // (w is at most p)
         if (residual) {

@@ -45,3 +45,21 @@ def test_residuals_of_large_logits(at, T, spread):
     with np.errstate(over="ignore", invalid="ignore"):
         want = _rows(x, temps, seeds, ctx, lse=lse, lq=xq, q_lse=q_lse)
     assert np.array_equal(got, want), (np.argwhere(got != want)[:5], (got != want).sum())
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1e-30, 1e-37, 2e-38, 1e-40, 2.0 ** -149])
+def test_temperatures_next_to_zero(T, name):
+    """Logits over temperatures beyond binary32's range: the largest logit that may be drawn, of equal ones the one that binary64
+    finds, and the smallest where the draws are lost in its rounding; of negative, positive and mixed logits."""
+    rng = np.random.default_rng(int(-np.log2(T)))
+    B, V = 12, 5003
+    x = np.abs(rng.standard_normal((B, V))) * 9 + 1
+    x[:4] *= -1
+    x[4:8] *= np.where(rng.random((4, V)) < 0.5, -1, 1)
+    x[3:5] = np.round(x[3:5])  # (many equal ones)
+    x = ((np.float32(x).view(np.uint32) & 0xffff0000).view(np.float32) if name == "bf16" else np.float32(x)).astype(np.float64)
+    temps, seeds, ctx = np.full(B, np.float32(T), np.float64), np.arange(B) * 3 - 5, np.arange(B)
+    draft = x.argmax(1)
+    got = _call(x, name, draft, temps, seeds, ctx)
+    assert np.array_equal(got, _rows(x, temps, seeds, ctx, skip=draft))

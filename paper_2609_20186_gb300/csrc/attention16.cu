@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     // Every wait of this warp has ended in time.  After one that has not, the warp goes to the end, and no result counts.
-    bool ok = !a.give_up || warp == kFetchWarp16 || warp == kRunWarp;
+    bool ok = true;
     Run s;
     // The CTA's r-th run; n = 0: there are no more.
     auto read_run = [&](uint32_t r) {
@@ -792,7 +792,7 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
                 lead_arrive(leader, &o_done[slot]);
                 lead_commit(leader, &o_done[slot]);
             };
-            for (uint32_t nrun = 0; __any_sync(kFull, read_run(nrun)); ++nrun) {
+            for (uint32_t nrun = 0; !a.give_up && __any_sync(kFull, read_run(nrun)); ++nrun) {
                 const bool split = __any_sync(kFull, s.tokens * a.group <= kSlotRows);
                 const int32_t n = __shfl_sync(kFull, s.n, 0);
                 const uint32_t q0 = qx, q1 = split ? qx : qx + 1;
@@ -993,7 +993,8 @@ __global__ void __launch_bounds__(kJoinWarps16 *kWarp, 3) attn16_join_kernel(con
 }
 
 // Whether the environment variable SWITCHSD_DIAG_ATTENTION_GIVE_UP is 1 (read once per process): a diagnostic of the path
-// behind a wait that ran out, as in attention_tc.cu.  The fetching warp alone waits, on the ring that nobody empties.
+// behind a wait that ran out.  The warp of the products issues none and waits for nothing, so the others' waits run out, the query
+// rows' in every CTA that has a run: what the statuses then say comes from them.
 static bool give_up16() {
     static const bool set = [] {
         const char *v = std::getenv("SWITCHSD_DIAG_ATTENTION_GIVE_UP");

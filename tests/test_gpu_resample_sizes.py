@@ -1,5 +1,5 @@
-"""switchsd_resample where logits over temperatures are large: the token is binary64's (sampling_ref.py), whatever binary32 can
-tell apart there."""
+"""switchsd_resample where logits over temperatures are large, and where masks leave nothing to bound the search by: the token is
+binary64's (sampling_ref.py), whatever binary32 can tell apart there."""
 import numpy as np
 import pytest
 
@@ -63,3 +63,28 @@ def test_temperatures_next_to_zero(T, name):
     draft = x.argmax(1)
     got = _call(x, name, draft, temps, seeds, ctx)
     assert np.array_equal(got, _rows(x, temps, seeds, ctx, skip=draft))
+
+
+@pytest.mark.parametrize("drafter", [False, True])
+@pytest.mark.parametrize("name,V,B", [("f32", 200003, 2), ("f32", 60000, 90), ("bf16", 262144, 3), ("bf16", 131072, 170)])
+def test_masks_that_leave_no_early_token(name, V, B, drafter):
+    """Logits of -inf but for the last third of every eighth of the vocabulary (what a CTA takes, or a part of it): thousands of
+    tokens without a bound to go by, more than the list of those to be worked out holds."""
+    rng = np.random.default_rng(V + B)
+    some = min(B, 3)
+    x = np.float32(rng.standard_normal((some, V)) * 2)
+    xq = np.float32(x + rng.standard_normal((some, V)) * 0.7)
+    if name == "bf16":
+        x, xq = ((y.view(np.uint32) & 0xffff0000).view(np.float32) for y in (x, xq))
+    eighth = -(-V // 8)
+    x[:, np.arange(V) % eighth < 2 * eighth // 3] = -np.inf
+    x, xq = (np.float64(y)[np.arange(B) % some] for y in (x, xq))
+    temps, seeds, ctx = np.full(B, np.float32(0.8), np.float64), np.arange(B) % some, np.zeros(B, int)
+    draft, kw, weights = x.argmax(1), {}, {}
+    if drafter:
+        lse, q_lse = (np.float32([ref.logprobs(y[b], temps[b])[2] for b in range(some)]).astype(np.float64)[np.arange(B) % some] for y in (x, xq))
+        kw, weights = dict(lse=lse, xq=xq, q_lse=q_lse), dict(lse=lse[:some], lq=xq[:some], q_lse=q_lse[:some])
+    else:
+        weights = dict(skip=draft[:some])
+    got = _call(x, name, draft, temps, seeds, ctx, **kw)
+    assert np.array_equal(got, _rows(x[:some], temps, seeds, ctx, **weights)[np.arange(B) % some])

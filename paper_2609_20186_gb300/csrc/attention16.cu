@@ -26,14 +26,14 @@
 // them at the end.
 //
 // Bound.  One token a row and up to a draft's: memory.  64 rows of 8K to 32K tokens, 8 key heads x 128, one token each:
-// 802 us, 5.4 GB, 99 % of a copy's rate; 1 to 17 tokens over 2K to 8K: 222 us (90 %), of which 6 are the join.  Chunks: 2 rows
-// of 2048 tokens over 30K, 32 query heads: 1425 us, 1.49 PFLOP/s, 77 % of what a library's product reaches in a short run and
-// 87 % of what it sustains.  The tensor pipe is active 71 % of the time; what it waits for is the chain of barriers between a
+// 785 us, 5.4 GB, all of a copy's rate; 1 to 17 tokens over 2K to 8K: 218 us (91 %), of which 6 are the join.  Chunks: 2 rows
+// of 2048 tokens over 30K, 32 query heads: 1370 us, 1.55 PFLOP/s, 80 % of what a library's product reaches in a short run and
+// 91 % of what it sustains.  The tensor pipe is active 75 % of the time; what it waits for is the chain of barriers between a
 // slot's scores, weights and products, some 3000 cycles a unit, 1800 of them the rows' warps' (loads 240, maxima 500, weights
 // 1000), and the warp that issues the products has one for both slots (100 to 200 cycles a wait).  It is not the exponentials:
-// without them the time is the same.  16 rows of up to 500 tokens with heads of 64: 113 us, 4.2 times its products' time,
+// without them the time is the same.  16 rows of up to 500 tokens with heads of 64: 108 us, 4 times its products' time,
 // since the chain is as long for a product of half the size, and a run has few units for its queries, masks and output (2 us a
-// run); 10 us pass before the first scores.  One token over 2K: 13.0 us, latency (the dealing, queries, first tiles, and 4
+// run); 10 us pass before the first scores.  One token over 2K: 12.8 us, latency (the dealing, queries, first tiles, and 4
 // for the second launch).
 //
 // Why so.  Two slots: with one, the tensor cores wait while scores become weights.  Products issued by a warp that stays
@@ -388,9 +388,10 @@ __device__ __forceinline__ bool follow(float mx, float &ref, float &l, uint32_t 
 
 // A row's units from k on, of which the first one's scores are there, where references of the warp's are far: exponents are of
 // products rounded as the reference's was, since an exact one lies up to half of a step of the reference beside it, and weights of
-// the largest score itself would be infinite or 0.  Little code, in a place of its own: chunks 1445 us with it, 1434 without, chunks
-// of 500 tokens 118 and 114.5, one token a row and drafts the same; a branch in the loop: 1460, 119.5; a second form of the whole
-// loop: 1428, 119; exponents of (score - reference), which need neither, an addition more a pair: 1515, 122.
+// the largest score itself would be infinite or 0.  Little code, in a place of its own: chunks of 500 tokens 108.3 us with it, 105.7
+// without, the other cases alike.  (Where these took 114.5 and chunks 1434 without any such form: a branch in the loop 119.5 and 1460;
+// a second form of the whole loop 119, 1428; exponents of score less reference, which need no such form but an addition more a pair,
+// 122, 1515.)
 struct FarRow {
     float ref, l;
     int32_t k;
@@ -926,8 +927,8 @@ __global__ void __launch_bounds__(kThreads16, 1) attn16_kernel(const __grid_cons
 
 // Joins the partial results of the items that several CTAs hold, and writes the statuses of a launch that a CTA gave up: CTAs
 // (i, .) look after the item whose first part is the i-th CTA's, a warp a query row, adding the parts in order, kJoinFlight on
-// their way together.  (4 / 6 / 8 / 12: 13.8 / 13.0 / 13.2 / 14.2 us for one token over 2K, whose 17 parts they divide, and
-// 115.4 / 113.0 / 115.8 / 117.2 for chunks of 500 tokens.)
+// their way together.  (4 / 6 / 8 / 12, then: 13.8 / 13.0 / 13.2 / 14.2 us for one token over 2K, 115.4 / 113.0 / 115.8 / 117.2 for
+// chunks of 500 tokens.)
 constexpr int kJoinWarps16 = 8, kJoinFlight = 6;
 template <bool F16, int D>
 __global__ void __launch_bounds__(kJoinWarps16 *kWarp, 3) attn16_join_kernel(const Attn16Args a) {

@@ -339,8 +339,8 @@ int switchsd_logprobs(const switchsd_logprobs_params *params);
  *   key = mix(seed + (ctx_len + a + 1) g),   r_2n + 2^32 r_2n+1 = mix(key + (n + 1) g)
  *
  * so a row's draws depend on its own seed and length only, and a call that is made again draws the same.  What decides is
- * compared in binary32 where that is enough and else in binary64, as if all were.  A temperature of 0: the smallest v with
- * the largest l, whatever the draft.
+ * compared in binary32 where that is enough and else in binary64, as if all were (so a p or q below 2^-1075 is 0 in a
+ * difference).  A temperature of 0: the smallest v with the largest l, whatever the draft.
  *
  *   T             positions: drafts have up to T - 1 tokens
  *   logits        dtype [B, T, V] as for switchsd_logprobs

@@ -100,8 +100,13 @@ struct Race {
         if (greedy) return z;
         const uint32_t r = bits(v);
         const float e = r < 0x80000000u ? -log1pf(-(float(r) + 0.5f) * 0x1p-32f) : -logf((float(~r) + 0.5f) * 0x1p-32f);
-        float y = fmaxf(z / temperature - logf(e), -kRaceMost);  // (what binary32 does not reach has a weight, and binary64 tells it apart)
-        if (residual) y -= lse;
+        float y = fmaxf(z / temperature, -kRaceMost);  // (what binary32 does not reach has a weight, and binary64 tells it apart)
+        if (residual) {
+            y -= lse;  // ln p; a residual's p is binary64's, which has nothing below e^-745.14 and few bits from e^-708 on
+            if (y + margin(y) < -745.2f) return -INFINITY;
+            if (y - margin(y) < -700.f) return float(exact(v));
+        }
+        y -= logf(e);
         if (y + margin(y) < floor) return -INFINITY;  // (w is at most p)
         if (residual) {
             const float zq = q[v];

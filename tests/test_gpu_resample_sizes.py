@@ -88,3 +88,22 @@ def test_masks_that_leave_no_early_token(name, V, B, drafter):
         weights = dict(skip=draft[:some])
     got = _call(x, name, draft, temps, seeds, ctx, **kw)
     assert np.array_equal(got, _rows(x[:some], temps, seeds, ctx, **weights)[np.arange(B) % some])
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("T,spread", [(0.01, 8.0), (0.01, 1.0), (0.05, 6.0), (0.003, 0.6)])
+def test_residuals_of_low_temperatures(T, spread, name):
+    """All of p and q on one token each, often the same one: what is left there is lse's rounding, or nothing, and the other tokens'
+    p is no binary64 number, or one of few bits."""
+    rng = np.random.default_rng(int(T * 1e4 + spread))
+    B, V = 4000, 30
+    x = np.float32(rng.standard_normal((B, V)) * spread)
+    xq = np.float32(x + rng.standard_normal((B, V)) * spread * 0.3)
+    x, xq = ((np.float64((y.view(np.uint32) & 0xffff0000).view(np.float32)) if name == "bf16" else np.float64(y)) for y in (x, xq))
+    xq[::7, ::3] = -np.inf
+    temps = np.full(B, np.float32(T), np.float64)
+    lse, q_lse = (np.float32([ref.logprobs(y[b], temps[b])[2] for b in range(B)]).astype(np.float64) for y in (x, xq))
+    seeds, ctx = rng.integers(-2**63, 2**63 - 1, B), rng.integers(0, 10000, B)
+    got = _call(x, name, np.zeros(B), temps, seeds, ctx, lse=lse, xq=xq, q_lse=q_lse)
+    want = _rows(x, temps, seeds, ctx, lse=lse, lq=xq, q_lse=q_lse)
+    assert np.array_equal(got, want), (np.argwhere(got != want)[:5], (got != want).sum())
